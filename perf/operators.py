@@ -338,7 +338,7 @@ def _softmax_product(z, seen, v):
     m = z.amax(-1, keepdim=True)
     p = torch.exp(z - torch.where(m == -math.inf, 0.0, m))
     total = p.sum(-1, keepdim=True)
-    return torch.where(total > 0, torch.matmul(p, v) / total, 0.0)
+    return torch.where(total == 0, 0.0, torch.matmul(p, v) / total)
 
 
 def _tree_plain(st):
