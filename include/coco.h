@@ -282,6 +282,145 @@ int coco_layer_set_timing(coco_layer_t h, int32_t on);
  * launches were made than the pool holds (4096 per read). */
 int coco_layer_read_timing(coco_layer_t h, double* ms, int64_t* launches, int32_t n_kinds);
 
+/* ---------------------------------------------------------------------------
+ * Pages of the cache. Block tables and reference counts are the caller's
+ * device arrays, updated in place by the kernels in stream order, so that a
+ * serving loop needs no copy to the host to know which blocks are free, and
+ * the calls can be captured in a HIP graph:
+ *   block_table[n_seqs][max_blocks_per_seq]  physical block ids, -1: none
+ *   ref_counts[num_blocks]                   rows that hold the block, 0: free
+ * (num_blocks: the smallest of the handle's layers). A block id means that
+ * block in every layer. Requests take the free blocks of lowest id in the
+ * order of the call; they are served in order until one does not fit, and from
+ * there on only those that need no block are: status[i] = 1 where request i
+ * is served, else 0 (its rows and the counts are as if it had not been made;
+ * fork: the child's row is empty). A call holds at most 65535 requests
+ * (alloc, fork: at most max_seqs). Rows or lengths out of range are not served
+ * (status 0) or skipped; validation mode reports them.
+ * ------------------------------------------------------------------------- */
+
+/* Blocks for every empty (-1) entry of row seq_idx[i] below ceil(lens[i] / 16);
+ * entries that hold a block keep it. Rows must be distinct. */
+int coco_kv_alloc(coco_layer_t h, const int32_t* seq_idx, const int32_t* lens, int32_t n,
+                  int32_t* block_table, int32_t n_seqs, int32_t* ref_counts, int32_t* status,
+                  coco_stream_t stream);
+
+/* Row dst_seq[i] becomes a fork of the first lens[i] tokens of row src_seq[i]:
+ * it shares the parent's full blocks (counts + 1) and, where lens[i] is no
+ * multiple of 16, gets a block of its own with a copy of the parent's next
+ * block, keys and values of layers first_layer .. + n_layers - 1. dst_seq
+ * rows must be distinct, empty, and no parent of the call; several children
+ * may have one parent. (Layers of another handle over the same table: pass
+ * the table entries lens[i] / 16 of both rows to its coco_kv_copy.) */
+int coco_kv_fork(coco_layer_t h, int32_t first_layer, int32_t n_layers, const int32_t* src_seq,
+                 const int32_t* dst_seq, const int32_t* lens, int32_t n, int32_t* block_table,
+                 int32_t n_seqs, int32_t* ref_counts, int32_t* status, coco_stream_t stream);
+
+/* Row seq_idx[i] lets go of its blocks from entry ceil(keep_lens[i] / 16) on
+ * (keep_lens NULL: of all): counts - 1, entries -1. A row named twice lets go
+ * of a block once. */
+int coco_kv_free(coco_layer_t h, const int32_t* seq_idx, const int32_t* keep_lens, int32_t n,
+                 int32_t* block_table, int32_t n_seqs, int32_t* ref_counts,
+                 coco_stream_t stream);
+
+/* Copy block src_blocks[i] to dst_blocks[i], keys and values of layers
+ * first_layer .. + n_layers - 1. dst_blocks must be distinct and none of them
+ * a source of another pair; pairs with an id outside the pools are skipped. */
+int coco_kv_copy(coco_layer_t h, int32_t first_layer, int32_t n_layers, const int32_t* src_blocks,
+                 const int32_t* dst_blocks, int32_t n, coco_stream_t stream);
+
+/* Move the tokens of row seq_idx[i] at positions kept[kept_starts[i]],
+ * kept[kept_starts[i] + 1], .. (ascending) to positions base_lens[i],
+ * base_lens[i] + 1, .. of the row, in layers first_layer .. + n_layers - 1: the
+ * accepted path of a tree of drafted tokens moves up to its prefix, or a
+ * context loses evicted tokens. A bit copy (keys keep the rotation of the
+ * position they were computed at), as if every token were read before any is
+ * written. kept[kept_starts[i] + k] >= base_lens[i] + k; rows distinct; the
+ * blocks from base_lens[i] on must be the row's own (count 1). kept_starts
+ * [n + 1] runs from 0 to n_kept. */
+int coco_kv_compact(coco_layer_t h, int32_t first_layer, int32_t n_layers, const int32_t* seq_idx,
+                    const int32_t* base_lens, const int32_t* kept, const int32_t* kept_starts,
+                    int32_t n, int32_t n_kept, const int32_t* block_table, int32_t n_seqs,
+                    coco_stream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * Attention for trees of drafted tokens.
+ * ------------------------------------------------------------------------- */
+
+/* Make room for tree calls of up to max_rows rows and max_seqs sequences
+ * (allocates; not under graph capture). May be called again to make more;
+ * what it outgrows is kept until coco_layer_destroy, so that graphs captured
+ * before stay valid. */
+int coco_tree_reserve(coco_layer_t h, int32_t max_rows, int32_t max_seqs);
+
+/* Attention of drafted tokens over layer `layer`'s cache. The call rows
+ * seq_starts[s] .. seq_starts[s+1]-1 are the nodes of sequence s's tree, whose
+ * keys and values are in the cache already (coco_kv_append) in its last slots:
+ * node j of its N nodes at position ctx_lens[s] - N + j (ctx_lens[s] counts
+ * them). Node j attends every token before the tree, and node i where bit
+ * i % 64 of tree_mask[row][i / 64] is set (its path to the root and itself;
+ * any other set is taken too). Bits from N on are ignored; N <= 64 mask_words.
+ *   q, o [n_rows][Hq][hd], the handle's dtype, q rotated, 16-byte aligned;
+ *   tree_mask [n_rows][mask_words] 64-bit words
+ * A row that attends nothing (no prefix, no bit) gives zeros; what it does not
+ * attend may hold anything. A row's result does not depend on the other
+ * sequences of the call. Needs coco_tree_reserve (COCO_ESTATE without). */
+int coco_tree_attention(coco_layer_t h, int32_t layer, const void* q, void* o, int32_t n_rows,
+                        const int32_t* seq_starts, int32_t n_seqs, const int32_t* block_table,
+                        const int32_t* ctx_lens, const uint64_t* tree_mask, int32_t mask_words,
+                        coco_stream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * Attention over the blocks that a cheap score selects for each query.
+ * ------------------------------------------------------------------------- */
+
+/* Write the summaries of the blocks that hold tokens first_lens[s] (NULL: 0)
+ * .. ctx_lens[s] - 1 of each sequence, from the keys in layer `layer`'s cache:
+ *   summary [num_blocks][Hkv][2][hd] int8, 16-byte aligned; scales
+ *   [num_blocks][Hkv] fp32 (the caller's; num_blocks as the layer's pools)
+ * With hi_d, lo_d the largest and smallest of the block's cached keys in
+ * dimension d (tokens below ctx_lens[s]; a non-finite element counts as 0) and
+ * x in [-100, 100] the exponent with max(|hi|, |lo|) < 2^x: scale 2^(x - 7),
+ * summary[0] = ceil(hi / scale), summary[1] = floor(lo / scale), held within
+ * +-127. Blocks shared by several sequences of the call must be full in each. */
+int coco_kv_summarize(coco_layer_t h, int32_t layer, int8_t* summary, float* scales,
+                      const int32_t* first_lens, const int32_t* ctx_lens, int32_t n_seqs,
+                      const int32_t* block_table, coco_stream_t stream);
+
+/* Make room for block_select / sparse_attention calls of up to max_rows rows
+ * and max_blocks selected blocks (as coco_tree_reserve). */
+int coco_sparse_reserve(coco_layer_t h, int32_t max_rows, int32_t max_blocks);
+
+/* Choose n_select blocks of its sequence for each row and kv head. The row
+ * attends min(ctx_lens, position + 1) keys; of the nb blocks that hold them
+ * the first keep_first and the last keep_last are always chosen, then those
+ * of the highest score, the lowest block among equals; all nb if
+ * nb <= n_select. With q8 = round(q 2^(7 - x)), held within +-127, x the exponent
+ * with |q| < 2^x over the head group (held within +-100, non-finite elements
+ * 0), the score is the largest over the group's query heads of
+ * sum_d q8_d (q8_d > 0 ? summary[0]_d : summary[1]_d), times the block's
+ * scale: all in whole numbers, so equal inputs choose equal blocks.
+ *   q [n_rows][Hq][hd]; positions [n_rows]; seq_starts as in
+ *   coco_layer_forward (NULL: row i is sequence i);
+ *   num_blocks: blocks in summary and scales (ids beyond score as block 0)
+ *   selected [n_rows][Hkv][n_select] int32: blocks of the sequence (entries of
+ *   its table row), ascending, then -1 */
+int coco_block_select(coco_layer_t h, const int8_t* summary, const float* scales,
+                      int64_t num_blocks, const void* q, int32_t n_rows, const int32_t* positions,
+                      const int32_t* seq_starts, int32_t n_seqs, const int32_t* block_table,
+                      const int32_t* ctx_lens, int32_t keep_first, int32_t keep_last,
+                      int32_t* selected, int32_t n_select, coco_stream_t stream);
+
+/* Attention of each row over its keys (positions 0 .. min(ctx_lens,
+ * position + 1) - 1) in the blocks selected[row][kv head] lists, of
+ * coco_block_select or the caller's own: distinct blocks in any order;
+ * entries outside the row's blocks (-1) are skipped. A row without keys gives
+ * zeros. q, o as in coco_tree_attention. */
+int coco_sparse_attention(coco_layer_t h, int32_t layer, const void* q, void* o, int32_t n_rows,
+                          const int32_t* positions, const int32_t* seq_starts, int32_t n_seqs,
+                          const int32_t* block_table, const int32_t* ctx_lens,
+                          const int32_t* selected, int32_t n_select, coco_stream_t stream);
+
 /* Peak probes for benchmarks (not part of the layer): the rates this GPU
  * sustains, against which measured kernels are quoted next to the published
  * peaks. Both enqueue one kernel on `stream` and return COCO_EINVAL for bad

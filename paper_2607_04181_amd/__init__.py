@@ -12,5 +12,7 @@ from ._lib import (  # noqa: F401
     coco_layer_workspace, coco_version, make_config, coco_layer_set_timing,
     coco_layer_read_timing, KERNEL_KINDS, coco_probe_read, coco_probe_mfma_bf16,
     make_scale_model, coco_split_batch, coco_comm_time, coco_speedup, coco_cost_mem,
-    coco_cost_comp, coco_speedup_vec, coco_scale_candidates,
+    coco_cost_comp, coco_speedup_vec, coco_scale_candidates, coco_kv_alloc, coco_kv_fork,
+    coco_kv_free, coco_kv_copy, coco_kv_compact, coco_tree_reserve, coco_tree_attention,
+    coco_kv_summarize, coco_sparse_reserve, coco_block_select, coco_sparse_attention,
 )

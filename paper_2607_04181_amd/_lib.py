@@ -25,6 +25,9 @@ EXPORTS = ["coco_layer_init", "coco_layer_destroy", "coco_last_error", "coco_ver
            "coco_layer_span_forward", "coco_layer_forward_noalloc", "coco_layer_workspace",
            "coco_layer_set_timing",
            "coco_layer_read_timing", "coco_probe_read", "coco_probe_mfma_bf16",
+           "coco_kv_alloc", "coco_kv_fork", "coco_kv_free", "coco_kv_copy", "coco_kv_compact",
+           "coco_tree_reserve", "coco_tree_attention", "coco_kv_summarize",
+           "coco_sparse_reserve", "coco_block_select", "coco_sparse_attention",
            # include/coco_scaling.h: host arithmetic of the speedup/cost model
            "coco_split_batch", "coco_comm_time", "coco_speedup", "coco_cost_mem",
            "coco_cost_comp", "coco_speedup_vec", "coco_scale_candidates"]
@@ -90,6 +93,20 @@ def _load():
         "coco_probe_read": (ctypes.c_int, [vp, i64, vp, i32, i32, vp]),
         "coco_probe_mfma_bf16": (ctypes.c_int, [i64, vp, i32, i32, i32,
                                                 ctypes.POINTER(ctypes.c_double), vp]),
+        "coco_kv_alloc": (ctypes.c_int, [vp, vp, vp, i32, vp, i32, vp, vp, vp]),
+        "coco_kv_fork": (ctypes.c_int, [vp, i32, i32, vp, vp, vp, i32, vp, i32, vp, vp, vp]),
+        "coco_kv_free": (ctypes.c_int, [vp, vp, vp, i32, vp, i32, vp, vp]),
+        "coco_kv_copy": (ctypes.c_int, [vp, i32, i32, vp, vp, i32, vp]),
+        "coco_kv_compact": (ctypes.c_int, [vp, i32, i32, vp, vp, vp, vp, i32, i32, vp, i32, vp]),
+        "coco_tree_reserve": (ctypes.c_int, [vp, i32, i32]),
+        "coco_tree_attention": (ctypes.c_int, [vp, i32, vp, vp, i32, vp, i32, vp, vp, vp, i32,
+                                               vp]),
+        "coco_kv_summarize": (ctypes.c_int, [vp, i32, vp, vp, vp, vp, i32, vp, vp]),
+        "coco_sparse_reserve": (ctypes.c_int, [vp, i32, i32]),
+        "coco_block_select": (ctypes.c_int, [vp, vp, vp, i64, vp, i32, vp, vp, i32, vp, vp, i32,
+                                             i32, vp, i32, vp]),
+        "coco_sparse_attention": (ctypes.c_int, [vp, i32, vp, vp, i32, vp, vp, i32, vp, vp, vp,
+                                                 i32, vp]),
         "coco_split_batch": (ctypes.c_int, [i64, i32, ctypes.POINTER(i64)]),
         "coco_comm_time": (ctypes.c_double, [ctypes.POINTER(coco_scale_model), i32]),
         "coco_speedup": (ctypes.c_double, [ctypes.POINTER(coco_scale_model), i32, i32]),
@@ -144,9 +161,10 @@ def _stream(stream):
 class Handle:
     """An initialised replica; keeps the borrowed tensors alive."""
 
-    def __init__(self, raw, cfg, keep):
+    def __init__(self, raw, cfg, keep, num_blocks=()):
         self.raw = raw
         self.cfg = cfg
+        self.num_blocks = num_blocks  # of each layer's pools
         self._keep = keep
 
     def __del__(self):
@@ -184,7 +202,7 @@ def coco_layer_init(cfg: coco_layer_config, layers) -> Handle:
         arr[i].num_blocks = int(w["k_cache"].shape[0])
     raw = ctypes.c_void_p()
     _check(_lib.coco_layer_init(ctypes.byref(cfg), arr, ctypes.byref(raw)))
-    return Handle(raw, cfg, keep)
+    return Handle(raw, cfg, keep, [int(w["k_cache"].shape[0]) for w in layers])
 
 
 def coco_layer_destroy(h: Handle) -> None:
@@ -289,6 +307,195 @@ def coco_layer_span_forward(h: Handle, first_layer: int, n_layers: int, hidden, 
         _ptr(row_idx, i32, "row_idx"), int(row_idx.numel()), _ptr(positions, i32, "positions"),
         _ptr(seq_starts, i32, "seq_starts"), n_seqs, _ptr(block_table, i32, "block_table"),
         _ptr(ctx_lens, i32, "ctx_lens"), _stream(stream)))
+
+
+def _check_table(h: Handle, block_table, n_seqs=None):
+    _shape_check(isinstance(block_table, torch.Tensor) and block_table.dim() == 2 and
+                 block_table.shape[1] == h.cfg.max_blocks_per_seq,
+                 f"block_table must be [n_seqs, {h.cfg.max_blocks_per_seq}]")
+    _shape_check(n_seqs is None or block_table.shape[0] >= n_seqs,
+                 f"block_table has {block_table.shape[0]} rows for {n_seqs} sequences")
+
+
+def _check_len(name: str, t, n: int):
+    _shape_check(isinstance(t, torch.Tensor) and t.numel() == n, f"{name} must have {n} entries")
+
+
+def _check_counts(h: Handle, ref_counts):
+    n = min(h.num_blocks, default=0)
+    _shape_check(isinstance(ref_counts, torch.Tensor) and ref_counts.numel() >= n,
+                 f"ref_counts must have {n} entries, one per block")
+
+
+def coco_kv_alloc(h: Handle, seq_idx, lens, block_table, ref_counts, status, stream=None):
+    i32 = torch.int32
+    n = int(seq_idx.numel())
+    _check_len("lens", lens, n)
+    _check_len("status", status, n)
+    _check_table(h, block_table)
+    _check_counts(h, ref_counts)
+    _check(_lib.coco_kv_alloc(h.raw, _ptr(seq_idx, i32, "seq_idx"), _ptr(lens, i32, "lens"), n,
+                              _ptr(block_table, i32, "block_table"), int(block_table.shape[0]),
+                              _ptr(ref_counts, i32, "ref_counts"), _ptr(status, i32, "status"),
+                              _stream(stream)))
+
+
+def coco_kv_fork(h: Handle, first_layer: int, n_layers: int, src_seq, dst_seq, lens, block_table,
+                 ref_counts, status, stream=None):
+    i32 = torch.int32
+    n = int(dst_seq.numel())
+    _check_len("src_seq", src_seq, n)
+    _check_len("lens", lens, n)
+    _check_len("status", status, n)
+    _check_table(h, block_table)
+    _check_counts(h, ref_counts)
+    _check(_lib.coco_kv_fork(h.raw, first_layer, n_layers, _ptr(src_seq, i32, "src_seq"),
+                             _ptr(dst_seq, i32, "dst_seq"), _ptr(lens, i32, "lens"), n,
+                             _ptr(block_table, i32, "block_table"), int(block_table.shape[0]),
+                             _ptr(ref_counts, i32, "ref_counts"), _ptr(status, i32, "status"),
+                             _stream(stream)))
+
+
+def coco_kv_free(h: Handle, seq_idx, keep_lens, block_table, ref_counts, stream=None):
+    """keep_lens None: the rows let go of all their blocks."""
+    i32 = torch.int32
+    n = int(seq_idx.numel())
+    if keep_lens is not None:
+        _check_len("keep_lens", keep_lens, n)
+    _check_table(h, block_table)
+    _check_counts(h, ref_counts)
+    _check(_lib.coco_kv_free(h.raw, _ptr(seq_idx, i32, "seq_idx"),
+                             _ptr(keep_lens, i32, "keep_lens"), n,
+                             _ptr(block_table, i32, "block_table"), int(block_table.shape[0]),
+                             _ptr(ref_counts, i32, "ref_counts"), _stream(stream)))
+
+
+def coco_kv_copy(h: Handle, first_layer: int, n_layers: int, src_blocks, dst_blocks, stream=None):
+    i32 = torch.int32
+    n = int(src_blocks.numel())
+    _check_len("dst_blocks", dst_blocks, n)
+    _check(_lib.coco_kv_copy(h.raw, first_layer, n_layers, _ptr(src_blocks, i32, "src_blocks"),
+                             _ptr(dst_blocks, i32, "dst_blocks"), n, _stream(stream)))
+
+
+def coco_kv_compact(h: Handle, first_layer: int, n_layers: int, seq_idx, base_lens, kept,
+                    kept_starts, block_table, stream=None):
+    i32 = torch.int32
+    n = int(seq_idx.numel())
+    _check_len("base_lens", base_lens, n)
+    _check_len("kept_starts", kept_starts, n + 1)
+    _check_table(h, block_table)
+    _check(_lib.coco_kv_compact(h.raw, first_layer, n_layers, _ptr(seq_idx, i32, "seq_idx"),
+                                _ptr(base_lens, i32, "base_lens"), _ptr(kept, i32, "kept"),
+                                _ptr(kept_starts, i32, "kept_starts"), n, int(kept.numel()),
+                                _ptr(block_table, i32, "block_table"), int(block_table.shape[0]),
+                                _stream(stream)))
+
+
+def _check_heads(h: Handle, name: str, t):
+    cfg = h.cfg
+    if not isinstance(t, torch.Tensor) or t.dtype != _elem_dtype(cfg):
+        raise TypeError(f"{name} must be a {_elem_dtype(cfg)} tensor")
+    _shape_check(t.dim() >= 2 and t.numel() == t.shape[0] * cfg.n_q_heads * cfg.head_dim,
+                 f"{name} must be [rows, {cfg.n_q_heads}, {cfg.head_dim}], got {tuple(t.shape)}")
+    return int(t.shape[0])
+
+
+def coco_tree_reserve(h: Handle, max_rows: int, max_seqs: int) -> None:
+    _check(_lib.coco_tree_reserve(h.raw, max_rows, max_seqs))
+
+
+def coco_tree_attention(h: Handle, layer: int, q, o, seq_starts, block_table, ctx_lens, tree_mask,
+                        stream=None):
+    """tree_mask: int64 [rows, words]."""
+    i32 = torch.int32
+    n = _check_heads(h, "q", q)
+    _shape_check(_check_heads(h, "o", o) == n, f"o must have {n} rows")
+    n_seqs = int(ctx_lens.numel())
+    _check_len("seq_starts", seq_starts, n_seqs + 1)
+    _check_table(h, block_table, n_seqs)
+    _shape_check(isinstance(tree_mask, torch.Tensor) and tree_mask.dim() == 2 and
+                 tree_mask.shape[0] == n, f"tree_mask must be [{n}, words]")
+    _check(_lib.coco_tree_attention(
+        h.raw, layer, _ptr(q, what="q"), _ptr(o, what="o"), n, _ptr(seq_starts, i32, "seq_starts"),
+        n_seqs, _ptr(block_table, i32, "block_table"), _ptr(ctx_lens, i32, "ctx_lens"),
+        _ptr(tree_mask, torch.int64, "tree_mask"), int(tree_mask.shape[1]), _stream(stream)))
+
+
+def _check_summary(h: Handle, summary, scales):
+    cfg = h.cfg
+    _shape_check(isinstance(summary, torch.Tensor) and summary.dim() == 4 and
+                 tuple(summary.shape[1:]) == (cfg.n_kv_heads, 2, cfg.head_dim),
+                 f"summary must be [num_blocks, {cfg.n_kv_heads}, 2, {cfg.head_dim}]")
+    _check_len("scales", scales, summary.shape[0] * cfg.n_kv_heads)
+
+
+def coco_kv_summarize(h: Handle, layer: int, summary, scales, first_lens, ctx_lens, block_table,
+                      stream=None):
+    """first_lens None: the whole sequences."""
+    i32 = torch.int32
+    n_seqs = int(ctx_lens.numel())
+    _check_summary(h, summary, scales)
+    blocks = h.num_blocks[layer] if 0 <= layer < len(h.num_blocks) else 0
+    _shape_check(summary.shape[0] >= blocks, f"summary must have the layer's {blocks} blocks")
+    if first_lens is not None:
+        _check_len("first_lens", first_lens, n_seqs)
+    _check_table(h, block_table, n_seqs)
+    _check(_lib.coco_kv_summarize(
+        h.raw, layer, _ptr(summary, torch.int8, "summary"), _ptr(scales, torch.float32, "scales"),
+        _ptr(first_lens, i32, "first_lens"), _ptr(ctx_lens, i32, "ctx_lens"), n_seqs,
+        _ptr(block_table, i32, "block_table"), _stream(stream)))
+
+
+def coco_sparse_reserve(h: Handle, max_rows: int, max_blocks: int) -> None:
+    _check(_lib.coco_sparse_reserve(h.raw, max_rows, max_blocks))
+
+
+def _check_selected(h: Handle, selected, n: int) -> int:
+    _shape_check(isinstance(selected, torch.Tensor) and selected.dim() == 3 and
+                 tuple(selected.shape[:2]) == (n, h.cfg.n_kv_heads),
+                 f"selected must be [{n}, {h.cfg.n_kv_heads}, blocks]")
+    return int(selected.shape[2])
+
+
+def _check_row_arrays(h: Handle, n: int, positions, seq_starts, block_table, ctx_lens) -> int:
+    _check_len("positions", positions, n)
+    n_seqs = int(ctx_lens.numel())
+    if seq_starts is None:
+        _shape_check(n_seqs == n, f"ctx_lens has {n_seqs} entries for {n} rows")
+    else:
+        _check_len("seq_starts", seq_starts, n_seqs + 1)
+    _check_table(h, block_table, n_seqs)
+    return n_seqs
+
+
+def coco_block_select(h: Handle, summary, scales, q, positions, seq_starts, block_table, ctx_lens,
+                      keep_first: int, keep_last: int, selected, stream=None):
+    i32 = torch.int32
+    n = _check_heads(h, "q", q)
+    n_seqs = _check_row_arrays(h, n, positions, seq_starts, block_table, ctx_lens)
+    _check_summary(h, summary, scales)
+    n_select = _check_selected(h, selected, n)
+    _check(_lib.coco_block_select(
+        h.raw, _ptr(summary, torch.int8, "summary"), _ptr(scales, torch.float32, "scales"),
+        int(summary.shape[0]), _ptr(q, what="q"), n, _ptr(positions, i32, "positions"),
+        _ptr(seq_starts, i32, "seq_starts"), n_seqs, _ptr(block_table, i32, "block_table"),
+        _ptr(ctx_lens, i32, "ctx_lens"), keep_first, keep_last, _ptr(selected, i32, "selected"),
+        n_select, _stream(stream)))
+
+
+def coco_sparse_attention(h: Handle, layer: int, q, o, positions, seq_starts, block_table,
+                          ctx_lens, selected, stream=None):
+    i32 = torch.int32
+    n = _check_heads(h, "q", q)
+    _shape_check(_check_heads(h, "o", o) == n, f"o must have {n} rows")
+    n_seqs = _check_row_arrays(h, n, positions, seq_starts, block_table, ctx_lens)
+    n_select = _check_selected(h, selected, n)
+    _check(_lib.coco_sparse_attention(
+        h.raw, layer, _ptr(q, what="q"), _ptr(o, what="o"), n, _ptr(positions, i32, "positions"),
+        _ptr(seq_starts, i32, "seq_starts"), n_seqs, _ptr(block_table, i32, "block_table"),
+        _ptr(ctx_lens, i32, "ctx_lens"), _ptr(selected, i32, "selected"), n_select,
+        _stream(stream)))
 
 
 def coco_layer_workspace(h: Handle, which: int, dst, stream=None) -> None:

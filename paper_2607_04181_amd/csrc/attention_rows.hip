@@ -1,0 +1,259 @@
+// Attention of rows that do not see a plain causal prefix of the paged cache:
+// the nodes of a tree of drafted tokens, and rows that attend selected blocks.
+//
+// One workgroup per row and GH query heads of one key/value head, eight waves
+// striding over the row's blocks with an online softmax each, merged in LDS in
+// wave order. Lane (t, j4) holds token t's part of a key tile and, of a value
+// tile, tokens 4 j4 .. + 3 of dims 32 p + t and + 16.
+#include <math.h>
+
+#include "common.h"
+#include "kernels.h"
+
+namespace coco {
+
+namespace {
+
+constexpr int kRowsWaves = 8;
+
+struct F8 {
+  float e[8];
+};
+__device__ __forceinline__ F8 load8(const float* p) {
+  const f32x4_t a = *(const f32x4_t*)p, b = *(const f32x4_t*)(p + 4);
+  return F8{{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]}};
+}
+__device__ __forceinline__ F8 load8(const bf16_t* p) {
+  const u32x4_t a = *(const u32x4_t*)p;
+  F8 r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    r.e[2 * i] = bf16_to_f32(a[i] & 0xFFFFu);
+    r.e[2 * i + 1] = __uint_as_float(a[i] & 0xFFFF0000u);
+  }
+  return r;
+}
+__device__ __forceinline__ void store1(float* p, float x) { *p = x; }
+__device__ __forceinline__ void store1(bf16_t* p, float x) { *p = (bf16_t)f32_to_bf16(x); }
+
+// Bits k0 .. k0 + 15 of what a tree node sees, k0 counted from the first node:
+// set before it (the prefix), the row's mask among the n nodes, clear behind.
+__device__ __forceinline__ uint32_t tree_bits(const uint64_t* mask, int words, int n, int k0) {
+  if (k0 <= -16) return 0xFFFFu;
+  uint64_t v;
+  if (k0 >= 0) {
+    const int w = k0 >> 6, sh = k0 & 63;
+    v = w < words ? mask[w] >> sh : 0;
+    if (sh > 48 && w + 1 < words) v |= mask[w + 1] << (64 - sh);
+  } else {
+    v = mask[0] << -k0 | ((1ull << -k0) - 1);
+  }
+  const int left = n - k0;
+  if (left < 16) v &= left > 0 ? (1ull << left) - 1 : 0;
+  return (uint32_t)v & 0xFFFFu;
+}
+
+// HS: head_dim / 32.
+template <typename T, int HS, int GH, bool TREE>
+__global__ __launch_bounds__(64 * kRowsWaves) void attn_rows_kernel(
+    const T* __restrict__ q, const T* __restrict__ k_cache, const T* __restrict__ v_cache,
+    RowKeys rk, int Hq, int Hkv, T* __restrict__ o, bool tiled) {
+  constexpr int hd = 32 * HS;
+  __shared__ float sm_m[kRowsWaves][GH], sm_l[kRowsWaves][GH];
+  __shared__ float sm_o[kRowsWaves][GH][hd];
+  const int i = blockIdx.x, h0 = blockIdx.y * GH;
+  const int lane = threadIdx.x & 63;
+  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int t = lane & 15, j4 = lane >> 4;
+  const int s = row_to_seq(rk.seq_starts, rk.n_seqs, i);
+  const int g = h0 / (Hq / Hkv);
+  // Keys of the row's sequence that it may attend; tree: nodes, and the first
+  // node's place among the keys.
+  int n, nodes = 0, prefix = 0;
+  const uint64_t* mask = nullptr;
+  const int32_t* list = nullptr;
+  int entries;
+  if constexpr (TREE) {
+    n = rk.ctx_lens[s];
+    nodes = rk.seq_starts[s + 1] - rk.seq_starts[s];
+    prefix = n - nodes;
+    mask = rk.mask + (int64_t)i * rk.words;
+  } else {
+    n = min(rk.ctx_lens[s], rk.positions[i] + 1);
+    list = rk.selected + ((int64_t)i * Hkv + g) * rk.top;
+  }
+  n = min(max(n, 0), rk.max_blocks * kBlockTokens);
+  const int blocks = (n + kBlockTokens - 1) / kBlockTokens;
+  entries = TREE ? blocks : rk.top;
+  const int32_t* bt = rk.block_table + (int64_t)s * rk.max_blocks;
+  const float scale = 1.0f / sqrtf((float)hd);
+
+  // This lane's part of the queries: dims 32 p + 8 j4 .. + 7.
+  F8 qv[GH][HS];
+#pragma unroll
+  for (int e = 0; e < GH; ++e)
+#pragma unroll
+    for (int p = 0; p < HS; ++p)
+      qv[e][p] = load8(q + ((int64_t)i * Hq + h0 + e) * hd + 32 * p + 8 * j4);
+
+  float m[GH], l[GH], acc[GH][HS][2];
+#pragma unroll
+  for (int e = 0; e < GH; ++e) {
+    m[e] = -INFINITY;
+    l[e] = 0.f;
+#pragma unroll
+    for (int p = 0; p < HS; ++p) acc[e][p][0] = acc[e][p][1] = 0.f;
+  }
+  for (int x = wv; x < entries; x += kRowsWaves) {
+    const int b = TREE ? x : list[x];
+    if (!TREE && (b < 0 || b >= blocks)) continue;
+    const int tok0 = b * kBlockTokens;
+    uint32_t seen;
+    if constexpr (TREE) {
+      seen = tree_bits(mask, rk.words, nodes, tok0 - prefix);
+      if (seen == 0) continue;
+    } else {
+      seen = n - tok0 < 16 ? (1u << (n - tok0)) - 1 : 0xFFFFu;
+    }
+    const int64_t tile = ((int64_t)bt[b] * Hkv + g) * (kBlockTokens * hd);
+    F8 kf[HS], vf[HS];
+#pragma unroll
+    for (int p = 0; p < HS; ++p) {
+      kf[p] = load8(k_cache + tile + (p * 64 + lane) * 8);
+      vf[p] = load8(v_cache + tile + (p * 64 + lane) * 8);
+    }
+    const bool live = seen >> t & 1;
+    // Values of tokens that the row does not see may be anything, NaN among it.
+#pragma unroll
+    for (int p = 0; p < HS; ++p)
+#pragma unroll
+      for (int c = 0; c < 8; ++c)
+        if (!(seen >> (4 * j4 + c % 4) & 1)) vf[p].e[c] = 0.f;
+#pragma unroll
+    for (int e = 0; e < GH; ++e) {
+      float z = 0.f;
+#pragma unroll
+      for (int p = 0; p < HS; ++p)
+#pragma unroll
+        for (int c = 0; c < 8; ++c) z = fmaf(qv[e][p].e[c], kf[p].e[c], z);
+      z += __shfl_xor(z, 16, kWave);
+      z += __shfl_xor(z, 32, kWave);
+      z = live ? z * scale : -INFINITY;
+      float mx = z;
+#pragma unroll
+      for (int d = 8; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor(mx, d, kWave));
+      const float m_new = fmaxf(m[e], mx);
+      // A block of keys that all score -inf leaves m at -inf.
+      const float m_ref = m_new == -INFINITY ? 0.f : m_new;
+      const float alpha = expf(m[e] - m_ref);
+      const float pr = expf(z - m_ref);
+      float ls = pr;
+#pragma unroll
+      for (int d = 8; d > 0; d >>= 1) ls += __shfl_xor(ls, d, kWave);
+      l[e] = l[e] * alpha + ls;
+      m[e] = m_new;
+      float p4[4];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) p4[c] = __shfl(pr, 4 * j4 + c, kWave);
+#pragma unroll
+      for (int p = 0; p < HS; ++p)
+#pragma unroll
+        for (int f = 0; f < 2; ++f) {
+          float a = acc[e][p][f] * alpha;
+#pragma unroll
+          for (int c = 0; c < 4; ++c) a = fmaf(p4[c], vf[p].e[4 * f + c], a);
+          acc[e][p][f] = a;
+        }
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < GH; ++e) {
+    if (lane == 0) {
+      sm_m[wv][e] = m[e];
+      sm_l[wv][e] = l[e];
+    }
+#pragma unroll
+    for (int p = 0; p < HS; ++p)
+#pragma unroll
+      for (int f = 0; f < 2; ++f) {
+        float a = acc[e][p][f];  // dim 32 p + 16 f + lane % 16, tokens 4 j4 ..
+        a += __shfl_xor(a, 16, kWave);
+        a += __shfl_xor(a, 32, kWave);
+        if (j4 == 0) sm_o[wv][e][32 * p + 16 * f + t] = a;
+      }
+  }
+  __syncthreads();
+  for (int x = threadIdx.x; x < GH * hd; x += 64 * kRowsWaves) {
+    const int e = x / hd, dim = x - e * hd;
+    float mx = sm_m[0][e];
+#pragma unroll
+    for (int w = 1; w < kRowsWaves; ++w) mx = fmaxf(mx, sm_m[w][e]);
+    const float ref = mx == -INFINITY ? 0.f : mx;
+    float a = 0.f, L = 0.f;
+#pragma unroll
+    for (int w = 0; w < kRowsWaves; ++w) {
+      const float f = expf(sm_m[w][e] - ref);
+      a = fmaf(f, sm_o[w][e][dim], a);
+      L = fmaf(f, sm_l[w][e], L);
+    }
+    const int col = (h0 + e) * hd + dim;
+    store1(o + (tiled ? tile_off(i, col, Hq * hd) : (int64_t)i * Hq * hd + col),
+           L == 0.f ? 0.f : a / L);
+  }
+}
+
+}  // namespace
+
+template <typename T>
+hipError_t launch_attn_rows(const T* q, const T* k_cache, const T* v_cache, const RowKeys& rk,
+                            int n_rows, int Hq, int Hkv, int hd, T* o, bool tiled,
+                            hipStream_t st) {
+  if (n_rows <= 0) return hipSuccess;
+  // Heads per workgroup: they share the key/value loads; the queries they
+  // keep in registers (hd / 4 floats per lane each) bound their number.
+  const int G = Hq / Hkv;
+  const int gh = (G % 4 == 0 && hd <= 64) ? 4 : (G % 2 == 0 && hd <= 128) ? 2 : 1;
+  const dim3 grid(n_rows, Hq / gh), block(64 * kRowsWaves);
+#define COCO_ROWS(HS, GH)                                                                     \
+  do {                                                                                        \
+    if (rk.mask)                                                                              \
+      COCO_LAUNCH((attn_rows_kernel<T, HS, GH, true>), grid, block, 0, st, q, k_cache,        \
+                  v_cache, rk, Hq, Hkv, o, tiled);                                            \
+    else                                                                                      \
+      COCO_LAUNCH((attn_rows_kernel<T, HS, GH, false>), grid, block, 0, st, q, k_cache,       \
+                  v_cache, rk, Hq, Hkv, o, tiled);                                            \
+  } while (0)
+#define COCO_ROWS4(HS) \
+  if (gh == 4) COCO_ROWS(HS, 4); else if (gh == 2) COCO_ROWS(HS, 2); else COCO_ROWS(HS, 1)
+#define COCO_ROWS2(HS) \
+  if (gh == 2) COCO_ROWS(HS, 2); else COCO_ROWS(HS, 1)
+  if constexpr (sizeof(T) == 2) {
+    if (hd != 128) return hipErrorInvalidValue;
+    COCO_ROWS2(4);
+  } else {
+    switch (hd) {
+      case 32: COCO_ROWS4(1); break;
+      case 64: COCO_ROWS4(2); break;
+      case 96: COCO_ROWS2(3); break;
+      case 128: COCO_ROWS2(4); break;
+      case 160: COCO_ROWS(5, 1); break;
+      case 192: COCO_ROWS(6, 1); break;
+      case 224: COCO_ROWS(7, 1); break;
+      case 256: COCO_ROWS(8, 1); break;
+      default: return hipErrorInvalidValue;
+    }
+  }
+#undef COCO_ROWS4
+#undef COCO_ROWS2
+#undef COCO_ROWS
+  return hipGetLastError();
+}
+
+template hipError_t launch_attn_rows<bf16_t>(const bf16_t*, const bf16_t*, const bf16_t*,
+                                             const RowKeys&, int, int, int, int, bf16_t*, bool,
+                                             hipStream_t);
+template hipError_t launch_attn_rows<float>(const float*, const float*, const float*,
+                                            const RowKeys&, int, int, int, int, float*, bool,
+                                            hipStream_t);
+
+}  // namespace coco

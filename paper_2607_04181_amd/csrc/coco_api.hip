@@ -8,81 +8,29 @@
 #include <mutex>
 #include <vector>
 
-#include "../../include/coco.h"
-#include "common.h"
-#include "kernels.h"
+#include "handle.h"
 
 using namespace coco;
 
 namespace {
-
-// Message of the last failure on this thread (a fixed buffer: reporting an
-// error allocates nothing).
+// Message of the last failure on this thread.
 thread_local char g_err[512];
+}  // namespace
 
-int fail(int code, const char* fmt, ...) {
+int coco::mark_done(coco_layer* H, hipStream_t st) {
+  hipStreamCaptureStatus cs = hipStreamCaptureStatusNone;
+  HIPCHK(hipStreamIsCapturing(st, &cs));
+  if (cs == hipStreamCaptureStatusNone) HIPCHK(hipEventRecord(H->done, st));
+  return COCO_OK;
+}
+
+int coco::fail(int code, const char* fmt, ...) {
   va_list ap;
   va_start(ap, fmt);
   vsnprintf(g_err, sizeof g_err, fmt, ap);
   va_end(ap);
   return code;
 }
-
-#define HIPCHK(expr)                                                                  \
-  do {                                                                                \
-    hipError_t e_ = (expr);                                                           \
-    if (e_ != hipSuccess) return fail(COCO_EHIP, "%s: %s", #expr, hipGetErrorString(e_)); \
-  } while (0)
-
-}  // namespace
-
-// Per-call buffers of the launch sequence, carved out of one region (the
-// handle's workspace, or the static scratch array of the no-alloc entry
-// point).
-struct Work {
-  void *x = nullptr, *h = nullptr, *q = nullptr, *o = nullptr, *h2 = nullptr, *u = nullptr;
-  float *x1 = nullptr, *part = nullptr, *attn_o = nullptr, *attn_ml = nullptr;
-  // Row sums of squares per K-slice (decode QKV with RMSNorm_1 folded in). The
-  // prefill O projection's, per 32 columns ([rows][d / 32]), are in `part`,
-  // which prefill has no other use for.
-  float* ss = nullptr;
-  int32_t* split_off = nullptr;  // decode attention work list
-  int32_t* row_info = nullptr;   // prefill row slots [rows][2] (position, cache block)
-};
-
-struct coco_layer {
-  coco_layer_config cfg;
-  std::vector<coco_layer_weights> layers;
-  int device = 0;
-  int num_cus = 0;  // compute units of `device` (persistent grid sizes)
-  bool validate = false;
-  char* ws = nullptr;
-  size_t ws_bytes = 0;
-  // bf16: the library's tile-order copies of every layer's four weight
-  // matrices (layers[l].w_* point into it after init).
-  char* packed = nullptr;
-  size_t packed_bytes = 0;
-  Work w;  // the workspace's per-call buffers, sized for max_rows
-  double* inv_freq = nullptr;
-  float* rope = nullptr;  // RoPE table [rope_rows][head_dim / 2] (cos, sin)
-  int rope_rows = 0;      // positions the configuration admits
-  size_t act_rows_bytes[7] = {};
-  int max_splits = 0;
-  int dec_rows = 0;
-  // Which of the last regular call's activations h, o, h2, u are in tile
-  // order (act_layout), read back row-major by coco_layer_workspace, and
-  // that call's rows.
-  bool ws_tiled[7] = {};
-  int last_rows = 0;
-  // Per-kernel timing (benchmark mode).
-  bool timing = false;
-  std::vector<hipEvent_t> ev;  // pairs: start, stop
-  std::vector<int> ev_kind;    // kind of each recorded pair
-  bool ev_overflow = false;
-  hipStream_t ev_stream = nullptr;
-  // Recorded at the end of every call made outside graph capture.
-  hipEvent_t done = nullptr;
-};
 
 namespace coco {
 LaunchEvents& launch_events() {
@@ -128,10 +76,6 @@ struct KernelTimer {
 }  // namespace
 
 namespace {
-
-size_t align256(size_t b) { return (b + 255) & ~(size_t)255; }
-
-int elem_bytes(int dtype) { return dtype == COCO_BF16 ? 2 : 4; }
 
 // Fp32 partials [splits][rows][N] that `part` counts: the decode GEMMs'
 // K-slices, and at least one per 8192 k (up to four) where N <= 12,032. The
@@ -398,7 +342,11 @@ int coco_layer_init(const coco_layer_config* cfg, const coco_layer_weights* laye
   carve_work(c, R, H->dec_rows, H->max_splits, nullptr, nullptr, &work_bytes);
   const size_t freq_bytes = align256((size_t)(c.head_dim / 2) * 8);
   const size_t rope_bytes = align256((size_t)H->rope_rows * (c.head_dim / 2) * 8);
-  H->ws_bytes = work_bytes + freq_bytes + rope_bytes;
+  int64_t max_blocks = 0;
+  for (const coco_layer_weights& w : H->layers)
+    if (w.num_blocks > max_blocks) max_blocks = w.num_blocks;
+  const size_t page_bytes = align256((size_t)max_blocks * 4);
+  H->ws_bytes = work_bytes + freq_bytes + rope_bytes + page_bytes + align256((size_t)c.max_seqs * 4);
   if (hipMalloc((void**)&H->ws, H->ws_bytes) != hipSuccess) {
     (void)hipGetLastError();
     const size_t want = H->ws_bytes;
@@ -408,6 +356,8 @@ int coco_layer_init(const coco_layer_config* cfg, const coco_layer_weights* laye
   carve_work(c, R, H->dec_rows, H->max_splits, H->ws, &H->w);
   H->inv_freq = (double*)(H->ws + work_bytes);
   H->rope = (float*)(H->ws + work_bytes + freq_bytes);
+  H->page_list = (int32_t*)(H->ws + work_bytes + freq_bytes + rope_bytes);
+  H->page_off = (int32_t*)(H->ws + work_bytes + freq_bytes + rope_bytes + page_bytes);
   H->act_rows_bytes[COCO_WS_X] = R * d * eb;
   H->act_rows_bytes[COCO_WS_H] = R * d * eb;
   H->act_rows_bytes[COCO_WS_Q] = R * qd * eb;
@@ -458,6 +408,7 @@ void coco_layer_destroy(coco_layer_t H) {
   for (auto& e : H->ev) (void)hipEventDestroy(e);
   (void)hipFree(H->ws);
   if (H->packed) (void)hipFree(H->packed);
+  for (char* p : H->extra) (void)hipFree(p);
   (void)hipSetDevice(cur);
   delete H;
 }
@@ -534,15 +485,6 @@ int coco_layer_workspace(coco_layer_t H, int32_t which, void* dst, int64_t dst_b
 // Validation of device-side index arrays (debug mode; synchronises).
 // ----------------------------------------------------------------------------
 namespace {
-
-template <typename V>
-int fetch(std::vector<V>& dst, const V* src, size_t n, hipStream_t st) {
-  dst.resize(n);
-  if (n == 0) return COCO_OK;
-  HIPCHK(hipMemcpyAsync(dst.data(), src, n * sizeof(V), hipMemcpyDeviceToHost, st));
-  HIPCHK(hipStreamSynchronize(st));
-  return COCO_OK;
-}
 
 int validate_batch(coco_layer* H, int64_t hidden_rows, const int32_t* row_idx, int n_rows,
                    const int32_t* positions, const int32_t* seq_starts, int n_seqs,
@@ -935,16 +877,6 @@ int check_batch(coco_layer* H, int first, int nl, const void* hidden, int64_t hi
   } else if (n_seqs > n_rows) {
     return fail(COCO_EINVAL, "more sequences than rows");
   }
-  return COCO_OK;
-}
-
-// Records the handle's completion event behind the call's last kernel, unless
-// the stream is being captured into a graph (the event would then only fire
-// on replays).
-int mark_done(coco_layer* H, hipStream_t st) {
-  hipStreamCaptureStatus cs = hipStreamCaptureStatusNone;
-  HIPCHK(hipStreamIsCapturing(st, &cs));
-  if (cs == hipStreamCaptureStatusNone) HIPCHK(hipEventRecord(H->done, st));
   return COCO_OK;
 }
 

@@ -1,0 +1,109 @@
+// The replica handle and the error reporting that the library's entry points
+// share (internal to libcoco).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <vector>
+
+#include "../../include/coco.h"
+#include "common.h"
+#include "kernels.h"
+
+namespace coco {
+
+// Records the message of a failed call on this thread (a fixed buffer:
+// reporting an error allocates nothing) and returns `code`.
+__attribute__((format(printf, 2, 3))) int fail(int code, const char* fmt, ...);
+
+#define HIPCHK(expr)                                                                  \
+  do {                                                                                \
+    hipError_t e_ = (expr);                                                           \
+    if (e_ != hipSuccess)                                                             \
+      return ::coco::fail(COCO_EHIP, "%s: %s", #expr, hipGetErrorString(e_));         \
+  } while (0)
+
+inline size_t align256(size_t b) { return (b + 255) & ~(size_t)255; }
+
+inline int elem_bytes(int dtype) { return dtype == COCO_BF16 ? 2 : 4; }
+
+// Copies n values of a device array to the host behind the stream's work
+// (validation mode; synchronises).
+template <typename V>
+int fetch(std::vector<V>& dst, const V* src, size_t n, hipStream_t st) {
+  dst.resize(n);
+  if (n == 0) return COCO_OK;
+  HIPCHK(hipMemcpyAsync(dst.data(), src, n * sizeof(V), hipMemcpyDeviceToHost, st));
+  HIPCHK(hipStreamSynchronize(st));
+  return COCO_OK;
+}
+
+}  // namespace coco
+
+// Per-call buffers of the launch sequence, carved out of one region (the
+// handle's workspace, or the static scratch array of the no-alloc entry
+// point).
+struct Work {
+  void *x = nullptr, *h = nullptr, *q = nullptr, *o = nullptr, *h2 = nullptr, *u = nullptr;
+  float *x1 = nullptr, *part = nullptr, *attn_o = nullptr, *attn_ml = nullptr;
+  // Row sums of squares per K-slice (decode QKV with RMSNorm_1 folded in). The
+  // prefill O projection's, per 32 columns ([rows][d / 32]), are in `part`,
+  // which prefill has no other use for.
+  float* ss = nullptr;
+  int32_t* split_off = nullptr;  // decode attention work list
+  int32_t* row_info = nullptr;   // prefill row slots [rows][2] (position, cache block)
+};
+
+struct coco_layer {
+  coco_layer_config cfg;
+  std::vector<coco_layer_weights> layers;
+  int device = 0;
+  int num_cus = 0;  // compute units of `device` (persistent grid sizes)
+  bool validate = false;
+  char* ws = nullptr;
+  size_t ws_bytes = 0;
+  // bf16: the library's tile-order copies of every layer's four weight
+  // matrices (layers[l].w_* point into it after init).
+  char* packed = nullptr;
+  size_t packed_bytes = 0;
+  Work w;  // the workspace's per-call buffers, sized for max_rows
+  double* inv_freq = nullptr;
+  float* rope = nullptr;  // RoPE table [rope_rows][head_dim / 2] (cos, sin)
+  int rope_rows = 0;      // positions the configuration admits
+  size_t act_rows_bytes[7] = {};
+  int max_splits = 0;
+  int dec_rows = 0;
+  // Which of the last regular call's activations h, o, h2, u are in tile
+  // order (act_layout), read back row-major by coco_layer_workspace, and
+  // that call's rows.
+  bool ws_tiled[7] = {};
+  int last_rows = 0;
+  // Per-kernel timing (benchmark mode).
+  bool timing = false;
+  std::vector<hipEvent_t> ev;  // pairs: start, stop
+  std::vector<int> ev_kind;    // kind of each recorded pair
+  bool ev_overflow = false;
+  hipStream_t ev_stream = nullptr;
+  // Recorded at the end of every call made outside graph capture.
+  hipEvent_t done = nullptr;
+  // Page requests: the free blocks found (one per block) and each request's
+  // first place among them (max_seqs).
+  int32_t *page_list = nullptr, *page_off = nullptr;
+  // What coco_tree_reserve and coco_sparse_reserve made room for, and the
+  // buffers (in `extra`, which keeps outgrown ones until destroy).
+  int tree_rows = 0, tree_seqs = 0;
+  int sparse_rows = 0, sparse_top = 0;
+  char* sparse_keys = nullptr;
+  size_t sparse_keys_bytes = 0;
+  std::vector<char*> extra;
+};
+
+namespace coco {
+
+// Records the handle's completion event behind the call's last kernel, unless
+// the stream is being captured into a graph (the event would then only fire
+// on replays).
+int mark_done(coco_layer* H, hipStream_t st);
+
+}  // namespace coco

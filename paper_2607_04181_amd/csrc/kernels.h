@@ -276,4 +276,83 @@ hipError_t launch_attn_f32(const float* q, const float* k_cache, const float* v_
                            const int32_t* seq_starts, int n_seqs, int n_rows, int Hq,
                            int Hkv, int hd, float* o, hipStream_t st);
 
+// ---------------------------------------------------------------- pages
+// Pools of a call's layers, key and value pools in turn (kernel argument).
+constexpr int kMaxPools = 128;
+struct CachePools {
+  char* p[kMaxPools];
+  int n = 0;
+};
+
+// Requests for blocks: request i's row dst[i] (fork: from row src[i]) and
+// length. list: the free blocks found; off: each request's first place in it;
+// status (the caller's): 1 where the request is served, else 0.
+struct PageArgs {
+  const int32_t* src = nullptr;  // null: alloc
+  const int32_t* dst = nullptr;
+  const int32_t* lens = nullptr;
+  int n = 0, n_seqs = 0, max_blocks = 0;
+  int64_t num_blocks = 0;
+  int32_t* table = nullptr;
+  int32_t* refs = nullptr;
+  int32_t* status = nullptr;
+  int32_t* list = nullptr;  // [num_blocks]
+  int32_t* off = nullptr;   // [n]
+};
+hipError_t launch_page_plan(const PageArgs& a, hipStream_t st);
+hipError_t launch_page_alloc(const PageArgs& a, hipStream_t st);
+// tables: also the children's table rows and the counts (a call's first group
+// of pools); bytes: one block of one pool.
+hipError_t launch_page_fork(const PageArgs& a, const CachePools& pools, int64_t bytes,
+                            bool tables, hipStream_t st);
+hipError_t launch_page_free(const int32_t* seq, const int32_t* keep, int n, int n_seqs,
+                            int32_t* table, int max_blocks, int32_t* refs, int64_t num_blocks,
+                            hipStream_t st);
+hipError_t launch_page_copy(const int32_t* src, const int32_t* dst, int n, int64_t num_blocks,
+                            const CachePools& pools, int64_t bytes, hipStream_t st);
+template <typename T>
+hipError_t launch_page_compact(const int32_t* seq, const int32_t* base, const int32_t* kept,
+                               const int32_t* starts, int n, int n_kept, const int32_t* table,
+                               int n_seqs, int max_blocks, int64_t num_blocks,
+                               const CachePools& pools, int Hkv, int hd, hipStream_t st);
+
+// ------------------------------------------- attention of rows of their own
+// Which keys a call's rows attend. Tree: the rows of sequence s
+// (seq_starts[s] ..) are the nodes in its last cached slots; all keys before
+// those, and the nodes whose bit is set in the row's mask words. Blocks: keys
+// up to the row's position in the blocks that selected[row][kv head] lists.
+struct RowKeys {
+  const int32_t* block_table = nullptr;
+  const int32_t* ctx_lens = nullptr;
+  const int32_t* seq_starts = nullptr;  // blocks: null: row i is sequence i
+  int n_seqs = 0, max_blocks = 0;
+  int64_t num_blocks = 0;
+  const uint64_t* mask = nullptr;       // tree: [rows][words]
+  int words = 0;
+  const int32_t* positions = nullptr;   // blocks
+  const int32_t* selected = nullptr;    // blocks: [rows][Hkv][top], -1: none
+  int top = 0;
+};
+// o [rows][Hq][hd], or (bf16) in tile order.
+template <typename T>
+hipError_t launch_attn_rows(const T* q, const T* k_cache, const T* v_cache, const RowKeys& rk,
+                            int n_rows, int Hq, int Hkv, int hd, T* o, bool tiled,
+                            hipStream_t st);
+
+// ---------------------------------------------------------- block summaries
+// summary [block][Hkv][2][hd] and scales [block][Hkv] of the blocks that hold
+// tokens first[s] (null: 0) .. ctx_lens[s] - 1 of each sequence.
+template <typename T>
+hipError_t launch_summarize(const T* k_cache, int Hkv, int hd, const int32_t* block_table,
+                            int n_seqs, int max_blocks, int64_t num_blocks, const int32_t* first,
+                            const int32_t* ctx_lens, int8_t* summary, float* scales, int num_cus,
+                            hipStream_t st);
+// Scores of every block a row can choose, as order-preserving keys
+// [rows][Hkv][max_blocks], then the choice.
+template <typename T>
+hipError_t launch_block_select(const T* q, const int8_t* summary, const float* scales,
+                               const RowKeys& rk, int n_rows, int Hq, int Hkv, int hd,
+                               int keep_first, int keep_last, uint32_t* keys, int32_t* selected,
+                               hipStream_t st);
+
 }  // namespace coco
