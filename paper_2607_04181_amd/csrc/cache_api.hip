@@ -368,8 +368,31 @@ int coco_kv_compact(coco_layer_t H, int32_t first_layer, int32_t n_layers, const
 int coco_tree_reserve(coco_layer_t H, int32_t max_rows, int32_t max_seqs) {
   if (!H) return fail(COCO_EINVAL, "handle is NULL");
   if (max_rows < 1 || max_seqs < 1) return fail(COCO_EINVAL, "sizes must be positive");
-  if (max_rows > H->tree_rows) H->tree_rows = max_rows;
-  if (max_seqs > H->tree_seqs) H->tree_seqs = max_seqs;
+  const int rows = max_rows > H->tree_rows ? max_rows : H->tree_rows;
+  const int seqs = max_seqs > H->tree_seqs ? max_seqs : H->tree_seqs;
+  const coco_layer_config& c = H->cfg;
+  if (c.dtype == COCO_BF16) {
+    const int64_t parts =
+        tree_column_parts(rows, seqs, c.n_q_heads, c.n_kv_heads, c.max_blocks_per_seq);
+    if (parts > INT32_MAX)
+      return fail(COCO_EINVAL, "%d rows of %d sequences: %lld partial columns exceed 2^31 - 1",
+                  rows, seqs, (long long)parts);
+    const size_t o = align256((size_t)parts * c.head_dim * 4), ml = align256((size_t)parts * 8);
+    const size_t plan = align256((size_t)seqs * 8), redo = (size_t)rows * c.n_q_heads * 4;
+    const char* had = H->tree_ws;
+    const int rc = grow(H, &H->tree_ws, &H->tree_bytes, o + ml + plan + redo);
+    if (rc) return rc;
+    if (H->tree_ws != had) {  // calls on any stream are to find it zero
+      HIPCHK(hipMemset(H->tree_ws + o + ml + plan, 0, redo));
+      HIPCHK(hipDeviceSynchronize());
+    }
+    H->tree_part_o = (float*)H->tree_ws;
+    H->tree_part_ml = (float*)(H->tree_ws + o);
+    H->tree_plan = (int32_t*)(H->tree_ws + o + ml);
+    H->tree_redo = (int32_t*)(H->tree_ws + o + ml + plan);
+  }
+  H->tree_rows = rows;
+  H->tree_seqs = seqs;
   return COCO_OK;
 }
 
@@ -414,9 +437,11 @@ int coco_tree_attention(coco_layer_t H, int32_t layer, const void* q, void* o, i
   rk.mask = tree_mask;
   rk.words = mask_words;
   if (c.dtype == COCO_BF16)
-    HIPCHK(launch_attn_rows((const bf16_t*)q, (const bf16_t*)w.k_cache, (const bf16_t*)w.v_cache,
-                            rk, n_rows, c.n_q_heads, c.n_kv_heads, c.head_dim, (bf16_t*)o, false,
-                            st));
+    HIPCHK(launch_tree_attention_bf16((const bf16_t*)q, (const bf16_t*)w.k_cache,
+                                      (const bf16_t*)w.v_cache, rk, n_rows, c.n_q_heads,
+                                      c.n_kv_heads, (bf16_t*)o, false, H->tree_part_o,
+                                      H->tree_part_ml, H->tree_plan, H->tree_redo, H->num_cus,
+                                      st));
   else
     HIPCHK(launch_attn_rows((const float*)q, (const float*)w.k_cache, (const float*)w.v_cache, rk,
                             n_rows, c.n_q_heads, c.n_kv_heads, c.head_dim, (float*)o, false, st));
