@@ -386,6 +386,7 @@ int coco_tree_reserve(coco_layer_t H, int32_t max_rows, int32_t max_seqs) {
       HIPCHK(hipMemset(H->tree_ws + o + ml + plan, 0, redo));
       HIPCHK(hipDeviceSynchronize());
     }
+    H->tree_parts = parts;
     H->tree_part_o = (float*)H->tree_ws;
     H->tree_part_ml = (float*)(H->tree_ws + o);
     H->tree_plan = (int32_t*)(H->tree_ws + o + ml);
@@ -440,8 +441,8 @@ int coco_tree_attention(coco_layer_t H, int32_t layer, const void* q, void* o, i
     HIPCHK(launch_tree_attention_bf16((const bf16_t*)q, (const bf16_t*)w.k_cache,
                                       (const bf16_t*)w.v_cache, rk, n_rows, c.n_q_heads,
                                       c.n_kv_heads, (bf16_t*)o, false, H->tree_part_o,
-                                      H->tree_part_ml, H->tree_plan, H->tree_redo, H->num_cus,
-                                      st));
+                                      H->tree_part_ml, H->tree_parts, H->tree_plan, H->tree_redo,
+                                      H->num_cus, st));
   else
     HIPCHK(launch_attn_rows((const float*)q, (const float*)w.k_cache, (const float*)w.v_cache, rk,
                             n_rows, c.n_q_heads, c.n_kv_heads, c.head_dim, (float*)o, false, st));

@@ -97,6 +97,7 @@ struct coco_layer {
   char *tree_ws = nullptr, *sparse_keys = nullptr;
   size_t tree_bytes = 0, sparse_keys_bytes = 0;
   float *tree_part_o = nullptr, *tree_part_ml = nullptr;
+  int64_t tree_parts = 0;
   int32_t *tree_plan = nullptr, *tree_redo = nullptr;
   std::vector<char*> extra;
 };

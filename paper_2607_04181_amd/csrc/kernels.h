@@ -342,15 +342,15 @@ hipError_t launch_attn_rows(const T* q, const T* k_cache, const T* v_cache, cons
 // Tree rows of bf16 handles (hd 128). The keys of a sequence are split into
 // at most kTreeSplitsFew parts where it has at most 128 columns (nodes times
 // query heads of a group), else kTreeSplits; part_o [column parts][128] and
-// part_ml [column parts][2] hold tree_column_parts of them, plan [n_seqs][2];
+// part_ml [column parts][2] hold part_cap = tree_column_parts, plan [n_seqs][2];
 // redo [n_rows][Hq] must be zero and is left so.
 constexpr int kTreeSplitsFew = 32, kTreeSplits = 16;
 int64_t tree_column_parts(int64_t max_rows, int64_t max_seqs, int Hq, int Hkv, int max_blocks);
 hipError_t launch_tree_attention_bf16(const uint16_t* q, const uint16_t* k_cache,
                                       const uint16_t* v_cache, const RowKeys& rk, int n_rows,
                                       int Hq, int Hkv, uint16_t* o, bool tiled, float* part_o,
-                                      float* part_ml, int32_t* plan, int32_t* redo,
-                                      int num_cus, hipStream_t st);
+                                      float* part_ml, int64_t part_cap, int32_t* plan,
+                                      int32_t* redo, int num_cus, hipStream_t st);
 
 // ---------------------------------------------------------- block summaries
 // summary [block][Hkv][2][hd] and scales [block][Hkv] of the blocks that hold

@@ -12,11 +12,12 @@
 // operands of two products (dims h and h + 16) for 16 keys.
 //
 // What is read: keys and values once per column tile, so a tile takes as many
-// columns as its eight waves hold: 32 RG columns with RG in {1, 2, 4, 8} groups,
-// the other 8 / RG waves of a group taking other keys. RG = 1 (a token, a short
-// chain) is bound by the cache's bytes: each wave streams its own keys into
-// registers. Above, the eight waves share keys through LDS, 128 at a time,
-// double-buffered; from RG = 4 on matrix products and softmax bound it.
+// columns as its eight waves hold: 32 RG columns with RG in {2, 4, 8} groups, the
+// other 8 / RG waves of a group taking other keys. The waves share the keys
+// through LDS, 128 at a time, double-buffered. Few columns are bound by the
+// cache's bytes; from RG = 4 on matrix products and softmax bound it. (A path
+// of its own for up to 32 columns, keys straight to registers, cost registers
+// the other one needs and was no faster.)
 //
 // The keys of a sequence are split into parts (tree_plan) that depend on its
 // own length and columns only, merged by a second kernel in order: a row's
@@ -46,31 +47,25 @@ constexpr int kXCDs = 8;
 constexpr float kLazy = 8.f;  // log2 units a running max may lag
 
 // Column tiles of a sequence with `groups` 32-column groups: full tiles of 8,
-// then the rest in powers of two (3 as one tile of 4, 7 of 8: an idle wave in
-// each costs less than reading the keys again).
+// then the rest as tiles of 2, 4 (3 groups, or 5 with a 2), 6 as 4 and 2, 7 as 8:
+// an idle group costs less than reading the keys again.
 __device__ __forceinline__ int tree_tiles(int groups) {
   const int r = groups & 7;
-  return (groups >> 3) + (r == 3 || r == 7 ? 1 : __popc(r));
+  return (groups >> 3) + (r == 0 ? 0 : r == 5 || r == 6 ? 2 : 1);
 }
 // Tile t's first group, and its width.
 __device__ __forceinline__ int tree_tile(int groups, int t, int* rg) {
-  const int full = groups >> 3;
+  const int full = groups >> 3, r = groups & 7;
   if (t < full) {
     *rg = 8;
     return 8 * t;
   }
-  const int r = groups & 7;
-  if (r == 3 || r == 7) {
-    *rg = r + 1;
-    return 8 * full;
+  if (t > full) {
+    *rg = 2;
+    return 8 * full + 4;
   }
-  const int big = r & 4 ? 4 : r & 2 ? 2 : 1;
-  if (t == full) {
-    *rg = big;
-    return 8 * full;
-  }
-  *rg = r - big;  // r in {5, 6}: one tile more
-  return 8 * full + big;
+  *rg = r == 7 ? 8 : r >= 3 ? 4 : 2;
+  return 8 * full;
 }
 
 struct TreeSeq {
@@ -79,22 +74,33 @@ struct TreeSeq {
   int splits, part; // parts of the keys, and keys of one
 };
 
-// Parts of the keys. Few columns: parts of 256 keys, so that one sequence
-// fills the chip; more columns make a part's partial result (512 bytes per
-// column) dear next to its keys (512 bytes each), so parts grow with them.
+// Keys of one of the parts that `len` keys of a sequence with `cols` columns
+// are split into. Few columns: one stage (128 keys), so that one sequence fills
+// the chip; more columns make a part's partial result (512 bytes per column)
+// dear next to its keys (512 bytes each), so parts grow with them. The number
+// of parts falls with cols and grows with len (tree_column_parts counts on it).
+__host__ __device__ __forceinline__ int tree_part(int64_t cols, int len) {
+  const int least = cols <= 16 ? 128 : cols <= 64 ? 512 : 1024;
+  const int most = cols <= 128 ? kTreeSplitsFew : kTreeSplits;
+  int want = (len + least - 1) / least;
+  want = want < 1 ? 1 : want > most ? most : want;
+  const int part = ((len + want - 1) / want + 127) / 128 * 128;
+  return part > 128 ? part : 128;
+}
+__host__ __device__ __forceinline__ int tree_splits(int64_t cols, int len) {
+  const int part = tree_part(cols, len);
+  return len > part ? (len + part - 1) / part : 1;
+}
+
 __device__ __forceinline__ TreeSeq tree_plan(const int32_t* seq_starts, const int32_t* ctx_lens,
                                              int s, int G, int max_blocks) {
   TreeSeq t;
   t.nodes = max(seq_starts[s + 1] - seq_starts[s], 0);
   t.len = min(max(ctx_lens[s], 0), max_blocks * kBlockTokens);
   const int64_t cols = (int64_t)t.nodes * G;
-  const int groups = (int)((cols + kCols - 1) / kCols);
-  t.tiles = tree_tiles(groups);
-  const int least = cols <= 16 ? 256 : cols <= 64 ? 512 : 1024;
-  const int most = cols <= 128 ? kTreeSplitsFew : kTreeSplits;
-  const int want = min(most, max(1, (t.len + least - 1) / least));
-  t.part = max(((t.len + want - 1) / want + 255) & ~255, 256);
-  t.splits = max(1, (t.len + t.part - 1) / t.part);
+  t.tiles = tree_tiles((int)((cols + kCols - 1) / kCols));
+  t.part = tree_part(cols, t.len);
+  t.splits = tree_splits(cols, t.len);
   return t;
 }
 
@@ -132,9 +138,21 @@ struct TreeArgs {
   bool tiled;
   float* part_o;    // [column part][HD]
   float* part_ml;   // [column part][2]
+  int64_t part_cap; // column parts they hold
   int32_t* plan;    // [n_seqs][2]: first column part, parts
   int32_t* redo;    // [rows * Hq]: rows to compute again (zero between calls)
 };
+
+// Where a lane's run of four dims goes that starts at value v (a multiple of 4)
+// of its 64: dims D + 4 hf .. + 3 with D from v alone; and, in tile order, the
+// run's place from its head's first.
+__device__ __forceinline__ int run_dim(int v) {
+  return 64 * (v >> 5) + 16 * (v >> 4 & 1) + 32 * (v >> 3 & 1) + 8 * (v >> 2 & 1);
+}
+__device__ __forceinline__ int run_tiled(int v) {
+  const int d = run_dim(v);
+  return (d >> 5) * 512 + (d >> 3 & 3) * 128;
+}
 
 // Key fragments of two blocks: step s holds dims 16 s + 8 hf .. + 7 of key m.
 // kb[i]: the tile of block i.
@@ -157,13 +175,8 @@ __device__ __forceinline__ f32x16_t tree_scores(const u32x4_t kf[8], const bf16x
 }
 
 // Softmax step of 32 keys; p: the probabilities as operands of two products.
-__device__ __forceinline__ void tree_softmax(Cols& c, f32x16_t s, bool masked, uint32_t seen,
-                                             float scale_log2, u32x4_t p[2]) {
-  if (masked) {
-#pragma unroll
-    for (int r = 0; r < 16; ++r)
-      s[r] = (seen >> (8 * (r / 4) + r % 4) & 1) ? s[r] : -INFINITY;
-  }
+__device__ __forceinline__ void tree_softmax(Cols& c, const f32x16_t& s, float scale_log2,
+                                             u32x4_t p[2]) {
   float mx = s[0];
 #pragma unroll
   for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
@@ -214,13 +227,16 @@ __device__ __forceinline__ void tree_pv(Cols& c, const u32x4_t v[2][2][2], const
     }
 }
 
-// The same for keys among or behind the nodes. Those from `left` on are dropped
-// (their slots may hold anything). A product with a probability of 0 would let
-// a non-finite value of a node reach the columns that do not see it: such
-// elements are left out, and the result is whether this lane's column sees one
-// (the merge kernel then computes its row again, key by key).
-__device__ __forceinline__ bool tree_pv_masked(Cols& c, u32x4_t v[2][2][2], const u32x4_t p[2],
-                                               int hf, int left, uint32_t seen) {
+// Keys among or behind the nodes: scores that the column does not see count as
+// -inf, and values from key `left` on are dropped (their slots may hold
+// anything). A product with a probability of 0 would let a non-finite value of a
+// node reach the columns that do not see it: such elements are left out, and the
+// result is whether this lane's column sees one (the merge kernel then computes
+// its row again, key by key).
+__device__ __forceinline__ bool tree_mask(f32x16_t& s, u32x4_t v[2][2][2], int hf, int left,
+                                          uint32_t seen) {
+#pragma unroll
+  for (int r = 0; r < 16; ++r) s[r] = (seen >> (8 * (r / 4) + r % 4) & 1) ? s[r] : -INFINITY;
   uint32_t odd = 0;  // bit 8 j + 4 u + k: key 16 j + 8 u + 4 hf + k, in any of this lane's dims
 #pragma unroll
   for (int j = 0; j < 2; ++j)
@@ -239,7 +255,6 @@ __device__ __forceinline__ bool tree_pv_masked(Cols& c, u32x4_t v[2][2][2], cons
           odd |= ((lo ? 1u : 0u) | (hi ? 2u : 0u)) << (8 * j + 4 * u + 2 * (e & 1));
           v[j][d][u][e] = w;
         }
-  tree_pv(c, v, p);
   if (__ballot(odd != 0) == 0) return false;
   uint32_t mine = 0;  // this half's keys of the chunk that hold one in any lane's dims
 #pragma unroll 1
@@ -312,6 +327,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_kernel(TreeArgs a)
   if (tid == 0) items_s[rk.n_seqs] = carry_i;
   __syncthreads();
   const int total = carry_i;
+  if (carry_b > a.part_cap) return;  // more rows than the call named: no room for their parts
 
   // Consecutive items on one XCD (blockIdx % 8), so that the column tiles of
   // the same keys read them from its L2.
@@ -365,98 +381,54 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_kernel(TreeArgs a)
     for (int i = 0; i < 4; ++i) c.acc[i] = f32x16_t{};
 
     // Softmax and values of the 32 keys from tok0 on.
-    auto finish = [&](f32x16_t sc, u32x4_t v[2][2][2], int tok0) {
-      u32x4_t p[2];
-      if (tok0 + kChunk <= prefix) {
-        tree_softmax(c, sc, false, 0, a.scale_log2, p);
-        tree_pv(c, v, p);
-      } else {
+    auto finish = [&](f32x16_t& sc, u32x4_t v[2][2][2], int tok0) {
+      if (tok0 + kChunk > prefix) {
         // Bit k: key tok0 + 4 hf + k (a lane's keys are 8 q + 4 hf + r).
         const uint32_t seen = tree_bits32(mask, rk.words, ts.nodes, tok0 - prefix) >> (4 * hf);
-        tree_softmax(c, sc, true, seen, a.scale_log2, p);
-        if (tree_pv_masked(c, v, p, hf, t1 - tok0, seen)) a.redo[(int64_t)row * a.Hq + head] = 1;
+        if (tree_mask(sc, v, hf, t1 - tok0, seen)) a.redo[(int64_t)row * a.Hq + head] = 1;
       }
+      u32x4_t p[2];
+      tree_softmax(c, sc, a.scale_log2, p);
+      tree_pv(c, v, p);
     };
 
-    if (rgs == 1) {
-      // Own keys, straight to registers: the next step's keys are on their way
-      // while this one's values are used, and the other way round.
-      const int steps = (t1 - t0 + kChunk * kWaves - 1) / (kChunk * kWaves);
-      u32x4_t kf[8], vf[2][2][2];
-      int64_t pb[2];
-      auto blocks = [&](int st) {
-        const int b = t0 / kBlockTokens + 2 * (st * kWaves + wv);
-        pb[0] = block_of(b);
-        pb[1] = block_of(b + 1);
-      };
-      auto load_k = [&]() {
-        const bf16_t* kb = a.k_cache + ((lane & 16 ? pb[1] : pb[0]) * a.Hkv + g) * kTile;
+    const int stages = (t1 - t0 + kStBlk * kBlockTokens - 1) / (kStBlk * kBlockTokens);
+    auto issue = [&](int st) {
+      const int64_t b = block_of(t0 / kBlockTokens + st * kStBlk + wv);
+      bf16_t* dst = kv + ((st & 1) * kStBlk + wv) * 2 * kTile;
+      const bf16_t* src[2] = {a.k_cache + (b * a.Hkv + g) * kTile + lane * 8,
+                              a.v_cache + (b * a.Hkv + g) * kTile + lane * 8};
 #pragma unroll
-        for (int i = 0; i < 8; ++i) kf[i] = *(const u32x4_t*)(kb + k_frag_off(lane, i));
-      };
-      auto load_v = [&](const int64_t b[2]) {
+      for (int w = 0; w < 2; ++w)
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const bf16_t* vb = a.v_cache + (b[j] * a.Hkv + g) * kTile;
+        for (int pc = 0; pc < 4; ++pc)
+          __builtin_amdgcn_global_load_lds(src[w] + pc * 512,
+                                           (lds_void_t*)(dst + w * kTile + pc * 512), 16, 0, 0);
+    };
+    issue(0);
+    __syncthreads();
+    for (int st = 0; st < stages; ++st) {
+      if (st + 1 < stages) issue(st + 1);
+      for (int ch = ks; ch < kStBlk / 2; ch += kss) {
+        const int tok0 = t0 + (st * kStBlk + 2 * ch) * kBlockTokens;
+        if (idle || tok0 >= t1) continue;
+        const bf16_t* kb = kv + ((st & 1) * kStBlk + 2 * ch) * 2 * kTile;
+        const bf16_t* kl = kb + (lane & 16 ? 2 * kTile : 0);
+        u32x4_t kf[8], vf[2][2][2];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) kf[i] = *(const u32x4_t*)(kl + k_frag_off(lane, i));
+        f32x16_t sc = tree_scores(kf, qf);
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
 #pragma unroll
           for (int d = 0; d < 2; ++d)
 #pragma unroll
             for (int u = 0; u < 2; ++u)
-              vf[j][d][u] = *(const u32x4_t*)(vb + v_frag_off(lane, d) + u * 256);
-        }
-      };
-      blocks(0);
-      load_k();
-      load_v(pb);
-      blocks(1);
-      for (int st = 0; st < steps; ++st) {
-        const f32x16_t sc = tree_scores(kf, qf);
-        load_k();
-        const int64_t nb[2] = {pb[0], pb[1]};
-        blocks(st + 2);
-        const int tok0 = t0 + (st * kWaves + wv) * kChunk;
-        if (tok0 < t1) finish(sc, vf, tok0);
-        load_v(nb);
+              vf[j][d][u] = *(const u32x4_t*)(kb + (2 * j + 1) * kTile + v_frag_off(lane, d) +
+                                              u * 256);
+        finish(sc, vf, tok0);
       }
-    } else {
-      const int stages = (t1 - t0 + kStBlk * kBlockTokens - 1) / (kStBlk * kBlockTokens);
-      auto issue = [&](int st) {
-        const int64_t b = block_of(t0 / kBlockTokens + st * kStBlk + wv);
-        bf16_t* dst = kv + ((st & 1) * kStBlk + wv) * 2 * kTile;
-        const bf16_t* src[2] = {a.k_cache + (b * a.Hkv + g) * kTile + lane * 8,
-                                a.v_cache + (b * a.Hkv + g) * kTile + lane * 8};
-#pragma unroll
-        for (int w = 0; w < 2; ++w)
-#pragma unroll
-          for (int pc = 0; pc < 4; ++pc)
-            __builtin_amdgcn_global_load_lds(src[w] + pc * 512,
-                                             (lds_void_t*)(dst + w * kTile + pc * 512), 16, 0, 0);
-      };
-      issue(0);
-      __syncthreads();
-      for (int st = 0; st < stages; ++st) {
-        if (st + 1 < stages) issue(st + 1);
-        for (int ch = ks; ch < kStBlk / 2; ch += kss) {
-          const int tok0 = t0 + (st * kStBlk + 2 * ch) * kBlockTokens;
-          if (idle || tok0 >= t1) continue;
-          const bf16_t* kb = kv + ((st & 1) * kStBlk + 2 * ch) * 2 * kTile;
-          const bf16_t* kl = kb + (lane & 16 ? 2 * kTile : 0);
-          u32x4_t kf[8], vf[2][2][2];
-#pragma unroll
-          for (int i = 0; i < 8; ++i) kf[i] = *(const u32x4_t*)(kl + k_frag_off(lane, i));
-          const f32x16_t sc = tree_scores(kf, qf);
-#pragma unroll
-          for (int j = 0; j < 2; ++j)
-#pragma unroll
-            for (int d = 0; d < 2; ++d)
-#pragma unroll
-              for (int u = 0; u < 2; ++u)
-                vf[j][d][u] = *(const u32x4_t*)(kb + (2 * j + 1) * kTile + v_frag_off(lane, d) +
-                                                u * 256);
-          finish(sc, vf, tok0);
-        }
-        __syncthreads();  // stage st + 1 landed; stage st's buffer is free
-      }
+      __syncthreads();  // stage st + 1 landed; stage st's buffer is free
     }
 
     // Merge the key sets of each column group: weights from the sets' maxima,
@@ -467,6 +439,12 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_kernel(TreeArgs a)
       c.l = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
     }
     float M = c.m, L = c.l;
+    // Where this lane's column goes: a part, or the output row.
+    const bool live = !idle && col < cols;
+    const int64_t idx = base_s[s] + ((int64_t)(row - row0) * a.Hq + head) * ts.splits + sp;
+    float* const part = ts.splits > 1 ? a.part_o + idx * HD + 4 * hf : nullptr;
+    bf16_t* const out = a.o + 4 * hf + (a.tiled ? tile_off(row, head * HD, a.Hq * HD)
+                                                : ((int64_t)row * a.Hq + head) * HD);
     float* xs = reinterpret_cast<float*>(kv);
     if (kss > 1) {
       __syncthreads();  // every wave is done with kv (register path: with the last merge)
@@ -493,58 +471,42 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_kernel(TreeArgs a)
         }
       }
       const int per_w = 64 / kss;
-      const bool live = !idle && col < cols;
-      const int64_t idx = base_s[s] + ((int64_t)(row - row0) * a.Hq + head) * ts.splits + sp;
+      const float inv = L == 0.f ? 0.f : 1.0f / L;
       for (int v4 = ks * per_w; v4 < (ks + 1) * per_w; v4 += 4) {
         f32x4_t y = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int k = 0; k < kWaves; ++k)
           if (k < kss) {
+            const float* w = xs + ((k * rgs + rg) * 64 + v4) * 64 + lane;
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
-              y[r] = fmaf(f[k], xs[((k * rgs + rg) * 64 + v4 + r) * 64 + lane], y[r]);
+            for (int r = 0; r < 4; ++r) y[r] = fmaf(f[k], w[r * 64], y[r]);
           }
-        const int i = v4 >> 4, m = 8 * ((v4 & 15) >> 2) + 4 * hf;
-        const int dim = 32 * (2 * (i >> 1) + m / 16) + 16 * (i & 1) + m % 16;
         if (!live) continue;
-        if (ts.splits > 1) {
-          *(f32x4_t*)(a.part_o + idx * HD + dim) = y;
-        } else {
-          const float inv = L == 0.f ? 0.f : 1.0f / L;
-          const int cc = head * HD + dim;
-          bf16_t* out = a.o + (a.tiled ? tile_off(row, cc, a.Hq * HD) : (int64_t)row * a.Hq * HD + cc);
-          store4(out, y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv);
-        }
-      }
-      if (live && ts.splits > 1 && ks == 0 && hf == 0) {
-        a.part_ml[2 * idx] = M;
-        a.part_ml[2 * idx + 1] = L;
+        if (part)
+          *(f32x4_t*)(part + run_dim(v4)) = y;
+        else
+          store4(out + (a.tiled ? run_tiled(v4) : run_dim(v4)), y[0] * inv, y[1] * inv, y[2] * inv,
+                 y[3] * inv);
       }
       __syncthreads();  // LDS is free for the next item
-    } else if (!idle && col < cols) {
-      const int64_t idx = base_s[s] + ((int64_t)(row - row0) * a.Hq + head) * ts.splits + sp;
+    } else if (live) {
       const float inv = L == 0.f ? 0.f : 1.0f / L;
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int r = 0; r < 16; r += 4) {
-          const int m = 2 * r + 4 * hf;
-          const int dim = 32 * (2 * (i >> 1) + m / 16) + 16 * (i & 1) + m % 16;
-          if (ts.splits > 1) {
-            *(f32x4_t*)(a.part_o + idx * HD + dim) =
-                f32x4_t{c.acc[i][r], c.acc[i][r + 1], c.acc[i][r + 2], c.acc[i][r + 3]};
-          } else {
-            const int cc = head * HD + dim;
-            bf16_t* out =
-                a.o + (a.tiled ? tile_off(row, cc, a.Hq * HD) : (int64_t)row * a.Hq * HD + cc);
-            store4(out, c.acc[i][r] * inv, c.acc[i][r + 1] * inv, c.acc[i][r + 2] * inv,
-                   c.acc[i][r + 3] * inv);
-          }
+          const f32x4_t y = {c.acc[i][r], c.acc[i][r + 1], c.acc[i][r + 2], c.acc[i][r + 3]};
+          const int v4 = 16 * i + r;
+          if (part)
+            *(f32x4_t*)(part + run_dim(v4)) = y;
+          else
+            store4(out + (a.tiled ? run_tiled(v4) : run_dim(v4)), y[0] * inv, y[1] * inv,
+                   y[2] * inv, y[3] * inv);
         }
-      if (ts.splits > 1 && hf == 0) {
-        a.part_ml[2 * idx] = M;
-        a.part_ml[2 * idx + 1] = L;
-      }
+    }
+    if (part && live && ks == 0 && hf == 0) {
+      a.part_ml[2 * idx] = M;
+      a.part_ml[2 * idx + 1] = L;
     }
   }
 }
@@ -618,20 +580,25 @@ __global__ __launch_bounds__(256) void tree_combine_kernel(TreeArgs a) {
 
 }  // namespace
 
-// A sequence with C = nodes * G columns per key/value head has at most
-// kTreeSplitsFew parts where C <= 128, else kTreeSplits.
+// The most that any call of so many rows and sequences can need. A sequence of
+// len keys has tree_splits(cols, len) parts: at most `few` of kTreeSplitsFew where
+// it has up to 128 columns per key/value head, `many` above. (Part sizes are
+// rounded up to 128 keys, which is why a shorter sequence may have more parts
+// than a longer one: the bounds are those of any length up to the longest.)
 int64_t tree_column_parts(int64_t max_rows, int64_t max_seqs, int Hq, int Hkv, int max_blocks) {
   const int64_t len = (int64_t)max_blocks * kBlockTokens;
-  auto cap = [&](int64_t most) { return len / 256 + 1 < most ? len / 256 + 1 : most; };
-  const int64_t few = max_seqs * Hkv * 128 < max_rows * Hq ? max_seqs * Hkv * 128 : max_rows * Hq;
-  return few * cap(kTreeSplitsFew) + (max_rows * Hq - few) * cap(kTreeSplits);
+  // A part holds at least 128 keys (few columns), 1024 before rounding (many).
+  const int64_t few = len / 128 + 1 < kTreeSplitsFew ? len / 128 + 1 : kTreeSplitsFew;
+  const int64_t many = len / 1024 + 1 < kTreeSplits ? len / 1024 + 1 : kTreeSplits;
+  const int64_t cols = max_seqs * Hkv * 128 < max_rows * Hq ? max_seqs * Hkv * 128 : max_rows * Hq;
+  return cols * few + (max_rows * Hq - cols) * many;
 }
 
 hipError_t launch_tree_attention_bf16(const uint16_t* q, const uint16_t* k_cache,
                                       const uint16_t* v_cache, const RowKeys& rk, int n_rows,
                                       int Hq, int Hkv, uint16_t* o, bool tiled, float* part_o,
-                                      float* part_ml, int32_t* plan, int32_t* redo,
-                                      int num_cus, hipStream_t st) {
+                                      float* part_ml, int64_t part_cap, int32_t* plan,
+                                      int32_t* redo, int num_cus, hipStream_t st) {
   if (n_rows <= 0) return hipSuccess;
   TreeArgs a;
   a.q = q;
@@ -645,6 +612,7 @@ hipError_t launch_tree_attention_bf16(const uint16_t* q, const uint16_t* k_cache
   a.tiled = tiled;
   a.part_o = part_o;
   a.part_ml = part_ml;
+  a.part_cap = part_cap;
   a.plan = plan;
   a.redo = redo;
   // One workgroup per CU (its LDS); batches of more than kMaxSeqs sequences
