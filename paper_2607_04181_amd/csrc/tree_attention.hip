@@ -1,8 +1,8 @@
 // Attention of trees of drafted tokens over the paged cache (bf16, hd = 128).
 //
 // The columns of a sequence and key/value head are its nodes times the group's
-// query heads, C = N G (column c: node c / G, head c % G). Every wave owns 32
-// of them and walks 32 keys (two blocks) at a time:
+// query heads, C = N G (column c: node c / G, head c % G). Every wave owns 32 of
+// them and walks 32 keys (two blocks) at a time:
 //   S^T[32 keys][32 cols] = K[32][hd] Q^T[hd][32]    8 x mfma 32x32x16
 //   online softmax per column, 16 keys in each of its two lanes
 //   O^T[hd][32 cols] += V^T[hd][32] P^T[32][32]      8 x mfma 32x32x16
@@ -11,15 +11,16 @@
 // of four keys, two dims side by side, so that two 16-byte reads give the
 // operands of two products (dims h and h + 16) for 16 keys.
 //
-// What is read: keys and values once per column tile, so a tile takes as many
-// columns as its eight waves hold: 32 RG columns with RG in {2, 4, 8} groups, the
-// other 8 / RG waves of a group taking other keys. The waves share the keys
-// through LDS, 128 at a time, double-buffered. Few columns are bound by the
-// cache's bytes; from RG = 4 on matrix products and softmax bound it. (A path
-// of its own for up to 32 columns, keys straight to registers, cost registers
-// the other one needs and was no faster.)
+// A workgroup is eight waves that take 64, 128 or 256 columns (RG = 2, 4, 8
+// column groups) and KS = 8 / RG sets of keys; one workgroup per CU. Keys and
+// values go through LDS in stages of 128 keys, double-buffered, one barrier
+// each. Within a stage a wave takes its 4 / KS steps of 32 keys alone: the next
+// step's key operands are read while this one's go through softmax, so that of
+// the two waves of a SIMD one can multiply while the other does vector work.
+// Few columns are bound by the cache's bytes, many by products and softmax,
+// which take about as long each.
 //
-// The keys of a sequence are split into parts (tree_plan) that depend on its
+// The keys of a sequence are split into parts (tree_part) that depend on its
 // own length and columns only, merged by a second kernel in order: a row's
 // bits do not depend on the rest of the call.
 #include <math.h>
@@ -41,14 +42,14 @@ constexpr int kThreads = kWaves * kWave;
 constexpr int kCols = 32;   // columns of a wave
 constexpr int kChunk = 32;  // keys of a step
 constexpr int kTile = kBlockTokens * HD;
-constexpr int kStBlk = 8;   // blocks of a stage (128 keys)
+constexpr int kStBlk = 8;   // blocks of a stage
+constexpr int kStKeys = kStBlk * kBlockTokens;
 constexpr int kMaxSeqs = 1024;  // sequences of a launch
-constexpr int kXCDs = 8;
 constexpr float kLazy = 8.f;  // log2 units a running max may lag
 
 // Column tiles of a sequence with `groups` 32-column groups: full tiles of 8,
-// then the rest as tiles of 2, 4 (3 groups, or 5 with a 2), 6 as 4 and 2, 7 as 8:
-// an idle group costs less than reading the keys again.
+// then the rest as a tile of 2, of 4 (3 or 4 groups), of 4 and 2 (5, 6) or of 8
+// (7): an idle group costs less than reading the keys again.
 __device__ __forceinline__ int tree_tiles(int groups) {
   const int r = groups & 7;
   return (groups >> 3) + (r == 0 ? 0 : r == 5 || r == 6 ? 2 : 1);
@@ -56,16 +57,8 @@ __device__ __forceinline__ int tree_tiles(int groups) {
 // Tile t's first group, and its width.
 __device__ __forceinline__ int tree_tile(int groups, int t, int* rg) {
   const int full = groups >> 3, r = groups & 7;
-  if (t < full) {
-    *rg = 8;
-    return 8 * t;
-  }
-  if (t > full) {
-    *rg = 2;
-    return 8 * full + 4;
-  }
-  *rg = r == 7 ? 8 : r >= 3 ? 4 : 2;
-  return 8 * full;
+  *rg = t < full || (t == full && r == 7) ? 8 : t == full && r >= 3 ? 4 : 2;
+  return t <= full ? 8 * t : 8 * full + 4;
 }
 
 struct TreeSeq {
@@ -120,13 +113,6 @@ __device__ __forceinline__ uint32_t tree_bits32(const uint64_t* mask, int words,
   return (uint32_t)v;
 }
 
-// One wave's columns: running softmax and O^T. acc[2 p + y]: dims 32 (2 p +
-// m / 16) + 16 y + m % 16, m = 8 (r / 4) + 4 hf + r % 4.
-struct Cols {
-  float m, l;
-  f32x16_t acc[4];
-};
-
 struct TreeArgs {
   const bf16_t* q;
   const bf16_t* k_cache;
@@ -140,6 +126,7 @@ struct TreeArgs {
   float* part_ml;   // [column part][2]
   int64_t part_cap; // column parts they hold
   int32_t* plan;    // [n_seqs][2]: first column part, parts
+  int32_t* drawn;   // items drawn (zero between calls)
   int32_t* redo;    // [rows * Hq]: rows to compute again (zero between calls)
 };
 
@@ -165,46 +152,12 @@ __device__ __forceinline__ int v_frag_off(int lane, int p) {
   return ((2 * p + ((lane >> 4) & 1)) * 64 + hf * 16 + (lane & 15)) * 8;
 }
 
-__device__ __forceinline__ f32x16_t tree_scores(const u32x4_t kf[8], const bf16x8_t qf[8]) {
-  f32x16_t s = {};
+// Largest of 16 values (NaN loses).
+__device__ __forceinline__ float max16(const f32x16_t& s) {
+  float m = fmaxf(fmaxf(s[0], s[1]), s[2]);
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
-    s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kf[i]), qf[i], s, 0,
-                                                0, 0);
-  return s;
-}
-
-// Softmax step of 32 keys; p: the probabilities as operands of two products.
-__device__ __forceinline__ void tree_softmax(Cols& c, const f32x16_t& s, float scale_log2,
-                                             u32x4_t p[2]) {
-  float mx = s[0];
-#pragma unroll
-  for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
-  const auto sw =
-      __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
-  mx = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * scale_log2;
-  // The running max moves only when a step exceeds it by kLazy.
-  const float m_new = mx > c.m + kLazy ? mx : c.m;
-  const float m_ref = m_new == -INFINITY ? 0.f : m_new;
-  const float alpha = __builtin_amdgcn_exp2f(c.m - m_ref);
-  float pr[16];
-#pragma unroll
-  for (int r = 0; r < 16; ++r)
-    pr[r] = __builtin_amdgcn_exp2f(fmaf(s[r], scale_log2, -m_ref));
-  float ls = 0.f;
-#pragma unroll
-  for (int r = 0; r < 16; r += 4) ls += (pr[r] + pr[r + 1]) + (pr[r + 2] + pr[r + 3]);
-  if (__ballot(m_new != c.m) != 0) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) c.acc[i] *= alpha;
-    c.l *= alpha;
-  }
-  c.m = m_new;
-  c.l += ls;
-#pragma unroll
-  for (int j = 0; j < 2; ++j)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) p[j][e] = pack_bf16x2(pr[8 * j + 2 * e], pr[8 * j + 2 * e + 1]);
+  for (int r = 3; r + 1 < 16; r += 2) m = fmaxf(fmaxf(m, s[r]), s[r + 1]);
+  return fmaxf(m, s[15]);
 }
 
 __device__ __forceinline__ f32x16_t pv_step(uint32_t a0, uint32_t a1, uint32_t b0, uint32_t b1,
@@ -214,29 +167,18 @@ __device__ __forceinline__ f32x16_t pv_step(uint32_t a0, uint32_t a1, uint32_t b
       0, 0, 0);
 }
 
-// O^T += V^T P^T. v[j][p]: the two chunks (keys 4 hf .. and 8 + 4 hf ..) of
-// block j, dim pair p.
-__device__ __forceinline__ void tree_pv(Cols& c, const u32x4_t v[2][2][2], const u32x4_t p[2]) {
-#pragma unroll
-  for (int j = 0; j < 2; ++j)
-#pragma unroll
-    for (int d = 0; d < 2; ++d) {
-      const u32x4_t a = v[j][d][0], b = v[j][d][1];
-      c.acc[2 * d] = pv_step(a.x, a.y, b.x, b.y, p[j], c.acc[2 * d]);
-      c.acc[2 * d + 1] = pv_step(a.z, a.w, b.z, b.w, p[j], c.acc[2 * d + 1]);
-    }
-}
-
-// Keys among or behind the nodes: scores that the column does not see count as
-// -inf, and values from key `left` on are dropped (their slots may hold
-// anything). A product with a probability of 0 would let a non-finite value of a
-// node reach the columns that do not see it: such elements are left out, and the
-// result is whether this lane's column sees one (the merge kernel then computes
-// its row again, key by key).
-__device__ __forceinline__ bool tree_mask(f32x16_t& s, u32x4_t v[2][2][2], int hf, int left,
-                                          uint32_t seen) {
+// Scores of keys among or behind the nodes: -inf where the column does not see
+// the key. Bit k of seen: key 4 hf + k of the 32 (a lane holds 8 q + 4 hf + r).
+__device__ __forceinline__ void mask_scores(f32x16_t& s, uint32_t seen) {
 #pragma unroll
   for (int r = 0; r < 16; ++r) s[r] = (seen >> (8 * (r / 4) + r % 4) & 1) ? s[r] : -INFINITY;
+}
+
+// Values of such keys: those from key `left` on are dropped (their slots may
+// hold anything). A product with a probability of 0 would let a non-finite value
+// of a node reach the columns that do not see it: such elements are left out.
+// Returns the keys (as bits of `seen`) that held one.
+__device__ __forceinline__ uint32_t mask_values(u32x4_t v[2][2][2], int hf, int left) {
   uint32_t odd = 0;  // bit 8 j + 4 u + k: key 16 j + 8 u + 4 hf + k, in any of this lane's dims
 #pragma unroll
   for (int j = 0; j < 2; ++j)
@@ -255,23 +197,195 @@ __device__ __forceinline__ bool tree_mask(f32x16_t& s, u32x4_t v[2][2][2], int h
           odd |= ((lo ? 1u : 0u) | (hi ? 2u : 0u)) << (8 * j + 4 * u + 2 * (e & 1));
           v[j][d][u][e] = w;
         }
-  if (__ballot(odd != 0) == 0) return false;
-  uint32_t mine = 0;  // this half's keys of the chunk that hold one in any lane's dims
+  if (__ballot(odd != 0) == 0) return 0;
+  uint32_t mine = 0;  // this half of the lanes' keys
 #pragma unroll 1
   for (int i = 0; i < 16; ++i) {
     const uint64_t any = __ballot(odd >> i & 1);
     const uint32_t here = hf == 0 ? (uint32_t)any : (uint32_t)(any >> 32);
-    mine |= (here != 0 ? 1u : 0u) << (8 * (i >> 2) + (i & 3));  // its place in `seen`
+    mine |= (here != 0 ? 1u : 0u) << (8 * (i >> 2) + (i & 3));
   }
-  return (mine & seen) != 0;
+  return mine;
+}
+
+// One wave's columns: running softmax and O^T. acc[2 p + y]: dims 32 (2 p +
+// m / 16) + 16 y + m % 16, m = 8 (r / 4) + 4 hf + r % 4.
+struct Cols {
+  float m, l;
+  f32x16_t acc[4];
+};
+
+// What a wave needs of its item.
+struct Walk {
+  const bf16_t *k_cache, *v_cache;  // of the kv head: block b's tile at b * stride
+  int stride, last_block;
+  const int32_t* bt;
+  const uint64_t* mask;
+  int words, nodes, prefix;
+  int t0, t1;
+  int ks;
+  bool idle;
+  float scale_log2;
+  int32_t* redo;
+};
+
+// The keys t0 .. t1 - 1 in stages of 128, of which this wave takes every
+// KS-th 32. kv: two stages of eight blocks' key and value tiles.
+template <int KS>
+__device__ __forceinline__ void tree_walk(const Walk& w, const bf16x8_t qf[8], bf16_t* kv,
+                                          int lane, int wv, Cols& c) {
+  const int hf = lane >> 5;
+  const int stages = (w.t1 - w.t0 + kStKeys - 1) / kStKeys;
+  const int b_last = (w.t1 - 1) / kBlockTokens;
+
+  // A wave brings one block of each stage (past the last key: the last block
+  // again, whose scores count as unseen). Called with st = 0, 1, ..: the blocks
+  // of 64 stages at a time in a register's lanes.
+  int ids = 0;
+  // (The address goes through a register of its own: the compiler would
+  // otherwise wait for every load in flight before each operand read.)
+  uint32_t kv_at = (uint32_t)(uintptr_t)(lds_void_t*)kv;
+  asm volatile("" : "+s"(kv_at));
+  auto issue = [&](int st) {
+    if ((st & 63) == 0) {
+      const int b = w.t0 / kBlockTokens + (st + lane) * kStBlk + wv;
+      ids = min(max(w.bt[min(b, b_last)], 0), w.last_block);
+    }
+    const int64_t at = (int64_t)__builtin_amdgcn_readlane(ids, st & 63) * w.stride + lane * 8;
+    const uint32_t dst = kv_at + ((st & 1) * kStBlk + wv) * (2 * kTile * 2);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      __builtin_amdgcn_global_load_lds(w.k_cache + at + i * 512,
+                                       (lds_void_t*)(uintptr_t)(dst + i * 1024), 16, 0, 0);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      __builtin_amdgcn_global_load_lds(w.v_cache + at + i * 512,
+                                       (lds_void_t*)(uintptr_t)(dst + kTile * 2 + i * 1024), 16, 0,
+                                       0);
+  };
+  // Operands of the 32 keys of step ch of a stage.
+  auto read_k = [&](int st, int ch, u32x4_t kf[8]) {
+    const bf16_t* kb =
+        kv + ((st & 1) * kStBlk + 2 * ch) * 2 * kTile + (lane & 16 ? 2 * kTile : 0);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) kf[i] = *(const u32x4_t*)(kb + k_frag_off(lane, i));
+  };
+  auto read_v = [&](int st, int ch, u32x4_t vf[2][2][2]) {
+    const bf16_t* vb = kv + ((st & 1) * kStBlk + 2 * ch) * 2 * kTile + kTile;
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int d = 0; d < 2; ++d)
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+          vf[j][d][u] = *(const u32x4_t*)(vb + 2 * j * kTile + v_frag_off(lane, d) + u * 256);
+  };
+  auto scores = [&](const u32x4_t kf[8]) {
+    f32x16_t s = {};
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kf[i]), qf[i], s,
+                                                  0, 0, 0);
+    return s;
+  };
+  // Probabilities of 32 keys as operands of two products. The running max of a
+  // column moves only when a step exceeds it by kLazy.
+  auto softmax = [&](const f32x16_t& s, u32x4_t p[2]) {
+    const float mx = max16(s);
+    const auto sw =
+        __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+    const float top = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * w.scale_log2;
+    const float m_new = top > c.m + kLazy ? top : c.m;
+    if (__ballot(m_new != c.m) != 0) {
+      const float alpha = __builtin_amdgcn_exp2f(c.m - (m_new == -INFINITY ? 0.f : m_new));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) c.acc[i] *= alpha;
+      c.l *= alpha;
+      c.m = m_new;
+    }
+    const float m_ref = c.m == -INFINITY ? 0.f : c.m;
+    float pr[16];
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+      pr[r] = __builtin_amdgcn_exp2f(fmaf(s[r], w.scale_log2, -m_ref));
+    float ls = 0.f;
+#pragma unroll
+    for (int r = 0; r < 16; r += 4) ls += (pr[r] + pr[r + 1]) + (pr[r + 2] + pr[r + 3]);
+    c.l += ls;
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) p[j][e] = pack_bf16x2(pr[8 * j + 2 * e], pr[8 * j + 2 * e + 1]);
+  };
+  auto values = [&](const u32x4_t v[2][2][2], const u32x4_t p[2]) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int d = 0; d < 2; ++d) {
+        const u32x4_t a = v[j][d][0], b = v[j][d][1];
+        c.acc[2 * d] = pv_step(a.x, a.y, b.x, b.y, p[j], c.acc[2 * d]);
+        c.acc[2 * d + 1] = pv_step(a.z, a.w, b.z, b.w, p[j], c.acc[2 * d + 1]);
+      }
+  };
+  auto begin = [&](int st) {
+    wait_vmcnt<0>();  // this wave's block of stage st
+    stage_barrier();  // every wave's; and all are done with stage st - 1
+    if (st + 1 < stages) issue(st + 1);
+  };
+
+  issue(0);
+  if (w.idle) {
+#pragma unroll 1
+    for (int st = 0; st < stages; ++st) begin(st);
+    return;
+  }
+  // Stages that every column sees whole; then the others.
+  const int clear = min(stages, max(w.prefix - w.t0, 0) / kStKeys);
+  int st = 0;
+#pragma unroll 1
+  for (; st < clear; ++st) {
+    begin(st);
+    u32x4_t kf[8];
+    read_k(st, w.ks, kf);
+#pragma unroll 1
+    for (int ch = w.ks; ch < 4; ch += KS) {
+      u32x4_t vf[2][2][2], p[2];
+      const f32x16_t s = scores(kf);
+      read_v(st, ch, vf);
+      if (KS < 4) read_k(st, min(ch + KS, 3), kf);
+      softmax(s, p);
+      values(vf, p);
+    }
+  }
+#pragma unroll 1
+  for (; st < stages; ++st) {
+    begin(st);
+#pragma unroll 1
+    for (int ch = w.ks; ch < 4; ch += KS) {
+      const int tok0 = w.t0 + st * kStKeys + ch * kChunk;
+      if (tok0 >= w.t1) continue;
+      u32x4_t kf[8], vf[2][2][2], p[2];
+      read_k(st, ch, kf);
+      f32x16_t s = scores(kf);
+      read_v(st, ch, vf);
+      if (tok0 + kChunk > w.prefix) {
+        const uint32_t seen =
+            tree_bits32(w.mask, w.words, w.nodes, tok0 - w.prefix) >> (4 * hf);
+        mask_scores(s, seen);
+        if (mask_values(vf, hf, w.t1 - tok0) & seen) *w.redo = 1;
+      }
+      softmax(s, p);
+      values(vf, p);
+    }
+  }
 }
 
 __global__ __launch_bounds__(kThreads, 2) void tree_attention_kernel(TreeArgs a) {
-  // Two stages of eight blocks' key and value tiles; at the end the waves'
-  // O^T ([wave][64 values][64 lanes] floats), 128 KB either way.
+  // Two stages of keys and values; at the end the waves' O^T ([wave][64
+  // values][64 lanes] floats), 128 KB either way.
   __shared__ __attribute__((aligned(16))) bf16_t kv[2 * kStBlk * 2 * kTile];
   __shared__ int items_s[kMaxSeqs + 1], base_s[kMaxSeqs];
-  __shared__ int wsum[2][kWaves];
+  __shared__ int wsum[2][kWaves], next_s[2];
   __shared__ float sm_m[kWaves][kCols], sm_l[kWaves][kCols];
   const RowKeys& rk = a.rk;
   const int tid = threadIdx.x, lane = tid & 63;
@@ -324,169 +438,134 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_kernel(TreeArgs a)
     }
     __syncthreads();
   }
-  if (tid == 0) items_s[rk.n_seqs] = carry_i;
-  __syncthreads();
   const int total = carry_i;
   if (carry_b > a.part_cap) return;  // more rows than the call named: no room for their parts
 
-  // Consecutive items on one XCD (blockIdx % 8), so that the column tiles of
-  // the same keys read them from its L2.
-  const int grid = gridDim.x;
-  const int per = grid / kXCDs;
-  const int me = grid % kXCDs == 0 ? (blockIdx.x % kXCDs) * per + blockIdx.x / kXCDs : blockIdx.x;
-
-  for (int item = me; item < total; item += grid) {
+  // Workgroups draw items in order, each its next one while it works (the merge
+  // kernel sets the count back to zero). A fixed share of the items left a
+  // quarter of the chip idle at the end.
+  int item = blockIdx.x;
+#pragma unroll 1
+  for (int k = 0; item < total; ++k) {
+    int drawn = 0;
+    if (tid == 0) drawn = (int)gridDim.x + atomicAdd(a.drawn, 1);
     int lo = 0, hi = rk.n_seqs - 1;
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
       if (items_s[mid] <= item) lo = mid; else hi = mid - 1;
     }
-    const int s = lo;
-    const TreeSeq ts = tree_plan(rk.seq_starts, rk.ctx_lens, s, G, rk.max_blocks);
-    int x = item - items_s[s];
+    const int s = __builtin_amdgcn_readfirstlane(lo);
+    const TreeSeq ts = tree_plan((const int32_t*)rk.seq_starts, rk.ctx_lens, s, G, rk.max_blocks);
+    int x = __builtin_amdgcn_readfirstlane(item - items_s[s]);
     const int tile_i = x % ts.tiles;
     x /= ts.tiles;
     const int g = x % a.Hkv, sp = x / a.Hkv;
     const int cols = ts.nodes * G, row0 = rk.seq_starts[s];
     int rgs;
     const int group0 = tree_tile((cols + kCols - 1) / kCols, tile_i, &rgs);
-    const int kss = kWaves / rgs;              // key sets
-    const int rg = wv % rgs, ks = wv / rgs;    // this wave's columns and keys
-    const int prefix = ts.len - ts.nodes;
-    const int t0 = sp * ts.part, t1 = min(ts.len, t0 + ts.part);
-    const int32_t* bt = rk.block_table + (int64_t)s * rk.max_blocks;
-    const int b_last = (max(t1, 1) - 1) / kBlockTokens;
-    auto block_of = [&](int b) -> int64_t {
-      const int64_t id = bt[min(b, b_last)];
-      return id < 0 ? 0 : id >= rk.num_blocks ? rk.num_blocks - 1 : id;
-    };
+    const int kss = kWaves / rgs;  // key sets
+    Walk w;
+    const int rg = wv & (rgs - 1);  // this wave's columns; and keys:
+    w.ks = rgs == 8 ? 0 : rgs == 4 ? wv >> 2 : wv >> 1;
+    w.stride = a.Hkv * kTile;
+    w.k_cache = a.k_cache + g * kTile;
+    w.v_cache = a.v_cache + g * kTile;
+    w.last_block = (int)min(rk.num_blocks, (int64_t)INT32_MAX) - 1;
+    w.bt = rk.block_table + (int64_t)s * rk.max_blocks;
+    w.words = rk.words;
+    w.nodes = ts.nodes;
+    w.prefix = ts.len - ts.nodes;
+    w.t0 = sp * ts.part;
+    w.t1 = min(ts.len, w.t0 + ts.part);
+    w.scale_log2 = a.scale_log2;
+    w.idle = (group0 + rg) * kCols >= cols;
 
-    // This wave's column in this lane; columns past the last repeat it.
+    // This lane's column; columns past the last repeat it.
     const int col = (group0 + rg) * kCols + (lane & 31);
     const int colc = min(col, cols - 1);
+    const bool live = col < cols;
     const int row = row0 + colc / G, head = g * G + colc % G;
-    const uint64_t* mask = rk.mask + (int64_t)row * rk.words;
-    const bool idle = (group0 + rg) * kCols >= cols;
+    w.mask = rk.mask + (int64_t)row * rk.words;
+    w.redo = a.redo + (int64_t)row * a.Hq + head;
     bf16x8_t qf[8];
-    {
-      const bf16_t* qp = a.q + ((int64_t)row * a.Hq + head) * HD + 8 * hf;
+    const bf16_t* qp = a.q + ((int64_t)row * a.Hq + head) * HD + 8 * hf;
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        qf[i] = __builtin_bit_cast(bf16x8_t, *(const u32x4_t*)(qp + 16 * i));
-    }
+    for (int i = 0; i < 8; ++i)
+      qf[i] = __builtin_bit_cast(bf16x8_t, *(const u32x4_t*)(qp + 16 * i));
     Cols c;
     c.m = -INFINITY;
     c.l = 0.f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) c.acc[i] = f32x16_t{};
-
-    // Softmax and values of the 32 keys from tok0 on.
-    auto finish = [&](f32x16_t& sc, u32x4_t v[2][2][2], int tok0) {
-      if (tok0 + kChunk > prefix) {
-        // Bit k: key tok0 + 4 hf + k (a lane's keys are 8 q + 4 hf + r).
-        const uint32_t seen = tree_bits32(mask, rk.words, ts.nodes, tok0 - prefix) >> (4 * hf);
-        if (tree_mask(sc, v, hf, t1 - tok0, seen)) a.redo[(int64_t)row * a.Hq + head] = 1;
-      }
-      u32x4_t p[2];
-      tree_softmax(c, sc, a.scale_log2, p);
-      tree_pv(c, v, p);
-    };
-
-    const int stages = (t1 - t0 + kStBlk * kBlockTokens - 1) / (kStBlk * kBlockTokens);
-    auto issue = [&](int st) {
-      const int64_t b = block_of(t0 / kBlockTokens + st * kStBlk + wv);
-      bf16_t* dst = kv + ((st & 1) * kStBlk + wv) * 2 * kTile;
-      const bf16_t* src[2] = {a.k_cache + (b * a.Hkv + g) * kTile + lane * 8,
-                              a.v_cache + (b * a.Hkv + g) * kTile + lane * 8};
-#pragma unroll
-      for (int w = 0; w < 2; ++w)
-#pragma unroll
-        for (int pc = 0; pc < 4; ++pc)
-          __builtin_amdgcn_global_load_lds(src[w] + pc * 512,
-                                           (lds_void_t*)(dst + w * kTile + pc * 512), 16, 0, 0);
-    };
-    issue(0);
-    __syncthreads();
-    for (int st = 0; st < stages; ++st) {
-      if (st + 1 < stages) issue(st + 1);
-      for (int ch = ks; ch < kStBlk / 2; ch += kss) {
-        const int tok0 = t0 + (st * kStBlk + 2 * ch) * kBlockTokens;
-        if (idle || tok0 >= t1) continue;
-        const bf16_t* kb = kv + ((st & 1) * kStBlk + 2 * ch) * 2 * kTile;
-        const bf16_t* kl = kb + (lane & 16 ? 2 * kTile : 0);
-        u32x4_t kf[8], vf[2][2][2];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) kf[i] = *(const u32x4_t*)(kl + k_frag_off(lane, i));
-        f32x16_t sc = tree_scores(kf, qf);
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-          for (int d = 0; d < 2; ++d)
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-              vf[j][d][u] = *(const u32x4_t*)(kb + (2 * j + 1) * kTile + v_frag_off(lane, d) +
-                                              u * 256);
-        finish(sc, vf, tok0);
-      }
-      __syncthreads();  // stage st + 1 landed; stage st's buffer is free
+    if (ts.len > 0) {
+      if (kss == 4)
+        tree_walk<4>(w, qf, kv, lane, wv, c);
+      else if (kss == 2)
+        tree_walk<2>(w, qf, kv, lane, wv, c);
+      else
+        tree_walk<1>(w, qf, kv, lane, wv, c);
     }
+    if (tid == 0) next_s[k & 1] = drawn;
+    __syncthreads();  // every wave is done with kv
+    item = next_s[k & 1];
 
-    // Merge the key sets of each column group: weights from the sets' maxima,
-    // sums in set order, wave (rg, ks) adding values 64 ks / kss .. of all sets.
-    {
-      const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(c.l), __float_as_uint(c.l),
-                                                       false, false);
-      c.l = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
-    }
-    float M = c.m, L = c.l;
+    const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(c.l), __float_as_uint(c.l),
+                                                     false, false);
+    float M = c.m, L = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
     // Where this lane's column goes: a part, or the output row.
-    const bool live = !idle && col < cols;
     const int64_t idx = base_s[s] + ((int64_t)(row - row0) * a.Hq + head) * ts.splits + sp;
     float* const part = ts.splits > 1 ? a.part_o + idx * HD + 4 * hf : nullptr;
     bf16_t* const out = a.o + 4 * hf + (a.tiled ? tile_off(row, head * HD, a.Hq * HD)
                                                 : ((int64_t)row * a.Hq + head) * HD);
-    float* xs = reinterpret_cast<float*>(kv);
+    auto put = [&](int v4, f32x4_t y, float inv) {
+      if (part)
+        *(f32x4_t*)(part + run_dim(v4)) = y;
+      else
+        store4(out + (a.tiled ? run_tiled(v4) : run_dim(v4)), y[0] * inv, y[1] * inv, y[2] * inv,
+               y[3] * inv);
+    };
     if (kss > 1) {
-      __syncthreads();  // every wave is done with kv (register path: with the last merge)
+      // Merge the key sets of each column group: weights from the sets' maxima,
+      // sums in set order, wave (rg, ks) adding values 64 ks / kss .. of all.
+      float* xs = reinterpret_cast<float*>(kv);
       if (hf == 0) {
-        sm_m[wv][lane] = c.m;
-        sm_l[wv][lane] = c.l;
+        sm_m[wv][lane] = M;
+        sm_l[wv][lane] = L;
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int r = 0; r < 16; ++r) xs[(wv * 64 + i * 16 + r) * 64 + lane] = c.acc[i][r];
       __syncthreads();
+      const int lc = lane & 31;
+      float f[4];
       M = -INFINITY;
-      for (int k = 0; k < kss; ++k) M = fmaxf(M, sm_m[k * rgs + rg][lane & 31]);
-      const float ref = M == -INFINITY ? 0.f : M;
       L = 0.f;
-      float f[kWaves];
 #pragma unroll
-      for (int k = 0; k < kWaves; ++k) {
+      for (int k = 0; k < 4; ++k)
+        if (k < kss) M = fmaxf(M, sm_m[k * rgs + rg][lc]);
+      const float ref = M == -INFINITY ? 0.f : M;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
         f[k] = 0.f;
         if (k < kss) {
-          f[k] = __builtin_amdgcn_exp2f(sm_m[k * rgs + rg][lane & 31] - ref);
-          L = fmaf(f[k], sm_l[k * rgs + rg][lane & 31], L);
+          f[k] = __builtin_amdgcn_exp2f(sm_m[k * rgs + rg][lc] - ref);
+          L = fmaf(f[k], sm_l[k * rgs + rg][lc], L);
         }
       }
-      const int per_w = 64 / kss;
+      const int per_w = kss == 4 ? 16 : 32;
       const float inv = L == 0.f ? 0.f : 1.0f / L;
-      for (int v4 = ks * per_w; v4 < (ks + 1) * per_w; v4 += 4) {
+#pragma unroll 1
+      for (int v4 = w.ks * per_w; v4 < (w.ks + 1) * per_w; v4 += 4) {
         f32x4_t y = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int k = 0; k < kWaves; ++k)
+        for (int k = 0; k < 4; ++k)
           if (k < kss) {
-            const float* w = xs + ((k * rgs + rg) * 64 + v4) * 64 + lane;
+            const float* z = xs + ((k * rgs + rg) * 64 + v4) * 64 + lane;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) y[r] = fmaf(f[k], w[r * 64], y[r]);
+            for (int r = 0; r < 4; ++r) y[r] = fmaf(f[k], z[r * 64], y[r]);
           }
-        if (!live) continue;
-        if (part)
-          *(f32x4_t*)(part + run_dim(v4)) = y;
-        else
-          store4(out + (a.tiled ? run_tiled(v4) : run_dim(v4)), y[0] * inv, y[1] * inv, y[2] * inv,
-                 y[3] * inv);
+        if (live) put(v4, y, inv);
       }
       __syncthreads();  // LDS is free for the next item
     } else if (live) {
@@ -494,17 +573,11 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_kernel(TreeArgs a)
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int r = 0; r < 16; r += 4) {
-          const f32x4_t y = {c.acc[i][r], c.acc[i][r + 1], c.acc[i][r + 2], c.acc[i][r + 3]};
-          const int v4 = 16 * i + r;
-          if (part)
-            *(f32x4_t*)(part + run_dim(v4)) = y;
-          else
-            store4(out + (a.tiled ? run_tiled(v4) : run_dim(v4)), y[0] * inv, y[1] * inv,
-                   y[2] * inv, y[3] * inv);
-        }
+        for (int r = 0; r < 16; r += 4)
+          put(16 * i + r,
+              f32x4_t{c.acc[i][r], c.acc[i][r + 1], c.acc[i][r + 2], c.acc[i][r + 3]}, inv);
     }
-    if (part && live && ks == 0 && hf == 0) {
+    if (part && live && w.ks == 0 && hf == 0) {
       a.part_ml[2 * idx] = M;
       a.part_ml[2 * idx + 1] = L;
     }
@@ -514,6 +587,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_kernel(TreeArgs a)
 // The parts of a row's heads, in order: four dims per thread, 32 threads per
 // head, eight heads per workgroup.
 __global__ __launch_bounds__(256) void tree_combine_kernel(TreeArgs a) {
+  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *a.drawn = 0;
   const int row = blockIdx.x + a.rk.seq_starts[0];
   if (row >= a.rk.seq_starts[a.rk.n_seqs]) return;
   const int s = row_to_seq(a.rk.seq_starts, a.rk.n_seqs, row);
@@ -614,7 +688,8 @@ hipError_t launch_tree_attention_bf16(const uint16_t* q, const uint16_t* k_cache
   a.part_ml = part_ml;
   a.part_cap = part_cap;
   a.plan = plan;
-  a.redo = redo;
+  a.drawn = redo;
+  a.redo = redo + 1;
   // One workgroup per CU (its LDS); batches of more than kMaxSeqs sequences
   // in several launches, which share the partial buffers in turn.
   for (int s0 = 0; s0 < rk.n_seqs; s0 += kMaxSeqs) {
