@@ -343,8 +343,8 @@ hipError_t launch_attn_rows(const T* q, const T* k_cache, const T* v_cache, cons
 // at most kTreeSplitsFew parts where it has at most 128 columns (nodes times
 // query heads of a group), else kTreeSplits; part_o [column parts][128] and
 // part_ml [column parts][2] hold part_cap = tree_column_parts, plan [n_seqs][2];
-// redo [1 + n_rows * Hq] (items drawn; rows to compute again) must be zero and
-// is left so.
+// redo [8 + n_rows * Hq] (items drawn per XCD; rows to compute again) must be
+// zero and is left so.
 constexpr int kTreeSplitsFew = 32, kTreeSplits = 16;
 int64_t tree_column_parts(int64_t max_rows, int64_t max_seqs, int Hq, int Hkv, int max_blocks);
 hipError_t launch_tree_attention_bf16(const uint16_t* q, const uint16_t* k_cache,

@@ -11,14 +11,15 @@
 // of four keys, two dims side by side, so that two 16-byte reads give the
 // operands of two products (dims h and h + 16) for 16 keys.
 //
-// A workgroup is eight waves that take 64, 128 or 256 columns (RG = 2, 4, 8
-// column groups) and KS = 8 / RG sets of keys; one workgroup per CU. Keys and
-// values go through LDS in stages of 128 keys, double-buffered, one barrier
-// each. Within a stage a wave takes its 4 / KS steps of 32 keys alone: the next
-// step's key operands are read while this one's go through softmax, so that of
-// the two waves of a SIMD one can multiply while the other does vector work.
-// Few columns are bound by the cache's bytes, many by products and softmax,
-// which take about as long each.
+// A workgroup is four waves with 128 columns (a column tile); two workgroups
+// per CU. They share the keys through LDS, 32 at a time, in a ring of four
+// stages with three on their way: what a tile of few columns is bound by is the
+// bytes in flight. (Eight waves of 256 columns and stages of 128 keys, two in
+// LDS, reached 2.7 TB/s on 64 sequences of 4 nodes and 4k keys; this 5.) Many
+// columns are bound by products and softmax, which take about as long each; of
+// the two waves of a SIMD, in different workgroups, one multiplies while the
+// other does vector work. The column tiles of the same keys run at the same
+// time on one XCD and read them from its L2.
 //
 // The keys of a sequence are split into parts (tree_part) that depend on its
 // own length and columns only, merged by a second kernel in order: a row's
@@ -34,32 +35,22 @@ namespace {
 
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef __attribute__((address_space(3))) void lds_void_t;
+typedef __attribute__((address_space(3))) bf16_t lds_bf16_t;
+typedef __attribute__((address_space(3))) u32x2_t lds_u32x2_t;
 
 constexpr int HD = 128;
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr int kWaves = 8;
+constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * kWave;
 constexpr int kCols = 32;   // columns of a wave
-constexpr int kChunk = 32;  // keys of a step
+constexpr int kTileCols = kWaves * kCols;
+constexpr int kStKeys = 32;  // keys of a stage
 constexpr int kTile = kBlockTokens * HD;
-constexpr int kStBlk = 8;   // blocks of a stage
-constexpr int kStKeys = kStBlk * kBlockTokens;
+constexpr int kRing = 4;    // stages in LDS
+constexpr int kStage = 4 * kTile;  // elements: keys and values of two blocks
+constexpr int kXCDs = 8;
 constexpr int kMaxSeqs = 1024;  // sequences of a launch
 constexpr float kLazy = 8.f;  // log2 units a running max may lag
-
-// Column tiles of a sequence with `groups` 32-column groups: full tiles of 8,
-// then the rest as a tile of 2, of 4 (3 or 4 groups), of 4 and 2 (5, 6) or of 8
-// (7): an idle group costs less than reading the keys again.
-__device__ __forceinline__ int tree_tiles(int groups) {
-  const int r = groups & 7;
-  return (groups >> 3) + (r == 0 ? 0 : r == 5 || r == 6 ? 2 : 1);
-}
-// Tile t's first group, and its width.
-__device__ __forceinline__ int tree_tile(int groups, int t, int* rg) {
-  const int full = groups >> 3, r = groups & 7;
-  *rg = t < full || (t == full && r == 7) ? 8 : t == full && r >= 3 ? 4 : 2;
-  return t <= full ? 8 * t : 8 * full + 4;
-}
 
 struct TreeSeq {
   int nodes, len;   // nodes, cached tokens (nodes included)
@@ -91,7 +82,7 @@ __device__ __forceinline__ TreeSeq tree_plan(const int32_t* seq_starts, const in
   t.nodes = max(seq_starts[s + 1] - seq_starts[s], 0);
   t.len = min(max(ctx_lens[s], 0), max_blocks * kBlockTokens);
   const int64_t cols = (int64_t)t.nodes * G;
-  t.tiles = tree_tiles((int)((cols + kCols - 1) / kCols));
+  t.tiles = (int)((cols + kTileCols - 1) / kTileCols);
   t.part = tree_part(cols, t.len);
   t.splits = tree_splits(cols, t.len);
   return t;
@@ -160,13 +151,6 @@ __device__ __forceinline__ float max16(const f32x16_t& s) {
   return fmaxf(m, s[15]);
 }
 
-__device__ __forceinline__ f32x16_t pv_step(uint32_t a0, uint32_t a1, uint32_t b0, uint32_t b1,
-                                            u32x4_t p, f32x16_t acc) {
-  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-      __builtin_bit_cast(bf16x8_t, u32x4_t{a0, a1, b0, b1}), __builtin_bit_cast(bf16x8_t, p), acc,
-      0, 0, 0);
-}
-
 // Scores of keys among or behind the nodes: -inf where the column does not see
 // the key. Bit k of seen: key 4 hf + k of the 32 (a lane holds 8 q + 4 hf + r).
 __device__ __forceinline__ void mask_scores(f32x16_t& s, uint32_t seen) {
@@ -185,17 +169,17 @@ __device__ __forceinline__ uint32_t mask_values(u32x4_t v[2][2][2], int hf, int 
 #pragma unroll
     for (int d = 0; d < 2; ++d)
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
+      for (int y = 0; y < 2; ++y)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const int k = 16 * j + 8 * u + 4 * hf + 2 * (e & 1);
-          uint32_t w = v[j][d][u][e];
+          const int u = e >> 1, k = 16 * j + 8 * u + 4 * hf + 2 * (e & 1);
+          uint32_t w = v[j][d][y][e];
           w &= (k < left ? 0xFFFFu : 0u) | (k + 1 < left ? 0xFFFF0000u : 0u);
           const bool lo = (w & 0x7F80u) == 0x7F80u, hi = (w & 0x7F800000u) == 0x7F800000u;
           if (lo) w &= 0xFFFF0000u;
           if (hi) w &= 0xFFFFu;
           odd |= ((lo ? 1u : 0u) | (hi ? 2u : 0u)) << (8 * j + 4 * u + 2 * (e & 1));
-          v[j][d][u][e] = w;
+          v[j][d][y][e] = w;
         }
   if (__ballot(odd != 0) == 0) return 0;
   uint32_t mine = 0;  // this half of the lanes' keys
@@ -215,278 +199,176 @@ struct Cols {
   f32x16_t acc[4];
 };
 
-// What a wave needs of its item.
-struct Walk {
-  const bf16_t *k_cache, *v_cache;  // of the kv head: block b's tile at b * stride
-  int stride, last_block;
-  const int32_t* bt;
-  const uint64_t* mask;
-  int words, nodes, prefix;
-  int t0, t1;
-  int ks;
-  bool idle;
-  float scale_log2;
-  int32_t* redo;
-};
-
-// The keys t0 .. t1 - 1 in stages of 128, of which this wave takes every
-// KS-th 32. kv: two stages of eight blocks' key and value tiles.
-template <int KS>
-__device__ __forceinline__ void tree_walk(const Walk& w, const bf16x8_t qf[8], bf16_t* kv,
-                                          int lane, int wv, Cols& c) {
-  const int hf = lane >> 5;
-  const int stages = (w.t1 - w.t0 + kStKeys - 1) / kStKeys;
-  const int b_last = (w.t1 - 1) / kBlockTokens;
-
-  // A wave brings one block of each stage (past the last key: the last block
-  // again, whose scores count as unseen). Called with st = 0, 1, ..: the blocks
-  // of 64 stages at a time in a register's lanes.
-  int ids = 0;
-  // (The address goes through a register of its own: the compiler would
-  // otherwise wait for every load in flight before each operand read.)
-  uint32_t kv_at = (uint32_t)(uintptr_t)(lds_void_t*)kv;
-  asm volatile("" : "+s"(kv_at));
-  auto issue = [&](int st) {
-    if ((st & 63) == 0) {
-      const int b = w.t0 / kBlockTokens + (st + lane) * kStBlk + wv;
-      ids = min(max(w.bt[min(b, b_last)], 0), w.last_block);
-    }
-    const int64_t at = (int64_t)__builtin_amdgcn_readlane(ids, st & 63) * w.stride + lane * 8;
-    const uint32_t dst = kv_at + ((st & 1) * kStBlk + wv) * (2 * kTile * 2);
+// The running max of a column moves only when a step's largest score (of this
+// lane's 16 keys: mx) exceeds it by kLazy.
+__device__ __forceinline__ void tree_rescale(Cols& c, float mx, float scale_log2) {
+  const auto sw =
+      __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+  const float top = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * scale_log2;
+  const float m_new = top > c.m + kLazy ? top : c.m;
+  if (__ballot(m_new != c.m) != 0) {
+    const float alpha = __builtin_amdgcn_exp2f(c.m - (m_new == -INFINITY ? 0.f : m_new));
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      __builtin_amdgcn_global_load_lds(w.k_cache + at + i * 512,
-                                       (lds_void_t*)(uintptr_t)(dst + i * 1024), 16, 0, 0);
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      __builtin_amdgcn_global_load_lds(w.v_cache + at + i * 512,
-                                       (lds_void_t*)(uintptr_t)(dst + kTile * 2 + i * 1024), 16, 0,
-                                       0);
-  };
-  // Operands of the 32 keys of step ch of a stage.
-  auto read_k = [&](int st, int ch, u32x4_t kf[8]) {
-    const bf16_t* kb =
-        kv + ((st & 1) * kStBlk + 2 * ch) * 2 * kTile + (lane & 16 ? 2 * kTile : 0);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) kf[i] = *(const u32x4_t*)(kb + k_frag_off(lane, i));
-  };
-  auto read_v = [&](int st, int ch, u32x4_t vf[2][2][2]) {
-    const bf16_t* vb = kv + ((st & 1) * kStBlk + 2 * ch) * 2 * kTile + kTile;
-#pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-      for (int d = 0; d < 2; ++d)
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-          vf[j][d][u] = *(const u32x4_t*)(vb + 2 * j * kTile + v_frag_off(lane, d) + u * 256);
-  };
-  auto scores = [&](const u32x4_t kf[8]) {
-    f32x16_t s = {};
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kf[i]), qf[i], s,
-                                                  0, 0, 0);
-    return s;
-  };
-  // Probabilities of 32 keys as operands of two products. The running max of a
-  // column moves only when a step exceeds it by kLazy.
-  auto softmax = [&](const f32x16_t& s, u32x4_t p[2]) {
-    const float mx = max16(s);
-    const auto sw =
-        __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
-    const float top = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * w.scale_log2;
-    const float m_new = top > c.m + kLazy ? top : c.m;
-    if (__ballot(m_new != c.m) != 0) {
-      const float alpha = __builtin_amdgcn_exp2f(c.m - (m_new == -INFINITY ? 0.f : m_new));
-#pragma unroll
-      for (int i = 0; i < 4; ++i) c.acc[i] *= alpha;
-      c.l *= alpha;
-      c.m = m_new;
-    }
-    const float m_ref = c.m == -INFINITY ? 0.f : c.m;
-    float pr[16];
-#pragma unroll
-    for (int r = 0; r < 16; ++r)
-      pr[r] = __builtin_amdgcn_exp2f(fmaf(s[r], w.scale_log2, -m_ref));
-    float ls = 0.f;
-#pragma unroll
-    for (int r = 0; r < 16; r += 4) ls += (pr[r] + pr[r + 1]) + (pr[r + 2] + pr[r + 3]);
-    c.l += ls;
-#pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) p[j][e] = pack_bf16x2(pr[8 * j + 2 * e], pr[8 * j + 2 * e + 1]);
-  };
-  auto values = [&](const u32x4_t v[2][2][2], const u32x4_t p[2]) {
-#pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-      for (int d = 0; d < 2; ++d) {
-        const u32x4_t a = v[j][d][0], b = v[j][d][1];
-        c.acc[2 * d] = pv_step(a.x, a.y, b.x, b.y, p[j], c.acc[2 * d]);
-        c.acc[2 * d + 1] = pv_step(a.z, a.w, b.z, b.w, p[j], c.acc[2 * d + 1]);
-      }
-  };
-  auto begin = [&](int st) {
-    wait_vmcnt<0>();  // this wave's block of stage st
-    stage_barrier();  // every wave's; and all are done with stage st - 1
-    if (st + 1 < stages) issue(st + 1);
-  };
-
-  issue(0);
-  if (w.idle) {
-#pragma unroll 1
-    for (int st = 0; st < stages; ++st) begin(st);
-    return;
-  }
-  // Stages that every column sees whole; then the others.
-  const int clear = min(stages, max(w.prefix - w.t0, 0) / kStKeys);
-  int st = 0;
-#pragma unroll 1
-  for (; st < clear; ++st) {
-    begin(st);
-    u32x4_t kf[8];
-    read_k(st, w.ks, kf);
-#pragma unroll 1
-    for (int ch = w.ks; ch < 4; ch += KS) {
-      u32x4_t vf[2][2][2], p[2];
-      const f32x16_t s = scores(kf);
-      read_v(st, ch, vf);
-      if (KS < 4) read_k(st, min(ch + KS, 3), kf);
-      softmax(s, p);
-      values(vf, p);
-    }
-  }
-#pragma unroll 1
-  for (; st < stages; ++st) {
-    begin(st);
-#pragma unroll 1
-    for (int ch = w.ks; ch < 4; ch += KS) {
-      const int tok0 = w.t0 + st * kStKeys + ch * kChunk;
-      if (tok0 >= w.t1) continue;
-      u32x4_t kf[8], vf[2][2][2], p[2];
-      read_k(st, ch, kf);
-      f32x16_t s = scores(kf);
-      read_v(st, ch, vf);
-      if (tok0 + kChunk > w.prefix) {
-        const uint32_t seen =
-            tree_bits32(w.mask, w.words, w.nodes, tok0 - w.prefix) >> (4 * hf);
-        mask_scores(s, seen);
-        if (mask_values(vf, hf, w.t1 - tok0) & seen) *w.redo = 1;
-      }
-      softmax(s, p);
-      values(vf, p);
-    }
+    for (int i = 0; i < 4; ++i) c.acc[i] *= alpha;
+    c.l *= alpha;
+    c.m = m_new;
   }
 }
 
+// Probabilities of 32 keys as operands of two products.
+__device__ __forceinline__ void tree_probs(Cols& c, const f32x16_t& s, float scale_log2,
+                                           u32x4_t p[2]) {
+  const float m_ref = c.m == -INFINITY ? 0.f : c.m;
+  float pr[16];
+#pragma unroll
+  for (int r = 0; r < 16; ++r) pr[r] = __builtin_amdgcn_exp2f(fmaf(s[r], scale_log2, -m_ref));
+  float ls = 0.f;
+#pragma unroll
+  for (int r = 0; r < 16; r += 4) ls += (pr[r] + pr[r + 1]) + (pr[r + 2] + pr[r + 3]);
+  c.l += ls;
+#pragma unroll
+  for (int j = 0; j < 2; ++j)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) p[j][e] = pack_bf16x2(pr[8 * j + 2 * e], pr[8 * j + 2 * e + 1]);
+}
+
+// O^T += V^T P^T. v[j][d][y]: block j's operand of dims 32 (2 d + m / 16) + 16 y
+// + m % 16: keys 4 hf .. + 3, then 8 + 4 hf .. + 3.
+__device__ __forceinline__ void tree_values(Cols& c, const u32x4_t v[2][2][2],
+                                            const u32x4_t p[2]) {
+#pragma unroll
+  for (int j = 0; j < 2; ++j)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      c.acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+          __builtin_bit_cast(bf16x8_t, v[j][i >> 1][i & 1]), __builtin_bit_cast(bf16x8_t, p[j]),
+          c.acc[i], 0, 0, 0);
+}
+
+// Inclusive sum of x over the workgroup's threads so far: `carry` before, the
+// whole added to it. red: one int per wave.
+__device__ __forceinline__ int block_scan(int x, int* red, int& carry) {
+  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+#pragma unroll
+  for (int d = 1; d < kWave; d <<= 1) {
+    const int y = __shfl_up(x, d, kWave);
+    if (lane >= d) x += y;
+  }
+  if (lane == kWave - 1) red[wv] = x;
+  __syncthreads();
+  x += carry;
+  for (int w = 0; w < kWaves; ++w) {
+    if (w < wv) x += red[w];
+    carry += red[w];
+  }
+  __syncthreads();
+  return x;
+}
+
 __global__ __launch_bounds__(kThreads, 2) void tree_attention_kernel(TreeArgs a) {
-  // Two stages of keys and values; at the end the waves' O^T ([wave][64
-  // values][64 lanes] floats), 128 KB either way.
-  __shared__ __attribute__((aligned(16))) bf16_t kv[2 * kStBlk * 2 * kTile];
-  __shared__ int items_s[kMaxSeqs + 1], base_s[kMaxSeqs];
-  __shared__ int wsum[2][kWaves], next_s[2];
-  __shared__ float sm_m[kWaves][kCols], sm_l[kWaves][kCols];
+  __shared__ __attribute__((aligned(16))) bf16_t ring[kRing * kStage];
+  __shared__ int units_s[kMaxSeqs], base_s[kMaxSeqs], items_s[kMaxSeqs];
+  __shared__ int red[kWaves], next_s[2];
   const RowKeys& rk = a.rk;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int hf = lane >> 5;
   const int G = a.Hq / a.Hkv;
 
-  // The work list: sequences' items (part, kv head, column tile) in order, and
-  // where their column parts start.
-  int carry_i = 0, carry_b = 0;
+  // Units (part, kv head) of all sequences in order go round the XCDs (blockIdx
+  // % 8); an XCD's list of items is its units' column tiles.
+  const int queues = gridDim.x % kXCDs == 0 ? kXCDs : 1;
+  const int queue = blockIdx.x % queues;
+  int n_units = 0, n_parts = 0, total = 0;
   for (int s0 = 0; s0 < rk.n_seqs; s0 += kThreads) {
     const int s = s0 + tid;
-    int ni = 0, nb = 0;
-    TreeSeq t{};
+    int nu = 0, np = 0, tiles = 0;
     if (s < rk.n_seqs) {
-      t = tree_plan(rk.seq_starts, rk.ctx_lens, s, G, rk.max_blocks);
-      ni = t.tiles * t.splits * a.Hkv;
-      nb = t.splits > 1 ? t.nodes * a.Hq * t.splits : 0;
+      const TreeSeq t = tree_plan(rk.seq_starts, rk.ctx_lens, s, G, rk.max_blocks);
+      tiles = t.tiles;
+      nu = t.tiles > 0 ? t.splits * a.Hkv : 0;
+      np = t.splits > 1 ? t.nodes * a.Hq * t.splits : 0;
+      if (blockIdx.x == 0) a.plan[2 * s + 1] = t.splits;
     }
-    int si = ni, sb = nb;
-#pragma unroll
-    for (int d = 1; d < kWave; d <<= 1) {
-      const int x = __shfl_up(si, d, kWave), y = __shfl_up(sb, d, kWave);
-      if (lane >= d) {
-        si += x;
-        sb += y;
-      }
-    }
-    if (lane == kWave - 1) {
-      wsum[0][wv] = si;
-      wsum[1][wv] = sb;
-    }
-    __syncthreads();
-    int bi = carry_i, bb = carry_b;
-    for (int w = 0; w < kWaves; ++w) {
-      if (w < wv) {
-        bi += wsum[0][w];
-        bb += wsum[1][w];
-      }
-      carry_i += wsum[0][w];
-      carry_b += wsum[1][w];
-    }
+    const int u1 = block_scan(nu, red, n_units), u0 = u1 - nu;
+    const int p0 = block_scan(np, red, n_parts) - np;
+    // The queue's units among u0 .. u1 - 1.
+    const int mine = ((u1 - queue + queues - 1) / queues - (u0 - queue + queues - 1) / queues);
+    const int ni = mine * tiles;
+    const int i0 = block_scan(ni, red, total) - ni;
     if (s < rk.n_seqs) {
-      items_s[s] = bi + si - ni;
-      base_s[s] = bb + sb - nb;
-      if (blockIdx.x == 0) {
-        a.plan[2 * s] = bb + sb - nb;
-        a.plan[2 * s + 1] = t.splits;
-      }
+      units_s[s] = u0;
+      base_s[s] = p0;
+      items_s[s] = i0;
+      if (blockIdx.x == 0) a.plan[2 * s] = p0;
     }
-    __syncthreads();
   }
-  const int total = carry_i;
-  if (carry_b > a.part_cap) return;  // more rows than the call named: no room for their parts
+  __syncthreads();
+  if (n_parts > a.part_cap) return;  // more rows than the call named: no room for their parts
+
+  // (The ring's address goes through a register of its own: the compiler would
+  // otherwise wait for every load in flight before each operand read.)
+  uint32_t ring_at = (uint32_t)(uintptr_t)(lds_void_t*)ring;
+  asm volatile("" : "+s"(ring_at));
 
   // Workgroups draw items in order, each its next one while it works (the merge
-  // kernel sets the count back to zero). A fixed share of the items left a
+  // kernel sets the counts back to zero). A fixed share of the items left a
   // quarter of the chip idle at the end.
-  int item = blockIdx.x;
+  int item = blockIdx.x / queues;
 #pragma unroll 1
   for (int k = 0; item < total; ++k) {
     int drawn = 0;
-    if (tid == 0) drawn = (int)gridDim.x + atomicAdd(a.drawn, 1);
+    if (tid == 0) drawn = (int)gridDim.x / queues + atomicAdd(a.drawn + queue, 1);
     int lo = 0, hi = rk.n_seqs - 1;
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
       if (items_s[mid] <= item) lo = mid; else hi = mid - 1;
     }
     const int s = __builtin_amdgcn_readfirstlane(lo);
-    const TreeSeq ts = tree_plan((const int32_t*)rk.seq_starts, rk.ctx_lens, s, G, rk.max_blocks);
-    int x = __builtin_amdgcn_readfirstlane(item - items_s[s]);
-    const int tile_i = x % ts.tiles;
-    x /= ts.tiles;
-    const int g = x % a.Hkv, sp = x / a.Hkv;
+    const TreeSeq ts = tree_plan(rk.seq_starts, rk.ctx_lens, s, G, rk.max_blocks);
+    const int x = __builtin_amdgcn_readfirstlane(item - items_s[s]);
+    const int u0 = __builtin_amdgcn_readfirstlane(units_s[s]);
+    // The sequence's unit: the queue's (x / tiles)-th from u0 on.
+    const int u = (queue - u0 % queues + queues) % queues + x / ts.tiles * queues;
+    const int g = u % a.Hkv, sp = u / a.Hkv;
     const int cols = ts.nodes * G, row0 = rk.seq_starts[s];
-    int rgs;
-    const int group0 = tree_tile((cols + kCols - 1) / kCols, tile_i, &rgs);
-    const int kss = kWaves / rgs;  // key sets
-    Walk w;
-    const int rg = wv & (rgs - 1);  // this wave's columns; and keys:
-    w.ks = rgs == 8 ? 0 : rgs == 4 ? wv >> 2 : wv >> 1;
-    w.stride = a.Hkv * kTile;
-    w.k_cache = a.k_cache + g * kTile;
-    w.v_cache = a.v_cache + g * kTile;
-    w.last_block = (int)min(rk.num_blocks, (int64_t)INT32_MAX) - 1;
-    w.bt = rk.block_table + (int64_t)s * rk.max_blocks;
-    w.words = rk.words;
-    w.nodes = ts.nodes;
-    w.prefix = ts.len - ts.nodes;
-    w.t0 = sp * ts.part;
-    w.t1 = min(ts.len, w.t0 + ts.part);
-    w.scale_log2 = a.scale_log2;
-    w.idle = (group0 + rg) * kCols >= cols;
+    const int col0 = x % ts.tiles * kTileCols + wv * kCols;
+    const bool idle = col0 >= cols;
+    const int prefix = ts.len - ts.nodes;
+    const int t0 = sp * ts.part, t1 = min(ts.len, t0 + ts.part);
+    const int stages = (t1 - t0 + kStKeys - 1) / kStKeys;
+
+    // A wave brings one tile of each stage, keys (waves 0, 2) or values of one
+    // of its two blocks; past the last key the last block again, whose scores
+    // count as unseen. Called with st = 0, 1, ..: the blocks of 64 stages at a
+    // time in a register's lanes.
+    const int32_t* bt = rk.block_table + (int64_t)s * rk.max_blocks;
+    const bf16_t* cache = (wv & 1 ? a.v_cache : a.k_cache) + g * kTile + lane * 8;
+    const int b_last = (t1 - 1) / kBlockTokens;
+    int ids = 0;
+    auto issue = [&](int st) {
+      if ((st & 63) == 0) {
+        const int b = t0 / kBlockTokens + (st + lane) * 2 + (wv >> 1);
+        const int64_t id = bt[min(b, b_last)];
+        ids = (int)(id < 0 ? 0 : id >= rk.num_blocks ? rk.num_blocks - 1 : id);
+      }
+      const bf16_t* src =
+          cache + (int64_t)__builtin_amdgcn_readlane(ids, st & 63) * (a.Hkv * kTile);
+      const uint32_t dst = ring_at + ((st % kRing) * kStage + wv * kTile) * 2;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        __builtin_amdgcn_global_load_lds(src + i * 512, (lds_void_t*)(uintptr_t)(dst + i * 1024),
+                                         16, 0, 0);
+    };
+    if (stages > 0) issue(0);
+    if (stages > 1) issue(1);
+    if (stages > 2) issue(2);
 
     // This lane's column; columns past the last repeat it.
-    const int col = (group0 + rg) * kCols + (lane & 31);
+    const int col = col0 + (lane & 31);
     const int colc = min(col, cols - 1);
-    const bool live = col < cols;
     const int row = row0 + colc / G, head = g * G + colc % G;
-    w.mask = rk.mask + (int64_t)row * rk.words;
-    w.redo = a.redo + (int64_t)row * a.Hq + head;
+    const uint64_t* mask = rk.mask + (int64_t)row * rk.words;
     bf16x8_t qf[8];
     const bf16_t* qp = a.q + ((int64_t)row * a.Hq + head) * HD + 8 * hf;
 #pragma unroll
@@ -497,89 +379,146 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_kernel(TreeArgs a)
     c.l = 0.f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) c.acc[i] = f32x16_t{};
-    if (ts.len > 0) {
-      if (kss == 4)
-        tree_walk<4>(w, qf, kv, lane, wv, c);
-      else if (kss == 2)
-        tree_walk<2>(w, qf, kv, lane, wv, c);
+
+    auto begin = [&](int st) {
+      // This wave's tile of stage st + 1, with one later on its way.
+      if (st + 2 < stages)
+        wait_vmcnt<4>();
       else
-        tree_walk<1>(w, qf, kv, lane, wv, c);
+        wait_vmcnt<0>();
+      stage_barrier();  // every wave's; and all are done with stage st - 1
+      if (st + 3 < stages) issue(st + 3);
+    };
+    auto read_k = [&](int st, u32x4_t kf[8]) {
+      const bf16_t* kb = ring + (st % kRing) * kStage + (lane & 16 ? 2 * kTile : 0);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) kf[i] = *(const u32x4_t*)(kb + k_frag_off(lane, i));
+    };
+    auto scores = [&](const u32x4_t kf[8]) {
+      f32x16_t z = {};
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kf[i]), qf[i], z,
+                                                    0, 0, 0);
+      return z;
+    };
+    // Value operands of block j: per dim pair d, dims h and h + 16, as two runs
+    // of four keys 512 bytes apart (one read of two 8-byte halves each; the
+    // second address is hidden, or the compiler would read 16 bytes at a time
+    // and move the halves).
+    auto read_v = [&](int st, u32x4_t vf[2][2][2]) {
+      const bf16_t* lo = ring + (st % kRing) * kStage + kTile + v_frag_off(lane, 0);
+      uint32_t at = (uint32_t)(uintptr_t)(lds_bf16_t*)lo + 8;
+      asm volatile("" : "+v"(at));
+      const lds_bf16_t* hi = (const lds_bf16_t*)(uintptr_t)at;
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int d = 0; d < 2; ++d) {
+          const int off = j * 2 * kTile + d * 1024;
+          const u32x2_t a = *(const u32x2_t*)(lo + off), b = *(const u32x2_t*)(lo + off + 256);
+          const u32x2_t e = *(const lds_u32x2_t*)(hi + off),
+                        f = *(const lds_u32x2_t*)(hi + off + 256);
+          vf[j][d][0] = u32x4_t{a.x, a.y, b.x, b.y};
+          vf[j][d][1] = u32x4_t{e.x, e.y, f.x, f.y};
+        }
+    };
+    if (stages > 2)
+      wait_vmcnt<8>();
+    else
+      wait_vmcnt<0>();
+    stage_barrier();  // stage 0 is here
+    if (idle) {
+#pragma unroll 1
+      for (int st = 0; st < stages; ++st) begin(st);
+    } else if (stages > 0) {
+      // Scores of a stage are computed while the one before goes through softmax
+      // and its values. z, mx: those of the next stage.
+      f32x16_t z;
+      float mx;
+      auto next_scores = [&](int st) {
+        u32x4_t kf[8];
+        read_k(st, kf);
+        z = scores(kf);
+        const int tok0 = t0 + st * kStKeys;
+        if (tok0 + kStKeys > prefix)
+          mask_scores(z, tree_bits32(mask, rk.words, ts.nodes, tok0 - prefix) >> (4 * hf));
+        mx = max16(z);
+      };
+      next_scores(0);
+      // Stages that, with their next, every column sees whole; then the others.
+      const int clear = min(stages, max(prefix - t0, 0) / kStKeys) - 1;
+      int st = 0;
+      auto step = [&](const f32x16_t& now, f32x16_t& next) {
+        begin(st);
+        tree_rescale(c, mx, a.scale_log2);
+        u32x4_t kf[8], vf[2][2][2], p[2];
+        read_k(st + 1, kf);
+        read_v(st, vf);
+        next = scores(kf);
+        tree_probs(c, now, a.scale_log2, p);
+        tree_values(c, vf, p);
+        mx = max16(next);
+        ++st;
+      };
+      f32x16_t z2;  // two steps a turn: the scores change places without moves
+#pragma unroll 1
+      while (st + 1 < clear) {
+        step(z, z2);
+        step(z2, z);
+      }
+      if (st < clear) {
+        step(z, z2);
+        z = z2;
+      }
+#pragma unroll 1
+      for (; st < stages; ++st) {
+        begin(st);
+        tree_rescale(c, mx, a.scale_log2);
+        const int tok0 = t0 + st * kStKeys;
+        u32x4_t vf[2][2][2], p[2];
+        read_v(st, vf);
+        if (tok0 + kStKeys > prefix) {
+          const uint32_t seen = tree_bits32(mask, rk.words, ts.nodes, tok0 - prefix) >> (4 * hf);
+          if (mask_values(vf, hf, t1 - tok0) & seen) a.redo[(int64_t)row * a.Hq + head] = 1;
+        }
+        tree_probs(c, z, a.scale_log2, p);
+        tree_values(c, vf, p);
+        if (st + 1 < stages) next_scores(st + 1);
+      }
     }
     if (tid == 0) next_s[k & 1] = drawn;
-    __syncthreads();  // every wave is done with kv
+    __syncthreads();  // every wave is done with the ring
     item = next_s[k & 1];
 
-    const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(c.l), __float_as_uint(c.l),
-                                                     false, false);
-    float M = c.m, L = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
-    // Where this lane's column goes: a part, or the output row.
-    const int64_t idx = base_s[s] + ((int64_t)(row - row0) * a.Hq + head) * ts.splits + sp;
-    float* const part = ts.splits > 1 ? a.part_o + idx * HD + 4 * hf : nullptr;
-    bf16_t* const out = a.o + 4 * hf + (a.tiled ? tile_off(row, head * HD, a.Hq * HD)
-                                                : ((int64_t)row * a.Hq + head) * HD);
-    auto put = [&](int v4, f32x4_t y, float inv) {
-      if (part)
-        *(f32x4_t*)(part + run_dim(v4)) = y;
-      else
-        store4(out + (a.tiled ? run_tiled(v4) : run_dim(v4)), y[0] * inv, y[1] * inv, y[2] * inv,
-               y[3] * inv);
-    };
-    if (kss > 1) {
-      // Merge the key sets of each column group: weights from the sets' maxima,
-      // sums in set order, wave (rg, ks) adding values 64 ks / kss .. of all.
-      float* xs = reinterpret_cast<float*>(kv);
-      if (hf == 0) {
-        sm_m[wv][lane] = M;
-        sm_l[wv][lane] = L;
-      }
+    if (col < cols) {
+      const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(c.l),
+                                                       __float_as_uint(c.l), false, false);
+      const float L = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+      if (ts.splits > 1) {
+        const int64_t idx = base_s[s] + ((int64_t)(row - row0) * a.Hq + head) * ts.splits + sp;
+        float* part = a.part_o + idx * HD + 4 * hf;
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+        for (int v = 0; v < 64; v += 4) {
+          const f32x16_t& o = c.acc[v >> 4];
+          *(f32x4_t*)(part + run_dim(v)) =
+              f32x4_t{o[v & 15], o[(v & 15) + 1], o[(v & 15) + 2], o[(v & 15) + 3]};
+        }
+        if (hf == 0) {
+          a.part_ml[2 * idx] = c.m;
+          a.part_ml[2 * idx + 1] = L;
+        }
+      } else {
+        const float inv = L == 0.f ? 0.f : 1.0f / L;
+        bf16_t* out = a.o + 4 * hf + (a.tiled ? tile_off(row, head * HD, a.Hq * HD)
+                                              : ((int64_t)row * a.Hq + head) * HD);
 #pragma unroll
-        for (int r = 0; r < 16; ++r) xs[(wv * 64 + i * 16 + r) * 64 + lane] = c.acc[i][r];
-      __syncthreads();
-      const int lc = lane & 31;
-      float f[4];
-      M = -INFINITY;
-      L = 0.f;
-#pragma unroll
-      for (int k = 0; k < 4; ++k)
-        if (k < kss) M = fmaxf(M, sm_m[k * rgs + rg][lc]);
-      const float ref = M == -INFINITY ? 0.f : M;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        f[k] = 0.f;
-        if (k < kss) {
-          f[k] = __builtin_amdgcn_exp2f(sm_m[k * rgs + rg][lc] - ref);
-          L = fmaf(f[k], sm_l[k * rgs + rg][lc], L);
+        for (int v = 0; v < 64; v += 4) {
+          const f32x16_t& o = c.acc[v >> 4];
+          store4(out + (a.tiled ? run_tiled(v) : run_dim(v)), o[v & 15] * inv,
+                 o[(v & 15) + 1] * inv, o[(v & 15) + 2] * inv, o[(v & 15) + 3] * inv);
         }
       }
-      const int per_w = kss == 4 ? 16 : 32;
-      const float inv = L == 0.f ? 0.f : 1.0f / L;
-#pragma unroll 1
-      for (int v4 = w.ks * per_w; v4 < (w.ks + 1) * per_w; v4 += 4) {
-        f32x4_t y = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          if (k < kss) {
-            const float* z = xs + ((k * rgs + rg) * 64 + v4) * 64 + lane;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) y[r] = fmaf(f[k], z[r * 64], y[r]);
-          }
-        if (live) put(v4, y, inv);
-      }
-      __syncthreads();  // LDS is free for the next item
-    } else if (live) {
-      const float inv = L == 0.f ? 0.f : 1.0f / L;
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int r = 0; r < 16; r += 4)
-          put(16 * i + r,
-              f32x4_t{c.acc[i][r], c.acc[i][r + 1], c.acc[i][r + 2], c.acc[i][r + 3]}, inv);
-    }
-    if (part && live && w.ks == 0 && hf == 0) {
-      a.part_ml[2 * idx] = M;
-      a.part_ml[2 * idx + 1] = L;
     }
   }
 }
@@ -587,7 +526,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_kernel(TreeArgs a)
 // The parts of a row's heads, in order: four dims per thread, 32 threads per
 // head, eight heads per workgroup.
 __global__ __launch_bounds__(256) void tree_combine_kernel(TreeArgs a) {
-  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *a.drawn = 0;
+  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x < kXCDs) a.drawn[threadIdx.x] = 0;
   const int row = blockIdx.x + a.rk.seq_starts[0];
   if (row >= a.rk.seq_starts[a.rk.n_seqs]) return;
   const int s = row_to_seq(a.rk.seq_starts, a.rk.n_seqs, row);
@@ -602,15 +541,33 @@ __global__ __launch_bounds__(256) void tree_combine_kernel(TreeArgs a) {
   if (!again) {
     const int64_t idx =
         a.plan[2 * s] + ((int64_t)(row - a.rk.seq_starts[s]) * a.Hq + head) * splits;
-    for (int p = 0; p < splits; ++p) M = fmaxf(M, a.part_ml[2 * (idx + p)]);
-    const float ref = M == -INFINITY ? 0.f : M;
-#pragma unroll 4
-    for (int p = 0; p < splits; ++p) {
-      const float f = __builtin_amdgcn_exp2f(a.part_ml[2 * (idx + p)] - ref);
-      L = fmaf(f, a.part_ml[2 * (idx + p) + 1], L);
-      const f32x4_t v = *(const f32x4_t*)(a.part_o + (idx + p) * HD + dim);
+    // Four parts at a time, all their loads together.
+    for (int p0 = 0; p0 < splits; p0 += 4) {
+      f32x4_t v[4];
+      f32x2_t ml[4];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) y[r] = fmaf(f, v[r], y[r]);
+      for (int u = 0; u < 4; ++u) {
+        const int64_t i = idx + min(p0 + u, splits - 1);
+        ml[u] = *(const f32x2_t*)(a.part_ml + 2 * i);
+        v[u] = *(const f32x4_t*)(a.part_o + i * HD + dim);
+      }
+      float m_new = M;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) m_new = fmaxf(m_new, ml[u][0]);
+      const float ref = m_new == -INFINITY ? 0.f : m_new;
+      const float alpha = __builtin_amdgcn_exp2f(M - ref);
+      L *= alpha;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) y[r] *= alpha;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        if (p0 + u >= splits) break;
+        const float f = __builtin_amdgcn_exp2f(ml[u][0] - ref);
+        L = fmaf(f, ml[u][1], L);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) y[r] = fmaf(f, v[u][r], y[r]);
+      }
+      M = m_new;
     }
   } else {
     // A row that sees a non-finite value among the nodes: key by key.
@@ -689,15 +646,15 @@ hipError_t launch_tree_attention_bf16(const uint16_t* q, const uint16_t* k_cache
   a.part_cap = part_cap;
   a.plan = plan;
   a.drawn = redo;
-  a.redo = redo + 1;
-  // One workgroup per CU (its LDS); batches of more than kMaxSeqs sequences
+  a.redo = redo + kXCDs;
+  // Two workgroups per CU (LDS, registers); batches of more than kMaxSeqs sequences
   // in several launches, which share the partial buffers in turn.
   for (int s0 = 0; s0 < rk.n_seqs; s0 += kMaxSeqs) {
     a.rk.seq_starts = rk.seq_starts + s0;
     a.rk.ctx_lens = rk.ctx_lens + s0;
     a.rk.block_table = rk.block_table + (int64_t)s0 * rk.max_blocks;
     a.rk.n_seqs = rk.n_seqs - s0 < kMaxSeqs ? rk.n_seqs - s0 : kMaxSeqs;
-    COCO_LAUNCH(tree_attention_kernel, dim3(num_cus), dim3(kThreads), 0, st, a);
+    COCO_LAUNCH(tree_attention_kernel, dim3(2 * num_cus), dim3(kThreads), 0, st, a);
     COCO_LAUNCH(tree_combine_kernel, dim3(n_rows, (Hq + 7) / 8), dim3(256), 0, st, a);
   }
   return hipGetLastError();
