@@ -26,7 +26,7 @@ FLAGS = ["-O3", "-std=c++17", f"--offload-arch={ARCH}", "-fPIC", "-Wall",
 SOURCES = ["rows.hip", "gemm_skinny.hip", "gemm_prefill_qkv.hip", "gemm_prefill_resid.hip",
            "gemm_prefill_swiglu.hip", "gemm_prefill_scatter.hip", "gemm_prefill_partial.hip",
            "attention.hip", "layer_f32.hip", "pages.hip", "attention_rows.hip", "tree_attention.hip",
-           "block_select.hip",
+           "block_select.hip", "sparse_attention.hip",
            "coco_api.hip", "cache_api.hip", "probe.hip", "scaling.cpp"]
 
 

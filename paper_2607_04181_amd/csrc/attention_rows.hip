@@ -1,5 +1,6 @@
-// Attention of rows that do not see a plain causal prefix of the paged cache:
-// the nodes of a tree of drafted tokens, and rows that attend selected blocks.
+// fp32 attention of rows that do not see a plain causal prefix of the paged
+// cache: the nodes of a tree of drafted tokens, and rows that attend selected
+// blocks.
 //
 // One workgroup per row and GH query heads of one key/value head, eight waves
 // striding over the row's blocks with an online softmax each, merged in LDS in
@@ -23,18 +24,6 @@ __device__ __forceinline__ F8 load8(const float* p) {
   const f32x4_t a = *(const f32x4_t*)p, b = *(const f32x4_t*)(p + 4);
   return F8{{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]}};
 }
-__device__ __forceinline__ F8 load8(const bf16_t* p) {
-  const u32x4_t a = *(const u32x4_t*)p;
-  F8 r;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    r.e[2 * i] = bf16_to_f32(a[i] & 0xFFFFu);
-    r.e[2 * i + 1] = __uint_as_float(a[i] & 0xFFFF0000u);
-  }
-  return r;
-}
-__device__ __forceinline__ void store1(float* p, float x) { *p = x; }
-__device__ __forceinline__ void store1(bf16_t* p, float x) { *p = (bf16_t)f32_to_bf16(x); }
 
 // Bits k0 .. k0 + 15 of what a tree node sees, k0 counted from the first node:
 // set before it (the prefix), the row's mask among the n nodes, clear behind.
@@ -54,10 +43,10 @@ __device__ __forceinline__ uint32_t tree_bits(const uint64_t* mask, int words, i
 }
 
 // HS: head_dim / 32.
-template <typename T, int HS, int GH, bool TREE>
+template <int HS, int GH, bool TREE>
 __global__ __launch_bounds__(64 * kRowsWaves) void attn_rows_kernel(
-    const T* __restrict__ q, const T* __restrict__ k_cache, const T* __restrict__ v_cache,
-    RowKeys rk, int Hq, int Hkv, T* __restrict__ o, bool tiled) {
+    const float* __restrict__ q, const float* __restrict__ k_cache,
+    const float* __restrict__ v_cache, RowKeys rk, int Hq, int Hkv, float* __restrict__ o) {
   constexpr int hd = 32 * HS;
   __shared__ float sm_m[kRowsWaves][GH], sm_l[kRowsWaves][GH];
   __shared__ float sm_o[kRowsWaves][GH][hd];
@@ -196,18 +185,15 @@ __global__ __launch_bounds__(64 * kRowsWaves) void attn_rows_kernel(
       a = fmaf(f, sm_o[w][e][dim], a);
       L = fmaf(f, sm_l[w][e], L);
     }
-    const int col = (h0 + e) * hd + dim;
-    store1(o + (tiled ? tile_off(i, col, Hq * hd) : (int64_t)i * Hq * hd + col),
-           L == 0.f ? 0.f : a / L);
+    o[((int64_t)i * Hq + h0 + e) * hd + dim] = L == 0.f ? 0.f : a / L;
   }
 }
 
 }  // namespace
 
-template <typename T>
-hipError_t launch_attn_rows(const T* q, const T* k_cache, const T* v_cache, const RowKeys& rk,
-                            int n_rows, int Hq, int Hkv, int hd, T* o, bool tiled,
-                            hipStream_t st) {
+hipError_t launch_attn_rows_f32(const float* q, const float* k_cache, const float* v_cache,
+                                const RowKeys& rk, int n_rows, int Hq, int Hkv, int hd, float* o,
+                                hipStream_t st) {
   if (n_rows <= 0) return hipSuccess;
   // Heads per workgroup: they share the key/value loads; the queries they
   // keep in registers (hd / 4 floats per lane each) bound their number.
@@ -217,43 +203,31 @@ hipError_t launch_attn_rows(const T* q, const T* k_cache, const T* v_cache, cons
 #define COCO_ROWS(HS, GH)                                                                     \
   do {                                                                                        \
     if (rk.mask)                                                                              \
-      COCO_LAUNCH((attn_rows_kernel<T, HS, GH, true>), grid, block, 0, st, q, k_cache,        \
-                  v_cache, rk, Hq, Hkv, o, tiled);                                            \
+      COCO_LAUNCH((attn_rows_kernel<HS, GH, true>), grid, block, 0, st, q, k_cache, v_cache,  \
+                  rk, Hq, Hkv, o);                                                            \
     else                                                                                      \
-      COCO_LAUNCH((attn_rows_kernel<T, HS, GH, false>), grid, block, 0, st, q, k_cache,       \
-                  v_cache, rk, Hq, Hkv, o, tiled);                                            \
+      COCO_LAUNCH((attn_rows_kernel<HS, GH, false>), grid, block, 0, st, q, k_cache, v_cache, \
+                  rk, Hq, Hkv, o);                                                            \
   } while (0)
 #define COCO_ROWS4(HS) \
   if (gh == 4) COCO_ROWS(HS, 4); else if (gh == 2) COCO_ROWS(HS, 2); else COCO_ROWS(HS, 1)
 #define COCO_ROWS2(HS) \
   if (gh == 2) COCO_ROWS(HS, 2); else COCO_ROWS(HS, 1)
-  if constexpr (sizeof(T) == 2) {
-    if (hd != 128) return hipErrorInvalidValue;
-    COCO_ROWS2(4);
-  } else {
-    switch (hd) {
-      case 32: COCO_ROWS4(1); break;
-      case 64: COCO_ROWS4(2); break;
-      case 96: COCO_ROWS2(3); break;
-      case 128: COCO_ROWS2(4); break;
-      case 160: COCO_ROWS(5, 1); break;
-      case 192: COCO_ROWS(6, 1); break;
-      case 224: COCO_ROWS(7, 1); break;
-      case 256: COCO_ROWS(8, 1); break;
-      default: return hipErrorInvalidValue;
-    }
+  switch (hd) {
+    case 32: COCO_ROWS4(1); break;
+    case 64: COCO_ROWS4(2); break;
+    case 96: COCO_ROWS2(3); break;
+    case 128: COCO_ROWS2(4); break;
+    case 160: COCO_ROWS(5, 1); break;
+    case 192: COCO_ROWS(6, 1); break;
+    case 224: COCO_ROWS(7, 1); break;
+    case 256: COCO_ROWS(8, 1); break;
+    default: return hipErrorInvalidValue;
   }
 #undef COCO_ROWS4
 #undef COCO_ROWS2
 #undef COCO_ROWS
   return hipGetLastError();
 }
-
-template hipError_t launch_attn_rows<bf16_t>(const bf16_t*, const bf16_t*, const bf16_t*,
-                                             const RowKeys&, int, int, int, int, bf16_t*, bool,
-                                             hipStream_t);
-template hipError_t launch_attn_rows<float>(const float*, const float*, const float*,
-                                            const RowKeys&, int, int, int, int, float*, bool,
-                                            hipStream_t);
 
 }  // namespace coco

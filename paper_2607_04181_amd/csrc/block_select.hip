@@ -93,15 +93,17 @@ __device__ __forceinline__ int row_keys(const RowKeys& rk, int s, int i) {
 constexpr int kScoreWaves = 4;
 constexpr int kScoreHeads = 64;  // query heads of a group at a time
 
-// Scores of a row's blocks for one kv head, 16 blocks per wave and step: lane
-// (c, j4) holds bytes 16 j4 .. of a 64-byte step of block c's summary and of
-// query head c's bytes; the product leaves blocks 4 j4 .. + 3 of head c. HS:
-// head_dim / 32 (the steps unrolled: with the sums of a loop over them read in
-// the block behind it, the compiler left too few wait states before the first).
+// Scores of a row's blocks for one kv head, 64 blocks per wave and step, all
+// loads of the first step issued before the queries are turned into bytes: lane
+// (c, j4) holds bytes 16 j4 .. of each 64-byte piece of the summaries of blocks
+// c, 16 + c, ..; the product with the same bytes of query head c leaves heads
+// 4 j4 .. + 3 of block c. HS: head_dim / 32 (the pieces unrolled: with the sums of
+// a loop over them read in the block behind it, the compiler left too few wait
+// states before the first).
 template <typename T, int HS>
 __global__ __launch_bounds__(64 * kScoreWaves) void block_score_kernel(
     const T* __restrict__ q, const int8_t* __restrict__ summary, const float* __restrict__ scales,
-    RowKeys rk, int Hq, int Hkv, uint32_t* __restrict__ keys) {
+    RowKeys rk, int Hq, int Hkv, int64_t stride, uint32_t* __restrict__ keys) {
   constexpr int hd = 32 * HS;
   __shared__ __attribute__((aligned(16))) int8_t q8[kScoreHeads][2 * hd + 16];
   __shared__ float red[kScoreWaves];
@@ -111,7 +113,26 @@ __global__ __launch_bounds__(64 * kScoreWaves) void block_score_kernel(
   const int c16 = lane & 15, j4 = lane >> 4;
   const int s = row_to_seq(rk.seq_starts, rk.n_seqs, i);
   const int nb = (row_keys(rk, s, i) + kBlockTokens - 1) / kBlockTokens;
-  if ((int)blockIdx.x * 16 * kScoreWaves >= nb) return;
+  if ((int)blockIdx.x * 64 * kScoreWaves >= nb) return;
+  const int32_t* bt = rk.block_table + (int64_t)s * rk.max_blocks;
+
+  i32x4_t sv[4][HS];
+  float sc = 0.f;
+  auto load = [&](int b0) {  // blocks b0 .. + 63 (past the end: the last)
+    int blk = bt[min(b0 + lane, nb - 1)];
+    if (blk < 0 || blk >= rk.num_blocks) blk = 0;
+    sc = scales[(int64_t)blk * Hkv + g];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int64_t at = __shfl(blk, 16 * u + c16, kWave);
+      const int8_t* sp = summary + (at * Hkv + g) * 2 * hd + 16 * j4;
+#pragma unroll
+      for (int k = 0; k < HS; ++k) sv[u][k] = *(const i32x4_t*)(sp + 64 * k);
+    }
+  };
+  const int first = (blockIdx.x * kScoreWaves + wv) * 64;
+  if (first < nb) load(first);
+
   const T* qp = q + ((int64_t)i * Hq + g * G) * hd;
   float a = 0.f;
   for (int x = threadIdx.x; x < G * hd; x += 64 * kScoreWaves)
@@ -122,52 +143,46 @@ __global__ __launch_bounds__(64 * kScoreWaves) void block_score_kernel(
 #pragma unroll
   for (int w = 0; w < kScoreWaves; ++w) a = fmaxf(a, red[w]);
   const float up = ldexpf(1.f, 7 - exponent_of(a));
-  const int32_t* bt = rk.block_table + (int64_t)s * rk.max_blocks;
-  uint32_t* out = keys + ((int64_t)i * Hkv + g) * rk.max_blocks;
+  uint32_t* out = keys + ((int64_t)i * Hkv + g) * stride;
   for (int h0 = 0; h0 < G; h0 += kScoreHeads) {
     const int heads = min(G - h0, kScoreHeads);
     const int padded = (heads + 15) / 16 * 16;
     __syncthreads();
     for (int x = threadIdx.x; x < padded * hd; x += 64 * kScoreWaves) {
       const int h = x / hd, d = x - h * hd;
-      // Columns past the group repeat its last head.
+      // Rows past the group repeat its last head.
       const float v = finite_or_0(elem(qp + (int64_t)(h0 + min(h, heads - 1)) * hd + d));
       const int b = (int)fminf(fmaxf(rintf(v * up), -127.f), 127.f);
       q8[h][d] = (int8_t)max(b, 0);
       q8[h][hd + d] = (int8_t)min(b, 0);
     }
     __syncthreads();
-    for (int b0 = (blockIdx.x * kScoreWaves + wv) * 16; b0 < nb;
-         b0 += gridDim.x * kScoreWaves * 16) {
-      int64_t blk = bt[min(b0 + c16, nb - 1)];
-      if (blk < 0 || blk >= rk.num_blocks) blk = 0;
-      const int8_t* sp = summary + (blk * Hkv + g) * 2 * hd + 16 * j4;
-      i32x4_t sv[HS];
-#pragma unroll
-      for (int k = 0; k < HS; ++k) sv[k] = *(const i32x4_t*)(sp + 64 * k);
+    for (int b0 = first; b0 < nb; b0 += gridDim.x * kScoreWaves * 64) {
+      if (h0 != 0 || b0 != first) load(b0);
       int best[4] = {INT32_MIN, INT32_MIN, INT32_MIN, INT32_MIN};
       for (int ht = 0; ht < padded; ht += 16) {
-        i32x4_t acc = {0, 0, 0, 0};
+        i32x4_t qv[HS];
 #pragma unroll
-        for (int k = 0; k < HS; ++k)
-          acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(
-              sv[k], *(const i32x4_t*)&q8[ht + c16][64 * k + 16 * j4], acc, 0, 0, 0);
+        for (int k = 0; k < HS; ++k) qv[k] = *(const i32x4_t*)&q8[ht + c16][64 * k + 16 * j4];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) best[r] = max(best[r], acc[r]);
+        for (int u = 0; u < 4; ++u) {
+          i32x4_t acc = {0, 0, 0, 0};
+#pragma unroll
+          for (int k = 0; k < HS; ++k)
+            acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(qv[k], sv[u][k], acc, 0, 0, 0);
+          best[u] = max(best[u], max(max(acc[0], acc[1]), max(acc[2], acc[3])));
+        }
       }
 #pragma unroll
-      for (int r = 0; r < 4; ++r)
-#pragma unroll
-        for (int d = 1; d < 16; d <<= 1) best[r] = max(best[r], __shfl_xor(best[r], d, kWave));
-      if (c16 < 4) {
-        const int b = b0 + 4 * j4 + c16;
-        if (b < nb) {
-          int64_t pb = bt[b];
-          if (pb < 0 || pb >= rk.num_blocks) pb = 0;
-          const int x = c16 == 0 ? best[0] : c16 == 1 ? best[1] : c16 == 2 ? best[2] : best[3];
-          const uint32_t key = order_key((float)x * scales[pb * Hkv + g]);
-          out[b] = h0 == 0 ? key : max(out[b], key);
-        }
+      for (int u = 0; u < 4; ++u) {
+        best[u] = max(best[u], __shfl_xor(best[u], 16, kWave));
+        best[u] = max(best[u], __shfl_xor(best[u], 32, kWave));
+      }
+      const int x = j4 == 0 ? best[0] : j4 == 1 ? best[1] : j4 == 2 ? best[2] : best[3];
+      const int b = b0 + lane;
+      if (b < nb) {
+        const uint32_t key = order_key((float)x * sc);
+        out[b] = h0 == 0 ? key : max(out[b], key);
       }
     }
   }
@@ -175,18 +190,44 @@ __global__ __launch_bounds__(64 * kScoreWaves) void block_score_kernel(
 
 constexpr int kSelThreads = 256;
 constexpr int kSelWaves = kSelThreads / kWave;
+constexpr int kSelKeys = 8;  // of a thread, consecutive
+constexpr int kSelChunk = kSelThreads * kSelKeys;
+
+// Inclusive sum over the workgroup's threads; red: one int per wave, free again
+// once every thread has passed the next barrier.
+__device__ __forceinline__ int sel_scan(int x, int* red, int& all) {
+  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+#pragma unroll
+  for (int d = 1; d < kWave; d <<= 1) {
+    const int y = __shfl_up(x, d, kWave);
+    if (lane >= d) x += y;
+  }
+  if (lane == kWave - 1) red[wv] = x;
+  __syncthreads();
+  all = 0;
+#pragma unroll
+  for (int w = 0; w < kSelWaves; ++w) {
+    if (w < wv) x += red[w];
+    all += red[w];
+  }
+  return x;
+}
 
 // The choice of one (row, kv head): the always attended blocks, then the
-// highest keys, ties to the lowest block; ids ascending, then -1. A radix
-// search over four bytes finds the lowest chosen key.
+// highest keys, ties to the lowest block; ids ascending, then -1. The lowest
+// chosen key is found digit by digit, 8 bits at a time from the highest bit in
+// which the keys differ, until all keys that share the digits so far are chosen;
+// a thread's consecutive keys stay in its registers where a row has no more
+// than 2048 blocks.
 __global__ __launch_bounds__(kSelThreads) void block_choose_kernel(
-    RowKeys rk, int Hkv, int keep_first, int keep_last, const uint32_t* __restrict__ keys,
-    int32_t* __restrict__ selected) {
-  __shared__ int hist[256], digit_s, above_s, sums[2 * kSelWaves];
+    RowKeys rk, int Hkv, int keep_first, int keep_last, int64_t stride,
+    const uint32_t* __restrict__ keys, int32_t* __restrict__ selected) {
+  __shared__ int hist[256], red[2][kSelWaves], digit_s, above_s, count_s;
+  __shared__ uint32_t ends[2][kSelWaves];
   const int i = blockIdx.y, g = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
   const int s = row_to_seq(rk.seq_starts, rk.n_seqs, i);
   const int nb = (row_keys(rk, s, i) + kBlockTokens - 1) / kBlockTokens;
-  const uint32_t* kp = keys + ((int64_t)i * Hkv + g) * rk.max_blocks;
+  const uint32_t* kp = keys + ((int64_t)i * Hkv + g) * stride;
   int32_t* out = selected + ((int64_t)i * Hkv + g) * rk.top;
   if (nb <= rk.top) {
     for (int x = tid; x < rk.top; x += kSelThreads) out[x] = x < nb ? x : -1;
@@ -196,60 +237,118 @@ __global__ __launch_bounds__(kSelThreads) void block_choose_kernel(
   // still has to choose among the blocks between them:
   const int lo = keep_first, hi = nb - keep_last;
   int want = rk.top - keep_first - keep_last;
+  uint32_t k[kSelKeys];
+  int held = -1;
+  auto fetch = [&](int c0) {  // the thread's keys of the chunk at block c0
+    if (held == c0) return;
+    held = c0;
+#pragma unroll
+    for (int e = 0; e < kSelKeys; e += 4) {
+      const int b = c0 + tid * kSelKeys + e;
+      u32x4_t v = {0, 0, 0, 0};
+      if (b < nb) v = *(const u32x4_t*)(kp + b);  // (rows are padded to 4 keys)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) k[e + r] = v[r];
+    }
+  };
   uint32_t prefix = 0;
+  int shift = 32;
   if (want > 0) {
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      hist[tid] = 0;
-      __syncthreads();
-      for (int b = lo + tid; b < hi; b += kSelThreads) {
-        const uint32_t k = kp[b];
-        if (shift == 24 || (k >> (shift + 8)) == (prefix >> (shift + 8)))
-          atomicAdd(&hist[(k >> shift) & 255], 1);
+    uint32_t least = ~0u, most = 0;
+    for (int c0 = 0; c0 < nb; c0 += kSelChunk) {
+      fetch(c0);
+#pragma unroll
+      for (int e = 0; e < kSelKeys; ++e) {
+        const int b = c0 + tid * kSelKeys + e;
+        if (b >= lo && b < hi) {
+          least = min(least, k[e]);
+          most = max(most, k[e]);
+        }
+      }
+    }
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) {
+      least = min(least, (uint32_t)__shfl_xor((int)least, d, kWave));
+      most = max(most, (uint32_t)__shfl_xor((int)most, d, kWave));
+    }
+    if (lane == 0) {
+      ends[0][wv] = least;
+      ends[1][wv] = most;
+    }
+    hist[tid] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kSelWaves; ++w) {
+      least = min(least, ends[0][w]);
+      most = max(most, ends[1][w]);
+    }
+    // Digits below `shift` are open; all keys agree above it.
+    shift = least == most ? 0 : 32 - __builtin_clz(least ^ most);
+    prefix = shift >= 32 ? 0 : most >> shift << shift;
+    while (shift > 0) {
+      const int top_bits = shift;
+      shift = max(shift - 8, 0);
+      for (int c0 = 0; c0 < nb; c0 += kSelChunk) {
+        fetch(c0);
+#pragma unroll
+        for (int e = 0; e < kSelKeys; ++e) {
+          const int b = c0 + tid * kSelKeys + e;
+          if (b >= lo && b < hi && (uint64_t)k[e] >> top_bits == (uint64_t)prefix >> top_bits)
+            atomicAdd(&hist[(k[e] >> shift) & ((1u << (top_bits - shift)) - 1)], 1);
+        }
       }
       __syncthreads();
-      if (tid == 0) {
-        int above = 0, d = 255;
-        for (; d > 0 && above + hist[d] < want; --d) above += hist[d];
-        digit_s = d;
-        above_s = above;
+      // From the highest digit down: the one that the last wanted key has.
+      const int mine = hist[255 - tid];
+      hist[255 - tid] = 0;
+      int all;
+      const int upto = sel_scan(mine, red[0], all);
+      if (upto >= want && upto - mine < want) {
+        digit_s = 255 - tid;
+        above_s = upto - mine;
+        count_s = mine;
       }
       __syncthreads();
       prefix |= (uint32_t)digit_s << shift;
       want -= above_s;
-      __syncthreads();
+      if (count_s == want) break;
     }
   }
-  // prefix: the lowest chosen key; want: how many of the blocks that have it.
-  const bool search = rk.top > keep_first + keep_last;
+  // Keys above prefix from bit `shift` on are chosen, and the first `want` of
+  // the blocks that equal it there.
   int placed = 0, ties = 0;
-  for (int b0 = 0; b0 < nb; b0 += kSelThreads) {
-    const int b = b0 + tid;
-    const bool always = b < lo || (b >= hi && b < nb);
-    const uint32_t k = (!always && b < nb) ? kp[b] : 0;
-    const bool tie = search && !always && b < nb && k == prefix;
-    const uint64_t tv = __ballot(tie);
-    if (lane == 0) sums[wv] = __popcll(tv);
-    __syncthreads();
-    int tr = ties;
-    for (int w = 0; w < kSelWaves; ++w) {
-      if (w < wv) tr += sums[w];
-      ties += sums[w];
+  for (int c0 = 0; c0 < nb; c0 += kSelChunk) {
+    fetch(c0);
+    uint32_t over = 0, tie = 0, always = 0;
+#pragma unroll
+    for (int e = 0; e < kSelKeys; ++e) {
+      const int b = c0 + tid * kSelKeys + e;
+      if (b >= nb) continue;
+      if (b < lo || b >= hi) {
+        always |= 1u << e;
+      } else if (shift < 32) {
+        over |= (uint32_t)(k[e] >> shift > prefix >> shift) << e;
+        tie |= (uint32_t)(k[e] >> shift == prefix >> shift) << e;
+      }
     }
-    tr += __popcll(tv & ((1ull << lane) - 1));
-    const bool take =
-        always || (search && b < nb && (k > prefix || (tie && tr < want)));
-    const uint64_t cv = __ballot(take);
-    if (lane == 0) sums[kSelWaves + wv] = __popcll(cv);
-    __syncthreads();
-    int at = placed;
-    for (int w = 0; w < kSelWaves; ++w) {
-      const int c = sums[kSelWaves + w];
-      if (w < wv) at += c;
-      placed += c;
-    }
-    at += __popcll(cv & ((1ull << lane) - 1));
-    if (take && at < rk.top) out[at] = b;
-    __syncthreads();
+    int all;
+    int rank = ties + sel_scan(__popc(tie), red[0], all) - __popc(tie);
+    ties += all;
+    uint32_t take = always | over;
+#pragma unroll
+    for (int e = 0; e < kSelKeys; ++e)
+      if (tie >> e & 1) {
+        if (rank < want) take |= 1u << e;
+        ++rank;
+      }
+    int at = placed + sel_scan(__popc(take), red[1], all) - __popc(take);
+    placed += all;
+#pragma unroll
+    for (int e = 0; e < kSelKeys; ++e)
+      if (take >> e & 1) {
+        if (at < rk.top) out[at] = c0 + tid * kSelKeys + e;
+        ++at;
+      }
   }
 }
 
@@ -277,11 +376,12 @@ hipError_t launch_block_select(const T* q, const int8_t* summary, const float* s
                                hipStream_t st) {
   if (n_rows <= 0) return hipSuccess;
   if (hd % 32 != 0 || hd > 256 || n_rows > 65535 || Hkv > 65535) return hipErrorInvalidValue;
-  const int chunks = (rk.max_blocks + 16 * kScoreWaves - 1) / (16 * kScoreWaves);
-  const dim3 grid(chunks < 64 ? chunks : 64, Hkv, n_rows);
+  const int chunks = (rk.max_blocks + 64 * kScoreWaves - 1) / (64 * kScoreWaves);
+  const dim3 grid(chunks < 16 ? chunks : 16, Hkv, n_rows);
+  const int64_t stride = select_stride(rk.max_blocks);
 #define COCO_SCORE(HS)                                                                       \
   COCO_LAUNCH((block_score_kernel<T, HS>), grid, dim3(64 * kScoreWaves), 0, st, q, summary, \
-              scales, rk, Hq, Hkv, keys)
+              scales, rk, Hq, Hkv, stride, keys)
   if constexpr (sizeof(T) == 2) {
     if (hd != 128) return hipErrorInvalidValue;
     COCO_SCORE(4);
@@ -302,7 +402,7 @@ hipError_t launch_block_select(const T* q, const int8_t* summary, const float* s
   RowKeys chosen = rk;
   chosen.selected = nullptr;
   COCO_LAUNCH(block_choose_kernel, dim3(Hkv, n_rows), dim3(kSelThreads), 0, st, chosen, Hkv,
-              keep_first, keep_last, keys, selected);
+              keep_first, keep_last, stride, keys, selected);
   return hipGetLastError();
 }
 

@@ -444,8 +444,8 @@ int coco_tree_attention(coco_layer_t H, int32_t layer, const void* q, void* o, i
                                       H->tree_part_ml, H->tree_parts, H->tree_plan, H->tree_redo,
                                       H->num_cus, st));
   else
-    HIPCHK(launch_attn_rows((const float*)q, (const float*)w.k_cache, (const float*)w.v_cache, rk,
-                            n_rows, c.n_q_heads, c.n_kv_heads, c.head_dim, (float*)o, false, st));
+    HIPCHK(launch_attn_rows_f32((const float*)q, (const float*)w.k_cache, (const float*)w.v_cache,
+                                rk, n_rows, c.n_q_heads, c.n_kv_heads, c.head_dim, (float*)o, st));
   return mark_done(H, st);
 }
 
@@ -495,9 +495,18 @@ int coco_sparse_reserve(coco_layer_t H, int32_t max_rows, int32_t max_blocks) {
   const int rows = max_rows > H->sparse_rows ? max_rows : H->sparse_rows;
   const int top = max_blocks > H->sparse_top ? max_blocks : H->sparse_top;
   const coco_layer_config& c = H->cfg;
-  const int rc = grow(H, &H->sparse_keys, &H->sparse_keys_bytes,
-                      (size_t)rows * c.n_kv_heads * c.max_blocks_per_seq * 4);
+  const size_t keys =
+      align256((size_t)rows * c.n_kv_heads * select_stride(c.max_blocks_per_seq) * 4);
+  // fp32 handles attend a list whole.
+  const size_t parts = c.dtype == COCO_BF16 && sparse_parts(top) > 1
+                           ? (size_t)rows * c.n_q_heads * sparse_parts(top)
+                           : 0;
+  const size_t part_o = parts * c.head_dim * 4;
+  const int rc = grow(H, &H->sparse_ws, &H->sparse_bytes, keys + part_o + parts * 8);
   if (rc) return rc;
+  H->sparse_keys = (uint32_t*)H->sparse_ws;
+  H->sparse_part_o = (float*)(H->sparse_ws + keys);
+  H->sparse_part_ml = (float*)(H->sparse_ws + keys + part_o);
   H->sparse_rows = rows;
   H->sparse_top = top;
   return COCO_OK;
@@ -544,11 +553,11 @@ int coco_block_select(coco_layer_t H, const int8_t* summary, const float* scales
   if (c.dtype == COCO_BF16)
     HIPCHK(launch_block_select((const bf16_t*)q, summary, scales, rk, n_rows, c.n_q_heads,
                                c.n_kv_heads, c.head_dim, keep_first, keep_last,
-                               (uint32_t*)H->sparse_keys, selected, st));
+                               H->sparse_keys, selected, st));
   else
     HIPCHK(launch_block_select((const float*)q, summary, scales, rk, n_rows, c.n_q_heads,
                                c.n_kv_heads, c.head_dim, keep_first, keep_last,
-                               (uint32_t*)H->sparse_keys, selected, st));
+                               H->sparse_keys, selected, st));
   return mark_done(H, st);
 }
 
@@ -603,12 +612,13 @@ int coco_sparse_attention(coco_layer_t H, int32_t layer, const void* q, void* o,
   rk.selected = selected;
   rk.top = n_select;
   if (c.dtype == COCO_BF16)
-    HIPCHK(launch_attn_rows((const bf16_t*)q, (const bf16_t*)w.k_cache, (const bf16_t*)w.v_cache,
-                            rk, n_rows, c.n_q_heads, c.n_kv_heads, c.head_dim, (bf16_t*)o, false,
-                            st));
+    HIPCHK(launch_sparse_attention_bf16((const bf16_t*)q, (const bf16_t*)w.k_cache,
+                                        (const bf16_t*)w.v_cache, rk, n_rows, c.n_q_heads,
+                                        c.n_kv_heads, (bf16_t*)o, H->sparse_part_o,
+                                        H->sparse_part_ml, st));
   else
-    HIPCHK(launch_attn_rows((const float*)q, (const float*)w.k_cache, (const float*)w.v_cache, rk,
-                            n_rows, c.n_q_heads, c.n_kv_heads, c.head_dim, (float*)o, false, st));
+    HIPCHK(launch_attn_rows_f32((const float*)q, (const float*)w.k_cache, (const float*)w.v_cache,
+                                rk, n_rows, c.n_q_heads, c.n_kv_heads, c.head_dim, (float*)o, st));
   return mark_done(H, st);
 }
 

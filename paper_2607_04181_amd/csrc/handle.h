@@ -94,11 +94,13 @@ struct coco_layer {
   // buffers (in `extra`, which keeps outgrown ones until destroy).
   int tree_rows = 0, tree_seqs = 0;
   int sparse_rows = 0, sparse_top = 0;
-  char *tree_ws = nullptr, *sparse_keys = nullptr;
-  size_t tree_bytes = 0, sparse_keys_bytes = 0;
+  char *tree_ws = nullptr, *sparse_ws = nullptr;
+  size_t tree_bytes = 0, sparse_bytes = 0;
   float *tree_part_o = nullptr, *tree_part_ml = nullptr;
   int64_t tree_parts = 0;
   int32_t *tree_plan = nullptr, *tree_redo = nullptr;
+  float *sparse_part_o = nullptr, *sparse_part_ml = nullptr;
+  uint32_t* sparse_keys = nullptr;
   std::vector<char*> extra;
 };
 

@@ -333,11 +333,20 @@ struct RowKeys {
   const int32_t* selected = nullptr;    // blocks: [rows][Hkv][top], -1: none
   int top = 0;
 };
-// o [rows][Hq][hd], or (bf16) in tile order.
-template <typename T>
-hipError_t launch_attn_rows(const T* q, const T* k_cache, const T* v_cache, const RowKeys& rk,
-                            int n_rows, int Hq, int Hkv, int hd, T* o, bool tiled,
-                            hipStream_t st);
+// fp32 handles, tree and blocks. q, o [rows][Hq][hd].
+hipError_t launch_attn_rows_f32(const float* q, const float* k_cache, const float* v_cache,
+                                const RowKeys& rk, int n_rows, int Hq, int Hkv, int hd, float* o,
+                                hipStream_t st);
+
+// Blocks, bf16 handles (hd 128, up to 16 query heads in a group). A list of top
+// entries is attended in sparse_parts(top) parts; with more than one,
+// part_o [rows][Hkv][parts][Hq / Hkv][128] and part_ml [..][2] hold them.
+constexpr int kSparsePart = 32;
+inline int sparse_parts(int top) { return (top + kSparsePart - 1) / kSparsePart; }
+hipError_t launch_sparse_attention_bf16(const uint16_t* q, const uint16_t* k_cache,
+                                        const uint16_t* v_cache, const RowKeys& rk, int n_rows,
+                                        int Hq, int Hkv, uint16_t* o, float* part_o,
+                                        float* part_ml, hipStream_t st);
 
 // Tree rows of bf16 handles (hd 128). The keys of a sequence are split into
 // at most kTreeSplitsFew parts where it has at most 128 columns (nodes times
@@ -362,7 +371,8 @@ hipError_t launch_summarize(const T* k_cache, int Hkv, int hd, const int32_t* bl
                             const int32_t* ctx_lens, int8_t* summary, float* scales, int num_cus,
                             hipStream_t st);
 // Scores of every block a row can choose, as order-preserving keys
-// [rows][Hkv][max_blocks], then the choice.
+// [rows][Hkv][select_stride(max_blocks)], then the choice.
+inline int64_t select_stride(int max_blocks) { return ((int64_t)max_blocks + 3) / 4 * 4; }
 template <typename T>
 hipError_t launch_block_select(const T* q, const int8_t* summary, const float* scales,
                                const RowKeys& rk, int n_rows, int Hq, int Hkv, int hd,
