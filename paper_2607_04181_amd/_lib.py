@@ -143,7 +143,7 @@ def _ptr(t, dtype=None, what="tensor"):
         return None
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{what} must be a torch tensor")
-    if t.device.type != "cuda":
+    if not t.is_cuda:
         raise ValueError(f"{what} must be on the GPU")
     if not t.is_contiguous():
         raise ValueError(f"{what} must be contiguous")
@@ -153,8 +153,8 @@ def _ptr(t, dtype=None, what="tensor"):
 
 
 def _stream(stream):
-    if stream is None:
-        stream = torch.cuda.current_stream()
+    if stream is None:  # without the Stream object of torch.cuda.current_stream(): 2 us a call
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
     return stream.cuda_stream if isinstance(stream, torch.cuda.Stream) else stream
 
 
@@ -310,21 +310,23 @@ def coco_layer_span_forward(h: Handle, first_layer: int, n_layers: int, hidden, 
 
 
 def _check_table(h: Handle, block_table, n_seqs=None):
-    _shape_check(isinstance(block_table, torch.Tensor) and block_table.dim() == 2 and
-                 block_table.shape[1] == h.cfg.max_blocks_per_seq,
-                 f"block_table must be [n_seqs, {h.cfg.max_blocks_per_seq}]")
-    _shape_check(n_seqs is None or block_table.shape[0] >= n_seqs,
-                 f"block_table has {block_table.shape[0]} rows for {n_seqs} sequences")
+    width = h.cfg.max_blocks_per_seq
+    if not (isinstance(block_table, torch.Tensor) and block_table.dim() == 2 and
+            block_table.shape[1] == width):
+        raise ValueError(f"block_table must be [n_seqs, {width}]")
+    if n_seqs is not None and block_table.shape[0] < n_seqs:
+        raise ValueError(f"block_table has {block_table.shape[0]} rows for {n_seqs} sequences")
 
 
 def _check_len(name: str, t, n: int):
-    _shape_check(isinstance(t, torch.Tensor) and t.numel() == n, f"{name} must have {n} entries")
+    if not (isinstance(t, torch.Tensor) and t.numel() == n):
+        raise ValueError(f"{name} must have {n} entries")
 
 
 def _check_counts(h: Handle, ref_counts):
     n = min(h.num_blocks, default=0)
-    _shape_check(isinstance(ref_counts, torch.Tensor) and ref_counts.numel() >= n,
-                 f"ref_counts must have {n} entries, one per block")
+    if not (isinstance(ref_counts, torch.Tensor) and ref_counts.numel() >= n):
+        raise ValueError(f"ref_counts must have {n} entries, one per block")
 
 
 def coco_kv_alloc(h: Handle, seq_idx, lens, block_table, ref_counts, status, stream=None):
@@ -396,9 +398,16 @@ def _check_heads(h: Handle, name: str, t):
     cfg = h.cfg
     if not isinstance(t, torch.Tensor) or t.dtype != _elem_dtype(cfg):
         raise TypeError(f"{name} must be a {_elem_dtype(cfg)} tensor")
-    _shape_check(t.dim() >= 2 and t.numel() == t.shape[0] * cfg.n_q_heads * cfg.head_dim,
-                 f"{name} must be [rows, {cfg.n_q_heads}, {cfg.head_dim}], got {tuple(t.shape)}")
-    return int(t.shape[0])
+    n = t.shape[0] if t.dim() >= 2 else -1
+    if t.numel() != n * cfg.n_q_heads * cfg.head_dim:
+        raise ValueError(f"{name} must be [rows, {cfg.n_q_heads}, {cfg.head_dim}], "
+                         f"got {tuple(t.shape)}")
+    return n
+
+
+def _check_out(h: Handle, o, n: int):
+    if _check_heads(h, "o", o) != n:
+        raise ValueError(f"o must have {n} rows")
 
 
 def coco_tree_reserve(h: Handle, max_rows: int, max_seqs: int) -> None:
@@ -410,12 +419,13 @@ def coco_tree_attention(h: Handle, layer: int, q, o, seq_starts, block_table, ct
     """tree_mask: int64 [rows, words]."""
     i32 = torch.int32
     n = _check_heads(h, "q", q)
-    _shape_check(_check_heads(h, "o", o) == n, f"o must have {n} rows")
+    _check_out(h, o, n)
     n_seqs = int(ctx_lens.numel())
     _check_len("seq_starts", seq_starts, n_seqs + 1)
     _check_table(h, block_table, n_seqs)
-    _shape_check(isinstance(tree_mask, torch.Tensor) and tree_mask.dim() == 2 and
-                 tree_mask.shape[0] == n, f"tree_mask must be [{n}, words]")
+    if not (isinstance(tree_mask, torch.Tensor) and tree_mask.dim() == 2 and
+            tree_mask.shape[0] == n):
+        raise ValueError(f"tree_mask must be [{n}, words]")
     _check(_lib.coco_tree_attention(
         h.raw, layer, _ptr(q, what="q"), _ptr(o, what="o"), n, _ptr(seq_starts, i32, "seq_starts"),
         n_seqs, _ptr(block_table, i32, "block_table"), _ptr(ctx_lens, i32, "ctx_lens"),
@@ -424,9 +434,9 @@ def coco_tree_attention(h: Handle, layer: int, q, o, seq_starts, block_table, ct
 
 def _check_summary(h: Handle, summary, scales):
     cfg = h.cfg
-    _shape_check(isinstance(summary, torch.Tensor) and summary.dim() == 4 and
-                 tuple(summary.shape[1:]) == (cfg.n_kv_heads, 2, cfg.head_dim),
-                 f"summary must be [num_blocks, {cfg.n_kv_heads}, 2, {cfg.head_dim}]")
+    if not (isinstance(summary, torch.Tensor) and summary.dim() == 4 and
+            summary.shape[1:] == (cfg.n_kv_heads, 2, cfg.head_dim)):
+        raise ValueError(f"summary must be [num_blocks, {cfg.n_kv_heads}, 2, {cfg.head_dim}]")
     _check_len("scales", scales, summary.shape[0] * cfg.n_kv_heads)
 
 
@@ -437,7 +447,8 @@ def coco_kv_summarize(h: Handle, layer: int, summary, scales, first_lens, ctx_le
     n_seqs = int(ctx_lens.numel())
     _check_summary(h, summary, scales)
     blocks = h.num_blocks[layer] if 0 <= layer < len(h.num_blocks) else 0
-    _shape_check(summary.shape[0] >= blocks, f"summary must have the layer's {blocks} blocks")
+    if summary.shape[0] < blocks:
+        raise ValueError(f"summary must have the layer's {blocks} blocks")
     if first_lens is not None:
         _check_len("first_lens", first_lens, n_seqs)
     _check_table(h, block_table, n_seqs)
@@ -452,9 +463,9 @@ def coco_sparse_reserve(h: Handle, max_rows: int, max_blocks: int) -> None:
 
 
 def _check_selected(h: Handle, selected, n: int) -> int:
-    _shape_check(isinstance(selected, torch.Tensor) and selected.dim() == 3 and
-                 tuple(selected.shape[:2]) == (n, h.cfg.n_kv_heads),
-                 f"selected must be [{n}, {h.cfg.n_kv_heads}, blocks]")
+    if not (isinstance(selected, torch.Tensor) and selected.dim() == 3 and
+            selected.shape[:2] == (n, h.cfg.n_kv_heads)):
+        raise ValueError(f"selected must be [{n}, {h.cfg.n_kv_heads}, blocks]")
     return int(selected.shape[2])
 
 
@@ -462,7 +473,8 @@ def _check_row_arrays(h: Handle, n: int, positions, seq_starts, block_table, ctx
     _check_len("positions", positions, n)
     n_seqs = int(ctx_lens.numel())
     if seq_starts is None:
-        _shape_check(n_seqs == n, f"ctx_lens has {n_seqs} entries for {n} rows")
+        if n_seqs != n:
+            raise ValueError(f"ctx_lens has {n_seqs} entries for {n} rows")
     else:
         _check_len("seq_starts", seq_starts, n_seqs + 1)
     _check_table(h, block_table, n_seqs)
@@ -488,7 +500,7 @@ def coco_sparse_attention(h: Handle, layer: int, q, o, positions, seq_starts, bl
                           ctx_lens, selected, stream=None):
     i32 = torch.int32
     n = _check_heads(h, "q", q)
-    _shape_check(_check_heads(h, "o", o) == n, f"o must have {n} rows")
+    _check_out(h, o, n)
     n_seqs = _check_row_arrays(h, n, positions, seq_starts, block_table, ctx_lens)
     n_select = _check_selected(h, selected, n)
     _check(_lib.coco_sparse_attention(

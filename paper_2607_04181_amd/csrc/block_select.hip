@@ -33,15 +33,76 @@ __device__ __forceinline__ int exponent_of(float a) {
   return min(100, max(-100, x));
 }
 
-// Bytes of one wave's summary: lane l holds dims l, l + 64, ..
-template <typename T>
+// The value of the lane whose index differs in bit BIT, and for 4 in bits 2 to 0
+// (a mirror of eight lanes).
+template <int BIT>
+__device__ __forceinline__ float swap_lanes(float x) {
+  constexpr int ctrl = BIT == 8 ? 0x128 : BIT == 4 ? 0x141 : BIT == 2 ? 0x4E : 0xB1;
+  return __int_as_float(
+      __builtin_amdgcn_update_dpp(0, __float_as_int(x), ctrl, 0xF, 0xF, false));
+}
+
+// One step of the largest and smallest of N values over 16 lanes: a lane gives
+// one half of its values away and keeps the other (N even), or keeps all.
+// Pairs of lanes hold the same values up to here. FIRST: hi and lo are one.
+template <int BIT, int N, bool FIRST>
+__device__ __forceinline__ void spread_step(float* hi, float* lo, int lane, int& base) {
+  if constexpr (N % 2 != 0) {
+#pragma unroll
+    for (int v = 0; v < N; ++v) {
+      hi[v] = fmaxf(hi[v], swap_lanes<BIT>(hi[v]));
+      lo[v] = fminf(lo[v], swap_lanes<BIT>(lo[v]));
+    }
+  } else {
+    const bool up = lane & BIT;
+    base += up ? N / 2 : 0;
+#pragma unroll
+    for (int v = 0; v < N / 2; ++v) {
+      const float got = swap_lanes<BIT>(up ? hi[v] : hi[v + N / 2]);
+      const float own = up ? hi[v + N / 2] : hi[v];
+      if constexpr (FIRST) {
+        hi[v] = fmaxf(own, got);
+        lo[v] = fminf(own, got);
+      } else {
+        const float got2 = swap_lanes<BIT>(up ? lo[v] : lo[v + N / 2]);
+        const float own2 = up ? lo[v + N / 2] : lo[v];
+        hi[v] = fmaxf(own, got);
+        lo[v] = fminf(own2, got2);
+      }
+    }
+  }
+}
+
+__device__ __forceinline__ void load8(const float* p, float* x) {
+  const f32x4_t a = *(const f32x4_t*)p, b = *(const f32x4_t*)(p + 4);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[i] = finite_or_0(a[i]);
+    x[4 + i] = finite_or_0(b[i]);
+  }
+}
+__device__ __forceinline__ void load8(const bf16_t* p, float* x) {
+  const u32x4_t a = *(const u32x4_t*)p;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[2 * i] = finite_or_0(bf16_to_f32(a[i] & 0xFFFFu));
+    x[2 * i + 1] = finite_or_0(__uint_as_float(a[i] & 0xFFFF0000u));
+  }
+}
+
+// A tile's summary by one wave: lane (t, j4) reads token t's dims 32 p + 8 j4 ..
+// + 7 as they lie, and the 16 lanes of a j4 halve what they hold in each step of
+// the reduction over tokens. HS: head_dim / 32.
+template <typename T, int HS>
 __global__ __launch_bounds__(256) void summarize_kernel(
-    const T* __restrict__ k_cache, int Hkv, int hd, const int32_t* __restrict__ block_table,
+    const T* __restrict__ k_cache, int Hkv, const int32_t* __restrict__ block_table,
     int max_blocks, int64_t num_blocks, const int32_t* __restrict__ first,
     const int32_t* __restrict__ ctx_lens, int8_t* __restrict__ summary,
     float* __restrict__ scales) {
+  constexpr int hd = 32 * HS, V = 8 * HS;
+  constexpr int V1 = V / 2, V2 = V1 / 2, V3 = V2 / 2, V4 = V3 % 2 ? V3 : V3 / 2;
   const int s = blockIdx.y;
-  const int lane = threadIdx.x & 63;
+  const int lane = threadIdx.x & 63, j4 = lane >> 4;
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = min(ctx_lens[s], max_blocks * kBlockTokens);
   const int b0 = first ? max(first[s], 0) / kBlockTokens : 0;
@@ -50,31 +111,40 @@ __global__ __launch_bounds__(256) void summarize_kernel(
     const int b = b0 + it / Hkv, g = it % Hkv;
     const int64_t blk = block_table[(int64_t)s * max_blocks + b];
     if (blk < 0 || blk >= num_blocks) continue;
-    const int left = min(n - b * kBlockTokens, kBlockTokens);
-    const T* tile = k_cache + (blk * Hkv + g) * (int64_t)(kBlockTokens * hd);
-    float hi[4], lo[4], a = 0.f;
+    // Lanes past the last token repeat it.
+    const int t = min(lane & 15, n - b * kBlockTokens - 1);
+    const T* tile = k_cache + (blk * Hkv + g) * (int64_t)(kBlockTokens * hd) + (j4 * 16 + t) * 8;
+    float hi[V], lo[V1];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int h = lane + 64 * u;
-      hi[u] = -INFINITY;
-      lo[u] = INFINITY;
-      if (h >= hd) continue;
-      for (int t = 0; t < left; ++t) {
-        const float x = finite_or_0(elem(tile + k_tile_offset(t, h)));
-        hi[u] = fmaxf(hi[u], x);
-        lo[u] = fminf(lo[u], x);
-      }
-      a = fmaxf(a, fmaxf(fabsf(hi[u]), fabsf(lo[u])));
-    }
+    for (int p = 0; p < HS; ++p) load8(tile + 512 * p, hi + 8 * p);
+    int base = 0;  // the lane's values are V4 from here on, value 8 p + e dim 32 p + 8 j4 + e
+    spread_step<8, V, true>(hi, lo, lane, base);
+    spread_step<4, V1, false>(hi, lo, lane, base);
+    spread_step<2, V2, false>(hi, lo, lane, base);
+    spread_step<1, V3, false>(hi, lo, lane, base);
+    float a = 0.f;
+#pragma unroll
+    for (int v = 0; v < V4; ++v) a = fmaxf(a, fmaxf(fabsf(hi[v]), fabsf(lo[v])));
     const int x = exponent_of(wave_max(a));
     const float up = ldexpf(1.f, 7 - x);
     int8_t* out = summary + (blk * Hkv + g) * 2 * hd;
+    int bh[V4], bl[V4];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int h = lane + 64 * u;
-      if (h >= hd) continue;
-      out[h] = (int8_t)fminf(fmaxf(ceilf(hi[u] * up), -127.f), 127.f);
-      out[hd + h] = (int8_t)fminf(fmaxf(floorf(lo[u] * up), -127.f), 127.f);
+    for (int v = 0; v < V4; ++v) {
+      bh[v] = (int)fminf(fmaxf(ceilf(hi[v] * up), -127.f), 127.f);
+      bl[v] = (int)fminf(fmaxf(floorf(lo[v] * up), -127.f), 127.f);
+    }
+    const int d0 = 8 * j4 + (base >> 3) * 32 + (base & 7);
+    if constexpr (V4 == 2) {
+      *(uint16_t*)(out + d0) = (uint16_t)((bh[0] & 0xFF) | (bh[1] & 0xFF) << 8);
+      *(uint16_t*)(out + hd + d0) = (uint16_t)((bl[0] & 0xFF) | (bl[1] & 0xFF) << 8);
+    } else {
+#pragma unroll
+      for (int v = 0; v < V4; ++v) {
+        const int d = 8 * j4 + ((base + v) >> 3) * 32 + ((base + v) & 7);
+        out[d] = (int8_t)bh[v];
+        out[hd + d] = (int8_t)bl[v];
+      }
     }
     if (lane == 0) scales[blk * Hkv + g] = ldexpf(1.f, x - 7);
   }
@@ -354,6 +424,26 @@ __global__ __launch_bounds__(kSelThreads) void block_choose_kernel(
 
 }  // namespace
 
+#define COCO_BY_HEAD_DIM(KERNEL)             \
+  do {                                       \
+    if constexpr (sizeof(T) == 2) {          \
+      if (hd != 128) return hipErrorInvalidValue; \
+      KERNEL(4);                             \
+    } else {                                 \
+      switch (hd / 32) {                     \
+        case 1: KERNEL(1); break;            \
+        case 2: KERNEL(2); break;            \
+        case 3: KERNEL(3); break;            \
+        case 4: KERNEL(4); break;            \
+        case 5: KERNEL(5); break;            \
+        case 6: KERNEL(6); break;            \
+        case 7: KERNEL(7); break;            \
+        case 8: KERNEL(8); break;            \
+        default: return hipErrorInvalidValue; \
+      }                                      \
+    }                                        \
+  } while (0)
+
 template <typename T>
 hipError_t launch_summarize(const T* k_cache, int Hkv, int hd, const int32_t* block_table,
                             int n_seqs, int max_blocks, int64_t num_blocks, const int32_t* first,
@@ -363,9 +453,12 @@ hipError_t launch_summarize(const T* k_cache, int Hkv, int hd, const int32_t* bl
   if (hd % 32 != 0 || hd > 256 || n_seqs > 65535) return hipErrorInvalidValue;
   const int64_t most = ((int64_t)max_blocks * Hkv + 3) / 4;
   const int64_t fill = (16LL * num_cus + n_seqs - 1) / n_seqs;
-  COCO_LAUNCH((summarize_kernel<T>), dim3((unsigned)(most < fill ? most : fill), n_seqs),
-              dim3(256), 0, st, k_cache, Hkv, hd, block_table, max_blocks, num_blocks, first,
-              ctx_lens, summary, scales);
+  const dim3 grid((unsigned)(most < fill ? most : fill), n_seqs);
+#define COCO_SUMMARY(HS)                                                                    \
+  COCO_LAUNCH((summarize_kernel<T, HS>), grid, dim3(256), 0, st, k_cache, Hkv, block_table, \
+              max_blocks, num_blocks, first, ctx_lens, summary, scales)
+  COCO_BY_HEAD_DIM(COCO_SUMMARY);
+#undef COCO_SUMMARY
   return hipGetLastError();
 }
 
@@ -382,22 +475,7 @@ hipError_t launch_block_select(const T* q, const int8_t* summary, const float* s
 #define COCO_SCORE(HS)                                                                       \
   COCO_LAUNCH((block_score_kernel<T, HS>), grid, dim3(64 * kScoreWaves), 0, st, q, summary, \
               scales, rk, Hq, Hkv, stride, keys)
-  if constexpr (sizeof(T) == 2) {
-    if (hd != 128) return hipErrorInvalidValue;
-    COCO_SCORE(4);
-  } else {
-    switch (hd) {
-      case 32: COCO_SCORE(1); break;
-      case 64: COCO_SCORE(2); break;
-      case 96: COCO_SCORE(3); break;
-      case 128: COCO_SCORE(4); break;
-      case 160: COCO_SCORE(5); break;
-      case 192: COCO_SCORE(6); break;
-      case 224: COCO_SCORE(7); break;
-      case 256: COCO_SCORE(8); break;
-      default: return hipErrorInvalidValue;
-    }
-  }
+  COCO_BY_HEAD_DIM(COCO_SCORE);
 #undef COCO_SCORE
   RowKeys chosen = rk;
   chosen.selected = nullptr;
@@ -416,5 +494,6 @@ hipError_t launch_block_select(const T* q, const int8_t* summary, const float* s
 COCO_INST(bf16_t)
 COCO_INST(float)
 #undef COCO_INST
+#undef COCO_BY_HEAD_DIM
 
 }  // namespace coco
