@@ -424,26 +424,6 @@ __global__ __launch_bounds__(kSelThreads) void block_choose_kernel(
 
 }  // namespace
 
-#define COCO_BY_HEAD_DIM(KERNEL)             \
-  do {                                       \
-    if constexpr (sizeof(T) == 2) {          \
-      if (hd != 128) return hipErrorInvalidValue; \
-      KERNEL(4);                             \
-    } else {                                 \
-      switch (hd / 32) {                     \
-        case 1: KERNEL(1); break;            \
-        case 2: KERNEL(2); break;            \
-        case 3: KERNEL(3); break;            \
-        case 4: KERNEL(4); break;            \
-        case 5: KERNEL(5); break;            \
-        case 6: KERNEL(6); break;            \
-        case 7: KERNEL(7); break;            \
-        case 8: KERNEL(8); break;            \
-        default: return hipErrorInvalidValue; \
-      }                                      \
-    }                                        \
-  } while (0)
-
 template <typename T>
 hipError_t launch_summarize(const T* k_cache, int Hkv, int hd, const int32_t* block_table,
                             int n_seqs, int max_blocks, int64_t num_blocks, const int32_t* first,
@@ -494,6 +474,5 @@ hipError_t launch_block_select(const T* q, const int8_t* summary, const float* s
 COCO_INST(bf16_t)
 COCO_INST(float)
 #undef COCO_INST
-#undef COCO_BY_HEAD_DIM
 
 }  // namespace coco

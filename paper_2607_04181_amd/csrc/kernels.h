@@ -23,6 +23,28 @@ LaunchEvents& launch_events();
     le_ = ::coco::LaunchEvents{};                                                             \
   } while (0)
 
+// KERNEL(head_dim / 32) for a handle of type T: bf16 has one head_dim, fp32 the
+// multiples of 32 up to 256.
+#define COCO_BY_HEAD_DIM(KERNEL)                  \
+  do {                                            \
+    if constexpr (sizeof(T) == 2) {               \
+      if (hd != 128) return hipErrorInvalidValue; \
+      KERNEL(4);                                  \
+    } else {                                      \
+      switch (hd / 32) {                          \
+        case 1: KERNEL(1); break;                 \
+        case 2: KERNEL(2); break;                 \
+        case 3: KERNEL(3); break;                 \
+        case 4: KERNEL(4); break;                 \
+        case 5: KERNEL(5); break;                 \
+        case 6: KERNEL(6); break;                 \
+        case 7: KERNEL(7); break;                 \
+        case 8: KERNEL(8); break;                 \
+        default: return hipErrorInvalidValue;     \
+      }                                           \
+    }                                             \
+  } while (0)
+
 // ---------------------------------------------------------------- row kernels
 // Prefill row slots (optional output of the gather kernel): row_info[2i] =
 // positions[i] clamped to [0, rope_rows), row_info[2i + 1] = the cache block

@@ -17,7 +17,8 @@ namespace {
 
 constexpr int kPlanThreads = 1024;
 constexpr int kPlanWaves = kPlanThreads / kWave;
-constexpr int kPlanIds = 8;  // blocks a thread looks at per round
+constexpr int kPlanIds = 16;      // consecutive blocks a thread looks at per round
+constexpr int kPlanEntries = 8;   // table entries a lane reads at a time
 
 // Inclusive sum over a wave's lanes.
 __device__ __forceinline__ int wave_scan(int x) {
@@ -41,85 +42,92 @@ __device__ __forceinline__ bool page_request_ok(const PageArgs& a, int i) {
   return src >= 0 && src < a.n_seqs && src != row;
 }
 
+// Exclusive sum over the workgroup's threads, and the whole. Its barriers also
+// keep one call's sums from the next's.
+__device__ __forceinline__ int plan_scan(int x, int* sums, int& all) {
+  const int lane = threadIdx.x & 63;
+  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int upto = wave_scan(x);
+  __syncthreads();
+  if (lane == kWave - 1) sums[wv] = upto;
+  __syncthreads();
+  int before = 0;
+  all = 0;
+#pragma unroll
+  for (int w = 0; w < kPlanWaves; ++w) {
+    const int c = sums[w];
+    if (w < wv) before += c;
+    all += c;
+  }
+  return before + upto - x;
+}
+
 __global__ __launch_bounds__(kPlanThreads) void page_plan_kernel(PageArgs a) {
-  __shared__ int sums[kPlanIds * kPlanWaves];
-  __shared__ int carry;
-  const int tid = threadIdx.x, lane = tid & 63;
-  const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
-  // What each request needs, into off[].
-  if (a.src != nullptr) {
-    for (int i = tid; i < a.n; i += kPlanThreads)
-      a.off[i] = page_request_ok(a, i) ? (a.lens[i] % kBlockTokens != 0) : -1;
-  } else {
-    for (int i = wv; i < a.n; i += kPlanWaves) {
-      int need = -1;
-      if (page_request_ok(a, i)) {
+  __shared__ int sums[kPlanWaves];
+  const int tid = threadIdx.x;
+  if (a.src == nullptr) {
+    // What each request needs, into off[]: a wave per request, or 16 lanes
+    // where there are more requests than waves (reads in flight, not lanes, are
+    // what the scan of a table row lacks).
+    const int lanes = a.n > kPlanWaves ? 16 : kWave;
+    const int at = tid & (lanes - 1);
+    for (int i = tid / lanes; i < a.n; i += kPlanThreads / lanes) {
+      const bool ok = page_request_ok(a, i);
+      int c = 0;
+      if (ok) {
         const int nb = (a.lens[i] + kBlockTokens - 1) / kBlockTokens;
         const int32_t* bt = a.table + (int64_t)a.dst[i] * a.max_blocks;
-        int c = 0;
-        for (int b = lane; b < nb; b += kWave) c += bt[b] < 0;
-        need = __shfl(wave_scan(c), kWave - 1, kWave);
+        for (int b0 = at; b0 < nb; b0 += lanes * kPlanEntries) {
+          int e[kPlanEntries];
+#pragma unroll
+          for (int u = 0; u < kPlanEntries; ++u) e[u] = bt[min(b0 + u * lanes, nb - 1)];
+#pragma unroll
+          for (int u = 0; u < kPlanEntries; ++u) c += b0 + u * lanes < nb && e[u] < 0;
+        }
       }
-      if (lane == 0) a.off[i] = need;
+      for (int d = 1; d < lanes; d <<= 1) c += __shfl_xor(c, d, kWave);
+      if (at == 0) a.off[i] = ok ? c : -1;
     }
+    __syncthreads();
   }
-  if (tid == 0) carry = 0;
-  __syncthreads();
   // Their places in the list, in request order (off[] becomes the exclusive
-  // sum, off[n] the whole), and in status[] what each needs.
+  // sum), and in status[] what each needs.
+  int total = 0;
   for (int i0 = 0; i0 < a.n; i0 += kPlanThreads) {
     const int i = i0 + tid;
-    const int need = i < a.n ? a.off[i] : 0;
-    const int x = need > 0 ? need : 0;
-    const int s = wave_scan(x);
-    if (lane == kWave - 1) sums[wv] = s;
-    __syncthreads();
-    int before = carry;
-    for (int w = 0; w < wv; ++w) before += sums[w];
+    int need = 0;
     if (i < a.n) {
-      a.off[i] = before + s - x;
+      if (a.src == nullptr)
+        need = a.off[i];
+      else
+        need = page_request_ok(a, i) ? (a.lens[i] % kBlockTokens != 0) : -1;
+    }
+    int all;
+    const int before = plan_scan(max(need, 0), sums, all);
+    if (i < a.n) {
+      a.off[i] = total + before;
       a.status[i] = need;
     }
-    __syncthreads();
-    if (tid == kPlanThreads - 1) carry = before + s;
-    __syncthreads();
+    total += all;
   }
-  const int total = carry;
   // The free blocks of lowest id, as many as are needed.
   int found = 0;
   for (int64_t base = 0; base < a.num_blocks && found < total;
        base += kPlanThreads * kPlanIds) {
-    bool free_blk[kPlanIds];
+    const int64_t first = base + tid * kPlanIds;
+    int32_t r[kPlanIds];
 #pragma unroll
-    for (int u = 0; u < kPlanIds; ++u) {
-      const int64_t id = base + u * kPlanThreads + tid;
-      free_blk[u] = id < a.num_blocks && a.refs[id] == 0;
-    }
-    uint64_t votes[kPlanIds];
+    for (int u = 0; u < kPlanIds; ++u)
+      r[u] = a.refs[first + u < a.num_blocks ? first + u : a.num_blocks - 1];
+    uint32_t free_ids = 0;
 #pragma unroll
-    for (int u = 0; u < kPlanIds; ++u) {
-      votes[u] = __ballot(free_blk[u]);
-      if (lane == 0) sums[u * kPlanWaves + wv] = __popcll(votes[u]);
-    }
-    __syncthreads();
-    // Each thread sums what lies before its own eight places.
-    int place[kPlanIds], at = found;
-#pragma unroll
-    for (int u = 0; u < kPlanIds; ++u) {
-      place[u] = at;
-      for (int w = 0; w < kPlanWaves; ++w) {
-        const int c = sums[u * kPlanWaves + w];
-        if (w < wv) place[u] += c;
-        at += c;
-      }
-    }
-#pragma unroll
-    for (int u = 0; u < kPlanIds; ++u) {
-      const int p = place[u] + __popcll(votes[u] & ((1ull << lane) - 1));
-      if (free_blk[u] && p < total) a.list[p] = (int)(base + u * kPlanThreads + tid);
-    }
-    found = at;
-    __syncthreads();
+    for (int u = 0; u < kPlanIds; ++u)
+      free_ids |= (uint32_t)(first + u < a.num_blocks && r[u] == 0) << u;
+    int all;
+    int place = found + plan_scan(__popc(free_ids), sums, all);
+    for (; free_ids && place < total; free_ids &= free_ids - 1)
+      a.list[place++] = (int)(first + __builtin_ctz(free_ids));
+    found += all;
   }
   // A request is served while those up to it fit.
   for (int i = tid; i < a.n; i += kPlanThreads) {
@@ -214,22 +222,26 @@ __global__ __launch_bounds__(256) void page_copy_kernel(const int32_t* __restric
 // Tokens kept[starts[i] ..] of row seq[i] to positions base[i], base[i] + 1,
 // ... of it, for one head of one pool: 16 at a time through registers. A token
 // never moves up (kept[k] >= base + k, ascending), so no group writes where a
-// later one still reads.
-template <typename T>
+// later one still reads. A key tile holds 8 dims of a token together and moves
+// in 16-byte pieces; a value tile has its tokens innermost, four by four, so a
+// token moves by elements, 32 of a half wave 4 elements apart. HS: head_dim / 32.
+template <typename T, int HS>
 __global__ __launch_bounds__(256) void page_compact_kernel(
     const int32_t* __restrict__ seq, const int32_t* __restrict__ base,
     const int32_t* __restrict__ kept, const int32_t* __restrict__ starts, int n_kept,
     const int32_t* __restrict__ table, int n_seqs, int max_blocks, int64_t num_blocks,
-    CachePools pools, int Hkv, int hd) {
-  constexpr int kTok = 16, kMaxPer = kTok * 256 / 256;
+    CachePools pools, int Hkv) {
+  constexpr int kTok = 16, kTile = kBlockTokens * 32 * HS;
+  constexpr int kPer = 16 / sizeof(T);                    // elements of a piece
+  constexpr int kPieces = kTok * 32 * HS / kPer;          // of 16 tokens
+  constexpr int kKeys = (kPieces + 255) / 256, kVals = 2 * HS;
   __shared__ int64_t from_s[kTok], to_s[kTok];  // tile << 4 | slot; -1: nothing moves
-  const int i = blockIdx.x, g = blockIdx.y;
+  const int i = blockIdx.x, g = blockIdx.y, tid = threadIdx.x;
   T* pool = (T*)pools.p[blockIdx.z];
-  const bool values = blockIdx.z & 1;
   const int row = seq[i];
+  const int k0 = max(starts[i], 0), k1 = min(starts[i + 1], n_kept), b0 = base[i];
   if (row < 0 || row >= n_seqs) return;
   const int32_t* bt = table + (int64_t)row * max_blocks;
-  const int k0 = max(starts[i], 0), k1 = min(starts[i + 1], n_kept), b0 = base[i];
   const int last = max_blocks * kBlockTokens;
   auto place = [&](int pos) -> int64_t {
     if (pos < 0 || pos >= last) return -1;
@@ -238,42 +250,61 @@ __global__ __launch_bounds__(256) void page_compact_kernel(
                ? -1
                : (((int64_t)blk * Hkv + g) << 4 | (pos % kBlockTokens));
   };
-  const int tile = kBlockTokens * hd;
   for (int k = k0; k < k1; k += kTok) {
-    if (threadIdx.x < kTok) {
-      const bool live = k + (int)threadIdx.x < k1;
-      const int pos = live ? kept[k + threadIdx.x] : -1;
-      const int to = b0 + (k - k0) + (int)threadIdx.x;
+    if (tid < kTok) {
+      const bool live = k + tid < k1;
+      const int pos = live ? kept[k + tid] : -1;
+      const int to = b0 + (k - k0) + tid;
       const bool moves = live && pos != to;
-      from_s[threadIdx.x] = moves ? place(pos) : -1;
-      to_s[threadIdx.x] = moves ? place(to) : -1;
+      const int64_t f = moves ? place(pos) : -1, t = moves ? place(to) : -1;
+      from_s[tid] = t < 0 ? -1 : f;
+      to_s[tid] = f < 0 ? -1 : t;
     }
     __syncthreads();
-    T r[kMaxPer];
-    const int n = kTok * hd;
+    if (blockIdx.z & 1) {
+      const int w = tid & 31;
+      T r[kVals];
 #pragma unroll
-    for (int u = 0; u < kMaxPer; ++u) {
-      const int x = threadIdx.x + u * 256;
-      if (x >= n) break;
-      const int t = x / hd, h = x - t * hd;
-      const int64_t f = from_s[t];
-      if (f < 0 || to_s[t] < 0) continue;
-      const int slot = (int)(f & 15);
-      r[u] = pool[(f >> 4) * tile + (values ? v_tile_offset(slot, h) : k_tile_offset(slot, h))];
-    }
-    wait_vmcnt<0>();  // every value is here before any is overwritten
-    __syncthreads();
+      for (int u = 0; u < kVals; ++u) {  // unit (token, 32 dims) of a half wave
+        const int unit = (tid >> 5) + 8 * u;
+        const int64_t f = from_s[unit & 15];
+        if (f >= 0)
+          r[u] = pool[(f >> 4) * kTile + (unit >> 4) * 512 + ((int)f & 12) * 32 + w * 4 +
+                      ((int)f & 3)];
+      }
+      wait_vmcnt<0>();  // every value is here before any is overwritten
+      __syncthreads();
 #pragma unroll
-    for (int u = 0; u < kMaxPer; ++u) {
-      const int x = threadIdx.x + u * 256;
-      if (x >= n) break;
-      const int t = x / hd, h = x - t * hd;
-      const int64_t f = to_s[t];
-      if (f < 0 || from_s[t] < 0) continue;
-      const int slot = (int)(f & 15);
-      pool[(f >> 4) * tile + (values ? v_tile_offset(slot, h) : k_tile_offset(slot, h))] = r[u];
+      for (int u = 0; u < kVals; ++u) {
+        const int unit = (tid >> 5) + 8 * u;
+        const int64_t t = to_s[unit & 15];
+        if (t >= 0)
+          pool[(t >> 4) * kTile + (unit >> 4) * 512 + ((int)t & 12) * 32 + w * 4 + ((int)t & 3)] =
+              r[u];
+      }
+    } else {
+      // Piece c of a token: elements c kPer .. of it.
+      u32x4_t r[kKeys];
+      const auto at = [&](int64_t x, int c) -> u32x4_t* {
+        const int h = c * kPer;
+        return (u32x4_t*)(pool + (x >> 4) * kTile + (h >> 3) * 128 + ((int)x & 15) * 8 + (h & 7));
+      };
+#pragma unroll
+      for (int u = 0; u < kKeys; ++u) {
+        const int x = tid + 256 * u;
+        const int64_t f = from_s[x & 15];
+        if (x < kPieces && f >= 0) r[u] = *at(f, x >> 4);
+      }
+      wait_vmcnt<0>();
+      __syncthreads();
+#pragma unroll
+      for (int u = 0; u < kKeys; ++u) {
+        const int x = tid + 256 * u;
+        const int64_t t = to_s[x & 15];
+        if (x < kPieces && t >= 0) *at(t, x >> 4) = r[u];
+      }
     }
-    __syncthreads();
+    __syncthreads();  // the places are read, and the group is written
   }
 }
 
@@ -323,8 +354,11 @@ hipError_t launch_page_compact(const int32_t* seq, const int32_t* base, const in
                                const CachePools& pools, int Hkv, int hd, hipStream_t st) {
   if (n <= 0 || n_kept <= 0) return hipSuccess;
   if (hd % 32 != 0 || hd > 256 || Hkv > 65535) return hipErrorInvalidValue;
-  COCO_LAUNCH((page_compact_kernel<T>), dim3(n, Hkv, pools.n), dim3(256), 0, st, seq, base, kept,
-              starts, n_kept, table, n_seqs, max_blocks, num_blocks, pools, Hkv, hd);
+#define COCO_COMPACT(HS)                                                                        \
+  COCO_LAUNCH((page_compact_kernel<T, HS>), dim3(n, Hkv, pools.n), dim3(256), 0, st, seq, base, \
+              kept, starts, n_kept, table, n_seqs, max_blocks, num_blocks, pools, Hkv)
+  COCO_BY_HEAD_DIM(COCO_COMPACT);
+#undef COCO_COMPACT
   return hipGetLastError();
 }
 
