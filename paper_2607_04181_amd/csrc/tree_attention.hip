@@ -524,14 +524,16 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_kernel(TreeArgs a)
 }
 
 // The parts of a row's heads, in order: four dims per thread, 32 threads per
-// head, eight heads per workgroup.
-__global__ __launch_bounds__(256) void tree_combine_kernel(TreeArgs a) {
+// head, four heads per workgroup (eight: one token 15.4 us with the merge
+// instead of 13.8, 32 trees of 64 nodes 519 instead of 506).
+constexpr int kMergeHeads = 4;
+__global__ __launch_bounds__(32 * kMergeHeads) void tree_combine_kernel(TreeArgs a) {
   if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x < kXCDs) a.drawn[threadIdx.x] = 0;
   const int row = blockIdx.x + a.rk.seq_starts[0];
   if (row >= a.rk.seq_starts[a.rk.n_seqs]) return;
   const int s = row_to_seq(a.rk.seq_starts, a.rk.n_seqs, row);
   const int splits = a.plan[2 * s + 1];
-  const int head = blockIdx.y * 8 + threadIdx.x / 32, dim = threadIdx.x % 32 * 4;
+  const int head = blockIdx.y * kMergeHeads + threadIdx.x / 32, dim = threadIdx.x % 32 * 4;
   if (head >= a.Hq) return;
   int32_t* redo = a.redo + (int64_t)row * a.Hq + head;
   const bool again = *redo != 0;
@@ -655,7 +657,8 @@ hipError_t launch_tree_attention_bf16(const uint16_t* q, const uint16_t* k_cache
     a.rk.block_table = rk.block_table + (int64_t)s0 * rk.max_blocks;
     a.rk.n_seqs = rk.n_seqs - s0 < kMaxSeqs ? rk.n_seqs - s0 : kMaxSeqs;
     COCO_LAUNCH(tree_attention_kernel, dim3(2 * num_cus), dim3(kThreads), 0, st, a);
-    COCO_LAUNCH(tree_combine_kernel, dim3(n_rows, (Hq + 7) / 8), dim3(256), 0, st, a);
+    COCO_LAUNCH(tree_combine_kernel, dim3(n_rows, (Hq + kMergeHeads - 1) / kMergeHeads),
+                dim3(32 * kMergeHeads), 0, st, a);
   }
   return hipGetLastError();
 }
