@@ -253,8 +253,8 @@ int coco_layer_workspace(coco_layer_t h, int32_t which, void* dst, int64_t dst_b
 
 /* Per-kernel timing for benchmarks (calls of any handle are unaffected while
  * it is off; kinds whose work runs inside another kernel count no launches).
- * When on, every kernel launched by coco_layer_forward /
- * coco_layer_span_forward on this handle is launched with a pair of HIP events
+ * When on, every kernel launched by coco_layer_forward and the span, tree and
+ * sparse forwards on this handle is launched with a pair of HIP events
  * (hipExtLaunchKernelGGL) that the runtime timestamps at the kernel's own
  * start and end, from a pool of events created here (so switching it on
  * allocates; timed calls themselves do not). Switch it off before capturing
@@ -263,7 +263,8 @@ enum {
   COCO_K_GATHER_NORM = 0,    /* gather + RMSNorm_1 (or RMSNorm_1 inside a span) */
   COCO_K_GEMM_QKV = 1,       /* QKV projection */
   COCO_K_QKV_EPILOGUE = 2,   /* split-K sum + RoPE + cache append */
-  COCO_K_ATTENTION = 3,      /* paged attention (decode partitions or prefill) */
+  COCO_K_ATTENTION = 3,      /* paged attention (decode partitions or prefill); of
+                                trees and selected blocks all kernels, as one launch */
   COCO_K_ATTN_COMBINE = 4,   /* decode partition merge */
   COCO_K_GEMM_O = 5,         /* O projection */
   COCO_K_RESIDUAL_NORM = 6,  /* residual + RMSNorm_2 */
@@ -370,6 +371,19 @@ int coco_tree_attention(coco_layer_t h, int32_t layer, const void* q, void* o, i
                         const int32_t* ctx_lens, const uint64_t* tree_mask, int32_t mask_words,
                         coco_stream_t stream);
 
+/* Layers first_layer .. first_layer + n_layers - 1 for the nodes of drafted
+ * trees, as coco_layer_span_forward for prompts, except: row i of sequence s,
+ * its node j = i - seq_starts[s] of N, is cached in slot ctx_lens[s] - N + j
+ * (the pages must be there: coco_kv_alloc); its position is only its rotation,
+ * the number of tokens before it on its path, so that an accepted path can
+ * move up to its place (coco_kv_compact) as it is; and it attends as in
+ * coco_tree_attention. Needs coco_tree_reserve. */
+int coco_layer_tree_forward(coco_layer_t h, int32_t first_layer, int32_t n_layers, void* hidden,
+                            int64_t hidden_rows, const int32_t* row_idx, int32_t n_rows,
+                            const int32_t* positions, const int32_t* seq_starts, int32_t n_seqs,
+                            const int32_t* block_table, const int32_t* ctx_lens,
+                            const uint64_t* tree_mask, int32_t mask_words, coco_stream_t stream);
+
 /* ---------------------------------------------------------------------------
  * Attention over the blocks that a cheap score selects for each query.
  * ------------------------------------------------------------------------- */
@@ -414,12 +428,26 @@ int coco_block_select(coco_layer_t h, const int8_t* summary, const float* scales
 /* Attention of each row over its keys (positions 0 .. min(ctx_lens,
  * position + 1) - 1) in the blocks selected[row][kv head] lists, of
  * coco_block_select or the caller's own: distinct blocks in any order;
- * entries outside the row's blocks (-1) are skipped. A row without keys gives
- * zeros. q, o as in coco_tree_attention. */
+ * entries outside the row's blocks (-1) are skipped. (Validation mode takes
+ * ascending blocks of the row and -1 only.) A row without keys gives zeros.
+ * q, o as in coco_tree_attention. */
 int coco_sparse_attention(coco_layer_t h, int32_t layer, const void* q, void* o, int32_t n_rows,
                           const int32_t* positions, const int32_t* seq_starts, int32_t n_seqs,
                           const int32_t* block_table, const int32_t* ctx_lens,
                           const int32_t* selected, int32_t n_select, coco_stream_t stream);
+
+/* A decode step of one layer (coco_layer_forward with seq_starts NULL: row i is
+ * sequence i) whose rows attend selected blocks: once the new token is cached,
+ * the summaries of its block are written (coco_kv_summarize from positions
+ * on; those of the blocks before it must be there), n_select blocks chosen as by
+ * coco_block_select and written to selected, and attended. summary and scales
+ * cover the layer's blocks. Needs coco_sparse_reserve. */
+int coco_layer_sparse_forward(coco_layer_t h, int32_t layer, void* hidden, int64_t hidden_rows,
+                              const int32_t* row_idx, int32_t n_rows, const int32_t* positions,
+                              const int32_t* block_table, const int32_t* ctx_lens,
+                              int8_t* summary, float* scales, int32_t keep_first,
+                              int32_t keep_last, int32_t* selected, int32_t n_select,
+                              coco_stream_t stream);
 
 /* Peak probes for benchmarks (not part of the layer): the rates this GPU
  * sustains, against which measured kernels are quoted next to the published

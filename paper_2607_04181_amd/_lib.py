@@ -28,6 +28,7 @@ EXPORTS = ["coco_layer_init", "coco_layer_destroy", "coco_last_error", "coco_ver
            "coco_kv_alloc", "coco_kv_fork", "coco_kv_free", "coco_kv_copy", "coco_kv_compact",
            "coco_tree_reserve", "coco_tree_attention", "coco_kv_summarize",
            "coco_sparse_reserve", "coco_block_select", "coco_sparse_attention",
+           "coco_layer_tree_forward", "coco_layer_sparse_forward",
            # include/coco_scaling.h: host arithmetic of the speedup/cost model
            "coco_split_batch", "coco_comm_time", "coco_speedup", "coco_cost_mem",
            "coco_cost_comp", "coco_speedup_vec", "coco_scale_candidates"]
@@ -101,6 +102,10 @@ def _load():
         "coco_tree_reserve": (ctypes.c_int, [vp, i32, i32]),
         "coco_tree_attention": (ctypes.c_int, [vp, i32, vp, vp, i32, vp, i32, vp, vp, vp, i32,
                                                vp]),
+        "coco_layer_tree_forward": (ctypes.c_int, [vp, i32, i32, vp, i64, vp, i32, vp, vp, i32, vp,
+                                                   vp, vp, i32, vp]),
+        "coco_layer_sparse_forward": (ctypes.c_int, [vp, i32, vp, i64, vp, i32, vp, vp, vp, vp, vp,
+                                                     i32, i32, vp, i32, vp]),
         "coco_kv_summarize": (ctypes.c_int, [vp, i32, vp, vp, vp, vp, i32, vp, vp]),
         "coco_sparse_reserve": (ctypes.c_int, [vp, i32, i32]),
         "coco_block_select": (ctypes.c_int, [vp, vp, vp, i64, vp, i32, vp, vp, i32, vp, vp, i32,
@@ -423,13 +428,34 @@ def coco_tree_attention(h: Handle, layer: int, q, o, seq_starts, block_table, ct
     n_seqs = int(ctx_lens.numel())
     _check_len("seq_starts", seq_starts, n_seqs + 1)
     _check_table(h, block_table, n_seqs)
-    if not (isinstance(tree_mask, torch.Tensor) and tree_mask.dim() == 2 and
-            tree_mask.shape[0] == n):
-        raise ValueError(f"tree_mask must be [{n}, words]")
+    _check_mask(tree_mask, n)
     _check(_lib.coco_tree_attention(
         h.raw, layer, _ptr(q, what="q"), _ptr(o, what="o"), n, _ptr(seq_starts, i32, "seq_starts"),
         n_seqs, _ptr(block_table, i32, "block_table"), _ptr(ctx_lens, i32, "ctx_lens"),
         _ptr(tree_mask, torch.int64, "tree_mask"), int(tree_mask.shape[1]), _stream(stream)))
+
+
+def _check_mask(tree_mask, n: int):
+    if not (isinstance(tree_mask, torch.Tensor) and tree_mask.dim() == 2 and
+            tree_mask.shape[0] == n):
+        raise ValueError(f"tree_mask must be [{n}, words]")
+
+
+def coco_layer_tree_forward(h: Handle, first_layer: int, n_layers: int, hidden, row_idx, positions,
+                            seq_starts, block_table, ctx_lens, tree_mask, stream=None):
+    """tree_mask: int64 [rows, words]."""
+    i32 = torch.int32
+    if seq_starts is None:
+        raise ValueError("seq_starts must be given")
+    _check_batch(h, hidden, row_idx, positions, seq_starts, block_table, ctx_lens)
+    n, n_seqs = int(row_idx.numel()), int(ctx_lens.numel())
+    _check_mask(tree_mask, n)
+    _check(_lib.coco_layer_tree_forward(
+        h.raw, first_layer, n_layers, _ptr(hidden, what="hidden"), int(hidden.shape[0]),
+        _ptr(row_idx, i32, "row_idx"), n, _ptr(positions, i32, "positions"),
+        _ptr(seq_starts, i32, "seq_starts"), n_seqs, _ptr(block_table, i32, "block_table"),
+        _ptr(ctx_lens, i32, "ctx_lens"), _ptr(tree_mask, torch.int64, "tree_mask"),
+        int(tree_mask.shape[1]), _stream(stream)))
 
 
 def _check_summary(h: Handle, summary, scales):
@@ -440,15 +466,19 @@ def _check_summary(h: Handle, summary, scales):
     _check_len("scales", scales, summary.shape[0] * cfg.n_kv_heads)
 
 
+def _check_layer_summary(h: Handle, layer: int, summary):
+    blocks = h.num_blocks[layer] if 0 <= layer < len(h.num_blocks) else 0
+    if summary.shape[0] < blocks:
+        raise ValueError(f"summary must have the layer's {blocks} blocks")
+
+
 def coco_kv_summarize(h: Handle, layer: int, summary, scales, first_lens, ctx_lens, block_table,
                       stream=None):
     """first_lens None: the whole sequences."""
     i32 = torch.int32
     n_seqs = int(ctx_lens.numel())
     _check_summary(h, summary, scales)
-    blocks = h.num_blocks[layer] if 0 <= layer < len(h.num_blocks) else 0
-    if summary.shape[0] < blocks:
-        raise ValueError(f"summary must have the layer's {blocks} blocks")
+    _check_layer_summary(h, layer, summary)
     if first_lens is not None:
         _check_len("first_lens", first_lens, n_seqs)
     _check_table(h, block_table, n_seqs)
@@ -508,6 +538,23 @@ def coco_sparse_attention(h: Handle, layer: int, q, o, positions, seq_starts, bl
         _ptr(seq_starts, i32, "seq_starts"), n_seqs, _ptr(block_table, i32, "block_table"),
         _ptr(ctx_lens, i32, "ctx_lens"), _ptr(selected, i32, "selected"), n_select,
         _stream(stream)))
+
+
+def coco_layer_sparse_forward(h: Handle, layer: int, hidden, row_idx, positions, block_table,
+                              ctx_lens, summary, scales, keep_first: int, keep_last: int, selected,
+                              stream=None):
+    i32 = torch.int32
+    _check_batch(h, hidden, row_idx, positions, None, block_table, ctx_lens)
+    n = int(row_idx.numel())
+    _check_summary(h, summary, scales)
+    _check_layer_summary(h, layer, summary)
+    n_select = _check_selected(h, selected, n)
+    _check(_lib.coco_layer_sparse_forward(
+        h.raw, layer, _ptr(hidden, what="hidden"), int(hidden.shape[0]),
+        _ptr(row_idx, i32, "row_idx"), n, _ptr(positions, i32, "positions"),
+        _ptr(block_table, i32, "block_table"), _ptr(ctx_lens, i32, "ctx_lens"),
+        _ptr(summary, torch.int8, "summary"), _ptr(scales, torch.float32, "scales"), keep_first,
+        keep_last, _ptr(selected, i32, "selected"), n_select, _stream(stream)))
 
 
 def coco_layer_workspace(h: Handle, which: int, dst, stream=None) -> None:

@@ -206,7 +206,147 @@ int grow(coco_layer* H, char** buf, size_t* have, size_t want) {
   return COCO_OK;
 }
 
+int check_sparse_room(const coco_layer* H, int n_rows, int n_select) {
+  if (n_select < 1) return fail(COCO_EINVAL, "n_select must be >= 1");
+  if (n_rows > H->sparse_rows || n_select > H->sparse_top)
+    return fail(COCO_ESTATE, "%d rows of %d blocks; coco_sparse_reserve made room for %d of %d",
+                n_rows, n_select, H->sparse_rows, H->sparse_top);
+  return COCO_OK;
+}
+
+RowKeys row_keys(const coco_layer* H, const int32_t* seq_starts, int n_seqs, const int32_t* bt,
+                 const int32_t* ctx, int64_t num_blocks) {
+  RowKeys rk;
+  rk.block_table = bt;
+  rk.ctx_lens = ctx;
+  rk.seq_starts = seq_starts;
+  rk.n_seqs = n_seqs;
+  rk.max_blocks = H->cfg.max_blocks_per_seq;
+  rk.num_blocks = num_blocks;
+  return rk;
+}
+
 }  // namespace
+
+namespace coco {
+
+int check_tree(const coco_layer* H, int n_rows, const int32_t* seq_starts, int n_seqs,
+               const uint64_t* mask, int words) {
+  if (!seq_starts || !mask) return fail(COCO_EINVAL, "NULL argument");
+  if ((uintptr_t)mask % 8) return fail(COCO_EINVAL, "tree_mask is not 8-byte aligned");
+  if (words < 1) return fail(COCO_EINVAL, "mask_words must be >= 1");
+  if (n_rows > H->tree_rows || n_seqs > H->tree_seqs)
+    return fail(COCO_ESTATE, "%d rows of %d sequences; coco_tree_reserve made room for %d of %d",
+                n_rows, n_seqs, H->tree_rows, H->tree_seqs);
+  return COCO_OK;
+}
+
+int validate_tree(const coco_layer* H, int n_rows, const int32_t* positions,
+                  const int32_t* seq_starts, int n_seqs, const int32_t* bt, const int32_t* ctx_lens,
+                  int words, int64_t num_blocks, hipStream_t st) {
+  std::vector<int32_t> ss, ctx;
+  int rc;
+  if ((rc = validate_rows(H, n_rows, positions, seq_starts, n_seqs, bt, ctx_lens, num_blocks, ss,
+                          ctx, st)))
+    return rc;
+  for (int s = 0; s < n_seqs; ++s) {
+    if (ss[s + 1] - ss[s] > ctx[s])
+      return fail(COCO_EINVAL, "sequence %d has %d nodes in %d cached tokens", s,
+                  ss[s + 1] - ss[s], ctx[s]);
+    if (ss[s + 1] - ss[s] > 64LL * words)
+      return fail(COCO_EINVAL, "sequence %d has %d nodes for %d mask words", s,
+                  ss[s + 1] - ss[s], words);
+  }
+  return COCO_OK;
+}
+
+int run_tree(coco_layer* H, const coco_layer_weights& w, const void* q, void* o, bool tiled,
+             int n_rows, const int32_t* seq_starts, int n_seqs, const int32_t* bt,
+             const int32_t* ctx, const uint64_t* mask, int words, hipStream_t st) {
+  const coco_layer_config& c = H->cfg;
+  RowKeys rk = row_keys(H, seq_starts, n_seqs, bt, ctx, w.num_blocks);
+  rk.mask = mask;
+  rk.words = words;
+  if (c.dtype == COCO_BF16)
+    HIPCHK(launch_tree_attention_bf16((const bf16_t*)q, (const bf16_t*)w.k_cache,
+                                      (const bf16_t*)w.v_cache, rk, n_rows, c.n_q_heads,
+                                      c.n_kv_heads, (bf16_t*)o, tiled, H->tree_part_o,
+                                      H->tree_part_ml, H->tree_parts, H->tree_plan, H->tree_redo,
+                                      H->num_cus, st));
+  else
+    HIPCHK(launch_attn_rows_f32((const float*)q, (const float*)w.k_cache, (const float*)w.v_cache,
+                                rk, n_rows, c.n_q_heads, c.n_kv_heads, c.head_dim, (float*)o, st));
+  return COCO_OK;
+}
+
+int check_select(const coco_layer* H, int n_rows, const int8_t* summary, const float* scales,
+                 int64_t num_blocks, int keep_first, int keep_last, const int32_t* selected,
+                 int n_select) {
+  if (!summary || !scales || !selected) return fail(COCO_EINVAL, "NULL argument");
+  if ((uintptr_t)summary % 16) return fail(COCO_EINVAL, "summary is not 16-byte aligned");
+  if (num_blocks < 1) return fail(COCO_EINVAL, "num_blocks must be >= 1");
+  if (n_select < 1) return fail(COCO_EINVAL, "n_select must be >= 1");
+  if (keep_first < 0 || keep_last < 0 || keep_first > n_select || keep_last > n_select - keep_first)
+    return fail(COCO_EINVAL, "keep_first = %d and keep_last = %d outside n_select = %d", keep_first,
+                keep_last, n_select);
+  return check_sparse_room(H, n_rows, n_select);
+}
+
+int run_summarize(coco_layer* H, const coco_layer_weights& w, int8_t* summary, float* scales,
+                  const int32_t* first, const int32_t* ctx, int n_seqs, const int32_t* bt,
+                  hipStream_t st) {
+  const coco_layer_config& c = H->cfg;
+  if (c.dtype == COCO_BF16)
+    HIPCHK(launch_summarize((const bf16_t*)w.k_cache, c.n_kv_heads, c.head_dim, bt, n_seqs,
+                            c.max_blocks_per_seq, w.num_blocks, first, ctx, summary, scales,
+                            H->num_cus, st));
+  else
+    HIPCHK(launch_summarize((const float*)w.k_cache, c.n_kv_heads, c.head_dim, bt, n_seqs,
+                            c.max_blocks_per_seq, w.num_blocks, first, ctx, summary, scales,
+                            H->num_cus, st));
+  return COCO_OK;
+}
+
+int run_select(coco_layer* H, const int8_t* summary, const float* scales, int64_t num_blocks,
+               const void* q, int n_rows, const int32_t* positions, const int32_t* seq_starts,
+               int n_seqs, const int32_t* bt, const int32_t* ctx, int keep_first, int keep_last,
+               int32_t* selected, int n_select, hipStream_t st) {
+  const coco_layer_config& c = H->cfg;
+  RowKeys rk = row_keys(H, seq_starts, n_seqs, bt, ctx, num_blocks);
+  rk.positions = positions;
+  rk.top = n_select;
+  if (c.dtype == COCO_BF16)
+    HIPCHK(launch_block_select((const bf16_t*)q, summary, scales, rk, n_rows, c.n_q_heads,
+                               c.n_kv_heads, c.head_dim, keep_first, keep_last, H->sparse_keys,
+                               selected, st));
+  else
+    HIPCHK(launch_block_select((const float*)q, summary, scales, rk, n_rows, c.n_q_heads,
+                               c.n_kv_heads, c.head_dim, keep_first, keep_last, H->sparse_keys,
+                               selected, st));
+  return COCO_OK;
+}
+
+int run_sparse(coco_layer* H, const coco_layer_weights& w, const void* q, void* o, bool tiled,
+               int n_rows, const int32_t* positions, const int32_t* seq_starts, int n_seqs,
+               const int32_t* bt, const int32_t* ctx, const int32_t* selected, int n_select,
+               hipStream_t st) {
+  const coco_layer_config& c = H->cfg;
+  RowKeys rk = row_keys(H, seq_starts, n_seqs, bt, ctx, w.num_blocks);
+  rk.positions = positions;
+  rk.selected = selected;
+  rk.top = n_select;
+  if (c.dtype == COCO_BF16)
+    HIPCHK(launch_sparse_attention_bf16((const bf16_t*)q, (const bf16_t*)w.k_cache,
+                                        (const bf16_t*)w.v_cache, rk, n_rows, c.n_q_heads,
+                                        c.n_kv_heads, (bf16_t*)o, tiled, H->sparse_part_o,
+                                        H->sparse_part_ml, st));
+  else
+    HIPCHK(launch_attn_rows_f32((const float*)q, (const float*)w.k_cache, (const float*)w.v_cache,
+                                rk, n_rows, c.n_q_heads, c.n_kv_heads, c.head_dim, (float*)o, st));
+  return COCO_OK;
+}
+
+}  // namespace coco
 
 extern "C" {
 
@@ -404,48 +544,16 @@ int coco_tree_attention(coco_layer_t H, int32_t layer, const void* q, void* o, i
   if (!H) return fail(COCO_EINVAL, "handle is NULL");
   int rc = check_rows(H, layer, q, o, n_rows, nullptr, seq_starts, n_seqs, block_table, ctx_lens);
   if (rc || n_rows == 0) return rc;
-  if (!seq_starts || !tree_mask) return fail(COCO_EINVAL, "NULL argument");
-  if ((uintptr_t)tree_mask % 8) return fail(COCO_EINVAL, "tree_mask is not 8-byte aligned");
-  if (mask_words < 1) return fail(COCO_EINVAL, "mask_words must be >= 1");
-  if (n_rows > H->tree_rows || n_seqs > H->tree_seqs)
-    return fail(COCO_ESTATE, "%d rows of %d sequences; coco_tree_reserve made room for %d of %d",
-                n_rows, n_seqs, H->tree_rows, H->tree_seqs);
-  const coco_layer_config& c = H->cfg;
+  if ((rc = check_tree(H, n_rows, seq_starts, n_seqs, tree_mask, mask_words))) return rc;
   const coco_layer_weights& w = H->layers[layer];
   hipStream_t st = (hipStream_t)stream;
   HIPCHK(hipSetDevice(H->device));
-  if (H->validate) {
-    std::vector<int32_t> ss, ctx;
-    if ((rc = validate_rows(H, n_rows, nullptr, seq_starts, n_seqs, block_table, ctx_lens,
-                            w.num_blocks, ss, ctx, st)))
-      return rc;
-    for (int s = 0; s < n_seqs; ++s) {
-      if (ss[s + 1] - ss[s] > ctx[s])
-        return fail(COCO_EINVAL, "sequence %d has %d nodes in %d cached tokens", s,
-                    ss[s + 1] - ss[s], ctx[s]);
-      if (ss[s + 1] - ss[s] > 64LL * mask_words)
-        return fail(COCO_EINVAL, "sequence %d has %d nodes for %d mask words", s,
-                    ss[s + 1] - ss[s], mask_words);
-    }
-  }
-  RowKeys rk;
-  rk.block_table = block_table;
-  rk.ctx_lens = ctx_lens;
-  rk.seq_starts = seq_starts;
-  rk.n_seqs = n_seqs;
-  rk.max_blocks = c.max_blocks_per_seq;
-  rk.num_blocks = w.num_blocks;
-  rk.mask = tree_mask;
-  rk.words = mask_words;
-  if (c.dtype == COCO_BF16)
-    HIPCHK(launch_tree_attention_bf16((const bf16_t*)q, (const bf16_t*)w.k_cache,
-                                      (const bf16_t*)w.v_cache, rk, n_rows, c.n_q_heads,
-                                      c.n_kv_heads, (bf16_t*)o, false, H->tree_part_o,
-                                      H->tree_part_ml, H->tree_parts, H->tree_plan, H->tree_redo,
-                                      H->num_cus, st));
-  else
-    HIPCHK(launch_attn_rows_f32((const float*)q, (const float*)w.k_cache, (const float*)w.v_cache,
-                                rk, n_rows, c.n_q_heads, c.n_kv_heads, c.head_dim, (float*)o, st));
+  if (H->validate && (rc = validate_tree(H, n_rows, nullptr, seq_starts, n_seqs, block_table,
+                                         ctx_lens, mask_words, w.num_blocks, st)))
+    return rc;
+  if ((rc = run_tree(H, w, q, o, false, n_rows, seq_starts, n_seqs, block_table, ctx_lens,
+                     tree_mask, mask_words, st)))
+    return rc;
   return mark_done(H, st);
 }
 
@@ -463,9 +571,9 @@ int coco_kv_summarize(coco_layer_t H, int32_t layer, int8_t* summary, float* sca
   const coco_layer_weights& w = H->layers[layer];
   hipStream_t st = (hipStream_t)stream;
   HIPCHK(hipSetDevice(H->device));
+  int rc;
   if (H->validate) {
     std::vector<int32_t> f, ctx, bt;
-    int rc;
     const int64_t top = (int64_t)c.max_blocks_per_seq * kBlockTokens;
     if ((first_lens && ((rc = fetch(f, first_lens, n_seqs, st)) ||
                         (rc = check_range("first_lens", f, 0, top + 1)))) ||
@@ -476,14 +584,8 @@ int coco_kv_summarize(coco_layer_t H, int32_t layer, int8_t* summary, float* sca
     for (int s = 0; s < n_seqs; ++s)
       if ((rc = check_blocks(bt, c.max_blocks_per_seq, s, ctx[s], w.num_blocks))) return rc;
   }
-  if (c.dtype == COCO_BF16)
-    HIPCHK(launch_summarize((const bf16_t*)w.k_cache, c.n_kv_heads, c.head_dim, block_table,
-                            n_seqs, c.max_blocks_per_seq, w.num_blocks, first_lens, ctx_lens,
-                            summary, scales, H->num_cus, st));
-  else
-    HIPCHK(launch_summarize((const float*)w.k_cache, c.n_kv_heads, c.head_dim, block_table,
-                            n_seqs, c.max_blocks_per_seq, w.num_blocks, first_lens, ctx_lens,
-                            summary, scales, H->num_cus, st));
+  if ((rc = run_summarize(H, w, summary, scales, first_lens, ctx_lens, n_seqs, block_table, st)))
+    return rc;
   return mark_done(H, st);
 }
 
@@ -521,18 +623,10 @@ int coco_block_select(coco_layer_t H, const int8_t* summary, const float* scales
   int rc = check_rows(H, 0, q, q, n_rows, positions, seq_starts, n_seqs, block_table,
                       ctx_lens);
   if (rc || n_rows == 0) return rc;
-  if (!summary || !scales || !positions || !selected)
-    return fail(COCO_EINVAL, "NULL argument");
-  if ((uintptr_t)summary % 16) return fail(COCO_EINVAL, "summary is not 16-byte aligned");
-  if (num_blocks < 1) return fail(COCO_EINVAL, "num_blocks must be >= 1");
-  if (n_select < 1) return fail(COCO_EINVAL, "n_select must be >= 1");
-  if (keep_first < 0 || keep_last < 0 || keep_first > n_select || keep_last > n_select - keep_first)
-    return fail(COCO_EINVAL, "keep_first = %d and keep_last = %d outside n_select = %d", keep_first,
-                keep_last, n_select);
-  if (n_rows > H->sparse_rows || n_select > H->sparse_top)
-    return fail(COCO_ESTATE, "%d rows of %d blocks; coco_sparse_reserve made room for %d of %d",
-                n_rows, n_select, H->sparse_rows, H->sparse_top);
-  const coco_layer_config& c = H->cfg;
+  if (!positions) return fail(COCO_EINVAL, "NULL argument");
+  if ((rc = check_select(H, n_rows, summary, scales, num_blocks, keep_first, keep_last, selected,
+                         n_select)))
+    return rc;
   hipStream_t st = (hipStream_t)stream;
   HIPCHK(hipSetDevice(H->device));
   if (H->validate) {
@@ -541,23 +635,9 @@ int coco_block_select(coco_layer_t H, const int8_t* summary, const float* scales
                             num_blocks, ss, ctx, st)))
       return rc;
   }
-  RowKeys rk;
-  rk.block_table = block_table;
-  rk.ctx_lens = ctx_lens;
-  rk.seq_starts = seq_starts;
-  rk.n_seqs = n_seqs;
-  rk.max_blocks = c.max_blocks_per_seq;
-  rk.num_blocks = num_blocks;
-  rk.positions = positions;
-  rk.top = n_select;
-  if (c.dtype == COCO_BF16)
-    HIPCHK(launch_block_select((const bf16_t*)q, summary, scales, rk, n_rows, c.n_q_heads,
-                               c.n_kv_heads, c.head_dim, keep_first, keep_last,
-                               H->sparse_keys, selected, st));
-  else
-    HIPCHK(launch_block_select((const float*)q, summary, scales, rk, n_rows, c.n_q_heads,
-                               c.n_kv_heads, c.head_dim, keep_first, keep_last,
-                               H->sparse_keys, selected, st));
+  if ((rc = run_select(H, summary, scales, num_blocks, q, n_rows, positions, seq_starts, n_seqs,
+                       block_table, ctx_lens, keep_first, keep_last, selected, n_select, st)))
+    return rc;
   return mark_done(H, st);
 }
 
@@ -569,10 +649,7 @@ int coco_sparse_attention(coco_layer_t H, int32_t layer, const void* q, void* o,
   int rc = check_rows(H, layer, q, o, n_rows, positions, seq_starts, n_seqs, block_table, ctx_lens);
   if (rc || n_rows == 0) return rc;
   if (!positions || !selected) return fail(COCO_EINVAL, "NULL argument");
-  if (n_select < 1) return fail(COCO_EINVAL, "n_select must be >= 1");
-  if (n_rows > H->sparse_rows || n_select > H->sparse_top)
-    return fail(COCO_ESTATE, "%d rows of %d blocks; coco_sparse_reserve made room for %d of %d",
-                n_rows, n_select, H->sparse_rows, H->sparse_top);
+  if ((rc = check_sparse_room(H, n_rows, n_select))) return rc;
   const coco_layer_config& c = H->cfg;
   const coco_layer_weights& w = H->layers[layer];
   hipStream_t st = (hipStream_t)stream;
@@ -601,24 +678,9 @@ int coco_sparse_attention(coco_layer_t H, int32_t layer, const void* q, void* o,
         }
       }
   }
-  RowKeys rk;
-  rk.block_table = block_table;
-  rk.ctx_lens = ctx_lens;
-  rk.seq_starts = seq_starts;
-  rk.n_seqs = n_seqs;
-  rk.max_blocks = c.max_blocks_per_seq;
-  rk.num_blocks = w.num_blocks;
-  rk.positions = positions;
-  rk.selected = selected;
-  rk.top = n_select;
-  if (c.dtype == COCO_BF16)
-    HIPCHK(launch_sparse_attention_bf16((const bf16_t*)q, (const bf16_t*)w.k_cache,
-                                        (const bf16_t*)w.v_cache, rk, n_rows, c.n_q_heads,
-                                        c.n_kv_heads, (bf16_t*)o, H->sparse_part_o,
-                                        H->sparse_part_ml, st));
-  else
-    HIPCHK(launch_attn_rows_f32((const float*)q, (const float*)w.k_cache, (const float*)w.v_cache,
-                                rk, n_rows, c.n_q_heads, c.n_kv_heads, c.head_dim, (float*)o, st));
+  if ((rc = run_sparse(H, w, q, o, false, n_rows, positions, seq_starts, n_seqs, block_table,
+                       ctx_lens, selected, n_select, st)))
+    return rc;
   return mark_done(H, st);
 }
 

@@ -45,12 +45,15 @@ constexpr int kTimingPairs = 4096;
 
 // Times the one kernel launched in its scope when timing is on: the launch
 // timestamps the event pair at the kernel's own start and end. A scope that
-// launches nothing (empty work) records an empty interval.
+// launches nothing (empty work) records an empty interval; one that launches
+// several ends with the stream's work so far.
 struct KernelTimer {
   coco_layer* H;
   int kind;
+  bool several;
   int pair = -1;
-  KernelTimer(coco_layer* h, int k, hipStream_t st) : H(h), kind(k) {
+  KernelTimer(coco_layer* h, int k, hipStream_t st, bool many = false)
+      : H(h), kind(k), several(many) {
     if (!H->timing) return;
     const int n = (int)H->ev_kind.size();
     if (n >= kTimingPairs) {
@@ -60,15 +63,18 @@ struct KernelTimer {
     pair = n;
     H->ev_kind.push_back(kind);
     H->ev_stream = st;
-    coco::launch_events() = coco::LaunchEvents{H->ev[2 * pair], H->ev[2 * pair + 1]};
+    coco::launch_events() =
+        coco::LaunchEvents{H->ev[2 * pair], several ? nullptr : H->ev[2 * pair + 1]};
   }
   ~KernelTimer() {
     if (pair < 0) return;
     coco::LaunchEvents& le = coco::launch_events();
     if (le.start != nullptr) {
       (void)hipEventRecord(le.start, H->ev_stream);
-      (void)hipEventRecord(le.stop, H->ev_stream);
+      (void)hipEventRecord(H->ev[2 * pair + 1], H->ev_stream);
       le = coco::LaunchEvents{};
+    } else if (several) {
+      (void)hipEventRecord(H->ev[2 * pair + 1], H->ev_stream);
     }
   }
 };
@@ -489,7 +495,7 @@ namespace {
 int validate_batch(coco_layer* H, int64_t hidden_rows, const int32_t* row_idx, int n_rows,
                    const int32_t* positions, const int32_t* seq_starts, int n_seqs,
                    const int32_t* block_table, const int32_t* ctx_lens, int first_layer,
-                   int n_layers, hipStream_t st) {
+                   int n_layers, int tree_words, hipStream_t st) {
   const coco_layer_config& c = H->cfg;
   std::vector<int32_t> ri, pos, ss, bt, cl;
   int rc;
@@ -516,6 +522,9 @@ int validate_batch(coco_layer* H, int64_t hidden_rows, const int32_t* row_idx, i
   int64_t min_blocks = INT64_MAX;
   for (int l = first_layer; l < first_layer + n_layers; ++l)
     if (H->layers[l].num_blocks < min_blocks) min_blocks = H->layers[l].num_blocks;
+  if (tree_words)  // (siblings share a position)
+    return validate_tree(H, n_rows, positions, seq_starts, n_seqs, block_table, ctx_lens,
+                         tree_words, min_blocks, st);
   for (int s = 0; s < n_seqs; ++s) {
     if (ss[s + 1] < ss[s]) return fail(COCO_EINVAL, "seq_starts not monotone at %d", s);
     if (cl[s] < 1 || cl[s] > c.max_blocks_per_seq * kBlockTokens)
@@ -619,10 +628,31 @@ ActLayout act_layout(const coco_layer* H, bool prefill, int M) {
   return a;
 }
 
+// Attention of a layer's rows over what they attend.
+int attend_rows(coco_layer* H, const Work& W, const coco_layer_weights& w, int M,
+                const int32_t* positions, const int32_t* seq_starts, int n_seqs, const int32_t* bt,
+                const int32_t* ctx, const LayerRows& rows, bool o_tiled, hipStream_t st) {
+  KernelTimer t(H, COCO_K_ATTENTION, st, true);
+  if (rows.mask)
+    return run_tree(H, w, W.q, W.o, o_tiled, M, seq_starts, n_seqs, bt, ctx, rows.mask, rows.words,
+                    st);
+  // The new token's block first: it may be among the selected.
+  int rc;
+  if ((rc = run_summarize(H, w, rows.summary, rows.scales, positions, ctx, n_seqs, bt, st)) ||
+      (rc = run_select(H, rows.summary, rows.scales, w.num_blocks, W.q, M, positions, seq_starts,
+                       n_seqs, bt, ctx, rows.keep_first, rows.keep_last, rows.selected,
+                       rows.n_select, st)))
+    return rc;
+  return run_sparse(H, w, W.q, W.o, o_tiled, M, positions, seq_starts, n_seqs, bt, ctx,
+                    rows.selected, rows.n_select, st);
+}
+
 int attention(coco_layer* H, const Work& W, const coco_layer_weights& w, int M,
               const int32_t* positions, const int32_t* seq_starts, int n_seqs, const int32_t* bt,
-              const int32_t* ctx, bool o_tiled, hipStream_t st) {
+              const int32_t* ctx, const LayerRows* rows, bool o_tiled, hipStream_t st) {
   const coco_layer_config& c = H->cfg;
+  if (rows)
+    return attend_rows(H, W, w, M, positions, seq_starts, n_seqs, bt, ctx, *rows, o_tiled, st);
   if (!seq_starts) {
     {
       KernelTimer t(H, COCO_K_ATTENTION, st);
@@ -659,7 +689,8 @@ int attention(coco_layer* H, const Work& W, const coco_layer_weights& w, int M,
 int prefill_layer(coco_layer* H, const Work& W, const coco_layer_weights& w, const bf16_t* x_src,
                   const int32_t* x_idx, bf16_t* y, const int32_t* y_idx, int M,
                   const int32_t* positions, const int32_t* seq_starts, int n_seqs,
-                  const int32_t* bt, const int32_t* ctx, const RowSlotArgs& rs, hipStream_t st) {
+                  const int32_t* bt, const int32_t* ctx, const LayerRows* rows,
+                  const RowSlotArgs& rs, hipStream_t st) {
   const coco_layer_config& c = H->cfg;
   const int d = c.d_model, F = c.d_ffn, qd = c.n_q_heads * c.head_dim;
   bf16_t *h = (bf16_t*)W.h, *o = (bf16_t*)W.o, *h2 = (bf16_t*)W.h2, *u = (bf16_t*)W.u;
@@ -677,7 +708,7 @@ int prefill_layer(coco_layer* H, const Work& W, const coco_layer_weights& w, con
   TIMED(COCO_K_GEMM_QKV,
         HIPCHK(launch_prefill_qkv_bf16(h, (const bf16_t*)w.w_qkv, M, d, qa, H->num_cus, st)));
   int rc;
-  if ((rc = attention(H, W, w, M, positions, seq_starts, n_seqs, bt, ctx, true, st)))
+  if ((rc = attention(H, W, w, M, positions, seq_starts, n_seqs, bt, ctx, rows, true, st)))
     return rc;
   float* const ss = W.part;
   TIMED(COCO_K_GEMM_O,
@@ -700,7 +731,7 @@ int prefill_layer(coco_layer* H, const Work& W, const coco_layer_weights& w, con
 int decode_layer(coco_layer* H, const Work& W, const coco_layer_weights& w, const bf16_t* x_src,
                  const int32_t* x_idx, bf16_t* y, const int32_t* y_idx, int M,
                  const int32_t* positions, const int32_t* bt, const int32_t* ctx,
-                 hipStream_t st) {
+                 const LayerRows* rows, hipStream_t st) {
   const coco_layer_config& c = H->cfg;
   const int d = c.d_model, Hq = c.n_q_heads, Hkv = c.n_kv_heads, hd = c.head_dim, F = c.d_ffn;
   const int nqkv = (Hq + 2 * Hkv) * hd;
@@ -729,7 +760,7 @@ int decode_layer(coco_layer* H, const Work& W, const coco_layer_weights& w, cons
                                         (bf16_t*)w.k_cache, (bf16_t*)w.v_cache, ctx, W.split_off,
                                         H->max_splits, W.ss, d, c.rms_eps, st)));
   // Attention over the paged cache.
-  if ((rc = attention(H, W, w, M, positions, nullptr, M, bt, ctx, lay.o, st))) return rc;
+  if ((rc = attention(H, W, w, M, positions, nullptr, M, bt, ctx, rows, lay.o, st))) return rc;
   // O projection + residual + RMSNorm_2.
   TIMED(COCO_K_GEMM_O,
         if ((rc = gemm(H, W.part, o, (const bf16_t*)w.w_o, M, d, Hq * hd, &S, st))) return rc);
@@ -764,7 +795,7 @@ int decode_layer(coco_layer* H, const Work& W, const coco_layer_weights& w, cons
 int f32_layer(coco_layer* H, const Work& W, const coco_layer_weights& w, const float* x_src,
               const int32_t* x_idx, float* y, const int32_t* y_idx, int M,
               const int32_t* positions, const int32_t* seq_starts, int n_seqs, const int32_t* bt,
-              const int32_t* ctx, hipStream_t st) {
+              const int32_t* ctx, const LayerRows* rows, hipStream_t st) {
   const coco_layer_config& c = H->cfg;
   const int d = c.d_model, Hq = c.n_q_heads, Hkv = c.n_kv_heads, hd = c.head_dim, F = c.d_ffn;
   F32EpiArgs qa;
@@ -775,6 +806,7 @@ int f32_layer(coco_layer* H, const Work& W, const coco_layer_weights& w, const f
   qa.positions = positions;
   qa.seq_starts = seq_starts;
   qa.block_table = bt;
+  if (rows && rows->mask) qa.tree_lens = ctx;
   qa.inv_freq = H->inv_freq;
   qa.q_out = (float*)W.q;
   qa.k_cache = (float*)w.k_cache;
@@ -785,10 +817,16 @@ int f32_layer(coco_layer* H, const Work& W, const coco_layer_weights& w, const f
   qa.Hkv = Hkv;
   qa.hd = hd;
   TIMED(COCO_K_GEMM_QKV, HIPCHK(launch_f32_qkv(x_src, (const float*)w.w_qkv, M, d, qa, st)));
-  TIMED(COCO_K_ATTENTION,
-        HIPCHK(launch_attn_f32((const float*)W.q, (const float*)w.k_cache,
-                               (const float*)w.v_cache, bt, c.max_blocks_per_seq, ctx, positions,
-                               seq_starts, n_seqs, M, Hq, Hkv, hd, (float*)W.o, st)));
+  if (rows) {
+    const int rc =
+        attend_rows(H, W, w, M, positions, seq_starts, n_seqs, bt, ctx, *rows, false, st);
+    if (rc) return rc;
+  } else {
+    KernelTimer t(H, COCO_K_ATTENTION, st);
+    HIPCHK(launch_attn_f32((const float*)W.q, (const float*)w.k_cache,
+                           (const float*)w.v_cache, bt, c.max_blocks_per_seq, ctx, positions,
+                           seq_starts, n_seqs, M, Hq, Hkv, hd, (float*)W.o, st));
+  }
   F32EpiArgs oa;
   oa.row_idx = x_idx;
   oa.res = x_src;
@@ -814,7 +852,7 @@ int f32_layer(coco_layer* H, const Work& W, const coco_layer_weights& w, const f
 template <typename T>
 int run_span(coco_layer* H, const Work& W, int first, int nl, T* hidden, const int32_t* row_idx,
              int M, const int32_t* positions, const int32_t* seq_starts, int n_seqs,
-             const int32_t* bt, const int32_t* ctx, hipStream_t st) {
+             const int32_t* bt, const int32_t* ctx, const LayerRows* rows, hipStream_t st) {
   T* x = (T*)W.x;
   for (int l = first; l < first + nl; ++l) {
     const coco_layer_weights& w = H->layers[l];
@@ -829,9 +867,9 @@ int run_span(coco_layer* H, const Work& W, int first, int nl, T* hidden, const i
     int rc;
     if constexpr (std::is_same<T, float>::value) {
       rc = f32_layer(H, W, w, x_src, x_idx, y, y_idx, M, positions, seq_starts, n_seqs, bt, ctx,
-                     st);
+                     rows, st);
     } else if (seq_starts == nullptr) {
-      rc = decode_layer(H, W, w, x_src, x_idx, y, y_idx, M, positions, bt, ctx, st);
+      rc = decode_layer(H, W, w, x_src, x_idx, y, y_idx, M, positions, bt, ctx, rows, st);
     } else {
       // Prefill row slots (position, cache block), written once per call by
       // the first layer's gather.
@@ -844,9 +882,10 @@ int run_span(coco_layer* H, const Work& W, int first, int nl, T* hidden, const i
         rs.n_seqs = n_seqs;
         rs.max_blocks = H->cfg.max_blocks_per_seq;
         rs.rope_rows = H->rope_rows;
+        if (rows && rows->mask) rs.tree_lens = ctx;
       }
       rc = prefill_layer(H, W, w, x_src, x_idx, y, y_idx, M, positions, seq_starts, n_seqs, bt,
-                         ctx, rs, st);
+                         ctx, rows, rs, st);
     }
     if (rc) return rc;
   }
@@ -886,13 +925,15 @@ int check_batch(coco_layer* H, int first, int nl, const void* hidden, int64_t hi
 int forward_impl(coco_layer* H, int first, int nl, void* hidden, int64_t hidden_rows,
                  const int32_t* row_idx, int n_rows, const int32_t* positions,
                  const int32_t* seq_starts, int n_seqs, const int32_t* bt, const int32_t* ctx,
-                 coco_stream_t stream, bool use_static = false) {
+                 coco_stream_t stream, bool use_static = false, const LayerRows* rows = nullptr) {
   if (!H) return fail(COCO_EINVAL, "handle is NULL");
   int rc = check_batch(H, first, nl, hidden, hidden_rows, row_idx, n_rows, positions,
                        seq_starts, n_seqs, bt, ctx);
   if (rc || n_rows == 0) return rc;
   hipStream_t st = (hipStream_t)stream;
   HIPCHK(hipSetDevice(H->device));
+  const bool tree = rows && rows->mask;
+  if (tree && (rc = check_tree(H, n_rows, seq_starts, n_seqs, rows->mask, rows->words))) return rc;
   Work W = H->w;
   if (use_static) {
     const int64_t dec_seqs = seq_starts ? 0 : n_seqs;
@@ -906,7 +947,7 @@ int forward_impl(coco_layer* H, int first, int nl, void* hidden, int64_t hidden_
     carve_work(H->cfg, n_rows, dec_seqs, H->max_splits, base, &W);
   } else if (H->validate &&
              (rc = validate_batch(H, hidden_rows, row_idx, n_rows, positions, seq_starts, n_seqs,
-                                  bt, ctx, first, nl, st))) {
+                                  bt, ctx, first, nl, tree ? rows->words : 0, st))) {
     return rc;
   }
   if (!use_static) {
@@ -920,10 +961,10 @@ int forward_impl(coco_layer* H, int first, int nl, void* hidden, int64_t hidden_
   }
   if (H->cfg.dtype == COCO_BF16)
     rc = run_span<bf16_t>(H, W, first, nl, (bf16_t*)hidden, row_idx, n_rows, positions,
-                          seq_starts, n_seqs, bt, ctx, st);
+                          seq_starts, n_seqs, bt, ctx, rows, st);
   else
     rc = run_span<float>(H, W, first, nl, (float*)hidden, row_idx, n_rows, positions,
-                         seq_starts, n_seqs, bt, ctx, st);
+                         seq_starts, n_seqs, bt, ctx, rows, st);
   if (rc) return rc;
   return mark_done(H, st);
 }
@@ -956,6 +997,45 @@ int coco_layer_span_forward(coco_layer_t H, int32_t first_layer, int32_t n_layer
                             coco_stream_t stream) {
   return forward_impl(H, first_layer, n_layers, hidden, hidden_rows, row_idx, n_rows, positions,
                       seq_starts, n_seqs, block_table, ctx_lens, stream);
+}
+
+int coco_layer_tree_forward(coco_layer_t H, int32_t first_layer, int32_t n_layers, void* hidden,
+                            int64_t hidden_rows, const int32_t* row_idx, int32_t n_rows,
+                            const int32_t* positions, const int32_t* seq_starts, int32_t n_seqs,
+                            const int32_t* block_table, const int32_t* ctx_lens,
+                            const uint64_t* tree_mask, int32_t mask_words, coco_stream_t stream) {
+  if (!H) return fail(COCO_EINVAL, "handle is NULL");
+  if (n_rows > 0 && (!tree_mask || !seq_starts)) return fail(COCO_EINVAL, "NULL batch pointer");
+  LayerRows rows;
+  rows.mask = tree_mask;
+  rows.words = mask_words;
+  return forward_impl(H, first_layer, n_layers, hidden, hidden_rows, row_idx, n_rows, positions,
+                      seq_starts, n_seqs, block_table, ctx_lens, stream, false, &rows);
+}
+
+int coco_layer_sparse_forward(coco_layer_t H, int32_t layer, void* hidden, int64_t hidden_rows,
+                              const int32_t* row_idx, int32_t n_rows, const int32_t* positions,
+                              const int32_t* block_table, const int32_t* ctx_lens,
+                              int8_t* summary, float* scales, int32_t keep_first,
+                              int32_t keep_last, int32_t* selected, int32_t n_select,
+                              coco_stream_t stream) {
+  if (!H) return fail(COCO_EINVAL, "handle is NULL");
+  if (layer < 0 || layer >= H->cfg.n_layers)
+    return fail(COCO_EINVAL, "layer %d out of range", layer);
+  if (n_rows > 0) {
+    const int rc = check_select(H, n_rows, summary, scales, H->layers[layer].num_blocks,
+                                keep_first, keep_last, selected, n_select);
+    if (rc) return rc;
+  }
+  LayerRows rows;
+  rows.summary = summary;
+  rows.scales = scales;
+  rows.keep_first = keep_first;
+  rows.keep_last = keep_last;
+  rows.selected = selected;
+  rows.n_select = n_select;
+  return forward_impl(H, layer, 1, hidden, hidden_rows, row_idx, n_rows, positions, nullptr,
+                      n_rows, block_table, ctx_lens, stream, false, &rows);
 }
 
 int coco_kv_append(coco_layer_t H, int32_t layer, const void* k, const void* v,

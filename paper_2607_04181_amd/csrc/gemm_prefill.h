@@ -554,9 +554,9 @@ __global__ __launch_bounds__(T::NT) void gemm_prefill_kernel(const bf16_t* __res
           *(u32x4_t*)dst = vl;
           *(u32x4_t*)(dst + 64) = vu;
         } else {
-          const u32x2_t sl = slots[RG * p + rq];
-          const int slot = (int)sl.x % kBlockTokens;
-          bf16_t* tile = ea.k_cache + ((int64_t)(int)sl.y * ea.Hkv + (hh - ea.Hq)) * kTile;
+          const int at = (int)slots[RG * p + rq].y, slot = at & (kBlockTokens - 1);
+          bf16_t* tile =
+              ea.k_cache + ((int64_t)(at / kBlockTokens) * ea.Hkv + (hh - ea.Hq)) * kTile;
           *(u32x4_t*)(tile + k_tile_offset(slot, jd0)) = vl;
           *(u32x4_t*)(tile + k_tile_offset(slot, jd0 + 64)) = vu;
         }
@@ -572,26 +572,25 @@ __global__ __launch_bounds__(T::NT) void gemm_prefill_kernel(const bf16_t* __res
         const int lr0 = RG * p + 4 * quad;
         bf16_t* const vbase = ea.v_cache + (int64_t)(hh - ea.Hq - ea.Hkv) * kTile;
         uint32_t e4[4];
-        u32x2_t sl[4];
+        int at[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           e4[e] = f32_to_bf16(st_row(4 * quad + e)[col]);
-          sl[e] = slots[lr0 + e];
+          at[e] = (int)slots[lr0 + e].y;
         }
-        const int t0 = (int)sl[0].x % kBlockTokens;
-        bool run = m0 + lr0 + 3 < M && t0 % 4 == 0;
+        bool run = m0 + lr0 + 3 < M && at[0] % 4 == 0;
 #pragma unroll
-        for (int e = 1; e < 4; ++e)
-          run = run && sl[e].y == sl[0].y && (int)sl[e].x % kBlockTokens == t0 + e;
+        for (int e = 1; e < 4; ++e) run = run && at[e] == at[0] + e;
+        const auto place = [&](int a) {
+          return vbase + (int64_t)(a / kBlockTokens) * ea.Hkv * kTile +
+                 v_tile_offset(a & (kBlockTokens - 1), dim);
+        };
         if (run) {
-          *(u32x2_t*)(vbase + (int64_t)(int)sl[0].y * ea.Hkv * kTile + v_tile_offset(t0, dim)) =
-              u32x2_t{e4[0] | (e4[1] << 16), e4[2] | (e4[3] << 16)};
+          *(u32x2_t*)place(at[0]) = u32x2_t{e4[0] | (e4[1] << 16), e4[2] | (e4[3] << 16)};
         } else {
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            if (m0 + lr0 + e < M)
-              vbase[(int64_t)(int)sl[e].y * ea.Hkv * kTile +
-                    v_tile_offset((int)sl[e].x % kBlockTokens, dim)] = (bf16_t)e4[e];
+            if (m0 + lr0 + e < M) *place(at[e]) = (bf16_t)e4[e];
         }
       }
       __syncthreads();  // the group's staging is read

@@ -52,7 +52,7 @@ struct Work {
   // which prefill has no other use for.
   float* ss = nullptr;
   int32_t* split_off = nullptr;  // decode attention work list
-  int32_t* row_info = nullptr;   // prefill row slots [rows][2] (position, cache block)
+  int32_t* row_info = nullptr;   // prefill row slots [rows][2] (RowSlotArgs)
 };
 
 struct coco_layer {
@@ -110,5 +110,44 @@ namespace coco {
 // the stream is being captured into a graph (the event would then only fire
 // on replays).
 int mark_done(coco_layer* H, hipStream_t st);
+
+// What the rows of a layer call attend where that is not their causal prefix.
+struct LayerRows {
+  // Trees.
+  const uint64_t* mask = nullptr;
+  int words = 0;
+  // Selected blocks.
+  int8_t* summary = nullptr;
+  float* scales = nullptr;
+  int keep_first = 0, keep_last = 0, n_select = 0;
+  int32_t* selected = nullptr;
+};
+
+// The attention operators without their entry points' checks of the handle and
+// batch: what the host can check, validation mode's checks of device arrays
+// (positions may be null), and the launches. q, o: the handle's type; tiled: o
+// of a bf16 handle in tile order.
+int check_tree(const coco_layer* H, int n_rows, const int32_t* seq_starts, int n_seqs,
+               const uint64_t* mask, int words);
+int validate_tree(const coco_layer* H, int n_rows, const int32_t* positions,
+                  const int32_t* seq_starts, int n_seqs, const int32_t* bt, const int32_t* ctx_lens,
+                  int words, int64_t num_blocks, hipStream_t st);
+int run_tree(coco_layer* H, const coco_layer_weights& w, const void* q, void* o, bool tiled,
+             int n_rows, const int32_t* seq_starts, int n_seqs, const int32_t* bt,
+             const int32_t* ctx, const uint64_t* mask, int words, hipStream_t st);
+int check_select(const coco_layer* H, int n_rows, const int8_t* summary, const float* scales,
+                 int64_t num_blocks, int keep_first, int keep_last, const int32_t* selected,
+                 int n_select);
+int run_summarize(coco_layer* H, const coco_layer_weights& w, int8_t* summary, float* scales,
+                  const int32_t* first, const int32_t* ctx, int n_seqs, const int32_t* bt,
+                  hipStream_t st);
+int run_select(coco_layer* H, const int8_t* summary, const float* scales, int64_t num_blocks,
+               const void* q, int n_rows, const int32_t* positions, const int32_t* seq_starts,
+               int n_seqs, const int32_t* bt, const int32_t* ctx, int keep_first, int keep_last,
+               int32_t* selected, int n_select, hipStream_t st);
+int run_sparse(coco_layer* H, const coco_layer_weights& w, const void* q, void* o, bool tiled,
+               int n_rows, const int32_t* positions, const int32_t* seq_starts, int n_seqs,
+               const int32_t* bt, const int32_t* ctx, const int32_t* selected, int n_select,
+               hipStream_t st);
 
 }  // namespace coco

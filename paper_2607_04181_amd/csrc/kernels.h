@@ -47,14 +47,18 @@ LaunchEvents& launch_events();
 
 // ---------------------------------------------------------------- row kernels
 // Prefill row slots (optional output of the gather kernel): row_info[2i] =
-// positions[i] clamped to [0, rope_rows), row_info[2i + 1] = the cache block
-// of that position in row i's sequence (rows of a sequence contiguous).
+// positions[i] clamped to [0, rope_rows), row_info[2i + 1] = 16 * the cache block
+// of that position in row i's sequence + its slot there (rows of a sequence
+// contiguous).
 struct RowSlotArgs {
   const int32_t* positions = nullptr;
   const int32_t* seq_starts = nullptr;
   const int32_t* block_table = nullptr;
   int32_t* row_info = nullptr;  // null: not written
   int n_seqs = 0, max_blocks = 0, rope_rows = 0;
+  // Trees: row i of sequence s is cached at tree_lens[s] - (rows of s) + (its
+  // place among them), not at its position.
+  const int32_t* tree_lens = nullptr;
 };
 
 // h_out[i] = RMSNorm(src[row_idx ? row_idx[i] : i]) * gamma, in tile order
@@ -243,6 +247,7 @@ struct F32EpiArgs {
   float* q_out = nullptr;
   float* k_cache = nullptr;
   float* v_cache = nullptr;
+  const int32_t* tree_lens = nullptr;  // as in RowSlotArgs
   int n_seqs = 0, max_blocks = 0, Hq = 0, Hkv = 0, hd = 0;
 };
 // RMSNorm_1, QKV projection, RoPE, queries to q_out [M][Hq*hd], keys and
@@ -365,9 +370,10 @@ hipError_t launch_attn_rows_f32(const float* q, const float* k_cache, const floa
 // part_o [rows][Hkv][parts][Hq / Hkv][128] and part_ml [..][2] hold them.
 constexpr int kSparsePart = 32;
 inline int sparse_parts(int top) { return (top + kSparsePart - 1) / kSparsePart; }
+// tiled: o in tile order.
 hipError_t launch_sparse_attention_bf16(const uint16_t* q, const uint16_t* k_cache,
                                         const uint16_t* v_cache, const RowKeys& rk, int n_rows,
-                                        int Hq, int Hkv, uint16_t* o, float* part_o,
+                                        int Hq, int Hkv, uint16_t* o, bool tiled, float* part_o,
                                         float* part_ml, hipStream_t st);
 
 // Tree rows of bf16 handles (hd 128). The keys of a sequence are split into

@@ -55,6 +55,7 @@ __global__ __launch_bounds__(kFThreads) void layer_f32_gemm_kernel(const float* 
   __shared__ float inv[TM];
   __shared__ int arow[TM];     // source (QKV: hidden) or output (scatter) row
   __shared__ int pos_s[TM];    // QKV: position
+  __shared__ int slot_s[TM];   // QKV: slot in the cache block
   __shared__ int64_t blk_s[TM];  // QKV: cache block
   __shared__ float rot[MODE == kFQkv ? TM * 16 : 1][2];
 
@@ -159,7 +160,12 @@ __global__ __launch_bounds__(kFThreads) void layer_f32_gemm_kernel(const float* 
       const int seq = row_to_seq(ea.seq_starts, ea.n_seqs, m);
       arow[tid] = ea.row_idx ? ea.row_idx[m] : m;
       pos_s[tid] = pos;
-      blk_s[tid] = ea.block_table[(int64_t)seq * ea.max_blocks + pos / kBlockTokens];
+      int at = pos;
+      if (ea.tree_lens != nullptr)
+        at = min(max(ea.tree_lens[seq] - ea.seq_starts[seq + 1] + m, 0),
+                 ea.max_blocks * kBlockTokens - 1);
+      slot_s[tid] = at % kBlockTokens;
+      blk_s[tid] = ea.block_table[(int64_t)seq * ea.max_blocks + at / kBlockTokens];
     } else if constexpr (MODE == kFScatter || MODE == kFResid) {
       arow[tid] = ea.row_idx ? ea.row_idx[m] : m;
     }
@@ -254,7 +260,7 @@ __global__ __launch_bounds__(kFThreads) void layer_f32_gemm_kernel(const float* 
         dst[0] = v0;
         dst[hd / 2] = v1;
       } else {
-        const int slot = pos_s[rl] % kBlockTokens;
+        const int slot = slot_s[rl];
         const bool key = head < ea.Hq + ea.Hkv;
         const int g = head - ea.Hq - (key ? 0 : ea.Hkv);
         float* tile = (key ? ea.k_cache : ea.v_cache) +

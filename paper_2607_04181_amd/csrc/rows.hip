@@ -60,7 +60,7 @@ __device__ __forceinline__ u32x4_t pack_bf16x8(const float* f) {
 // ----------------------------------------------------------------------------
 // Segment-boundary gather of the sub-batch rows, fused with the first RMSNorm,
 // and the prefill row slots: row_info[i] = (position clamped to the RoPE table,
-// cache block of the position), for the QKV projection's fused epilogue.
+// cache slot), for the QKV projection's fused epilogue.
 // d % 8 == 0: 16-byte vectors, row held in registers.
 //   * Row of a workgroup: consecutive rows run on one XCD
 //     (blockIdx % 8 is the XCD), so the 16 rows that share each 1 KB
@@ -82,11 +82,14 @@ __device__ __forceinline__ void write_row_slot_uniform(const RowSlotArgs& rs, in
     const int mid = (lo + hi + 1) >> 1;
     if (seq_starts[mid] <= i) lo = mid; else hi = mid - 1;
   }
-  const int blk =
-      block_table[(int64_t)lo * rs.max_blocks + min(max(pos, 0) / kBlockTokens, rs.max_blocks - 1)];
+  int at = pos;
+  if (rs.tree_lens != nullptr)
+    at = ((cint_ptr)rs.tree_lens)[lo] - seq_starts[lo + 1] + i;
+  at = min(max(at, 0), rs.max_blocks * kBlockTokens - 1);
+  const int blk = block_table[(int64_t)lo * rs.max_blocks + at / kBlockTokens];
   if (threadIdx.x == 0) {
     rs.row_info[2 * i] = min(max(pos, 0), rs.rope_rows - 1);
-    rs.row_info[2 * i + 1] = blk;
+    rs.row_info[2 * i + 1] = blk * kBlockTokens + at % kBlockTokens;
   }
 }
 

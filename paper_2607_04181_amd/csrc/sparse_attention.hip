@@ -38,9 +38,15 @@ struct SparseArgs {
   int Hq, Hkv, parts;
   float scale_log2;
   bf16_t* o;
+  bool tiled;      // o in tile order
   float* part_o;   // [rows][Hkv][parts][G][128]
   float* part_ml;  // [rows][Hkv][parts][G][2]
 };
+
+__device__ __forceinline__ bf16_t* out_at(const SparseArgs& a, int i, int head, int dim) {
+  const int c = head * HD + dim;
+  return a.o + (a.tiled ? tile_off(i, c, a.Hq * HD) : (int64_t)i * a.Hq * HD + c);
+}
 
 struct Tile {
   u32x4_t k[4], v[4];
@@ -189,8 +195,7 @@ __global__ __launch_bounds__(64 * kWaves, 3) void sparse_attention_kernel(Sparse
     }
     if (a.parts == 1) {
       const float inv = L == 0.f ? 0.f : 1.0f / L;
-      store4(a.o + ((int64_t)i * a.Hq + g * G + h) * HD + dim, y[0] * inv, y[1] * inv, y[2] * inv,
-             y[3] * inv);
+      store4(out_at(a, i, g * G + h, dim), y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv);
     } else {
       *(f32x4_t*)(a.part_o + (at + h) * HD + dim) = y;
       if (dim == 0) {
@@ -237,15 +242,14 @@ __global__ __launch_bounds__(256) void sparse_combine_kernel(SparseArgs a) {
     M = m_new;
   }
   const float inv = L == 0.f ? 0.f : 1.0f / L;
-  store4(a.o + ((int64_t)i * a.Hq + head) * HD + dim, y[0] * inv, y[1] * inv, y[2] * inv,
-         y[3] * inv);
+  store4(out_at(a, i, head, dim), y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv);
 }
 
 }  // namespace
 
 hipError_t launch_sparse_attention_bf16(const uint16_t* q, const uint16_t* k_cache,
                                         const uint16_t* v_cache, const RowKeys& rk, int n_rows,
-                                        int Hq, int Hkv, uint16_t* o, float* part_o,
+                                        int Hq, int Hkv, uint16_t* o, bool tiled, float* part_o,
                                         float* part_ml, hipStream_t st) {
   if (n_rows <= 0) return hipSuccess;
   if (Hq > 16 * Hkv || n_rows > 65535 || Hkv > 65535) return hipErrorInvalidValue;
@@ -259,6 +263,7 @@ hipError_t launch_sparse_attention_bf16(const uint16_t* q, const uint16_t* k_cac
   a.parts = sparse_parts(rk.top);
   a.scale_log2 = kLog2e / sqrtf((float)HD);
   a.o = o;
+  a.tiled = tiled;
   a.part_o = part_o;
   a.part_ml = part_ml;
   COCO_LAUNCH(sparse_attention_kernel, dim3(a.parts, Hkv, n_rows), dim3(64 * kWaves), 0, st, a);

@@ -100,11 +100,38 @@ def test_sparse_calls_refuse_mismatched_shapes():
         coco.coco_sparse_attention(h, 0, q, q, ints(3), None, table, ints(3), sel)
 
 
+def test_layers_refuse_mismatched_shapes():
+    import paper_2607_04181_amd as coco
+    h, rows = handle(), torch.zeros(6, 512, dtype=torch.bfloat16)
+    table, mask = torch.zeros(2, 8, dtype=I32), torch.zeros(5, 1, dtype=torch.int64)
+    batch = [rows, ints(5), ints(5), ints(3), table, ints(2)]
+    with pytest.raises(ValueError, match="seq_starts must be given"):
+        coco.coco_layer_tree_forward(h, 0, 1, *batch[:3], None, *batch[4:], mask)
+    with pytest.raises(ValueError, match="tree_mask must be"):
+        coco.coco_layer_tree_forward(h, 0, 1, *batch, mask[:4])
+    with pytest.raises(ValueError, match="seq_starts must have"):
+        coco.coco_layer_tree_forward(h, 0, 1, *batch[:3], ints(2), *batch[4:], mask)
+    with pytest.raises(ValueError, match="on the GPU"):
+        coco.coco_layer_tree_forward(h, 0, 1, *batch, mask)
+    summary, scales = torch.zeros(30, 2, 2, 128, dtype=torch.int8), torch.zeros(30, 2)
+    sel = torch.zeros(2, 2, 4, dtype=I32)
+    step = [rows, ints(2), ints(2), table, ints(2)]
+    with pytest.raises(ValueError, match="layer's 30 blocks"):
+        coco.coco_layer_sparse_forward(h, 1, *step, summary[:20], scales[:20], 0, 0, sel)
+    with pytest.raises(ValueError, match="selected must be"):
+        coco.coco_layer_sparse_forward(h, 1, *step, summary, scales, 0, 0, sel[:1])
+    with pytest.raises(ValueError, match="ctx_lens has 3"):
+        coco.coco_layer_sparse_forward(h, 1, *step[:4], ints(3), summary, scales, 0, 0, sel)
+    with pytest.raises(ValueError, match="on the GPU"):
+        coco.coco_layer_sparse_forward(h, 1, *step, summary, scales, 0, 0, sel)
+
+
 def test_calls_without_a_handle_are_errors():
     from paper_2607_04181_amd import _lib
     for name in ("coco_kv_alloc", "coco_kv_fork", "coco_kv_free", "coco_kv_copy",
                  "coco_kv_compact", "coco_tree_attention", "coco_kv_summarize",
-                 "coco_block_select", "coco_sparse_attention"):
+                 "coco_block_select", "coco_sparse_attention", "coco_layer_tree_forward",
+                 "coco_layer_sparse_forward"):
         args = [0 if t in (_lib.ctypes.c_int32, _lib.ctypes.c_int64) else None
                 for t in getattr(_lib._lib, name).argtypes]
         assert _lib.raw_call(name, *args) == _lib.COCO_EINVAL
