@@ -200,14 +200,14 @@ hipError_t launch_attn_rows_f32(const float* q, const float* k_cache, const floa
   const int G = Hq / Hkv;
   const int gh = (G % 4 == 0 && hd <= 64) ? 4 : (G % 2 == 0 && hd <= 128) ? 2 : 1;
   const dim3 grid(n_rows, Hq / gh), block(64 * kRowsWaves);
-#define COCO_ROWS(HS, GH)                                                                     \
-  do {                                                                                        \
-    if (rk.mask)                                                                              \
-      COCO_LAUNCH((attn_rows_kernel<HS, GH, true>), grid, block, 0, st, q, k_cache, v_cache,  \
-                  rk, Hq, Hkv, o);                                                            \
-    else                                                                                      \
-      COCO_LAUNCH((attn_rows_kernel<HS, GH, false>), grid, block, 0, st, q, k_cache, v_cache, \
-                  rk, Hq, Hkv, o);                                                            \
+#define COCO_ROWS(HS, GH)                                                                       \
+  do {                                                                                          \
+    if (rk.mask)                                                                                \
+      COCO_LAUNCH_LAST((attn_rows_kernel<HS, GH, true>), grid, block, 0, st, q, k_cache, v_cache, \
+                       rk, Hq, Hkv, o);                                                         \
+    else                                                                                        \
+      COCO_LAUNCH_LAST((attn_rows_kernel<HS, GH, false>), grid, block, 0, st, q, k_cache,       \
+                       v_cache, rk, Hq, Hkv, o);                                                \
   } while (0)
 #define COCO_ROWS4(HS) \
   if (gh == 4) COCO_ROWS(HS, 4); else if (gh == 2) COCO_ROWS(HS, 2); else COCO_ROWS(HS, 1)

@@ -126,6 +126,7 @@ int page_requests(coco_layer* H, int first, int nl, const int32_t* src, const in
       }
     }
   }
+  CallEnd end(H, st, !fork || 2 * nl <= kMaxPools);
   HIPCHK(launch_page_plan(a, st));
   if (fork) {
     const int rc = for_pools(H, first, nl, [&](const CachePools& p, bool tables) -> int {
@@ -136,7 +137,7 @@ int page_requests(coco_layer* H, int first, int nl, const int32_t* src, const in
   } else {
     HIPCHK(launch_page_alloc(a, st));
   }
-  return mark_done(H, st);
+  return end.finish();
 }
 
 // Attention rows' shapes and pointers that the host can check.
@@ -410,9 +411,10 @@ int coco_kv_free(coco_layer_t H, const int32_t* seq_idx, const int32_t* keep_len
       }
     }
   }
+  CallEnd end(H, st);
   HIPCHK(launch_page_free(seq_idx, keep_lens, n, n_seqs, block_table, c.max_blocks_per_seq,
                           ref_counts, blocks, st));
-  return mark_done(H, st);
+  return end.finish();
 }
 
 int coco_kv_copy(coco_layer_t H, int32_t first_layer, int32_t n_layers, const int32_t* src_blocks,
@@ -440,11 +442,12 @@ int coco_kv_copy(coco_layer_t H, int32_t first_layer, int32_t n_layers, const in
       if (to[s[i]] && s[i] != d[i])
         return fail(COCO_EINVAL, "block %d is copied from and to in one call", s[i]);
   }
+  CallEnd end(H, st, 2 * n_layers <= kMaxPools);
   rc = for_pools(H, first_layer, n_layers, [&](const CachePools& p, bool) -> int {
     HIPCHK(launch_page_copy(src_blocks, dst_blocks, n, blocks, p, page_bytes(H->cfg), st));
     return COCO_OK;
   });
-  return rc ? rc : mark_done(H, st);
+  return rc ? rc : end.finish();
 }
 
 int coco_kv_compact(coco_layer_t H, int32_t first_layer, int32_t n_layers, const int32_t* seq_idx,
@@ -491,6 +494,7 @@ int coco_kv_compact(coco_layer_t H, int32_t first_layer, int32_t n_layers, const
       }
     }
   }
+  CallEnd end(H, st, 2 * n_layers <= kMaxPools);
   rc = for_pools(H, first_layer, n_layers, [&](const CachePools& p, bool) -> int {
     if (c.dtype == COCO_BF16)
       HIPCHK(launch_page_compact<uint16_t>(seq_idx, base_lens, kept, kept_starts, n, n_kept,
@@ -502,7 +506,7 @@ int coco_kv_compact(coco_layer_t H, int32_t first_layer, int32_t n_layers, const
                                            c.n_kv_heads, c.head_dim, st));
     return COCO_OK;
   });
-  return rc ? rc : mark_done(H, st);
+  return rc ? rc : end.finish();
 }
 
 int coco_tree_reserve(coco_layer_t H, int32_t max_rows, int32_t max_seqs) {
@@ -551,10 +555,11 @@ int coco_tree_attention(coco_layer_t H, int32_t layer, const void* q, void* o, i
   if (H->validate && (rc = validate_tree(H, n_rows, nullptr, seq_starts, n_seqs, block_table,
                                          ctx_lens, mask_words, w.num_blocks, st)))
     return rc;
+  CallEnd end(H, st, n_seqs <= kTreeLaunchSeqs);
   if ((rc = run_tree(H, w, q, o, false, n_rows, seq_starts, n_seqs, block_table, ctx_lens,
                      tree_mask, mask_words, st)))
     return rc;
-  return mark_done(H, st);
+  return end.finish();
 }
 
 int coco_kv_summarize(coco_layer_t H, int32_t layer, int8_t* summary, float* scales,
@@ -584,9 +589,10 @@ int coco_kv_summarize(coco_layer_t H, int32_t layer, int8_t* summary, float* sca
     for (int s = 0; s < n_seqs; ++s)
       if ((rc = check_blocks(bt, c.max_blocks_per_seq, s, ctx[s], w.num_blocks))) return rc;
   }
+  CallEnd end(H, st);
   if ((rc = run_summarize(H, w, summary, scales, first_lens, ctx_lens, n_seqs, block_table, st)))
     return rc;
-  return mark_done(H, st);
+  return end.finish();
 }
 
 int coco_sparse_reserve(coco_layer_t H, int32_t max_rows, int32_t max_blocks) {
@@ -635,10 +641,11 @@ int coco_block_select(coco_layer_t H, const int8_t* summary, const float* scales
                             num_blocks, ss, ctx, st)))
       return rc;
   }
+  CallEnd end(H, st);
   if ((rc = run_select(H, summary, scales, num_blocks, q, n_rows, positions, seq_starts, n_seqs,
                        block_table, ctx_lens, keep_first, keep_last, selected, n_select, st)))
     return rc;
-  return mark_done(H, st);
+  return end.finish();
 }
 
 int coco_sparse_attention(coco_layer_t H, int32_t layer, const void* q, void* o, int32_t n_rows,
@@ -678,10 +685,11 @@ int coco_sparse_attention(coco_layer_t H, int32_t layer, const void* q, void* o,
         }
       }
   }
+  CallEnd end(H, st);
   if ((rc = run_sparse(H, w, q, o, false, n_rows, positions, seq_starts, n_seqs, block_table,
                        ctx_lens, selected, n_select, st)))
     return rc;
-  return mark_done(H, st);
+  return end.finish();
 }
 
 }  // extern "C"

@@ -64,7 +64,7 @@ struct KernelTimer {
     H->ev_kind.push_back(kind);
     H->ev_stream = st;
     coco::launch_events() =
-        coco::LaunchEvents{H->ev[2 * pair], several ? nullptr : H->ev[2 * pair + 1]};
+        coco::LaunchEvents{H->ev[2 * pair], several ? nullptr : H->ev[2 * pair + 1], nullptr};
   }
   ~KernelTimer() {
     if (pair < 0) return;

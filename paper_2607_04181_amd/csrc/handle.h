@@ -111,6 +111,25 @@ namespace coco {
 // on replays).
 int mark_done(coco_layer* H, hipStream_t st);
 
+// The handle's completion event for a call whose last kernel is launched with
+// COCO_LAUNCH_LAST: that kernel completes it (recorded behind a kernel, the event
+// costs a small call 1 to 2.5 us more). Without such a launch between, or where
+// the call is captured or launches its last kernel in several groups (whole
+// false), finish() is mark_done.
+struct CallEnd {
+  coco_layer* H;
+  hipStream_t st;
+  bool attached = false;
+  CallEnd(coco_layer* h, hipStream_t s, bool whole = true) : H(h), st(s) {
+    hipStreamCaptureStatus cs = hipStreamCaptureStatusNone;
+    attached = whole && hipStreamIsCapturing(s, &cs) == hipSuccess &&
+               cs == hipStreamCaptureStatusNone;
+    if (attached) launch_events().done = H->done;
+  }
+  ~CallEnd() { launch_events().done = nullptr; }
+  int finish() { return attached && !launch_events().done ? COCO_OK : mark_done(H, st); }
+};
+
 // What the rows of a layer call attend where that is not their causal prefix.
 struct LayerRows {
   // Trees.

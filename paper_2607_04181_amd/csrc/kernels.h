@@ -10,8 +10,10 @@ namespace coco {
 // Per-kernel timing (benchmark mode): events that the next kernel launch of
 // this thread passes to hipExtLaunchKernelGGL, which timestamps them at the
 // kernel's own start and end, then clears. Null events: a plain launch.
+// done: an event for the last kernel of a call of a few kernels
+// (COCO_LAUNCH_LAST), which then needs none recorded behind it (CallEnd).
 struct LaunchEvents {
-  hipEvent_t start = nullptr, stop = nullptr;
+  hipEvent_t start = nullptr, stop = nullptr, done = nullptr;
 };
 LaunchEvents& launch_events();
 
@@ -20,7 +22,17 @@ LaunchEvents& launch_events();
     ::coco::LaunchEvents& le_ = ::coco::launch_events();                                      \
     hipExtLaunchKernelGGL(kernel, grid, block, shmem, stream, le_.start, le_.stop, 0,         \
                           __VA_ARGS__);                                                       \
-    le_ = ::coco::LaunchEvents{};                                                             \
+    le_.start = le_.stop = nullptr;                                                           \
+  } while (0)
+
+#define COCO_LAUNCH_LAST(...)                          \
+  do {                                                 \
+    ::coco::LaunchEvents& last_ = ::coco::launch_events(); \
+    if (last_.done) {                                  \
+      last_.stop = last_.done;                         \
+      last_.done = nullptr;                            \
+    }                                                  \
+    COCO_LAUNCH(__VA_ARGS__);                          \
   } while (0)
 
 // KERNEL(head_dim / 32) for a handle of type T: bf16 has one head_dim, fp32 the
@@ -383,6 +395,7 @@ hipError_t launch_sparse_attention_bf16(const uint16_t* q, const uint16_t* k_cac
 // redo [8 + n_rows * Hq] (items drawn per XCD; rows to compute again) must be
 // zero and is left so.
 constexpr int kTreeSplitsFew = 32, kTreeSplits = 16;
+constexpr int kTreeLaunchSeqs = 1024;  // sequences of a launch; more take several
 int64_t tree_column_parts(int64_t max_rows, int64_t max_seqs, int Hq, int Hkv, int max_blocks);
 hipError_t launch_tree_attention_bf16(const uint16_t* q, const uint16_t* k_cache,
                                       const uint16_t* v_cache, const RowKeys& rk, int n_rows,

@@ -318,15 +318,15 @@ hipError_t launch_page_plan(const PageArgs& a, hipStream_t st) {
 
 hipError_t launch_page_alloc(const PageArgs& a, hipStream_t st) {
   if (a.n <= 0) return hipSuccess;
-  COCO_LAUNCH(page_alloc_kernel, dim3(a.n), dim3(kWave), 0, st, a);
+  COCO_LAUNCH_LAST(page_alloc_kernel, dim3(a.n), dim3(kWave), 0, st, a);
   return hipGetLastError();
 }
 
 hipError_t launch_page_fork(const PageArgs& a, const CachePools& pools, int64_t bytes,
                             bool tables, hipStream_t st) {
   if (a.n <= 0) return hipSuccess;
-  COCO_LAUNCH(page_fork_kernel, dim3(a.n, pools.n + (tables ? 1 : 0)), dim3(256), 0, st, a, pools,
-              bytes, tables);
+  COCO_LAUNCH_LAST(page_fork_kernel, dim3(a.n, pools.n + (tables ? 1 : 0)), dim3(256), 0, st, a,
+                   pools, bytes, tables);
   return hipGetLastError();
 }
 
@@ -334,16 +334,16 @@ hipError_t launch_page_free(const int32_t* seq, const int32_t* keep, int n, int 
                             int32_t* table, int max_blocks, int32_t* refs, int64_t num_blocks,
                             hipStream_t st) {
   if (n <= 0) return hipSuccess;
-  COCO_LAUNCH(page_free_kernel, dim3((max_blocks + 255) / 256, n), dim3(256), 0, st, seq, keep,
-              n_seqs, table, max_blocks, refs, num_blocks);
+  COCO_LAUNCH_LAST(page_free_kernel, dim3((max_blocks + 255) / 256, n), dim3(256), 0, st, seq,
+                   keep, n_seqs, table, max_blocks, refs, num_blocks);
   return hipGetLastError();
 }
 
 hipError_t launch_page_copy(const int32_t* src, const int32_t* dst, int n, int64_t num_blocks,
                             const CachePools& pools, int64_t bytes, hipStream_t st) {
   if (n <= 0) return hipSuccess;
-  COCO_LAUNCH(page_copy_kernel, dim3(n, pools.n), dim3(256), 0, st, src, dst, num_blocks, pools,
-              bytes);
+  COCO_LAUNCH_LAST(page_copy_kernel, dim3(n, pools.n), dim3(256), 0, st, src, dst, num_blocks,
+                   pools, bytes);
   return hipGetLastError();
 }
 
@@ -355,8 +355,8 @@ hipError_t launch_page_compact(const int32_t* seq, const int32_t* base, const in
   if (n <= 0 || n_kept <= 0) return hipSuccess;
   if (hd % 32 != 0 || hd > 256 || Hkv > 65535) return hipErrorInvalidValue;
 #define COCO_COMPACT(HS)                                                                        \
-  COCO_LAUNCH((page_compact_kernel<T, HS>), dim3(n, Hkv, pools.n), dim3(256), 0, st, seq, base, \
-              kept, starts, n_kept, table, n_seqs, max_blocks, num_blocks, pools, Hkv)
+  COCO_LAUNCH_LAST((page_compact_kernel<T, HS>), dim3(n, Hkv, pools.n), dim3(256), 0, st, seq,  \
+                   base, kept, starts, n_kept, table, n_seqs, max_blocks, num_blocks, pools, Hkv)
   COCO_BY_HEAD_DIM(COCO_COMPACT);
 #undef COCO_COMPACT
   return hipGetLastError();

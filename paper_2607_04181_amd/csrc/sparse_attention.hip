@@ -266,9 +266,13 @@ hipError_t launch_sparse_attention_bf16(const uint16_t* q, const uint16_t* k_cac
   a.tiled = tiled;
   a.part_o = part_o;
   a.part_ml = part_ml;
-  COCO_LAUNCH(sparse_attention_kernel, dim3(a.parts, Hkv, n_rows), dim3(64 * kWaves), 0, st, a);
-  if (a.parts > 1)
-    COCO_LAUNCH(sparse_combine_kernel, dim3(n_rows, (Hq + 7) / 8), dim3(256), 0, st, a);
+  const dim3 grid(a.parts, Hkv, n_rows), block(64 * kWaves);
+  if (a.parts == 1) {
+    COCO_LAUNCH_LAST(sparse_attention_kernel, grid, block, 0, st, a);
+  } else {
+    COCO_LAUNCH(sparse_attention_kernel, grid, block, 0, st, a);
+    COCO_LAUNCH_LAST(sparse_combine_kernel, dim3(n_rows, (Hq + 7) / 8), dim3(256), 0, st, a);
+  }
   return hipGetLastError();
 }
 

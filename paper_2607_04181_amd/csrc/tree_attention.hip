@@ -49,7 +49,7 @@ constexpr int kTile = kBlockTokens * HD;
 constexpr int kRing = 4;    // stages in LDS
 constexpr int kStage = 4 * kTile;  // elements: keys and values of two blocks
 constexpr int kXCDs = 8;
-constexpr int kMaxSeqs = 1024;  // sequences of a launch
+constexpr int kMaxSeqs = kTreeLaunchSeqs;
 constexpr float kLazy = 8.f;  // log2 units a running max may lag
 
 struct TreeSeq {
@@ -657,8 +657,8 @@ hipError_t launch_tree_attention_bf16(const uint16_t* q, const uint16_t* k_cache
     a.rk.block_table = rk.block_table + (int64_t)s0 * rk.max_blocks;
     a.rk.n_seqs = rk.n_seqs - s0 < kMaxSeqs ? rk.n_seqs - s0 : kMaxSeqs;
     COCO_LAUNCH(tree_attention_kernel, dim3(2 * num_cus), dim3(kThreads), 0, st, a);
-    COCO_LAUNCH(tree_combine_kernel, dim3(n_rows, (Hq + kMergeHeads - 1) / kMergeHeads),
-                dim3(32 * kMergeHeads), 0, st, a);
+    COCO_LAUNCH_LAST(tree_combine_kernel, dim3(n_rows, (Hq + kMergeHeads - 1) / kMergeHeads),
+                     dim3(32 * kMergeHeads), 0, st, a);
   }
   return hipGetLastError();
 }

@@ -171,6 +171,19 @@ def test_long_context_and_odd_queries(dtype, hq, hkv, hd):
     r.check_attention()
 
 
+@pytest.mark.parametrize("dtype,hq,hkv,hd", [("bf16", 4, 1, 128), ("f32", 3, 1, 32)])
+def test_contexts_of_more_than_8192_blocks(dtype, hq, hkv, hd):
+    r = Rows(dtype, hq, hkv, hd, [16 * 8192, 70, 16 * 8192 + 33, 16 * 10000], top=33, seed=9)
+    r.summarize()
+    for first, last in ((1, 4), (0, 0), (20, 13)):
+        r.select(first, last)
+        torch.cuda.synchronize()
+        r.check_select(first, last)
+    r.select(1, 4)
+    r.attention()
+    r.check_attention()
+
+
 @pytest.mark.parametrize("dtype,hq,hkv,hd", [("bf16", 8, 2, 128), ("f32", 4, 2, 64)])
 def test_lists_of_the_callers_own(dtype, hq, hkv, hd):
     """Any order, gaps, entries outside the row's blocks, an empty list; keys
