@@ -401,8 +401,8 @@ int coco_kv_summarize(coco_layer_t h, int32_t layer, int8_t* summary, float* sca
                       const int32_t* first_lens, const int32_t* ctx_lens, int32_t n_seqs,
                       const int32_t* block_table, coco_stream_t stream);
 
-/* Make room for block_select / sparse_attention calls of up to max_rows rows
- * and max_blocks selected blocks (as coco_tree_reserve). */
+/* Make room for calls that select or attend blocks of up to max_rows rows (at
+ * most 65535) and max_blocks selected blocks (as coco_tree_reserve). */
 int coco_sparse_reserve(coco_layer_t h, int32_t max_rows, int32_t max_blocks);
 
 /* Choose n_select blocks of its sequence for each row and kv head. The row

@@ -597,8 +597,8 @@ int coco_kv_summarize(coco_layer_t H, int32_t layer, int8_t* summary, float* sca
 
 int coco_sparse_reserve(coco_layer_t H, int32_t max_rows, int32_t max_blocks) {
   if (!H) return fail(COCO_EINVAL, "handle is NULL");
-  if (max_rows < 1 || max_rows > 65535 || max_blocks < 1)
-    return fail(COCO_EINVAL, "max_rows = %d outside [1, 65535] or max_blocks = %d below 1",
+  if (max_rows < 1 || max_rows > 65535 || max_blocks < 1 || max_blocks > (1 << 24))
+    return fail(COCO_EINVAL, "max_rows = %d outside [1, 65535] or max_blocks = %d outside [1, 2^24]",
                 max_rows, max_blocks);
   const int rows = max_rows > H->sparse_rows ? max_rows : H->sparse_rows;
   const int top = max_blocks > H->sparse_top ? max_blocks : H->sparse_top;

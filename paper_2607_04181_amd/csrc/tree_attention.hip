@@ -15,11 +15,15 @@
 // per CU. They share the keys through LDS, 32 at a time, in a ring of four
 // stages with three on their way: what a tile of few columns is bound by is the
 // bytes in flight. (Eight waves of 256 columns and stages of 128 keys, two in
-// LDS, reached 2.7 TB/s on 64 sequences of 4 nodes and 4k keys; this 5.) Many
-// columns are bound by products and softmax, which take about as long each; of
-// the two waves of a SIMD, in different workgroups, one multiplies while the
-// other does vector work. The column tiles of the same keys run at the same
-// time on one XCD and read them from its L2.
+// LDS, reached 2.7 TB/s on 64 sequences of 4 nodes and 4k keys; this 4.2, of the
+// 4.9 of a large copy.) Many columns are bound by products and softmax, which
+// take about as long each and of which the two waves of a SIMD, in different
+// workgroups, overlap about a third: 480 TFLOP/s for 32 trees of up to 64
+// nodes, merge included, of the 1150 of a large bf16 product. (Scheduling by
+// hand or priorities around the products changed it by less than 3%; 64 columns
+// per wave, which would halve the operand reads, need more than the 512
+// registers of a wave alone on its SIMD.) The column tiles of the same keys run
+// at the same time on one XCD and read them from its L2.
 //
 // The keys of a sequence are split into parts (tree_part) that depend on its
 // own length and columns only, merged by a second kernel in order: a row's
@@ -59,10 +63,14 @@ struct TreeSeq {
 };
 
 // Keys of one of the parts that `len` keys of a sequence with `cols` columns
-// are split into. Few columns: one stage (128 keys), so that one sequence fills
+// are split into. Few columns: a part of 128 keys, so that one sequence fills
 // the chip; more columns make a part's partial result (512 bytes per column)
-// dear next to its keys (512 bytes each), so parts grow with them. The number
-// of parts falls with cols and grows with len (tree_column_parts counts on it).
+// dear next to its keys (512 bytes each), so parts grow with them. Measured:
+// parts of 512 keys instead of 1024 gain one or eight trees of 26 nodes over 2k
+// keys 16 and 12% and cost 64 of them 6 and 32 trees of 64 nodes 13%; parts
+// of 2048 above 256 columns gain the latter 9% and cost one of them 28. The
+// number of parts falls with cols and grows with len (tree_column_parts counts
+// on it).
 __host__ __device__ __forceinline__ int tree_part(int64_t cols, int len) {
   const int least = cols <= 16 ? 128 : cols <= 64 ? 512 : 1024;
   const int most = cols <= 128 ? kTreeSplitsFew : kTreeSplits;
@@ -543,6 +551,7 @@ __global__ __launch_bounds__(32 * kMergeHeads) void tree_combine_kernel(TreeArgs
   if (!again) {
     const int64_t idx =
         a.plan[2 * s] + ((int64_t)(row - a.rk.seq_starts[s]) * a.Hq + head) * splits;
+    if (idx + splits > a.part_cap) return;  // (as the parts' kernel)
     // Four parts at a time, all their loads together.
     for (int p0 = 0; p0 < splits; p0 += 4) {
       f32x4_t v[4];

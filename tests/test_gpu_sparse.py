@@ -261,6 +261,9 @@ def test_refusals():
         r.select(2, 2)
     with pytest.raises(coco.CocoError, match="keep_first"):
         r.select(-1, 2)
+    for rows, blocks in ((0, 3), (65536, 3), (2, 0), (2, (1 << 24) + 1)):
+        with pytest.raises(coco.CocoError, match="outside"):
+            coco.coco_sparse_reserve(h, rows, blocks)
     more = torch.empty(2, 2, 4, dtype=torch.int32, device="cuda")
     with pytest.raises(coco.CocoError, match="coco_sparse_reserve") as e:
         coco.coco_block_select(h, r.summary, r.scales, r.q, pos, None, table, lens, 0, 0, more)

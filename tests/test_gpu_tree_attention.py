@@ -166,6 +166,18 @@ def test_rows_do_not_depend_on_the_rest_of_the_call(dtype, hq, hkv, hd):
         assert torch.equal(o, whole[rows]), pick
 
 
+@pytest.mark.parametrize("dtype,hq,hkv,hd", [("bf16", 8, 2, 128), ("f32", 4, 2, 64)])
+def test_more_sequences_than_a_launch_takes(dtype, hq, hkv, hd):
+    rng = np.random.default_rng(5)
+    trees = [(int(p), int(n)) for p, n in zip(rng.integers(0, 40, 2100), rng.integers(0, 3, 2100))]
+    trees[1023], trees[1024], trees[2099] = (500, 30), (400, 2), (700, 20)
+    call = Call(dtype, hq, hkv, hd, trees, seed=18)
+    for _ in range(2):  # the counters of every launch are left as they were found
+        call.o.fill_(7.0)
+        call.run()
+        call.check()
+
+
 def test_blocks_past_32_bit_offsets():
     """Pools of more than 2^31 elements, the sequence in their last blocks."""
     hkv, n = 8, (1 << 31) // (8 * B * 128) + 64
