@@ -266,12 +266,13 @@ def coco_kv_append(h: Handle, layer: int, k, v, seq_idx, positions, block_table,
     for name, t in (("k", k), ("v", v)):
         if t.dtype != _elem_dtype(cfg):
             raise TypeError(f"{name} must be {_elem_dtype(cfg)}, got {t.dtype}")
-        _shape_check(t.numel() == n_tok * per_tok,
-                     f"{name} must hold [{n_tok}, {cfg.n_kv_heads}, {cfg.head_dim}] elements")
-    _shape_check(seq_idx.numel() == n_tok, f"seq_idx has {seq_idx.numel()} entries for {n_tok} tokens")
-    _shape_check(block_table.dim() == 2 and block_table.shape[1] == cfg.max_blocks_per_seq,
-                 f"block_table must be [n_seqs, {cfg.max_blocks_per_seq}], "
-                 f"got {tuple(block_table.shape)}")
+        if t.numel() != n_tok * per_tok:
+            raise ValueError(f"{name} must hold [{n_tok}, {cfg.n_kv_heads}, {cfg.head_dim}] elements")
+    if seq_idx.numel() != n_tok:
+        raise ValueError(f"seq_idx has {seq_idx.numel()} entries for {n_tok} tokens")
+    if block_table.dim() != 2 or block_table.shape[1] != cfg.max_blocks_per_seq:
+        raise ValueError(f"block_table must be [n_seqs, {cfg.max_blocks_per_seq}], "
+                         f"got {tuple(block_table.shape)}")
     _check(_lib.coco_kv_append(h.raw, layer, _ptr(k, what="k"), _ptr(v, what="v"),
                                _ptr(seq_idx, i32, "seq_idx"), _ptr(positions, i32, "positions"),
                                int(positions.numel()), _ptr(block_table, i32, "block_table"),

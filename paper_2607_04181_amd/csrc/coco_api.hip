@@ -1067,6 +1067,7 @@ int coco_kv_append(coco_layer_t H, int32_t layer, const void* k, const void* v,
     }
   }
   const coco_layer_weights& w = H->layers[layer];
+  CallEnd end(H, st);
   if (c.dtype == COCO_BF16)
     HIPCHK(launch_kv_append<bf16_t>((const bf16_t*)k, (const bf16_t*)v, seq_idx, positions, n_tok,
                                     c.n_kv_heads, c.head_dim, block_table, c.max_blocks_per_seq,
@@ -1075,7 +1076,7 @@ int coco_kv_append(coco_layer_t H, int32_t layer, const void* k, const void* v,
     HIPCHK(launch_kv_append<float>((const float*)k, (const float*)v, seq_idx, positions, n_tok,
                                    c.n_kv_heads, c.head_dim, block_table, c.max_blocks_per_seq,
                                    (float*)w.k_cache, (float*)w.v_cache, st));
-  return mark_done(H, st);
+  return end.finish();
 }
 
 }  // extern "C"

@@ -65,6 +65,16 @@ __device__ __forceinline__ int plan_scan(int x, int* sums, int& all) {
 __global__ __launch_bounds__(kPlanThreads) void page_plan_kernel(PageArgs a) {
   __shared__ int sums[kPlanWaves];
   const int tid = threadIdx.x;
+  // Counts of the first round of the search below, read while the needs are
+  // found.
+  int32_t r[kPlanIds];
+  auto counts = [&](int64_t base) {
+    const int64_t first = base + tid * kPlanIds;
+#pragma unroll
+    for (int u = 0; u < kPlanIds; ++u)
+      r[u] = a.refs[first + u < a.num_blocks ? first + u : a.num_blocks - 1];
+  };
+  counts(0);
   if (a.src == nullptr) {
     // What each request needs, into off[]: a wave per request, or 16 lanes
     // where there are more requests than waves (reads in flight, not lanes, are
@@ -92,10 +102,10 @@ __global__ __launch_bounds__(kPlanThreads) void page_plan_kernel(PageArgs a) {
   }
   // Their places in the list, in request order (off[] becomes the exclusive
   // sum), and in status[] what each needs.
-  int total = 0;
+  int total = 0, need = 0, at = 0;  // (of the thread's last request)
   for (int i0 = 0; i0 < a.n; i0 += kPlanThreads) {
     const int i = i0 + tid;
-    int need = 0;
+    need = 0;
     if (i < a.n) {
       if (a.src == nullptr)
         need = a.off[i];
@@ -104,8 +114,9 @@ __global__ __launch_bounds__(kPlanThreads) void page_plan_kernel(PageArgs a) {
     }
     int all;
     const int before = plan_scan(max(need, 0), sums, all);
+    at = total + before;
     if (i < a.n) {
-      a.off[i] = total + before;
+      a.off[i] = at;
       a.status[i] = need;
     }
     total += all;
@@ -115,10 +126,7 @@ __global__ __launch_bounds__(kPlanThreads) void page_plan_kernel(PageArgs a) {
   for (int64_t base = 0; base < a.num_blocks && found < total;
        base += kPlanThreads * kPlanIds) {
     const int64_t first = base + tid * kPlanIds;
-    int32_t r[kPlanIds];
-#pragma unroll
-    for (int u = 0; u < kPlanIds; ++u)
-      r[u] = a.refs[first + u < a.num_blocks ? first + u : a.num_blocks - 1];
+    if (base > 0) counts(base);
     uint32_t free_ids = 0;
 #pragma unroll
     for (int u = 0; u < kPlanIds; ++u)
@@ -130,9 +138,11 @@ __global__ __launch_bounds__(kPlanThreads) void page_plan_kernel(PageArgs a) {
     found += all;
   }
   // A request is served while those up to it fit.
-  for (int i = tid; i < a.n; i += kPlanThreads) {
-    const int need = a.status[i];
-    a.status[i] = need >= 0 && (need == 0 || a.off[i] + need <= found);
+  const int last = (a.n - 1) / kPlanThreads * kPlanThreads + tid;
+  if (last < a.n) a.status[last] = need >= 0 && (need == 0 || at + need <= found);
+  for (int i = tid; i < last && i < a.n; i += kPlanThreads) {
+    const int n = a.status[i];
+    a.status[i] = n >= 0 && (n == 0 || a.off[i] + n <= found);
   }
 }
 

@@ -694,13 +694,13 @@ hipError_t launch_kv_append(const T* k, const T* v, const int32_t* seq_idx,
   const int64_t wgs = (int64_t)((n - 1) / kApTok + 1) * Hkv;
   if (wgs > 0x7fffffff) return hipErrorInvalidValue;
   if (hd == 128)
-    COCO_LAUNCH((kv_append_kernel<T, 128>), dim3((unsigned)wgs), dim3(kRowThreads), 0, st, k, v,
-                seq_idx, positions, n, Hkv, hd, block_table, max_blocks, aligned, k_cache,
-                v_cache);
+    COCO_LAUNCH_LAST((kv_append_kernel<T, 128>), dim3((unsigned)wgs), dim3(kRowThreads), 0, st, k,
+                     v, seq_idx, positions, n, Hkv, hd, block_table, max_blocks, aligned, k_cache,
+                     v_cache);
   else
-    COCO_LAUNCH((kv_append_kernel<T, 0>), dim3((unsigned)wgs), dim3(kRowThreads), 0, st, k, v,
-                seq_idx, positions, n, Hkv, hd, block_table, max_blocks, aligned, k_cache,
-                v_cache);
+    COCO_LAUNCH_LAST((kv_append_kernel<T, 0>), dim3((unsigned)wgs), dim3(kRowThreads), 0, st, k, v,
+                     seq_idx, positions, n, Hkv, hd, block_table, max_blocks, aligned, k_cache,
+                     v_cache);
   return hipGetLastError();
 }
 
