@@ -175,18 +175,24 @@ constexpr int kScoreHeads = 64;  // query heads of a group at a time
 template <typename T, int HS>
 __global__ __launch_bounds__(64 * kScoreWaves) void block_score_kernel(
     const T* __restrict__ q, const int8_t* __restrict__ summary, const float* __restrict__ scales,
-    RowKeys rk, int Hq, int Hkv, int64_t stride, uint32_t* __restrict__ keys) {
+    RowKeys rk, int n_rows, int chunks, int Hq, int Hkv, int64_t stride,
+    uint32_t* __restrict__ keys) {
   constexpr int hd = 32 * HS;
   __shared__ __attribute__((aligned(16))) int8_t q8[kScoreHeads][2 * hd + 16];
   __shared__ float red[kScoreWaves];
-  const int i = blockIdx.z, g = blockIdx.y, G = Hq / Hkv;
+  // The heads of a (row, chunk) run on one XCD (blockIdx % 8): they share the
+  // lines of the scales and of the block table.
+  const int at8 = blockIdx.x / 8, g = at8 % Hkv, unit = at8 / Hkv * 8 + blockIdx.x % 8;
+  const int i = unit / chunks, chunk = unit - i * chunks;
+  if (i >= n_rows) return;
+  const int G = Hq / Hkv;
   const int lane = threadIdx.x & 63;
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c16 = lane & 15, j4 = lane >> 4;
   const int s = row_to_seq(rk.seq_starts, rk.n_seqs, i);
   const int nb = (row_keys(rk, s, i) + kBlockTokens - 1) / kBlockTokens;
   // Rows that choose all their blocks need no scores.
-  if (nb <= rk.top || (int)blockIdx.x * 64 * kScoreWaves >= nb) return;
+  if (nb <= rk.top || chunk * 64 * kScoreWaves >= nb) return;
   const int32_t* bt = rk.block_table + (int64_t)s * rk.max_blocks;
 
   i32x4_t sv[4][HS];
@@ -203,7 +209,7 @@ __global__ __launch_bounds__(64 * kScoreWaves) void block_score_kernel(
       for (int k = 0; k < HS; ++k) sv[u][k] = *(const i32x4_t*)(sp + 64 * k);
     }
   };
-  const int first = (blockIdx.x * kScoreWaves + wv) * 64;
+  const int first = (chunk * kScoreWaves + wv) * 64;
   if (first < nb) load(first);
 
   const T* qp = q + ((int64_t)i * Hq + g * G) * hd;
@@ -230,7 +236,7 @@ __global__ __launch_bounds__(64 * kScoreWaves) void block_score_kernel(
       q8[h][hd + d] = (int8_t)min(b, 0);
     }
     __syncthreads();
-    for (int b0 = first; b0 < nb; b0 += gridDim.x * kScoreWaves * 64) {
+    for (int b0 = first; b0 < nb; b0 += chunks * kScoreWaves * 64) {
       if (h0 != 0 || b0 != first) load(b0);
       int best[4] = {INT32_MIN, INT32_MIN, INT32_MIN, INT32_MIN};
       for (int ht = 0; ht < padded; ht += 16) {
@@ -270,11 +276,7 @@ constexpr int kSelChunk = kSelThreads * kSelKeys;
 // once every thread has passed the next barrier.
 __device__ __forceinline__ int sel_scan(int x, int* red, int& all) {
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
-#pragma unroll
-  for (int d = 1; d < kWave; d <<= 1) {
-    const int y = __shfl_up(x, d, kWave);
-    if (lane >= d) x += y;
-  }
+  x = wave_scan(x);
   if (lane == kWave - 1) red[wv] = x;
   __syncthreads();
   all = 0;
@@ -452,12 +454,15 @@ hipError_t launch_block_select(const T* q, const int8_t* summary, const float* s
                                hipStream_t st) {
   if (n_rows <= 0) return hipSuccess;
   if (hd % 32 != 0 || hd > 256 || n_rows > 65535 || Hkv > 65535) return hipErrorInvalidValue;
-  const int chunks = (rk.max_blocks + 64 * kScoreWaves - 1) / (64 * kScoreWaves);
-  const dim3 grid(chunks < 16 ? chunks : 16, Hkv, n_rows);
+  int chunks = (rk.max_blocks + 64 * kScoreWaves - 1) / (64 * kScoreWaves);
+  if (chunks > 16) chunks = 16;
+  const int64_t wgs = ((int64_t)chunks * n_rows + 7) / 8 * 8 * Hkv;
+  if (wgs > INT32_MAX) return hipErrorInvalidValue;
+  const dim3 grid((unsigned)wgs);
   const int64_t stride = select_stride(rk.max_blocks);
 #define COCO_SCORE(HS)                                                                       \
   COCO_LAUNCH((block_score_kernel<T, HS>), grid, dim3(64 * kScoreWaves), 0, st, q, summary, \
-              scales, rk, Hq, Hkv, stride, keys)
+              scales, rk, n_rows, chunks, Hq, Hkv, stride, keys)
   COCO_BY_HEAD_DIM(COCO_SCORE);
 #undef COCO_SCORE
   RowKeys chosen = rk;

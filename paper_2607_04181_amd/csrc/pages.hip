@@ -20,17 +20,6 @@ constexpr int kPlanWaves = kPlanThreads / kWave;
 constexpr int kPlanIds = 16;      // consecutive blocks a thread looks at per round
 constexpr int kPlanEntries = 8;   // table entries a lane reads at a time
 
-// Inclusive sum over a wave's lanes.
-__device__ __forceinline__ int wave_scan(int x) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int d = 1; d < kWave; d <<= 1) {
-    const int y = __shfl_up(x, d, kWave);
-    if (lane >= d) x += y;
-  }
-  return x;
-}
-
 // Blocks that request i needs; -1: it names no valid row or length.
 //   alloc: its row's empty entries below ceil(len / 16);
 //   fork: one, where the shared length ends inside a block.
