@@ -75,7 +75,8 @@ __global__ __launch_bounds__(64 * kRowsWaves) void attn_rows_kernel(
   const int blocks = (n + kBlockTokens - 1) / kBlockTokens;
   entries = TREE ? blocks : rk.top;
   const int32_t* bt = rk.block_table + (int64_t)s * rk.max_blocks;
-  const float scale = 1.0f / sqrtf((float)hd);
+  // Scores in powers of two: 2^x is one instruction, within 1 ulp.
+  const float scale_log2 = 1.4426950408889634f / sqrtf((float)hd);
 
   // This lane's part of the queries: dims 32 p + 8 j4 .. + 7.
   F8 qv[GH][HS];
@@ -93,9 +94,21 @@ __global__ __launch_bounds__(64 * kRowsWaves) void attn_rows_kernel(
 #pragma unroll
     for (int p = 0; p < HS; ++p) acc[e][p][0] = acc[e][p][1] = 0.f;
   }
-  for (int x = wv; x < entries; x += kRowsWaves) {
-    const int b = TREE ? x : list[x];
-    if (!TREE && (b < 0 || b >= blocks)) continue;
+  // A wave's next 64 entries in its lanes, block of the sequence and of the pool
+  // (-1: nothing there), so that an entry costs one dependent read, not three.
+  // (Reading a tile while the one before is attended gained nothing more: two
+  // waves to a SIMD, it is the instructions that take the time.)
+  int b_l = -1, blk_l = 0;
+  for (int x = 0; wv + x * kRowsWaves < entries; ++x) {
+    if (x % kWave == 0) {
+      const int mine = wv + (x + lane) * kRowsWaves;
+      b_l = -1;
+      if (mine < entries) b_l = TREE ? mine : list[mine];
+      if (b_l >= blocks) b_l = -1;
+      if (b_l >= 0) blk_l = bt[b_l];
+    }
+    const int b = __builtin_amdgcn_readlane(b_l, x % kWave);
+    if (b < 0) continue;
     const int tok0 = b * kBlockTokens;
     uint32_t seen;
     if constexpr (TREE) {
@@ -104,7 +117,8 @@ __global__ __launch_bounds__(64 * kRowsWaves) void attn_rows_kernel(
     } else {
       seen = n - tok0 < 16 ? (1u << (n - tok0)) - 1 : 0xFFFFu;
     }
-    const int64_t tile = ((int64_t)bt[b] * Hkv + g) * (kBlockTokens * hd);
+    const int64_t tile =
+        ((int64_t)__builtin_amdgcn_readlane(blk_l, x % kWave) * Hkv + g) * (kBlockTokens * hd);
     F8 kf[HS], vf[HS];
 #pragma unroll
     for (int p = 0; p < HS; ++p) {
@@ -113,11 +127,13 @@ __global__ __launch_bounds__(64 * kRowsWaves) void attn_rows_kernel(
     }
     const bool live = seen >> t & 1;
     // Values of tokens that the row does not see may be anything, NaN among it.
+    if (seen != 0xFFFFu) {
 #pragma unroll
-    for (int p = 0; p < HS; ++p)
+      for (int p = 0; p < HS; ++p)
 #pragma unroll
-      for (int c = 0; c < 8; ++c)
-        if (!(seen >> (4 * j4 + c % 4) & 1)) vf[p].e[c] = 0.f;
+        for (int c = 0; c < 8; ++c)
+          if (!(seen >> (4 * j4 + c % 4) & 1)) vf[p].e[c] = 0.f;
+    }
 #pragma unroll
     for (int e = 0; e < GH; ++e) {
       float z = 0.f;
@@ -125,21 +141,14 @@ __global__ __launch_bounds__(64 * kRowsWaves) void attn_rows_kernel(
       for (int p = 0; p < HS; ++p)
 #pragma unroll
         for (int c = 0; c < 8; ++c) z = fmaf(qv[e][p].e[c], kf[p].e[c], z);
-      z += __shfl_xor(z, 16, kWave);
-      z += __shfl_xor(z, 32, kWave);
-      z = live ? z * scale : -INFINITY;
-      float mx = z;
-#pragma unroll
-      for (int d = 8; d > 0; d >>= 1) mx = fmaxf(mx, __shfl_xor(mx, d, kWave));
-      const float m_new = fmaxf(m[e], mx);
+      z = col_sum4(z);
+      z = live ? z * scale_log2 : -INFINITY;
+      const float m_new = fmaxf(m[e], row_max16(z));
       // A block of keys that all score -inf leaves m at -inf.
       const float m_ref = m_new == -INFINITY ? 0.f : m_new;
-      const float alpha = expf(m[e] - m_ref);
-      const float pr = expf(z - m_ref);
-      float ls = pr;
-#pragma unroll
-      for (int d = 8; d > 0; d >>= 1) ls += __shfl_xor(ls, d, kWave);
-      l[e] = l[e] * alpha + ls;
+      const float alpha = __builtin_amdgcn_exp2f(m[e] - m_ref);
+      const float pr = __builtin_amdgcn_exp2f(z - m_ref);
+      l[e] = fmaf(l[e], alpha, row_sum16(pr));
       m[e] = m_new;
       float p4[4];
 #pragma unroll
@@ -166,8 +175,7 @@ __global__ __launch_bounds__(64 * kRowsWaves) void attn_rows_kernel(
 #pragma unroll
       for (int f = 0; f < 2; ++f) {
         float a = acc[e][p][f];  // dim 32 p + 16 f + lane % 16, tokens 4 j4 ..
-        a += __shfl_xor(a, 16, kWave);
-        a += __shfl_xor(a, 32, kWave);
+        a = col_sum4(a);
         if (j4 == 0) sm_o[wv][e][32 * p + 16 * f + t] = a;
       }
   }
@@ -181,7 +189,7 @@ __global__ __launch_bounds__(64 * kRowsWaves) void attn_rows_kernel(
     float a = 0.f, L = 0.f;
 #pragma unroll
     for (int w = 0; w < kRowsWaves; ++w) {
-      const float f = expf(sm_m[w][e] - ref);
+      const float f = __builtin_amdgcn_exp2f(sm_m[w][e] - ref);
       a = fmaf(f, sm_o[w][e][dim], a);
       L = fmaf(f, sm_l[w][e], L);
     }
@@ -193,12 +201,16 @@ __global__ __launch_bounds__(64 * kRowsWaves) void attn_rows_kernel(
 
 hipError_t launch_attn_rows_f32(const float* q, const float* k_cache, const float* v_cache,
                                 const RowKeys& rk, int n_rows, int Hq, int Hkv, int hd, float* o,
-                                hipStream_t st) {
+                                int num_cus, hipStream_t st) {
   if (n_rows <= 0) return hipSuccess;
   // Heads per workgroup: they share the key/value loads; the queries they
-  // keep in registers (hd / 4 floats per lane each) bound their number.
+  // keep in registers (hd / 4 floats per lane each) bound their number. Fewer of
+  // them while the call leaves CUs without a workgroup (a head's bits are its own):
+  // 5 rows of 16 heads over 16k keys 85 us with one head, 169 with four; 5 rows of
+  // 24 blocks 4.4 and 7.8.
   const int G = Hq / Hkv;
-  const int gh = (G % 4 == 0 && hd <= 64) ? 4 : (G % 2 == 0 && hd <= 128) ? 2 : 1;
+  int gh = (G % 4 == 0 && hd <= 64) ? 4 : (G % 2 == 0 && hd <= 128) ? 2 : 1;
+  while (gh > 1 && (int64_t)n_rows * (Hq / gh) < num_cus) gh /= 2;
   const dim3 grid(n_rows, Hq / gh), block(64 * kRowsWaves);
 #define COCO_ROWS(HS, GH)                                                                       \
   do {                                                                                          \

@@ -276,7 +276,8 @@ int run_tree(coco_layer* H, const coco_layer_weights& w, const void* q, void* o,
                                       H->num_cus, st));
   else
     HIPCHK(launch_attn_rows_f32((const float*)q, (const float*)w.k_cache, (const float*)w.v_cache,
-                                rk, n_rows, c.n_q_heads, c.n_kv_heads, c.head_dim, (float*)o, st));
+                                rk, n_rows, c.n_q_heads, c.n_kv_heads, c.head_dim, (float*)o,
+                                H->num_cus, st));
   return COCO_OK;
 }
 
@@ -343,7 +344,8 @@ int run_sparse(coco_layer* H, const coco_layer_weights& w, const void* q, void* 
                                         H->sparse_part_ml, st));
   else
     HIPCHK(launch_attn_rows_f32((const float*)q, (const float*)w.k_cache, (const float*)w.v_cache,
-                                rk, n_rows, c.n_q_heads, c.n_kv_heads, c.head_dim, (float*)o, st));
+                                rk, n_rows, c.n_q_heads, c.n_kv_heads, c.head_dim, (float*)o,
+                                H->num_cus, st));
   return COCO_OK;
 }
 

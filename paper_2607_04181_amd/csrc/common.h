@@ -109,6 +109,26 @@ __device__ __forceinline__ float col_sum4(float x) {
   return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
+// Reductions over the 16 lanes of a row (lane / 16): lanes exchanged within
+// quads, then eight and sixteen mirrored. Every lane gets the same bits.
+template <int CTRL>
+__device__ __forceinline__ float row_swap(float x) {
+  return __uint_as_float(
+      __builtin_amdgcn_update_dpp(0, __float_as_uint(x), CTRL, 0xF, 0xF, false));
+}
+__device__ __forceinline__ float row_max16(float x) {
+  x = fmaxf(x, row_swap<0xB1>(x));
+  x = fmaxf(x, row_swap<0x4E>(x));
+  x = fmaxf(x, row_swap<0x141>(x));
+  return fmaxf(x, row_swap<0x140>(x));
+}
+__device__ __forceinline__ float row_sum16(float x) {
+  x += row_swap<0xB1>(x);
+  x += row_swap<0x4E>(x);
+  x += row_swap<0x141>(x);
+  return x + row_swap<0x140>(x);
+}
+
 // Inclusive sum over the wave's lanes, all of which take part: lane shifts
 // within rows of 16, then the rows' last lanes on.
 __device__ __forceinline__ int wave_scan(int x) {

@@ -375,7 +375,7 @@ struct RowKeys {
 // fp32 handles, tree and blocks. q, o [rows][Hq][hd].
 hipError_t launch_attn_rows_f32(const float* q, const float* k_cache, const float* v_cache,
                                 const RowKeys& rk, int n_rows, int Hq, int Hkv, int hd, float* o,
-                                hipStream_t st);
+                                int num_cus, hipStream_t st);
 
 // Blocks, bf16 handles (hd 128, up to 16 query heads in a group). A list of top
 // entries is attended in sparse_parts(top) parts; with more than one,

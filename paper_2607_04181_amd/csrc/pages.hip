@@ -18,6 +18,7 @@ namespace {
 constexpr int kPlanThreads = 1024;
 constexpr int kPlanWaves = kPlanThreads / kWave;
 constexpr int kPlanIds = 16;      // consecutive blocks a thread looks at per round
+constexpr int kAllocEntries = 8;
 constexpr int kPlanEntries = 8;   // table entries a lane reads at a time
 
 // Blocks that request i needs; -1: it names no valid row or length.
@@ -142,16 +143,22 @@ __global__ __launch_bounds__(kWave) void page_alloc_kernel(PageArgs a) {
   const int nb = (a.lens[i] + kBlockTokens - 1) / kBlockTokens;
   int32_t* bt = a.table + (int64_t)a.dst[i] * a.max_blocks;
   int at = a.off[i];
-  for (int b0 = 0; b0 < nb; b0 += kWave) {
-    const int b = b0 + lane;
-    const bool empty = b < nb && bt[b] < 0;
-    const uint64_t votes = __ballot(empty);
-    if (empty) {
-      const int id = a.list[at + __popcll(votes & ((1ull << lane) - 1))];
-      bt[b] = id;
-      a.refs[id] = 1;
+  for (int b0 = 0; b0 < nb; b0 += kWave * kAllocEntries) {
+    int e[kAllocEntries];
+#pragma unroll
+    for (int u = 0; u < kAllocEntries; ++u) e[u] = bt[min(b0 + u * kWave + lane, nb - 1)];
+#pragma unroll
+    for (int u = 0; u < kAllocEntries; ++u) {
+      const int b = b0 + u * kWave + lane;
+      const bool empty = b < nb && e[u] < 0;
+      const uint64_t votes = __ballot(empty);
+      if (empty) {
+        const int id = a.list[at + __popcll(votes & ((1ull << lane) - 1))];
+        bt[b] = id;
+        a.refs[id] = 1;
+      }
+      at += __popcll(votes);
     }
-    at += __popcll(votes);
   }
 }
 

@@ -166,6 +166,23 @@ def test_rows_do_not_depend_on_the_rest_of_the_call(dtype, hq, hkv, hd):
         assert torch.equal(o, whole[rows]), pick
 
 
+@pytest.mark.parametrize("hq,hkv,hd", [(16, 4, 64), (8, 1, 128), (12, 2, 32)])
+def test_fp32_rows_of_a_full_chip_and_alone(hq, hkv, hd):
+    """The number of heads per workgroup follows the call's rows; the bits do not."""
+    call = Call("f32", hq, hkv, hd, [(500, 60), (30, 50)], seed=19)
+    call.run()
+    call.check()
+    starts, table, lens, mask = call.args
+    # A tree's first nodes (which see none behind them) in calls of few rows.
+    for s, (prefix, nodes) in enumerate(call.trees):
+        r0 = int(call.starts[s])
+        for n in (1, 7):
+            few = torch.empty_like(call.o[:n])
+            coco.coco_tree_attention(call.c.h, 0, call.q[r0:r0 + n], few, i32([0, n]),
+                                     table[s:s + 1], i32([prefix + n]), mask[r0:r0 + n])
+            assert torch.equal(few, call.o[r0:r0 + n]), (s, n)
+
+
 @pytest.mark.parametrize("dtype,hq,hkv,hd", [("bf16", 8, 2, 128), ("f32", 4, 2, 64)])
 def test_more_sequences_than_a_launch_takes(dtype, hq, hkv, hd):
     rng = np.random.default_rng(5)
