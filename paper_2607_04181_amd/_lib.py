@@ -136,6 +136,8 @@ def _load():
 
 _lib = _load()
 
+_I32 = torch.int32
+
 
 def _check(rc: int) -> int:
     if rc < 0:
@@ -163,13 +165,35 @@ def _stream(stream):
     return stream.cuda_stream if isinstance(stream, torch.cuda.Stream) else stream
 
 
+def _arg(h, t, dtype, what):
+    """_ptr of a tensor that must be on the handle's device."""
+    if type(t) is torch.Tensor and t.dtype is dtype and t.get_device() == h.device and \
+            t.is_contiguous():
+        return t.data_ptr()
+    p = _ptr(t, dtype, what)
+    if p is not None and t.get_device() != h.device:
+        raise ValueError(f"{what} must be on the handle's GPU, cuda:{h.device}")
+    return p
+
+
+def _handle_stream(h, stream):
+    """None: the current stream of the handle's device."""
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(h.device)
+    return _stream(stream)
+
+
 class Handle:
     """An initialised replica; keeps the borrowed tensors alive."""
 
-    def __init__(self, raw, cfg, keep, num_blocks=()):
+    def __init__(self, raw, cfg, keep, num_blocks=(), device=None):
         self.raw = raw
         self.cfg = cfg
         self.num_blocks = num_blocks  # of each layer's pools
+        self.device = device          # index
+        # (fields of a ctypes structure take a call each to read)
+        self.elem, self.width = _elem_dtype(cfg), cfg.max_blocks_per_seq
+        self.hq, self.hkv, self.hd = cfg.n_q_heads, cfg.n_kv_heads, cfg.head_dim
         self._keep = keep
 
     def __del__(self):
@@ -207,7 +231,8 @@ def coco_layer_init(cfg: coco_layer_config, layers) -> Handle:
         arr[i].num_blocks = int(w["k_cache"].shape[0])
     raw = ctypes.c_void_p()
     _check(_lib.coco_layer_init(ctypes.byref(cfg), arr, ctypes.byref(raw)))
-    return Handle(raw, cfg, keep, [int(w["k_cache"].shape[0]) for w in layers])
+    return Handle(raw, cfg, keep, [int(w["k_cache"].shape[0]) for w in layers],
+                  torch.cuda.current_device())
 
 
 def coco_layer_destroy(h: Handle) -> None:
@@ -267,7 +292,8 @@ def coco_kv_append(h: Handle, layer: int, k, v, seq_idx, positions, block_table,
         if t.dtype != _elem_dtype(cfg):
             raise TypeError(f"{name} must be {_elem_dtype(cfg)}, got {t.dtype}")
         if t.numel() != n_tok * per_tok:
-            raise ValueError(f"{name} must hold [{n_tok}, {cfg.n_kv_heads}, {cfg.head_dim}] elements")
+            raise ValueError(
+                f"{name} must hold [{n_tok}, {cfg.n_kv_heads}, {cfg.head_dim}] elements")
     if seq_idx.numel() != n_tok:
         raise ValueError(f"seq_idx has {seq_idx.numel()} entries for {n_tok} tokens")
     if block_table.dim() != 2 or block_table.shape[1] != cfg.max_blocks_per_seq:
@@ -316,7 +342,7 @@ def coco_layer_span_forward(h: Handle, first_layer: int, n_layers: int, hidden, 
 
 
 def _check_table(h: Handle, block_table, n_seqs=None):
-    width = h.cfg.max_blocks_per_seq
+    width = h.width
     if not (isinstance(block_table, torch.Tensor) and block_table.dim() == 2 and
             block_table.shape[1] == width):
         raise ValueError(f"block_table must be [n_seqs, {width}]")
@@ -336,78 +362,74 @@ def _check_counts(h: Handle, ref_counts):
 
 
 def coco_kv_alloc(h: Handle, seq_idx, lens, block_table, ref_counts, status, stream=None):
-    i32 = torch.int32
     n = int(seq_idx.numel())
     _check_len("lens", lens, n)
     _check_len("status", status, n)
     _check_table(h, block_table)
     _check_counts(h, ref_counts)
-    _check(_lib.coco_kv_alloc(h.raw, _ptr(seq_idx, i32, "seq_idx"), _ptr(lens, i32, "lens"), n,
-                              _ptr(block_table, i32, "block_table"), int(block_table.shape[0]),
-                              _ptr(ref_counts, i32, "ref_counts"), _ptr(status, i32, "status"),
-                              _stream(stream)))
+    _check(_lib.coco_kv_alloc(h.raw, _arg(h, seq_idx, _I32, "seq_idx"),
+                              _arg(h, lens, _I32, "lens"), n,
+                              _arg(h, block_table, _I32, "block_table"), int(block_table.shape[0]),
+                              _arg(h, ref_counts, _I32, "ref_counts"),
+                              _arg(h, status, _I32, "status"),
+                              _handle_stream(h, stream)))
 
 
 def coco_kv_fork(h: Handle, first_layer: int, n_layers: int, src_seq, dst_seq, lens, block_table,
                  ref_counts, status, stream=None):
-    i32 = torch.int32
     n = int(dst_seq.numel())
     _check_len("src_seq", src_seq, n)
     _check_len("lens", lens, n)
     _check_len("status", status, n)
     _check_table(h, block_table)
     _check_counts(h, ref_counts)
-    _check(_lib.coco_kv_fork(h.raw, first_layer, n_layers, _ptr(src_seq, i32, "src_seq"),
-                             _ptr(dst_seq, i32, "dst_seq"), _ptr(lens, i32, "lens"), n,
-                             _ptr(block_table, i32, "block_table"), int(block_table.shape[0]),
-                             _ptr(ref_counts, i32, "ref_counts"), _ptr(status, i32, "status"),
-                             _stream(stream)))
+    _check(_lib.coco_kv_fork(h.raw, first_layer, n_layers, _arg(h, src_seq, _I32, "src_seq"),
+                             _arg(h, dst_seq, _I32, "dst_seq"), _arg(h, lens, _I32, "lens"), n,
+                             _arg(h, block_table, _I32, "block_table"), int(block_table.shape[0]),
+                             _arg(h, ref_counts, _I32, "ref_counts"),
+                             _arg(h, status, _I32, "status"),
+                             _handle_stream(h, stream)))
 
 
 def coco_kv_free(h: Handle, seq_idx, keep_lens, block_table, ref_counts, stream=None):
     """keep_lens None: the rows let go of all their blocks."""
-    i32 = torch.int32
     n = int(seq_idx.numel())
     if keep_lens is not None:
         _check_len("keep_lens", keep_lens, n)
     _check_table(h, block_table)
     _check_counts(h, ref_counts)
-    _check(_lib.coco_kv_free(h.raw, _ptr(seq_idx, i32, "seq_idx"),
-                             _ptr(keep_lens, i32, "keep_lens"), n,
-                             _ptr(block_table, i32, "block_table"), int(block_table.shape[0]),
-                             _ptr(ref_counts, i32, "ref_counts"), _stream(stream)))
+    _check(_lib.coco_kv_free(h.raw, _arg(h, seq_idx, _I32, "seq_idx"),
+                             _arg(h, keep_lens, _I32, "keep_lens"), n,
+                             _arg(h, block_table, _I32, "block_table"), int(block_table.shape[0]),
+                             _arg(h, ref_counts, _I32, "ref_counts"), _handle_stream(h, stream)))
 
 
 def coco_kv_copy(h: Handle, first_layer: int, n_layers: int, src_blocks, dst_blocks, stream=None):
-    i32 = torch.int32
     n = int(src_blocks.numel())
     _check_len("dst_blocks", dst_blocks, n)
-    _check(_lib.coco_kv_copy(h.raw, first_layer, n_layers, _ptr(src_blocks, i32, "src_blocks"),
-                             _ptr(dst_blocks, i32, "dst_blocks"), n, _stream(stream)))
+    _check(_lib.coco_kv_copy(h.raw, first_layer, n_layers, _arg(h, src_blocks, _I32, "src_blocks"),
+                             _arg(h, dst_blocks, _I32, "dst_blocks"), n, _handle_stream(h, stream)))
 
 
 def coco_kv_compact(h: Handle, first_layer: int, n_layers: int, seq_idx, base_lens, kept,
                     kept_starts, block_table, stream=None):
-    i32 = torch.int32
     n = int(seq_idx.numel())
     _check_len("base_lens", base_lens, n)
     _check_len("kept_starts", kept_starts, n + 1)
     _check_table(h, block_table)
-    _check(_lib.coco_kv_compact(h.raw, first_layer, n_layers, _ptr(seq_idx, i32, "seq_idx"),
-                                _ptr(base_lens, i32, "base_lens"), _ptr(kept, i32, "kept"),
-                                _ptr(kept_starts, i32, "kept_starts"), n, int(kept.numel()),
-                                _ptr(block_table, i32, "block_table"), int(block_table.shape[0]),
-                                _stream(stream)))
+    _check(_lib.coco_kv_compact(h.raw, first_layer, n_layers, _arg(h, seq_idx, _I32, "seq_idx"),
+                                _arg(h, base_lens, _I32, "base_lens"), _arg(h, kept, _I32, "kept"),
+                                _arg(h, kept_starts, _I32, "kept_starts"), n, int(kept.numel()),
+                                _arg(h, block_table, _I32, "block_table"),
+                                int(block_table.shape[0]), _handle_stream(h, stream)))
 
 
 def _check_heads(h: Handle, name: str, t):
-    cfg = h.cfg
-    if not isinstance(t, torch.Tensor) or t.dtype != _elem_dtype(cfg):
-        raise TypeError(f"{name} must be a {_elem_dtype(cfg)} tensor")
+    if not isinstance(t, torch.Tensor) or t.dtype != h.elem:
+        raise TypeError(f"{name} must be a {h.elem} tensor")
     n = t.shape[0] if t.dim() >= 2 else -1
-    if t.numel() != n * cfg.n_q_heads * cfg.head_dim:
-        raise ValueError(f"{name} must be [rows, {cfg.n_q_heads}, {cfg.head_dim}], "
-                         f"got {tuple(t.shape)}")
+    if t.numel() != n * h.hq * h.hd:
+        raise ValueError(f"{name} must be [rows, {h.hq}, {h.hd}], got {tuple(t.shape)}")
     return n
 
 
@@ -423,7 +445,6 @@ def coco_tree_reserve(h: Handle, max_rows: int, max_seqs: int) -> None:
 def coco_tree_attention(h: Handle, layer: int, q, o, seq_starts, block_table, ctx_lens, tree_mask,
                         stream=None):
     """tree_mask: int64 [rows, words]."""
-    i32 = torch.int32
     n = _check_heads(h, "q", q)
     _check_out(h, o, n)
     n_seqs = int(ctx_lens.numel())
@@ -431,9 +452,11 @@ def coco_tree_attention(h: Handle, layer: int, q, o, seq_starts, block_table, ct
     _check_table(h, block_table, n_seqs)
     _check_mask(tree_mask, n)
     _check(_lib.coco_tree_attention(
-        h.raw, layer, _ptr(q, what="q"), _ptr(o, what="o"), n, _ptr(seq_starts, i32, "seq_starts"),
-        n_seqs, _ptr(block_table, i32, "block_table"), _ptr(ctx_lens, i32, "ctx_lens"),
-        _ptr(tree_mask, torch.int64, "tree_mask"), int(tree_mask.shape[1]), _stream(stream)))
+        h.raw, layer, _arg(h, q, h.elem, "q"), _arg(h, o, h.elem, "o"), n,
+        _arg(h, seq_starts, _I32, "seq_starts"), n_seqs,
+        _arg(h, block_table, _I32, "block_table"), _arg(h, ctx_lens, _I32, "ctx_lens"),
+        _arg(h, tree_mask, torch.int64, "tree_mask"), int(tree_mask.shape[1]),
+        _handle_stream(h, stream)))
 
 
 def _check_mask(tree_mask, n: int):
@@ -445,26 +468,24 @@ def _check_mask(tree_mask, n: int):
 def coco_layer_tree_forward(h: Handle, first_layer: int, n_layers: int, hidden, row_idx, positions,
                             seq_starts, block_table, ctx_lens, tree_mask, stream=None):
     """tree_mask: int64 [rows, words]."""
-    i32 = torch.int32
     if seq_starts is None:
         raise ValueError("seq_starts must be given")
     _check_batch(h, hidden, row_idx, positions, seq_starts, block_table, ctx_lens)
     n, n_seqs = int(row_idx.numel()), int(ctx_lens.numel())
     _check_mask(tree_mask, n)
     _check(_lib.coco_layer_tree_forward(
-        h.raw, first_layer, n_layers, _ptr(hidden, what="hidden"), int(hidden.shape[0]),
-        _ptr(row_idx, i32, "row_idx"), n, _ptr(positions, i32, "positions"),
-        _ptr(seq_starts, i32, "seq_starts"), n_seqs, _ptr(block_table, i32, "block_table"),
-        _ptr(ctx_lens, i32, "ctx_lens"), _ptr(tree_mask, torch.int64, "tree_mask"),
-        int(tree_mask.shape[1]), _stream(stream)))
+        h.raw, first_layer, n_layers, _arg(h, hidden, h.elem, "hidden"), int(hidden.shape[0]),
+        _arg(h, row_idx, _I32, "row_idx"), n, _arg(h, positions, _I32, "positions"),
+        _arg(h, seq_starts, _I32, "seq_starts"), n_seqs, _arg(h, block_table, _I32, "block_table"),
+        _arg(h, ctx_lens, _I32, "ctx_lens"), _arg(h, tree_mask, torch.int64, "tree_mask"),
+        int(tree_mask.shape[1]), _handle_stream(h, stream)))
 
 
 def _check_summary(h: Handle, summary, scales):
-    cfg = h.cfg
     if not (isinstance(summary, torch.Tensor) and summary.dim() == 4 and
-            summary.shape[1:] == (cfg.n_kv_heads, 2, cfg.head_dim)):
-        raise ValueError(f"summary must be [num_blocks, {cfg.n_kv_heads}, 2, {cfg.head_dim}]")
-    _check_len("scales", scales, summary.shape[0] * cfg.n_kv_heads)
+            summary.shape[1:] == (h.hkv, 2, h.hd)):
+        raise ValueError(f"summary must be [num_blocks, {h.hkv}, 2, {h.hd}]")
+    _check_len("scales", scales, summary.shape[0] * h.hkv)
 
 
 def _check_layer_summary(h: Handle, layer: int, summary):
@@ -476,7 +497,6 @@ def _check_layer_summary(h: Handle, layer: int, summary):
 def coco_kv_summarize(h: Handle, layer: int, summary, scales, first_lens, ctx_lens, block_table,
                       stream=None):
     """first_lens None: the whole sequences."""
-    i32 = torch.int32
     n_seqs = int(ctx_lens.numel())
     _check_summary(h, summary, scales)
     _check_layer_summary(h, layer, summary)
@@ -484,9 +504,10 @@ def coco_kv_summarize(h: Handle, layer: int, summary, scales, first_lens, ctx_le
         _check_len("first_lens", first_lens, n_seqs)
     _check_table(h, block_table, n_seqs)
     _check(_lib.coco_kv_summarize(
-        h.raw, layer, _ptr(summary, torch.int8, "summary"), _ptr(scales, torch.float32, "scales"),
-        _ptr(first_lens, i32, "first_lens"), _ptr(ctx_lens, i32, "ctx_lens"), n_seqs,
-        _ptr(block_table, i32, "block_table"), _stream(stream)))
+        h.raw, layer, _arg(h, summary, torch.int8, "summary"),
+        _arg(h, scales, torch.float32, "scales"),
+        _arg(h, first_lens, _I32, "first_lens"), _arg(h, ctx_lens, _I32, "ctx_lens"), n_seqs,
+        _arg(h, block_table, _I32, "block_table"), _handle_stream(h, stream)))
 
 
 def coco_sparse_reserve(h: Handle, max_rows: int, max_blocks: int) -> None:
@@ -495,8 +516,8 @@ def coco_sparse_reserve(h: Handle, max_rows: int, max_blocks: int) -> None:
 
 def _check_selected(h: Handle, selected, n: int) -> int:
     if not (isinstance(selected, torch.Tensor) and selected.dim() == 3 and
-            selected.shape[:2] == (n, h.cfg.n_kv_heads)):
-        raise ValueError(f"selected must be [{n}, {h.cfg.n_kv_heads}, blocks]")
+            selected.shape[:2] == (n, h.hkv)):
+        raise ValueError(f"selected must be [{n}, {h.hkv}, blocks]")
     return int(selected.shape[2])
 
 
@@ -514,48 +535,47 @@ def _check_row_arrays(h: Handle, n: int, positions, seq_starts, block_table, ctx
 
 def coco_block_select(h: Handle, summary, scales, q, positions, seq_starts, block_table, ctx_lens,
                       keep_first: int, keep_last: int, selected, stream=None):
-    i32 = torch.int32
     n = _check_heads(h, "q", q)
     n_seqs = _check_row_arrays(h, n, positions, seq_starts, block_table, ctx_lens)
     _check_summary(h, summary, scales)
     n_select = _check_selected(h, selected, n)
     _check(_lib.coco_block_select(
-        h.raw, _ptr(summary, torch.int8, "summary"), _ptr(scales, torch.float32, "scales"),
-        int(summary.shape[0]), _ptr(q, what="q"), n, _ptr(positions, i32, "positions"),
-        _ptr(seq_starts, i32, "seq_starts"), n_seqs, _ptr(block_table, i32, "block_table"),
-        _ptr(ctx_lens, i32, "ctx_lens"), keep_first, keep_last, _ptr(selected, i32, "selected"),
-        n_select, _stream(stream)))
+        h.raw, _arg(h, summary, torch.int8, "summary"), _arg(h, scales, torch.float32, "scales"),
+        int(summary.shape[0]), _arg(h, q, h.elem, "q"), n, _arg(h, positions, _I32, "positions"),
+        _arg(h, seq_starts, _I32, "seq_starts"), n_seqs, _arg(h, block_table, _I32, "block_table"),
+        _arg(h, ctx_lens, _I32, "ctx_lens"), keep_first, keep_last,
+        _arg(h, selected, _I32, "selected"), n_select, _handle_stream(h, stream)))
 
 
 def coco_sparse_attention(h: Handle, layer: int, q, o, positions, seq_starts, block_table,
                           ctx_lens, selected, stream=None):
-    i32 = torch.int32
     n = _check_heads(h, "q", q)
     _check_out(h, o, n)
     n_seqs = _check_row_arrays(h, n, positions, seq_starts, block_table, ctx_lens)
     n_select = _check_selected(h, selected, n)
     _check(_lib.coco_sparse_attention(
-        h.raw, layer, _ptr(q, what="q"), _ptr(o, what="o"), n, _ptr(positions, i32, "positions"),
-        _ptr(seq_starts, i32, "seq_starts"), n_seqs, _ptr(block_table, i32, "block_table"),
-        _ptr(ctx_lens, i32, "ctx_lens"), _ptr(selected, i32, "selected"), n_select,
-        _stream(stream)))
+        h.raw, layer, _arg(h, q, h.elem, "q"), _arg(h, o, h.elem, "o"), n,
+        _arg(h, positions, _I32, "positions"),
+        _arg(h, seq_starts, _I32, "seq_starts"), n_seqs, _arg(h, block_table, _I32, "block_table"),
+        _arg(h, ctx_lens, _I32, "ctx_lens"), _arg(h, selected, _I32, "selected"), n_select,
+        _handle_stream(h, stream)))
 
 
 def coco_layer_sparse_forward(h: Handle, layer: int, hidden, row_idx, positions, block_table,
                               ctx_lens, summary, scales, keep_first: int, keep_last: int, selected,
                               stream=None):
-    i32 = torch.int32
     _check_batch(h, hidden, row_idx, positions, None, block_table, ctx_lens)
     n = int(row_idx.numel())
     _check_summary(h, summary, scales)
     _check_layer_summary(h, layer, summary)
     n_select = _check_selected(h, selected, n)
     _check(_lib.coco_layer_sparse_forward(
-        h.raw, layer, _ptr(hidden, what="hidden"), int(hidden.shape[0]),
-        _ptr(row_idx, i32, "row_idx"), n, _ptr(positions, i32, "positions"),
-        _ptr(block_table, i32, "block_table"), _ptr(ctx_lens, i32, "ctx_lens"),
-        _ptr(summary, torch.int8, "summary"), _ptr(scales, torch.float32, "scales"), keep_first,
-        keep_last, _ptr(selected, i32, "selected"), n_select, _stream(stream)))
+        h.raw, layer, _arg(h, hidden, h.elem, "hidden"), int(hidden.shape[0]),
+        _arg(h, row_idx, _I32, "row_idx"), n, _arg(h, positions, _I32, "positions"),
+        _arg(h, block_table, _I32, "block_table"), _arg(h, ctx_lens, _I32, "ctx_lens"),
+        _arg(h, summary, torch.int8, "summary"), _arg(h, scales, torch.float32, "scales"),
+        keep_first, keep_last, _arg(h, selected, _I32, "selected"), n_select,
+        _handle_stream(h, stream)))
 
 
 def coco_layer_workspace(h: Handle, which: int, dst, stream=None) -> None:

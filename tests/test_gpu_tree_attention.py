@@ -294,3 +294,13 @@ def test_refusals():
     assert (call.o == 7.0).all()
     call.run()
     call.check()
+
+
+def test_tensors_of_another_device_are_refused():
+    call = Call("bf16", 8, 2, 128, [(20, 3)], seed=20)
+    here, call.c.h.device = call.c.h.device, call.c.h.device + 1
+    with pytest.raises(ValueError, match="q must be on the handle's GPU"):
+        call.run()
+    call.c.h.device = here
+    call.run()
+    call.check()
