@@ -524,7 +524,7 @@ int coco_tree_reserve(coco_layer_t H, int32_t max_rows, int32_t max_seqs) {
       return fail(COCO_EINVAL, "%d rows of %d sequences: %lld partial columns exceed 2^31 - 1",
                   rows, seqs, (long long)parts);
     const size_t o = align256((size_t)parts * c.head_dim * 4), ml = align256((size_t)parts * 8);
-    const size_t plan = align256((size_t)seqs * 8), redo = ((size_t)rows * c.n_q_heads + 8) * 4;
+    const size_t plan = align256((size_t)seqs * 8), redo = ((size_t)rows * c.n_q_heads + 16) * 4;
     const char* had = H->tree_ws;
     const int rc = grow(H, &H->tree_ws, &H->tree_bytes, o + ml + plan + redo);
     if (rc) return rc;

@@ -52,6 +52,7 @@ constexpr int kStKeys = 32;  // keys of a stage
 constexpr int kTile = kBlockTokens * HD;
 constexpr int kRing = 4;    // stages in LDS
 constexpr int kStage = 4 * kTile;  // elements: keys and values of two blocks
+constexpr int kFewCols = 16;  // most columns of a sequence without the ring
 constexpr int kXCDs = 8;
 constexpr int kMaxSeqs = kTreeLaunchSeqs;
 constexpr float kLazy = 8.f;  // log2 units a running max may lag
@@ -63,17 +64,18 @@ struct TreeSeq {
 };
 
 // Keys of one of the parts that `len` keys of a sequence with `cols` columns
-// are split into. Few columns: a part of 128 keys, so that one sequence fills
-// the chip; more columns make a part's partial result (512 bytes per column)
-// dear next to its keys (512 bytes each), so parts grow with them. Measured:
-// parts of 512 keys instead of 1024 gain one or eight trees of 26 nodes over 2k
-// keys 16 and 12% and cost 64 of them 6 and 32 trees of 64 nodes 13%; parts
-// of 2048 above 256 columns gain the latter 9% and cost one of them 28. The
-// number of parts falls with cols and grows with len (tree_column_parts counts
-// on it).
+// are split into: so many parts that one sequence fills the chip, but more
+// columns make a part's partial result (512 bytes per column) dear next to its
+// keys (512 bytes each), so parts grow with them, and their number is bounded by
+// what the merge of one row takes. Measured: with up to 16 columns, parts of
+// 128 keys instead of 512 gain one token over 1k keys 3% and cost eight of them
+// 44 and 64 trees of 4 nodes 7, and 32 parts instead of 16 cost one token over 16k
+// 17; with 104 columns, parts of 512 keys instead of 1024 gain one or eight
+// trees over 2k keys 16 and 12% and cost 64 of them 6, and 32 trees of 64 nodes
+// 13; parts of 2048 above 256 columns gain the latter 9% and cost one of them 28.
 __host__ __device__ __forceinline__ int tree_part(int64_t cols, int len) {
-  const int least = cols <= 16 ? 128 : cols <= 64 ? 512 : 1024;
-  const int most = cols <= 128 ? kTreeSplitsFew : kTreeSplits;
+  const int least = cols <= 64 ? 512 : 1024;
+  const int most = cols <= kFewCols || cols > 128 ? kTreeSplits : kTreeSplitsFew;
   int want = (len + least - 1) / least;
   want = want < 1 ? 1 : want > most ? most : want;
   const int part = ((len + want - 1) / want + 127) / 128 * 128;
@@ -253,6 +255,189 @@ __device__ __forceinline__ void tree_values(Cols& c, const u32x4_t v[2][2][2],
           c.acc[i], 0, 0, 0);
 }
 
+// ---- Few columns (up to 16): they share their operands with too few others to
+// pay for LDS. Each wave takes every fourth block of the part straight into
+// registers, three blocks on their way, with 16x16 tiles of the columns:
+//   S[16 keys][16 cols] = K Q^T    4 x mfma 16x16x32
+//   O^T[hd][16 cols] += V^T P^T    8 x mfma 16x16x16
+// P comes out as the operand of the second (lane (c, j4): keys 4 j4 .. + 3 of
+// column c); the waves' results meet in LDS in wave order. One token over 1k keys
+// takes 11.9 us with the merge, through the ring 13.7; 64 trees of 4 nodes over
+// 4k keys 289 (4.7 TB/s) and 325. (32 columns, two tiles, spill registers in
+// this kernel and lose at 64 trees what they gain at one.)
+struct FewTile {
+  u32x4_t k[4], v[4];
+};
+
+// As mask_values for one block: lane (m, j4) holds keys 4 j4 .. + 3 of dims
+// 32 x + m and + 16. Returns the block's keys that held a non-finite value.
+__device__ __forceinline__ uint32_t few_mask_values(u32x4_t v[4], int j4, int left) {
+  uint32_t odd = 0;
+#pragma unroll
+  for (int x = 0; x < 4; ++x)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int c = 2 * (e & 1), k = 4 * j4 + c;
+      uint32_t w = v[x][e];
+      w &= (k < left ? 0xFFFFu : 0u) | (k + 1 < left ? 0xFFFF0000u : 0u);
+      const bool lo = (w & 0x7F80u) == 0x7F80u, hi = (w & 0x7F800000u) == 0x7F800000u;
+      if (lo) w &= 0xFFFF0000u;
+      if (hi) w &= 0xFFFFu;
+      odd |= ((lo ? 1u : 0u) | (hi ? 2u : 0u)) << c;
+      v[x][e] = w;
+    }
+  if (__ballot(odd != 0) == 0) return 0;
+  uint32_t keys = 0;
+#pragma unroll 1
+  for (int c = 0; c < 4; ++c) {
+    const uint64_t any = __ballot(odd >> c & 1);
+    for (int j = 0; j < 4; ++j) keys |= (any >> (16 * j) & 0xFFFFu ? 1u : 0u) << (4 * j + c);
+  }
+  return keys;
+}
+
+// Part sp of sequence s for kv head g; part0: the sequence's first column part.
+// sm_o: [4][16][128], the 16-byte pieces of column c at place ^ c.
+__device__ __forceinline__ void few_columns(const TreeArgs& a, const TreeSeq& ts, int s, int g,
+                                            int sp, int64_t part0, float* sm_o,
+                                            float (*sm_ml)[kFewCols][2]) {
+  const RowKeys& rk = a.rk;
+  const int tid = threadIdx.x, lane = tid & 63, c16 = lane & 15, j4 = lane >> 4;
+  const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int G = a.Hq / a.Hkv, cols = ts.nodes * G, row0 = rk.seq_starts[s];
+  const int prefix = ts.len - ts.nodes;
+  const int t0 = sp * ts.part, t1 = min(ts.len, t0 + ts.part);
+  const int b0 = t0 / kBlockTokens + wv;
+  const int left_blocks = (t1 + kBlockTokens - 1) / kBlockTokens - b0;
+  const int mine = left_blocks > 0 ? (left_blocks + kWaves - 1) / kWaves : 0;
+  const int32_t* bt = rk.block_table + (int64_t)s * rk.max_blocks;
+
+  int ids = 0;
+  auto load = [&](FewTile& t, int j) {  // with j = 0, 1, ..
+    if ((j & 63) == 0) {
+      const int64_t id = bt[min(b0 + (j + lane) * kWaves, rk.max_blocks - 1)];
+      ids = (int)(id < 0 ? 0 : id >= rk.num_blocks ? rk.num_blocks - 1 : id);
+    }
+    const int64_t at = ((int64_t)__builtin_amdgcn_readlane(ids, j & 63) * a.Hkv + g) * kTile;
+    const u32x4_t* kp = (const u32x4_t*)(a.k_cache + at);
+    const u32x4_t* vp = (const u32x4_t*)(a.v_cache + at);
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+      t.k[p] = kp[64 * p + lane];
+      t.v[p] = vp[64 * p + lane];
+    }
+  };
+  FewTile ta, tb, tc;
+  if (mine > 0) load(ta, 0);
+  if (mine > 1) load(tb, 1);
+  if (mine > 2) load(tc, 2);
+
+  // This lane's column (past the last: the last).
+  const int c = min(c16, cols - 1), row = row0 + c / G;
+  const int64_t rowhead = (int64_t)row * a.Hq + g * G + c % G;
+  const uint64_t* mask = rk.mask + (int64_t)row * rk.words;
+  bf16x8_t qf[4];
+#pragma unroll
+  for (int p = 0; p < 4; ++p)
+    qf[p] = __builtin_bit_cast(bf16x8_t,
+                               *(const u32x4_t*)(a.q + rowhead * HD + 32 * p + 8 * j4));
+  float m = -INFINITY, l = 0.f;
+  f32x4_t acc[8];
+#pragma unroll
+  for (int x = 0; x < 8; ++x) acc[x] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+
+  auto attend = [&](FewTile& t, int j) {
+    f32x4_t z = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int p = 0; p < 4; ++p)
+      z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, t.k[p]), qf[p], z,
+                                                  0, 0, 0);
+    const int tok0 = (b0 + j * kWaves) * kBlockTokens;
+    if (tok0 + kBlockTokens > prefix) {
+      const uint32_t odd = few_mask_values(t.v, j4, t1 - tok0);
+      const uint32_t seen = tree_bits32(mask, rk.words, ts.nodes, tok0 - prefix);
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (!(seen >> (4 * j4 + r) & 1)) z[r] = -INFINITY;
+      if (odd & seen) a.redo[rowhead] = 1;
+    }
+    const float top = col_max4(fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3]))) * a.scale_log2;
+    const float m_new = top > m + kLazy ? top : m;
+    if (__ballot(m_new != m) != 0) {
+      const float alpha = __builtin_amdgcn_exp2f(m - (m_new == -INFINITY ? 0.f : m_new));
+#pragma unroll
+      for (int x = 0; x < 8; ++x) acc[x] *= alpha;
+      l *= alpha;
+      m = m_new;
+    }
+    const float ref = m == -INFINITY ? 0.f : m;
+    float p[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) p[r] = __builtin_amdgcn_exp2f(fmaf(z[r], a.scale_log2, -ref));
+    l += (p[0] + p[1]) + (p[2] + p[3]);
+    const s16x4_t pb = __builtin_bit_cast(
+        s16x4_t, u32x2_t{pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3])});
+#pragma unroll
+    for (int x = 0; x < 8; ++x)
+      acc[x] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(
+          __builtin_bit_cast(s16x4_t, u32x2_t{t.v[x / 2][x % 2 * 2], t.v[x / 2][x % 2 * 2 + 1]}),
+          pb, acc[x], 0, 0, 0);
+  };
+#pragma unroll 1
+  for (int j = 0; j < mine; j += 3) {
+    attend(ta, j);
+    if (j + 3 < mine) load(ta, j + 3);
+    if (j + 1 >= mine) break;
+    attend(tb, j + 1);
+    if (j + 4 < mine) load(tb, j + 4);
+    if (j + 2 >= mine) break;
+    attend(tc, j + 2);
+    if (j + 5 < mine) load(tc, j + 5);
+  }
+
+  l = col_sum4(l);
+  if (j4 == 0) {
+    sm_ml[wv][c16][0] = m;
+    sm_ml[wv][c16][1] = l;
+  }
+#pragma unroll
+  for (int x = 0; x < 8; ++x)
+    *(f32x4_t*)(sm_o + (wv * kFewCols + c16) * HD + (((4 * x + j4) ^ c16) << 2)) = acc[x];
+  __syncthreads();
+  for (int i = tid; i < cols * (HD / 4); i += kThreads) {
+    const int c = i / (HD / 4), q4 = i % (HD / 4);
+    float M = sm_ml[0][c][0];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) M = fmaxf(M, sm_ml[w][c][0]);
+    const float ref = M == -INFINITY ? 0.f : M;
+    f32x4_t y = {0.f, 0.f, 0.f, 0.f};
+    float L = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const float f = __builtin_amdgcn_exp2f(sm_ml[w][c][0] - ref);
+      const f32x4_t v = *(const f32x4_t*)(sm_o + (w * kFewCols + c) * HD + ((q4 ^ c) << 2));
+#pragma unroll
+      for (int r = 0; r < 4; ++r) y[r] = fmaf(f, v[r], y[r]);
+      L = fmaf(f, sm_ml[w][c][1], L);
+    }
+    const int n = c / G, head = g * G + c % G;
+    if (ts.splits > 1) {
+      const int64_t idx = part0 + ((int64_t)n * a.Hq + head) * ts.splits + sp;
+      *(f32x4_t*)(a.part_o + idx * HD + 4 * q4) = y;
+      if (q4 == 0) {
+        a.part_ml[2 * idx] = M;
+        a.part_ml[2 * idx + 1] = L;
+      }
+    } else {
+      const float inv = L == 0.f ? 0.f : 1.0f / L;
+      const int col = head * HD + 4 * q4;
+      store4(a.o + (a.tiled ? tile_off(row0 + n, col, a.Hq * HD)
+                            : (int64_t)(row0 + n) * a.Hq * HD + col),
+             y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv);
+    }
+  }
+}
+
 // Inclusive sum of x over the workgroup's threads so far: `carry` before, the
 // whole added to it. red: one int per wave.
 __device__ __forceinline__ int block_scan(int x, int* red, int& carry) {
@@ -271,8 +456,9 @@ __device__ __forceinline__ int block_scan(int x, int* red, int& carry) {
 
 __global__ __launch_bounds__(kThreads, 2) void tree_attention_kernel(TreeArgs a) {
   __shared__ __attribute__((aligned(16))) bf16_t ring[kRing * kStage];
-  __shared__ int units_s[kMaxSeqs], base_s[kMaxSeqs], items_s[kMaxSeqs];
+  __shared__ int units_s[kMaxSeqs], base_s[kMaxSeqs], items_s[kMaxSeqs], few_s[kMaxSeqs];
   __shared__ int red[kWaves], next_s[2];
+  __shared__ float few_ml[kWaves][kFewCols][2];
   const RowKeys& rk = a.rk;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -283,13 +469,15 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_kernel(TreeArgs a)
   // % 8); an XCD's list of items is its units' column tiles.
   const int queues = gridDim.x % kXCDs == 0 ? kXCDs : 1;
   const int queue = blockIdx.x % queues;
-  int n_units = 0, n_parts = 0, total = 0;
+  int n_units = 0, n_parts = 0, total = 0, total_few = 0;
   for (int s0 = 0; s0 < rk.n_seqs; s0 += kThreads) {
     const int s = s0 + tid;
     int nu = 0, np = 0, tiles = 0;
+    bool few = false;
     if (s < rk.n_seqs) {
       const TreeSeq t = tree_plan(rk.seq_starts, rk.ctx_lens, s, G, rk.max_blocks);
       tiles = t.tiles;
+      few = t.nodes * G <= kFewCols;
       nu = t.tiles > 0 ? t.splits * a.Hkv : 0;
       np = t.splits > 1 ? t.nodes * a.Hq * t.splits : 0;
       if (blockIdx.x == 0) a.plan[2 * s + 1] = t.splits;
@@ -298,37 +486,63 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_kernel(TreeArgs a)
     const int p0 = block_scan(np, red, n_parts) - np;
     // The queue's units among u0 .. u1 - 1.
     const int mine = ((u1 - queue + queues - 1) / queues - (u0 - queue + queues - 1) / queues);
-    const int ni = mine * tiles;
+    const int ni = few ? 0 : mine * tiles, nf = few ? mine : 0;
     const int i0 = block_scan(ni, red, total) - ni;
+    const int f0 = block_scan(nf, red, total_few) - nf;
     if (s < rk.n_seqs) {
       units_s[s] = u0;
       base_s[s] = p0;
       items_s[s] = i0;
+      few_s[s] = f0;
       if (blockIdx.x == 0) a.plan[2 * s] = p0;
     }
   }
   __syncthreads();
   if (n_parts > a.part_cap) return;  // more rows than the call named: no room for their parts
 
+  // Workgroups draw items in order, each its next one while it works (the merge
+  // kernel sets the counts back to zero). A fixed share of the items left a
+  // quarter of the chip idle at the end.
+  const int first = blockIdx.x / queues, per_queue = (int)gridDim.x / queues;
+  auto seq_of = [&](const int* starts, int item) {
+    int lo = 0, hi = rk.n_seqs - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (starts[mid] <= item) lo = mid; else hi = mid - 1;
+    }
+    return __builtin_amdgcn_readfirstlane(lo);
+  };
+  // The sequences of few columns.
+  int item = first;
+#pragma unroll 1
+  for (int k = 0; item < total_few; ++k) {
+    int drawn = 0;
+    if (tid == 0) drawn = per_queue + atomicAdd(a.drawn + kXCDs + queue, 1);
+    const int s = seq_of(few_s, item);
+    const TreeSeq ts = tree_plan(rk.seq_starts, rk.ctx_lens, s, G, rk.max_blocks);
+    const int x = __builtin_amdgcn_readfirstlane(item - few_s[s]);
+    const int u0 = __builtin_amdgcn_readfirstlane(units_s[s]);
+    const int u = (queue - u0 % queues + queues) % queues + x * queues;
+    const int g = u % a.Hkv, sp = u / a.Hkv;
+    const int base = __builtin_amdgcn_readfirstlane(base_s[s]);
+    few_columns(a, ts, s, g, sp, base, (float*)ring, few_ml);
+    if (tid == 0) next_s[k & 1] = drawn;
+    __syncthreads();
+    item = __builtin_amdgcn_readfirstlane(next_s[k & 1]);
+  }
+  __syncthreads();
+
   // (The ring's address goes through a register of its own: the compiler would
   // otherwise wait for every load in flight before each operand read.)
   uint32_t ring_at = (uint32_t)(uintptr_t)(lds_void_t*)ring;
   asm volatile("" : "+s"(ring_at));
 
-  // Workgroups draw items in order, each its next one while it works (the merge
-  // kernel sets the counts back to zero). A fixed share of the items left a
-  // quarter of the chip idle at the end.
-  int item = blockIdx.x / queues;
+  item = first;
 #pragma unroll 1
   for (int k = 0; item < total; ++k) {
     int drawn = 0;
-    if (tid == 0) drawn = (int)gridDim.x / queues + atomicAdd(a.drawn + queue, 1);
-    int lo = 0, hi = rk.n_seqs - 1;
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (items_s[mid] <= item) lo = mid; else hi = mid - 1;
-    }
-    const int s = __builtin_amdgcn_readfirstlane(lo);
+    if (tid == 0) drawn = per_queue + atomicAdd(a.drawn + queue, 1);
+    const int s = seq_of(items_s, item);
     const TreeSeq ts = tree_plan(rk.seq_starts, rk.ctx_lens, s, G, rk.max_blocks);
     const int x = __builtin_amdgcn_readfirstlane(item - items_s[s]);
     const int u0 = __builtin_amdgcn_readfirstlane(units_s[s]);
@@ -532,7 +746,7 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_kernel(TreeArgs a)
 // instead of 13.8, 32 trees of 64 nodes 519 instead of 506).
 constexpr int kMergeHeads = 4;
 __global__ __launch_bounds__(32 * kMergeHeads) void tree_combine_kernel(TreeArgs a) {
-  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x < kXCDs) a.drawn[threadIdx.x] = 0;
+  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x < 2 * kXCDs) a.drawn[threadIdx.x] = 0;
   const int row = blockIdx.x + a.rk.seq_starts[0];
   if (row >= a.rk.seq_starts[a.rk.n_seqs]) return;
   // The row's sequence: the starts after the first that are not behind it, read
@@ -626,14 +840,12 @@ __global__ __launch_bounds__(32 * kMergeHeads) void tree_combine_kernel(TreeArgs
 }  // namespace
 
 // The most that any call of so many rows and sequences can need. A sequence of
-// len keys has tree_splits(cols, len) parts: at most `few` of kTreeSplitsFew where
-// it has up to 128 columns per key/value head, `many` above. (Part sizes are
-// rounded up to 128 keys, which is why a shorter sequence may have more parts
-// than a longer one: the bounds are those of any length up to the longest.)
+// len keys has tree_splits(cols, len) parts: at most `few` where it has up to 128
+// columns per key/value head, `many` above (a part holds at least 512 or 1024
+// keys before it is rounded up).
 int64_t tree_column_parts(int64_t max_rows, int64_t max_seqs, int Hq, int Hkv, int max_blocks) {
   const int64_t len = (int64_t)max_blocks * kBlockTokens;
-  // A part holds at least 128 keys (few columns), 1024 before rounding (many).
-  const int64_t few = len / 128 + 1 < kTreeSplitsFew ? len / 128 + 1 : kTreeSplitsFew;
+  const int64_t few = len / 512 + 1 < kTreeSplitsFew ? len / 512 + 1 : kTreeSplitsFew;
   const int64_t many = len / 1024 + 1 < kTreeSplits ? len / 1024 + 1 : kTreeSplits;
   const int64_t cols = max_seqs * Hkv * 128 < max_rows * Hq ? max_seqs * Hkv * 128 : max_rows * Hq;
   return cols * few + (max_rows * Hq - cols) * many;
@@ -660,7 +872,7 @@ hipError_t launch_tree_attention_bf16(const uint16_t* q, const uint16_t* k_cache
   a.part_cap = part_cap;
   a.plan = plan;
   a.drawn = redo;
-  a.redo = redo + kXCDs;
+  a.redo = redo + 2 * kXCDs;
   // Two workgroups per CU (LDS, registers); batches of more than kMaxSeqs sequences
   // in several launches, which share the partial buffers in turn.
   for (int s0 = 0; s0 < rk.n_seqs; s0 += kMaxSeqs) {
