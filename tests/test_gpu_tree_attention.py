@@ -141,6 +141,60 @@ def test_unseen_nodes_may_hold_anything(dtype, hq, hkv, hd):
     call.check()
 
 
+# Up to 16 columns (nodes times heads of a group) and just above, in one call.
+FEW = [(8, 2, [(0, 1), (20, 4), (530, 3), (1100, 2), (40, 5), (5000, 4), (3, 4)]),
+       (16, 1, [(0, 1), (15, 1), (700, 1), (31, 2)]),
+       (4, 4, [(0, 16), (9, 15), (640, 12), (50, 17), (2047, 1), (7, 3)]),
+       (5, 1, [(511, 1), (512, 3), (513, 2), (100, 4), (16400, 1)])]
+
+
+@pytest.mark.parametrize("hq,hkv,trees", FEW)
+def test_few_columns_with_masks_of_any_kind(hq, hkv, trees):
+    def any_set(rng, n, words):
+        seen = rng.random((n, 64 * words)) < 0.6
+        seen[rng.random(n) < 0.2] = False
+        return seen & (np.arange(64 * words) < n)[None]
+    for masks in (path_masks, any_set):
+        call = Call("bf16", hq, hkv, 128, trees, words=2, seed=21, masks=masks)
+        call.run()
+        call.check()
+
+
+@pytest.mark.parametrize("hq,hkv,trees", FEW)
+def test_few_columns_among_nodes_that_hold_anything(hq, hkv, trees):
+    call = Call("bf16", hq, hkv, 128, trees, seed=22)
+    k, v = call.c.tokens()
+    hit = np.zeros(int(call.starts[-1]), bool)
+    for s, (prefix, nodes) in enumerate(trees):
+        if nodes < 2:
+            continue
+        j = nodes // 2
+        k[call.table[s, (prefix + j) // B], (prefix + j) % B] = np.nan
+        v[call.table[s, (prefix + j) // B], (prefix + j) % B] = np.nan
+        hit[call.starts[s] + np.nonzero(call.seen[s][:, j])[0]] = True
+    call.c.put(0, k, v)
+    call.run()
+    torch.cuda.synchronize()
+    got = call.o.cpu().double().numpy()
+    assert np.isnan(got[hit]).all() and np.isfinite(got[~hit]).all()
+    call.c.put(0, np.nan_to_num(k), np.nan_to_num(v))
+    call.run()
+    torch.cuda.synchronize()
+    assert np.array_equal(call.o.cpu().double().numpy()[~hit], got[~hit])
+    # A value that is seen but infinite comes out, in its sign.
+    s = max(range(len(trees)), key=lambda i: trees[i][1])
+    at = trees[s][0]  # the first node
+    v[call.table[s, at // B], at % B] = -np.inf
+    call.c.put(0, np.nan_to_num(k), np.where(np.isnan(v), 0, v))
+    call.run()
+    torch.cuda.synchronize()
+    got = call.o.cpu().double().numpy()
+    rows = call.starts[s] + np.nonzero(call.seen[s][:, 0])[0]
+    assert (got[rows] == -np.inf).all()
+    rest = np.setdiff1d(np.arange(len(got)), rows)
+    assert np.isfinite(got[rest]).all()
+
+
 @pytest.mark.parametrize("dtype,hq,hkv,hd", [("bf16", 8, 1, 128), ("f32", 2, 1, 32)])
 def test_long_contexts(dtype, hq, hkv, hd):
     call = Call(dtype, hq, hkv, hd, [(40000, 7), (3, 2), (20011, 30), (9000, 1)], seed=7)
