@@ -165,7 +165,9 @@ constexpr int kScoreHeads = 64;  // query heads of a group at a time
 
 // Scores of a row's blocks for one kv head, in a grid of their own: scored and
 // chosen by one workgroup per row and head, a row of 1900 blocks takes 10 us
-// longer and 96 rows of 640 2 us less. 64 blocks per wave and step, all
+// longer and 96 rows of 640 2 us less. Bound by the summaries' bytes in pieces of
+// 256 (those rows: 141 MB in 42 us; loading a step ahead, with fewer workgroups
+// and more steps of each, changes nothing). 64 blocks per wave and step, all
 // loads of the first step issued before the queries are turned into bytes: lane
 // (c, j4) holds bytes 16 j4 .. of each 64-byte piece of the summaries of blocks
 // c, 16 + c, ..; the product with the same bytes of query head c leaves heads
