@@ -197,11 +197,17 @@ int grow(coco_layer* H, char** buf, size_t* have, size_t want) {
   if (want <= *have) return COCO_OK;
   HIPCHK(hipSetDevice(H->device));
   char* p = nullptr;
+  try {
+    H->extra.push_back(nullptr);
+  } catch (const std::exception&) {
+    return fail(COCO_ENOMEM, "out of host memory");
+  }
   if (hipMalloc((void**)&p, want) != hipSuccess) {
     (void)hipGetLastError();
+    H->extra.pop_back();
     return fail(COCO_ENOMEM, "workspace of %zu bytes does not fit", want);
   }
-  H->extra.push_back(p);
+  H->extra.back() = p;
   *buf = p;
   *have = want;
   return COCO_OK;

@@ -5,6 +5,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <exception>
 #include <vector>
 
 #include "../../include/coco.h"
@@ -32,7 +33,11 @@ inline int elem_bytes(int dtype) { return dtype == COCO_BF16 ? 2 : 4; }
 // (validation mode; synchronises).
 template <typename V>
 int fetch(std::vector<V>& dst, const V* src, size_t n, hipStream_t st) {
-  dst.resize(n);
+  try {
+    dst.resize(n);
+  } catch (const std::exception&) {
+    return fail(COCO_ENOMEM, "%zu values do not fit host memory", n);
+  }
   if (n == 0) return COCO_OK;
   HIPCHK(hipMemcpyAsync(dst.data(), src, n * sizeof(V), hipMemcpyDeviceToHost, st));
   HIPCHK(hipStreamSynchronize(st));

@@ -241,6 +241,16 @@ def test_graph_replay_of_a_speculative_step():
         assert all(torch.equal(a, b) for a, b in zip(got, want))
 
 
+def test_validation_of_arrays_that_fit_no_memory_is_an_error():
+    """n_seqs of a table that no host could copy: an error code, no abort."""
+    c = Cache("f32", 1, 1, 32, 4, 1 << 22)
+    coco.coco_layer_set_validate(c.h, True)
+    one, table, refs = i32([0]), i32(np.full(64, -1)), i32(np.zeros(4))
+    rc = coco._lib.raw_call("coco_kv_free", c.h.raw, one.data_ptr(), None, 1, table.data_ptr(),
+                            2 ** 31 - 1, refs.data_ptr(), None)
+    assert rc == coco._lib.COCO_ENOMEM and "host memory" in coco.coco_last_error()
+
+
 def test_refusals():
     c = Cache("bf16", 4, 2, 128, 20, 4, n_layers=2, max_seqs=3)
     table, refs = i32(np.full((5, 4), -1)), i32(np.zeros(20))
