@@ -365,7 +365,8 @@ int coco_tree_reserve(coco_layer_t h, int32_t max_rows, int32_t max_seqs);
  *   tree_mask [n_rows][mask_words] 64-bit words
  * A row that attends nothing (no prefix, no bit) gives zeros; what it does not
  * attend may hold anything. A row's result does not depend on the other
- * sequences of the call. Needs coco_tree_reserve (COCO_ESTATE without). */
+ * sequences of the call; rows from seq_starts[n_seqs] on (a padded call) are
+ * left as they are. Needs coco_tree_reserve (COCO_ESTATE without). */
 int coco_tree_attention(coco_layer_t h, int32_t layer, const void* q, void* o, int32_t n_rows,
                         const int32_t* seq_starts, int32_t n_seqs, const int32_t* block_table,
                         const int32_t* ctx_lens, const uint64_t* tree_mask, int32_t mask_words,
@@ -429,8 +430,9 @@ int coco_block_select(coco_layer_t h, const int8_t* summary, const float* scales
  * position + 1) - 1) in the blocks selected[row][kv head] lists, of
  * coco_block_select or the caller's own: distinct blocks in any order;
  * entries outside the row's blocks (-1) are skipped. (Validation mode takes
- * ascending blocks of the row and -1 only.) A row without keys gives zeros.
- * q, o as in coco_tree_attention. */
+ * ascending blocks of the row and -1 only.) A row without keys gives zeros. q, o
+ * and rows past the sequences as in coco_tree_attention (and so there and in
+ * coco_block_select). */
 int coco_sparse_attention(coco_layer_t h, int32_t layer, const void* q, void* o, int32_t n_rows,
                           const int32_t* positions, const int32_t* seq_starts, int32_t n_seqs,
                           const int32_t* block_table, const int32_t* ctx_lens,

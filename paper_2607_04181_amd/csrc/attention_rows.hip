@@ -54,6 +54,7 @@ __global__ __launch_bounds__(64 * kRowsWaves) void attn_rows_kernel(
   const int lane = threadIdx.x & 63;
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int t = lane & 15, j4 = lane >> 4;
+  if (row_past_seqs(rk.seq_starts, rk.n_seqs, i)) return;
   const int s = row_to_seq(rk.seq_starts, rk.n_seqs, i);
   const int g = h0 / (Hq / Hkv);
   // Keys of the row's sequence that it may attend; tree: nodes, and the first
@@ -68,7 +69,7 @@ __global__ __launch_bounds__(64 * kRowsWaves) void attn_rows_kernel(
     prefix = n - nodes;
     mask = rk.mask + (int64_t)i * rk.words;
   } else {
-    n = min(rk.ctx_lens[s], rk.positions[i] + 1);
+    n = min(rk.ctx_lens[s] - 1, rk.positions[i]) + 1;
     list = rk.selected + ((int64_t)i * Hkv + g) * rk.top;
   }
   n = min(max(n, 0), rk.max_blocks * kBlockTokens);

@@ -157,7 +157,7 @@ __device__ __forceinline__ uint32_t order_key(float f) {
 }
 
 __device__ __forceinline__ int row_keys(const RowKeys& rk, int s, int i) {
-  return min(max(min(rk.ctx_lens[s], rk.positions[i] + 1), 0), rk.max_blocks * kBlockTokens);
+  return min(max(min(rk.ctx_lens[s] - 1, rk.positions[i]) + 1, 0), rk.max_blocks * kBlockTokens);
 }
 
 constexpr int kScoreWaves = 4;
@@ -191,6 +191,7 @@ __global__ __launch_bounds__(64 * kScoreWaves) void block_score_kernel(
   const int lane = threadIdx.x & 63;
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c16 = lane & 15, j4 = lane >> 4;
+  if (row_past_seqs(rk.seq_starts, rk.n_seqs, i)) return;
   const int s = row_to_seq(rk.seq_starts, rk.n_seqs, i);
   const int nb = (row_keys(rk, s, i) + kBlockTokens - 1) / kBlockTokens;
   // Rows that choose all their blocks need no scores.
@@ -302,6 +303,7 @@ __global__ __launch_bounds__(kSelThreads) void block_choose_kernel(
   __shared__ int hist[256], red[2][kSelWaves], digit_s, above_s, count_s;
   __shared__ uint32_t ends[2][kSelWaves];
   const int i = blockIdx.y, g = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+  if (row_past_seqs(rk.seq_starts, rk.n_seqs, i)) return;
   const int s = row_to_seq(rk.seq_starts, rk.n_seqs, i);
   const int nb = (row_keys(rk, s, i) + kBlockTokens - 1) / kBlockTokens;
   const uint32_t* kp = keys + ((int64_t)i * Hkv + g) * stride;

@@ -201,4 +201,9 @@ __device__ __forceinline__ int row_to_seq(const int32_t* seq_starts, int n_seqs,
   return lo;
 }
 
+// Whether a call row belongs to no sequence (a padded call: left as it is).
+__device__ __forceinline__ bool row_past_seqs(const int32_t* seq_starts, int n_seqs, int row) {
+  return seq_starts != nullptr && row >= seq_starts[n_seqs];
+}
+
 }  // namespace coco

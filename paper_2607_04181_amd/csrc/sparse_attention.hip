@@ -60,8 +60,9 @@ __global__ __launch_bounds__(64 * kWaves, 3) void sparse_attention_kernel(Sparse
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c16 = lane & 15, j4 = lane >> 4;
   const RowKeys& rk = a.rk;
+  if (row_past_seqs(rk.seq_starts, rk.n_seqs, i)) return;
   const int s = row_to_seq(rk.seq_starts, rk.n_seqs, i);
-  const int n = min(max(min(rk.ctx_lens[s], rk.positions[i] + 1), 0),
+  const int n = min(max(min(rk.ctx_lens[s] - 1, rk.positions[i]) + 1, 0),
                     rk.max_blocks * kBlockTokens);
   const int blocks = (n + kBlockTokens - 1) / kBlockTokens;
 
@@ -210,7 +211,7 @@ __global__ __launch_bounds__(64 * kWaves, 3) void sparse_attention_kernel(Sparse
 __global__ __launch_bounds__(256) void sparse_combine_kernel(SparseArgs a) {
   const int i = blockIdx.x, head = blockIdx.y * 8 + (threadIdx.x >> 5);
   const int dim = (threadIdx.x & 31) * 4, G = a.Hq / a.Hkv;
-  if (head >= a.Hq) return;
+  if (head >= a.Hq || row_past_seqs(a.rk.seq_starts, a.rk.n_seqs, i)) return;
   const int64_t at = ((int64_t)i * a.Hkv + head / G) * a.parts * G + head % G;
   float M = -INFINITY, L = 0.f;
   f32x4_t y = {0.f, 0.f, 0.f, 0.f};

@@ -144,6 +144,43 @@ def test_rows_of_a_prompt_and_rows_without_keys():
 
 
 @pytest.mark.parametrize("dtype,hq,hkv,hd", [("bf16", 8, 2, 128), ("f32", 4, 2, 64)])
+def test_positions_past_the_cache_attend_all_of_it(dtype, hq, hkv, hd):
+    r = Rows(dtype, hq, hkv, hd, [200, 33], rows=[[150, 199, 10 ** 6, 2 ** 31 - 1], [2 ** 31 - 2]],
+             top=5, seed=11)
+    r.summarize()
+    r.select(1, 1)
+    torch.cuda.synchronize()
+    r.check_select(1, 1)
+    r.attention()
+    r.check_attention()
+
+
+@pytest.mark.parametrize("dtype,hq,hkv,hd", [("bf16", 8, 2, 128), ("f32", 4, 2, 64)])
+@pytest.mark.parametrize("top", [4, 40])
+def test_rows_past_the_last_sequence_are_left_as_they_are(dtype, hq, hkv, hd, top):
+    rows = [[0, 15, 1299], [5, 39], [99]]
+    r = Rows(dtype, hq, hkv, hd, [1300, 40, 100], rows=rows, top=top, seed=10)
+    r.summarize()
+    r.select(1, 1)
+    r.attention()
+    torch.cuda.synchronize()
+    want = r.selected.clone(), r.o.clone()
+    # The same sequences in a call of more rows, whose arrays hold anything.
+    pos, starts, table, lens = r.rest
+    more = 5
+    q = torch.cat([r.q, torch.full_like(r.q[:more], float("nan"))])
+    pos = torch.cat([pos, i32([10 ** 9, -7, 3, 2 ** 31 - 1, 0])])
+    sel = torch.cat([torch.full_like(r.selected, 55), torch.full_like(r.selected[:more], 66)])
+    o = torch.full_like(q, 7.0)
+    coco.coco_sparse_reserve(r.c.h, r.n + more, top)
+    coco.coco_block_select(r.c.h, r.summary, r.scales, q, pos, starts, table, lens, 1, 1, sel)
+    coco.coco_sparse_attention(r.c.h, 0, q, o, pos, starts, table, lens, sel)
+    torch.cuda.synchronize()
+    assert torch.equal(sel[:r.n], want[0]) and torch.equal(o[:r.n], want[1])
+    assert (sel[r.n:] == 66).all() and (o[r.n:] == 7.0).all()
+
+
+@pytest.mark.parametrize("dtype,hq,hkv,hd", [("bf16", 8, 2, 128), ("f32", 4, 2, 64)])
 def test_ties_go_to_the_lowest_block(dtype, hq, hkv, hd):
     r = Rows(dtype, hq, hkv, hd, [16 * 90, 16 * 700], top=30, seed=4)
     r.summarize()

@@ -350,6 +350,22 @@ def test_refusals():
     call.check()
 
 
+@pytest.mark.parametrize("dtype,hq,hkv,hd", [("bf16", 8, 2, 128), ("f32", 4, 2, 64)])
+def test_rows_past_the_last_sequence_are_left_as_they_are(dtype, hq, hkv, hd):
+    call = Call(dtype, hq, hkv, hd, [(600, 3), (40, 30), (0, 2)], seed=23)
+    call.run()
+    torch.cuda.synchronize()
+    n, more = len(call.o), 6
+    starts, table, lens, mask = call.args
+    q = torch.cat([call.q, torch.full_like(call.q[:more], float("nan"))])
+    o = torch.full_like(q, 7.0)
+    masks = torch.cat([mask, torch.full_like(mask[:more], -1)])
+    coco.coco_tree_reserve(call.c.h, n + more, 3)
+    coco.coco_tree_attention(call.c.h, 0, q, o, starts, table, lens, masks)
+    torch.cuda.synchronize()
+    assert torch.equal(o[:n], call.o) and (o[n:] == 7.0).all()
+
+
 def test_tensors_of_another_device_are_refused():
     call = Call("bf16", 8, 2, 128, [(20, 3)], seed=20)
     here, call.c.h.device = call.c.h.device, call.c.h.device + 1
