@@ -74,6 +74,9 @@
  *   block_table[n_seqs][max_blocks_per_seq]   physical block ids, -1 unused
  *   ctx_lens[n_seqs]       cached tokens of sequence s once this call's tokens
  *                          are appended (decode, normally positions[i] + 1)
+ * A token whose block_table entry is no block of the pools (-1, or from
+ * num_blocks on: pages that coco_kv_alloc did not serve) is not cached by any
+ * call, and nothing is written in its place; validation mode refuses such calls.
  * Every token attends to the cached keys of its own sequence at positions
  * 0 .. its own position (causal), its own key included: a decode row i
  * attends min(ctx_lens[i], positions[i] + 1) keys, so cached tokens past its

@@ -6,14 +6,6 @@ using namespace coco;
 
 namespace {
 
-// Blocks every layer of [first, first + n) has.
-int64_t shared_blocks(const coco_layer* H, int first, int n) {
-  int64_t nb = INT64_MAX;
-  for (int l = first; l < first + n; ++l)
-    if (H->layers[l].num_blocks < nb) nb = H->layers[l].num_blocks;
-  return nb;
-}
-
 int check_layers(const coco_layer* H, int first, int n) {
   if (!H) return fail(COCO_EINVAL, "handle is NULL");
   // (first + n could wrap)

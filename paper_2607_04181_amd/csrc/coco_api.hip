@@ -519,9 +519,7 @@ int validate_batch(coco_layer* H, int64_t hidden_rows, const int32_t* row_idx, i
   }
   if (ss[0] != 0 || ss[n_seqs] != n_rows)
     return fail(COCO_EINVAL, "seq_starts must run from 0 to n_rows");
-  int64_t min_blocks = INT64_MAX;
-  for (int l = first_layer; l < first_layer + n_layers; ++l)
-    if (H->layers[l].num_blocks < min_blocks) min_blocks = H->layers[l].num_blocks;
+  const int64_t min_blocks = shared_blocks(H, first_layer, n_layers);
   if (tree_words)  // (siblings share a position)
     return validate_tree(H, n_rows, positions, seq_starts, n_seqs, block_table, ctx_lens,
                          tree_words, min_blocks, st);
@@ -756,7 +754,7 @@ int decode_layer(coco_layer* H, const Work& W, const coco_layer_weights& w, cons
   // RoPE, local cache append.
   TIMED(COCO_K_QKV_EPILOGUE,
         HIPCHK(launch_qkv_epilogue_bf16(W.part, plan.S, M, Hq, Hkv, hd, positions, bt,
-                                        c.max_blocks_per_seq, H->inv_freq, q,
+                                        c.max_blocks_per_seq, w.num_blocks, H->inv_freq, q,
                                         (bf16_t*)w.k_cache, (bf16_t*)w.v_cache, ctx, W.split_off,
                                         H->max_splits, W.ss, d, c.rms_eps, st)));
   // Attention over the paged cache.
@@ -806,6 +804,7 @@ int f32_layer(coco_layer* H, const Work& W, const coco_layer_weights& w, const f
   qa.positions = positions;
   qa.seq_starts = seq_starts;
   qa.block_table = bt;
+  qa.num_blocks = w.num_blocks;
   if (rows && rows->mask) qa.tree_lens = ctx;
   qa.inv_freq = H->inv_freq;
   qa.q_out = (float*)W.q;
@@ -882,6 +881,8 @@ int run_span(coco_layer* H, const Work& W, int first, int nl, T* hidden, const i
         rs.n_seqs = n_seqs;
         rs.max_blocks = H->cfg.max_blocks_per_seq;
         rs.rope_rows = H->rope_rows;
+        // (the slots are written once, for all of the call's layers)
+        rs.num_blocks = shared_blocks(H, first, nl);
         if (rows && rows->mask) rs.tree_lens = ctx;
       }
       rc = prefill_layer(H, W, w, x_src, x_idx, y, y_idx, M, positions, seq_starts, n_seqs, bt,
@@ -1071,11 +1072,11 @@ int coco_kv_append(coco_layer_t H, int32_t layer, const void* k, const void* v,
   if (c.dtype == COCO_BF16)
     HIPCHK(launch_kv_append<bf16_t>((const bf16_t*)k, (const bf16_t*)v, seq_idx, positions, n_tok,
                                     c.n_kv_heads, c.head_dim, block_table, c.max_blocks_per_seq,
-                                    (bf16_t*)w.k_cache, (bf16_t*)w.v_cache, st));
+                                    w.num_blocks, (bf16_t*)w.k_cache, (bf16_t*)w.v_cache, st));
   else
     HIPCHK(launch_kv_append<float>((const float*)k, (const float*)v, seq_idx, positions, n_tok,
                                    c.n_kv_heads, c.head_dim, block_table, c.max_blocks_per_seq,
-                                   (float*)w.k_cache, (float*)w.v_cache, st));
+                                   w.num_blocks, (float*)w.k_cache, (float*)w.v_cache, st));
   return end.finish();
 }
 

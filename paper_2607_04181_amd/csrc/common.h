@@ -201,6 +201,13 @@ __device__ __forceinline__ int row_to_seq(const int32_t* seq_starts, int n_seqs,
   return lo;
 }
 
+// A token's place in the pool, 16 * block + slot; -1 where its table entry names
+// no block of the pool (pages that a request did not get): it is not cached, and
+// the -1 must not be divided (towards zero: 15 of 16 slots would lie in block 0).
+__device__ __forceinline__ int cache_place(int block, int64_t num_blocks, int pos) {
+  return block < 0 || block >= num_blocks ? -1 : block * kBlockTokens + pos % kBlockTokens;
+}
+
 // Whether a call row belongs to no sequence (a padded call: left as it is).
 __device__ __forceinline__ bool row_past_seqs(const int32_t* seq_starts, int n_seqs, int row) {
   return seq_starts != nullptr && row >= seq_starts[n_seqs];

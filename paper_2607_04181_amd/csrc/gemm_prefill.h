@@ -555,6 +555,7 @@ __global__ __launch_bounds__(T::NT) void gemm_prefill_kernel(const bf16_t* __res
           *(u32x4_t*)(dst + 64) = vu;
         } else {
           const int at = (int)slots[RG * p + rq].y, slot = at & (kBlockTokens - 1);
+          if (at < 0) continue;  // no page: not cached
           bf16_t* tile =
               ea.k_cache + ((int64_t)(at / kBlockTokens) * ea.Hkv + (hh - ea.Hq)) * kTile;
           *(u32x4_t*)(tile + k_tile_offset(slot, jd0)) = vl;
@@ -578,7 +579,7 @@ __global__ __launch_bounds__(T::NT) void gemm_prefill_kernel(const bf16_t* __res
           e4[e] = f32_to_bf16(st_row(4 * quad + e)[col]);
           at[e] = (int)slots[lr0 + e].y;
         }
-        bool run = m0 + lr0 + 3 < M && at[0] % 4 == 0;
+        bool run = m0 + lr0 + 3 < M && at[0] >= 0 && at[0] % 4 == 0;
 #pragma unroll
         for (int e = 1; e < 4; ++e) run = run && at[e] == at[0] + e;
         const auto place = [&](int a) {
@@ -590,7 +591,7 @@ __global__ __launch_bounds__(T::NT) void gemm_prefill_kernel(const bf16_t* __res
         } else {
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            if (m0 + lr0 + e < M) *place(at[e]) = (bf16_t)e4[e];
+            if (m0 + lr0 + e < M && at[e] >= 0) *place(at[e]) = (bf16_t)e4[e];
         }
       }
       __syncthreads();  // the group's staging is read

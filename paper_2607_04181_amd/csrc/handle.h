@@ -111,6 +111,14 @@ struct coco_layer {
 
 namespace coco {
 
+// Blocks every layer of [first, first + n) has.
+inline int64_t shared_blocks(const coco_layer* H, int first, int n) {
+  int64_t nb = INT64_MAX;
+  for (int l = first; l < first + n; ++l)
+    if (H->layers[l].num_blocks < nb) nb = H->layers[l].num_blocks;
+  return nb;
+}
+
 // Records the handle's completion event behind the call's last kernel, unless
 // the stream is being captured into a graph (the event would then only fire
 // on replays).

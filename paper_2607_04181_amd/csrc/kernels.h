@@ -61,13 +61,15 @@ LaunchEvents& launch_events();
 // Prefill row slots (optional output of the gather kernel): row_info[2i] =
 // positions[i] clamped to [0, rope_rows), row_info[2i + 1] = 16 * the cache block
 // of that position in row i's sequence + its slot there (rows of a sequence
-// contiguous).
+// contiguous), -1 where the row has no place in the cache: its entry is no block
+// of the pool.
 struct RowSlotArgs {
   const int32_t* positions = nullptr;
   const int32_t* seq_starts = nullptr;
   const int32_t* block_table = nullptr;
   int32_t* row_info = nullptr;  // null: not written
   int n_seqs = 0, max_blocks = 0, rope_rows = 0;
+  int64_t num_blocks = 0;
   // Trees: row i of sequence s is cached at tree_lens[s] - (rows of s) + (its
   // place among them), not at its position.
   const int32_t* tree_lens = nullptr;
@@ -96,14 +98,14 @@ hipError_t launch_rope_table(const double* inv_freq, int half, int n_pos, float*
 // Decode: sum of S split-K partials of the QKV projection, each row's sums
 // scaled by 1 / sqrt(sum_s ss[s][row] / d + eps) (RMSNorm_1, folded into the
 // projection), RoPE on query and key heads, queries to q_out [M][Hq*hd],
-// keys/values into the paged cache. One workgroup also writes the decode
-// attention's work list split_off (layout at launch_attn_decode_bf16) from the
+// keys/values into the paged cache (not where the position's table entry is no
+// block of the pool). One workgroup also writes the decode attention's work list split_off (layout at launch_attn_decode_bf16) from the
 // keys each row attends, min(ctx_lens, positions + 1) (partition counts capped
 // at max_splits).
 hipError_t launch_qkv_epilogue_bf16(const float* part, int S, int M, int Hq, int Hkv, int hd,
                                     const int32_t* positions, const int32_t* block_table,
-                                    int max_blocks, const double* inv_freq, uint16_t* q_out,
-                                    uint16_t* k_cache, uint16_t* v_cache,
+                                    int max_blocks, int64_t num_blocks, const double* inv_freq,
+                                    uint16_t* q_out, uint16_t* k_cache, uint16_t* v_cache,
                                     const int32_t* ctx_lens, int32_t* split_off, int max_splits,
                                     const float* ss, int d, float eps, hipStream_t st);
 
@@ -127,12 +129,13 @@ hipError_t launch_untile(const uint16_t* src, int M, int K, uint16_t* dst, int64
 hipError_t launch_residual_scatter_bf16(const float* part, int S, int M, int d, const float* x1,
                                         uint16_t* out, const int32_t* row_idx, hipStream_t st);
 
-// Bit copy of [n][Hkv][hd] keys/values into the paged cache.
+// Bit copy of [n][Hkv][hd] keys/values into the paged cache; tokens whose table
+// entry is no block of the pool are left out.
 template <typename T>
 hipError_t launch_kv_append(const T* k, const T* v, const int32_t* seq_idx,
                             const int32_t* positions, int n, int Hkv, int hd,
-                            const int32_t* block_table, int max_blocks, T* k_cache,
-                            T* v_cache, hipStream_t st);
+                            const int32_t* block_table, int max_blocks, int64_t num_blocks,
+                            T* k_cache, T* v_cache, hipStream_t st);
 
 // ---------------------------------------------------------------- GEMMs
 // Every bf16 GEMM below reads its weights W [N][K] in tile order: the 1 KB
@@ -260,10 +263,11 @@ struct F32EpiArgs {
   float* k_cache = nullptr;
   float* v_cache = nullptr;
   const int32_t* tree_lens = nullptr;  // as in RowSlotArgs
+  int64_t num_blocks = 0;
   int n_seqs = 0, max_blocks = 0, Hq = 0, Hkv = 0, hd = 0;
 };
 // RMSNorm_1, QKV projection, RoPE, queries to q_out [M][Hq*hd], keys and
-// values into the paged cache.
+// values into the paged cache (not where the table entry is no block of the pool).
 hipError_t launch_f32_qkv(const float* x, const float* w_qkv, int M, int d, const F32EpiArgs& ea,
                           hipStream_t st);
 // out[m] = res[row_idx[m]] + o[m] W_o^T.

@@ -56,7 +56,7 @@ __global__ __launch_bounds__(kFThreads) void layer_f32_gemm_kernel(const float* 
   __shared__ int arow[TM];     // source (QKV: hidden) or output (scatter) row
   __shared__ int pos_s[TM];    // QKV: position
   __shared__ int slot_s[TM];   // QKV: slot in the cache block
-  __shared__ int64_t blk_s[TM];  // QKV: cache block
+  __shared__ int64_t blk_s[TM];  // QKV: cache block (-1: no page)
   __shared__ float rot[MODE == kFQkv ? TM * 16 : 1][2];
 
   const int tid = threadIdx.x, lane = tid & 63;
@@ -165,7 +165,8 @@ __global__ __launch_bounds__(kFThreads) void layer_f32_gemm_kernel(const float* 
         at = min(max(ea.tree_lens[seq] - ea.seq_starts[seq + 1] + m, 0),
                  ea.max_blocks * kBlockTokens - 1);
       slot_s[tid] = at % kBlockTokens;
-      blk_s[tid] = ea.block_table[(int64_t)seq * ea.max_blocks + at / kBlockTokens];
+      const int64_t blk = ea.block_table[(int64_t)seq * ea.max_blocks + at / kBlockTokens];
+      blk_s[tid] = blk < ea.num_blocks ? blk : -1;
     } else if constexpr (MODE == kFScatter || MODE == kFResid) {
       arow[tid] = ea.row_idx ? ea.row_idx[m] : m;
     }
@@ -259,7 +260,7 @@ __global__ __launch_bounds__(kFThreads) void layer_f32_gemm_kernel(const float* 
         float* dst = ea.q_out + ((int64_t)m * ea.Hq + head) * hd + j;
         dst[0] = v0;
         dst[hd / 2] = v1;
-      } else {
+      } else if (blk_s[rl] >= 0) {
         const int slot = slot_s[rl];
         const bool key = head < ea.Hq + ea.Hkv;
         const int g = head - ea.Hq - (key ? 0 : ea.Hkv);

@@ -89,7 +89,7 @@ __device__ __forceinline__ void write_row_slot_uniform(const RowSlotArgs& rs, in
   const int blk = block_table[(int64_t)lo * rs.max_blocks + at / kBlockTokens];
   if (threadIdx.x == 0) {
     rs.row_info[2 * i] = min(max(pos, 0), rs.rope_rows - 1);
-    rs.row_info[2 * i + 1] = blk * kBlockTokens + at % kBlockTokens;
+    rs.row_info[2 * i + 1] = cache_place(blk, rs.num_blocks, at);
   }
 }
 
@@ -209,8 +209,8 @@ template <int S>
 __global__ __launch_bounds__(kEpiHeads * kWave) void qkv_epilogue_kernel(
     const float* __restrict__ part, int M, int Hq, int Hkv, int hd,
     const int32_t* __restrict__ positions, const int32_t* __restrict__ block_table,
-    int max_blocks, const double* __restrict__ inv_freq, bf16_t* __restrict__ q_out,
-    bf16_t* __restrict__ k_cache, bf16_t* __restrict__ v_cache,
+    int max_blocks, int64_t num_blocks, const double* __restrict__ inv_freq,
+    bf16_t* __restrict__ q_out, bf16_t* __restrict__ k_cache, bf16_t* __restrict__ v_cache,
     const int32_t* __restrict__ ctx_lens, int32_t* __restrict__ split_off, int max_splits,
     const float* __restrict__ ss, int d, float eps) {
   __shared__ float rot[2][128];  // cos, sin of the row's angles (hd / 2 <= 128)
@@ -322,7 +322,8 @@ __global__ __launch_bounds__(kEpiHeads * kWave) void qkv_epilogue_kernel(
       if (rem != 0) split_off[M + 2 + atomicAdd(&wl_rank[rem], 1)] = s;
     }
   }
-  if (!live) return;
+  // (a token without a page is not cached)
+  if (!live || (h >= Hq && (blk < 0 || blk >= num_blocks))) return;
 #pragma unroll
   for (int t = 0; t < 4; ++t) val[t] *= rscale;
   if (h < Hq + Hkv) {
@@ -367,17 +368,17 @@ __global__ __launch_bounds__(kEpiHeads * kWave) void qkv_epilogue_kernel(
 
 hipError_t launch_qkv_epilogue_bf16(const float* part, int S, int M, int Hq, int Hkv, int hd,
                                     const int32_t* positions, const int32_t* block_table,
-                                    int max_blocks, const double* inv_freq, bf16_t* q_out,
-                                    bf16_t* k_cache, bf16_t* v_cache, const int32_t* ctx_lens,
-                                    int32_t* split_off, int max_splits, const float* ss, int d,
-                                    float eps, hipStream_t st) {
+                                    int max_blocks, int64_t num_blocks, const double* inv_freq,
+                                    bf16_t* q_out, bf16_t* k_cache, bf16_t* v_cache,
+                                    const int32_t* ctx_lens, int32_t* split_off, int max_splits,
+                                    const float* ss, int d, float eps, hipStream_t st) {
   if (M <= 0) return hipSuccess;
   if (hd > 256 || hd % 2 != 0 || !ss || !split_off) return hipErrorInvalidValue;
   const dim3 grid((Hq + 2 * Hkv + kEpiHeads - 1) / kEpiHeads, M);
   COCO_SWITCH_S(S, COCO_LAUNCH((qkv_epilogue_kernel<S_>), grid, dim3(kEpiHeads * kWave), 0, st,
                                part, M, Hq, Hkv, hd, positions, block_table, max_blocks,
-                               inv_freq, q_out, k_cache, v_cache, ctx_lens, split_off,
-                               max_splits, ss, d, eps));
+                               num_blocks, inv_freq, q_out, k_cache, v_cache, ctx_lens,
+                               split_off, max_splits, ss, d, eps));
   return hipGetLastError();
 }
 
@@ -570,7 +571,7 @@ template <typename T, int HD>
 __global__ __launch_bounds__(kRowThreads) void kv_append_kernel(
     const T* __restrict__ k, const T* __restrict__ v, const int32_t* __restrict__ seq_idx,
     const int32_t* __restrict__ positions, int n, int Hkv, int hd_arg,
-    const int32_t* __restrict__ block_table, int max_blocks, bool aligned,
+    const int32_t* __restrict__ block_table, int max_blocks, int64_t num_blocks, bool aligned,
     T* __restrict__ k_cache, T* __restrict__ v_cache) {
   constexpr int kMaxHd = HD ? HD : 256;
   const int hd = HD ? HD : hd_arg;
@@ -579,7 +580,7 @@ __global__ __launch_bounds__(kRowThreads) void kv_append_kernel(
   __shared__ __attribute__((aligned(16))) T ks[kApTok * (kMaxHd + kPad)];
   __shared__ __attribute__((aligned(16))) T vs[(kApTok + kApHalo) * (kMaxHd + kPad)];
   __shared__ int64_t blk_s[kInfo];  // cache block and slot of tokens t0 - 3 .. t0 + 18
-  __shared__ int slot_s[kInfo];     // (-1: no such token)
+  __shared__ int slot_s[kInfo];     // (both -1: no such token, or no page for it)
   __shared__ int lead[kApTok / 4], n_lead, lone;  // runs' first tokens; tokens of no run (bits)
   // Consecutive windows on one XCD (blockIdx % 8), so that a tile shared by two
   // windows fills up in that XCD's L2 and leaves as whole lines.
@@ -616,9 +617,10 @@ __global__ __launch_bounds__(kRowThreads) void kv_append_kernel(
     }
   }
   if (threadIdx.x < kInfo) {
-    blk_s[threadIdx.x] =
-        info ? block_table[(int64_t)seq * max_blocks + pos / kBlockTokens] : -1;
-    slot_s[threadIdx.x] = info ? pos % kBlockTokens : -1;
+    const int64_t blk = info ? block_table[(int64_t)seq * max_blocks + pos / kBlockTokens] : -1;
+    const bool paged = blk >= 0 && blk < num_blocks;
+    blk_s[threadIdx.x] = paged ? blk : -1;
+    slot_s[threadIdx.x] = paged ? pos % kBlockTokens : -1;
   }
 #pragma unroll
   for (int u = 0; u < kPer; ++u) {
@@ -645,8 +647,8 @@ __global__ __launch_bounds__(kRowThreads) void kv_append_kernel(
     const uint64_t mask = __ballot(l);
     if (l) lead[__popcll(mask & ((1ull << threadIdx.x) - 1))] = threadIdx.x;
     const int x = min((int)threadIdx.x, live - 1);
-    const uint64_t none =
-        __ballot(threadIdx.x < live && !leads(x - slot_s[x + kApHalo] % 4));
+    const int slot = slot_s[x + kApHalo];
+    const uint64_t none = __ballot(threadIdx.x < live && slot >= 0 && !leads(x - slot % 4));
     if (threadIdx.x == 0) {
       n_lead = __popcll(mask);
       lone = (int)none;
@@ -656,7 +658,7 @@ __global__ __launch_bounds__(kRowThreads) void kv_append_kernel(
   const int64_t tile_elems = (int64_t)kBlockTokens * hd;
   for (int i = threadIdx.x; i < kApTok * pieces; i += kRowThreads) {
     const int t = i % kApTok, c = i / kApTok;
-    if (t >= live) continue;
+    if (t >= live || slot_s[t + kApHalo] < 0) continue;
     T* tile = k_cache + (blk_s[t + kApHalo] * Hkv + h) * tile_elems;
     *(Piece8<T>*)(tile + k_tile_offset(slot_s[t + kApHalo], 8 * c)) =
         *(const Piece8<T>*)(ks + t * stride + 8 * c);
@@ -686,8 +688,8 @@ __global__ __launch_bounds__(kRowThreads) void kv_append_kernel(
 template <typename T>
 hipError_t launch_kv_append(const T* k, const T* v, const int32_t* seq_idx,
                             const int32_t* positions, int n, int Hkv, int hd,
-                            const int32_t* block_table, int max_blocks, T* k_cache,
-                            T* v_cache, hipStream_t st) {
+                            const int32_t* block_table, int max_blocks, int64_t num_blocks,
+                            T* k_cache, T* v_cache, hipStream_t st) {
   if (n <= 0) return hipSuccess;
   if (hd % 32 != 0 || hd > 256) return hipErrorInvalidValue;
   const bool aligned = ((uintptr_t)k | (uintptr_t)v) % 16 == 0;
@@ -695,20 +697,20 @@ hipError_t launch_kv_append(const T* k, const T* v, const int32_t* seq_idx,
   if (wgs > 0x7fffffff) return hipErrorInvalidValue;
   if (hd == 128)
     COCO_LAUNCH_LAST((kv_append_kernel<T, 128>), dim3((unsigned)wgs), dim3(kRowThreads), 0, st, k,
-                     v, seq_idx, positions, n, Hkv, hd, block_table, max_blocks, aligned, k_cache,
-                     v_cache);
+                     v, seq_idx, positions, n, Hkv, hd, block_table, max_blocks, num_blocks,
+                     aligned, k_cache, v_cache);
   else
     COCO_LAUNCH_LAST((kv_append_kernel<T, 0>), dim3((unsigned)wgs), dim3(kRowThreads), 0, st, k, v,
-                     seq_idx, positions, n, Hkv, hd, block_table, max_blocks, aligned, k_cache,
-                     v_cache);
+                     seq_idx, positions, n, Hkv, hd, block_table, max_blocks, num_blocks,
+                     aligned, k_cache, v_cache);
   return hipGetLastError();
 }
 
 template hipError_t launch_kv_append<bf16_t>(const bf16_t*, const bf16_t*, const int32_t*,
                                              const int32_t*, int, int, int, const int32_t*, int,
-                                             bf16_t*, bf16_t*, hipStream_t);
+                                             int64_t, bf16_t*, bf16_t*, hipStream_t);
 template hipError_t launch_kv_append<float>(const float*, const float*, const int32_t*,
                                             const int32_t*, int, int, int, const int32_t*, int,
-                                            float*, float*, hipStream_t);
+                                            int64_t, float*, float*, hipStream_t);
 
 }  // namespace coco
