@@ -106,7 +106,7 @@ __global__ __launch_bounds__(64 * kRowsWaves) void attn_rows_kernel(
       b_l = -1;
       if (mine < entries) b_l = TREE ? mine : list[mine];
       if (b_l >= blocks) b_l = -1;
-      if (b_l >= 0) blk_l = bt[b_l];
+      if (b_l >= 0) blk_l = readable_block(bt[b_l], rk.num_blocks);
     }
     const int b = __builtin_amdgcn_readlane(b_l, x % kWave);
     if (b < 0) continue;

@@ -208,6 +208,12 @@ __device__ __forceinline__ int cache_place(int block, int64_t num_blocks, int po
   return block < 0 || block >= num_blocks ? -1 : block * kBlockTokens + pos % kBlockTokens;
 }
 
+// The block that is read for a table entry: block 0 for what is no block of the
+// pool, so that the rows of a request without its pages read in bounds.
+__device__ __forceinline__ int readable_block(int block, int64_t num_blocks) {
+  return block < 0 || block >= num_blocks ? 0 : block;
+}
+
 // Whether a call row belongs to no sequence (a padded call: left as it is).
 __device__ __forceinline__ bool row_past_seqs(const int32_t* seq_starts, int n_seqs, int row) {
   return seq_starts != nullptr && row >= seq_starts[n_seqs];

@@ -75,10 +75,7 @@ __global__ __launch_bounds__(64 * kWaves, 3) void sparse_attention_kernel(Sparse
     if (b >= blocks) b = -1;
   }
   int blk = 0;
-  if (b >= 0) {
-    const int id = rk.block_table[(int64_t)s * rk.max_blocks + b];
-    blk = id < 0 || id >= rk.num_blocks ? 0 : id;
-  }
+  if (b >= 0) blk = readable_block(rk.block_table[(int64_t)s * rk.max_blocks + b], rk.num_blocks);
   uint64_t left = __ballot(b >= 0);
 
   // Operands of the queries: columns past the group are zero.

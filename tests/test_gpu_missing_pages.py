@@ -184,3 +184,60 @@ def test_a_step_after_a_short_allocation(dtype):
         for got, was in zip(pools[layer], x.start[layer]):
             rest = sorted(set(range(len(got))) - {GUARD + b for b in table[table >= 0]})
             assert torch.equal(got[rest], was[rest])
+
+
+@pytest.mark.parametrize("dtype,hq,hkv,hd", [("bf16", 8, 2, 128), ("f32", 4, 2, 64),
+                                             ("f32", 3, 1, 160)])
+def test_attention_reads_inside_the_pool(dtype, hq, hkv, hd):
+    """With NaN on both sides of the pools, every row of the call is finite, and
+    the served requests' rows are as with all pages."""
+    rng = np.random.default_rng(6)
+    lens, nodes = np.array([70, 900, 33, 20, 9]), np.array([5, 9, 3, 20, 9])
+    width, num_blocks = 60, 80
+    whole, pools = guarded_pools(dtype, hkv, hd, num_blocks, 1, 6)
+    for w in whole[0]:
+        w[:GUARD], w[-GUARD:] = float("nan"), float("nan")
+    c = Cache(dtype, hq, hkv, hd, num_blocks, width, pools=pools)
+    full = tables(rng, lens, width, num_blocks)
+    short = full.copy()
+    short[1, [3, 40, 56]], short[2, 2], short[4, 0] = -1, num_blocks + 2, -GUARD
+    rows = int(nodes.sum())
+    starts, ctx = i32(np.concatenate([[0], np.cumsum(nodes)])), i32(lens)
+    q, out = c.normal(rows, hq, hd), [torch.empty(rows, hq, hd, dtype=DT[dtype], device="cuda")
+                                      for _ in range(2)]
+    mask = torch.full((rows, 1), -1, dtype=torch.int64, device="cuda")
+    coco.coco_tree_reserve(c.h, rows, 5)
+    coco.coco_sparse_reserve(c.h, rows, 60)
+    selected = i32(np.broadcast_to(np.arange(60), (rows, hkv, 60)))
+    positions = i32(np.repeat(lens - 1, nodes))
+
+    def tree(table, o):
+        coco.coco_tree_attention(c.h, 0, q, o, starts, i32(table), ctx, mask)
+
+    def sparse(table, o):
+        coco.coco_sparse_attention(c.h, 0, q, o, positions, starts, i32(table), ctx, selected)
+
+    served = np.isin(np.repeat(np.arange(5), nodes), [0, 3])
+    for call in (tree, sparse):
+        for table, o in zip((full, short), out):
+            call(table, o)
+        torch.cuda.synchronize()
+        assert torch.isfinite(out[1]).all()
+        assert torch.equal(out[0][served], out[1][served])
+
+
+@pytest.mark.parametrize("dtype", sorted(SHAPES))
+@pytest.mark.parametrize("kind", ["tree", "sparse"])
+def test_layers_read_inside_the_pool(kind, dtype):
+    rng = np.random.default_rng(7)
+    lens = np.array([70, 49, 33, 20, 9, 97])
+    news = np.ones(6, np.int64) if kind in ("decode", "sparse") else np.array([9, 20, 6, 1, 9, 30])
+    width, num_blocks = 8, 26
+    x = Layers(dtype, num_blocks, width)
+    for layer in x.start:
+        for p in layer:
+            p[:GUARD], p[-GUARD:] = float("nan"), float("nan")
+    table = tables(rng, lens, width, num_blocks)
+    table[1, 3], table[1, 0], table[2, 2], table[4, 0] = -1, -2, num_blocks + 1, -1
+    hidden, _ = x.run(kind, table, lens, news)
+    assert torch.isfinite(hidden).all()
