@@ -76,10 +76,9 @@
  *                          are appended (decode, normally positions[i] + 1)
  * A token whose block_table entry is no block of the pools (-1, or from
  * num_blocks on: pages that coco_kv_alloc did not serve) is not cached by any
- * call, and nothing is written in its place. A row of the tree and sparse calls
- * below that attends such an entry reads some block of the pool instead: its
- * output means nothing, other rows' are as without it. Validation mode refuses
- * such calls.
+ * call, and nothing is written in its place. A row that attends such an entry
+ * reads some block of the pool instead: its output means nothing, other rows'
+ * are as without it. Validation mode refuses such calls.
  * Every token attends to the cached keys of its own sequence at positions
  * 0 .. its own position (causal), its own key included: a decode row i
  * attends min(ctx_lens[i], positions[i] + 1) keys, so cached tokens past its

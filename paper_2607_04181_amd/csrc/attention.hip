@@ -73,7 +73,7 @@ constexpr int kDecBPW = kDecodeSplit / kBlockTokens / kDecWaves;
 
 struct DecItem {
   int s, g, sp, t1, b_first, b_last;
-  int64_t pb[kDecBPW];  // physical blocks of this wave's share (clamped to b_last)
+  int pb[kDecBPW];  // table entries of this wave's share (clamped to b_last)
 };
 
 // Keys a decode row attends: positions 0 .. its own position, within the
@@ -130,7 +130,7 @@ __device__ __forceinline__ void decode_item_blocks(DecItem& it, const int32_t* b
 __global__ __launch_bounds__(kDecWaves * 64, 4) void attn_decode_kernel(
     const bf16_t* __restrict__ q, const bf16_t* __restrict__ k_cache,
     const bf16_t* __restrict__ v_cache, const int32_t* __restrict__ block_table, int max_blocks,
-    const int32_t* __restrict__ ctx_lens, const int32_t* __restrict__ positions,
+    int64_t num_blocks, const int32_t* __restrict__ ctx_lens, const int32_t* __restrict__ positions,
     const int32_t* __restrict__ split_off, int n_seqs, int Hq, int Hkv,
     float* __restrict__ part_o, float* __restrict__ part_ml, int max_splits, float scale_log2) {
   __shared__ float sm_m[kDecWaves][16], sm_l[kDecWaves][16];
@@ -155,9 +155,10 @@ __global__ __launch_bounds__(kDecWaves * 64, 4) void attn_decode_kernel(
 #pragma unroll
     for (int t = 0; t < 4; ++t) qr[t] = *(const u32x4_t*)(qp + t * 32);
 #pragma unroll
-    for (int u = 0; u < kDecBPW; ++u)
-      load_kv(k_cache + (it.pb[u] * Hkv + it.g) * tile, v_cache + (it.pb[u] * Hkv + it.g) * tile,
-              c16, j4, kf[u], vf[u]);
+    for (int u = 0; u < kDecBPW; ++u) {
+      const int64_t at = ((int64_t)readable_block(it.pb[u], num_blocks) * Hkv + it.g) * tile;
+      load_kv(k_cache + at, v_cache + at, c16, j4, kf[u], vf[u]);
+    }
   };
   // The descriptor of the item after the current one, block-table entries
   // included, is looked up one item ahead: its chain of dependent scalar
@@ -387,7 +388,7 @@ template <int WAVES, int COLS, int KS>
 __global__ __launch_bounds__(WAVES * KS * 64) void attn_prefill_kernel(
     const bf16_t* __restrict__ q, const bf16_t* __restrict__ k_cache,
     const bf16_t* __restrict__ v_cache, const int32_t* __restrict__ block_table, int max_blocks,
-    const int32_t* __restrict__ ctx_lens, const int32_t* __restrict__ positions,
+    int64_t num_blocks, const int32_t* __restrict__ ctx_lens, const int32_t* __restrict__ positions,
     const int32_t* __restrict__ seq_starts, int n_seqs, int Hq, int Hkv, float scale_log2,
     bf16_t* __restrict__ o) {
   static_assert(KS == 1 || KS == 2, "one or two key sets");
@@ -465,7 +466,8 @@ __global__ __launch_bounds__(WAVES * KS * 64) void attn_prefill_kernel(
       const int kvsel = tt / kStBlk, bi = tt % kStBlk;
       const int blk = min(st * kStBlk + bi, n_blk - 1);
       const bf16_t* src = (kvsel ? v_cache : k_cache) +
-                          ((int64_t)bt[blk] * Hkv + g) * kTileElems + lane * 8;
+                          ((int64_t)readable_block(bt[blk], num_blocks) * Hkv + g) * kTileElems +
+                          lane * 8;
       bf16_t* dst = (kvsel ? v_slot(st) : k_slot(st)) + bi * kTileElems;
 #pragma unroll
       for (int pc = 0; pc < 4; ++pc)
@@ -695,7 +697,7 @@ bool attn_combine_fits(int max_splits) {
 
 hipError_t launch_attn_decode_bf16(const uint16_t* q, const uint16_t* k_cache,
                                    const uint16_t* v_cache, const int32_t* block_table,
-                                   int max_blocks, const int32_t* ctx_lens,
+                                   int max_blocks, int64_t num_blocks, const int32_t* ctx_lens,
                                    const int32_t* positions, const int32_t* split_off,
                                    int n_seqs, int Hq, int Hkv, float* part_o, float* part_ml,
                                    int max_splits, int num_cus, hipStream_t st) {
@@ -707,8 +709,8 @@ hipError_t launch_attn_decode_bf16(const uint16_t* q, const uint16_t* k_cache,
   const int64_t work_bound = (int64_t)n_seqs * max_splits * Hkv;
   const int grid = (int)(work_bound < 2 * num_cus ? work_bound : 2 * num_cus);
   COCO_LAUNCH(attn_decode_kernel, dim3(grid), dim3(kDecWaves * 64), 0, st, q, k_cache,
-                     v_cache, block_table, max_blocks, ctx_lens, positions, split_off, n_seqs,
-                     Hq, Hkv, part_o, part_ml, max_splits, scale_log2);
+                     v_cache, block_table, max_blocks, num_blocks, ctx_lens, positions, split_off,
+                     n_seqs, Hq, Hkv, part_o, part_ml, max_splits, scale_log2);
   return hipGetLastError();
 }
 
@@ -725,7 +727,7 @@ hipError_t launch_attn_combine_bf16(const float* part_o, const float* part_ml,
 
 hipError_t launch_attn_prefill_bf16(const uint16_t* q, const uint16_t* k_cache,
                                     const uint16_t* v_cache, const int32_t* block_table,
-                                    int max_blocks, const int32_t* ctx_lens,
+                                    int max_blocks, int64_t num_blocks, const int32_t* ctx_lens,
                                     const int32_t* positions, const int32_t* seq_starts,
                                     int n_seqs, int n_rows, int Hq, int Hkv, uint16_t* o,
                                     int num_cus, hipStream_t st) {
@@ -749,11 +751,13 @@ hipError_t launch_attn_prefill_bf16(const uint16_t* q, const uint16_t* k_cache,
   if (few)
     COCO_LAUNCH((attn_prefill_kernel<kPfWavesFew, 1, kPfKeySets>), grid,
                 dim3(kPfWavesFew * kPfKeySets * 64), 0, st, q, k_cache, v_cache, block_table,
-                max_blocks, ctx_lens, positions, seq_starts, n_seqs, Hq, Hkv, scale_log2, o);
+                max_blocks, num_blocks, ctx_lens, positions, seq_starts, n_seqs, Hq, Hkv, scale_log2,
+                o);
   else
     COCO_LAUNCH((attn_prefill_kernel<kPfWaves, 1, kPfKeySets>), grid,
                 dim3(kPfWaves * kPfKeySets * 64), 0, st, q, k_cache, v_cache, block_table,
-                max_blocks, ctx_lens, positions, seq_starts, n_seqs, Hq, Hkv, scale_log2, o);
+                max_blocks, num_blocks, ctx_lens, positions, seq_starts, n_seqs, Hq, Hkv, scale_log2,
+                o);
   return hipGetLastError();
 }
 

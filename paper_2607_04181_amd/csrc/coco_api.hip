@@ -331,6 +331,8 @@ int coco_layer_init(const coco_layer_config* cfg, const coco_layer_weights* laye
   coco_layer* H = new coco_layer();
   H->cfg = c;
   H->layers.assign(layers, layers + c.n_layers);
+  for (coco_layer_weights& w : H->layers)  // (block ids are int32)
+    if (w.num_blocks > INT32_MAX) w.num_blocks = INT32_MAX;
   H->device = dev;
   H->num_cus = cus;
 
@@ -655,9 +657,9 @@ int attention(coco_layer* H, const Work& W, const coco_layer_weights& w, int M,
     {
       KernelTimer t(H, COCO_K_ATTENTION, st);
       HIPCHK(launch_attn_decode_bf16((const bf16_t*)W.q, (const bf16_t*)w.k_cache,
-                                     (const bf16_t*)w.v_cache, bt, c.max_blocks_per_seq, ctx,
-                                     positions, W.split_off, n_seqs, c.n_q_heads, c.n_kv_heads,
-                                     W.attn_o, W.attn_ml, H->max_splits, H->num_cus, st));
+                                     (const bf16_t*)w.v_cache, bt, c.max_blocks_per_seq,
+                                     w.num_blocks, ctx, positions, W.split_off, n_seqs,
+                                     c.n_q_heads, c.n_kv_heads, W.attn_o, W.attn_ml, H->max_splits, H->num_cus, st));
     }
     KernelTimer t(H, COCO_K_ATTN_COMBINE, st);
     HIPCHK(launch_attn_combine_bf16(W.attn_o, W.attn_ml, ctx, positions, n_seqs, c.n_q_heads,
@@ -665,9 +667,9 @@ int attention(coco_layer* H, const Work& W, const coco_layer_weights& w, int M,
   } else {
     KernelTimer t(H, COCO_K_ATTENTION, st);
     HIPCHK(launch_attn_prefill_bf16((const bf16_t*)W.q, (const bf16_t*)w.k_cache,
-                                    (const bf16_t*)w.v_cache, bt, c.max_blocks_per_seq, ctx,
-                                    positions, seq_starts, n_seqs, M, c.n_q_heads, c.n_kv_heads,
-                                    (bf16_t*)W.o, H->num_cus, st));
+                                    (const bf16_t*)w.v_cache, bt, c.max_blocks_per_seq,
+                                    w.num_blocks, ctx, positions, seq_starts, n_seqs, M,
+                                    c.n_q_heads, c.n_kv_heads, (bf16_t*)W.o, H->num_cus, st));
   }
   return COCO_OK;
 }
@@ -823,8 +825,8 @@ int f32_layer(coco_layer* H, const Work& W, const coco_layer_weights& w, const f
   } else {
     KernelTimer t(H, COCO_K_ATTENTION, st);
     HIPCHK(launch_attn_f32((const float*)W.q, (const float*)w.k_cache,
-                           (const float*)w.v_cache, bt, c.max_blocks_per_seq, ctx, positions,
-                           seq_starts, n_seqs, M, Hq, Hkv, hd, (float*)W.o, st));
+                           (const float*)w.v_cache, bt, c.max_blocks_per_seq, w.num_blocks, ctx,
+                           positions, seq_starts, n_seqs, M, Hq, Hkv, hd, (float*)W.o, st));
   }
   F32EpiArgs oa;
   oa.row_idx = x_idx;

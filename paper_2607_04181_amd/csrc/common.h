@@ -201,17 +201,23 @@ __device__ __forceinline__ int row_to_seq(const int32_t* seq_starts, int n_seqs,
   return lo;
 }
 
+// Whether a table entry names a block of the pool (ids are 32-bit, and
+// coco_layer_init holds num_blocks below 2^31: one unsigned comparison).
+__device__ __forceinline__ bool in_pool(int block, int64_t num_blocks) {
+  return (uint32_t)block < (uint32_t)num_blocks;
+}
+
 // A token's place in the pool, 16 * block + slot; -1 where its table entry names
 // no block of the pool (pages that a request did not get): it is not cached, and
 // the -1 must not be divided (towards zero: 15 of 16 slots would lie in block 0).
 __device__ __forceinline__ int cache_place(int block, int64_t num_blocks, int pos) {
-  return block < 0 || block >= num_blocks ? -1 : block * kBlockTokens + pos % kBlockTokens;
+  return in_pool(block, num_blocks) ? block * kBlockTokens + pos % kBlockTokens : -1;
 }
 
 // The block that is read for a table entry: block 0 for what is no block of the
 // pool, so that the rows of a request without its pages read in bounds.
 __device__ __forceinline__ int readable_block(int block, int64_t num_blocks) {
-  return block < 0 || block >= num_blocks ? 0 : block;
+  return in_pool(block, num_blocks) ? block : 0;
 }
 
 // Whether a call row belongs to no sequence (a padded call: left as it is).

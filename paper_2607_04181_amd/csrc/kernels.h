@@ -293,7 +293,7 @@ bool attn_combine_fits(int max_splits);
 // Decode row s attends min(ctx_lens[s], positions[s] + 1) keys.
 hipError_t launch_attn_decode_bf16(const uint16_t* q, const uint16_t* k_cache,
                                    const uint16_t* v_cache, const int32_t* block_table,
-                                   int max_blocks, const int32_t* ctx_lens,
+                                   int max_blocks, int64_t num_blocks, const int32_t* ctx_lens,
                                    const int32_t* positions, const int32_t* split_off,
                                    int n_seqs, int Hq, int Hkv, float* part_o, float* part_ml,
                                    int max_splits, int num_cus, hipStream_t st);
@@ -307,14 +307,14 @@ hipError_t launch_attn_combine_bf16(const float* part_o, const float* part_ml,
 // [Hq * 128] is written in tile order (the O projection's A operand).
 hipError_t launch_attn_prefill_bf16(const uint16_t* q, const uint16_t* k_cache,
                                     const uint16_t* v_cache, const int32_t* block_table,
-                                    int max_blocks, const int32_t* ctx_lens,
+                                    int max_blocks, int64_t num_blocks, const int32_t* ctx_lens,
                                     const int32_t* positions, const int32_t* seq_starts,
                                     int n_seqs, int n_rows, int Hq, int Hkv, uint16_t* o,
                                     int num_cus, hipStream_t st);
 
 // fp32 path, decode and prefill alike (hd a multiple of 32, at most 256).
 hipError_t launch_attn_f32(const float* q, const float* k_cache, const float* v_cache,
-                           const int32_t* block_table, int max_blocks,
+                           const int32_t* block_table, int max_blocks, int64_t num_blocks,
                            const int32_t* ctx_lens, const int32_t* positions,
                            const int32_t* seq_starts, int n_seqs, int n_rows, int Hq,
                            int Hkv, int hd, float* o, hipStream_t st);

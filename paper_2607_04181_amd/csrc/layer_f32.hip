@@ -165,8 +165,8 @@ __global__ __launch_bounds__(kFThreads) void layer_f32_gemm_kernel(const float* 
         at = min(max(ea.tree_lens[seq] - ea.seq_starts[seq + 1] + m, 0),
                  ea.max_blocks * kBlockTokens - 1);
       slot_s[tid] = at % kBlockTokens;
-      const int64_t blk = ea.block_table[(int64_t)seq * ea.max_blocks + at / kBlockTokens];
-      blk_s[tid] = blk < ea.num_blocks ? blk : -1;
+      const int blk = ea.block_table[(int64_t)seq * ea.max_blocks + at / kBlockTokens];
+      blk_s[tid] = in_pool(blk, ea.num_blocks) ? blk : -1;
     } else if constexpr (MODE == kFScatter || MODE == kFResid) {
       arow[tid] = ea.row_idx ? ea.row_idx[m] : m;
     }
@@ -343,7 +343,7 @@ template <int HS, int GH>  // hd = 32 HS
 __global__ __launch_bounds__(64 * kAWaves) void attn_f32_kernel(
     const float* __restrict__ q, const float* __restrict__ k_cache,
     const float* __restrict__ v_cache, const int32_t* __restrict__ block_table, int max_blocks,
-    const int32_t* __restrict__ ctx_lens, const int32_t* __restrict__ positions,
+    int64_t num_blocks, const int32_t* __restrict__ ctx_lens, const int32_t* __restrict__ positions,
     const int32_t* __restrict__ seq_starts, int n_seqs, int Hq, int Hkv, float* __restrict__ o) {
   constexpr int hd = 32 * HS;
   __shared__ float sm_m[kAWaves][GH], sm_l[kAWaves][GH];
@@ -379,7 +379,8 @@ __global__ __launch_bounds__(64 * kAWaves) void attn_f32_kernel(
     for (int p = 0; p < HS; ++p) acc[e][p][0] = acc[e][p][1] = 0.f;
   }
   for (int b = wv; b < blocks; b += kAWaves) {
-    const int64_t tile = ((int64_t)bt[b] * Hkv + g) * (kBlockTokens * hd);
+    const int64_t tile = ((int64_t)readable_block(bt[b], num_blocks) * Hkv + g) *
+                         (kBlockTokens * hd);
     f32x4_t kf[HS][2], vf[HS][2];
 #pragma unroll
     for (int p = 0; p < HS; ++p)
@@ -467,9 +468,10 @@ __global__ __launch_bounds__(64 * kAWaves) void attn_f32_kernel(
 }  // namespace
 
 hipError_t launch_attn_f32(const float* q, const float* k_cache, const float* v_cache,
-                           const int32_t* block_table, int max_blocks, const int32_t* ctx_lens,
-                           const int32_t* positions, const int32_t* seq_starts, int n_seqs,
-                           int n_rows, int Hq, int Hkv, int hd, float* o, hipStream_t st) {
+                           const int32_t* block_table, int max_blocks, int64_t num_blocks,
+                           const int32_t* ctx_lens, const int32_t* positions,
+                           const int32_t* seq_starts, int n_seqs, int n_rows, int Hq, int Hkv,
+                           int hd, float* o, hipStream_t st) {
   if (n_rows <= 0) return hipSuccess;
   // Heads per workgroup: they share the key/value loads; the queries they
   // keep in registers (hd / 4 floats per lane each) bound their number.
@@ -478,7 +480,8 @@ hipError_t launch_attn_f32(const float* q, const float* k_cache, const float* v_
   const dim3 grid(n_rows, Hq / gh);
 #define COCO_ATT(HS, GH)                                                                       \
   COCO_LAUNCH((attn_f32_kernel<HS, GH>), grid, dim3(64 * kAWaves), 0, st, q, k_cache, v_cache, \
-              block_table, max_blocks, ctx_lens, positions, seq_starts, n_seqs, Hq, Hkv, o)
+              block_table, max_blocks, num_blocks, ctx_lens, positions, seq_starts, n_seqs,    \
+              Hq, Hkv, o)
 #define COCO_ATT4(HS) \
   if (gh == 4) COCO_ATT(HS, 4); else if (gh == 2) COCO_ATT(HS, 2); else COCO_ATT(HS, 1)
 #define COCO_ATT2(HS) \

@@ -248,8 +248,7 @@ __global__ __launch_bounds__(kEpiHeads * kWave) void qkv_epilogue_kernel(
   // per-slice sums of squares, added in slice order.
   const float rscale = 1.0f / sqrtf(sum_parts1<S>(ss + i, M) / (float)d + eps);
   const int pos = positions[i];
-  int64_t blk = 0;
-  int slot = 0;
+  int blk = 0, slot = 0;
   if (live && h >= Hq) {
     blk = block_table[(int64_t)i * max_blocks + pos / kBlockTokens];
     slot = pos % kBlockTokens;
@@ -323,7 +322,7 @@ __global__ __launch_bounds__(kEpiHeads * kWave) void qkv_epilogue_kernel(
     }
   }
   // (a token without a page is not cached)
-  if (!live || (h >= Hq && (blk < 0 || blk >= num_blocks))) return;
+  if (!live || !in_pool(blk, num_blocks)) return;
 #pragma unroll
   for (int t = 0; t < 4; ++t) val[t] *= rscale;
   if (h < Hq + Hkv) {
@@ -339,14 +338,14 @@ __global__ __launch_bounds__(kEpiHeads * kWave) void qkv_epilogue_kernel(
           dst[j] = (bf16_t)f32_to_bf16(rlo);
           dst[j + half] = (bf16_t)f32_to_bf16(rhi);
         } else {
-          bf16_t* tile = k_cache + (blk * Hkv + (h - Hq)) * kBlockTokens * hd;
+          bf16_t* tile = k_cache + ((int64_t)blk * Hkv + (h - Hq)) * kBlockTokens * hd;
           tile[k_tile_offset(slot, j)] = (bf16_t)f32_to_bf16(rlo);
           tile[k_tile_offset(slot, j + half)] = (bf16_t)f32_to_bf16(rhi);
         }
       }
     }
   } else {
-    bf16_t* tile = v_cache + (blk * Hkv + (h - Hq - Hkv)) * kBlockTokens * hd;
+    bf16_t* tile = v_cache + ((int64_t)blk * Hkv + (h - Hq - Hkv)) * kBlockTokens * hd;
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
       const int e = lane + kWave * t;
@@ -617,8 +616,8 @@ __global__ __launch_bounds__(kRowThreads) void kv_append_kernel(
     }
   }
   if (threadIdx.x < kInfo) {
-    const int64_t blk = info ? block_table[(int64_t)seq * max_blocks + pos / kBlockTokens] : -1;
-    const bool paged = blk >= 0 && blk < num_blocks;
+    const int blk = info ? block_table[(int64_t)seq * max_blocks + pos / kBlockTokens] : -1;
+    const bool paged = in_pool(blk, num_blocks);
     blk_s[threadIdx.x] = paged ? blk : -1;
     slot_s[threadIdx.x] = paged ? pos % kBlockTokens : -1;
   }

@@ -227,7 +227,7 @@ def test_attention_reads_inside_the_pool(dtype, hq, hkv, hd):
 
 
 @pytest.mark.parametrize("dtype", sorted(SHAPES))
-@pytest.mark.parametrize("kind", ["tree", "sparse"])
+@pytest.mark.parametrize("kind", ["decode", "prefill", "tree", "sparse"])
 def test_layers_read_inside_the_pool(kind, dtype):
     rng = np.random.default_rng(7)
     lens = np.array([70, 49, 33, 20, 9, 97])
