@@ -150,7 +150,8 @@ int check_rows(const coco_layer* H, int layer, const void* q, const void* o, int
   return COCO_OK;
 }
 
-// Validation mode: sequences' rows, lengths and blocks.
+// Validation mode: sequences' rows, lengths and blocks. Rows past the last
+// sequence (a padded call) are left alone, and their arrays may hold anything.
 int validate_rows(const coco_layer* H, int n_rows, const int32_t* positions,
                   const int32_t* seq_starts, int n_seqs, const int32_t* block_table,
                   const int32_t* ctx_lens, int64_t num_blocks, std::vector<int32_t>& starts,
@@ -162,18 +163,18 @@ int validate_rows(const coco_layer* H, int n_rows, const int32_t* positions,
       (rc = fetch(bt, block_table, (size_t)n_seqs * c.max_blocks_per_seq, st)) ||
       (rc = check_range("ctx_lens", ctx, 0, (int64_t)c.max_blocks_per_seq * kBlockTokens + 1)))
     return rc;
-  if (positions && ((rc = fetch(pos, positions, n_rows, st)) ||
-                    (rc = check_range("positions", pos, 0,
-                                      (int64_t)c.max_blocks_per_seq * kBlockTokens))))
-    return rc;
   if (seq_starts) {
     if ((rc = fetch(starts, seq_starts, n_seqs + 1, st))) return rc;
   } else {
     starts.resize(n_seqs + 1);
     for (int s = 0; s <= n_seqs; ++s) starts[s] = s;
   }
-  if (starts[0] != 0 || starts[n_seqs] != n_rows)
-    return fail(COCO_EINVAL, "seq_starts must run from 0 to n_rows");
+  if (starts[0] != 0 || starts[n_seqs] < 0 || starts[n_seqs] > n_rows)
+    return fail(COCO_EINVAL, "seq_starts must run from 0 to at most n_rows");
+  if (positions && ((rc = fetch(pos, positions, starts[n_seqs], st)) ||
+                    (rc = check_range("positions", pos, 0,
+                                      (int64_t)c.max_blocks_per_seq * kBlockTokens))))
+    return rc;
   for (int s = 0; s < n_seqs; ++s) {
     if (starts[s + 1] < starts[s]) return fail(COCO_EINVAL, "seq_starts not monotone at %d", s);
     if (starts[s + 1] > starts[s] &&

@@ -1,0 +1,47 @@
+"""Calls of more rows than their sequences have (one graph for several batch
+sizes): the rows past the last sequence are left as they are."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2607_04181_amd as coco
+from cache_ref import B, Cache, i32, tables
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dtype,hq,hkv,hd", [("bf16", 8, 2, 128), ("f32", 4, 2, 64)])
+def test_validation_takes_rows_past_the_last_sequence(dtype, hq, hkv, hd):
+    """Attention and choice with validation on, the padding's arrays arbitrary: as
+    the call of the sequences' rows alone. Sequences past the rows are refused."""
+    rng = np.random.default_rng(1)
+    lens, nodes, more, top = np.array([300, 40, 16]), np.array([3, 20, 2]), 6, 5
+    n, width, num_blocks = int(nodes.sum()), 20, 30
+    c = Cache(dtype, hq, hkv, hd, num_blocks, width, seed=1)
+    table, ctx = i32(tables(rng, lens, width, num_blocks)), i32(lens)
+    starts = i32(np.concatenate([[0], np.cumsum(nodes)]))
+    q = c.normal(n + more, hq, hd)
+    mask = torch.full((n + more, 1), -1, dtype=torch.int64, device="cuda")
+    pos = i32(np.concatenate([np.repeat(lens - 1, nodes), [10 ** 9, -7, 3, 2 ** 31 - 1, 0, -1]]))
+    summary = torch.zeros(num_blocks, hkv, 2, hd, dtype=torch.int8, device="cuda")
+    scales = torch.zeros(num_blocks, hkv, device="cuda")
+    coco.coco_tree_reserve(c.h, n + more, 3)
+    coco.coco_sparse_reserve(c.h, n + more, top)
+    coco.coco_kv_summarize(c.h, 0, summary, scales, None, ctx, table)
+
+    def calls(rows):
+        tree, o = (torch.full_like(q[:rows], 7.0) for _ in "to")
+        sel = torch.full((rows, hkv, top), 66, dtype=torch.int32, device="cuda")
+        coco.coco_tree_attention(c.h, 0, q[:rows], tree, starts, table, ctx, mask[:rows])
+        coco.coco_block_select(c.h, summary, scales, q[:rows], pos[:rows], starts, table, ctx, 1, 1,
+                               sel)
+        coco.coco_sparse_attention(c.h, 0, q[:rows], o, pos[:rows], starts, table, ctx, sel)
+        torch.cuda.synchronize()
+        return tree, sel, o
+
+    want = calls(n)
+    coco.coco_layer_set_validate(c.h, True)
+    for got, ref, fill in zip(calls(n + more), want, (7.0, 66, 7.0)):
+        assert torch.equal(got[:n], ref) and (got[n:] == fill).all()
+    with pytest.raises(coco.CocoError, match="seq_starts"):
+        calls(n - 1)
