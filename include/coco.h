@@ -383,7 +383,9 @@ int coco_tree_attention(coco_layer_t h, int32_t layer, const void* q, void* o, i
  * (the pages must be there: coco_kv_alloc); its position is only its rotation,
  * the number of tokens before it on its path, so that an accepted path can
  * move up to its place (coco_kv_compact) as it is; and it attends as in
- * coco_tree_attention. Needs coco_tree_reserve. */
+ * coco_tree_attention. seq_starts[n_seqs] must be n_rows (validation mode refuses
+ * other calls): a row of no sequence is not cached, but its hidden row is
+ * overwritten with what means nothing. Needs coco_tree_reserve. */
 int coco_layer_tree_forward(coco_layer_t h, int32_t first_layer, int32_t n_layers, void* hidden,
                             int64_t hidden_rows, const int32_t* row_idx, int32_t n_rows,
                             const int32_t* positions, const int32_t* seq_starts, int32_t n_seqs,

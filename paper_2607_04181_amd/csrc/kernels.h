@@ -62,7 +62,7 @@ LaunchEvents& launch_events();
 // positions[i] clamped to [0, rope_rows), row_info[2i + 1] = 16 * the cache block
 // of that position in row i's sequence + its slot there (rows of a sequence
 // contiguous), -1 where the row has no place in the cache: its entry is no block
-// of the pool.
+// of the pool, or it is a tree call's row of no sequence.
 struct RowSlotArgs {
   const int32_t* positions = nullptr;
   const int32_t* seq_starts = nullptr;

@@ -165,7 +165,9 @@ __global__ __launch_bounds__(kFThreads) void layer_f32_gemm_kernel(const float* 
         at = min(max(ea.tree_lens[seq] - ea.seq_starts[seq + 1] + m, 0),
                  ea.max_blocks * kBlockTokens - 1);
       slot_s[tid] = at % kBlockTokens;
-      const int blk = ea.block_table[(int64_t)seq * ea.max_blocks + at / kBlockTokens];
+      int blk = ea.block_table[(int64_t)seq * ea.max_blocks + at / kBlockTokens];
+      // (a tree call's row of no sequence must not reach the last one's pages)
+      if (ea.tree_lens != nullptr && row_past_seqs(ea.seq_starts, ea.n_seqs, m)) blk = -1;
       blk_s[tid] = in_pool(blk, ea.num_blocks) ? blk : -1;
     } else if constexpr (MODE == kFScatter || MODE == kFResid) {
       arow[tid] = ea.row_idx ? ea.row_idx[m] : m;

@@ -86,7 +86,9 @@ __device__ __forceinline__ void write_row_slot_uniform(const RowSlotArgs& rs, in
   if (rs.tree_lens != nullptr)
     at = ((cint_ptr)rs.tree_lens)[lo] - seq_starts[lo + 1] + i;
   at = min(max(at, 0), rs.max_blocks * kBlockTokens - 1);
-  const int blk = block_table[(int64_t)lo * rs.max_blocks + at / kBlockTokens];
+  int blk = block_table[(int64_t)lo * rs.max_blocks + at / kBlockTokens];
+  // (a tree call's row of no sequence must not reach the last one's pages)
+  if (rs.tree_lens != nullptr && i >= seq_starts[rs.n_seqs]) blk = -1;
   if (threadIdx.x == 0) {
     rs.row_info[2 * i] = min(max(pos, 0), rs.rope_rows - 1);
     rs.row_info[2 * i + 1] = cache_place(blk, rs.num_blocks, at);

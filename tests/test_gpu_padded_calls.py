@@ -5,7 +5,8 @@ import pytest
 import torch
 
 import paper_2607_04181_amd as coco
-from cache_ref import B, Cache, i32, tables
+from cache_ref import B, Cache, i32, pack_masks, tables
+from test_gpu_missing_pages import SHAPES, Layers
 
 pytestmark = pytest.mark.gpu
 
@@ -45,3 +46,33 @@ def test_validation_takes_rows_past_the_last_sequence(dtype, hq, hkv, hd):
         assert torch.equal(got[:n], ref) and (got[n:] == fill).all()
     with pytest.raises(coco.CocoError, match="seq_starts"):
         calls(n - 1)
+
+
+@pytest.mark.parametrize("dtype", sorted(SHAPES))
+def test_tree_layers_cache_no_row_of_no_sequence(dtype):
+    """Outside the contract of the layer call: the pages of the sequences, the slots
+    behind their tokens among them, and their rows are as without such rows."""
+    rng = np.random.default_rng(2)
+    lens, news, more = np.array([70, 20, 37]), np.array([9, 3, 30]), 7
+    width, num_blocks, n = 6, 14, int(news.sum())
+    x = Layers(dtype, num_blocks, width)
+    table = tables(rng, lens, width, num_blocks)
+    ref_hidden, ref_pools = x.run("tree", table, lens, news)
+    for layer, was in zip(x.whole, x.start):
+        for p, w in zip(layer, was):
+            p.copy_(w)
+    starts = np.concatenate([[0], np.cumsum(news)])
+    seq = np.repeat(np.arange(3), news)
+    pos = (lens - news)[seq] + np.arange(n) - starts[seq]
+    seen = np.zeros((n + more, 64), bool)
+    seen[np.arange(n), np.arange(n) - starts[seq]] = True
+    seen[:, 0] = True
+    hidden = x.hidden0.clone()
+    coco.coco_layer_tree_forward(x.h, 0, 2, hidden, i32(np.arange(n + more)),
+                                 i32(np.append(pos, np.arange(more))), i32(starts), i32(table),
+                                 i32(lens), pack_masks(seen, 1))
+    torch.cuda.synchronize()
+    assert torch.equal(hidden[:n], ref_hidden[:n])
+    assert torch.equal(hidden[n + more:], x.hidden0[n + more:])
+    for got, ref in zip(x.whole, ref_pools):
+        assert all(torch.equal(g, r) for g, r in zip(got, ref))
