@@ -316,7 +316,8 @@ int coco_kv_alloc(coco_layer_t h, const int32_t* seq_idx, const int32_t* lens, i
  * multiple of 16, gets a block of its own with a copy of the parent's next
  * block, keys and values of layers first_layer .. + n_layers - 1. dst_seq
  * rows must be distinct, empty, and no parent of the call; several children
- * may have one parent. (Layers of another handle over the same table: pass
+ * may have one parent. A row named as its own parent is not served and keeps
+ * what it holds. (Layers of another handle over the same table: pass
  * the table entries lens[i] / 16 of both rows to its coco_kv_copy.) */
 int coco_kv_fork(coco_layer_t h, int32_t first_layer, int32_t n_layers, const int32_t* src_seq,
                  const int32_t* dst_seq, const int32_t* lens, int32_t n, int32_t* block_table,

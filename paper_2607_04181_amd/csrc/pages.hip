@@ -184,7 +184,8 @@ __global__ __launch_bounds__(256) void page_fork_kernel(PageArgs a, CachePools p
     if (from >= 0 && from < a.num_blocks) copy_page(pools.p[p], bytes, from, a.list[a.off[i]]);
     return;
   }
-  if (dst < 0 || dst >= a.n_seqs) return;
+  // A row named as its own parent keeps what it holds.
+  if (dst < 0 || dst >= a.n_seqs || dst == src) return;
   for (int b = threadIdx.x; b < a.max_blocks; b += blockDim.x) {
     int id = -1;
     if (served && b < full) {

@@ -205,6 +205,26 @@ def test_compact(dtype, hkv, hd, layers):
             assert np.array_equal(got, want), l
 
 
+def test_a_fork_of_a_row_into_itself_is_not_served():
+    """Its row and counts are as if it had not been made, the others' served."""
+    rng = np.random.default_rng(8)
+    width, num_blocks = 6, 30
+    c = Cache("f32", 2, 1, 32, num_blocks, width, seed=8)
+    table, refs = state(rng, np.array([40, 33, 0, 0]), width, num_blocks)
+    dt, dr, status = i32(table), i32(refs), i32(np.full(3, 9))
+    pools = [p.clone() for p in c.pools[0]]
+    src, dst, lens = [0, 1, 1], [2, 1, 3], [37, 20, 33]
+    coco.coco_kv_fork(c.h, 0, 1, i32(src), i32(dst), i32(lens), dt, dr, status)
+    served, copies = ref_fork(table, refs, [0, 1], [2, 3], [37, 33])
+    same(status, np.array([served[0], 0, served[1]]))
+    same(dt, table)
+    same(dr, refs)
+    for got, want in zip(c.pools[0], pools):
+        for a, b in copies:
+            want[b] = want[a]
+        assert torch.equal(got, want)
+
+
 def test_graph_replay_of_a_speculative_step():
     """Trim, alloc and fork captured once and replayed: integers and pools as
     the eager run's every time."""
