@@ -32,16 +32,17 @@ __device__ __forceinline__ bool page_request_ok(const PageArgs& a, int i) {
   return src >= 0 && src < a.n_seqs && src != row;
 }
 
-// Exclusive sum over the workgroup's threads, and the whole. Its barriers also
-// keep one call's sums from the next's.
-__device__ __forceinline__ int plan_scan(int x, int* sums, int& all) {
+// Exclusive sum over the workgroup's threads, and the whole, of at most 2^24
+// each (a row's entries): a wave's sum fits 32 bits, 128 rows of that width do
+// not. Its barriers also keep one call's sums from the next's.
+__device__ __forceinline__ int64_t plan_scan(int x, int* sums, int64_t& all) {
   const int lane = threadIdx.x & 63;
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int upto = wave_scan(x);
   __syncthreads();
   if (lane == kWave - 1) sums[wv] = upto;
   __syncthreads();
-  int before = 0;
+  int64_t before = 0;
   all = 0;
 #pragma unroll
   for (int w = 0; w < kPlanWaves; ++w) {
@@ -91,8 +92,10 @@ __global__ __launch_bounds__(kPlanThreads) void page_plan_kernel(PageArgs a) {
     __syncthreads();
   }
   // Their places in the list, in request order (off[] becomes the exclusive
-  // sum), and in status[] what each needs.
-  int total = 0, need = 0, at = 0;  // (of the thread's last request)
+  // sum), and in status[] what each needs. A place past 2^31 is held there, where
+  // nothing fits either.
+  int64_t total = 0;
+  int need = 0, at = 0;  // (of the thread's last request)
   for (int i0 = 0; i0 < a.n; i0 += kPlanThreads) {
     const int i = i0 + tid;
     need = 0;
@@ -102,9 +105,9 @@ __global__ __launch_bounds__(kPlanThreads) void page_plan_kernel(PageArgs a) {
       else
         need = page_request_ok(a, i) ? (a.lens[i] % kBlockTokens != 0) : -1;
     }
-    int all;
-    const int before = plan_scan(max(need, 0), sums, all);
-    at = total + before;
+    int64_t all;
+    const int64_t before = plan_scan(max(need, 0), sums, all);
+    at = (int)min(total + before, (int64_t)INT32_MAX);
     if (i < a.n) {
       a.off[i] = at;
       a.status[i] = need;
@@ -121,18 +124,18 @@ __global__ __launch_bounds__(kPlanThreads) void page_plan_kernel(PageArgs a) {
 #pragma unroll
     for (int u = 0; u < kPlanIds; ++u)
       free_ids |= (uint32_t)(first + u < a.num_blocks && r[u] == 0) << u;
-    int all;
-    int place = found + plan_scan(__popc(free_ids), sums, all);
+    int64_t all;
+    int place = found + (int)plan_scan(__popc(free_ids), sums, all);
     for (; free_ids && place < total; free_ids &= free_ids - 1)
       a.list[place++] = (int)(first + __builtin_ctz(free_ids));
-    found += all;
+    found += (int)all;
   }
   // A request is served while those up to it fit.
   const int last = (a.n - 1) / kPlanThreads * kPlanThreads + tid;
-  if (last < a.n) a.status[last] = need >= 0 && (need == 0 || at + need <= found);
+  if (last < a.n) a.status[last] = need >= 0 && (need == 0 || need <= found - at);
   for (int i = tid; i < last && i < a.n; i += kPlanThreads) {
     const int n = a.status[i];
-    a.status[i] = n >= 0 && (n == 0 || a.off[i] + n <= found);
+    a.status[i] = n >= 0 && (n == 0 || n <= found - a.off[i]);
   }
 }
 

@@ -116,6 +116,21 @@ def test_alloc_of_many_requests_and_rows_out_of_range():
     same(dr, refs)
 
 
+def test_alloc_of_more_than_32_bits_of_blocks():
+    """139 rows that ask for 2^24 blocks each: none is served, whatever their sum."""
+    n, width, blocks = 140, 1 << 24, 40
+    c = Cache("f32", 1, 1, 32, blocks, width, max_seqs=n)
+    table = torch.full((n, width), -1, dtype=torch.int32, device="cuda")
+    lens = np.full(n, width * B)
+    lens[0], lens[77] = 40, 0
+    refs, status = i32(np.arange(blocks) % 2), i32(np.full(n, 9))
+    coco.coco_kv_alloc(c.h, i32(np.arange(n)), i32(lens), table, refs, status)
+    same(status, (lens <= 40).astype(np.int64))
+    assert table[0, :4].tolist() == [0, 2, 4, -1]
+    assert (table[1:] == -1).all() and (table[0, 3:] == -1).all()
+    same(refs, np.isin(np.arange(blocks), [0, 2, 4]) | (np.arange(blocks) % 2))
+
+
 @pytest.mark.parametrize("dtype,hkv,hd,layers", [("bf16", 2, 128, 3), ("f32", 1, 32, 1),
                                                  ("f32", 3, 96, 70), ("bf16", 8, 128, 1)])
 @pytest.mark.parametrize("short", [False, True])
