@@ -185,8 +185,9 @@ int validate_rows(const coco_layer* H, int n_rows, const int32_t* positions,
 }
 
 // A buffer of the handle's that grows; what it outgrows stays until destroy,
-// since captured graphs may hold its address.
-int grow(coco_layer* H, char** buf, size_t* have, size_t want) {
+// since captured graphs may hold its address. A new one's last `zero` bytes are
+// cleared for calls on any stream, before it becomes the handle's.
+int grow(coco_layer* H, char** buf, size_t* have, size_t want, size_t zero = 0) {
   if (want <= *have) return COCO_OK;
   HIPCHK(hipSetDevice(H->device));
   char* p = nullptr;
@@ -201,6 +202,10 @@ int grow(coco_layer* H, char** buf, size_t* have, size_t want) {
     return fail(COCO_ENOMEM, "workspace of %zu bytes does not fit", want);
   }
   H->extra.back() = p;
+  if (zero) {
+    HIPCHK(hipMemset(p + want - zero, 0, zero));
+    HIPCHK(hipDeviceSynchronize());
+  }
   *buf = p;
   *have = want;
   return COCO_OK;
@@ -524,13 +529,8 @@ int coco_tree_reserve(coco_layer_t H, int32_t max_rows, int32_t max_seqs) {
                   rows, seqs, (long long)parts);
     const size_t o = align256((size_t)parts * c.head_dim * 4), ml = align256((size_t)parts * 8);
     const size_t plan = align256((size_t)seqs * 8), redo = ((size_t)rows * c.n_q_heads + 16) * 4;
-    const char* had = H->tree_ws;
-    const int rc = grow(H, &H->tree_ws, &H->tree_bytes, o + ml + plan + redo);
+    const int rc = grow(H, &H->tree_ws, &H->tree_bytes, o + ml + plan + redo, redo);
     if (rc) return rc;
-    if (H->tree_ws != had) {  // calls on any stream are to find it zero
-      HIPCHK(hipMemset(H->tree_ws + o + ml + plan, 0, redo));
-      HIPCHK(hipDeviceSynchronize());
-    }
     H->tree_parts = parts;
     H->tree_part_o = (float*)H->tree_ws;
     H->tree_part_ml = (float*)(H->tree_ws + o);
