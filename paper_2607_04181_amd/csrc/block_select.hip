@@ -171,9 +171,9 @@ constexpr int kScoreHeads = 64;  // query heads of a group at a time
 // loads of the first step issued before the queries are turned into bytes: lane
 // (c, j4) holds bytes 16 j4 .. of each 64-byte piece of the summaries of blocks
 // c, 16 + c, ..; the product with the same bytes of query head c leaves heads
-// 4 j4 .. + 3 of block c. HS: head_dim / 32 (the pieces unrolled: with the sums of
-// a loop over them read in the block behind it, the compiler left too few wait
-// states before the first).
+// 4 j4 .. + 3 of block c. HS: head_dim / 32 (the pieces unrolled: behind a loop over
+// them the compiler read the first sum after two wait states in place of eight;
+// tests/test_mfma_waits.py looks for that in the assembly of every kernel).
 template <typename T, int HS>
 __global__ __launch_bounds__(64 * kScoreWaves) void block_score_kernel(
     const T* __restrict__ q, const int8_t* __restrict__ summary, const float* __restrict__ scales,
