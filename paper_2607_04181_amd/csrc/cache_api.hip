@@ -52,7 +52,9 @@ int check_range(const char* name, const std::vector<int32_t>& a, int64_t lo, int
 }
 
 int check_distinct(const char* name, const std::vector<int32_t>& a, int n_ids) {
-  std::vector<char> seen(n_ids, 0);
+  std::vector<char> seen;
+  const int rc = zeros(seen, n_ids);
+  if (rc) return rc;
   for (size_t i = 0; i < a.size(); ++i) {
     if (seen[a[i]]) return fail(COCO_EINVAL, "%s[%zu] = %d is a duplicate", name, i, a[i]);
     seen[a[i]] = 1;
@@ -102,7 +104,8 @@ int page_requests(coco_layer* H, int first, int nl, const int32_t* src, const in
       return rc;
     if (fork) {
       if ((rc = fetch(s, src, n, st)) || (rc = check_range("parent", s, 0, n_seqs))) return rc;
-      std::vector<char> child(n_seqs, 0);
+      std::vector<char> child;
+      if ((rc = zeros(child, n_seqs))) return rc;
       for (int i = 0; i < n; ++i) child[d[i]] = 1;
       for (int i = 0; i < n; ++i) {
         if (child[s[i]])
@@ -164,9 +167,9 @@ int validate_rows(const coco_layer* H, int n_rows, const int32_t* positions,
       (rc = check_range("ctx_lens", ctx, 0, (int64_t)c.max_blocks_per_seq * kBlockTokens + 1)))
     return rc;
   if (seq_starts) {
-    if ((rc = fetch(starts, seq_starts, n_seqs + 1, st))) return rc;
+    if ((rc = fetch(starts, seq_starts, (size_t)n_seqs + 1, st))) return rc;
   } else {
-    starts.resize(n_seqs + 1);
+    if ((rc = zeros(starts, (size_t)n_seqs + 1))) return rc;
     for (int s = 0; s <= n_seqs; ++s) starts[s] = s;
   }
   if (starts[0] != 0 || starts[n_seqs] < 0 || starts[n_seqs] > n_rows)
@@ -439,7 +442,8 @@ int coco_kv_copy(coco_layer_t H, int32_t first_layer, int32_t n_layers, const in
         (rc = check_range("src_blocks", s, 0, blocks)) ||
         (rc = check_range("dst_blocks", d, 0, blocks)))
       return rc;
-    std::vector<char> to(blocks, 0);
+    std::vector<char> to;
+    if ((rc = zeros(to, blocks))) return rc;
     for (int i = 0; i < n; ++i) {
       if (to[d[i]]) return fail(COCO_EINVAL, "dst_blocks[%d] = %d is a duplicate", i, d[i]);
       to[d[i]] = 1;
@@ -475,7 +479,7 @@ int coco_kv_compact(coco_layer_t H, int32_t first_layer, int32_t n_layers, const
   if (H->validate) {
     std::vector<int32_t> s, b, k, ks, bt;
     if ((rc = fetch(s, seq_idx, n, st)) || (rc = fetch(b, base_lens, n, st)) ||
-        (rc = fetch(k, kept, n_kept, st)) || (rc = fetch(ks, kept_starts, n + 1, st)) ||
+        (rc = fetch(k, kept, n_kept, st)) || (rc = fetch(ks, kept_starts, (size_t)n + 1, st)) ||
         (rc = fetch(bt, block_table, (size_t)n_seqs * c.max_blocks_per_seq, st)) ||
         (rc = check_range("sequence", s, 0, n_seqs)) ||
         (rc = check_distinct("sequence", s, n_seqs)) ||

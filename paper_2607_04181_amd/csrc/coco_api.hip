@@ -506,12 +506,13 @@ int validate_batch(coco_layer* H, int64_t hidden_rows, const int32_t* row_idx, i
       (rc = fetch(bt, block_table, (size_t)n_seqs * c.max_blocks_per_seq, st)))
     return rc;
   if (seq_starts) {
-    if ((rc = fetch(ss, seq_starts, n_seqs + 1, st))) return rc;
+    if ((rc = fetch(ss, seq_starts, (size_t)n_seqs + 1, st))) return rc;
   } else {
-    ss.resize(n_seqs + 1);
+    if ((rc = zeros(ss, (size_t)n_seqs + 1))) return rc;
     for (int s = 0; s <= n_seqs; ++s) ss[s] = s;
   }
-  std::vector<char> seen(hidden_rows, 0);
+  std::vector<char> seen;
+  if ((rc = zeros(seen, hidden_rows))) return rc;
   for (int i = 0; i < n_rows; ++i) {
     if (ri[i] < 0 || ri[i] >= hidden_rows)
       return fail(COCO_EINVAL, "row_idx[%d] = %d out of range [0, %lld)", i, ri[i],

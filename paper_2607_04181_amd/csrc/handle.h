@@ -29,16 +29,23 @@ inline size_t align256(size_t b) { return (b + 255) & ~(size_t)255; }
 
 inline int elem_bytes(int dtype) { return dtype == COCO_BF16 ? 2 : 4; }
 
+// n zeros: no exception leaves an entry point.
+template <typename V>
+int zeros(std::vector<V>& dst, size_t n) {
+  try {
+    dst.assign(n, V());
+  } catch (const std::exception&) {
+    return fail(COCO_ENOMEM, "%zu values do not fit host memory", n);
+  }
+  return COCO_OK;
+}
+
 // Copies n values of a device array to the host behind the stream's work
 // (validation mode; synchronises).
 template <typename V>
 int fetch(std::vector<V>& dst, const V* src, size_t n, hipStream_t st) {
-  try {
-    dst.resize(n);
-  } catch (const std::exception&) {
-    return fail(COCO_ENOMEM, "%zu values do not fit host memory", n);
-  }
-  if (n == 0) return COCO_OK;
+  const int rc = zeros(dst, n);
+  if (rc || n == 0) return rc;
   HIPCHK(hipMemcpyAsync(dst.data(), src, n * sizeof(V), hipMemcpyDeviceToHost, st));
   HIPCHK(hipStreamSynchronize(st));
   return COCO_OK;

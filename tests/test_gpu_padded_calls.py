@@ -76,3 +76,20 @@ def test_tree_layers_cache_no_row_of_no_sequence(dtype):
     assert torch.equal(hidden[n + more:], x.hidden0[n + more:])
     for got, ref in zip(x.whole, ref_pools):
         assert all(torch.equal(g, r) for g, r in zip(got, ref))
+
+
+@pytest.mark.parametrize("dtype", sorted(SHAPES))
+def test_validation_of_more_hidden_rows_than_host_memory_is_an_error(dtype):
+    """hidden_rows that no host could mark as taken: an error code, no abort."""
+    x = Layers(dtype, 4, 2)
+    coco.coco_layer_set_validate(x.h, True)
+    zero, one, starts, table = i32([0]), i32([1]), i32([0, 1]), i32([[2, -1]])
+    mask = torch.ones(1, 1, dtype=torch.int64, device="cuda")
+    at = [t.data_ptr() for t in (x.hidden0, zero, starts, table, one, mask)]
+    hidden, row, ss, bt, ctx, bits = at
+    for name, args in (("coco_layer_tree_forward", (0, 1, hidden, 1 << 60, row, 1, row, ss, 1, bt, ctx,
+                                                    bits, 1, None)),
+                       ("coco_layer_forward", (0, hidden, 1 << 60, row, 1, row, None, 1, bt, ctx,
+                                               None))):
+        assert coco._lib.raw_call(name, x.h.raw, *args) == coco._lib.COCO_ENOMEM
+        assert "host memory" in coco.coco_last_error()
