@@ -15,11 +15,10 @@ int check_layers(const coco_layer* H, int first, int n) {
   return COCO_OK;
 }
 
-int check_requests(const coco_layer* H, int n, int n_seqs) {
+int check_requests(int n, int n_seqs) {
   if (n < 0) return fail(COCO_EINVAL, "negative number of requests");
   if (n > 65535) return fail(COCO_EINVAL, "%d requests in a call (at most 65535)", n);
   if (n_seqs < 1) return fail(COCO_EINVAL, "n_seqs must be >= 1");
-  (void)H;
   return COCO_OK;
 }
 
@@ -137,8 +136,7 @@ int page_requests(coco_layer* H, int first, int nl, const int32_t* src, const in
 
 // Attention rows' shapes and pointers that the host can check.
 int check_rows(const coco_layer* H, int layer, const void* q, const void* o, int n_rows,
-               const int32_t* positions, const int32_t* seq_starts, int n_seqs, const int32_t* bt,
-               const int32_t* ctx) {
+               const int32_t* seq_starts, int n_seqs, const int32_t* bt, const int32_t* ctx) {
   const coco_layer_config& c = H->cfg;
   if (layer < 0 || layer >= c.n_layers) return fail(COCO_EINVAL, "layer %d out of range", layer);
   if (n_rows < 0) return fail(COCO_EINVAL, "n_rows < 0");
@@ -149,7 +147,6 @@ int check_rows(const coco_layer* H, int layer, const void* q, const void* o, int
   if (n_seqs < 1) return fail(COCO_EINVAL, "n_seqs must be >= 1");
   if (seq_starts == nullptr && n_seqs != n_rows)
     return fail(COCO_EINVAL, "rows without seq_starts need n_seqs == n_rows");
-  (void)positions;
   return COCO_OK;
 }
 
@@ -364,7 +361,7 @@ int coco_kv_alloc(coco_layer_t H, const int32_t* seq_idx, const int32_t* lens, i
                   int32_t* block_table, int32_t n_seqs, int32_t* ref_counts, int32_t* status,
                   coco_stream_t stream) {
   if (!H) return fail(COCO_EINVAL, "handle is NULL");
-  int rc = check_requests(H, n, n_seqs);
+  int rc = check_requests(n, n_seqs);
   if (rc || n == 0) return rc;
   if (!seq_idx || !lens || !block_table || !ref_counts || !status)
     return fail(COCO_EINVAL, "NULL argument");
@@ -378,7 +375,7 @@ int coco_kv_fork(coco_layer_t H, int32_t first_layer, int32_t n_layers, const in
                  const int32_t* dst_seq, const int32_t* lens, int32_t n, int32_t* block_table,
                  int32_t n_seqs, int32_t* ref_counts, int32_t* status, coco_stream_t stream) {
   int rc = check_layers(H, first_layer, n_layers);
-  if (!rc) rc = check_requests(H, n, n_seqs);
+  if (!rc) rc = check_requests(n, n_seqs);
   if (rc || n == 0) return rc;
   if (!src_seq || !dst_seq || !lens || !block_table || !ref_counts || !status)
     return fail(COCO_EINVAL, "NULL argument");
@@ -392,7 +389,7 @@ int coco_kv_free(coco_layer_t H, const int32_t* seq_idx, const int32_t* keep_len
                  int32_t* block_table, int32_t n_seqs, int32_t* ref_counts,
                  coco_stream_t stream) {
   if (!H) return fail(COCO_EINVAL, "handle is NULL");
-  int rc = check_requests(H, n, n_seqs);
+  int rc = check_requests(n, n_seqs);
   if (rc || n == 0) return rc;
   if (!seq_idx || !block_table || !ref_counts) return fail(COCO_EINVAL, "NULL argument");
   const coco_layer_config& c = H->cfg;
@@ -465,7 +462,7 @@ int coco_kv_compact(coco_layer_t H, int32_t first_layer, int32_t n_layers, const
                     int32_t n, int32_t n_kept, const int32_t* block_table, int32_t n_seqs,
                     coco_stream_t stream) {
   int rc = check_layers(H, first_layer, n_layers);
-  if (!rc) rc = check_requests(H, n, n_seqs);
+  if (!rc) rc = check_requests(n, n_seqs);
   if (rc) return rc;
   if (n_kept < 0) return fail(COCO_EINVAL, "n_kept < 0");
   if (n == 0 || n_kept == 0) return COCO_OK;
@@ -551,7 +548,7 @@ int coco_tree_attention(coco_layer_t H, int32_t layer, const void* q, void* o, i
                         const int32_t* ctx_lens, const uint64_t* tree_mask, int32_t mask_words,
                         coco_stream_t stream) {
   if (!H) return fail(COCO_EINVAL, "handle is NULL");
-  int rc = check_rows(H, layer, q, o, n_rows, nullptr, seq_starts, n_seqs, block_table, ctx_lens);
+  int rc = check_rows(H, layer, q, o, n_rows, seq_starts, n_seqs, block_table, ctx_lens);
   if (rc || n_rows == 0) return rc;
   if ((rc = check_tree(H, n_rows, seq_starts, n_seqs, tree_mask, mask_words))) return rc;
   const coco_layer_weights& w = H->layers[layer];
@@ -631,8 +628,7 @@ int coco_block_select(coco_layer_t H, const int8_t* summary, const float* scales
                       const int32_t* ctx_lens, int32_t keep_first, int32_t keep_last,
                       int32_t* selected, int32_t n_select, coco_stream_t stream) {
   if (!H) return fail(COCO_EINVAL, "handle is NULL");
-  int rc = check_rows(H, 0, q, q, n_rows, positions, seq_starts, n_seqs, block_table,
-                      ctx_lens);
+  int rc = check_rows(H, 0, q, q, n_rows, seq_starts, n_seqs, block_table, ctx_lens);
   if (rc || n_rows == 0) return rc;
   if (!positions) return fail(COCO_EINVAL, "NULL argument");
   if ((rc = check_select(H, n_rows, summary, scales, num_blocks, keep_first, keep_last, selected,
@@ -658,7 +654,7 @@ int coco_sparse_attention(coco_layer_t H, int32_t layer, const void* q, void* o,
                           const int32_t* block_table, const int32_t* ctx_lens,
                           const int32_t* selected, int32_t n_select, coco_stream_t stream) {
   if (!H) return fail(COCO_EINVAL, "handle is NULL");
-  int rc = check_rows(H, layer, q, o, n_rows, positions, seq_starts, n_seqs, block_table, ctx_lens);
+  int rc = check_rows(H, layer, q, o, n_rows, seq_starts, n_seqs, block_table, ctx_lens);
   if (rc || n_rows == 0) return rc;
   if (!positions || !selected) return fail(COCO_EINVAL, "NULL argument");
   if ((rc = check_sparse_room(H, n_rows, n_select))) return rc;
