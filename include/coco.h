@@ -367,7 +367,7 @@ int coco_tree_reserve(coco_layer_t h, int32_t max_rows, int32_t max_seqs);
  * them). Node j attends every token before the tree, and node i where bit
  * i % 64 of tree_mask[row][i / 64] is set (its path to the root and itself;
  * any other set is taken too). Bits from N on are ignored; N <= 64 mask_words.
- *   q, o [n_rows][Hq][hd], the handle's dtype, q rotated, 16-byte aligned;
+ *   q, o [n_rows][Hq][hd], the handle's dtype, q rotated, 16-byte aligned, apart;
  *   tree_mask [n_rows][mask_words] 64-bit words
  * A row that attends nothing (no prefix, no bit) gives zeros; what it does not
  * attend may hold anything. A row's result does not depend on the other

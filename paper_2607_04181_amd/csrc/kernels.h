@@ -396,7 +396,7 @@ hipError_t launch_sparse_attention_bf16(const uint16_t* q, const uint16_t* k_cac
 // at most kTreeSplitsFew parts where it has at most 128 columns (nodes times
 // query heads of a group), else kTreeSplits; part_o [column parts][128] and
 // part_ml [column parts][2] hold part_cap = tree_column_parts, plan [n_seqs][2];
-// redo [16 + n_rows * Hq] (items drawn per XCD, two kinds; rows to compute again) must be
+// redo [16 + n_rows * Hq] (items drawn per XCD, two kinds; rows with non-finite values) must be
 // zero and is left so.
 constexpr int kTreeSplitsFew = 32, kTreeSplits = 16;
 constexpr int kTreeLaunchSeqs = 704;  // sequences of a launch; more take several

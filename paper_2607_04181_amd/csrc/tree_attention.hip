@@ -128,7 +128,7 @@ struct TreeArgs {
   int64_t part_cap; // column parts they hold
   int32_t* plan;    // [n_seqs][2]: first column part, parts
   int32_t* drawn;   // items drawn (zero between calls)
-  int32_t* redo;    // [rows * Hq]: rows to compute again (zero between calls)
+  int32_t* redo;    // [rows * Hq]: rows with non-finite values to add (zero between calls)
 };
 
 // Where a lane's run of four dims goes that starts at value v (a multiple of 4)
@@ -763,9 +763,11 @@ __global__ __launch_bounds__(32 * kMergeHeads) void tree_combine_kernel(TreeArgs
   int32_t* redo = a.redo + (int64_t)row * a.Hq + head;
   const bool again = *redo != 0;
   if (splits <= 1 && !again) return;
-  float M = -INFINITY, L = 0.f;
+  const int cc = head * HD + dim;
+  bf16_t* out = a.o + (a.tiled ? tile_off(row, cc, a.Hq * HD) : (int64_t)row * a.Hq * HD + cc);
   f32x4_t y = {0.f, 0.f, 0.f, 0.f};
-  if (!again) {
+  if (splits > 1) {
+    float M = -INFINITY, L = 0.f;
     const int64_t idx =
         a.plan[2 * s] + ((int64_t)(row - a.rk.seq_starts[s]) * a.Hq + head) * splits;
     if (idx + splits > a.part_cap) return;  // (as the parts' kernel)
@@ -797,44 +799,48 @@ __global__ __launch_bounds__(32 * kMergeHeads) void tree_combine_kernel(TreeArgs
       }
       M = m_new;
     }
-  } else {
-    // A row that sees a non-finite value among the nodes: key by key.
+    y *= L == 0.f ? 0.f : 1.0f / L;
+  } else {  // (again: the parts' kernel wrote the row)
+    const u32x2_t w = *(const u32x2_t*)out;
+    y = f32x4_t{bf16_to_f32(w.x & 0xFFFFu), bf16_to_f32(w.x >> 16), bf16_to_f32(w.y & 0xFFFFu),
+                bf16_to_f32(w.y >> 16)};
+  }
+  if (again) {
+    // The row sees non-finite values in the stages that hold nodes, which left
+    // them out for the sake of the columns that do not see their key. Whatever
+    // its weight, such a value is the sum; a weight of 0 (a score of -inf) times
+    // it is NaN.
     const TreeSeq ts = tree_plan(a.rk.seq_starts, a.rk.ctx_lens, s, a.Hq / a.Hkv, a.rk.max_blocks);
     const int g = head / (a.Hq / a.Hkv), prefix = ts.len - ts.nodes;
     const int32_t* bt = a.rk.block_table + (int64_t)s * a.rk.max_blocks;
     const uint64_t* mask = a.rk.mask + (int64_t)row * a.rk.words;
-    float qv[4];
-#pragma unroll
-    for (int r = 0; r < 4; ++r)
-      qv[r] = bf16_to_f32(a.q[((int64_t)row * a.Hq + head) * HD + dim + r]);
-    for (int t = 0; t < ts.len; ++t) {
+    for (int t = max(prefix, 0) / kStKeys * kStKeys; t < ts.len; ++t) {
       if (!(tree_bits32(mask, a.rk.words, ts.nodes, t - prefix) & 1)) continue;
       const int64_t id = bt[t / kBlockTokens];
       const int64_t blk = id < 0 ? 0 : id >= a.rk.num_blocks ? a.rk.num_blocks - 1 : id;
       const int64_t tile = (blk * a.Hkv + g) * kTile;
+      float v[4];
+      bool odd = false;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        v[r] = bf16_to_f32(a.v_cache[tile + v_tile_offset(t % kBlockTokens, dim + r)]);
+        odd |= !__builtin_isfinite(v[r]);
+      }
+      if ((uint32_t)(__ballot(odd) >> (threadIdx.x & 32)) == 0) continue;  // (this head's lanes)
       float z = 0.f;
 #pragma unroll
       for (int r = 0; r < 4; ++r)
-        z = fmaf(qv[r], bf16_to_f32(a.k_cache[tile + k_tile_offset(t % kBlockTokens, dim + r)]), z);
+        z = fmaf(bf16_to_f32(a.q[((int64_t)row * a.Hq + head) * HD + dim + r]),
+                 bf16_to_f32(a.k_cache[tile + k_tile_offset(t % kBlockTokens, dim + r)]), z);
 #pragma unroll
       for (int d = 16; d > 0; d >>= 1) z += __shfl_xor(z, d, kWave);
-      z *= a.scale_log2;
-      const float m_new = fmaxf(M, z);
-      const float ref = m_new == -INFINITY ? 0.f : m_new;
-      const float alpha = __builtin_amdgcn_exp2f(M - ref), p = __builtin_amdgcn_exp2f(z - ref);
-      L = fmaf(L, alpha, p);
 #pragma unroll
       for (int r = 0; r < 4; ++r)
-        y[r] = fmaf(p, bf16_to_f32(a.v_cache[tile + v_tile_offset(t % kBlockTokens, dim + r)]),
-                    y[r] * alpha);
-      M = m_new;
+        if (!__builtin_isfinite(v[r])) y[r] += z == -INFINITY ? 0.f * v[r] : v[r];
     }
     if (dim == 0) *redo = 0;
   }
-  const float inv = L == 0.f ? 0.f : 1.0f / L;
-  const int cc = head * HD + dim;
-  bf16_t* out = a.o + (a.tiled ? tile_off(row, cc, a.Hq * HD) : (int64_t)row * a.Hq * HD + cc);
-  store4(out, y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv);
+  store4(out, y[0], y[1], y[2], y[3]);
 }
 
 }  // namespace
