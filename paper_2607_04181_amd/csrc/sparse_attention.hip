@@ -12,8 +12,10 @@
 // group: they are the 16 columns of a 16x16 tile (up to 16 - G of them idle),
 // S = K Q^T with K as it lies in the tile, and O^T += V^T P^T with V as it lies
 // and P^T as S leaves it in the registers (lane (c, j) holds head c's tokens
-// 4 j .. + 3), rounded to bf16: a weight relative to about its largest, half a
-// step off.
+// 4 j .. + 3). P goes in as the sum of two bf16 parts, 2^-16 of a weight off: the
+// cache's bytes bound the kernel, and the second product costs 0.4% (96 rows of
+// 128 blocks, summaries and choice included: 208.4 and 209.2 us; error against 64
+// bits 2.3e-3 with one part, 1.7e-3 with two, which is the output's rounding).
 #include <math.h>
 
 #include "common.h"
@@ -138,14 +140,22 @@ __global__ __launch_bounds__(64 * kWaves, 3) void sparse_attention_kernel(Sparse
 #pragma unroll
     for (int r = 0; r < 4; ++r) p[r] = __builtin_amdgcn_exp2f(fmaf(z[r], a.scale_log2, -ref));
     l += (p[0] + p[1]) + (p[2] + p[3]);
-    const s16x4_t pb = __builtin_bit_cast(
-        s16x4_t, u32x2_t{pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3])});
+    const u32x2_t high = {pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3])};
+    const auto rest = [](float a, float b, uint32_t h) {  // what the first parts leave
+      return pack_bf16x2(a - __uint_as_float(h << 16), b - __uint_as_float(h & 0xFFFF0000u));
+    };
+    const u32x2_t low = {rest(p[0], p[1], high.x), rest(p[2], p[3], high.y)};
 #pragma unroll
-    for (int x = 0; x < 4; ++x) {
-      acc[2 * x] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(
-          __builtin_bit_cast(s16x4_t, u32x2_t{t.v[x][0], t.v[x][1]}), pb, acc[2 * x], 0, 0, 0);
-      acc[2 * x + 1] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(
-          __builtin_bit_cast(s16x4_t, u32x2_t{t.v[x][2], t.v[x][3]}), pb, acc[2 * x + 1], 0, 0, 0);
+    for (int part = 0; part < 2; ++part) {
+      const s16x4_t pb = __builtin_bit_cast(s16x4_t, part == 0 ? high : low);
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        acc[2 * x] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(
+            __builtin_bit_cast(s16x4_t, u32x2_t{t.v[x][0], t.v[x][1]}), pb, acc[2 * x], 0, 0, 0);
+        acc[2 * x + 1] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(
+            __builtin_bit_cast(s16x4_t, u32x2_t{t.v[x][2], t.v[x][3]}), pb, acc[2 * x + 1], 0, 0,
+            0);
+      }
     }
   };
 

@@ -1,0 +1,58 @@
+"""The weights of sparse attention where their differences are the result."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2607_04181_amd as coco
+from cache_ref import B, Cache, i32
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dtype,hq,hkv,hd", [("bf16", 8, 2, 128), ("bf16", 16, 1, 128),
+                                             ("f32", 4, 2, 64)])
+@pytest.mark.parametrize("keys", [2, 200, 600])
+def test_opposite_values(dtype, hq, hkv, hd, keys):
+    """Values +1 and -1 in turn: a row's result is the difference of two halves of
+    the weights. A score is off by at most (hd + 4) fp32 half steps of the sum of its
+    terms' sizes, a weight by twice that, four half steps of its exponential and, in
+    bf16 handles, 2^-16 (two parts of 8 bits: the second's half step of what the
+    first's leaves), the sums by keys + 32 half steps, the result by its rounding.
+    Weights rounded to bf16 once fail it where there are two keys (of N such errors
+    1 / sqrt(N) is left)."""
+    rng = np.random.default_rng(keys)
+    rows, nb = 24, -(-keys // B)
+    c = Cache(dtype, hq, hkv, hd, rows * nb, nb, max_rows=rows, max_seqs=rows, seed=keys)
+    table = rng.permutation(rows * nb).reshape(rows, nb)
+    _, v = c.tokens()
+    v[:] = np.where(np.arange(B) % 2 == 0, 1.0, -1.0)[None, :, None, None]
+    k, _ = c.tokens()
+    c.put(0, k, v)
+    q = c.normal(rows, hq, hd, sigma=0.7)
+    o = torch.empty_like(q)
+    sel = i32(np.broadcast_to(np.arange(nb), (rows, hkv, nb)))
+    coco.coco_sparse_reserve(c.h, rows, nb)
+    coco.coco_sparse_attention(c.h, 0, q, o, i32(np.full(rows, keys - 1)), None, i32(table),
+                               i32(np.full(rows, keys)), sel)
+    got, q = o.cpu().double().numpy(), q.cpu().double().numpy()
+    f, worst = 2.0 ** -24, 0.0
+    for r in range(rows):
+        at = np.arange(keys)
+        kk = k[table[r, at // B], at % B]
+        for h in range(hq):
+            kh = kk[:, h // (hq // hkv)]
+            z = kh @ q[r, h] / math.sqrt(hd)
+            size = (np.abs(kh) @ np.abs(q[r, h])).max() / math.sqrt(hd)
+            p = np.exp(z - z.max())
+            want = (p / p.sum()) @ np.where(at % 2 == 0, 1.0, -1.0)
+            w = 2 * (hd + 4) * f * size + 4 * f + (2.0 ** -16 if dtype == "bf16" else 0.0)
+            tol = (2 * w + 2 * (keys + 32) * f) * 1.01 + abs(want) * (2.0 ** -8 if dtype == "bf16" else f)
+            off = np.abs(got[r, h] - want).max()
+            assert off <= tol, (r, h, want, off / tol)
+            if dtype == "bf16":  # the weights rounded once, by the formula
+                cut = torch.from_numpy(p).bfloat16().double().numpy()
+                once = (cut / p.sum()) @ np.where(at % 2 == 0, 1.0, -1.0)
+                worst = max(worst, abs(once - want) / tol)
+    assert dtype != "bf16" or keys > 2 or worst > 2
