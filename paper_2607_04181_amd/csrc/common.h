@@ -30,6 +30,12 @@ __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2_t{lo, hi}, bf16x2_t));
 }
 
+// What pack_bf16x2(lo, hi) = high leaves of the two, rounded itself: the two parts'
+// sum is 2^-16 of a value off.
+__device__ __forceinline__ uint32_t pack_rest(float lo, float hi, uint32_t high) {
+  return pack_bf16x2(lo - __uint_as_float(high << 16), hi - __uint_as_float(high & 0xFFFF0000u));
+}
+
 __device__ __forceinline__ uint32_t f32_to_bf16(float f) { return pack_bf16x2(f, 0.f) & 0xFFFFu; }
 
 // SwiGLU's product silu(g) u = g u / (1 + e^-g), with the hardware 2^x

@@ -141,10 +141,7 @@ __global__ __launch_bounds__(64 * kWaves, 3) void sparse_attention_kernel(Sparse
     for (int r = 0; r < 4; ++r) p[r] = __builtin_amdgcn_exp2f(fmaf(z[r], a.scale_log2, -ref));
     l += (p[0] + p[1]) + (p[2] + p[3]);
     const u32x2_t high = {pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3])};
-    const auto rest = [](float a, float b, uint32_t h) {  // what the first parts leave
-      return pack_bf16x2(a - __uint_as_float(h << 16), b - __uint_as_float(h & 0xFFFF0000u));
-    };
-    const u32x2_t low = {rest(p[0], p[1], high.x), rest(p[2], p[3], high.y)};
+    const u32x2_t low = {pack_rest(p[0], p[1], high.x), pack_rest(p[2], p[3], high.y)};
 #pragma unroll
     for (int part = 0; part < 2; ++part) {
       const s16x4_t pb = __builtin_bit_cast(s16x4_t, part == 0 ? high : low);

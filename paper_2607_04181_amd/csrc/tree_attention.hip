@@ -11,6 +11,13 @@
 // of four keys, two dims side by side, so that two 16-byte reads give the
 // operands of two products (dims h and h + 16) for 16 keys.
 //
+// P is rounded to bf16 for the second product, as the layers' attention does: half
+// a step of a weight (2^-9 on average), its sums in fp32. A second product with
+// what that leaves (as trees of few columns have it below) takes the error against
+// 64 bits from 2.3e-3 to the plain form's 1.7e-3, and 32 trees of up to 64 nodes on
+// 64 query heads from 353 us to 412, one of 61 from 98 to 118, 64 of 26 from 207 to
+// 212: many columns are bound by products.
+//
 // A workgroup is four waves with 128 columns (a column tile); two workgroups
 // per CU. They share the keys through LDS, 32 at a time, in a ring of four
 // stages with three on their way: what a tile of few columns is bound by is the
@@ -261,7 +268,7 @@ __device__ __forceinline__ void tree_values(Cols& c, const u32x4_t v[2][2][2],
 //   S[16 keys][16 cols] = K Q^T    4 x mfma 16x16x32
 //   O^T[hd][16 cols] += V^T P^T    8 x mfma 16x16x16
 // P comes out as the operand of the second (lane (c, j4): keys 4 j4 .. + 3 of
-// column c); the waves' results meet in LDS in wave order. One token over 1k keys
+// column c), in two bf16 parts; the waves' results meet in LDS in wave order. One token over 1k keys
 // takes 11.9 us with the merge, through the ring 13.7; 64 trees of 4 nodes over
 // 4k keys 289 (4.7 TB/s) and 325. (32 columns, two tiles, spill registers in
 // this kernel and lose at 64 trees what they gain at one.)
@@ -375,13 +382,17 @@ __device__ __forceinline__ void few_columns(const TreeArgs& a, const TreeSeq& ts
 #pragma unroll
     for (int r = 0; r < 4; ++r) p[r] = __builtin_amdgcn_exp2f(fmaf(z[r], a.scale_log2, -ref));
     l += (p[0] + p[1]) + (p[2] + p[3]);
-    const s16x4_t pb = __builtin_bit_cast(
-        s16x4_t, u32x2_t{pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3])});
+    const u32x2_t high = {pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3])};
+    const u32x2_t low = {pack_rest(p[0], p[1], high.x), pack_rest(p[2], p[3], high.y)};
 #pragma unroll
-    for (int x = 0; x < 8; ++x)
-      acc[x] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(
-          __builtin_bit_cast(s16x4_t, u32x2_t{t.v[x / 2][x % 2 * 2], t.v[x / 2][x % 2 * 2 + 1]}),
-          pb, acc[x], 0, 0, 0);
+    for (int part = 0; part < 2; ++part) {
+      const s16x4_t pb = __builtin_bit_cast(s16x4_t, part == 0 ? high : low);
+#pragma unroll
+      for (int x = 0; x < 8; ++x)
+        acc[x] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(
+            __builtin_bit_cast(s16x4_t, u32x2_t{t.v[x / 2][x % 2 * 2], t.v[x / 2][x % 2 * 2 + 1]}),
+            pb, acc[x], 0, 0, 0);
+    }
   };
 #pragma unroll 1
   for (int j = 0; j < mine; j += 3) {

@@ -1,4 +1,5 @@
-"""The weights of sparse attention where their differences are the result."""
+"""The weights of sparse attention, and of trees of few columns, where their
+differences are the result."""
 import math
 
 import numpy as np
@@ -14,7 +15,8 @@ pytestmark = pytest.mark.gpu
 @pytest.mark.parametrize("dtype,hq,hkv,hd", [("bf16", 8, 2, 128), ("bf16", 16, 1, 128),
                                              ("f32", 4, 2, 64)])
 @pytest.mark.parametrize("keys", [2, 200, 600])
-def test_opposite_values(dtype, hq, hkv, hd, keys):
+@pytest.mark.parametrize("tree", [False, True])
+def test_opposite_values(dtype, hq, hkv, hd, keys, tree):
     """Values +1 and -1 in turn: a row's result is the difference of two halves of
     the weights. A score is off by at most (hd + 4) fp32 half steps of the sum of its
     terms' sizes, a weight by twice that, four half steps of its exponential and, in
@@ -32,10 +34,15 @@ def test_opposite_values(dtype, hq, hkv, hd, keys):
     c.put(0, k, v)
     q = c.normal(rows, hq, hd, sigma=0.7)
     o = torch.empty_like(q)
-    sel = i32(np.broadcast_to(np.arange(nb), (rows, hkv, nb)))
-    coco.coco_sparse_reserve(c.h, rows, nb)
-    coco.coco_sparse_attention(c.h, 0, q, o, i32(np.full(rows, keys - 1)), None, i32(table),
-                               i32(np.full(rows, keys)), sel)
+    ctx = i32(np.full(rows, keys))
+    if tree:  # one node of its own each
+        coco.coco_tree_reserve(c.h, rows, rows)
+        coco.coco_tree_attention(c.h, 0, q, o, i32(np.arange(rows + 1)), i32(table), ctx,
+                                 torch.ones(rows, 1, dtype=torch.int64, device="cuda"))
+    else:
+        sel = i32(np.broadcast_to(np.arange(nb), (rows, hkv, nb)))
+        coco.coco_sparse_reserve(c.h, rows, nb)
+        coco.coco_sparse_attention(c.h, 0, q, o, ctx - 1, None, i32(table), ctx, sel)
     got, q = o.cpu().double().numpy(), q.cpu().double().numpy()
     f, worst = 2.0 ** -24, 0.0
     for r in range(rows):
