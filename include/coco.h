@@ -369,6 +369,9 @@ int coco_tree_reserve(coco_layer_t h, int32_t max_rows, int32_t max_seqs);
  * any other set is taken too). Bits from N on are ignored; N <= 64 mask_words.
  *   q, o [n_rows][Hq][hd], the handle's dtype, q rotated, 16-byte aligned, apart;
  *   tree_mask [n_rows][mask_words] 64-bit words
+ * (bf16: the softmax weights of a tree with more than 16 nodes times query heads
+ * per key/value head are rounded to bf16 for their product with the values, as in
+ * the layers; smaller trees' and those of coco_sparse_attention keep 16 bits.)
  * A row that attends nothing (no prefix, no bit) gives zeros; what it does not
  * attend may hold anything. A row's result does not depend on the other
  * sequences of the call; rows from seq_starts[n_seqs] on (a padded call) are

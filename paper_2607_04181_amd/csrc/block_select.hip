@@ -4,8 +4,10 @@
 // The summary of a (block, kv head) is the largest and the smallest value of
 // its keys in every dimension, as bytes against a power of two 2^(x - 7) with
 // max(|hi|, |lo|) < 2^x (x held within +-100): hi rounded up, lo down, so that
-// the bytes still enclose the keys. For a query q, sum_d max(q_d hi_d, q_d
-// lo_d) bounds q . k over the block's keys, and is the inner product of
+// the bytes still enclose the keys, but for what is held within +-127: elements
+// above 127/128 of 2^x (or of 2^100), by less than a step of the bytes (below 2^100).
+// For a query q, sum_d max(q_d hi_d, q_d lo_d) then bounds q . k over the block's
+// keys, or falls short of it by that little, and is the inner product of
 // [max(q, 0), min(q, 0)] with [hi, lo]: with q in bytes of its own power of two,
 // one int8 matrix product of 2 hd terms per block and head. A sum is a whole
 // number below 2^23, times 2^(x - 7) exactly a float: the scores, and with them

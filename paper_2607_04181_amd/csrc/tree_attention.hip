@@ -25,12 +25,15 @@
 // LDS, reached 2.7 TB/s on 64 sequences of 4 nodes and 4k keys; this 4.2, of the
 // 4.9 of a large copy.) Many columns are bound by products and softmax, which
 // take about as long each and of which the two waves of a SIMD, in different
-// workgroups, overlap about a third: 480 TFLOP/s for 32 trees of up to 64
-// nodes, merge included, of the 1150 of a large bf16 product. (Scheduling by
-// hand or priorities around the products changed it by less than 3%; 64 columns
-// per wave, which would halve the operand reads, need more than the 512
-// registers of a wave alone on its SIMD.) The column tiles of the same keys run
-// at the same time on one XCD and read them from its L2.
+// workgroups, overlap about a third: 555 TFLOP/s for 32 trees of up to 64
+// nodes, merge included, of the 1650 of a large bf16 product. (Scheduling by
+// hand or priorities around the products changed it by less than 3%. 64 columns
+// per wave, one wave to a SIMD, would halve the operand reads; as written once, the
+// compiler took all 512 registers and spilled 63 of them and 313 scalar ones, and
+// it was not taken further. This kernel spills 191 scalar registers to lanes of
+// vector ones, none of them between the products of a stage that every column
+// sees whole.) The column tiles of the same keys run at the same time on one XCD
+// and read them from its L2.
 //
 // The keys of a sequence are split into parts (tree_part) that depend on its
 // own length and columns only, merged by a second kernel in order: a row's
@@ -269,9 +272,10 @@ __device__ __forceinline__ void tree_values(Cols& c, const u32x4_t v[2][2][2],
 //   O^T[hd][16 cols] += V^T P^T    8 x mfma 16x16x16
 // P comes out as the operand of the second (lane (c, j4): keys 4 j4 .. + 3 of
 // column c), in two bf16 parts; the waves' results meet in LDS in wave order. One token over 1k keys
-// takes 11.9 us with the merge, through the ring 13.7; 64 trees of 4 nodes over
-// 4k keys 289 (4.7 TB/s) and 325. (32 columns, two tiles, spill registers in
-// this kernel and lose at 64 trees what they gain at one.)
+// takes 10.9 us with the merge (calls replayed from a graph), through the ring
+// 15.8; over 16k 24.1 and 33.5; 64 trees of 4 nodes over 4k keys 225 (4.8 TB/s) and
+// 226. (32 columns, two tiles, spill registers in this kernel and lose at 64
+// trees what they gain at one.)
 struct FewTile {
   u32x4_t k[4], v[4];
 };
@@ -753,8 +757,8 @@ __global__ __launch_bounds__(kThreads, 2) void tree_attention_kernel(TreeArgs a)
 }
 
 // The parts of a row's heads, in order: four dims per thread, 32 threads per
-// head, four heads per workgroup (eight: one token 15.4 us with the merge
-// instead of 13.8, 32 trees of 64 nodes 519 instead of 506).
+// head, four heads per workgroup (eight: one token 1.6 us more, 32 trees of 64
+// nodes 13).
 constexpr int kMergeHeads = 4;
 __global__ __launch_bounds__(32 * kMergeHeads) void tree_combine_kernel(TreeArgs a) {
   if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x < 2 * kXCDs) a.drawn[threadIdx.x] = 0;
