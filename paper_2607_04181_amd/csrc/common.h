@@ -30,10 +30,16 @@ __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2_t{lo, hi}, bf16x2_t));
 }
 
-// What pack_bf16x2(lo, hi) = high leaves of the two, rounded itself: the two parts'
-// sum is 2^-16 of a value off.
-__device__ __forceinline__ uint32_t pack_rest(float lo, float hi, uint32_t high) {
-  return pack_bf16x2(lo - __uint_as_float(high << 16), hi - __uint_as_float(high & 0xFFFF0000u));
+// Two weights (>= 0) as the sums of two bf16 parts, 2^-16 off: their first 8 bits,
+// and what those leave, rounded, which is kept above 0 where the weight is (2^-126 at
+// least): either part times an infinite value is that infinity, not NaN, and a
+// weight of 0 has parts of 0.
+__device__ __forceinline__ u32x2_t pack_two_parts(float lo, float hi) {
+  const uint32_t a = __float_as_uint(lo) & 0xFFFF0000u, b = __float_as_uint(hi) & 0xFFFF0000u;
+  const float least = 0x1p-126f;
+  return u32x2_t{a >> 16 | b,
+                 pack_bf16x2(__builtin_amdgcn_fmed3f(lo - __uint_as_float(a), least, lo),
+                             __builtin_amdgcn_fmed3f(hi - __uint_as_float(b), least, hi))};
 }
 
 __device__ __forceinline__ uint32_t f32_to_bf16(float f) { return pack_bf16x2(f, 0.f) & 0xFFFFu; }

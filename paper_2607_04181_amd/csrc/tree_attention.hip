@@ -386,11 +386,10 @@ __device__ __forceinline__ void few_columns(const TreeArgs& a, const TreeSeq& ts
 #pragma unroll
     for (int r = 0; r < 4; ++r) p[r] = __builtin_amdgcn_exp2f(fmaf(z[r], a.scale_log2, -ref));
     l += (p[0] + p[1]) + (p[2] + p[3]);
-    const u32x2_t high = {pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3])};
-    const u32x2_t low = {pack_rest(p[0], p[1], high.x), pack_rest(p[2], p[3], high.y)};
+    const u32x2_t p01 = pack_two_parts(p[0], p[1]), p23 = pack_two_parts(p[2], p[3]);
 #pragma unroll
     for (int part = 0; part < 2; ++part) {
-      const s16x4_t pb = __builtin_bit_cast(s16x4_t, part == 0 ? high : low);
+      const s16x4_t pb = __builtin_bit_cast(s16x4_t, u32x2_t{p01[part], p23[part]});
 #pragma unroll
       for (int x = 0; x < 8; ++x)
         acc[x] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(

@@ -63,3 +63,62 @@ def test_opposite_values(dtype, hq, hkv, hd, keys, tree):
                 once = (cut / p.sum()) @ np.where(at % 2 == 0, 1.0, -1.0)
                 worst = max(worst, abs(once - want) / tol)
     assert dtype != "bf16" or keys > 2 or worst > 2
+
+
+@pytest.mark.parametrize("dtype,hq,hkv,hd", [("bf16", 8, 2, 128), ("bf16", 16, 1, 128),
+                                             ("f32", 4, 2, 64)])
+@pytest.mark.parametrize("tree", [False, True])
+def test_infinite_values_come_out(dtype, hq, hkv, hd, tree):
+    """A seen value that is infinite is the result in its sign, whatever the key's
+    weight (also the largest, an exact power of two); NaN is NaN; the other
+    dimensions, and keys that a row does not see, are as without."""
+    rng = np.random.default_rng(51)
+    lens = [40, 700, 16, 33, 1100]
+    nb = [-(-n // B) for n in lens]
+    c = Cache(dtype, hq, hkv, hd, sum(nb) + 1, max(nb), max_rows=5, max_seqs=5, seed=51)
+    at = np.concatenate([[0], np.cumsum(nb)])
+    perm = rng.permutation(sum(nb) + 1)
+    table = np.full((5, max(nb)), -1, np.int64)
+    for s in range(5):
+        table[s, :nb[s]] = perm[at[s]:at[s + 1]]
+    k, v = c.tokens()
+    q = c.normal(5, hq, hd)
+    ctx = i32(lens)
+    if tree:
+        coco.coco_tree_reserve(c.h, 5, 5)
+    else:
+        sel = np.full((5, hkv, max(nb)), -1)
+        for s in range(5):
+            sel[s, :, :nb[s]] = np.arange(nb[s])
+        coco.coco_sparse_reserve(c.h, 5, max(nb))
+
+    def run(values):
+        c.put(0, k, values)
+        o = torch.empty_like(q)
+        if tree:
+            coco.coco_tree_attention(c.h, 0, q, o, i32(np.arange(6)), i32(table), ctx,
+                                     torch.ones(5, 1, dtype=torch.int64, device="cuda"))
+        else:
+            coco.coco_sparse_attention(c.h, 0, q, o, ctx - 1, None, i32(table), ctx, i32(sel))
+        return o.cpu().double().numpy()
+
+    clean = run(v)
+    q64 = q.cpu().double().numpy()
+    bad, want = v.copy(), {}
+    for s, n in enumerate(lens):
+        first = k[table[s, np.arange(n) // B], np.arange(n) % B]
+        top = int((first[:, 0] @ q64[s, 0]).argmax())  # the largest weight of head 0
+        for dim, t, x in ((3, top, np.inf), (4, 0, -np.inf), (5, n - 1, np.inf), (6, n // 2, np.nan),
+                          (7, top, -np.inf), (17, min(15, n - 1), np.inf), (30, n - 1, -np.inf)):
+            bad[table[s, t // B], t % B, :, dim] = x
+            want[s, dim] = x
+        if n % B:  # a slot behind the row's keys
+            bad[table[s, n // B], n % B] = np.inf
+    got = run(bad)
+    for (s, dim), x in want.items():
+        g = got[s, :, dim]
+        assert (np.isnan(g) if x != x else g == x).all(), (s, dim, x, g)
+    odd = np.zeros(got.shape, bool)
+    for s, dim in want:
+        odd[s, :, dim] = True
+    assert np.array_equal(got[~odd], clean[~odd])
