@@ -258,8 +258,8 @@ int coco_layer_workspace(coco_layer_t h, int32_t which, void* dst, int64_t dst_b
 
 /* Per-kernel timing for benchmarks (calls of any handle are unaffected while
  * it is off; kinds whose work runs inside another kernel count no launches).
- * When on, every kernel launched by coco_layer_forward and the span, tree and
- * sparse forwards on this handle is launched with a pair of HIP events
+ * When on, every kernel launched by coco_layer_forward and the span, tree, sparse
+ * and window forwards on this handle is launched with a pair of HIP events
  * (hipExtLaunchKernelGGL) that the runtime timestamps at the kernel's own
  * start and end, from a pool of events created here (so switching it on
  * allocates; timed calls themselves do not). Switch it off before capturing
@@ -269,7 +269,8 @@ enum {
   COCO_K_GEMM_QKV = 1,       /* QKV projection */
   COCO_K_QKV_EPILOGUE = 2,   /* split-K sum + RoPE + cache append */
   COCO_K_ATTENTION = 3,      /* paged attention (decode partitions or prefill); of
-                                trees and selected blocks all kernels, as one launch */
+                                trees, selected blocks and windows all kernels, as one
+                                launch */
   COCO_K_ATTN_COMBINE = 4,   /* decode partition merge */
   COCO_K_GEMM_O = 5,         /* O projection */
   COCO_K_RESIDUAL_NORM = 6,  /* residual + RMSNorm_2 */
@@ -344,7 +345,7 @@ int coco_kv_copy(coco_layer_t h, int32_t first_layer, int32_t n_layers, const in
  * position they were computed at), as if every token were read before any is
  * written. kept[kept_starts[i] + k] >= base_lens[i] + k; rows distinct; the
  * blocks from base_lens[i] on must be the row's own (count 1). kept_starts
- * [n + 1] runs from 0 to n_kept. */
+ * [n + 1] runs from 0 to at most n_kept. */
 int coco_kv_compact(coco_layer_t h, int32_t first_layer, int32_t n_layers, const int32_t* seq_idx,
                     const int32_t* base_lens, const int32_t* kept, const int32_t* kept_starts,
                     int32_t n, int32_t n_kept, const int32_t* block_table, int32_t n_seqs,
@@ -461,6 +462,75 @@ int coco_layer_sparse_forward(coco_layer_t h, int32_t layer, void* hidden, int64
                               int8_t* summary, float* scales, int32_t keep_first,
                               int32_t keep_last, int32_t* selected, int32_t n_select,
                               coco_stream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * Attention through a sliding window, and eviction by accumulated weight, for
+ * contexts that outgrow their cache.
+ * ------------------------------------------------------------------------- */
+
+/* Make room for window calls of up to max_rows rows and max_seqs (at most
+ * 65535) sequences, and, with weigh, for their weights (as coco_tree_reserve).
+ * A bf16 handle holds 4 bytes per query head and slot of a block-table row for
+ * each of min(max_rows, max_seqs) sequences then. */
+int coco_window_reserve(coco_layer_t h, int32_t max_rows, int32_t max_seqs, int32_t weigh);
+
+/* Attention of rows over the newest `window` tokens of layer `layer`'s cache and
+ * the first n_sinks, which stay visible. The N call rows seq_starts[s] ..
+ * seq_starts[s+1]-1 of sequence s (NULL: row i is sequence i) are its last
+ * cached tokens: row j has slot p = ctx_lens[s] - N + j and attends slots t <= p
+ * with t > p - window or t < n_sinks (window >= 1; 2147483647: all of them).
+ * Slots count what is cached, wherever its position was: after evictions the
+ * window is over the tokens that are left.
+ *   q, o and rows past the sequences as in coco_tree_attention (bf16: the softmax
+ *   weights of calls without seq_starts keep 16 bits for their product with the
+ *   values, prompts' are rounded to bf16). A row that attends nothing (slot below
+ *   0) gives zeros, what a row does not attend may hold anything, and table
+ *   entries that no row of a sequence reaches are not read.
+ *   weights [n_seqs][max_blocks_per_seq * 16] fp32, 16-byte aligned, or NULL:
+ *   weights[s][t] grows by the softmax weights of slot t, added up over the rows of
+ *   sequence s and the query heads (in fp32, in a fixed order); other places are
+ *   left as they are.
+ * A sequence's results do not depend on the others of the call; how its rows are
+ * spread over calls changes their rounding. Needs coco_window_reserve (COCO_ESTATE
+ * without). */
+int coco_window_attention(coco_layer_t h, int32_t layer, const void* q, void* o, int32_t n_rows,
+                          const int32_t* seq_starts, int32_t n_seqs, const int32_t* block_table,
+                          const int32_t* ctx_lens, int32_t window, int32_t n_sinks, float* weights,
+                          coco_stream_t stream);
+
+/* Layers first_layer .. first_layer + n_layers - 1 as coco_layer_span_forward,
+ * except: a row is cached in its slot (as in coco_window_attention; the pages must
+ * be there), its position is only its rotation (below max_blocks_per_seq * 16 with
+ * seq_starts and bf16; any, without), and it attends as in
+ * coco_window_attention; weights grow by those of every layer. seq_starts[n_seqs]
+ * must be n_rows (as in coco_layer_tree_forward). Needs coco_window_reserve. */
+int coco_layer_window_forward(coco_layer_t h, int32_t first_layer, int32_t n_layers, void* hidden,
+                              int64_t hidden_rows, const int32_t* row_idx, int32_t n_rows,
+                              const int32_t* positions, const int32_t* seq_starts, int32_t n_seqs,
+                              const int32_t* block_table, const int32_t* ctx_lens, int32_t window,
+                              int32_t n_sinks, float* weights, coco_stream_t stream);
+
+/* Choose the tokens that rows of the cache keep. Row s = seq_idx[i], with L =
+ * ctx_lens[s] tokens and B = keep_lens[i] < L, keeps its first keep_first and its
+ * last keep_last tokens (of B at most, the first ones first) and of the others
+ * those of the largest weights[s][t], the lowest slot among equals, B in all; a
+ * NaN counts as the lowest weight, and without weights (NULL) all are equal.
+ * Rows with L <= B keep everything.
+ *   new_lens [n]   B, or L for a row that keeps everything
+ *   base_lens, kept, kept_starts   what coco_kv_compact takes: the first token
+ *                  that goes (L if none does), and the kept ones behind it in
+ *                  order; kept has n_kept places, and those behind
+ *                  kept_starts[n] are left as they are
+ *   weights        move with the tokens; 0 from B to L - 1
+ * The tokens themselves move by coco_kv_compact, and the pages behind new_lens go
+ * by coco_kv_free. Lists are written in order until one does not fit; that row
+ * and those behind it that would list any keep everything. At most max_seqs
+ * requests of distinct rows; rows out of range count as empty. new_lens must not
+ * overlap ctx_lens. */
+int coco_kv_evict(coco_layer_t h, const int32_t* seq_idx, const int32_t* keep_lens, int32_t n,
+                  int32_t keep_first, int32_t keep_last, const int32_t* ctx_lens, float* weights,
+                  int32_t n_seqs, int32_t* new_lens, int32_t* base_lens, int32_t* kept,
+                  int32_t n_kept, int32_t* kept_starts, coco_stream_t stream);
 
 /* Peak probes for benchmarks (not part of the layer): the rates this GPU
  * sustains, against which measured kernels are quoted next to the published

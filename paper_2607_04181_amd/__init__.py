@@ -15,5 +15,6 @@ from ._lib import (  # noqa: F401
     coco_cost_comp, coco_speedup_vec, coco_scale_candidates, coco_kv_alloc, coco_kv_fork,
     coco_kv_free, coco_kv_copy, coco_kv_compact, coco_tree_reserve, coco_tree_attention,
     coco_kv_summarize, coco_sparse_reserve, coco_block_select, coco_sparse_attention,
-    coco_layer_tree_forward, coco_layer_sparse_forward,
+    coco_layer_tree_forward, coco_layer_sparse_forward, coco_window_reserve,
+    coco_window_attention, coco_layer_window_forward, coco_kv_evict,
 )

@@ -18,6 +18,7 @@ LIB_PATH = os.path.join(_HERE, "libcoco.so")
 
 COCO_OK, COCO_EINVAL, COCO_ENOMEM, COCO_EHIP, COCO_ESTATE = 0, -1, -2, -3, -4
 COCO_BF16, COCO_F32 = 0, 1
+BLOCK_TOKENS = 16
 COCO_WS_X, COCO_WS_H, COCO_WS_Q, COCO_WS_O, COCO_WS_X1, COCO_WS_H2, COCO_WS_U = range(7)
 
 EXPORTS = ["coco_layer_init", "coco_layer_destroy", "coco_last_error", "coco_version",
@@ -29,6 +30,8 @@ EXPORTS = ["coco_layer_init", "coco_layer_destroy", "coco_last_error", "coco_ver
            "coco_tree_reserve", "coco_tree_attention", "coco_kv_summarize",
            "coco_sparse_reserve", "coco_block_select", "coco_sparse_attention",
            "coco_layer_tree_forward", "coco_layer_sparse_forward",
+           "coco_window_reserve", "coco_window_attention", "coco_layer_window_forward",
+           "coco_kv_evict",
            # include/coco_scaling.h: host arithmetic of the speedup/cost model
            "coco_split_batch", "coco_comm_time", "coco_speedup", "coco_cost_mem",
            "coco_cost_comp", "coco_speedup_vec", "coco_scale_candidates"]
@@ -112,6 +115,13 @@ def _load():
                                              i32, vp, i32, vp]),
         "coco_sparse_attention": (ctypes.c_int, [vp, i32, vp, vp, i32, vp, vp, i32, vp, vp, vp,
                                                  i32, vp]),
+        "coco_window_reserve": (ctypes.c_int, [vp, i32, i32, i32]),
+        "coco_window_attention": (ctypes.c_int, [vp, i32, vp, vp, i32, vp, i32, vp, vp, i32, i32,
+                                                 vp, vp]),
+        "coco_layer_window_forward": (ctypes.c_int, [vp, i32, i32, vp, i64, vp, i32, vp, vp, i32,
+                                                     vp, vp, i32, i32, vp, vp]),
+        "coco_kv_evict": (ctypes.c_int, [vp, vp, vp, i32, i32, i32, vp, vp, i32, vp, vp, vp, i32,
+                                         vp, vp]),
         "coco_split_batch": (ctypes.c_int, [i64, i32, ctypes.POINTER(i64)]),
         "coco_comm_time": (ctypes.c_double, [ctypes.POINTER(coco_scale_model), i32]),
         "coco_speedup": (ctypes.c_double, [ctypes.POINTER(coco_scale_model), i32, i32]),
@@ -166,7 +176,7 @@ def _stream(stream):
 
 
 def _arg(h, t, dtype, what):
-    """_ptr of a tensor that must be on the handle's device."""
+    """_ptr of a tensor that must be on the handle's device (None: NULL)."""
     if type(t) is torch.Tensor and t.dtype is dtype and t.get_device() == h.device and \
             t.is_contiguous():
         return t.data_ptr()
@@ -576,6 +586,68 @@ def coco_layer_sparse_forward(h: Handle, layer: int, hidden, row_idx, positions,
         _arg(h, summary, torch.int8, "summary"), _arg(h, scales, torch.float32, "scales"),
         keep_first, keep_last, _arg(h, selected, _I32, "selected"), n_select,
         _handle_stream(h, stream)))
+
+
+def coco_window_reserve(h: Handle, max_rows: int, max_seqs: int, weigh: bool = False) -> None:
+    _check(_lib.coco_window_reserve(h.raw, max_rows, max_seqs, 1 if weigh else 0))
+
+
+def _check_weights(h: Handle, weights, n_seqs: int):
+    if weights is not None and not (
+            isinstance(weights, torch.Tensor) and weights.dim() == 2 and
+            weights.shape[0] >= n_seqs and weights.shape[1] == BLOCK_TOKENS * h.width):
+        raise ValueError(f"weights must be [{n_seqs}, {BLOCK_TOKENS * h.width}]")
+
+
+def coco_window_attention(h: Handle, layer: int, q, o, seq_starts, block_table, ctx_lens,
+                          window: int, n_sinks: int, weights=None, stream=None):
+    """seq_starts None: row i is sequence i. weights: fp32 [sequences, slots of a table row]."""
+    n = _check_heads(h, "q", q)
+    _check_out(h, o, n)
+    n_seqs = int(ctx_lens.numel())
+    if seq_starts is not None:
+        _check_len("seq_starts", seq_starts, n_seqs + 1)
+    elif n_seqs != n:
+        raise ValueError(f"ctx_lens has {n_seqs} entries for {n} rows")
+    _check_table(h, block_table, n_seqs)
+    _check_weights(h, weights, n_seqs)
+    _check(_lib.coco_window_attention(
+        h.raw, layer, _arg(h, q, h.elem, "q"), _arg(h, o, h.elem, "o"), n,
+        _arg(h, seq_starts, _I32, "seq_starts"), n_seqs,
+        _arg(h, block_table, _I32, "block_table"), _arg(h, ctx_lens, _I32, "ctx_lens"), window,
+        n_sinks, _arg(h, weights, torch.float32, "weights"), _handle_stream(h, stream)))
+
+
+def coco_layer_window_forward(h: Handle, first_layer: int, n_layers: int, hidden, row_idx,
+                              positions, seq_starts, block_table, ctx_lens, window: int,
+                              n_sinks: int, weights=None, stream=None):
+    _check_batch(h, hidden, row_idx, positions, seq_starts, block_table, ctx_lens)
+    n, n_seqs = int(row_idx.numel()), int(ctx_lens.numel())
+    _check_weights(h, weights, n_seqs)
+    _check(_lib.coco_layer_window_forward(
+        h.raw, first_layer, n_layers, _arg(h, hidden, h.elem, "hidden"), int(hidden.shape[0]),
+        _arg(h, row_idx, _I32, "row_idx"), n, _arg(h, positions, _I32, "positions"),
+        _arg(h, seq_starts, _I32, "seq_starts"), n_seqs, _arg(h, block_table, _I32, "block_table"),
+        _arg(h, ctx_lens, _I32, "ctx_lens"), window, n_sinks,
+        _arg(h, weights, torch.float32, "weights"), _handle_stream(h, stream)))
+
+
+def coco_kv_evict(h: Handle, seq_idx, keep_lens, keep_first: int, keep_last: int, ctx_lens, weights,
+                  new_lens, base_lens, kept, kept_starts, stream=None):
+    """weights None: all alike."""
+    n = int(seq_idx.numel())
+    n_seqs = int(ctx_lens.numel())
+    _check_len("keep_lens", keep_lens, n)
+    _check_len("new_lens", new_lens, n)
+    _check_len("base_lens", base_lens, n)
+    _check_len("kept_starts", kept_starts, n + 1)
+    _check_weights(h, weights, n_seqs)
+    _check(_lib.coco_kv_evict(
+        h.raw, _arg(h, seq_idx, _I32, "seq_idx"), _arg(h, keep_lens, _I32, "keep_lens"), n,
+        keep_first, keep_last, _arg(h, ctx_lens, _I32, "ctx_lens"),
+        _arg(h, weights, torch.float32, "weights"), n_seqs, _arg(h, new_lens, _I32, "new_lens"),
+        _arg(h, base_lens, _I32, "base_lens"), _arg(h, kept, _I32, "kept"), int(kept.numel()),
+        _arg(h, kept_starts, _I32, "kept_starts"), _handle_stream(h, stream)))
 
 
 def coco_layer_workspace(h: Handle, which: int, dst, stream=None) -> None:

@@ -1,6 +1,6 @@
 // fp32 attention of rows that do not see a plain causal prefix of the paged
-// cache: the nodes of a tree of drafted tokens, and rows that attend selected
-// blocks.
+// cache: the nodes of a tree of drafted tokens, rows that attend selected blocks,
+// and rows that see a sliding window and a context's first tokens.
 //
 // One workgroup per row and GH query heads of one key/value head, eight waves
 // striding over the row's blocks with an online softmax each, merged in LDS in
@@ -42,11 +42,14 @@ __device__ __forceinline__ uint32_t tree_bits(const uint64_t* mask, int words, i
   return (uint32_t)v & 0xFFFFu;
 }
 
+enum RowsMode { kRowsTree, kRowsBlocks, kRowsWindow };
+
 // HS: head_dim / 32.
-template <int HS, int GH, bool TREE>
+template <int HS, int GH, RowsMode MODE>
 __global__ __launch_bounds__(64 * kRowsWaves) void attn_rows_kernel(
     const float* __restrict__ q, const float* __restrict__ k_cache,
-    const float* __restrict__ v_cache, RowKeys rk, int Hq, int Hkv, float* __restrict__ o) {
+    const float* __restrict__ v_cache, RowKeys rk, int Hq, int Hkv, float* __restrict__ o,
+    float* __restrict__ stats) {
   constexpr int hd = 32 * HS;
   __shared__ float sm_m[kRowsWaves][GH], sm_l[kRowsWaves][GH];
   __shared__ float sm_o[kRowsWaves][GH][hd];
@@ -63,7 +66,12 @@ __global__ __launch_bounds__(64 * kRowsWaves) void attn_rows_kernel(
   const uint64_t* mask = nullptr;
   const int32_t* list = nullptr;
   int entries;
-  if constexpr (TREE) {
+  WindowList win{};
+  if constexpr (MODE == kRowsWindow) {
+    n = min(max(rk.ctx_lens[s], 0), rk.max_blocks * kBlockTokens);
+    if (rk.seq_starts != nullptr) n = max(n + i + 1 - rk.seq_starts[s + 1], 0);
+    win = window_list(n - 1, n - 1, rk.window, rk.sinks);
+  } else if constexpr (MODE == kRowsTree) {
     n = rk.ctx_lens[s];
     nodes = rk.seq_starts[s + 1] - rk.seq_starts[s];
     prefix = n - nodes;
@@ -74,7 +82,7 @@ __global__ __launch_bounds__(64 * kRowsWaves) void attn_rows_kernel(
   }
   n = min(max(n, 0), rk.max_blocks * kBlockTokens);
   const int blocks = (n + kBlockTokens - 1) / kBlockTokens;
-  entries = TREE ? blocks : rk.top;
+  entries = MODE == kRowsTree ? blocks : MODE == kRowsBlocks ? rk.top : win.entries;
   const int32_t* bt = rk.block_table + (int64_t)s * rk.max_blocks;
   // Scores in powers of two: 2^x is one instruction, within 1 ulp.
   const float scale_log2 = 1.4426950408889634f / sqrtf((float)hd);
@@ -104,7 +112,8 @@ __global__ __launch_bounds__(64 * kRowsWaves) void attn_rows_kernel(
     if (x % kWave == 0) {
       const int mine = wv + (x + lane) * kRowsWaves;
       b_l = -1;
-      if (mine < entries) b_l = TREE ? mine : list[mine];
+      if (mine < entries)
+        b_l = MODE == kRowsTree ? mine : MODE == kRowsBlocks ? list[mine] : win.block(mine);
       if (b_l >= blocks) b_l = -1;
       if (b_l >= 0) blk_l = readable_block(bt[b_l], rk.num_blocks);
     }
@@ -112,9 +121,11 @@ __global__ __launch_bounds__(64 * kRowsWaves) void attn_rows_kernel(
     if (b < 0) continue;
     const int tok0 = b * kBlockTokens;
     uint32_t seen;
-    if constexpr (TREE) {
+    if constexpr (MODE == kRowsTree) {
       seen = tree_bits(mask, rk.words, nodes, tok0 - prefix);
       if (seen == 0) continue;
+    } else if constexpr (MODE == kRowsWindow) {
+      seen = window_bits(tok0, n - 1, rk.window, rk.sinks);
     } else {
       seen = n - tok0 < 16 ? (1u << (n - tok0)) - 1 : 0xFFFFu;
     }
@@ -195,6 +206,11 @@ __global__ __launch_bounds__(64 * kRowsWaves) void attn_rows_kernel(
       L = fmaf(f, sm_l[w][e], L);
     }
     o[((int64_t)i * Hq + h0 + e) * hd + dim] = L == 0.f ? 0.f : a / L;
+    if (MODE == kRowsWindow && stats != nullptr && dim == 0) {
+      float* to = stats + ((int64_t)i * Hq + h0 + e) * 2;
+      to[0] = ref;
+      to[1] = L == 0.f ? 0.f : 1.0f / L;
+    }
   }
 }
 
@@ -202,7 +218,7 @@ __global__ __launch_bounds__(64 * kRowsWaves) void attn_rows_kernel(
 
 hipError_t launch_attn_rows_f32(const float* q, const float* k_cache, const float* v_cache,
                                 const RowKeys& rk, int n_rows, int Hq, int Hkv, int hd, float* o,
-                                int num_cus, hipStream_t st) {
+                                int num_cus, hipStream_t st, float* stats) {
   if (n_rows <= 0) return hipSuccess;
   // Heads per workgroup: they share the key/value loads; the queries they
   // keep in registers (hd / 4 floats per lane each) bound their number. Fewer of
@@ -213,14 +229,17 @@ hipError_t launch_attn_rows_f32(const float* q, const float* k_cache, const floa
   int gh = (G % 4 == 0 && hd <= 64) ? 4 : (G % 2 == 0 && hd <= 128) ? 2 : 1;
   while (gh > 1 && (int64_t)n_rows * (Hq / gh) < num_cus) gh /= 2;
   const dim3 grid(n_rows, Hq / gh), block(64 * kRowsWaves);
+#define COCO_ROWS_MODE(HS, GH, MODE)                                                            \
+  COCO_LAUNCH_LAST((attn_rows_kernel<HS, GH, MODE>), grid, block, 0, st, q, k_cache, v_cache,   \
+                   rk, Hq, Hkv, o, stats)
 #define COCO_ROWS(HS, GH)                                                                       \
   do {                                                                                          \
     if (rk.mask)                                                                                \
-      COCO_LAUNCH_LAST((attn_rows_kernel<HS, GH, true>), grid, block, 0, st, q, k_cache, v_cache, \
-                       rk, Hq, Hkv, o);                                                         \
+      COCO_ROWS_MODE(HS, GH, kRowsTree);                                                        \
+    else if (rk.window > 0)                                                                     \
+      COCO_ROWS_MODE(HS, GH, kRowsWindow);                                                      \
     else                                                                                        \
-      COCO_LAUNCH_LAST((attn_rows_kernel<HS, GH, false>), grid, block, 0, st, q, k_cache,       \
-                       v_cache, rk, Hq, Hkv, o);                                                \
+      COCO_ROWS_MODE(HS, GH, kRowsBlocks);                                                      \
   } while (0)
 #define COCO_ROWS4(HS) \
   if (gh == 4) COCO_ROWS(HS, 4); else if (gh == 2) COCO_ROWS(HS, 2); else COCO_ROWS(HS, 1)
@@ -240,6 +259,7 @@ hipError_t launch_attn_rows_f32(const float* q, const float* k_cache, const floa
 #undef COCO_ROWS4
 #undef COCO_ROWS2
 #undef COCO_ROWS
+#undef COCO_ROWS_MODE
   return hipGetLastError();
 }
 

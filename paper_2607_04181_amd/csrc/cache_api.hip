@@ -1,5 +1,6 @@
 // C ABI of the operators on a replica's paged cache: its pages, attention for
-// trees of drafted tokens, and attention over selected blocks.
+// trees of drafted tokens, over selected blocks, and through a window, and
+// eviction by accumulated weight.
 #include "handle.h"
 
 using namespace coco;
@@ -353,6 +354,107 @@ int run_sparse(coco_layer* H, const coco_layer_weights& w, const void* q, void* 
   return COCO_OK;
 }
 
+int check_window(const coco_layer* H, int n_rows, int n_seqs, int window, int n_sinks,
+                 const float* weights) {
+  if (window < 1) return fail(COCO_EINVAL, "window = %d must be >= 1", window);
+  if (n_sinks < 0) return fail(COCO_EINVAL, "n_sinks < 0");
+  if ((uintptr_t)weights % 16) return fail(COCO_EINVAL, "weights are not 16-byte aligned");
+  if (n_rows > H->window_rows || n_seqs > H->window_seqs)
+    return fail(COCO_ESTATE, "%d rows of %d sequences; coco_window_reserve made room for %d of %d",
+                n_rows, n_seqs, H->window_rows, H->window_seqs);
+  if (weights && !H->window_weigh)
+    return fail(COCO_ESTATE, "coco_window_reserve made no room for weights");
+  return COCO_OK;
+}
+
+int validate_window(const coco_layer* H, int n_rows, const int32_t* positions,
+                    const int32_t* seq_starts, int n_seqs, const int32_t* block_table,
+                    const int32_t* ctx_lens, int window, int n_sinks, int64_t num_blocks,
+                    hipStream_t st) {
+  const coco_layer_config& c = H->cfg;
+  const int64_t slots = (int64_t)c.max_blocks_per_seq * kBlockTokens;
+  std::vector<int32_t> ss, ctx, pos, bt;
+  int rc;
+  if ((rc = fetch(ctx, ctx_lens, n_seqs, st)) ||
+      (rc = fetch(bt, block_table, (size_t)n_seqs * c.max_blocks_per_seq, st)) ||
+      (rc = check_range("ctx_lens", ctx, 0, slots + 1)))
+    return rc;
+  if (seq_starts) {
+    if ((rc = fetch(ss, seq_starts, (size_t)n_seqs + 1, st))) return rc;
+  } else {
+    if ((rc = zeros(ss, (size_t)n_seqs + 1))) return rc;
+    for (int s = 0; s <= n_seqs; ++s) ss[s] = s;
+  }
+  if (ss[0] != 0 || ss[n_seqs] < 0 || ss[n_seqs] > n_rows)
+    return fail(COCO_EINVAL, "seq_starts must run from 0 to at most n_rows");
+  // (prompts' rotations come from a table of the cache's positions)
+  if (positions && ((rc = fetch(pos, positions, ss[n_seqs], st)) ||
+                    (rc = check_range("positions", pos, 0,
+                                      seq_starts && H->rope_rows ? H->rope_rows : INT32_MAX))))
+    return rc;
+  for (int s = 0; s < n_seqs; ++s) {
+    const int rows = ss[s + 1] - ss[s];
+    if (rows < 0) return fail(COCO_EINVAL, "seq_starts not monotone at %d", s);
+    if (rows == 0) continue;
+    if (rows > ctx[s])
+      return fail(COCO_EINVAL, "sequence %d has %d rows in %d cached tokens", s, rows, ctx[s]);
+    // What its rows see between them.
+    const int lo = ctx[s] - rows + 1 > window ? ctx[s] - rows + 1 - window : 0;
+    for (int b = 0; b < (ctx[s] + kBlockTokens - 1) / kBlockTokens; ++b) {
+      if (b * kBlockTokens >= n_sinks && (b + 1) * kBlockTokens <= lo) continue;
+      const int32_t v = bt[(size_t)s * c.max_blocks_per_seq + b];
+      if (v < 0 || v >= num_blocks)
+        return fail(COCO_EINVAL, "block_table[%d][%d] = %d out of range [0, %lld)", s, b, v,
+                    (long long)num_blocks);
+    }
+  }
+  return COCO_OK;
+}
+
+int run_window(coco_layer* H, const coco_layer_weights& w, const void* q, void* o, bool tiled,
+               int n_rows, const int32_t* seq_starts, int n_seqs, const int32_t* bt,
+               const int32_t* ctx, int window, int n_sinks, float* weights, hipStream_t st) {
+  const coco_layer_config& c = H->cfg;
+  RowKeys rk = row_keys(H, seq_starts, n_seqs, bt, ctx, w.num_blocks);
+  rk.window = window;
+  rk.sinks = n_sinks;
+  const bool bf16 = c.dtype == COCO_BF16;
+  if (bf16 && !seq_starts) {
+    HIPCHK(launch_window_decode_bf16(
+        (const bf16_t*)q, (const bf16_t*)w.k_cache, (const bf16_t*)w.v_cache, rk, n_rows,
+        c.n_q_heads, c.n_kv_heads, (bf16_t*)o, tiled,
+        window_parts(window, n_sinks, c.max_blocks_per_seq), H->window_part_o, H->window_part_ml,
+        H->window_scores, weights, st));
+    return COCO_OK;
+  }
+  // The weights' kernels come last where there are any.
+  LaunchEvents& le = launch_events();
+  const hipEvent_t done = le.done;
+  if (weights) le.done = nullptr;
+  float* stats = weights ? H->window_stats : nullptr;
+  if (bf16)
+    HIPCHK(launch_window_prompt_bf16((const bf16_t*)q, (const bf16_t*)w.k_cache,
+                                     (const bf16_t*)w.v_cache, rk, n_rows, c.n_q_heads,
+                                     c.n_kv_heads, (bf16_t*)o, tiled, H->window_part_o,
+                                     H->window_part_ml, H->window_parts, H->window_counts, stats,
+                                     H->num_cus, st));
+  else
+    HIPCHK(launch_attn_rows_f32((const float*)q, (const float*)w.k_cache, (const float*)w.v_cache,
+                                rk, n_rows, c.n_q_heads, c.n_kv_heads, c.head_dim, (float*)o,
+                                H->num_cus, st, stats));
+  if (!weights) return COCO_OK;
+  le.done = done;
+  if (bf16)
+    HIPCHK(launch_window_weights_bf16((const bf16_t*)q, (const bf16_t*)w.k_cache, rk, n_rows,
+                                      c.n_q_heads, c.n_kv_heads, stats, H->window_sums, weights,
+                                      H->num_cus, st));
+  else
+    HIPCHK(launch_window_weights_f32((const float*)q, (const float*)w.k_cache, rk, n_rows,
+                                     c.n_q_heads, c.n_kv_heads, c.head_dim, stats, weights,
+                                     H->num_cus, st));
+  return COCO_OK;
+}
+
 }  // namespace coco
 
 extern "C" {
@@ -480,11 +582,12 @@ int coco_kv_compact(coco_layer_t H, int32_t first_layer, int32_t n_layers, const
         (rc = fetch(bt, block_table, (size_t)n_seqs * c.max_blocks_per_seq, st)) ||
         (rc = check_range("sequence", s, 0, n_seqs)) ||
         (rc = check_distinct("sequence", s, n_seqs)) ||
-        (rc = check_range("kept", k, 0, (int64_t)c.max_blocks_per_seq * kBlockTokens)) ||
         (rc = check_range("base_lens", b, 0, (int64_t)c.max_blocks_per_seq * kBlockTokens + 1)))
       return rc;
-    if (ks[0] != 0 || ks[n] != n_kept)
-      return fail(COCO_EINVAL, "kept_starts must run from 0 to n_kept");
+    if (ks[0] != 0 || ks[n] < 0 || ks[n] > n_kept)
+      return fail(COCO_EINVAL, "kept_starts must run from 0 to at most n_kept");
+    k.resize(ks[n]);  // (places behind the last list may hold anything)
+    if ((rc = check_range("kept", k, 0, (int64_t)c.max_blocks_per_seq * kBlockTokens))) return rc;
     for (int i = 0; i < n; ++i) {
       if (ks[i + 1] < ks[i]) return fail(COCO_EINVAL, "kept_starts not monotone at %d", i);
       for (int j = ks[i]; j < ks[i + 1]; ++j)
@@ -690,6 +793,126 @@ int coco_sparse_attention(coco_layer_t H, int32_t layer, const void* q, void* o,
   if ((rc = run_sparse(H, w, q, o, false, n_rows, positions, seq_starts, n_seqs, block_table,
                        ctx_lens, selected, n_select, st)))
     return rc;
+  return end.finish();
+}
+
+int coco_window_reserve(coco_layer_t H, int32_t max_rows, int32_t max_seqs, int32_t weigh) {
+  if (!H) return fail(COCO_EINVAL, "handle is NULL");
+  if (max_rows < 1 || max_seqs < 1 || max_seqs > 65535)
+    return fail(COCO_EINVAL, "max_rows = %d must be positive, max_seqs = %d in [1, 65535]", max_rows,
+                max_seqs);
+  const int rows = max_rows > H->window_rows ? max_rows : H->window_rows;
+  const int seqs = max_seqs > H->window_seqs ? max_seqs : H->window_seqs;
+  const bool weights = weigh != 0 || H->window_weigh;
+  const coco_layer_config& c = H->cfg;
+  const size_t stats = weights ? align256((size_t)rows * c.n_q_heads * 8) : 0;
+  if (c.dtype == COCO_BF16) {
+    // Single tokens and prompts use the same room in turn.
+    const int64_t few = rows < seqs ? rows : seqs;
+    const int64_t blocks = (int64_t)window_parts(INT32_MAX, 0, c.max_blocks_per_seq) * kWindowPart;
+    const int64_t single = few * c.n_q_heads * (blocks / kWindowPart);
+    const int64_t prompt = window_column_parts(rows, seqs, c.n_q_heads, c.n_kv_heads);
+    const int64_t parts = single > prompt ? single : prompt;
+    const size_t o = align256((size_t)parts * c.head_dim * 4), ml = align256((size_t)parts * 8);
+    const size_t sums =
+        weights ? align256((size_t)seqs * c.n_kv_heads * c.max_blocks_per_seq * kBlockTokens * 4) : 0;
+    const size_t scores =
+        weights ? align256((size_t)few * c.n_q_heads * blocks * kBlockTokens * 4) : 0;
+    const size_t both = stats + sums > scores ? stats + sums : scores;
+    const size_t counts = kWindowCounts * 4;
+    const int rc =
+        grow(H, &H->window_ws, &H->window_bytes, o + ml + both + counts, counts);
+    if (rc) return rc;
+    H->window_parts = parts;
+    H->window_part_o = (float*)H->window_ws;
+    H->window_part_ml = (float*)(H->window_ws + o);
+    H->window_stats = (float*)(H->window_ws + o + ml);
+    H->window_sums = (float*)(H->window_ws + o + ml + stats);
+    H->window_scores = H->window_stats;
+    H->window_counts = (int32_t*)(H->window_ws + o + ml + both);
+  } else if (weights) {
+    const int rc = grow(H, &H->window_ws, &H->window_bytes, stats);
+    if (rc) return rc;
+    H->window_stats = (float*)H->window_ws;
+  }
+  H->window_rows = rows;
+  H->window_seqs = seqs;
+  H->window_weigh = weights;
+  return COCO_OK;
+}
+
+int coco_window_attention(coco_layer_t H, int32_t layer, const void* q, void* o, int32_t n_rows,
+                          const int32_t* seq_starts, int32_t n_seqs, const int32_t* block_table,
+                          const int32_t* ctx_lens, int32_t window, int32_t n_sinks, float* weights,
+                          coco_stream_t stream) {
+  if (!H) return fail(COCO_EINVAL, "handle is NULL");
+  int rc = check_rows(H, layer, q, o, n_rows, seq_starts, n_seqs, block_table, ctx_lens);
+  if (rc || n_rows == 0) return rc;
+  if ((rc = check_window(H, n_rows, n_seqs, window, n_sinks, weights))) return rc;
+  const coco_layer_weights& w = H->layers[layer];
+  hipStream_t st = (hipStream_t)stream;
+  HIPCHK(hipSetDevice(H->device));
+  if (H->validate && (rc = validate_window(H, n_rows, nullptr, seq_starts, n_seqs, block_table,
+                                           ctx_lens, window, n_sinks, w.num_blocks, st)))
+    return rc;
+  CallEnd end(H, st, n_seqs <= kWindowLaunchSeqs);
+  if ((rc = run_window(H, w, q, o, false, n_rows, seq_starts, n_seqs, block_table, ctx_lens, window,
+                       n_sinks, weights, st)))
+    return rc;
+  return end.finish();
+}
+
+int coco_kv_evict(coco_layer_t H, const int32_t* seq_idx, const int32_t* keep_lens, int32_t n,
+                  int32_t keep_first, int32_t keep_last, const int32_t* ctx_lens, float* weights,
+                  int32_t n_seqs, int32_t* new_lens, int32_t* base_lens, int32_t* kept,
+                  int32_t n_kept, int32_t* kept_starts, coco_stream_t stream) {
+  if (!H) return fail(COCO_EINVAL, "handle is NULL");
+  int rc = check_requests(n, n_seqs);
+  if (rc || n == 0) return rc;
+  const coco_layer_config& c = H->cfg;
+  if (n > c.max_seqs) return fail(COCO_EINVAL, "n = %d above max_seqs = %d", n, c.max_seqs);
+  if (!seq_idx || !keep_lens || !ctx_lens || !new_lens || !base_lens || !kept_starts)
+    return fail(COCO_EINVAL, "NULL argument");
+  if (n_kept < 0 || (n_kept > 0 && !kept)) return fail(COCO_EINVAL, "no room for the lists");
+  if (keep_first < 0 || keep_last < 0)
+    return fail(COCO_EINVAL, "keep_first = %d or keep_last = %d below 0", keep_first, keep_last);
+  if ((uintptr_t)weights % 16) return fail(COCO_EINVAL, "weights are not 16-byte aligned");
+  hipStream_t st = (hipStream_t)stream;
+  HIPCHK(hipSetDevice(H->device));
+  if (H->validate) {
+    std::vector<int32_t> s, k, ctx;
+    if ((rc = fetch(s, seq_idx, n, st)) || (rc = check_range("sequence", s, 0, n_seqs)) ||
+        (rc = check_distinct("sequence", s, n_seqs)) || (rc = fetch(k, keep_lens, n, st)) ||
+        (rc = check_range("keep_lens", k, 0, INT32_MAX)) ||
+        (rc = fetch(ctx, ctx_lens, n_seqs, st)) ||
+        (rc = check_range("ctx_lens", ctx, 0, (int64_t)c.max_blocks_per_seq * kBlockTokens + 1)))
+      return rc;
+    // (a list may be as long as its budget)
+    int64_t most = 0;
+    for (int i = 0; i < n; ++i)
+      if (k[i] < ctx[s[i]]) most += k[i];
+    if (most > n_kept)
+      return fail(COCO_EINVAL, "lists of up to %lld tokens do not fit n_kept = %d", (long long)most,
+                  n_kept);
+  }
+  EvictArgs a;
+  a.seq = seq_idx;
+  a.keep = keep_lens;
+  a.n = n;
+  a.n_seqs = n_seqs;
+  a.keep_first = keep_first;
+  a.keep_last = keep_last;
+  a.max_blocks = c.max_blocks_per_seq;
+  a.n_kept = n_kept;
+  a.ctx = ctx_lens;
+  a.weights = weights;
+  a.new_lens = new_lens;
+  a.base_lens = base_lens;
+  a.kept = kept;
+  a.kept_starts = kept_starts;
+  a.plan = H->evict_plan;
+  CallEnd end(H, st);
+  HIPCHK(launch_evict(a, st));
   return end.finish();
 }
 

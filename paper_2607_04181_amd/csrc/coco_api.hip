@@ -354,7 +354,8 @@ int coco_layer_init(const coco_layer_config* cfg, const coco_layer_weights* laye
   for (const coco_layer_weights& w : H->layers)
     if (w.num_blocks > max_blocks) max_blocks = w.num_blocks;
   const size_t page_bytes = align256((size_t)max_blocks * 4);
-  H->ws_bytes = work_bytes + freq_bytes + rope_bytes + page_bytes + align256((size_t)c.max_seqs * 4);
+  const size_t off_bytes = align256((size_t)c.max_seqs * 4), plan_bytes = (size_t)c.max_seqs * 16;
+  H->ws_bytes = work_bytes + freq_bytes + rope_bytes + page_bytes + off_bytes + plan_bytes;
   if (hipMalloc((void**)&H->ws, H->ws_bytes) != hipSuccess) {
     (void)hipGetLastError();
     const size_t want = H->ws_bytes;
@@ -366,6 +367,7 @@ int coco_layer_init(const coco_layer_config* cfg, const coco_layer_weights* laye
   H->rope = (float*)(H->ws + work_bytes + freq_bytes);
   H->page_list = (int32_t*)(H->ws + work_bytes + freq_bytes + rope_bytes);
   H->page_off = (int32_t*)(H->ws + work_bytes + freq_bytes + rope_bytes + page_bytes);
+  H->evict_plan = (uint32_t*)(H->ws + work_bytes + freq_bytes + rope_bytes + page_bytes + off_bytes);
   H->act_rows_bytes[COCO_WS_X] = R * d * eb;
   H->act_rows_bytes[COCO_WS_H] = R * d * eb;
   H->act_rows_bytes[COCO_WS_Q] = R * qd * eb;
@@ -497,7 +499,7 @@ namespace {
 int validate_batch(coco_layer* H, int64_t hidden_rows, const int32_t* row_idx, int n_rows,
                    const int32_t* positions, const int32_t* seq_starts, int n_seqs,
                    const int32_t* block_table, const int32_t* ctx_lens, int first_layer,
-                   int n_layers, int tree_words, hipStream_t st) {
+                   int n_layers, const LayerRows* rows, hipStream_t st) {
   const coco_layer_config& c = H->cfg;
   std::vector<int32_t> ri, pos, ss, bt, cl;
   int rc;
@@ -523,9 +525,12 @@ int validate_batch(coco_layer* H, int64_t hidden_rows, const int32_t* row_idx, i
   if (ss[0] != 0 || ss[n_seqs] != n_rows)
     return fail(COCO_EINVAL, "seq_starts must run from 0 to n_rows");
   const int64_t min_blocks = shared_blocks(H, first_layer, n_layers);
-  if (tree_words)  // (siblings share a position)
+  if (rows && rows->mask)  // (siblings share a position)
     return validate_tree(H, n_rows, positions, seq_starts, n_seqs, block_table, ctx_lens,
-                         tree_words, min_blocks, st);
+                         rows->words, min_blocks, st);
+  if (rows && rows->window > 0)
+    return validate_window(H, n_rows, positions, seq_starts, n_seqs, block_table, ctx_lens,
+                           rows->window, rows->n_sinks, min_blocks, st);
   for (int s = 0; s < n_seqs; ++s) {
     if (ss[s + 1] < ss[s]) return fail(COCO_EINVAL, "seq_starts not monotone at %d", s);
     if (cl[s] < 1 || cl[s] > c.max_blocks_per_seq * kBlockTokens)
@@ -637,6 +642,9 @@ int attend_rows(coco_layer* H, const Work& W, const coco_layer_weights& w, int M
   if (rows.mask)
     return run_tree(H, w, W.q, W.o, o_tiled, M, seq_starts, n_seqs, bt, ctx, rows.mask, rows.words,
                     st);
+  if (rows.window > 0)
+    return run_window(H, w, W.q, W.o, o_tiled, M, seq_starts, n_seqs, bt, ctx, rows.window,
+                      rows.n_sinks, rows.weights, st);
   // The new token's block first: it may be among the selected.
   int rc;
   if ((rc = run_summarize(H, w, rows.summary, rows.scales, positions, ctx, n_seqs, bt, st)) ||
@@ -759,7 +767,8 @@ int decode_layer(coco_layer* H, const Work& W, const coco_layer_weights& w, cons
         HIPCHK(launch_qkv_epilogue_bf16(W.part, plan.S, M, Hq, Hkv, hd, positions, bt,
                                         c.max_blocks_per_seq, w.num_blocks, H->inv_freq, q,
                                         (bf16_t*)w.k_cache, (bf16_t*)w.v_cache, ctx, W.split_off,
-                                        H->max_splits, W.ss, d, c.rms_eps, st)));
+                                        H->max_splits, W.ss, d, c.rms_eps,
+                                        rows && rows->window > 0, st)));
   // Attention over the paged cache.
   if ((rc = attention(H, W, w, M, positions, nullptr, M, bt, ctx, rows, lay.o, st))) return rc;
   // O projection + residual + RMSNorm_2.
@@ -808,7 +817,7 @@ int f32_layer(coco_layer* H, const Work& W, const coco_layer_weights& w, const f
   qa.seq_starts = seq_starts;
   qa.block_table = bt;
   qa.num_blocks = w.num_blocks;
-  if (rows && rows->mask) qa.tree_lens = ctx;
+  if (rows && rows->slots()) qa.tree_lens = ctx;
   qa.inv_freq = H->inv_freq;
   qa.q_out = (float*)W.q;
   qa.k_cache = (float*)w.k_cache;
@@ -886,7 +895,7 @@ int run_span(coco_layer* H, const Work& W, int first, int nl, T* hidden, const i
         rs.rope_rows = H->rope_rows;
         // (the slots are written once, for all of the call's layers)
         rs.num_blocks = shared_blocks(H, first, nl);
-        if (rows && rows->mask) rs.tree_lens = ctx;
+        if (rows && rows->slots()) rs.tree_lens = ctx;
       }
       rc = prefill_layer(H, W, w, x_src, x_idx, y, y_idx, M, positions, seq_starts, n_seqs, bt,
                          ctx, rows, rs, st);
@@ -938,6 +947,9 @@ int forward_impl(coco_layer* H, int first, int nl, void* hidden, int64_t hidden_
   HIPCHK(hipSetDevice(H->device));
   const bool tree = rows && rows->mask;
   if (tree && (rc = check_tree(H, n_rows, seq_starts, n_seqs, rows->mask, rows->words))) return rc;
+  if (rows && rows->window > 0 &&
+      (rc = check_window(H, n_rows, n_seqs, rows->window, rows->n_sinks, rows->weights)))
+    return rc;
   Work W = H->w;
   if (use_static) {
     const int64_t dec_seqs = seq_starts ? 0 : n_seqs;
@@ -951,7 +963,7 @@ int forward_impl(coco_layer* H, int first, int nl, void* hidden, int64_t hidden_
     carve_work(H->cfg, n_rows, dec_seqs, H->max_splits, base, &W);
   } else if (H->validate &&
              (rc = validate_batch(H, hidden_rows, row_idx, n_rows, positions, seq_starts, n_seqs,
-                                  bt, ctx, first, nl, tree ? rows->words : 0, st))) {
+                                  bt, ctx, first, nl, rows, st))) {
     return rc;
   }
   if (!use_static) {
@@ -1040,6 +1052,21 @@ int coco_layer_sparse_forward(coco_layer_t H, int32_t layer, void* hidden, int64
   rows.n_select = n_select;
   return forward_impl(H, layer, 1, hidden, hidden_rows, row_idx, n_rows, positions, nullptr,
                       n_rows, block_table, ctx_lens, stream, false, &rows);
+}
+
+int coco_layer_window_forward(coco_layer_t H, int32_t first_layer, int32_t n_layers, void* hidden,
+                              int64_t hidden_rows, const int32_t* row_idx, int32_t n_rows,
+                              const int32_t* positions, const int32_t* seq_starts, int32_t n_seqs,
+                              const int32_t* block_table, const int32_t* ctx_lens, int32_t window,
+                              int32_t n_sinks, float* weights, coco_stream_t stream) {
+  if (!H) return fail(COCO_EINVAL, "handle is NULL");
+  if (window < 1) return fail(COCO_EINVAL, "window = %d must be >= 1", window);
+  LayerRows rows;
+  rows.window = window;
+  rows.n_sinks = n_sinks;
+  rows.weights = weights;
+  return forward_impl(H, first_layer, n_layers, hidden, hidden_rows, row_idx, n_rows, positions,
+                      seq_starts, n_seqs, block_table, ctx_lens, stream, false, &rows);
 }
 
 int coco_kv_append(coco_layer_t H, int32_t layer, const void* k, const void* v,

@@ -232,6 +232,31 @@ __device__ __forceinline__ int readable_block(int block, int64_t num_blocks) {
   return in_pool(block, num_blocks) ? block : 0;
 }
 
+// The blocks that rows of slots p0 .. p1 (p0 <= p1) of a sequence see between them
+// through a window and the first `sinks` slots, as a list: `head` blocks from the
+// context's start, then those from `first` on, `entries` in all. A row of slot p
+// sees slots 0 .. p that are above p - window or below sinks.
+struct WindowList {
+  int head, first, entries;
+  __device__ __forceinline__ int block(int e) const { return e < head ? e : first + (e - head); }
+};
+__device__ __forceinline__ WindowList window_list(int p0, int p1, int window, int sinks) {
+  const int lo = max(p0 - window + 1, 0);  // (p0 >= -1: no overflow)
+  WindowList w;
+  w.first = lo / kBlockTokens;
+  const int s = min(sinks, lo);
+  w.head = min(s / kBlockTokens + (s % kBlockTokens != 0), w.first);
+  w.entries = p1 < 0 ? 0 : w.head + p1 / kBlockTokens + 1 - w.first;
+  return w;
+}
+
+// Of the 16 slots from t0 on, those that a row of slot p sees, as bits.
+__device__ __forceinline__ uint32_t window_bits(int t0, int p, int window, int sinks) {
+  const int hi = min(max(p + 1 - t0, 0), 16);
+  const int lo = min(max(max(p - window + 1, 0) - t0, 0), 16), s = min(max(sinks - t0, 0), 16);
+  return ((1u << hi) - 1) & (~((1u << lo) - 1) | ((1u << s) - 1));
+}
+
 // Whether a call row belongs to no sequence (a padded call: left as it is).
 __device__ __forceinline__ bool row_past_seqs(const int32_t* seq_starts, int n_seqs, int row) {
   return seq_starts != nullptr && row >= seq_starts[n_seqs];

@@ -113,6 +113,16 @@ struct coco_layer {
   int32_t *tree_plan = nullptr, *tree_redo = nullptr;
   float *sparse_part_o = nullptr, *sparse_part_ml = nullptr;
   uint32_t* sparse_keys = nullptr;
+  // As above of coco_window_reserve; what the evictions' kernels pass on ([max_seqs][4]).
+  int window_rows = 0, window_seqs = 0;
+  bool window_weigh = false;
+  char* window_ws = nullptr;
+  size_t window_bytes = 0;
+  float *window_part_o = nullptr, *window_part_ml = nullptr;
+  int64_t window_parts = 0;
+  float *window_stats = nullptr, *window_sums = nullptr, *window_scores = nullptr;
+  int32_t* window_counts = nullptr;
+  uint32_t* evict_plan = nullptr;
   std::vector<char*> extra;
 };
 
@@ -160,6 +170,11 @@ struct LayerRows {
   float* scales = nullptr;
   int keep_first = 0, keep_last = 0, n_select = 0;
   int32_t* selected = nullptr;
+  // Windows (window > 0).
+  int window = 0, n_sinks = 0;
+  float* weights = nullptr;
+  // The rows have slots of their own, apart from their positions.
+  bool slots() const { return mask != nullptr || window > 0; }
 };
 
 // The attention operators without their entry points' checks of the handle and
@@ -188,5 +203,14 @@ int run_sparse(coco_layer* H, const coco_layer_weights& w, const void* q, void* 
                int n_rows, const int32_t* positions, const int32_t* seq_starts, int n_seqs,
                const int32_t* bt, const int32_t* ctx, const int32_t* selected, int n_select,
                hipStream_t st);
+int check_window(const coco_layer* H, int n_rows, int n_seqs, int window, int n_sinks,
+                 const float* weights);
+int validate_window(const coco_layer* H, int n_rows, const int32_t* positions,
+                    const int32_t* seq_starts, int n_seqs, const int32_t* bt,
+                    const int32_t* ctx_lens, int window, int n_sinks, int64_t num_blocks,
+                    hipStream_t st);
+int run_window(coco_layer* H, const coco_layer_weights& w, const void* q, void* o, bool tiled,
+               int n_rows, const int32_t* seq_starts, int n_seqs, const int32_t* bt,
+               const int32_t* ctx, int window, int n_sinks, float* weights, hipStream_t st);
 
 }  // namespace coco

@@ -70,8 +70,8 @@ struct RowSlotArgs {
   int32_t* row_info = nullptr;  // null: not written
   int n_seqs = 0, max_blocks = 0, rope_rows = 0;
   int64_t num_blocks = 0;
-  // Trees: row i of sequence s is cached at tree_lens[s] - (rows of s) + (its
-  // place among them), not at its position.
+  // Trees and windows: row i of sequence s is cached at tree_lens[s] - (rows of s)
+  // + (its place among them), not at its position.
   const int32_t* tree_lens = nullptr;
 };
 
@@ -101,13 +101,14 @@ hipError_t launch_rope_table(const double* inv_freq, int half, int n_pos, float*
 // keys/values into the paged cache (not where the position's table entry is no
 // block of the pool). One workgroup also writes the decode attention's work list split_off (layout at launch_attn_decode_bf16) from the
 // keys each row attends, min(ctx_lens, positions + 1) (partition counts capped
-// at max_splits).
+// at max_splits). last_slot: row i is cached at ctx_lens[i] - 1, not at its position.
 hipError_t launch_qkv_epilogue_bf16(const float* part, int S, int M, int Hq, int Hkv, int hd,
                                     const int32_t* positions, const int32_t* block_table,
                                     int max_blocks, int64_t num_blocks, const double* inv_freq,
                                     uint16_t* q_out, uint16_t* k_cache, uint16_t* v_cache,
                                     const int32_t* ctx_lens, int32_t* split_off, int max_splits,
-                                    const float* ss, int d, float eps, hipStream_t st);
+                                    const float* ss, int d, float eps, bool last_slot,
+                                    hipStream_t st);
 
 // x1 = x + sum_s part[s]  (fp32);  h2 = RMSNorm(x1) * gamma. Row i of x is
 // x[row_idx ? row_idx[i] : i]. tiled: h2 in tile order.
@@ -364,6 +365,8 @@ hipError_t launch_page_compact(const int32_t* seq, const int32_t* base, const in
 // (seq_starts[s] ..) are the nodes in its last cached slots; all keys before
 // those, and the nodes whose bit is set in the row's mask words. Blocks: keys
 // up to the row's position in the blocks that selected[row][kv head] lists.
+// Window: row j of the N rows of a sequence with L cached tokens has slot p =
+// L - N + j and attends slots t <= p with t > p - window or t < sinks.
 struct RowKeys {
   const int32_t* block_table = nullptr;
   const int32_t* ctx_lens = nullptr;
@@ -375,11 +378,13 @@ struct RowKeys {
   const int32_t* positions = nullptr;   // blocks
   const int32_t* selected = nullptr;    // blocks: [rows][Hkv][top], -1: none
   int top = 0;
+  int window = 0, sinks = 0;            // window: > 0 (seq_starts null: row i is sequence i)
 };
-// fp32 handles, tree and blocks. q, o [rows][Hq][hd].
+// fp32 handles, tree, blocks and window. q, o [rows][Hq][hd]. stats (window; may be
+// null): as launch_window_prompt_bf16 writes them.
 hipError_t launch_attn_rows_f32(const float* q, const float* k_cache, const float* v_cache,
                                 const RowKeys& rk, int n_rows, int Hq, int Hkv, int hd, float* o,
-                                int num_cus, hipStream_t st);
+                                int num_cus, hipStream_t st, float* stats = nullptr);
 
 // Blocks, bf16 handles (hd 128, up to 16 query heads in a group). A list of top
 // entries is attended in sparse_parts(top) parts; with more than one,
@@ -406,6 +411,59 @@ hipError_t launch_tree_attention_bf16(const uint16_t* q, const uint16_t* k_cache
                                       int Hq, int Hkv, uint16_t* o, bool tiled, float* part_o,
                                       float* part_ml, int64_t part_cap, int32_t* plan,
                                       int32_t* redo, int num_cus, hipStream_t st);
+
+// Window rows of bf16 handles (hd 128, up to 16 query heads in a group); tiled: o
+// in tile order.
+// One row per sequence (rk.seq_starts null): the blocks that a row sees are
+// attended in parts of kWindowPart; parts: the most of any row of the call;
+// part_o [rows][Hkv][parts][Hq / Hkv][128] and part_ml [..][2] hold them where it
+// is above 1 or the weights are asked for. scores (null: no weights): every
+// score of the call, [rows][Hkv][entries][Hq / Hkv][16], entries >= parts *
+// kWindowPart; weights [n_seqs][max_blocks * 16] then grow by the rows' weights.
+constexpr int kWindowPart = 32;
+int window_parts(int window, int sinks, int max_blocks);
+hipError_t launch_window_decode_bf16(const uint16_t* q, const uint16_t* k_cache,
+                                     const uint16_t* v_cache, const RowKeys& rk, int n_rows, int Hq,
+                                     int Hkv, uint16_t* o, bool tiled, int parts, float* part_o,
+                                     float* part_ml, float* scores, float* weights,
+                                     hipStream_t st);
+// Rows of prompts. The keys of a sequence with few columns (rows times query
+// heads per key/value head) are attended in parts, whose results part_o [column
+// parts][128] and part_ml [..][2] hold, room for part_cap = window_column_parts;
+// counts [kWindowCounts] must be zero and is left so. stats (null: not asked for)
+// [rows][Hq][2]: each row's running maximum (in powers of two) and 1 / its sum
+// of weights (0: it sees nothing).
+constexpr int kWindowCounts = 16, kWindowLaunchSeqs = 1024;
+int64_t window_column_parts(int64_t max_rows, int64_t max_seqs, int Hq, int Hkv);
+hipError_t launch_window_prompt_bf16(const uint16_t* q, const uint16_t* k_cache,
+                                     const uint16_t* v_cache, const RowKeys& rk, int n_rows, int Hq,
+                                     int Hkv, uint16_t* o, bool tiled, float* part_o,
+                                     float* part_ml, int64_t part_cap, int32_t* counts,
+                                     float* stats, int num_cus, hipStream_t st);
+// weights [n_seqs][max_blocks * 16] grow by the weights of the rows' keys, from
+// the rows' stats; sums [n_seqs][Hkv][max_blocks * 16]: scratch.
+hipError_t launch_window_weights_bf16(const uint16_t* q, const uint16_t* k_cache, const RowKeys& rk,
+                                      int n_rows, int Hq, int Hkv, const float* stats, float* sums,
+                                      float* weights, int num_cus, hipStream_t st);
+// fp32 handles (the rows' attention is launch_attn_rows_f32).
+hipError_t launch_window_weights_f32(const float* q, const float* k_cache, const RowKeys& rk,
+                                     int n_rows, int Hq, int Hkv, int hd, const float* stats,
+                                     float* weights, int num_cus, hipStream_t st);
+
+// ---------------------------------------------------------------- eviction
+struct EvictArgs {
+  const int32_t* seq = nullptr;
+  const int32_t* keep = nullptr;  // budgets
+  int n = 0, n_seqs = 0, keep_first = 0, keep_last = 0, max_blocks = 0, n_kept = 0;
+  const int32_t* ctx = nullptr;
+  float* weights = nullptr;       // [n_seqs][max_blocks * 16]; null: all alike
+  int32_t* new_lens = nullptr;
+  int32_t* base_lens = nullptr;
+  int32_t* kept = nullptr;        // [n_kept]
+  int32_t* kept_starts = nullptr; // [n + 1]
+  uint32_t* plan = nullptr;       // [n][4]: scratch
+};
+hipError_t launch_evict(const EvictArgs& a, hipStream_t st);
 
 // ---------------------------------------------------------- block summaries
 // summary [block][Hkv][2][hd] and scales [block][Hkv] of the blocks that hold

@@ -161,13 +161,18 @@ __global__ __launch_bounds__(kFThreads) void layer_f32_gemm_kernel(const float* 
       arow[tid] = ea.row_idx ? ea.row_idx[m] : m;
       pos_s[tid] = pos;
       int at = pos;
-      if (ea.tree_lens != nullptr)
-        at = min(max(ea.tree_lens[seq] - ea.seq_starts[seq + 1] + m, 0),
-                 ea.max_blocks * kBlockTokens - 1);
+      bool no_slot = false;
+      if (ea.tree_lens != nullptr) {
+        at = ea.tree_lens[seq] + m - (ea.seq_starts ? ea.seq_starts[seq + 1] : m + 1);
+        no_slot = at < 0 || at >= ea.max_blocks * kBlockTokens;
+        at = min(max(at, 0), ea.max_blocks * kBlockTokens - 1);
+      }
       slot_s[tid] = at % kBlockTokens;
       int blk = ea.block_table[(int64_t)seq * ea.max_blocks + at / kBlockTokens];
-      // (a tree call's row of no sequence must not reach the last one's pages)
-      if (ea.tree_lens != nullptr && row_past_seqs(ea.seq_starts, ea.n_seqs, m)) blk = -1;
+      // (a row with a slot of its own, but of no sequence or outside its table, must
+      // not reach another's place)
+      if (no_slot || (ea.tree_lens != nullptr && row_past_seqs(ea.seq_starts, ea.n_seqs, m)))
+        blk = -1;
       blk_s[tid] = in_pool(blk, ea.num_blocks) ? blk : -1;
     } else if constexpr (MODE == kFScatter || MODE == kFResid) {
       arow[tid] = ea.row_idx ? ea.row_idx[m] : m;

@@ -85,10 +85,12 @@ __device__ __forceinline__ void write_row_slot_uniform(const RowSlotArgs& rs, in
   int at = pos;
   if (rs.tree_lens != nullptr)
     at = ((cint_ptr)rs.tree_lens)[lo] - seq_starts[lo + 1] + i;
+  const bool no_slot = at < 0 || at >= rs.max_blocks * kBlockTokens;
   at = min(max(at, 0), rs.max_blocks * kBlockTokens - 1);
   int blk = block_table[(int64_t)lo * rs.max_blocks + at / kBlockTokens];
-  // (a tree call's row of no sequence must not reach the last one's pages)
-  if (rs.tree_lens != nullptr && i >= seq_starts[rs.n_seqs]) blk = -1;
+  // (a row with a slot of its own, but of no sequence or outside its table, must
+  // not reach another's place)
+  if (rs.tree_lens != nullptr && (no_slot || i >= seq_starts[rs.n_seqs])) blk = -1;
   if (threadIdx.x == 0) {
     rs.row_info[2 * i] = min(max(pos, 0), rs.rope_rows - 1);
     rs.row_info[2 * i + 1] = cache_place(blk, rs.num_blocks, at);
@@ -214,7 +216,7 @@ __global__ __launch_bounds__(kEpiHeads * kWave) void qkv_epilogue_kernel(
     int max_blocks, int64_t num_blocks, const double* __restrict__ inv_freq,
     bf16_t* __restrict__ q_out, bf16_t* __restrict__ k_cache, bf16_t* __restrict__ v_cache,
     const int32_t* __restrict__ ctx_lens, int32_t* __restrict__ split_off, int max_splits,
-    const float* __restrict__ ss, int d, float eps) {
+    const float* __restrict__ ss, int d, float eps, bool last_slot) {
   __shared__ float rot[2][128];  // cos, sin of the row's angles (hd / 2 <= 128)
   __shared__ int wl_rank[kDecodeSplit];  // work list: partial partitions per size, then ranks
   const int i = blockIdx.y, lane = threadIdx.x & (kWave - 1), wv = threadIdx.x / kWave;
@@ -252,8 +254,10 @@ __global__ __launch_bounds__(kEpiHeads * kWave) void qkv_epilogue_kernel(
   const int pos = positions[i];
   int blk = 0, slot = 0;
   if (live && h >= Hq) {
-    blk = block_table[(int64_t)i * max_blocks + pos / kBlockTokens];
-    slot = pos % kBlockTokens;
+    const int at = last_slot ? ctx_lens[i] - 1 : pos;
+    const bool outside = last_slot && (at < 0 || at >= max_blocks * kBlockTokens);
+    blk = outside ? -1 : block_table[(int64_t)i * max_blocks + at / kBlockTokens];
+    slot = at % kBlockTokens;
   }
   // The row's rotation angles in fp64, once for all the heads of the block.
   for (int j = threadIdx.x; j < half; j += kEpiHeads * kWave) {
@@ -372,14 +376,15 @@ hipError_t launch_qkv_epilogue_bf16(const float* part, int S, int M, int Hq, int
                                     int max_blocks, int64_t num_blocks, const double* inv_freq,
                                     bf16_t* q_out, bf16_t* k_cache, bf16_t* v_cache,
                                     const int32_t* ctx_lens, int32_t* split_off, int max_splits,
-                                    const float* ss, int d, float eps, hipStream_t st) {
+                                    const float* ss, int d, float eps, bool last_slot,
+                                    hipStream_t st) {
   if (M <= 0) return hipSuccess;
   if (hd > 256 || hd % 2 != 0 || !ss || !split_off) return hipErrorInvalidValue;
   const dim3 grid((Hq + 2 * Hkv + kEpiHeads - 1) / kEpiHeads, M);
   COCO_SWITCH_S(S, COCO_LAUNCH((qkv_epilogue_kernel<S_>), grid, dim3(kEpiHeads * kWave), 0, st,
                                part, M, Hq, Hkv, hd, positions, block_table, max_blocks,
                                num_blocks, inv_freq, q_out, k_cache, v_cache, ctx_lens,
-                               split_off, max_splits, ss, d, eps));
+                               split_off, max_splits, ss, d, eps, last_slot));
   return hipGetLastError();
 }
 

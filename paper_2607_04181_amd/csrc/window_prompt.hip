@@ -1,0 +1,673 @@
+// Attention of prompts' rows through a sliding window and a context's first
+// tokens (bf16, hd = 128).
+//
+// The columns of a sequence and key/value head are its rows times the group's
+// query heads, C = N G (column c: row c / G, head c % G), so that the heads of a
+// group share every key and value that is read. A wave owns 64 columns, as two
+// tiles of 32, and walks 32 keys (two blocks) at a time:
+//   S^T[32 keys][32 cols] = K[32][hd] Q^T[hd][32]    8 x mfma 32x32x16
+//   online softmax per column, 16 keys in each of its two lanes
+//   O^T[hd][32 cols] += V^T[hd][32] P^T[32][32]      8 x mfma 32x32x16
+// P comes out of the first product in the operand layout of the second: lane
+// (c, hf) holds keys 8 q + 4 hf + r of column c.
+//
+// Why 64 columns: a 32x32x16 product takes 32 cycles and an operand of 1 KB from
+// LDS, so one tile per wave would ask LDS for all of its 128 bytes per cycle; two
+// tiles share each key and value operand. One wave to a SIMD then, with its 512
+// registers (accumulators 128, queries 64, operands 64, scores 32), and nothing
+// but its own instructions to fill the pipes: the two tiles are half a step apart,
+// so that the vector work of one tile's softmax stands beside the products of the
+// other (step st: scores of tile 0 for st + 1 and values of tile 0, softmax of
+// tile 1; then scores and values of tile 1, softmax of tile 0 for st + 1).
+//
+// A workgroup is four waves with 256 columns of one sequence and key/value head.
+// They share the keys through LDS in a ring of stages of 32. Its list of blocks is
+// what its rows see between them; a stage that every column of a wave sees whole
+// takes no mask.
+//
+// The list of a sequence with at most kSplitCols columns is split into parts by a
+// rule on the sequence's own columns and list, merged by a second kernel in order:
+// a row's bits depend on its sequence's rows and length alone.
+#include <math.h>
+
+#include "common.h"
+#include "kernels.h"
+
+namespace coco {
+
+namespace {
+
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+typedef __attribute__((address_space(3))) void lds_void_t;
+typedef __attribute__((address_space(3))) bf16_t lds_bf16_t;
+typedef __attribute__((address_space(3))) u32x2_t lds_u32x2_t;
+
+constexpr int HD = 128;
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kWaves = 4;
+constexpr int kThreads = kWaves * kWave;
+constexpr int kCols = 64;                   // columns of a wave
+constexpr int kTileCols = kWaves * kCols;   // of a workgroup
+constexpr int kTile = kBlockTokens * HD;
+constexpr int kRing = 8;                    // stages in LDS
+constexpr int kStage = 4 * kTile;           // elements: keys and values of two blocks
+constexpr int kXCDs = 8;
+constexpr int kMaxSeqs = kWindowLaunchSeqs;
+constexpr float kLazy = 8.f;                // log2 units a running max may lag
+
+// Parts of a list of `entries` blocks for `cols` columns: blocks of one part (a
+// multiple of a stage's two).
+constexpr int kSplitCols = 512, kPartBlocks = 64, kMaxParts = 16;
+__host__ __device__ __forceinline__ int window_part(int64_t cols, int entries) {
+  if (cols > kSplitCols) return entries > 0 ? (entries + 1) / 2 * 2 : 2;
+  const int least = (entries + kMaxParts - 1) / kMaxParts;
+  return least > kPartBlocks ? (least + 1) / 2 * 2 : kPartBlocks;
+}
+
+struct PromptArgs {
+  const bf16_t* q;
+  const bf16_t* k_cache;
+  const bf16_t* v_cache;
+  RowKeys rk;
+  int Hq, Hkv;
+  float scale_log2;
+  bf16_t* o;
+  bool tiled;        // o in tile order
+  float* part_o;     // [column part][HD]
+  float* part_ml;    // [column part][2]
+  int64_t part_cap;  // column parts they hold
+  int32_t* counts;   // [0 .. 7] items drawn, [8] workgroups that are done
+  float* stats;      // [rows][Hq][2] or null
+};
+
+// A sequence's rows: N of slots first .. first + N - 1, C columns per key/value
+// head in `tiles` workgroup tiles, and the parts of its list.
+struct PromptSeq {
+  int row0, n, first, tiles, part, splits;
+};
+__device__ __forceinline__ PromptSeq prompt_seq(const RowKeys& rk, int s, int G) {
+  PromptSeq x;
+  x.row0 = rk.seq_starts[s];
+  x.n = max(rk.seq_starts[s + 1] - x.row0, 0);
+  const int len = min(max(rk.ctx_lens[s], 0), rk.max_blocks * kBlockTokens);
+  x.first = len - x.n;
+  const int64_t cols = (int64_t)x.n * G;
+  x.tiles = (int)((cols + kTileCols - 1) / kTileCols);
+  const int entries = window_list(max(x.first, -1), len - 1, rk.window, rk.sinks).entries;
+  x.part = window_part(cols, entries);
+  x.splits = max(1, (entries + x.part - 1) / x.part);
+  return x;
+}
+
+// Key fragments of two blocks: step s holds dims 16 s + 8 hf .. + 7 of key m.
+__device__ __forceinline__ int k_frag_off(int lane, int s) {
+  const int hf = lane >> 5, t = lane & 15;
+  return ((s >> 1) * 64 + (2 * (s & 1) + hf) * 16 + t) * 8;
+}
+// Value operand (pair d, half y) of lane (m, hf): dim value_dim(2 d + y, m), keys
+// 4 hf .. + 3 and 8 + 4 hf .. + 3 of a block. A lane's 16-byte chunk of a value
+// tile holds two dims 16 apart; which of them is the first operand's alternates
+// with the lanes, or eight-byte reads 16 bytes apart would meet in half the banks.
+__device__ __forceinline__ int value_swap(int m) { return (m >> 3 ^ m >> 4) & 1; }
+__device__ __forceinline__ int value_dim(int i, int m) {
+  return 32 * (i & 2) + 32 * (m >> 4) + 16 * ((i & 1) ^ value_swap(m)) + (m & 15);
+}
+
+// Largest of 16 values (NaN loses).
+__device__ __forceinline__ float max16(const f32x16_t& s) {
+  float m = fmaxf(fmaxf(s[0], s[1]), s[2]);
+#pragma unroll
+  for (int r = 3; r + 1 < 16; r += 2) m = fmaxf(fmaxf(m, s[r]), s[r + 1]);
+  return fmaxf(m, s[15]);
+}
+
+// -inf where the column does not see the key. Bit k of seen: key k of the 32.
+__device__ __forceinline__ void mask_scores(f32x16_t& s, uint32_t seen, int hf) {
+  const uint32_t mine = seen >> (4 * hf);
+#pragma unroll
+  for (int r = 0; r < 16; ++r) s[r] = (mine >> (8 * (r / 4) + r % 4) & 1) ? s[r] : -INFINITY;
+}
+
+// A product with a weight of 0 would let a non-finite value of a key that some
+// columns do not see, or of a slot that holds anything, reach them: such elements
+// are left out (add_odd gives them to the columns that see the key). Whether there
+// were any, for the wave.
+__device__ __forceinline__ bool mask_values(u32x4_t v[2][2][2]) {
+  bool odd = false;
+#pragma unroll
+  for (int j = 0; j < 2; ++j)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        uint32_t w = v[j][i >> 1][i & 1][e];
+        const bool lo = (w & 0x7F80u) == 0x7F80u, hi = (w & 0x7F800000u) == 0x7F800000u;
+        if (lo) w &= 0xFFFF0000u;
+        if (hi) w &= 0xFFFFu;
+        odd |= lo | hi;
+        v[j][i >> 1][i & 1][e] = w;
+      }
+  return __ballot(odd) != 0;
+}
+
+// One tile's columns: running softmax and O^T. acc[i][r]: dim value_dim(i, m), m =
+// 8 (r / 4) + 4 hf + r % 4.
+struct Cols {
+  float m, l;
+  f32x16_t acc[4];
+};
+
+// The running max of a column moves only when a step's largest score exceeds it by kLazy.
+__device__ __forceinline__ void rescale(Cols& c, const f32x16_t& z, float scale_log2) {
+  const float mx = max16(z);
+  const auto sw =
+      __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+  const float top = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * scale_log2;
+  const float m_new = top > c.m + kLazy ? top : c.m;
+  if (__ballot(m_new != c.m) != 0) {
+    const float alpha = __builtin_amdgcn_exp2f(c.m - (m_new == -INFINITY ? 0.f : m_new));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c.acc[i] *= alpha;
+    c.l *= alpha;
+    c.m = m_new;
+  }
+}
+
+// Weights of 32 keys as operands of two products.
+__device__ __forceinline__ void weights_of(Cols& c, const f32x16_t& z, float scale_log2,
+                                           u32x4_t p[2]) {
+  const float m_ref = c.m == -INFINITY ? 0.f : c.m;
+  float pr[16];
+#pragma unroll
+  for (int r = 0; r < 16; ++r) pr[r] = __builtin_amdgcn_exp2f(fmaf(z[r], scale_log2, -m_ref));
+  float ls = 0.f;
+#pragma unroll
+  for (int r = 0; r < 16; r += 4) ls += (pr[r] + pr[r + 1]) + (pr[r + 2] + pr[r + 3]);
+  c.l += ls;
+#pragma unroll
+  for (int j = 0; j < 2; ++j)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) p[j][e] = pack_bf16x2(pr[8 * j + 2 * e], pr[8 * j + 2 * e + 1]);
+}
+
+__device__ __forceinline__ f32x16_t scores_of(const u32x4_t k[8], const bf16x8_t q[8]) {
+  f32x16_t z = {};
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, k[i]), q[i], z, 0, 0, 0);
+  return z;
+}
+// O^T += V^T P^T.
+__device__ __forceinline__ void add_values(Cols& c, const u32x4_t v[2][2][2], const u32x4_t p[2]) {
+#pragma unroll
+  for (int j = 0; j < 2; ++j)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      c.acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+          __builtin_bit_cast(bf16x8_t, v[j][i >> 1][i & 1]), __builtin_bit_cast(bf16x8_t, p[j]),
+          c.acc[i], 0, 0, 0);
+}
+
+// The non-finite values of a stage for the columns that see their keys (seen). A
+// product counts them: 1 for each infinity, 64 for each negative one, 4096 for each
+// NaN, times 1, or 4096 where the weight is 0 (times infinity: NaN).
+__device__ __forceinline__ uint32_t odd_count(uint32_t h) {  // of a value, as bf16
+  if ((h & 0x7F80u) != 0x7F80u) return 0;
+  return h & 0x7Fu ? 0x4580u : h & 0x8000u ? 0x4280u : 0x3F80u;
+}
+__device__ __forceinline__ void add_odd(Cols& c, const u32x4_t v[2][2][2], const u32x4_t p[2],
+                                        uint32_t seen, int hf) {
+  const uint32_t mine = seen >> (4 * hf);
+  u32x4_t n[2];
+#pragma unroll
+  for (int r = 0; r < 16; r += 2) {
+    const uint32_t w = p[r >> 3][r >> 1 & 3];
+    const int key = 8 * (r / 4) + r % 4;
+    n[r >> 3][r >> 1 & 3] = (mine >> key & 1 ? (w & 0xFFFFu ? 0x3F80u : 0x4580u) : 0u) |
+                            (mine >> key & 2 ? (w >> 16 ? 0x3F80u : 0x4580u) : 0u) << 16;
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    f32x16_t t = {};
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      u32x4_t k;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t w = v[j][i >> 1][i & 1][e];
+        k[e] = odd_count(w & 0xFFFFu) | odd_count(w >> 16) << 16;
+      }
+      t = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, k),
+                                                  __builtin_bit_cast(bf16x8_t, n[j]), t, 0, 0, 0);
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      // (whole numbers, exact as far as they are told apart; no branches: 128 of them)
+      const int count = (int)fminf(t[r], 8192.f);
+      const float one = count & 63 ? INFINITY : 0.f, other = count >> 6 & 63 ? -INFINITY : 0.f;
+      c.acc[i][r] += count >= 4096 ? NAN : one + other;
+    }
+  }
+}
+
+// Inclusive sum of x over the workgroup's threads so far: `carry` before, the
+// whole added to it. red: one int per wave.
+__device__ __forceinline__ int block_scan(int x, int* red, int& carry) {
+  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+  x = wave_scan(x);
+  if (lane == kWave - 1) red[wv] = x;
+  __syncthreads();
+  x += carry;
+  for (int w = 0; w < kWaves; ++w) {
+    if (w < wv) x += red[w];
+    carry += red[w];
+  }
+  __syncthreads();
+  return x;
+}
+
+__global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a) {
+  __shared__ __attribute__((aligned(16))) bf16_t ring[kRing * kStage];
+  __shared__ int items_s[kMaxSeqs], base_s[kMaxSeqs];
+  __shared__ int red[kWaves], next_s[2];
+  const RowKeys& rk = a.rk;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int hf = lane >> 5, G = a.Hq / a.Hkv;
+
+  // Items: per sequence (tile, part) times key/value heads, the heads innermost:
+  // item % 8 is the XCD, so that the tiles of a head share that L2's keys where the
+  // heads are a multiple of 8.
+  int total = 0, n_parts = 0;
+  for (int s0 = 0; s0 < rk.n_seqs; s0 += kThreads) {
+    const int s = s0 + tid;
+    int ni = 0, np = 0;
+    if (s < rk.n_seqs) {
+      const PromptSeq x = prompt_seq(rk, s, G);
+      ni = x.tiles * x.splits * a.Hkv;
+      np = x.splits > 1 ? x.n * a.Hq * x.splits : 0;
+    }
+    const int i0 = block_scan(ni, red, total) - ni;
+    const int p0 = block_scan(np, red, n_parts) - np;
+    if (s < rk.n_seqs) {
+      items_s[s] = i0;
+      base_s[s] = p0;
+    }
+  }
+  __syncthreads();
+  if (n_parts > a.part_cap) total = 0;  // more rows than the call named: no room for their parts
+
+  // (The ring's address goes through a register of its own: the compiler would
+  // otherwise wait for every load in flight before each operand read.)
+  uint32_t ring_at = (uint32_t)(uintptr_t)(lds_void_t*)ring;
+  asm volatile("" : "+s"(ring_at));
+
+  // Workgroups draw the items of their XCD in order.
+  const int queues = gridDim.x % kXCDs == 0 ? kXCDs : 1;
+  const int queue = blockIdx.x % queues, per_queue = (int)gridDim.x / queues;
+  int drawn_k = blockIdx.x / queues;
+#pragma unroll 1
+  for (int k = 0;; ++k) {
+    const int item = drawn_k * queues + queue;
+    if (item >= total) break;
+    int drawn = 0;
+    if (tid == 0) drawn = per_queue + atomicAdd(a.counts + queue, 1);
+    int lo = 0, hi = rk.n_seqs - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (items_s[mid] <= item) lo = mid; else hi = mid - 1;
+    }
+    const int s = __builtin_amdgcn_readfirstlane(lo);
+    const PromptSeq x = prompt_seq(rk, s, G);
+    const int at = __builtin_amdgcn_readfirstlane(item - items_s[s]);
+    const int g = at % a.Hkv, sp = at / a.Hkv % x.splits;
+    // Later rows see more: their tiles first.
+    const int tile = x.tiles - 1 - at / a.Hkv / x.splits;
+    const int cols = x.n * G, tile0 = tile * kTileCols;
+    const int tile_end = min(cols, tile0 + kTileCols) - 1;
+    const WindowList list = window_list(max(x.first + tile0 / G, -1), x.first + tile_end / G,
+                                        rk.window, rk.sinks);
+    const int e0 = sp * x.part, e1 = min(list.entries, e0 + x.part);
+    const int stages = e1 > e0 ? (e1 - e0 + 1) / 2 : 0;
+
+    // A wave brings one tile of each stage, keys (waves 0, 2) or values of one of
+    // its two blocks; past the list the last block again, whose keys count as
+    // unseen. Called with st = 0, 1, ..: the blocks of 64 stages at a time in a
+    // register's lanes.
+    const int32_t* bt = rk.block_table + (int64_t)s * rk.max_blocks;
+    const bf16_t* cache = (wv & 1 ? a.v_cache : a.k_cache) + g * kTile + lane * 8;
+    int ids = 0;
+    auto issue = [&](int st) {
+      if ((st & 63) == 0) {
+        const int e = min(e0 + (st + lane) * 2 + (wv >> 1), e1 - 1);
+        ids = readable_block(bt[list.block(e)], rk.num_blocks);
+      }
+      const bf16_t* src =
+          cache + (int64_t)__builtin_amdgcn_readlane(ids, st & 63) * (a.Hkv * kTile);
+      const uint32_t dst = ring_at + ((st % kRing) * kStage + wv * kTile) * 2;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        __builtin_amdgcn_global_load_lds(src + i * 512, (lds_void_t*)(uintptr_t)(dst + i * 1024),
+                                         16, 0, 0);
+    };
+#pragma unroll 1
+    for (int st = 0; st < kRing - 1 && st < stages; ++st) issue(st);
+
+    // This lane's columns; columns past the last repeat it.
+    const int col0 = tile0 + wv * kCols;
+    const bool idle = col0 >= cols;
+    int p[2];
+    int64_t rowhead[2];
+    bf16x8_t qf[2][8];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int c = min(col0 + 32 * t + (lane & 31), cols - 1), j = c / G;
+      p[t] = max(x.first + j, -1);
+      rowhead[t] = (int64_t)(x.row0 + j) * a.Hq + g * G + (c - j * G);
+      const bf16_t* qp = a.q + rowhead[t] * HD + 8 * hf;
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        qf[t][i] = __builtin_bit_cast(bf16x8_t, *(const u32x4_t*)(qp + 16 * i));
+    }
+    // Stages that every column of the wave sees whole: from..to. (Among the window's
+    // blocks only; slots above p - window for the latest row, up to p for the first.)
+    const int p_low = max(x.first + min(col0, cols - 1) / G, -1),
+              p_high = x.first + min(col0 + kCols, cols) / G;
+    const int b_low = max(p_high - rk.window + kBlockTokens, 0) / kBlockTokens,
+              b_high = (p_low + 1) / kBlockTokens - 1;
+    const int from = (list.head + max(b_low - list.first, 0) - e0 + 1) >> 1,
+              to = ((min(list.head + b_high - list.first, e1 - 1) - e0 + 1) >> 1) - 1;
+
+    Cols c[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      c[t].m = -INFINITY;
+      c[t].l = 0.f;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) c[t].acc[i] = f32x16_t{};
+    }
+
+    // Before stage st + 1 is read: this wave's share of it is here, with later ones
+    // on their way, and every wave's; all are done with the values of st - 1.
+    auto begin = [&](int st) {
+      if (st + kRing - 2 < stages)
+        wait_vmcnt<4 * (kRing - 3)>();
+      else
+        wait_vmcnt<0>();
+      stage_barrier();
+      if (st + kRing - 1 < stages) issue(st + kRing - 1);
+    };
+    auto read_k = [&](int st, u32x4_t kf[8]) {
+      const bf16_t* kb = ring + (st % kRing) * kStage + (lane & 16 ? 2 * kTile : 0);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) kf[i] = *(const u32x4_t*)(kb + k_frag_off(lane, i));
+    };
+    // (Two runs of four keys 512 bytes apart by one read; the second operand's
+    // address is hidden, or the compiler would read 16 bytes at a time and move
+    // the halves.)
+    auto read_v = [&](int st, u32x4_t vf[2][2][2]) {
+      const bf16_t* v0 = ring + (st % kRing) * kStage + kTile +
+                         ((lane >> 4 & 1) * 64 + hf * 16 + (lane & 15)) * 8;
+      uint32_t lo = (uint32_t)(uintptr_t)(lds_bf16_t*)v0 + 8 * value_swap(lane & 31);
+      uint32_t hi = lo ^ 8;
+      asm volatile("" : "+v"(lo), "+v"(hi));
+      const lds_bf16_t* va = (const lds_bf16_t*)(uintptr_t)lo;
+      const lds_bf16_t* vb = (const lds_bf16_t*)(uintptr_t)hi;
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int d = 0; d < 2; ++d) {
+          const int off = j * 2 * kTile + d * 1024;
+          const u32x2_t a0 = *(const lds_u32x2_t*)(va + off),
+                        a1 = *(const lds_u32x2_t*)(va + off + 256);
+          const u32x2_t b0 = *(const lds_u32x2_t*)(vb + off),
+                        b1 = *(const lds_u32x2_t*)(vb + off + 256);
+          vf[j][d][0] = u32x4_t{a0.x, a0.y, a1.x, a1.y};
+          vf[j][d][1] = u32x4_t{b0.x, b0.y, b1.x, b1.y};
+        }
+    };
+    // The keys of stage st that a row of slot p sees, as bits.
+    auto stage_bits = [&](int st, int p) {
+      const int e = e0 + 2 * st;
+      uint32_t seen = window_bits(list.block(e) * kBlockTokens, p, rk.window, rk.sinks);
+      if (e + 1 < e1)
+        seen |= window_bits(list.block(e + 1) * kBlockTokens, p, rk.window, rk.sinks) << 16;
+      return seen;
+    };
+    auto whole = [&](int st) { return st >= from && st <= to; };
+
+    if (stages > kRing - 2)
+      wait_vmcnt<4 * (kRing - 2)>();
+    else
+      wait_vmcnt<0>();
+    stage_barrier();  // stage 0 is here
+    if (idle) {
+#pragma unroll 1
+      for (int st = 0; st + 1 < stages; ++st) begin(st);
+    } else if (stages > 0) {
+      u32x4_t kf[8], vf[2][2][2], pw[2][2];
+      f32x16_t z0, z1;
+      // Scores of a stage that not every column sees whole.
+      auto masked_scores = [&](int st) {
+        z0 = scores_of(kf, qf[0]);
+        z1 = scores_of(kf, qf[1]);
+        if (!whole(st)) {
+          mask_scores(z0, stage_bits(st, p[0]), hf);
+          mask_scores(z1, stage_bits(st, p[1]), hf);
+        }
+        rescale(c[0], z0, a.scale_log2);
+        weights_of(c[0], z0, a.scale_log2, pw[0]);
+      };
+      read_k(0, kf);
+      masked_scores(0);
+      if (stages > 1) {
+        begin(0);
+        read_k(1, kf);
+      }
+      int st = 0;
+      auto masked_step = [&]() {
+        read_v(st, vf);
+        const bool part = !whole(st), odd = part && mask_values(vf);
+        rescale(c[1], z1, a.scale_log2);
+        weights_of(c[1], z1, a.scale_log2, pw[1]);
+        add_values(c[0], vf, pw[0]);
+        add_values(c[1], vf, pw[1]);
+        if (odd) {
+          read_v(st, vf);
+          add_odd(c[0], vf, pw[0], stage_bits(st, p[0]), hf);
+          add_odd(c[1], vf, pw[1], stage_bits(st, p[1]), hf);
+        }
+        if (st + 1 < stages) {
+          masked_scores(st + 1);
+          if (st + 2 < stages) {
+            begin(st + 1);
+            read_k(st + 2, kf);
+          }
+        }
+      };
+      // Steps that need no mask have loops of their own on either side: one loop for
+      // both spilled 298 registers.
+      const int whole_end = min(to, stages - 2);
+#pragma unroll 1
+      for (; st < min(from, stages); ++st) masked_step();
+#pragma unroll 1
+      for (; st < whole_end; ++st) {
+        read_v(st, vf);
+        const f32x16_t n0 = scores_of(kf, qf[0]);
+        rescale(c[1], z1, a.scale_log2);
+        weights_of(c[1], z1, a.scale_log2, pw[1]);
+        add_values(c[0], vf, pw[0]);
+        z1 = scores_of(kf, qf[1]);
+        rescale(c[0], n0, a.scale_log2);
+        weights_of(c[0], n0, a.scale_log2, pw[0]);
+        begin(st + 1);
+        read_k(st + 2, kf);
+        add_values(c[1], vf, pw[1]);
+      }
+#pragma unroll 1
+      for (; st < stages; ++st) masked_step();
+    }
+    if (tid == 0) next_s[k & 1] = drawn;
+    __syncthreads();  // every wave is done with the ring
+    drawn_k = __builtin_amdgcn_readfirstlane(next_s[k & 1]);
+
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int col = col0 + 32 * t + (lane & 31);
+      const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(c[t].l),
+                                                       __float_as_uint(c[t].l), false, false);
+      if (col >= cols) continue;
+      const float L = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+      const float inv = L == 0.f ? 0.f : 1.0f / L;
+      const bool whole_row = x.splits == 1;
+      const int64_t idx = base_s[s] + (rowhead[t] - (int64_t)x.row0 * a.Hq) * x.splits + sp;
+      const int head = (int)(rowhead[t] % a.Hq), row = (int)(rowhead[t] / a.Hq);
+      bf16_t* out = a.o + (a.tiled ? tile_off(row, head * HD, a.Hq * HD) : rowhead[t] * HD);
+      // Runs of four dims from dim(v), v = 16 i + 4 (m / 8): m = 8 (r / 4) + 4 hf ..
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+          const f32x16_t& o = c[t].acc[i];
+          const int d = value_dim(i, 2 * r) + 4 * hf;
+          if (whole_row) {
+            // (four dims from a multiple of 4 are contiguous in tile order)
+            store4(out + (a.tiled ? (d >> 5) * 512 + (d >> 3 & 3) * 128 + (d & 7) : d), o[r] * inv,
+                   o[r + 1] * inv, o[r + 2] * inv, o[r + 3] * inv);
+          } else {
+            *(f32x4_t*)(a.part_o + idx * HD + d) = f32x4_t{o[r], o[r + 1], o[r + 2], o[r + 3]};
+          }
+        }
+      if (hf == 0) {
+        if (!whole_row)
+          *(f32x2_t*)(a.part_ml + 2 * idx) = f32x2_t{c[t].m, L};
+        else if (a.stats != nullptr)
+          *(f32x2_t*)(a.stats + 2 * rowhead[t]) = f32x2_t{c[t].m == -INFINITY ? 0.f : c[t].m, inv};
+      }
+    }
+  }
+  // The last workgroup leaves the counts as it found them.
+  if (tid == 0 && atomicAdd(a.counts + kXCDs, 1) == (int)gridDim.x - 1)
+    for (int i = 0; i <= kXCDs; ++i) atomicExch(a.counts + i, 0);
+}
+
+// The parts of a row's heads, in order: four dims per thread, 32 threads per head.
+constexpr int kMergeHeads = 4;
+__global__ __launch_bounds__(32 * kMergeHeads) void window_prompt_merge_kernel(PromptArgs a) {
+  __shared__ int at_s[2];
+  const RowKeys& rk = a.rk;
+  const int row = blockIdx.x + rk.seq_starts[0], G = a.Hq / a.Hkv;
+  if (row >= rk.seq_starts[rk.n_seqs]) return;
+  // The row's sequence, and the column parts of the sequences before it.
+  int s = 0;
+  for (int s0 = 1; s0 < rk.n_seqs; s0 += kWave) {
+    const int at = s0 + (threadIdx.x & 63);
+    s += __popcll(__ballot(at < rk.n_seqs && rk.seq_starts[at] <= row));
+  }
+  const PromptSeq x = prompt_seq(rk, s, G);
+  if (x.splits <= 1) return;
+  int before = 0;
+  for (int j = threadIdx.x; j < s; j += 32 * kMergeHeads) {
+    const PromptSeq y = prompt_seq(rk, j, G);
+    before += y.splits > 1 ? y.n * a.Hq * y.splits : 0;
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) before += __shfl_xor(before, o, kWave);
+  if ((threadIdx.x & 63) == 0) at_s[threadIdx.x >> 6] = before;
+  __syncthreads();
+  const int head = blockIdx.y * kMergeHeads + threadIdx.x / 32, dim = threadIdx.x % 32 * 4;
+  if (head >= a.Hq) return;
+  const int64_t idx = (int64_t)(at_s[0] + at_s[1]) +
+                      ((int64_t)(row - x.row0) * a.Hq + head) * x.splits;
+  if (idx + x.splits > a.part_cap) return;  // (as the parts' kernel)
+  float M = -INFINITY, L = 0.f;
+  f32x4_t y = {0.f, 0.f, 0.f, 0.f};
+  for (int p0 = 0; p0 < x.splits; p0 += 4) {
+    f32x4_t v[4];
+    f32x2_t ml[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int64_t i = idx + min(p0 + u, x.splits - 1);
+      ml[u] = *(const f32x2_t*)(a.part_ml + 2 * i);
+      v[u] = *(const f32x4_t*)(a.part_o + i * HD + dim);
+    }
+    float m_new = M;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) m_new = fmaxf(m_new, ml[u][0]);
+    const float ref = m_new == -INFINITY ? 0.f : m_new;
+    const float alpha = __builtin_amdgcn_exp2f(M - ref);
+    y *= alpha;
+    L *= alpha;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (p0 + u >= x.splits) break;
+      const float f = __builtin_amdgcn_exp2f(ml[u][0] - ref);
+      L = fmaf(f, ml[u][1], L);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) y[r] = fmaf(f, v[u][r], y[r]);
+    }
+    M = m_new;
+  }
+  const float inv = L == 0.f ? 0.f : 1.0f / L;
+  const int cc = head * HD + dim;
+  store4(a.o + (a.tiled ? tile_off(row, cc, a.Hq * HD) : (int64_t)row * a.Hq * HD + cc), y[0] * inv,
+         y[1] * inv, y[2] * inv, y[3] * inv);
+  if (a.stats != nullptr && dim == 0)
+    *(f32x2_t*)(a.stats + ((int64_t)row * a.Hq + head) * 2) =
+        f32x2_t{M == -INFINITY ? 0.f : M, inv};
+}
+
+}  // namespace
+
+// The most that any call of so many rows and sequences can need.
+int64_t window_column_parts(int64_t max_rows, int64_t max_seqs, int Hq, int Hkv) {
+  const int64_t cols = max_seqs * Hkv * kSplitCols;
+  return (cols < max_rows * Hq ? cols : max_rows * Hq) * kMaxParts;
+}
+
+hipError_t launch_window_prompt_bf16(const uint16_t* q, const uint16_t* k_cache,
+                                     const uint16_t* v_cache, const RowKeys& rk, int n_rows, int Hq,
+                                     int Hkv, uint16_t* o, bool tiled, float* part_o,
+                                     float* part_ml, int64_t part_cap, int32_t* counts,
+                                     float* stats, int num_cus, hipStream_t st) {
+  if (n_rows <= 0) return hipSuccess;
+  if (Hq > 16 * Hkv || num_cus <= 0) return hipErrorInvalidValue;
+  PromptArgs a;
+  a.q = q;
+  a.k_cache = k_cache;
+  a.v_cache = v_cache;
+  a.rk = rk;
+  a.Hq = Hq;
+  a.Hkv = Hkv;
+  a.scale_log2 = kLog2e / sqrtf((float)HD);
+  a.o = o;
+  a.tiled = tiled;
+  a.part_o = part_o;
+  a.part_ml = part_ml;
+  a.part_cap = part_cap;
+  a.counts = counts;
+  a.stats = stats;
+  // Whether any sequence's list can be in parts.
+  const int64_t w = ((int64_t)rk.window + n_rows + 2 * kBlockTokens - 2) / kBlockTokens +
+                    ((int64_t)rk.sinks + kBlockTokens - 1) / kBlockTokens;
+  const bool parts = w > kPartBlocks && rk.max_blocks > kPartBlocks;
+  // One workgroup per CU; batches of more than kMaxSeqs sequences in several
+  // launches, which share the partial buffers in turn.
+  for (int s0 = 0; s0 < rk.n_seqs; s0 += kMaxSeqs) {
+    a.rk.seq_starts = rk.seq_starts + s0;
+    a.rk.ctx_lens = rk.ctx_lens + s0;
+    a.rk.block_table = rk.block_table + (int64_t)s0 * rk.max_blocks;
+    a.rk.n_seqs = rk.n_seqs - s0 < kMaxSeqs ? rk.n_seqs - s0 : kMaxSeqs;
+    if (parts) {
+      COCO_LAUNCH(window_prompt_kernel, dim3(num_cus), dim3(kThreads), 0, st, a);
+      COCO_LAUNCH_LAST(window_prompt_merge_kernel,
+                       dim3(n_rows, (Hq + kMergeHeads - 1) / kMergeHeads), dim3(32 * kMergeHeads),
+                       0, st, a);
+    } else {
+      COCO_LAUNCH_LAST(window_prompt_kernel, dim3(num_cus), dim3(kThreads), 0, st, a);
+    }
+  }
+  return hipGetLastError();
+}
+
+}  // namespace coco
