@@ -157,14 +157,16 @@ struct Cols {
   f32x16_t acc[4];
 };
 
-// The running max of a column moves only when a step's largest score exceeds it by kLazy.
-__device__ __forceinline__ void rescale(Cols& c, const f32x16_t& z, float scale_log2) {
-  const float mx = max16(z);
+// The largest score of a column's 32 keys (this lane's 16: mx), in powers of two.
+__device__ __forceinline__ float column_top(float mx, float scale_log2) {
   const auto sw =
       __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
-  const float top = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * scale_log2;
+  return fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * scale_log2;
+}
+// The running max of a column moves only when a step's largest score exceeds it by kLazy.
+__device__ __forceinline__ void rescale(Cols& c, float top) {
   const float m_new = top > c.m + kLazy ? top : c.m;
-  if (__ballot(m_new != c.m) != 0) {
+  if (__builtin_expect(__ballot(m_new != c.m) != 0, 0)) {
     const float alpha = __builtin_amdgcn_exp2f(c.m - (m_new == -INFINITY ? 0.f : m_new));
 #pragma unroll
     for (int i = 0; i < 4; ++i) c.acc[i] *= alpha;
@@ -206,6 +208,50 @@ __device__ __forceinline__ void add_values(Cols& c, const u32x4_t v[2][2][2], co
       c.acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
           __builtin_bit_cast(bf16x8_t, v[j][i >> 1][i & 1]), __builtin_bit_cast(bf16x8_t, p[j]),
           c.acc[i], 0, 0, 0);
+}
+
+// Half a step: sixteen products, and beside each a sixteenth of the other tile's
+// softmax. The products: scores z of the next stage (k, q), then values v with
+// weights p for cv's columns. The softmax: weights w of scores zs for cs's columns.
+// top: the next scores' largest. `mid` runs between scores and values. Nothing is
+// moved from one sixteenth to another: left to itself, the compiler puts the
+// products back to back and the exponentials behind them, and a wave that is alone
+// on its SIMD then has one pipe idle at a time.
+template <typename F>
+__device__ __forceinline__ void half_step(const u32x4_t k[8], const bf16x8_t q[8], f32x16_t& z,
+                                          Cols& cv, const u32x4_t v[2][2][2], const u32x4_t p[2],
+                                          Cols& cs, const f32x16_t& zs, u32x4_t w[2], float& top,
+                                          float scale_log2, F mid) {
+  const float m_ref = cs.m == -INFINITY ? 0.f : cs.m;
+  z = f32x16_t{};
+  float pr[16], ls = 0.f, mx = 0.f;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    if (i == 8) mid();
+    if (i < 8)
+      z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, k[i]), q[i], z, 0, 0,
+                                                  0);
+    else
+      cv.acc[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+          __builtin_bit_cast(bf16x8_t, v[i >> 2 & 1][i >> 1 & 1][i & 1]),
+          __builtin_bit_cast(bf16x8_t, p[i >> 2 & 1]), cv.acc[i & 3], 0, 0, 0);
+    pr[i] = __builtin_amdgcn_exp2f(fmaf(zs[i], scale_log2, -m_ref));
+    if (i & 1) {
+      uint32_t both = pack_bf16x2(pr[i - 1], pr[i]);
+      ls += pr[i - 1] + pr[i];
+      asm volatile("" : "+v"(both), "+v"(ls));  // (here, not where it is used)
+      w[i >> 3][i >> 1 & 3] = both;
+    }
+    if (i == 11) mx = fmaxf(fmaxf(z[0], z[1]), z[2]);
+    if (i >= 12 && i < 15) {
+      mx = fmaxf(fmaxf(mx, z[4 * i - 45]), z[4 * i - 44]);
+      mx = fmaxf(fmaxf(mx, z[4 * i - 43]), z[4 * i - 42]);
+    }
+    if (i == 15) mx = fmaxf(mx, z[15]);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  cs.l += ls;
+  top = column_top(mx, scale_log2);
 }
 
 // The non-finite values of a stage for the columns that see their keys (seen). A
@@ -455,7 +501,7 @@ __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a
           mask_scores(z0, stage_bits(st, p[0]), hf);
           mask_scores(z1, stage_bits(st, p[1]), hf);
         }
-        rescale(c[0], z0, a.scale_log2);
+        rescale(c[0], column_top(max16(z0), a.scale_log2));
         weights_of(c[0], z0, a.scale_log2, pw[0]);
       };
       read_k(0, kf);
@@ -468,7 +514,7 @@ __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a
       auto masked_step = [&]() {
         read_v(st, vf);
         const bool part = !whole(st), odd = part && mask_values(vf);
-        rescale(c[1], z1, a.scale_log2);
+        rescale(c[1], column_top(max16(z1), a.scale_log2));
         weights_of(c[1], z1, a.scale_log2, pw[1]);
         add_values(c[0], vf, pw[0]);
         add_values(c[1], vf, pw[1]);
@@ -489,23 +535,27 @@ __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a
       // both spilled 298 registers.
       const int whole_end = min(to, stages - 2);
 #pragma unroll 1
-      for (; st < min(from, stages); ++st) masked_step();
+      while (__builtin_expect(st < min(from, stages), 0)) {
+        masked_step();
+        ++st;
+      }
+      float top0, top1 = column_top(max16(z1), a.scale_log2);
 #pragma unroll 1
-      for (; st < whole_end; ++st) {
+      while (__builtin_expect_with_probability(st < whole_end, 1, 0.999)) {
+        rescale(c[1], top1);
         read_v(st, vf);
-        const f32x16_t n0 = scores_of(kf, qf[0]);
-        rescale(c[1], z1, a.scale_log2);
-        weights_of(c[1], z1, a.scale_log2, pw[1]);
-        add_values(c[0], vf, pw[0]);
-        z1 = scores_of(kf, qf[1]);
-        rescale(c[0], n0, a.scale_log2);
-        weights_of(c[0], n0, a.scale_log2, pw[0]);
+        half_step(kf, qf[0], z0, c[0], vf, pw[0], c[1], z1, pw[1], top0, a.scale_log2, [] {});
+        rescale(c[0], top0);
         begin(st + 1);
-        read_k(st + 2, kf);
-        add_values(c[1], vf, pw[1]);
+        half_step(kf, qf[1], z1, c[1], vf, pw[1], c[0], z0, pw[0], top1, a.scale_log2,
+                  [&] { read_k(st + 2, kf); });
+        ++st;
       }
 #pragma unroll 1
-      for (; st < stages; ++st) masked_step();
+      while (__builtin_expect(st < stages, 0)) {
+        masked_step();
+        ++st;
+      }
     }
     if (tid == 0) next_s[k & 1] = drawn;
     __syncthreads();  // every wave is done with the ring
