@@ -163,9 +163,12 @@ __device__ __forceinline__ float column_top(float mx, float scale_log2) {
       __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
   return fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * scale_log2;
 }
-// The running max of a column moves only when a step's largest score exceeds it by kLazy.
-__device__ __forceinline__ void rescale(Cols& c, float top) {
-  const float m_new = top > c.m + kLazy ? top : c.m;
+// The running max of a column moves only when a step's largest score exceeds it by
+// kLazy: to m_new, where any column's moves.
+__device__ __forceinline__ float next_max(const Cols& c, float top) {
+  return top > c.m + kLazy ? top : c.m;
+}
+__device__ __forceinline__ void rescale(Cols& c, float m_new) {
   if (__builtin_expect(__ballot(m_new != c.m) != 0, 0)) {
     const float alpha = __builtin_amdgcn_exp2f(c.m - (m_new == -INFINITY ? 0.f : m_new));
 #pragma unroll
@@ -173,6 +176,9 @@ __device__ __forceinline__ void rescale(Cols& c, float top) {
     c.l *= alpha;
     c.m = m_new;
   }
+}
+__device__ __forceinline__ void rescale_for(Cols& c, const f32x16_t& z, float scale_log2) {
+  rescale(c, next_max(c, column_top(max16(z), scale_log2)));
 }
 
 // Weights of 32 keys as operands of two products.
@@ -213,21 +219,20 @@ __device__ __forceinline__ void add_values(Cols& c, const u32x4_t v[2][2][2], co
 // Half a step: sixteen products, and beside each a sixteenth of the other tile's
 // softmax. The products: scores z of the next stage (k, q), then values v with
 // weights p for cv's columns. The softmax: weights w of scores zs for cs's columns.
-// top: the next scores' largest. `mid` runs between scores and values. Nothing is
-// moved from one sixteenth to another: left to itself, the compiler puts the
-// products back to back and the exponentials behind them, and a wave that is alone
-// on its SIMD then has one pipe idle at a time.
+// m_next: cv's running max with the next scores. `lds(i)`: operand reads that go out
+// behind product i. Nothing is moved from one sixteenth to another: left to itself,
+// the compiler puts the products back to back and the exponentials behind them, and
+// a wave that is alone on its SIMD then has one pipe idle at a time.
 template <typename F>
 __device__ __forceinline__ void half_step(const u32x4_t k[8], const bf16x8_t q[8], f32x16_t& z,
                                           Cols& cv, const u32x4_t v[2][2][2], const u32x4_t p[2],
-                                          Cols& cs, const f32x16_t& zs, u32x4_t w[2], float& top,
-                                          float scale_log2, F mid) {
+                                          Cols& cs, const f32x16_t& zs, u32x4_t w[2], float& m_next,
+                                          float scale_log2, F lds) {
   const float m_ref = cs.m == -INFINITY ? 0.f : cs.m;
   z = f32x16_t{};
   float pr[16], ls = 0.f, mx = 0.f;
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
-    if (i == 8) mid();
     if (i < 8)
       z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, k[i]), q[i], z, 0, 0,
                                                   0);
@@ -235,6 +240,7 @@ __device__ __forceinline__ void half_step(const u32x4_t k[8], const bf16x8_t q[8
       cv.acc[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
           __builtin_bit_cast(bf16x8_t, v[i >> 2 & 1][i >> 1 & 1][i & 1]),
           __builtin_bit_cast(bf16x8_t, p[i >> 2 & 1]), cv.acc[i & 3], 0, 0, 0);
+    lds(i);
     pr[i] = __builtin_amdgcn_exp2f(fmaf(zs[i], scale_log2, -m_ref));
     if (i & 1) {
       uint32_t both = pack_bf16x2(pr[i - 1], pr[i]);
@@ -242,16 +248,14 @@ __device__ __forceinline__ void half_step(const u32x4_t k[8], const bf16x8_t q[8
       asm volatile("" : "+v"(both), "+v"(ls));  // (here, not where it is used)
       w[i >> 3][i >> 1 & 3] = both;
     }
-    if (i == 11) mx = fmaxf(fmaxf(z[0], z[1]), z[2]);
-    if (i >= 12 && i < 15) {
-      mx = fmaxf(fmaxf(mx, z[4 * i - 45]), z[4 * i - 44]);
-      mx = fmaxf(fmaxf(mx, z[4 * i - 43]), z[4 * i - 42]);
-    }
-    if (i == 15) mx = fmaxf(mx, z[15]);
+    if (i == 10) mx = fmaxf(fmaxf(fmaxf(z[0], z[1]), z[2]), fmaxf(z[3], z[4]));
+    if (i == 11) mx = fmaxf(fmaxf(fmaxf(mx, z[5]), z[6]), fmaxf(z[7], z[8]));
+    if (i == 12) mx = fmaxf(fmaxf(fmaxf(mx, z[9]), z[10]), fmaxf(z[11], z[12]));
+    if (i == 13) mx = column_top(fmaxf(fmaxf(fmaxf(mx, z[13]), z[14]), z[15]), scale_log2);
+    if (i == 14) m_next = next_max(cv, mx);
     __builtin_amdgcn_sched_barrier(0);
   }
   cs.l += ls;
-  top = column_top(mx, scale_log2);
 }
 
 // The non-finite values of a stage for the columns that see their keys (seen). A
@@ -443,34 +447,28 @@ __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a
       stage_barrier();
       if (st + kRing - 1 < stages) issue(st + kRing - 1);
     };
+    const bf16_t* const k_lane = ring + (lane & 16 ? 2 * kTile : 0) + k_frag_off(lane, 0);
     auto read_k = [&](int st, u32x4_t kf[8]) {
-      const bf16_t* kb = ring + (st % kRing) * kStage + (lane & 16 ? 2 * kTile : 0);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) kf[i] = *(const u32x4_t*)(kb + k_frag_off(lane, i));
+      for (int i = 0; i < 8; ++i)
+        kf[i] = *(const u32x4_t*)(k_lane + (st % kRing) * kStage + k_frag_off(lane, i) -
+                                  k_frag_off(lane, 0));
     };
-    // (Two runs of four keys 512 bytes apart by one read; the second operand's
-    // address is hidden, or the compiler would read 16 bytes at a time and move
-    // the halves.)
+    // Operand i (block i / 4, pair i / 2 % 2, half i % 2): two runs of four keys 512
+    // bytes apart by one read. (From an address that the compiler does not see
+    // through, or it would read the 16 bytes of both halves and move them.)
+    uint32_t v_lane = ring_at + (kTile + ((lane >> 4 & 1) * 64 + hf * 16 + (lane & 15)) * 8) * 2 +
+                      8 * value_swap(lane & 31);
+    asm volatile("" : "+v"(v_lane));
+    auto read_v_part = [&](uint32_t at, int i, u32x4_t vf[2][2][2]) {
+      const lds_bf16_t* x = (const lds_bf16_t*)(uintptr_t)(at ^ (i & 1) * 8) +
+                            (i >> 2) * 2 * kTile + (i >> 1 & 1) * 1024;
+      const u32x2_t a0 = *(const lds_u32x2_t*)x, a1 = *(const lds_u32x2_t*)(x + 256);
+      vf[i >> 2][i >> 1 & 1][i & 1] = u32x4_t{a0.x, a0.y, a1.x, a1.y};
+    };
     auto read_v = [&](int st, u32x4_t vf[2][2][2]) {
-      const bf16_t* v0 = ring + (st % kRing) * kStage + kTile +
-                         ((lane >> 4 & 1) * 64 + hf * 16 + (lane & 15)) * 8;
-      uint32_t lo = (uint32_t)(uintptr_t)(lds_bf16_t*)v0 + 8 * value_swap(lane & 31);
-      uint32_t hi = lo ^ 8;
-      asm volatile("" : "+v"(lo), "+v"(hi));
-      const lds_bf16_t* va = (const lds_bf16_t*)(uintptr_t)lo;
-      const lds_bf16_t* vb = (const lds_bf16_t*)(uintptr_t)hi;
 #pragma unroll
-      for (int j = 0; j < 2; ++j)
-#pragma unroll
-        for (int d = 0; d < 2; ++d) {
-          const int off = j * 2 * kTile + d * 1024;
-          const u32x2_t a0 = *(const lds_u32x2_t*)(va + off),
-                        a1 = *(const lds_u32x2_t*)(va + off + 256);
-          const u32x2_t b0 = *(const lds_u32x2_t*)(vb + off),
-                        b1 = *(const lds_u32x2_t*)(vb + off + 256);
-          vf[j][d][0] = u32x4_t{a0.x, a0.y, a1.x, a1.y};
-          vf[j][d][1] = u32x4_t{b0.x, b0.y, b1.x, b1.y};
-        }
+      for (int i = 0; i < 8; ++i) read_v_part(v_lane + (st % kRing) * (kStage * 2), i, vf);
     };
     // The keys of stage st that a row of slot p sees, as bits.
     auto stage_bits = [&](int st, int p) {
@@ -501,7 +499,7 @@ __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a
           mask_scores(z0, stage_bits(st, p[0]), hf);
           mask_scores(z1, stage_bits(st, p[1]), hf);
         }
-        rescale(c[0], column_top(max16(z0), a.scale_log2));
+        rescale_for(c[0], z0, a.scale_log2);
         weights_of(c[0], z0, a.scale_log2, pw[0]);
       };
       read_k(0, kf);
@@ -514,7 +512,7 @@ __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a
       auto masked_step = [&]() {
         read_v(st, vf);
         const bool part = !whole(st), odd = part && mask_values(vf);
-        rescale(c[1], column_top(max16(z1), a.scale_log2));
+        rescale_for(c[1], z1, a.scale_log2);
         weights_of(c[1], z1, a.scale_log2, pw[1]);
         add_values(c[0], vf, pw[0]);
         add_values(c[1], vf, pw[1]);
@@ -539,16 +537,20 @@ __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a
         masked_step();
         ++st;
       }
-      float top0, top1 = column_top(max16(z1), a.scale_log2);
+      float m0, m1 = next_max(c[1], column_top(max16(z1), a.scale_log2));
 #pragma unroll 1
       while (__builtin_expect_with_probability(st < whole_end, 1, 0.999)) {
-        rescale(c[1], top1);
-        read_v(st, vf);
-        half_step(kf, qf[0], z0, c[0], vf, pw[0], c[1], z1, pw[1], top0, a.scale_log2, [] {});
-        rescale(c[0], top0);
+        rescale(c[1], m1);
+        const uint32_t v_at = v_lane + (st % kRing) * (kStage * 2);
+        half_step(kf, qf[0], z0, c[0], vf, pw[0], c[1], z1, pw[1], m0, a.scale_log2, [&](int i) {
+          if (i < 8) read_v_part(v_at, i, vf);
+        });
+        rescale(c[0], m0);
         begin(st + 1);
-        half_step(kf, qf[1], z1, c[1], vf, pw[1], c[0], z0, pw[0], top1, a.scale_log2,
-                  [&] { read_k(st + 2, kf); });
+        const bf16_t* kb = k_lane + (st + 2) % kRing * kStage;
+        half_step(kf, qf[1], z1, c[1], vf, pw[1], c[0], z0, pw[0], m1, a.scale_log2, [&](int i) {
+          if (i >= 8) kf[i - 8] = *(const u32x4_t*)(kb + k_frag_off(lane, i - 8) - k_frag_off(lane, 0));
+        });
         ++st;
       }
 #pragma unroll 1
