@@ -30,6 +30,14 @@ SOURCES = ["rows.hip", "gemm_skinny.hip", "gemm_prefill_qkv.hip", "gemm_prefill_
            "window_weights.hip", "evict.hip",
            "coco_api.hip", "cache_api.hip", "probe.hip", "scaling.cpp"]
 
+# Products that write vector registers of their own choice: the prompt windows' scores
+# go straight to the vector unit, where 16 moves per tile and step would take them.
+SOURCE_FLAGS = {"window_prompt.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
+
+
+def flags_of(src: str) -> list:
+    return FLAGS + SOURCE_FLAGS.get(src, [])
+
 
 def build(verbose: bool = False, jobs: int = 8) -> str:
     if not os.path.exists(HIPCC):
@@ -40,7 +48,7 @@ def build(verbose: bool = False, jobs: int = 8) -> str:
     for src in SOURCES:
         obj = os.path.join(BUILD, os.path.splitext(src)[0] + ".o")
         objs.append(obj)
-        cmd = [HIPCC, *FLAGS, "-c", os.path.join(CSRC, src), "-o", obj]
+        cmd = [HIPCC, *flags_of(src), "-c", os.path.join(CSRC, src), "-o", obj]
         if verbose:
             print(" ".join(cmd), flush=True)
         procs.append((src, subprocess.Popen(cmd, stdout=subprocess.PIPE,

@@ -99,6 +99,12 @@ __device__ __forceinline__ PromptSeq prompt_seq(const RowKeys& rk, int s, int G)
   return x;
 }
 
+// Piece i of four, 1 KB each, of a cache tile into LDS at byte `to`.
+template <int I>
+__device__ __forceinline__ void load_tile(const bf16_t* from, uint32_t to) {
+  __builtin_amdgcn_global_load_lds(from, (lds_void_t*)(uintptr_t)to, 16, I * 1024, 0);
+}
+
 // Key fragments of two blocks: step s holds dims 16 s + 8 hf .. + 7 of key m.
 __device__ __forceinline__ int k_frag_off(int lane, int s) {
   const int hf = lane >> 5, t = lane & 15;
@@ -387,19 +393,25 @@ __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a
     const int32_t* bt = rk.block_table + (int64_t)s * rk.max_blocks;
     const bf16_t* cache = (wv & 1 ? a.v_cache : a.k_cache) + g * kTile + lane * 8;
     int ids = 0;
-    auto issue = [&](int st) {
+    auto source = [&](int st) {
       if ((st & 63) == 0) {
         const int e = min(e0 + (st + lane) * 2 + (wv >> 1), e1 - 1);
         ids = readable_block(bt[list.block(e)], rk.num_blocks);
       }
-      const bf16_t* src =
-          cache + (int64_t)__builtin_amdgcn_readlane(ids, st & 63) * (a.Hkv * kTile);
-      const uint32_t dst = ring_at + ((st % kRing) * kStage + wv * kTile) * 2;
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        __builtin_amdgcn_global_load_lds(src + i * 512, (lds_void_t*)(uintptr_t)(dst + i * 1024),
-                                         16, 0, 0);
+      return cache + (int64_t)__builtin_amdgcn_readlane(ids, st & 63) * (a.Hkv * kTile);
     };
+    auto place = [&](int st) { return ring_at + ((st % kRing) * kStage + wv * kTile) * 2; };
+    auto issue = [&](int st) {
+      const bf16_t* src = source(st);
+      load_tile<0>(src, place(st));
+      load_tile<1>(src, place(st));
+      load_tile<2>(src, place(st));
+      load_tile<3>(src, place(st));
+    };
+    // A list of fewer stages than fill the ring is brought whole before it is walked;
+    // otherwise every step brings one, past the end the last again, so that the
+    // loads on their way are always as many.
+    const bool deep = stages >= kRing - 1;
 #pragma unroll 1
     for (int st = 0; st < kRing - 1 && st < stages; ++st) issue(st);
 
@@ -438,14 +450,15 @@ __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a
     }
 
     // Before stage st + 1 is read: this wave's share of it is here, with later ones
-    // on their way, and every wave's; all are done with the values of st - 1.
+    // on their way, and every wave's; all are done with the values of st - 1, whose
+    // place the next stage takes.
     auto begin = [&](int st) {
-      if (st + kRing - 2 < stages)
+      if (deep)
         wait_vmcnt<4 * (kRing - 3)>();
       else
         wait_vmcnt<0>();
       stage_barrier();
-      if (st + kRing - 1 < stages) issue(st + kRing - 1);
+      if (deep) issue(st + kRing - 1);
     };
     const bf16_t* const k_lane = ring + (lane & 16 ? 2 * kTile : 0) + k_frag_off(lane, 0);
     auto read_k = [&](int st, u32x4_t kf[8]) {
@@ -479,8 +492,15 @@ __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a
       return seen;
     };
     auto whole = [&](int st) { return st >= from && st <= to; };
+    // Whether any column of the wave sees a key of stage st (its first and last blocks'
+    // slots against the wave's rows).
+    auto any_seen = [&](int st) {
+      const int t0 = list.block(e0 + 2 * st) * kBlockTokens;
+      const int t1 = list.block(min(e0 + 2 * st + 1, e1 - 1)) * kBlockTokens + kBlockTokens - 1;
+      return t0 <= p_high && (t1 > p_low - rk.window || t0 < rk.sinks);
+    };
 
-    if (stages > kRing - 2)
+    if (deep)
       wait_vmcnt<4 * (kRing - 2)>();
     else
       wait_vmcnt<0>();
@@ -491,16 +511,19 @@ __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a
     } else if (stages > 0) {
       u32x4_t kf[8], vf[2][2][2], pw[2][2];
       f32x16_t z0, z1;
-      // Scores of a stage that not every column sees whole.
+      // Scores of a stage that not every column sees whole; a stage that none sees
+      // costs no products.
       auto masked_scores = [&](int st) {
-        z0 = scores_of(kf, qf[0]);
-        z1 = scores_of(kf, qf[1]);
-        if (!whole(st)) {
-          mask_scores(z0, stage_bits(st, p[0]), hf);
-          mask_scores(z1, stage_bits(st, p[1]), hf);
+        if (any_seen(st)) {
+          z0 = scores_of(kf, qf[0]);
+          z1 = scores_of(kf, qf[1]);
+          if (!whole(st)) {
+            mask_scores(z0, stage_bits(st, p[0]), hf);
+            mask_scores(z1, stage_bits(st, p[1]), hf);
+          }
+          rescale_for(c[0], z0, a.scale_log2);
+          weights_of(c[0], z0, a.scale_log2, pw[0]);
         }
-        rescale_for(c[0], z0, a.scale_log2);
-        weights_of(c[0], z0, a.scale_log2, pw[0]);
       };
       read_k(0, kf);
       masked_scores(0);
@@ -510,16 +533,18 @@ __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a
       }
       int st = 0;
       auto masked_step = [&]() {
-        read_v(st, vf);
-        const bool part = !whole(st), odd = part && mask_values(vf);
-        rescale_for(c[1], z1, a.scale_log2);
-        weights_of(c[1], z1, a.scale_log2, pw[1]);
-        add_values(c[0], vf, pw[0]);
-        add_values(c[1], vf, pw[1]);
-        if (odd) {
+        if (any_seen(st)) {
           read_v(st, vf);
-          add_odd(c[0], vf, pw[0], stage_bits(st, p[0]), hf);
-          add_odd(c[1], vf, pw[1], stage_bits(st, p[1]), hf);
+          const bool part = !whole(st), odd = part && mask_values(vf);
+          rescale_for(c[1], z1, a.scale_log2);
+          weights_of(c[1], z1, a.scale_log2, pw[1]);
+          add_values(c[0], vf, pw[0]);
+          add_values(c[1], vf, pw[1]);
+          if (odd) {
+            read_v(st, vf);
+            add_odd(c[0], vf, pw[0], stage_bits(st, p[0]), hf);
+            add_odd(c[1], vf, pw[1], stage_bits(st, p[1]), hf);
+          }
         }
         if (st + 1 < stages) {
           masked_scores(st + 1);
@@ -531,7 +556,7 @@ __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a
       };
       // Steps that need no mask have loops of their own on either side: one loop for
       // both spilled 298 registers.
-      const int whole_end = min(to, stages - 2);
+      const int whole_end = deep ? min(to, stages - 2) : 0;
 #pragma unroll 1
       while (__builtin_expect(st < min(from, stages), 0)) {
         masked_step();
@@ -546,9 +571,17 @@ __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a
           if (i < 8) read_v_part(v_at, i, vf);
         });
         rescale(c[0], m0);
-        begin(st + 1);
+        // begin(st + 1), its loads beside the first products.
+        wait_vmcnt<4 * (kRing - 3)>();
+        stage_barrier();
+        const bf16_t* src = source(st + kRing);
+        const uint32_t dst = place(st + kRing);
         const bf16_t* kb = k_lane + (st + 2) % kRing * kStage;
         half_step(kf, qf[1], z1, c[1], vf, pw[1], c[0], z0, pw[0], m1, a.scale_log2, [&](int i) {
+          if (i == 0) load_tile<0>(src, dst);
+          if (i == 1) load_tile<1>(src, dst);
+          if (i == 2) load_tile<2>(src, dst);
+          if (i == 3) load_tile<3>(src, dst);
           if (i >= 8) kf[i - 8] = *(const u32x4_t*)(kb + k_frag_off(lane, i - 8) - k_frag_off(lane, 0));
         });
         ++st;
@@ -560,6 +593,7 @@ __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a
       }
     }
     if (tid == 0) next_s[k & 1] = drawn;
+    wait_vmcnt<0>();  // (the stages past the end)
     __syncthreads();  // every wave is done with the ring
     drawn_k = __builtin_amdgcn_readfirstlane(next_s[k & 1]);
 
@@ -604,33 +638,52 @@ __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a
 }
 
 // The parts of a row's heads, in order: four dims per thread, 32 threads per head.
-constexpr int kMergeHeads = 4;
-__global__ __launch_bounds__(32 * kMergeHeads) void window_prompt_merge_kernel(PromptArgs a) {
-  __shared__ int at_s[2];
+// Workgroup b has the b-th row of those of sequences in parts.
+constexpr int kMergeHeads = 4, kMergeThreads = 32 * kMergeHeads;
+__global__ __launch_bounds__(kMergeThreads) void window_prompt_merge_kernel(PromptArgs a) {
+  __shared__ int rows_s[kMergeThreads / kWave], parts_s[kMergeThreads / kWave], found[3];
   const RowKeys& rk = a.rk;
-  const int row = blockIdx.x + rk.seq_starts[0], G = a.Hq / a.Hkv;
-  if (row >= rk.seq_starts[rk.n_seqs]) return;
-  // The row's sequence, and the column parts of the sequences before it.
-  int s = 0;
-  for (int s0 = 1; s0 < rk.n_seqs; s0 += kWave) {
-    const int at = s0 + (threadIdx.x & 63);
-    s += __popcll(__ballot(at < rk.n_seqs && rk.seq_starts[at] <= row));
+  const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, G = a.Hq / a.Hkv;
+  if (tid == 0) found[0] = -1;
+  int rows = 0, parts = 0;  // of the sequences so far
+  for (int s0 = 0; s0 < rk.n_seqs && rows <= (int)blockIdx.x; s0 += kMergeThreads) {
+    int n = 0, np = 0;
+    if (s0 + tid < rk.n_seqs) {
+      const PromptSeq y = prompt_seq(rk, s0 + tid, G);
+      n = y.splits > 1 ? y.n : 0;
+      np = y.splits > 1 ? y.n * a.Hq * y.splits : 0;
+    }
+    int row1 = wave_scan(n), part1 = wave_scan(np);
+    if (lane == kWave - 1) {
+      rows_s[wv] = row1;
+      parts_s[wv] = part1;
+    }
+    __syncthreads();
+    row1 += rows;
+    part1 += parts;
+    for (int w = 0; w < kMergeThreads / kWave; ++w) {
+      if (w < wv) {
+        row1 += rows_s[w];
+        part1 += parts_s[w];
+      }
+      rows += rows_s[w];
+      parts += parts_s[w];
+    }
+    if (row1 - n <= (int)blockIdx.x && (int)blockIdx.x < row1) {
+      found[0] = s0 + tid;
+      found[1] = (int)blockIdx.x - (row1 - n);
+      found[2] = part1 - np;
+    }
+    __syncthreads();
   }
-  const PromptSeq x = prompt_seq(rk, s, G);
-  if (x.splits <= 1) return;
-  int before = 0;
-  for (int j = threadIdx.x; j < s; j += 32 * kMergeHeads) {
-    const PromptSeq y = prompt_seq(rk, j, G);
-    before += y.splits > 1 ? y.n * a.Hq * y.splits : 0;
-  }
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) before += __shfl_xor(before, o, kWave);
-  if ((threadIdx.x & 63) == 0) at_s[threadIdx.x >> 6] = before;
   __syncthreads();
-  const int head = blockIdx.y * kMergeHeads + threadIdx.x / 32, dim = threadIdx.x % 32 * 4;
+  const int s = found[0];
+  if (s < 0) return;
+  const PromptSeq x = prompt_seq(rk, s, G);
+  const int row = x.row0 + found[1];
+  const int head = blockIdx.y * kMergeHeads + tid / 32, dim = tid % 32 * 4;
   if (head >= a.Hq) return;
-  const int64_t idx = (int64_t)(at_s[0] + at_s[1]) +
-                      ((int64_t)(row - x.row0) * a.Hq + head) * x.splits;
+  const int64_t idx = (int64_t)found[2] + ((int64_t)found[1] * a.Hq + head) * x.splits;
   if (idx + x.splits > a.part_cap) return;  // (as the parts' kernel)
   float M = -INFINITY, L = 0.f;
   f32x4_t y = {0.f, 0.f, 0.f, 0.f};
@@ -712,9 +765,10 @@ hipError_t launch_window_prompt_bf16(const uint16_t* q, const uint16_t* k_cache,
     a.rk.n_seqs = rk.n_seqs - s0 < kMaxSeqs ? rk.n_seqs - s0 : kMaxSeqs;
     if (parts) {
       COCO_LAUNCH(window_prompt_kernel, dim3(num_cus), dim3(kThreads), 0, st, a);
+      const int64_t most = (int64_t)a.rk.n_seqs * (kSplitCols / (Hq / Hkv));
       COCO_LAUNCH_LAST(window_prompt_merge_kernel,
-                       dim3(n_rows, (Hq + kMergeHeads - 1) / kMergeHeads), dim3(32 * kMergeHeads),
-                       0, st, a);
+                       dim3(most < n_rows ? (int)most : n_rows, (Hq + kMergeHeads - 1) / kMergeHeads),
+                       dim3(kMergeThreads), 0, st, a);
     } else {
       COCO_LAUNCH_LAST(window_prompt_kernel, dim3(num_cus), dim3(kThreads), 0, st, a);
     }
