@@ -433,7 +433,7 @@ hipError_t launch_window_decode_bf16(const uint16_t* q, const uint16_t* k_cache,
 // counts [kWindowCounts] must be zero and is left so. stats (null: not asked for)
 // [rows][Hq][2]: each row's running maximum (in powers of two) and 1 / its sum
 // of weights (0: it sees nothing).
-constexpr int kWindowCounts = 16, kWindowLaunchSeqs = 1024;
+constexpr int kWindowCounts = 16, kWindowLaunchSeqs = 512;
 int64_t window_column_parts(int64_t max_rows, int64_t max_seqs, int Hq, int Hkv);
 hipError_t launch_window_prompt_bf16(const uint16_t* q, const uint16_t* k_cache,
                                      const uint16_t* v_cache, const RowKeys& rk, int n_rows, int Hq,

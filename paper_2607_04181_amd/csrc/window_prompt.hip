@@ -81,9 +81,10 @@ struct PromptArgs {
 };
 
 // A sequence's rows: N of slots first .. first + N - 1, C columns per key/value
-// head in `tiles` workgroup tiles, and the parts of its list.
+// head in `tiles` workgroup tiles, and the parts of its list. item0, part0: its
+// first work item and column part.
 struct PromptSeq {
-  int row0, n, first, tiles, part, splits;
+  int row0, n, first, tiles, part, splits, item0, part0;
 };
 __device__ __forceinline__ PromptSeq prompt_seq(const RowKeys& rk, int s, int G) {
   PromptSeq x;
@@ -96,8 +97,12 @@ __device__ __forceinline__ PromptSeq prompt_seq(const RowKeys& rk, int s, int G)
   const int entries = window_list(max(x.first, -1), len - 1, rk.window, rk.sinks).entries;
   x.part = window_part(cols, entries);
   x.splits = max(1, (entries + x.part - 1) / x.part);
+  x.item0 = x.part0 = 0;
   return x;
 }
+// x / d for x < 4096 and d <= 16, by a product with inv = small_inv(d).
+__device__ __forceinline__ uint32_t small_inv(int d) { return (65535u + d) / d; }
+__device__ __forceinline__ int small_div(int x, uint32_t inv) { return (int)(x * inv >> 16); }
 
 // Piece i of four, 1 KB each, of a cache tile into LDS at byte `to`.
 template <int I>
@@ -131,29 +136,38 @@ __device__ __forceinline__ float max16(const f32x16_t& s) {
 __device__ __forceinline__ void mask_scores(f32x16_t& s, uint32_t seen, int hf) {
   const uint32_t mine = seen >> (4 * hf);
 #pragma unroll
-  for (int r = 0; r < 16; ++r) s[r] = (mine >> (8 * (r / 4) + r % 4) & 1) ? s[r] : -INFINITY;
+  for (int r = 0; r < 16; ++r) {
+    // (a bit spread over a word: comparisons would take 32 scalar registers)
+    const uint32_t m = (uint32_t)((int32_t)(mine << (31 - (8 * (r / 4) + r % 4))) >> 31);
+    s[r] = __uint_as_float((m & __float_as_uint(s[r])) | (~m & 0xFF800000u));
+  }
 }
 
 // A product with a weight of 0 would let a non-finite value of a key that some
-// columns do not see, or of a slot that holds anything, reach them: such elements
-// are left out (add_odd gives them to the columns that see the key). Whether there
-// were any, for the wave.
-__device__ __forceinline__ bool mask_values(u32x4_t v[2][2][2]) {
-  bool odd = false;
+// columns do not see, or of a slot that holds anything, reach them. Whether any of
+// the wave's values is one: their exponents' bits, plus one, carry.
+__device__ __forceinline__ bool any_odd(const u32x4_t v[2][2][2]) {
+  uint32_t odd = 0;
+#pragma unroll
+  for (int j = 0; j < 2; ++j)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) odd |= (v[j][i >> 1][i & 1][e] & 0x7F807F80u) + 0x00800080u;
+  return __ballot((odd & 0x80008000u) != 0) != 0;
+}
+// Such values are left out (add_odd gives them to the columns that see the key).
+__device__ __forceinline__ void drop_odd(u32x4_t v[2][2][2]) {
 #pragma unroll
   for (int j = 0; j < 2; ++j)
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        uint32_t w = v[j][i >> 1][i & 1][e];
-        const bool lo = (w & 0x7F80u) == 0x7F80u, hi = (w & 0x7F800000u) == 0x7F800000u;
-        if (lo) w &= 0xFFFF0000u;
-        if (hi) w &= 0xFFFFu;
-        odd |= lo | hi;
-        v[j][i >> 1][i & 1][e] = w;
+        const uint32_t w = v[j][i >> 1][i & 1][e];
+        const uint32_t x = ((w & 0x7F807F80u) + 0x00800080u) & 0x80008000u;
+        v[j][i >> 1][i & 1][e] = w & ~(x | (x - (x >> 15)));
       }
-  return __ballot(odd) != 0;
 }
 
 // One tile's columns: running softmax and O^T. acc[i][r]: dim value_dim(i, m), m =
@@ -324,12 +338,13 @@ __device__ __forceinline__ int block_scan(int x, int* red, int& carry) {
 
 __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a) {
   __shared__ __attribute__((aligned(16))) bf16_t ring[kRing * kStage];
-  __shared__ int items_s[kMaxSeqs], base_s[kMaxSeqs];
+  __shared__ PromptSeq seqs_s[kMaxSeqs];
   __shared__ int red[kWaves], next_s[2];
   const RowKeys& rk = a.rk;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int hf = lane >> 5, G = a.Hq / a.Hkv;
+  const uint32_t inv_G = small_inv(G);
 
   // Items: per sequence (tile, part) times key/value heads, the heads innermost:
   // item % 8 is the XCD, so that the tiles of a head share that L2's keys where the
@@ -337,18 +352,13 @@ __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a
   int total = 0, n_parts = 0;
   for (int s0 = 0; s0 < rk.n_seqs; s0 += kThreads) {
     const int s = s0 + tid;
-    int ni = 0, np = 0;
-    if (s < rk.n_seqs) {
-      const PromptSeq x = prompt_seq(rk, s, G);
-      ni = x.tiles * x.splits * a.Hkv;
-      np = x.splits > 1 ? x.n * a.Hq * x.splits : 0;
-    }
-    const int i0 = block_scan(ni, red, total) - ni;
-    const int p0 = block_scan(np, red, n_parts) - np;
-    if (s < rk.n_seqs) {
-      items_s[s] = i0;
-      base_s[s] = p0;
-    }
+    PromptSeq x{};
+    if (s < rk.n_seqs) x = prompt_seq(rk, s, G);
+    const int ni = x.tiles * x.splits * a.Hkv;
+    const int np = x.splits > 1 ? x.n * a.Hq * x.splits : 0;
+    x.item0 = block_scan(ni, red, total) - ni;
+    x.part0 = block_scan(np, red, n_parts) - np;
+    if (s < rk.n_seqs) seqs_s[s] = x;
   }
   __syncthreads();
   if (n_parts > a.part_cap) total = 0;  // more rows than the call named: no room for their parts
@@ -371,21 +381,41 @@ __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a
     int lo = 0, hi = rk.n_seqs - 1;
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
-      if (items_s[mid] <= item) lo = mid; else hi = mid - 1;
+      if (seqs_s[mid].item0 <= item) lo = mid; else hi = mid - 1;
     }
     const int s = __builtin_amdgcn_readfirstlane(lo);
-    const PromptSeq x = prompt_seq(rk, s, G);
-    const int at = __builtin_amdgcn_readfirstlane(item - items_s[s]);
-    const int g = at % a.Hkv, sp = at / a.Hkv % x.splits;
+    const PromptSeq& sq = seqs_s[s];
+    auto one = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+    const int row0 = one(sq.row0), first = one(sq.first), cols = one(sq.n) * G;
+    const int splits = one(sq.splits), part = one(sq.part), part0 = one(sq.part0);
+    const int at = one(item - sq.item0), at_head = at / a.Hkv;
+    const int g = at - at_head * a.Hkv, later = at_head / splits, sp = at_head - later * splits;
     // Later rows see more: their tiles first.
-    const int tile = x.tiles - 1 - at / a.Hkv / x.splits;
-    const int cols = x.n * G, tile0 = tile * kTileCols;
-    const int tile_end = min(cols, tile0 + kTileCols) - 1;
-    const WindowList list = window_list(max(x.first + tile0 / G, -1), x.first + tile_end / G,
+    const int tile0 = (one(sq.tiles) - 1 - later) * kTileCols;
+    const int j_tile = tile0 / G, r_tile = tile0 - j_tile * G;  // its first column's row and head
+    const int tile_last = min(cols - tile0, kTileCols) - 1;     // its last column
+    const WindowList list = window_list(max(first + j_tile, -1),
+                                        first + j_tile + small_div(r_tile + tile_last, inv_G),
                                         rk.window, rk.sinks);
-    const int e0 = sp * x.part, e1 = min(list.entries, e0 + x.part);
+    const int e0 = sp * part, e1 = min(list.entries, e0 + part);
     const int stages = e1 > e0 ? (e1 - e0 + 1) / 2 : 0;
 
+    // This lane's columns; columns past the last repeat it. row, head: in the call.
+    const int wave0 = wv * kCols;
+    const bool idle = wave0 > tile_last;
+    int p[2], row[2], head[2];
+    bf16x8_t qf[2][8];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int c = r_tile + min(wave0 + 32 * t + (lane & 31), tile_last), j = small_div(c, inv_G);
+      p[t] = max(first + j_tile + j, -1);
+      row[t] = row0 + j_tile + j;
+      head[t] = g * G + c - j * G;
+      const bf16_t* qp = a.q + ((int64_t)row[t] * a.Hq + head[t]) * HD + 8 * hf;
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        qf[t][i] = __builtin_bit_cast(bf16x8_t, *(const u32x4_t*)(qp + 16 * i));
+    }
     // A wave brings one tile of each stage, keys (waves 0, 2) or values of one of
     // its two blocks; past the list the last block again, whose keys count as
     // unseen. Called with st = 0, 1, ..: the blocks of 64 stages at a time in a
@@ -408,37 +438,18 @@ __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a
       load_tile<2>(src, place(st));
       load_tile<3>(src, place(st));
     };
-    // A list of fewer stages than fill the ring is brought whole before it is walked;
-    // otherwise every step brings one, past the end the last again, so that the
-    // loads on their way are always as many.
-    const bool deep = stages >= kRing - 1;
 #pragma unroll 1
     for (int st = 0; st < kRing - 1 && st < stages; ++st) issue(st);
 
-    // This lane's columns; columns past the last repeat it.
-    const int col0 = tile0 + wv * kCols;
-    const bool idle = col0 >= cols;
-    int p[2];
-    int64_t rowhead[2];
-    bf16x8_t qf[2][8];
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const int c = min(col0 + 32 * t + (lane & 31), cols - 1), j = c / G;
-      p[t] = max(x.first + j, -1);
-      rowhead[t] = (int64_t)(x.row0 + j) * a.Hq + g * G + (c - j * G);
-      const bf16_t* qp = a.q + rowhead[t] * HD + 8 * hf;
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        qf[t][i] = __builtin_bit_cast(bf16x8_t, *(const u32x4_t*)(qp + 16 * i));
-    }
     // Stages that every column of the wave sees whole: from..to. (Among the window's
     // blocks only; slots above p - window for the latest row, up to p for the first.)
-    const int p_low = max(x.first + min(col0, cols - 1) / G, -1),
-              p_high = x.first + min(col0 + kCols, cols) / G;
+    const int p_low = max(first + j_tile + small_div(r_tile + wave0, inv_G), -1),
+              p_high = first + j_tile + small_div(r_tile + min(wave0 + kCols - 1, tile_last), inv_G);
     const int b_low = max(p_high - rk.window + kBlockTokens, 0) / kBlockTokens,
               b_high = (p_low + 1) / kBlockTokens - 1;
     const int from = (list.head + max(b_low - list.first, 0) - e0 + 1) >> 1,
               to = ((min(list.head + b_high - list.first, e1 - 1) - e0 + 1) >> 1) - 1;
+    auto whole = [&](int st) { return st >= from && st <= to; };
 
     Cols c[2];
 #pragma unroll
@@ -450,15 +461,20 @@ __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a
     }
 
     // Before stage st + 1 is read: this wave's share of it is here, with later ones
-    // on their way, and every wave's; all are done with the values of st - 1, whose
-    // place the next stage takes.
-    auto begin = [&](int st) {
+    // on their way, and every wave's; all are done with stage st - 1, whose place
+    // the next one takes: past the end the last again, so that the loads on their way
+    // are always as many. (A list that does not fill the ring was brought whole.)
+    const bool deep = stages >= kRing - 1;
+    auto arrive = [&]() {
       if (deep)
         wait_vmcnt<4 * (kRing - 3)>();
       else
         wait_vmcnt<0>();
       stage_barrier();
-      if (deep) issue(st + kRing - 1);
+    };
+    auto begin = [&](int st) {
+      arrive();
+      issue(st + kRing - 1);
     };
     const bf16_t* const k_lane = ring + (lane & 16 ? 2 * kTile : 0) + k_frag_off(lane, 0);
     auto read_k = [&](int st, u32x4_t kf[8]) {
@@ -491,89 +507,67 @@ __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a
         seen |= window_bits(list.block(e + 1) * kBlockTokens, p, rk.window, rk.sinks) << 16;
       return seen;
     };
-    auto whole = [&](int st) { return st >= from && st <= to; };
-    // Whether any column of the wave sees a key of stage st (its first and last blocks'
-    // slots against the wave's rows).
-    auto any_seen = [&](int st) {
-      const int t0 = list.block(e0 + 2 * st) * kBlockTokens;
-      const int t1 = list.block(min(e0 + 2 * st + 1, e1 - 1)) * kBlockTokens + kBlockTokens - 1;
-      return t0 <= p_high && (t1 > p_low - rk.window || t0 < rk.sinks);
-    };
-
+    // (The queries are here: a wait for them inside the walk would be for every load.)
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) asm volatile("" : "+a"(qf[t][i]));
     if (deep)
       wait_vmcnt<4 * (kRing - 2)>();
     else
       wait_vmcnt<0>();
     stage_barrier();  // stage 0 is here
+    // (Every wave passes as many barriers: begin(0) .. begin(stages - 1) where there is
+    // more than one stage.)
     if (idle) {
 #pragma unroll 1
-      for (int st = 0; st + 1 < stages; ++st) begin(st);
+      for (int st = 0; stages > 1 && st < stages; ++st) begin(st);
     } else if (stages > 0) {
       u32x4_t kf[8], vf[2][2][2], pw[2][2];
       f32x16_t z0, z1;
-      // Scores of a stage that not every column sees whole; a stage that none sees
-      // costs no products.
-      auto masked_scores = [&](int st) {
-        if (any_seen(st)) {
-          z0 = scores_of(kf, qf[0]);
-          z1 = scores_of(kf, qf[1]);
-          if (!whole(st)) {
-            mask_scores(z0, stage_bits(st, p[0]), hf);
-            mask_scores(z1, stage_bits(st, p[1]), hf);
-          }
-          rescale_for(c[0], z0, a.scale_log2);
-          weights_of(c[0], z0, a.scale_log2, pw[0]);
-        }
+      float m0, m1;
+      // Scores of stage st where not every column sees all of it; m: the running max
+      // with them.
+      auto mask = [&](f32x16_t& z, float& m, int t, int st) {
+        mask_scores(z, stage_bits(st, p[t]), hf);
+        m = next_max(c[t], column_top(max16(z), a.scale_log2));
+      };
+      auto scores = [&](f32x16_t& z, float& m, int t, int st) {
+        z = scores_of(kf, qf[t]);
+        if (whole(st))
+          m = next_max(c[t], column_top(max16(z), a.scale_log2));
+        else
+          mask(z, m, t, st);
       };
       read_k(0, kf);
-      masked_scores(0);
+      scores(z0, m0, 0, 0);
+      scores(z1, m1, 1, 0);
+      rescale(c[0], m0);
+      weights_of(c[0], z0, a.scale_log2, pw[0]);
       if (stages > 1) {
         begin(0);
         read_k(1, kf);
       }
+      // Here and at the start of each step: tile 0's weights of stage st, tile 1's
+      // scores of it (m1 with them), the keys of st + 1.
       int st = 0;
-      auto masked_step = [&]() {
-        if (any_seen(st)) {
-          read_v(st, vf);
-          const bool part = !whole(st), odd = part && mask_values(vf);
-          rescale_for(c[1], z1, a.scale_log2);
-          weights_of(c[1], z1, a.scale_log2, pw[1]);
-          add_values(c[0], vf, pw[0]);
-          add_values(c[1], vf, pw[1]);
-          if (odd) {
-            read_v(st, vf);
-            add_odd(c[0], vf, pw[0], stage_bits(st, p[0]), hf);
-            add_odd(c[1], vf, pw[1], stage_bits(st, p[1]), hf);
-          }
-        }
-        if (st + 1 < stages) {
-          masked_scores(st + 1);
-          if (st + 2 < stages) {
-            begin(st + 1);
-            read_k(st + 2, kf);
-          }
-        }
-      };
-      // Steps that need no mask have loops of their own on either side: one loop for
-      // both spilled 298 registers.
-      const int whole_end = deep ? min(to, stages - 2) : 0;
 #pragma unroll 1
-      while (__builtin_expect(st < min(from, stages), 0)) {
-        masked_step();
-        ++st;
-      }
-      float m0, m1 = next_max(c[1], column_top(max16(z1), a.scale_log2));
-#pragma unroll 1
-      while (__builtin_expect_with_probability(st < whole_end, 1, 0.999)) {
+      while (__builtin_expect_with_probability(st + 1 < stages, 1, 0.99)) {
         rescale(c[1], m1);
+        if (__builtin_expect(!whole(st), 0)) {
+          read_v(st, vf);
+          if (any_odd(vf)) break;
+        }
         const uint32_t v_at = v_lane + (st % kRing) * (kStage * 2);
         half_step(kf, qf[0], z0, c[0], vf, pw[0], c[1], z1, pw[1], m0, a.scale_log2, [&](int i) {
-          if (i < 8) read_v_part(v_at, i, vf);
+          if (i < 2)
+#pragma unroll
+            for (int j = 4 * i; j < 4 * i + 4; ++j) read_v_part(v_at, j, vf);
         });
+        if (__builtin_expect(!whole(st + 1), 0)) mask(z0, m0, 0, st + 1);
         rescale(c[0], m0);
         // begin(st + 1), its loads beside the first products.
-        wait_vmcnt<4 * (kRing - 3)>();
-        stage_barrier();
+        arrive();
         const bf16_t* src = source(st + kRing);
         const uint32_t dst = place(st + kRing);
         const bf16_t* kb = k_lane + (st + 2) % kRing * kStage;
@@ -582,15 +576,36 @@ __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a
           if (i == 1) load_tile<1>(src, dst);
           if (i == 2) load_tile<2>(src, dst);
           if (i == 3) load_tile<3>(src, dst);
-          if (i >= 8) kf[i - 8] = *(const u32x4_t*)(kb + k_frag_off(lane, i - 8) - k_frag_off(lane, 0));
+          if (i >= 1 && i < 9)
+            kf[i - 1] = *(const u32x4_t*)(kb + k_frag_off(lane, i - 1) - k_frag_off(lane, 0));
         });
         ++st;
+        if (__builtin_expect(!whole(st), 0)) mask(z1, m1, 1, st);
       }
+      // The last stage; and all from one on with values that not every column may
+      // meet, one thing after the other. (Both in one loop spilled registers.)
 #pragma unroll 1
-      while (__builtin_expect(st < stages, 0)) {
-        masked_step();
-        ++st;
-      }
+      do {
+        read_v(st, vf);
+        const bool odd = !whole(st) && any_odd(vf);
+        if (odd) drop_odd(vf);
+        rescale(c[1], m1);
+        weights_of(c[1], z1, a.scale_log2, pw[1]);
+        add_values(c[0], vf, pw[0]);
+        add_values(c[1], vf, pw[1]);
+        if (odd) {
+          read_v(st, vf);
+          add_odd(c[0], vf, pw[0], stage_bits(st, p[0]), hf);
+          add_odd(c[1], vf, pw[1], stage_bits(st, p[1]), hf);
+        }
+        if (++st >= stages) break;
+        scores(z0, m0, 0, st);
+        scores(z1, m1, 1, st);
+        rescale(c[0], m0);
+        weights_of(c[0], z0, a.scale_log2, pw[0]);
+        begin(st);
+        read_k(st + 1, kf);
+      } while (true);
     }
     if (tid == 0) next_s[k & 1] = drawn;
     wait_vmcnt<0>();  // (the stages past the end)
@@ -599,24 +614,22 @@ __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a
 
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      const int col = col0 + 32 * t + (lane & 31);
       const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(c[t].l),
                                                        __float_as_uint(c[t].l), false, false);
-      if (col >= cols) continue;
+      if (wave0 + 32 * t + (lane & 31) > tile_last) continue;
       const float L = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
       const float inv = L == 0.f ? 0.f : 1.0f / L;
-      const bool whole_row = x.splits == 1;
-      const int64_t idx = base_s[s] + (rowhead[t] - (int64_t)x.row0 * a.Hq) * x.splits + sp;
-      const int head = (int)(rowhead[t] % a.Hq), row = (int)(rowhead[t] / a.Hq);
-      bf16_t* out = a.o + (a.tiled ? tile_off(row, head * HD, a.Hq * HD) : rowhead[t] * HD);
-      // Runs of four dims from dim(v), v = 16 i + 4 (m / 8): m = 8 (r / 4) + 4 hf ..
+      const int64_t rowhead = (int64_t)row[t] * a.Hq + head[t];
+      const int64_t idx = part0 + (rowhead - (int64_t)row0 * a.Hq) * splits + sp;
+      bf16_t* out = a.o + (a.tiled ? tile_off(row[t], head[t] * HD, a.Hq * HD) : rowhead * HD);
+      // Runs of four dims from the first of value_dim(i, m), m = 8 (r / 4) + 4 hf ..
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int r = 0; r < 16; r += 4) {
           const f32x16_t& o = c[t].acc[i];
           const int d = value_dim(i, 2 * r) + 4 * hf;
-          if (whole_row) {
+          if (splits == 1) {
             // (four dims from a multiple of 4 are contiguous in tile order)
             store4(out + (a.tiled ? (d >> 5) * 512 + (d >> 3 & 3) * 128 + (d & 7) : d), o[r] * inv,
                    o[r + 1] * inv, o[r + 2] * inv, o[r + 3] * inv);
@@ -625,10 +638,10 @@ __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a
           }
         }
       if (hf == 0) {
-        if (!whole_row)
+        if (splits > 1)
           *(f32x2_t*)(a.part_ml + 2 * idx) = f32x2_t{c[t].m, L};
         else if (a.stats != nullptr)
-          *(f32x2_t*)(a.stats + 2 * rowhead[t]) = f32x2_t{c[t].m == -INFINITY ? 0.f : c[t].m, inv};
+          *(f32x2_t*)(a.stats + 2 * rowhead) = f32x2_t{c[t].m == -INFINITY ? 0.f : c[t].m, inv};
       }
     }
   }
