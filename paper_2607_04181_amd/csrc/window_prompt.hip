@@ -250,7 +250,18 @@ __device__ __forceinline__ void half_step(const u32x4_t k[8], const bf16x8_t q[8
                                           float scale_log2, F lds) {
   const float m_ref = cs.m == -INFINITY ? 0.f : cs.m;
   z = f32x16_t{};
-  float pr[16], ls = 0.f, mx = 0.f;
+  // A result is used a sixteenth after it was asked for, or its latency would show:
+  // the exponential of score i stands behind product i, its argument one before, its
+  // sum and packing one or two behind.
+  float pr[16], l0 = 0.f, l1 = 0.f, mx = 0.f;
+  float x = fmaf(zs[0], scale_log2, -m_ref);
+  auto pack = [&](int i) {
+    uint32_t both = pack_bf16x2(pr[i], pr[i + 1]);
+    l0 += pr[i];
+    l1 += pr[i + 1];
+    asm volatile("" : "+v"(both), "+v"(l0), "+v"(l1));  // (here, not where they are used)
+    w[i >> 3][i >> 1 & 3] = both;
+  };
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
     if (i < 8)
@@ -261,13 +272,9 @@ __device__ __forceinline__ void half_step(const u32x4_t k[8], const bf16x8_t q[8
           __builtin_bit_cast(bf16x8_t, v[i >> 2 & 1][i >> 1 & 1][i & 1]),
           __builtin_bit_cast(bf16x8_t, p[i >> 2 & 1]), cv.acc[i & 3], 0, 0, 0);
     lds(i);
-    pr[i] = __builtin_amdgcn_exp2f(fmaf(zs[i], scale_log2, -m_ref));
-    if (i & 1) {
-      uint32_t both = pack_bf16x2(pr[i - 1], pr[i]);
-      ls += pr[i - 1] + pr[i];
-      asm volatile("" : "+v"(both), "+v"(ls));  // (here, not where it is used)
-      w[i >> 3][i >> 1 & 3] = both;
-    }
+    pr[i] = __builtin_amdgcn_exp2f(x);
+    if (i < 15) x = fmaf(zs[i + 1], scale_log2, -m_ref);
+    if (i >= 2 && i % 2 == 0) pack(i - 2);
     if (i == 10) mx = fmaxf(fmaxf(fmaxf(z[0], z[1]), z[2]), fmaxf(z[3], z[4]));
     if (i == 11) mx = fmaxf(fmaxf(fmaxf(mx, z[5]), z[6]), fmaxf(z[7], z[8]));
     if (i == 12) mx = fmaxf(fmaxf(fmaxf(mx, z[9]), z[10]), fmaxf(z[11], z[12]));
@@ -275,7 +282,8 @@ __device__ __forceinline__ void half_step(const u32x4_t k[8], const bf16x8_t q[8
     if (i == 14) m_next = next_max(cv, mx);
     __builtin_amdgcn_sched_barrier(0);
   }
-  cs.l += ls;
+  pack(14);
+  cs.l += l0 + l1;
 }
 
 // The non-finite values of a stage for the columns that see their keys (seen). A
