@@ -41,6 +41,7 @@ typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef __attribute__((address_space(3))) void lds_void_t;
 typedef __attribute__((address_space(3))) bf16_t lds_bf16_t;
 typedef __attribute__((address_space(3))) u32x2_t lds_u32x2_t;
+typedef __attribute__((address_space(3))) u32x4_t lds_u32x4_t;
 
 constexpr int HD = 128;
 constexpr float kLog2e = 1.4426950408889634f;
@@ -124,12 +125,17 @@ __device__ __forceinline__ int value_dim(int i, int m) {
   return 32 * (i & 2) + 32 * (m >> 4) + 16 * ((i & 1) ^ value_swap(m)) + (m & 15);
 }
 
-// Largest of 16 values (NaN loses).
+// The larger of two in one instruction (fmaxf quiets its operands first). With a NaN
+// the result is either: the column's weights are NaN then.
+__device__ __forceinline__ float max2(float a, float b) {
+  return __builtin_amdgcn_fmed3f(a, b, INFINITY);
+}
+// Largest of 16 values.
 __device__ __forceinline__ float max16(const f32x16_t& s) {
   float m = fmaxf(fmaxf(s[0], s[1]), s[2]);
 #pragma unroll
   for (int r = 3; r + 1 < 16; r += 2) m = fmaxf(fmaxf(m, s[r]), s[r + 1]);
-  return fmaxf(m, s[15]);
+  return max2(m, s[15]);
 }
 
 // -inf where the column does not see the key. Bit k of seen: key k of the 32.
@@ -156,6 +162,15 @@ __device__ __forceinline__ bool any_odd(const u32x4_t v[2][2][2]) {
       for (int e = 0; e < 4; ++e) odd |= (v[j][i >> 1][i & 1][e] & 0x7F807F80u) + 0x00800080u;
   return __ballot((odd & 0x80008000u) != 0) != 0;
 }
+// Whether any of a tile's sums is not a number, or infinities of both signs.
+__device__ __forceinline__ bool any_nan(const f32x16_t acc[4]) {
+  float t = 0.f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) t += acc[i][r];
+  return t != t;
+}
 // Such values are left out (add_odd gives them to the columns that see the key).
 __device__ __forceinline__ void drop_odd(u32x4_t v[2][2][2]) {
 #pragma unroll
@@ -170,6 +185,10 @@ __device__ __forceinline__ void drop_odd(u32x4_t v[2][2][2]) {
       }
 }
 
+// A column's running maximum before it has seen a key: below every score, and finite,
+// so that differences need no test.
+constexpr float kNoMax = -3.402823466e38f;
+
 // One tile's columns: running softmax and O^T. acc[i][r]: dim value_dim(i, m), m =
 // 8 (r / 4) + 4 hf + r % 4.
 struct Cols {
@@ -181,7 +200,7 @@ struct Cols {
 __device__ __forceinline__ float column_top(float mx, float scale_log2) {
   const auto sw =
       __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
-  return fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * scale_log2;
+  return max2(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * scale_log2;
 }
 // The running max of a column moves only when a step's largest score exceeds it by
 // kLazy: to m_new, where any column's moves.
@@ -190,24 +209,19 @@ __device__ __forceinline__ float next_max(const Cols& c, float top) {
 }
 __device__ __forceinline__ void rescale(Cols& c, float m_new) {
   if (__builtin_expect(__ballot(m_new != c.m) != 0, 0)) {
-    const float alpha = __builtin_amdgcn_exp2f(c.m - (m_new == -INFINITY ? 0.f : m_new));
+    const float alpha = __builtin_amdgcn_exp2f(c.m - m_new);
 #pragma unroll
     for (int i = 0; i < 4; ++i) c.acc[i] *= alpha;
     c.l *= alpha;
     c.m = m_new;
   }
 }
-__device__ __forceinline__ void rescale_for(Cols& c, const f32x16_t& z, float scale_log2) {
-  rescale(c, next_max(c, column_top(max16(z), scale_log2)));
-}
-
 // Weights of 32 keys as operands of two products.
 __device__ __forceinline__ void weights_of(Cols& c, const f32x16_t& z, float scale_log2,
                                            u32x4_t p[2]) {
-  const float m_ref = c.m == -INFINITY ? 0.f : c.m;
   float pr[16];
 #pragma unroll
-  for (int r = 0; r < 16; ++r) pr[r] = __builtin_amdgcn_exp2f(fmaf(z[r], scale_log2, -m_ref));
+  for (int r = 0; r < 16; ++r) pr[r] = __builtin_amdgcn_exp2f(fmaf(z[r], scale_log2, -c.m));
   float ls = 0.f;
 #pragma unroll
   for (int r = 0; r < 16; r += 4) ls += (pr[r] + pr[r + 1]) + (pr[r + 2] + pr[r + 3]);
@@ -240,28 +254,21 @@ __device__ __forceinline__ void add_values(Cols& c, const u32x4_t v[2][2][2], co
 // softmax. The products: scores z of the next stage (k, q), then values v with
 // weights p for cv's columns. The softmax: weights w of scores zs for cs's columns.
 // m_next: cv's running max with the next scores. `lds(i)`: operand reads that go out
-// behind product i. Nothing is moved from one sixteenth to another: left to itself,
-// the compiler puts the products back to back and the exponentials behind them, and
-// a wave that is alone on its SIMD then has one pipe idle at a time.
+// behind product i.
+// Nothing is moved from one sixteenth to another: left to itself, the compiler puts
+// the products back to back and the exponentials behind them, and a wave that is
+// alone on its SIMD then has one pipe idle at a time. A product takes 33 cycles and
+// lets 28 cycles of other instructions by, an exponential 8 and any other 4 to 5
+// (timed one by one), so every sixteenth has an exponential and about four others; a
+// result is used a sixteenth after it was asked for, or its latency would show.
 template <typename F>
 __device__ __forceinline__ void half_step(const u32x4_t k[8], const bf16x8_t q[8], f32x16_t& z,
                                           Cols& cv, const u32x4_t v[2][2][2], const u32x4_t p[2],
                                           Cols& cs, const f32x16_t& zs, u32x4_t w[2], float& m_next,
                                           float scale_log2, F lds) {
-  const float m_ref = cs.m == -INFINITY ? 0.f : cs.m;
   z = f32x16_t{};
-  // A result is used a sixteenth after it was asked for, or its latency would show:
-  // the exponential of score i stands behind product i, its argument one before, its
-  // sum and packing one or two behind.
-  float pr[16], l0 = 0.f, l1 = 0.f, mx = 0.f;
-  float x = fmaf(zs[0], scale_log2, -m_ref);
-  auto pack = [&](int i) {
-    uint32_t both = pack_bf16x2(pr[i], pr[i + 1]);
-    l0 += pr[i];
-    l1 += pr[i + 1];
-    asm volatile("" : "+v"(both), "+v"(l0), "+v"(l1));  // (here, not where they are used)
-    w[i >> 3][i >> 1 & 3] = both;
-  };
+  float pr[16], ls = 0.f, mx = 0.f, top = 0.f;
+  float x = fmaf(zs[0], scale_log2, -cs.m);
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
     if (i < 8)
@@ -273,17 +280,23 @@ __device__ __forceinline__ void half_step(const u32x4_t k[8], const bf16x8_t q[8
           __builtin_bit_cast(bf16x8_t, p[i >> 2 & 1]), cv.acc[i & 3], 0, 0, 0);
     lds(i);
     pr[i] = __builtin_amdgcn_exp2f(x);
-    if (i < 15) x = fmaf(zs[i + 1], scale_log2, -m_ref);
-    if (i >= 2 && i % 2 == 0) pack(i - 2);
-    if (i == 10) mx = fmaxf(fmaxf(fmaxf(z[0], z[1]), z[2]), fmaxf(z[3], z[4]));
-    if (i == 11) mx = fmaxf(fmaxf(fmaxf(mx, z[5]), z[6]), fmaxf(z[7], z[8]));
-    if (i == 12) mx = fmaxf(fmaxf(fmaxf(mx, z[9]), z[10]), fmaxf(z[11], z[12]));
-    if (i == 13) mx = column_top(fmaxf(fmaxf(fmaxf(mx, z[13]), z[14]), z[15]), scale_log2);
-    if (i == 14) m_next = next_max(cv, mx);
+    if (i < 15) x = fmaf(zs[i + 1], scale_log2, -cs.m);
+    if (i >= 1) ls = i == 1 ? pr[0] : ls + pr[i - 1];
+    if (i >= 2 && i % 2 == 0) w[i - 2 >> 3][i - 2 >> 1 & 3] = pack_bf16x2(pr[i - 2], pr[i - 1]);
+    if (i == 9) mx = fmaxf(fmaxf(z[0], z[1]), z[2]);
+    if (i == 10) mx = fmaxf(fmaxf(mx, z[3]), z[4]);
+    if (i == 11) mx = fmaxf(fmaxf(fmaxf(fmaxf(mx, z[5]), z[6]), z[7]), z[8]);
+    if (i == 12) mx = fmaxf(fmaxf(mx, z[9]), z[10]);
+    if (i == 13) mx = max2(fmaxf(fmaxf(fmaxf(fmaxf(mx, z[11]), z[12]), z[13]), z[14]), z[15]);
+    if (i == 14) top = column_top(mx, scale_log2);
+    // (here, not where they are used)
+    asm volatile("" : "+v"(pr[i]), "+v"(x), "+v"(ls), "+v"(mx));
+    if (i >= 2 && i % 2 == 0) asm volatile("" : "+v"(w[i - 2 >> 3][i - 2 >> 1 & 3]));
     __builtin_amdgcn_sched_barrier(0);
   }
-  pack(14);
-  cs.l += l0 + l1;
+  cs.l += ls + pr[15];
+  w[1][3] = pack_bf16x2(pr[14], pr[15]);
+  m_next = next_max(cv, top);
 }
 
 // The non-finite values of a stage for the columns that see their keys (seen). A
@@ -347,7 +360,7 @@ __device__ __forceinline__ int block_scan(int x, int* red, int& carry) {
 __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a) {
   __shared__ __attribute__((aligned(16))) bf16_t ring[kRing * kStage];
   __shared__ PromptSeq seqs_s[kMaxSeqs];
-  __shared__ int red[kWaves], next_s[2];
+  __shared__ int red[kWaves], next_s[2], bad_s[2];
   const RowKeys& rk = a.rk;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -379,90 +392,123 @@ __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a
   // Workgroups draw the items of their XCD in order.
   const int queues = gridDim.x % kXCDs == 0 ? kXCDs : 1;
   const int queue = blockIdx.x % queues, per_queue = (int)gridDim.x / queues;
-  int drawn_k = blockIdx.x / queues;
-#pragma unroll 1
-  for (int k = 0;; ++k) {
-    const int item = drawn_k * queues + queue;
-    if (item >= total) break;
-    int drawn = 0;
-    if (tid == 0) drawn = per_queue + atomicAdd(a.counts + queue, 1);
+  if (tid < 2) bad_s[tid] = 0;
+
+  // An item: one tile of one sequence and key/value head, and one part of its list.
+  struct Item {
+    int row0, first, splits, part0, sp, g;
+    int j_tile, r_tile;  // row of the tile's first column, and its head
+    int last;            // its last column
+    int e0, e1, stages;  // of its list
+    WindowList list;
+    const int32_t* bt;
+  };
+  Item it{};
+  auto one = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+  auto describe = [&](int item) {
     int lo = 0, hi = rk.n_seqs - 1;
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
       if (seqs_s[mid].item0 <= item) lo = mid; else hi = mid - 1;
     }
-    const int s = __builtin_amdgcn_readfirstlane(lo);
+    const int s = one(lo);
     const PromptSeq& sq = seqs_s[s];
-    auto one = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
-    const int row0 = one(sq.row0), first = one(sq.first), cols = one(sq.n) * G;
-    const int splits = one(sq.splits), part = one(sq.part), part0 = one(sq.part0);
-    const int at = one(item - sq.item0), at_head = at / a.Hkv;
-    const int g = at - at_head * a.Hkv, later = at_head / splits, sp = at_head - later * splits;
+    it.row0 = one(sq.row0);
+    it.first = one(sq.first);
+    it.splits = one(sq.splits);
+    it.part0 = one(sq.part0);
+    it.bt = rk.block_table + (int64_t)s * rk.max_blocks;
+    const int part = one(sq.part), at = one(item - sq.item0), at_head = at / a.Hkv;
+    it.g = at - at_head * a.Hkv;
+    const int later = at_head / it.splits;
+    it.sp = at_head - later * it.splits;
     // Later rows see more: their tiles first.
     const int tile0 = (one(sq.tiles) - 1 - later) * kTileCols;
-    const int j_tile = tile0 / G, r_tile = tile0 - j_tile * G;  // its first column's row and head
-    const int tile_last = min(cols - tile0, kTileCols) - 1;     // its last column
-    const WindowList list = window_list(max(first + j_tile, -1),
-                                        first + j_tile + small_div(r_tile + tile_last, inv_G),
-                                        rk.window, rk.sinks);
-    const int e0 = sp * part, e1 = min(list.entries, e0 + part);
-    const int stages = e1 > e0 ? (e1 - e0 + 1) / 2 : 0;
-
-    // This lane's columns; columns past the last repeat it. row, head: in the call.
-    const int wave0 = wv * kCols;
-    const bool idle = wave0 > tile_last;
-    int p[2], row[2], head[2];
-    bf16x8_t qf[2][8];
+    it.j_tile = tile0 / G;
+    it.r_tile = tile0 - it.j_tile * G;
+    it.last = min(one(sq.n) * G - tile0, kTileCols) - 1;
+    it.list = window_list(max(it.first + it.j_tile, -1),
+                          it.first + it.j_tile + small_div(it.r_tile + it.last, inv_G), rk.window,
+                          rk.sinks);
+    it.e0 = it.sp * part;
+    it.e1 = min(it.list.entries, it.e0 + part);
+    it.stages = it.e1 > it.e0 ? (it.e1 - it.e0 + 1) / 2 : 0;
+  };
+  // A wave brings one tile of each stage, keys (waves 0, 2) or values of one of
+  // its two blocks; past the list the last block again, whose keys count as
+  // unseen. Called with st = 0, 1, ..: the blocks of 64 stages at a time in a
+  // register's lanes.
+  int ids = 0;
+  auto refill = [&](int st) {
+    const int e = min(it.e0 + (st + lane) * 2 + (wv >> 1), it.e1 - 1);
+    ids = readable_block(it.bt[it.list.block(e)], rk.num_blocks);
+  };
+  auto source = [&](int st) {
+    return (wv & 1 ? a.v_cache : a.k_cache) +
+           ((int64_t)__builtin_amdgcn_readlane(ids, st & 63) * a.Hkv + it.g) * kTile;
+  };
+  auto place = [&](int st) { return ring_at + ((st % kRing) * kStage + wv * kTile) * 2; };
+  auto issue = [&](int st) {
+    if ((st & 63) == 0) refill(st);
+    const bf16_t* src = source(st) + lane * 8;
+    load_tile<0>(src, place(st));
+    load_tile<1>(src, place(st));
+    load_tile<2>(src, place(st));
+    load_tile<3>(src, place(st));
+  };
+  // This lane's columns; columns past the last repeat it. row, head: in the call.
+  const int wave0 = wv * kCols;
+  int p[2], row[2], head[2];
+  bf16x8_t qf[2][8];
+  auto columns = [&]() {
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      const int c = r_tile + min(wave0 + 32 * t + (lane & 31), tile_last), j = small_div(c, inv_G);
-      p[t] = max(first + j_tile + j, -1);
-      row[t] = row0 + j_tile + j;
-      head[t] = g * G + c - j * G;
+      const int c = it.r_tile + min(wave0 + 32 * t + (lane & 31), it.last), j = small_div(c, inv_G);
+      p[t] = max(it.first + it.j_tile + j, -1);
+      row[t] = it.row0 + it.j_tile + j;
+      head[t] = it.g * G + c - j * G;
+    }
+  };
+  auto begin_item = [&](int item) {
+    describe(item);
+#pragma unroll 1
+    for (int st = 0; st < kRing - 1 && st < it.stages; ++st) issue(st);
+  };
+
+  int drawn_k = blockIdx.x / queues;
+  int drawn = 0;
+  bool careful = false;  // an item that is done again
+  if (drawn_k * queues + queue < total) begin_item(drawn_k * queues + queue);
+#pragma unroll 1
+  for (int k = 0; drawn_k * queues + queue < total; ++k) {
+    if (tid == 0 && !careful) drawn = atomicAdd(a.counts + queue, 1);
+    columns();
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
       const bf16_t* qp = a.q + ((int64_t)row[t] * a.Hq + head[t]) * HD + 8 * hf;
 #pragma unroll
       for (int i = 0; i < 8; ++i)
         qf[t][i] = __builtin_bit_cast(bf16x8_t, *(const u32x4_t*)(qp + 16 * i));
     }
-    // A wave brings one tile of each stage, keys (waves 0, 2) or values of one of
-    // its two blocks; past the list the last block again, whose keys count as
-    // unseen. Called with st = 0, 1, ..: the blocks of 64 stages at a time in a
-    // register's lanes.
-    const int32_t* bt = rk.block_table + (int64_t)s * rk.max_blocks;
-    const bf16_t* cache = (wv & 1 ? a.v_cache : a.k_cache) + g * kTile + lane * 8;
-    int ids = 0;
-    auto source = [&](int st) {
-      if ((st & 63) == 0) {
-        const int e = min(e0 + (st + lane) * 2 + (wv >> 1), e1 - 1);
-        ids = readable_block(bt[list.block(e)], rk.num_blocks);
-      }
-      return cache + (int64_t)__builtin_amdgcn_readlane(ids, st & 63) * (a.Hkv * kTile);
-    };
-    auto place = [&](int st) { return ring_at + ((st % kRing) * kStage + wv * kTile) * 2; };
-    auto issue = [&](int st) {
-      const bf16_t* src = source(st);
-      load_tile<0>(src, place(st));
-      load_tile<1>(src, place(st));
-      load_tile<2>(src, place(st));
-      load_tile<3>(src, place(st));
-    };
-#pragma unroll 1
-    for (int st = 0; st < kRing - 1 && st < stages; ++st) issue(st);
+    const int stages = it.stages, last = it.last;
+    const bool idle = wave0 > last;
+    const int fast_end = careful ? 0 : stages - 1;
 
     // Stages that every column of the wave sees whole: from..to. (Among the window's
     // blocks only; slots above p - window for the latest row, up to p for the first.)
-    const int p_low = max(first + j_tile + small_div(r_tile + wave0, inv_G), -1),
-              p_high = first + j_tile + small_div(r_tile + min(wave0 + kCols - 1, tile_last), inv_G);
+    const int p_low = max(it.first + it.j_tile + small_div(it.r_tile + wave0, inv_G), -1),
+              p_high = it.first + it.j_tile +
+                       small_div(it.r_tile + min(wave0 + kCols - 1, last), inv_G);
     const int b_low = max(p_high - rk.window + kBlockTokens, 0) / kBlockTokens,
               b_high = (p_low + 1) / kBlockTokens - 1;
-    const int from = (list.head + max(b_low - list.first, 0) - e0 + 1) >> 1,
-              to = ((min(list.head + b_high - list.first, e1 - 1) - e0 + 1) >> 1) - 1;
+    const int from = (it.list.head + max(b_low - it.list.first, 0) - it.e0 + 1) >> 1,
+              to = ((min(it.list.head + b_high - it.list.first, it.e1 - 1) - it.e0 + 1) >> 1) - 1;
     auto whole = [&](int st) { return st >= from && st <= to; };
 
     Cols c[2];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      c[t].m = -INFINITY;
+      c[t].m = kNoMax;
       c[t].l = 0.f;
 #pragma unroll
       for (int i = 0; i < 4; ++i) c[t].acc[i] = f32x16_t{};
@@ -484,12 +530,15 @@ __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a
       arrive();
       issue(st + kRing - 1);
     };
-    const bf16_t* const k_lane = ring + (lane & 16 ? 2 * kTile : 0) + k_frag_off(lane, 0);
+    uint32_t k_lane = ring_at + ((lane & 16 ? 2 * kTile : 0) + k_frag_off(lane, 0)) * 2;
+    asm volatile("" : "+v"(k_lane));
+    auto read_k_part = [&](uint32_t at, int i) {
+      return *(const lds_u32x4_t*)((const lds_bf16_t*)(uintptr_t)at + k_frag_off(lane, i) -
+                                   k_frag_off(lane, 0));
+    };
     auto read_k = [&](int st, u32x4_t kf[8]) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        kf[i] = *(const u32x4_t*)(k_lane + (st % kRing) * kStage + k_frag_off(lane, i) -
-                                  k_frag_off(lane, 0));
+      for (int i = 0; i < 8; ++i) kf[i] = read_k_part(k_lane + (st % kRing) * (kStage * 2), i);
     };
     // Operand i (block i / 4, pair i / 2 % 2, half i % 2): two runs of four keys 512
     // bytes apart by one read. (From an address that the compiler does not see
@@ -509,22 +558,27 @@ __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a
     };
     // The keys of stage st that a row of slot p sees, as bits.
     auto stage_bits = [&](int st, int p) {
-      const int e = e0 + 2 * st;
-      uint32_t seen = window_bits(list.block(e) * kBlockTokens, p, rk.window, rk.sinks);
-      if (e + 1 < e1)
-        seen |= window_bits(list.block(e + 1) * kBlockTokens, p, rk.window, rk.sinks) << 16;
+      const int e = it.e0 + 2 * st;
+      if (e >= it.list.head && e + 1 < it.e1) {  // two blocks in a row
+        const int t0 = it.list.block(e) * kBlockTokens;
+        const int hi = min(max(p + 1 - t0, 0), 32);
+        const int lo = min(max(max(p - rk.window + 1, 0) - t0, 0), 32);
+        const uint32_t seen = (uint32_t)(((1ull << hi) - 1) & ~((1ull << lo) - 1));
+        if (t0 >= rk.sinks) return seen;
+      }
+      uint32_t seen = window_bits(it.list.block(e) * kBlockTokens, p, rk.window, rk.sinks);
+      if (e + 1 < it.e1)
+        seen |= window_bits(it.list.block(e + 1) * kBlockTokens, p, rk.window, rk.sinks) << 16;
       return seen;
     };
+
     // (The queries are here: a wait for them inside the walk would be for every load.)
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int i = 0; i < 8; ++i) asm volatile("" : "+a"(qf[t][i]));
-    if (deep)
-      wait_vmcnt<4 * (kRing - 2)>();
-    else
-      wait_vmcnt<0>();
-    stage_barrier();  // stage 0 is here
+    wait_vmcnt<0>();
+    stage_barrier();  // the first stages are here
     // (Every wave passes as many barriers: begin(0) .. begin(stages - 1) where there is
     // more than one stage.)
     if (idle) {
@@ -560,42 +614,40 @@ __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a
       // scores of it (m1 with them), the keys of st + 1.
       int st = 0;
 #pragma unroll 1
-      while (__builtin_expect_with_probability(st + 1 < stages, 1, 0.99)) {
+      while (__builtin_expect_with_probability(st < fast_end, 1, 0.99)) {
         rescale(c[1], m1);
-        if (__builtin_expect(!whole(st), 0)) {
-          read_v(st, vf);
-          if (any_odd(vf)) break;
-        }
         const uint32_t v_at = v_lane + (st % kRing) * (kStage * 2);
         half_step(kf, qf[0], z0, c[0], vf, pw[0], c[1], z1, pw[1], m0, a.scale_log2, [&](int i) {
-          if (i < 2)
-#pragma unroll
-            for (int j = 4 * i; j < 4 * i + 4; ++j) read_v_part(v_at, j, vf);
+          if (i < 4) {
+            read_v_part(v_at, 2 * i, vf);
+            read_v_part(v_at, 2 * i + 1, vf);
+          }
         });
         if (__builtin_expect(!whole(st + 1), 0)) mask(z0, m0, 0, st + 1);
         rescale(c[0], m0);
         // begin(st + 1), its loads beside the first products.
         arrive();
+        if (__builtin_expect((st + kRing & 63) == 0, 0)) refill(st + kRing);
         const bf16_t* src = source(st + kRing);
         const uint32_t dst = place(st + kRing);
-        const bf16_t* kb = k_lane + (st + 2) % kRing * kStage;
+        const uint32_t k_at = k_lane + (st + 2) % kRing * (kStage * 2);
         half_step(kf, qf[1], z1, c[1], vf, pw[1], c[0], z0, pw[0], m1, a.scale_log2, [&](int i) {
-          if (i == 0) load_tile<0>(src, dst);
-          if (i == 1) load_tile<1>(src, dst);
-          if (i == 2) load_tile<2>(src, dst);
-          if (i == 3) load_tile<3>(src, dst);
-          if (i >= 1 && i < 9)
-            kf[i - 1] = *(const u32x4_t*)(kb + k_frag_off(lane, i - 1) - k_frag_off(lane, 0));
+          if (i == 0) load_tile<0>(src + lane * 8, dst);
+          if (i == 1) load_tile<1>(src + lane * 8, dst);
+          if (i == 2) load_tile<2>(src + lane * 8, dst);
+          if (i == 3) load_tile<3>(src + lane * 8, dst);
+          if (i >= 2 && i < 10) kf[i - 2] = read_k_part(k_at, i - 2);
         });
         ++st;
         if (__builtin_expect(!whole(st), 0)) mask(z1, m1, 1, st);
       }
-      // The last stage; and all from one on with values that not every column may
-      // meet, one thing after the other. (Both in one loop spilled registers.)
+      // The last stage; and all of an item that is done again, since a sum was not a
+      // number: one thing after the other, with the values that not every column may
+      // meet held apart. (In one loop with the steps above it spilled registers.)
 #pragma unroll 1
       do {
         read_v(st, vf);
-        const bool odd = !whole(st) && any_odd(vf);
+        const bool odd = careful && !whole(st) && any_odd(vf);
         if (odd) drop_odd(vf);
         rescale(c[1], m1);
         weights_of(c[1], z1, a.scale_log2, pw[1]);
@@ -615,16 +667,30 @@ __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a
         read_k(st + 1, kf);
       } while (true);
     }
-    if (tid == 0) next_s[k & 1] = drawn;
+    if (!careful && (any_nan(c[0].acc) || any_nan(c[1].acc))) bad_s[k & 1] = 1;
+    if (tid == 0) {
+      next_s[k & 1] = per_queue + drawn;
+      bad_s[(k & 1) ^ 1] = 0;
+    }
     wait_vmcnt<0>();  // (the stages past the end)
     __syncthreads();  // every wave is done with the ring
-    drawn_k = __builtin_amdgcn_readfirstlane(next_s[k & 1]);
-
+    // A value that is not finite, of a key that some of the columns do not see, made
+    // sums of others NaN (as a NaN that they do see does): the item once more.
+    careful = !careful && one(bad_s[k & 1]) != 0;
+    if (careful) {
+#pragma unroll 1
+      for (int st = 0; st < kRing - 1 && st < it.stages; ++st) issue(st);
+      continue;
+    }
+    // The next item's first stages are on their way while this one's rows are written.
+    const int splits = it.splits, sp = it.sp, part0 = it.part0, row0 = it.row0;
+    drawn_k = one(next_s[k & 1]);
+    if (drawn_k * queues + queue < total) begin_item(drawn_k * queues + queue);
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(c[t].l),
                                                        __float_as_uint(c[t].l), false, false);
-      if (wave0 + 32 * t + (lane & 31) > tile_last) continue;
+      if (wave0 + 32 * t + (lane & 31) > last) continue;
       const float L = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
       const float inv = L == 0.f ? 0.f : 1.0f / L;
       const int64_t rowhead = (int64_t)row[t] * a.Hq + head[t];
@@ -649,7 +715,7 @@ __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a
         if (splits > 1)
           *(f32x2_t*)(a.part_ml + 2 * idx) = f32x2_t{c[t].m, L};
         else if (a.stats != nullptr)
-          *(f32x2_t*)(a.stats + 2 * rowhead) = f32x2_t{c[t].m == -INFINITY ? 0.f : c[t].m, inv};
+          *(f32x2_t*)(a.stats + 2 * rowhead) = f32x2_t{c[t].m == kNoMax ? 0.f : c[t].m, inv};
       }
     }
   }
