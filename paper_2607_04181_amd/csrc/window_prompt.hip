@@ -125,17 +125,17 @@ __device__ __forceinline__ int value_dim(int i, int m) {
   return 32 * (i & 2) + 32 * (m >> 4) + 16 * ((i & 1) ^ value_swap(m)) + (m & 15);
 }
 
-// The larger of two in one instruction (fmaxf quiets its operands first). With a NaN
-// the result is either: the column's weights are NaN then.
-__device__ __forceinline__ float max2(float a, float b) {
-  return __builtin_amdgcn_fmed3f(a, b, INFINITY);
-}
-// Largest of 16 values.
+// A column's running maximum before it has seen a key: below every score, and finite,
+// so that differences need no test.
+constexpr float kNoMax = -3.402823466e38f;
+
+// Largest of 16 values (NaN loses). Three at a time: a maximum of two quiets its
+// operands first.
 __device__ __forceinline__ float max16(const f32x16_t& s) {
   float m = fmaxf(fmaxf(s[0], s[1]), s[2]);
 #pragma unroll
   for (int r = 3; r + 1 < 16; r += 2) m = fmaxf(fmaxf(m, s[r]), s[r + 1]);
-  return max2(m, s[15]);
+  return fmaxf(fmaxf(m, s[15]), kNoMax);
 }
 
 // -inf where the column does not see the key. Bit k of seen: key k of the 32.
@@ -185,10 +185,6 @@ __device__ __forceinline__ void drop_odd(u32x4_t v[2][2][2]) {
       }
 }
 
-// A column's running maximum before it has seen a key: below every score, and finite,
-// so that differences need no test.
-constexpr float kNoMax = -3.402823466e38f;
-
 // One tile's columns: running softmax and O^T. acc[i][r]: dim value_dim(i, m), m =
 // 8 (r / 4) + 4 hf + r % 4.
 struct Cols {
@@ -200,7 +196,7 @@ struct Cols {
 __device__ __forceinline__ float column_top(float mx, float scale_log2) {
   const auto sw =
       __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
-  return max2(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * scale_log2;
+  return fmaxf(fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])), kNoMax) * scale_log2;
 }
 // The running max of a column moves only when a step's largest score exceeds it by
 // kLazy: to m_new, where any column's moves.
@@ -287,7 +283,7 @@ __device__ __forceinline__ void half_step(const u32x4_t k[8], const bf16x8_t q[8
     if (i == 10) mx = fmaxf(fmaxf(mx, z[3]), z[4]);
     if (i == 11) mx = fmaxf(fmaxf(fmaxf(fmaxf(mx, z[5]), z[6]), z[7]), z[8]);
     if (i == 12) mx = fmaxf(fmaxf(mx, z[9]), z[10]);
-    if (i == 13) mx = max2(fmaxf(fmaxf(fmaxf(fmaxf(mx, z[11]), z[12]), z[13]), z[14]), z[15]);
+    if (i == 13) mx = fmaxf(fmaxf(fmaxf(fmaxf(fmaxf(fmaxf(mx, z[11]), z[12]), z[13]), z[14]), z[15]), kNoMax);
     if (i == 14) top = column_top(mx, scale_log2);
     // (here, not where they are used)
     asm volatile("" : "+v"(pr[i]), "+v"(x), "+v"(ls), "+v"(mx));
@@ -456,19 +452,10 @@ __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a
     load_tile<2>(src, place(st));
     load_tile<3>(src, place(st));
   };
-  // This lane's columns; columns past the last repeat it. row, head: in the call.
+  // This lane's columns (columns past the last repeat it): their rows' slots, their queries.
   const int wave0 = wv * kCols;
-  int p[2], row[2], head[2];
+  int p[2];
   bf16x8_t qf[2][8];
-  auto columns = [&]() {
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const int c = it.r_tile + min(wave0 + 32 * t + (lane & 31), it.last), j = small_div(c, inv_G);
-      p[t] = max(it.first + it.j_tile + j, -1);
-      row[t] = it.row0 + it.j_tile + j;
-      head[t] = it.g * G + c - j * G;
-    }
-  };
   auto begin_item = [&](int item) {
     describe(item);
 #pragma unroll 1
@@ -482,10 +469,12 @@ __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a
 #pragma unroll 1
   for (int k = 0; drawn_k * queues + queue < total; ++k) {
     if (tid == 0 && !careful) drawn = atomicAdd(a.counts + queue, 1);
-    columns();
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      const bf16_t* qp = a.q + ((int64_t)row[t] * a.Hq + head[t]) * HD + 8 * hf;
+      const int x = it.r_tile + min(wave0 + 32 * t + (lane & 31), it.last), j = small_div(x, inv_G);
+      p[t] = max(it.first + it.j_tile + j, -1);
+      const bf16_t* qp = a.q + ((int64_t)(it.row0 + it.j_tile + j) * a.Hq + it.g * G + x - j * G) * HD +
+                         8 * hf;
 #pragma unroll
       for (int i = 0; i < 8; ++i)
         qf[t][i] = __builtin_bit_cast(bf16x8_t, *(const u32x4_t*)(qp + 16 * i));
@@ -517,13 +506,9 @@ __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a
     // Before stage st + 1 is read: this wave's share of it is here, with later ones
     // on their way, and every wave's; all are done with stage st - 1, whose place
     // the next one takes: past the end the last again, so that the loads on their way
-    // are always as many. (A list that does not fill the ring was brought whole.)
-    const bool deep = stages >= kRing - 1;
+    // are always as many. (The first kRing - 1 are waited for below.)
     auto arrive = [&]() {
-      if (deep)
-        wait_vmcnt<4 * (kRing - 3)>();
-      else
-        wait_vmcnt<0>();
+      wait_vmcnt<4 * (kRing - 3)>();
       stage_barrier();
     };
     auto begin = [&](int st) {
@@ -611,35 +596,45 @@ __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a
         read_k(1, kf);
       }
       // Here and at the start of each step: tile 0's weights of stage st, tile 1's
-      // scores of it (m1 with them), the keys of st + 1.
+      // scores of it (m1 with them), the keys of st + 1. masked: steps to stages that
+      // not every column sees whole. (A loop for each kind spilled registers.)
       int st = 0;
+      auto steps = [&](bool masked, int end) {
 #pragma unroll 1
-      while (__builtin_expect_with_probability(st < fast_end, 1, 0.99)) {
-        rescale(c[1], m1);
-        const uint32_t v_at = v_lane + (st % kRing) * (kStage * 2);
-        half_step(kf, qf[0], z0, c[0], vf, pw[0], c[1], z1, pw[1], m0, a.scale_log2, [&](int i) {
-          if (i < 4) {
-            read_v_part(v_at, 2 * i, vf);
-            read_v_part(v_at, 2 * i + 1, vf);
-          }
-        });
-        if (__builtin_expect(!whole(st + 1), 0)) mask(z0, m0, 0, st + 1);
-        rescale(c[0], m0);
-        // begin(st + 1), its loads beside the first products.
-        arrive();
-        if (__builtin_expect((st + kRing & 63) == 0, 0)) refill(st + kRing);
-        const bf16_t* src = source(st + kRing);
-        const uint32_t dst = place(st + kRing);
-        const uint32_t k_at = k_lane + (st + 2) % kRing * (kStage * 2);
-        half_step(kf, qf[1], z1, c[1], vf, pw[1], c[0], z0, pw[0], m1, a.scale_log2, [&](int i) {
-          if (i == 0) load_tile<0>(src + lane * 8, dst);
-          if (i == 1) load_tile<1>(src + lane * 8, dst);
-          if (i == 2) load_tile<2>(src + lane * 8, dst);
-          if (i == 3) load_tile<3>(src + lane * 8, dst);
-          if (i >= 2 && i < 10) kf[i - 2] = read_k_part(k_at, i - 2);
-        });
-        ++st;
-        if (__builtin_expect(!whole(st), 0)) mask(z1, m1, 1, st);
+        while (__builtin_expect_with_probability(st < end, 1, 0.99)) {
+          rescale(c[1], m1);
+          const uint32_t v_at = v_lane + (st % kRing) * (kStage * 2);
+          half_step(kf, qf[0], z0, c[0], vf, pw[0], c[1], z1, pw[1], m0, a.scale_log2, [&](int i) {
+            if (i < 4) {
+              read_v_part(v_at, 2 * i, vf);
+              read_v_part(v_at, 2 * i + 1, vf);
+            }
+          });
+          if (__builtin_expect(masked, 0)) mask(z0, m0, 0, st + 1);
+          rescale(c[0], m0);
+          // begin(st + 1), its loads beside the first products.
+          arrive();
+          const bf16_t* src = source(st + kRing) + lane * 8;
+          const uint32_t dst = place(st + kRing);
+          const uint32_t k_at = k_lane + (st + 2) % kRing * (kStage * 2);
+          half_step(kf, qf[1], z1, c[1], vf, pw[1], c[0], z0, pw[0], m1, a.scale_log2, [&](int i) {
+            if (i == 0) load_tile<0>(src, dst);
+            if (i == 1) load_tile<1>(src, dst);
+            if (i == 2) load_tile<2>(src, dst);
+            if (i == 3) load_tile<3>(src, dst);
+            if (i >= 2 && i < 10) kf[i - 2] = read_k_part(k_at, i - 2);
+          });
+          ++st;
+          if (__builtin_expect(masked, 0)) mask(z1, m1, 1, st);
+        }
+      };
+#pragma unroll 1
+      while (st < fast_end) {
+        // (up to the next step whose stage st + kRing starts another 64 table entries)
+        if ((st + kRing & 63) == 0) refill(st + kRing);
+        const int end = min(fast_end, (st + kRing & ~63) + 64 - kRing);
+        const bool all = whole(st + 1);
+        steps(!all, all ? min(end, to) : st + 1 < from ? min(end, from - 1) : end);
       }
       // The last stage; and all of an item that is done again, since a sum was not a
       // number: one thing after the other, with the values that not every column may
@@ -682,40 +677,93 @@ __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a
       for (int st = 0; st < kRing - 1 && st < it.stages; ++st) issue(st);
       continue;
     }
-    // The next item's first stages are on their way while this one's rows are written.
-    const int splits = it.splits, sp = it.sp, part0 = it.part0, row0 = it.row0;
+    // The next item's first stages are on their way while this one's rows are written:
+    // through a place of the ring that they leave free, 4 KB of it per wave, so that a
+    // row goes out in whole lines. (Straight from the accumulators, 8 bytes a lane,
+    // they took 8 us of an item.)
+    const Item was = it;
     drawn_k = one(next_s[k & 1]);
     if (drawn_k * queues + queue < total) begin_item(drawn_k * queues + queue);
+    char* const sp = (char*)(ring + (kRing - 1) * kStage) + wv * 4096;
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
+      const int c32 = lane & 31;
       const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(c[t].l),
                                                        __float_as_uint(c[t].l), false, false);
-      if (wave0 + 32 * t + (lane & 31) > last) continue;
       const float L = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
       const float inv = L == 0.f ? 0.f : 1.0f / L;
-      const int64_t rowhead = (int64_t)row[t] * a.Hq + head[t];
-      const int64_t idx = part0 + (rowhead - (int64_t)row0 * a.Hq) * splits + sp;
-      bf16_t* out = a.o + (a.tiled ? tile_off(row[t], head[t] * HD, a.Hq * HD) : rowhead * HD);
-      // Runs of four dims from the first of value_dim(i, m), m = 8 (r / 4) + 4 hf ..
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int r = 0; r < 16; r += 4) {
-          const f32x16_t& o = c[t].acc[i];
-          const int d = value_dim(i, 2 * r) + 4 * hf;
-          if (splits == 1) {
-            // (four dims from a multiple of 4 are contiguous in tile order)
-            store4(out + (a.tiled ? (d >> 5) * 512 + (d >> 3 & 3) * 128 + (d & 7) : d), o[r] * inv,
-                   o[r + 1] * inv, o[r + 2] * inv, o[r + 3] * inv);
-          } else {
-            *(f32x4_t*)(a.part_o + idx * HD + d) = f32x4_t{o[r], o[r + 1], o[r + 2], o[r + 3]};
-          }
-        }
-      if (hf == 0) {
-        if (splits > 1)
-          *(f32x2_t*)(a.part_ml + 2 * idx) = f32x2_t{c[t].m, L};
+      // Column x of the wave's 64: its row and head, and (parts) its place.
+      const auto rowhead_of = [&](int x, int& row, int& head) {
+        const int y = was.r_tile + wave0 + x, j = small_div(y, inv_G);
+        row = was.row0 + was.j_tile + j;
+        head = was.g * G + y - j * G;
+        return (int64_t)row * a.Hq + head;
+      };
+      const auto part_of = [&](int64_t rowhead) {
+        return was.part0 + (rowhead - (int64_t)was.row0 * a.Hq) * was.splits + was.sp;
+      };
+      int row, head;
+      if (hf == 0 && wave0 + 32 * t + c32 <= last) {
+        const int64_t rowhead = rowhead_of(32 * t + c32, row, head);
+        if (was.splits > 1)
+          *(f32x2_t*)(a.part_ml + 2 * part_of(rowhead)) = f32x2_t{c[t].m, L};
         else if (a.stats != nullptr)
           *(f32x2_t*)(a.stats + 2 * rowhead) = f32x2_t{c[t].m == kNoMax ? 0.f : c[t].m, inv};
+      }
+      // Runs of four dims from the first of value_dim(i, m), m = 8 (r / 4) + 4 hf ..
+#pragma unroll
+      for (int dh = 0; dh < 2; ++dh) {  // dims 64 dh ..
+        if (was.splits == 1) {
+          // 32 columns of 128 bytes in 16-byte pieces, piece u at u ^ (column % 8).
+#pragma unroll
+          for (int i = 2 * dh; i < 2 * dh + 2; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) {
+              const f32x16_t& o = c[t].acc[i];
+              const int u = value_dim(i, 2 * r) % 64 / 8;
+              *(u32x2_t*)(sp + c32 * 128 + ((u ^ (c32 & 7)) << 4) + 8 * hf) =
+                  u32x2_t{pack_bf16x2(o[r] * inv, o[r + 1] * inv),
+                          pack_bf16x2(o[r + 2] * inv, o[r + 3] * inv)};
+            }
+          wave_lds_order();
+#pragma unroll
+          for (int y = 0; y < 4; ++y) {
+            const int col = 8 * y + (lane >> 3), u = lane & 7;
+            const u32x4_t v = *(const u32x4_t*)(sp + col * 128 + ((u ^ (col & 7)) << 4));
+            if (wave0 + 32 * t + col > last) continue;
+            const int64_t rowhead = rowhead_of(32 * t + col, row, head);
+            const int d = 64 * dh + 8 * u;
+            *(u32x4_t*)(a.o + (a.tiled ? tile_off(row, head * HD + d, a.Hq * HD)
+                                       : rowhead * HD + d)) = v;
+          }
+          wave_lds_order();
+        } else {
+          // 16 columns of 256 bytes at a time.
+#pragma unroll
+          for (int ch = 0; ch < 2; ++ch) {
+            if (c32 >> 4 == ch) {
+#pragma unroll
+              for (int i = 2 * dh; i < 2 * dh + 2; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; r += 4) {
+                  const f32x16_t& o = c[t].acc[i];
+                  const int u = value_dim(i, 2 * r) % 64 / 4 + hf;
+                  *(f32x4_t*)(sp + (c32 & 15) * 256 + ((u ^ (c32 & 15)) << 4)) =
+                      f32x4_t{o[r], o[r + 1], o[r + 2], o[r + 3]};
+                }
+            }
+            wave_lds_order();
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+              const int col = 4 * y + (lane >> 4), u = lane & 15;
+              const f32x4_t v = *(const f32x4_t*)(sp + col * 256 + ((u ^ col) << 4));
+              if (wave0 + 32 * t + 16 * ch + col > last) continue;
+              const int64_t rowhead = rowhead_of(32 * t + 16 * ch + col, row, head);
+              *(f32x4_t*)(a.part_o + part_of(rowhead) * HD + 64 * dh + 4 * u) = v;
+            }
+            wave_lds_order();
+          }
+        }
       }
     }
   }
