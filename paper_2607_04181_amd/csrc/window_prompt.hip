@@ -395,6 +395,7 @@ __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a
     int row0, first, splits, part0, sp, g;
     int j_tile, r_tile;  // row of the tile's first column, and its head
     int last;            // its last column
+    int64_t rowhead;     // row * Hq + head of a first column of head 0
     int e0, e1, stages;  // of its list
     WindowList list;
     const int32_t* bt;
@@ -423,6 +424,7 @@ __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a
     it.j_tile = tile0 / G;
     it.r_tile = tile0 - it.j_tile * G;
     it.last = min(one(sq.n) * G - tile0, kTileCols) - 1;
+    it.rowhead = (int64_t)(it.row0 + it.j_tile) * a.Hq + it.g * G;
     it.list = window_list(max(it.first + it.j_tile, -1),
                           it.first + it.j_tile + small_div(it.r_tile + it.last, inv_G), rk.window,
                           rk.sinks);
@@ -473,8 +475,7 @@ __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a
     for (int t = 0; t < 2; ++t) {
       const int x = it.r_tile + min(wave0 + 32 * t + (lane & 31), it.last), j = small_div(x, inv_G);
       p[t] = max(it.first + it.j_tile + j, -1);
-      const bf16_t* qp = a.q + ((int64_t)(it.row0 + it.j_tile + j) * a.Hq + it.g * G + x - j * G) * HD +
-                         8 * hf;
+      const bf16_t* qp = a.q + it.rowhead * HD + (x + j * (a.Hq - G)) * HD + 8 * hf;
 #pragma unroll
       for (int i = 0; i < 8; ++i)
         qf[t][i] = __builtin_bit_cast(bf16x8_t, *(const u32x4_t*)(qp + 16 * i));
@@ -546,10 +547,9 @@ __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a
       const int e = it.e0 + 2 * st;
       if (e >= it.list.head && e + 1 < it.e1) {  // two blocks in a row
         const int t0 = it.list.block(e) * kBlockTokens;
-        const int hi = min(max(p + 1 - t0, 0), 32);
-        const int lo = min(max(max(p - rk.window + 1, 0) - t0, 0), 32);
-        const uint32_t seen = (uint32_t)(((1ull << hi) - 1) & ~((1ull << lo) - 1));
-        if (t0 >= rk.sinks) return seen;
+        const int hi = min(p + 1 - t0, 32), lo = min(max(p - rk.window + 1, 0) - t0, 32);
+        const auto below = [](int n) { return n <= 0 ? 0u : 0xFFFFFFFFu >> (32 - n); };
+        if (t0 >= rk.sinks) return below(hi) & ~below(lo);
       }
       uint32_t seen = window_bits(it.list.block(e) * kBlockTokens, p, rk.window, rk.sinks);
       if (e + 1 < it.e1)
@@ -692,23 +692,21 @@ __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a
                                                        __float_as_uint(c[t].l), false, false);
       const float L = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
       const float inv = L == 0.f ? 0.f : 1.0f / L;
-      // Column x of the wave's 64: its row and head, and (parts) its place.
-      const auto rowhead_of = [&](int x, int& row, int& head) {
-        const int y = was.r_tile + wave0 + x, j = small_div(y, inv_G);
-        row = was.row0 + was.j_tile + j;
-        head = was.g * G + y - j * G;
-        return (int64_t)row * a.Hq + head;
+      // Column x of the wave's 64: row * Hq + head, from the tile's first row on.
+      const auto rowhead_of = [&](int x) {
+        const int y = was.r_tile + wave0 + x;
+        return y + small_div(y, inv_G) * (a.Hq - G);
       };
-      const auto part_of = [&](int64_t rowhead) {
-        return was.part0 + (rowhead - (int64_t)was.row0 * a.Hq) * was.splits + was.sp;
+      const auto part_of = [&](int rowhead) {
+        return was.part0 + (was.rowhead + rowhead - (int64_t)was.row0 * a.Hq) * was.splits + was.sp;
       };
-      int row, head;
       if (hf == 0 && wave0 + 32 * t + c32 <= last) {
-        const int64_t rowhead = rowhead_of(32 * t + c32, row, head);
+        const int rowhead = rowhead_of(32 * t + c32);
         if (was.splits > 1)
           *(f32x2_t*)(a.part_ml + 2 * part_of(rowhead)) = f32x2_t{c[t].m, L};
         else if (a.stats != nullptr)
-          *(f32x2_t*)(a.stats + 2 * rowhead) = f32x2_t{c[t].m == kNoMax ? 0.f : c[t].m, inv};
+          *(f32x2_t*)(a.stats + 2 * (was.rowhead + rowhead)) =
+              f32x2_t{c[t].m == kNoMax ? 0.f : c[t].m, inv};
       }
       // Runs of four dims from the first of value_dim(i, m), m = 8 (r / 4) + 4 hf ..
 #pragma unroll
@@ -731,10 +729,14 @@ __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a
             const int col = 8 * y + (lane >> 3), u = lane & 7;
             const u32x4_t v = *(const u32x4_t*)(sp + col * 128 + ((u ^ (col & 7)) << 4));
             if (wave0 + 32 * t + col > last) continue;
-            const int64_t rowhead = rowhead_of(32 * t + col, row, head);
-            const int d = 64 * dh + 8 * u;
-            *(u32x4_t*)(a.o + (a.tiled ? tile_off(row, head * HD + d, a.Hq * HD)
-                                       : rowhead * HD + d)) = v;
+            const int rowhead = rowhead_of(32 * t + col), d = 64 * dh + 8 * u;
+            bf16_t* out = a.o + was.rowhead * HD + rowhead * HD + d;
+            if (a.tiled) {
+              const int x = was.r_tile + wave0 + 32 * t + col, j = small_div(x, inv_G);
+              out = a.o + tile_off(was.row0 + was.j_tile + j, (was.g * G + x - j * G) * HD + d,
+                                   a.Hq * HD);
+            }
+            *(u32x4_t*)out = v;
           }
           wave_lds_order();
         } else {
@@ -758,8 +760,8 @@ __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a
               const int col = 4 * y + (lane >> 4), u = lane & 15;
               const f32x4_t v = *(const f32x4_t*)(sp + col * 256 + ((u ^ col) << 4));
               if (wave0 + 32 * t + 16 * ch + col > last) continue;
-              const int64_t rowhead = rowhead_of(32 * t + 16 * ch + col, row, head);
-              *(f32x4_t*)(a.part_o + part_of(rowhead) * HD + 64 * dh + 4 * u) = v;
+              *(f32x4_t*)(a.part_o + part_of(rowhead_of(32 * t + 16 * ch + col)) * HD + 64 * dh +
+                          4 * u) = v;
             }
             wave_lds_order();
           }
