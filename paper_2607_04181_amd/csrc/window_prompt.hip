@@ -21,9 +21,16 @@
 // tile 1; then scores and values of tile 1, softmax of tile 0 for st + 1).
 //
 // A workgroup is four waves with 256 columns of one sequence and key/value head.
-// They share the keys through LDS in a ring of stages of 32. Its list of blocks is
-// what its rows see between them; a stage that every column of a wave sees whole
-// takes no mask.
+// They share the keys through LDS in a ring of eight stages of 32. Its list of blocks
+// is what its rows see between them; a stage that every column of a wave sees whole
+// takes no mask. Values that are not finite are looked for once, at the end: where a
+// sum is NaN, the item is done again with such values held apart.
+//
+// What bounds it: at 8000 tokens, 64 heads on 8 and a window of 4096, 400 GFLOP in 434
+// us (0.92 PFLOP/s, where a large product of matrices reaches 1.65). A step of 32 keys
+// takes 1930 cycles, 1024 of them products: a wave that is alone on its SIMD issues
+// about four vector instructions beside a product, and a step has 130 and 32
+// exponentials. 10 us of an item are its start and its end.
 //
 // The list of a sequence with at most kSplitCols columns is split into parts by a
 // rule on the sequence's own columns and list, merged by a second kernel in order:
@@ -164,12 +171,13 @@ __device__ __forceinline__ bool any_odd(const u32x4_t v[2][2][2]) {
 }
 // Whether any of a tile's sums is not a number, or infinities of both signs.
 __device__ __forceinline__ bool any_nan(const f32x16_t acc[4]) {
-  float t = 0.f;
+  f32x4_t t = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+  for (int r = 0; r < 16; ++r)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) t += acc[i][r];
-  return t != t;
+    for (int i = 0; i < 4; ++i) t[i] += acc[i][r];
+  const float sum = (t[0] + t[1]) + (t[2] + t[3]);
+  return sum != sum;
 }
 // Such values are left out (add_odd gives them to the columns that see the key).
 __device__ __forceinline__ void drop_odd(u32x4_t v[2][2][2]) {
@@ -462,15 +470,6 @@ __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a
     describe(item);
 #pragma unroll 1
     for (int st = 0; st < kRing - 1 && st < it.stages; ++st) issue(st);
-  };
-
-  int drawn_k = blockIdx.x / queues;
-  int drawn = 0;
-  bool careful = false;  // an item that is done again
-  if (drawn_k * queues + queue < total) begin_item(drawn_k * queues + queue);
-#pragma unroll 1
-  for (int k = 0; drawn_k * queues + queue < total; ++k) {
-    if (tid == 0 && !careful) drawn = atomicAdd(a.counts + queue, 1);
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       const int x = it.r_tile + min(wave0 + 32 * t + (lane & 31), it.last), j = small_div(x, inv_G);
@@ -480,6 +479,15 @@ __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a
       for (int i = 0; i < 8; ++i)
         qf[t][i] = __builtin_bit_cast(bf16x8_t, *(const u32x4_t*)(qp + 16 * i));
     }
+  };
+
+  int drawn_k = blockIdx.x / queues;
+  int drawn = 0;
+  bool careful = false;  // an item that is done again
+  if (drawn_k * queues + queue < total) begin_item(drawn_k * queues + queue);
+#pragma unroll 1
+  for (int k = 0; drawn_k * queues + queue < total; ++k) {
+    if (tid == 0 && !careful) drawn = atomicAdd(a.counts + queue, 1);
     const int stages = it.stages, last = it.last;
     const bool idle = wave0 > last;
     const int fast_end = careful ? 0 : stages - 1;
@@ -504,16 +512,20 @@ __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a
       for (int i = 0; i < 4; ++i) c[t].acc[i] = f32x16_t{};
     }
 
-    // Before stage st + 1 is read: this wave's share of it is here, with later ones
-    // on their way, and every wave's; all are done with stage st - 1, whose place
-    // the next one takes: past the end the last again, so that the loads on their way
-    // are always as many. (The first kRing - 1 are waited for below.)
-    auto arrive = [&]() {
-      wait_vmcnt<4 * (kRing - 3)>();
-      stage_barrier();
+    // Step st reads the keys of stage st + 2 and brings stage st + 7 to the place of
+    // st - 1. Every second one waits first, until this wave's shares of stages st + 2
+    // and st + 3 are here, with three later ones on their way, and until every wave's
+    // are: all are done with stage st then. (Past the end the last stage again, so that
+    // the loads on their way are always as many. The first kRing - 1 are waited for
+    // below. A barrier in every step took 8000 tokens with a window of 4096 439 us, this 434.)
+    auto arrive = [&](int st) {
+      if (st & 1) {
+        wait_vmcnt<4 * (kRing - 5)>();
+        stage_barrier();
+      }
     };
     auto begin = [&](int st) {
-      arrive();
+      arrive(st);
       issue(st + kRing - 1);
     };
     uint32_t k_lane = ring_at + ((lane & 16 ? 2 * kTile : 0) + k_frag_off(lane, 0)) * 2;
@@ -564,11 +576,10 @@ __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a
       for (int i = 0; i < 8; ++i) asm volatile("" : "+a"(qf[t][i]));
     wait_vmcnt<0>();
     stage_barrier();  // the first stages are here
-    // (Every wave passes as many barriers: begin(0) .. begin(stages - 1) where there is
-    // more than one stage.)
+    // (Every wave passes as many barriers: those of begin(0) .. begin(stages - 2).)
     if (idle) {
 #pragma unroll 1
-      for (int st = 0; stages > 1 && st < stages; ++st) begin(st);
+      for (int st = 0; st + 1 < stages; ++st) begin(st);
     } else if (stages > 0) {
       u32x4_t kf[8], vf[2][2][2], pw[2][2];
       f32x16_t z0, z1;
@@ -591,10 +602,7 @@ __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a
       scores(z1, m1, 1, 0);
       rescale(c[0], m0);
       weights_of(c[0], z0, a.scale_log2, pw[0]);
-      if (stages > 1) {
-        begin(0);
-        read_k(1, kf);
-      }
+      if (stages > 1) read_k(1, kf);
       // Here and at the start of each step: tile 0's weights of stage st, tile 1's
       // scores of it (m1 with them), the keys of st + 1. masked: steps to stages that
       // not every column sees whole. (A loop for each kind spilled registers.)
@@ -612,10 +620,10 @@ __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a
           });
           if (__builtin_expect(masked, 0)) mask(z0, m0, 0, st + 1);
           rescale(c[0], m0);
-          // begin(st + 1), its loads beside the first products.
-          arrive();
-          const bf16_t* src = source(st + kRing) + lane * 8;
-          const uint32_t dst = place(st + kRing);
+          // begin(st), its loads beside the first products.
+          arrive(st);
+          const bf16_t* src = source(st + kRing - 1) + lane * 8;
+          const uint32_t dst = place(st + kRing - 1);
           const uint32_t k_at = k_lane + (st + 2) % kRing * (kStage * 2);
           half_step(kf, qf[1], z1, c[1], vf, pw[1], c[0], z0, pw[0], m1, a.scale_log2, [&](int i) {
             if (i == 0) load_tile<0>(src, dst);
@@ -630,9 +638,9 @@ __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a
       };
 #pragma unroll 1
       while (st < fast_end) {
-        // (up to the next step whose stage st + kRing starts another 64 table entries)
-        if ((st + kRing & 63) == 0) refill(st + kRing);
-        const int end = min(fast_end, (st + kRing & ~63) + 64 - kRing);
+        // (up to the next step whose stage st + kRing - 1 starts another 64 table entries)
+        if ((st + kRing - 1 & 63) == 0) refill(st + kRing - 1);
+        const int end = min(fast_end, (st + kRing - 1 & ~63) + 65 - kRing);
         const bool all = whole(st + 1);
         steps(!all, all ? min(end, to) : st + 1 < from ? min(end, from - 1) : end);
       }
@@ -658,7 +666,7 @@ __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a
         scores(z1, m1, 1, st);
         rescale(c[0], m0);
         weights_of(c[0], z0, a.scale_log2, pw[0]);
-        begin(st);
+        begin(st - 1);
         read_k(st + 1, kf);
       } while (true);
     }
