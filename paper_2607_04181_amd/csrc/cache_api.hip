@@ -446,8 +446,8 @@ int run_window(coco_layer* H, const coco_layer_weights& w, const void* q, void* 
   le.done = done;
   if (bf16)
     HIPCHK(launch_window_weights_bf16((const bf16_t*)q, (const bf16_t*)w.k_cache, rk, n_rows,
-                                      c.n_q_heads, c.n_kv_heads, stats, H->window_sums, weights,
-                                      H->num_cus, st));
+                                      c.n_q_heads, c.n_kv_heads, stats, H->window_sums,
+                                      H->window_items, weights, H->num_cus, st));
   else
     HIPCHK(launch_window_weights_f32((const float*)q, (const float*)w.k_cache, rk, n_rows,
                                      c.n_q_heads, c.n_kv_heads, c.head_dim, stats, weights,
@@ -814,8 +814,9 @@ int coco_window_reserve(coco_layer_t H, int32_t max_rows, int32_t max_seqs, int3
     const int64_t prompt = window_column_parts(rows, seqs, c.n_q_heads, c.n_kv_heads);
     const int64_t parts = single > prompt ? single : prompt;
     const size_t o = align256((size_t)parts * c.head_dim * 4), ml = align256((size_t)parts * 8);
-    const size_t sums =
-        weights ? align256((size_t)seqs * c.n_kv_heads * c.max_blocks_per_seq * kBlockTokens * 4) : 0;
+    const int64_t items =
+        window_weight_items(rows, seqs, c.max_blocks_per_seq, c.n_q_heads, c.n_kv_heads);
+    const size_t sums = weights ? align256((size_t)window_sums_bytes(items)) : 0;
     const size_t scores =
         weights ? align256((size_t)few * c.n_q_heads * blocks * kBlockTokens * 4) : 0;
     const size_t both = stats + sums > scores ? stats + sums : scores;
@@ -824,6 +825,7 @@ int coco_window_reserve(coco_layer_t H, int32_t max_rows, int32_t max_seqs, int3
         grow(H, &H->window_ws, &H->window_bytes, o + ml + both + counts, counts);
     if (rc) return rc;
     H->window_parts = parts;
+    H->window_items = items;
     H->window_part_o = (float*)H->window_ws;
     H->window_part_ml = (float*)(H->window_ws + o);
     H->window_stats = (float*)(H->window_ws + o + ml);

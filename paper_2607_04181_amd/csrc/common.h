@@ -153,6 +153,27 @@ __device__ __forceinline__ int wave_scan(int x) {
   return x;
 }
 
+// Inclusive sum of x over the workgroup's threads so far: `carry` before, the
+// whole added to it. red: one int per wave.
+template <int WAVES>
+__device__ __forceinline__ int block_prefix(int x, int* red, int& carry) {
+  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+  x = wave_scan(x);
+  if (lane == kWave - 1) red[wv] = x;
+  __syncthreads();
+  x += carry;
+  for (int w = 0; w < WAVES; ++w) {
+    if (w < wv) x += red[w];
+    carry += red[w];
+  }
+  __syncthreads();
+  return x;
+}
+
+// x / d for x < 4096 and d <= 16, by a product with inv = small_inv(d).
+__device__ __forceinline__ uint32_t small_inv(int d) { return (65535u + d) / d; }
+__device__ __forceinline__ int small_div(int x, uint32_t inv) { return (int)(x * inv >> 16); }
+
 __device__ __forceinline__ float wave_max(float v) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, kWave));

@@ -120,6 +120,7 @@ struct coco_layer {
   size_t window_bytes = 0;
   float *window_part_o = nullptr, *window_part_ml = nullptr;
   int64_t window_parts = 0;
+  int64_t window_items = 0;
   float *window_stats = nullptr, *window_sums = nullptr, *window_scores = nullptr;
   int32_t* window_counts = nullptr;
   uint32_t* evict_plan = nullptr;

@@ -441,10 +441,14 @@ hipError_t launch_window_prompt_bf16(const uint16_t* q, const uint16_t* k_cache,
                                      float* part_ml, int64_t part_cap, int32_t* counts,
                                      float* stats, int num_cus, hipStream_t st);
 // weights [n_seqs][max_blocks * 16] grow by the weights of the rows' keys, from
-// the rows' stats; sums [n_seqs][Hkv][max_blocks * 16]: scratch.
+// the rows' stats; sums: scratch of window_sums_bytes(items_cap), items_cap at least
+// window_weight_items of the call.
+int64_t window_weight_items(int64_t max_rows, int64_t max_seqs, int max_blocks, int Hq, int Hkv);
+int64_t window_sums_bytes(int64_t items);
 hipError_t launch_window_weights_bf16(const uint16_t* q, const uint16_t* k_cache, const RowKeys& rk,
                                       int n_rows, int Hq, int Hkv, const float* stats, float* sums,
-                                      float* weights, int num_cus, hipStream_t st);
+                                      int64_t items_cap, float* weights, int num_cus,
+                                      hipStream_t st);
 // fp32 handles (the rows' attention is launch_attn_rows_f32).
 hipError_t launch_window_weights_f32(const float* q, const float* k_cache, const RowKeys& rk,
                                      int n_rows, int Hq, int Hkv, int hd, const float* stats,

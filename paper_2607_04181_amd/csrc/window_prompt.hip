@@ -108,9 +108,6 @@ __device__ __forceinline__ PromptSeq prompt_seq(const RowKeys& rk, int s, int G)
   x.item0 = x.part0 = 0;
   return x;
 }
-// x / d for x < 4096 and d <= 16, by a product with inv = small_inv(d).
-__device__ __forceinline__ uint32_t small_inv(int d) { return (65535u + d) / d; }
-__device__ __forceinline__ int small_div(int x, uint32_t inv) { return (int)(x * inv >> 16); }
 
 // Piece i of four, 1 KB each, of a cache tile into LDS at byte `to`.
 template <int I>
@@ -345,22 +342,6 @@ __device__ __forceinline__ void add_odd(Cols& c, const u32x4_t v[2][2][2], const
   }
 }
 
-// Inclusive sum of x over the workgroup's threads so far: `carry` before, the
-// whole added to it. red: one int per wave.
-__device__ __forceinline__ int block_scan(int x, int* red, int& carry) {
-  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
-  x = wave_scan(x);
-  if (lane == kWave - 1) red[wv] = x;
-  __syncthreads();
-  x += carry;
-  for (int w = 0; w < kWaves; ++w) {
-    if (w < wv) x += red[w];
-    carry += red[w];
-  }
-  __syncthreads();
-  return x;
-}
-
 __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a) {
   __shared__ __attribute__((aligned(16))) bf16_t ring[kRing * kStage];
   __shared__ PromptSeq seqs_s[kMaxSeqs];
@@ -381,8 +362,8 @@ __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a
     if (s < rk.n_seqs) x = prompt_seq(rk, s, G);
     const int ni = x.tiles * x.splits * a.Hkv;
     const int np = x.splits > 1 ? x.n * a.Hq * x.splits : 0;
-    x.item0 = block_scan(ni, red, total) - ni;
-    x.part0 = block_scan(np, red, n_parts) - np;
+    x.item0 = block_prefix<kWaves>(ni, red, total) - ni;
+    x.part0 = block_prefix<kWaves>(np, red, n_parts) - np;
     if (s < rk.n_seqs) seqs_s[s] = x;
   }
   __syncthreads();

@@ -4,13 +4,19 @@
 // row's whole sum). The scores are computed again, half of the attention's
 // products, rather than kept: a prompt has rows x heads of them per key.
 //
-// bf16: a workgroup has 128 keys of a sequence and key/value head, 32 of them in
-// the registers of each of its four waves as the operand of 32x32 products, and
+// bf16: a workgroup has 256 keys of a sequence and key/value head, 64 of them in
+// the registers of each of its four waves as the operands of 32x32 products, and
 // walks the columns (rows times query heads of the group) that can see them, 32
 // at a time through LDS: S[32 keys][32 columns] = K Q^T. A lane then holds one
-// column, whose m and 1 / l are two registers, and 16 keys, whose sums over the
-// columns it keeps; the 32 lanes' sums meet once, at the end. The heads' sums are
-// added by a second kernel, in order.
+// column, whose m and 1 / l are two registers, and 16 keys of each tile, whose sums
+// over the columns it keeps; the 32 lanes' sums meet once, at the end, and the sums of
+// the heads, and of the parts of many columns, in a second kernel, in order. Three
+// workgroups to a CU take such pieces in turn, one's products (16 of 33 cycles a step)
+// beside the others' exponentials (32 of 8, and 64 multiply-adds of 4), which bound it.
+// 16 sequences of 36 to 64 rows (32 heads on 8, 58500 cached tokens between them) take
+// 46 us, 4000 rows of a prompt 118: with 32 keys to a wave and all columns in one item
+// 57 and 393. Of the 46, the products are 10 and the vector instructions 20; the rest
+// are starts of items (tables, keys) and the last round, when some CUs have none.
 // fp32: a workgroup has 16 keys, its waves the key/value heads.
 #include <math.h>
 
@@ -23,12 +29,23 @@ namespace {
 
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef __attribute__((address_space(3))) void lds_void_t;
+typedef __attribute__((address_space(3))) bf16_t lds_bf16_t;
+typedef __attribute__((address_space(3))) f32x2_t lds_f32x2_t;
+typedef __attribute__((address_space(3))) u32x4_t lds_u32x4_t;
 
 constexpr int HD = 128;
 constexpr int kTile = kBlockTokens * HD;
 constexpr int kWaves = 4;
-constexpr int kTileBlocks = 2 * kWaves;  // blocks of a workgroup
+constexpr int kTileBlocks = 4 * kWaves;  // blocks of a workgroup
+constexpr int kTileKeys = kTileBlocks * kBlockTokens;
 constexpr int kCols = 32;                // columns of a step
+// Columns of an item: 4000 rows of 32 heads on 8 take 104 us with 512, 118 with 1024 and
+// 141 with 2048, 64 bytes of scratch a key for each; prompts of 64 rows are one item.
+constexpr int kPartCols = 1024;
+constexpr int kTurn = 8 * 37;
+constexpr int kRing = 3;                 // steps in LDS
+constexpr int kSlot = kCols * HD + kCols * 16;  // elements of one: queries, then statistics
+constexpr int kWorkgroups = 3;           // of a CU
 constexpr float kLog2e = 1.4426950408889634f;
 
 // A sequence's rows and cached tokens: N rows of slots first .. last (= L - 1).
@@ -57,120 +74,273 @@ __device__ __forceinline__ void rows_of(const RowKeys& rk, const SeqRows& x, int
     j1 = min(max(t1 + rk.window - x.first, 0), x.n);
 }
 
-__global__ __launch_bounds__(64 * kWaves, 2) void window_weights_kernel(
-    const bf16_t* __restrict__ q, const bf16_t* __restrict__ k_cache, RowKeys rk, int Hq, int Hkv,
-    float scale_log2, const float* __restrict__ stats, float* __restrict__ sums) {
-  __shared__ __attribute__((aligned(16))) bf16_t qs[2][kCols * HD];
-  const int g = blockIdx.x % Hkv, e0 = blockIdx.x / Hkv * kTileBlocks, s = blockIdx.y;
-  const int G = Hq / Hkv;
-  const int lane = threadIdx.x & 63;
-  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int c32 = lane & 31, hf = lane >> 5;
-  const SeqRows x = seq_rows(rk, s);
-  if (e0 >= x.list.entries) return;
-  const int e_last = min(e0 + kTileBlocks, x.list.entries) - 1;
-  int j0, j1;
+// Sums of 16 values over the 32 columns of a tile: lane (c, hf) returns that of value
+// c / 2. Half of the values go to the other half of the lanes at a time (37
+// instructions; value by value they are 145).
+__device__ __forceinline__ float column_sums(const float w[16], int lane) {
+  float x[8];
+#pragma unroll
+  for (int r = 0; r < 8; ++r) {
+    const auto sw = __builtin_amdgcn_permlane16_swap(__float_as_uint(w[r]),
+                                                     __float_as_uint(w[r + 8]), false, false);
+    x[r] = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+  }
+#pragma unroll
+  for (int r = 0; r < 4; ++r)  // rotated by 8 lanes of 16
+    x[r] = (lane & 8 ? x[r + 4] : x[r]) + row_swap<0x128>(lane & 8 ? x[r] : x[r + 4]);
+#pragma unroll
+  for (int r = 0; r < 2; ++r)  // 8 lanes mirrored
+    x[r] = (lane & 4 ? x[r + 2] : x[r]) + row_swap<0x141>(lane & 4 ? x[r] : x[r + 2]);
+  x[0] = (lane & 2 ? x[1] : x[0]) + row_swap<0x4E>(lane & 2 ? x[0] : x[1]);  // lane ^ 2
+  return x[0] + row_swap<0xB1>(x[0]);                                        // lane ^ 1
+}
+
+// A sequence's work: tile k, blocks k kTileBlocks .. of its list, in parts of kPartCols
+// of the columns that can see it; key/value heads innermost. Tiles below `many` (those
+// with first tokens, which every row sees) have `most` parts at most, the others `few`.
+// A part past a tile's columns has no work and leaves no sums.
+struct SeqItems {
+  int row0, n, last, item0;
+};
+struct Parts {
+  int tiles, many, most, few;
+};
+__device__ __forceinline__ int parts_of(int64_t rows, int G) {
+  return (int)((rows * G + kPartCols - 1) / kPartCols);
+}
+__device__ __forceinline__ Parts seq_parts(const RowKeys& rk, const SeqRows& x, int G) {
+  Parts y;
+  y.tiles = (x.list.entries + kTileBlocks - 1) / kTileBlocks;
+  const int first = min(rk.sinks / kBlockTokens + (rk.sinks % kBlockTokens != 0), x.list.entries);
+  y.many = (first + kTileBlocks - 1) / kTileBlocks;
+  y.most = parts_of(x.n, G);
+  // (slots t .. t + 255: rows of slots t .. t + 254 + window)
+  const int64_t rows = (int64_t)rk.window + kTileKeys - 1;
+  y.few = parts_of(rows < x.n ? rows : x.n, G);
+  return y;
+}
+// The rows j0 .. j1 - 1 that can see tile k, blocks e0 .. e_last of the list.
+__device__ __forceinline__ void tile_rows(const RowKeys& rk, const SeqRows& x, int k, int& e_last,
+                                          int& j0, int& j1) {
+  const int e0 = k * kTileBlocks;
+  e_last = min(e0 + kTileBlocks, x.list.entries) - 1;
   rows_of(rk, x, x.list.block(e0) * kBlockTokens,
           x.list.block(e_last) * kBlockTokens + kBlockTokens - 1, j0, j1);
+}
 
-  // The wave's two blocks (past the list the last one: not stored), and its keys:
-  // step u holds dims 16 u + 8 hf .. + 7 of key lane % 32.
-  int t[2];
-  u32x4_t kf[8];
-  {
-    const int32_t* bt = rk.block_table + (int64_t)s * rk.max_blocks;
-    const int ea = min(e0 + 2 * wv, e_last), eb = min(e0 + 2 * wv + 1, e_last);
-    t[0] = x.list.block(ea) * kBlockTokens;
-    t[1] = x.list.block(eb) * kBlockTokens;
-    const int id = readable_block(bt[(lane & 16 ? t[1] : t[0]) / kBlockTokens], rk.num_blocks);
-    const bf16_t* kb = k_cache + ((int64_t)id * Hkv + g) * kTile;
-#pragma unroll
-    for (int u = 0; u < 8; ++u)
-      kf[u] = *(const u32x4_t*)(kb + ((u >> 1) * 64 + (2 * (u & 1) + hf) * 16 + (lane & 15)) * 8);
+__global__ __launch_bounds__(64 * kWaves, kWorkgroups) void window_weights_kernel(
+    const bf16_t* __restrict__ q, const bf16_t* __restrict__ k_cache, RowKeys rk, int Hq, int Hkv,
+    float scale_log2, const float* __restrict__ stats, float* __restrict__ sums, int64_t sums_cap,
+    int32_t* __restrict__ items0) {
+  __shared__ __attribute__((aligned(128))) bf16_t ring[kRing * kSlot];
+  __shared__ SeqItems seqs_s[kWindowLaunchSeqs];
+  __shared__ int red[kWaves];
+  const int G = Hq / Hkv;
+  const uint32_t inv_G = small_inv(G);
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int c32 = lane & 31, hf = lane >> 5;
+  int total = 0;
+  for (int s0 = 0; s0 < rk.n_seqs; s0 += 64 * kWaves) {
+    SeqRows x{};
+    if (s0 + tid < rk.n_seqs) x = seq_rows(rk, s0 + tid);
+    const Parts y = seq_parts(rk, x, G);
+    const int items = (y.many * y.most + (y.tiles - y.many) * y.few) * Hkv;
+    const int item0 = block_prefix<kWaves>(items, red, total) - items;
+    if (s0 + tid < rk.n_seqs) {
+      seqs_s[s0 + tid] = SeqItems{x.row0, x.n, x.last, item0};
+      if (blockIdx.x == 0) items0[s0 + tid] = item0;
+    }
   }
-  const int t_low = min(t[0], t[1]), t_high = max(t[0], t[1]) + kBlockTokens - 1;
+  __syncthreads();
+  if (total > sums_cap) total = 0;  // more rows than the call named: no room for their sums
+  // (The ring's address goes through a register of its own: the compiler would
+  // otherwise wait for every load in flight before each operand read.)
+  uint32_t ring_at = (uint32_t)(uintptr_t)(lds_void_t*)ring;
+  asm volatile("" : "+s"(ring_at));
+  // Dims 16 u + 8 hf .. of column c32: chunk 2 u + hf of its halves.
+  const uint32_t q_at = ring_at + (c32 >> 3) * 2048 + (c32 & 7) * 128 + (hf ^ (c32 & 7)) * 16;
 
-  const int c_end = j1 * G;
-  // A step's columns in operand order: 1 KB pieces u of 16 dims, lane (c, hf) dims
-  // 16 u + 8 hf .. + 7 of column c. Each wave brings two.
-  auto issue = [&](int c0, int slot) {
-    const int c = min(c0 + c32, c_end - 1);
-    const bf16_t* qp =
-        q + ((int64_t)(x.row0 + c / G) * Hq + g * G + c % G) * HD + 8 * hf;
+  auto one = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+#pragma unroll 1
+  for (int item0 = 0, turn = blockIdx.x; item0 < total; item0 += gridDim.x) {
+    // (Turned from round to round, by a multiple of the XCDs: a tile's later parts are the
+    // ones without work, and a workgroup would get the same ones of several tiles.)
+    const int item = item0 + turn;
+    turn = (turn + kTurn) % gridDim.x;
+    if (item >= total) continue;
+    int lo = 0, hi = rk.n_seqs - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (seqs_s[mid].item0 <= item) lo = mid; else hi = mid - 1;
+    }
+    const int s = one(lo);
+    SeqRows x;
+    x.row0 = one(seqs_s[s].row0);
+    x.n = one(seqs_s[s].n);
+    x.last = one(seqs_s[s].last);
+    x.first = x.last + 1 - x.n;
+    x.list = window_list(max(x.first, -1), x.last, rk.window, rk.sinks);
+    const Parts y = seq_parts(rk, x, G);
+    const int at = one(item - seqs_s[s].item0), later = at / Hkv - y.many * y.most;
+    const int g = at % Hkv;
+    const int tile = later < 0 ? at / Hkv / y.most : y.many + later / y.few;
+    const int part = later < 0 ? at / Hkv % y.most : later % y.few;
+    const int e0 = tile * kTileBlocks;
+    int e_last, j0, j1;
+    tile_rows(rk, x, tile, e_last, j0, j1);
+    const int cols = max(j1 - j0, 0) * G, c0 = part * kPartCols;
+    if (c0 >= cols) continue;
+    // A step's columns, from row j's head r on, of `left`. Wave w brings columns 8 w .. + 7
+    // as two halves of their dims, 128 bytes a column, so that a load is of whole lines
+    // (in operand order, 32 bytes of a line at a time, 51 us for 48). Chunk x of a half at x ^ (column % 8): rows of 128 bytes would meet in the
+    // same banks. Then the columns' statistics, two floats in each 32 bytes.
+    struct Step {
+      int j, r, left;
+    };
+    const auto next = [&](Step& y) {
+      const int r = y.r + kCols, d = small_div(r, inv_G);
+      y = Step{y.j + d, r - d * G, y.left - kCols};
+    };
+    const bf16_t* const q_seq = q + ((int64_t)x.row0 * Hq + g * G) * HD;
+    const float* const stats_seq = stats + ((int64_t)x.row0 * Hq + g * G) * 2;
+    const auto issue = [&](const Step& y, int slot) {
+      // (row * Hq + head of this lane's column)
+      const int h = y.r + min(8 * wv + (lane >> 3), y.left - 1);
+      const int64_t head = (int64_t)y.j * Hq + (h + small_div(h, inv_G) * (Hq - G));
+      const bf16_t* qp = q_seq + head * HD + (lane & 7 ^ lane >> 3) * 8;
+      const uint32_t to = ring_at + slot * (kSlot * 2) + wv * 2048;
+      __builtin_amdgcn_global_load_lds(qp, (lds_void_t*)(uintptr_t)to, 16, 0, 0);
+      __builtin_amdgcn_global_load_lds(qp + 64, (lds_void_t*)(uintptr_t)(to + 1024), 16, 0, 0);
+      const uint32_t to_stats = ring_at + slot * (kSlot * 2) + kCols * HD * 2 + wv * 256;
+      __builtin_amdgcn_global_load_lds(stats_seq + head * 2 + (lane & 1),
+                                       (lds_void_t*)(uintptr_t)to_stats, 4, 0, 0);
+    };
+    Step now{j0 + c0 / G, c0 % G, min(cols - c0, kPartCols)}, ahead = now;
+    for (int i = 0; i < kRing - 1; ++i) {
+      issue(ahead, i);
+      if (ahead.left > kCols) next(ahead);
+    }
+
+    // The wave's four blocks (past the list the last one: not stored), and its keys:
+    // step u holds dims 16 u + 8 hf .. + 7 of key lane % 32 of two blocks.
+    int t[2][2];
+    u32x4_t kf[2][8];
 #pragma unroll
     for (int y = 0; y < 2; ++y) {
-      const int u = 2 * wv + y;
-      __builtin_amdgcn_global_load_lds(qp + 16 * u, (lds_void_t*)(qs[slot] + u * 512), 16, 0, 0);
+      const int32_t* bt = rk.block_table + (int64_t)s * rk.max_blocks;
+      const int e = e0 + 4 * wv + 2 * y;
+      t[y][0] = x.list.block(min(e, e_last)) * kBlockTokens;
+      t[y][1] = x.list.block(min(e + 1, e_last)) * kBlockTokens;
+      const int id =
+          readable_block(bt[(lane & 16 ? t[y][1] : t[y][0]) / kBlockTokens], rk.num_blocks);
+      const bf16_t* kb = k_cache + ((int64_t)id * Hkv + g) * kTile;
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        kf[y][u] =
+            *(const u32x4_t*)(kb + ((u >> 1) * 64 + (2 * (u & 1) + hf) * 16 + (lane & 15)) * 8);
     }
-  };
-  float w[16];
+    const int t_low = min(min(t[0][0], t[0][1]), min(t[1][0], t[1][1])),
+              t_high = max(max(t[0][0], t[0][1]), max(t[1][0], t[1][1])) + kBlockTokens - 1;
+    float w[2][16];
 #pragma unroll
-  for (int r = 0; r < 16; ++r) w[r] = 0.f;
-  int slot = 0;
-  if (j0 < j1) issue(j0 * G, 0);
-  for (int c0 = j0 * G; c0 < c_end; c0 += kCols) {
-    const int c = min(c0 + c32, c_end - 1), j = c / G;
-    const f32x2_t st =
-        *(const f32x2_t*)(stats + ((int64_t)(x.row0 + j) * Hq + g * G + c % G) * 2);
-    __syncthreads();  // the step is here, and the slot of the next free
-    if (c0 + kCols < c_end) issue(c0 + kCols, slot ^ 1);
-    f32x16_t z = {};
+    for (int r = 0; r < 16; ++r) w[0][r] = w[1][r] = 0.f;
+    int slot = 0;
+#pragma unroll 1
+    while (now.left > 0) {
+      wait_vmcnt<3 * (kRing - 2)>();
+      stage_barrier();  // the step is here, and the slot of the one before free
+      const lds_bf16_t* from = (const lds_bf16_t*)(uintptr_t)(ring_at + slot * (kSlot * 2));
+      const f32x2_t st = *(const lds_f32x2_t*)(from + kCols * HD + c32 * 16);
+      const float inv = c32 < now.left ? st[1] : 0.f;
+      issue(ahead, slot == 0 ? kRing - 1 : slot - 1);
+      if (ahead.left > kCols) next(ahead);
+      f32x16_t z[2] = {};
 #pragma unroll
-    for (int u = 0; u < 8; ++u) {
-      const u32x4_t b = *(const u32x4_t*)(qs[slot] + (u * 64 + lane) * 8);
-      z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kf[u]),
-                                                  __builtin_bit_cast(bf16x8_t, b), z, 0, 0, 0);
+      for (int u0 = 0; u0 < 8; u0 += 4) {
+        u32x4_t b[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) 
+          b[u] = *(const lds_u32x4_t*)(uintptr_t)((q_at + slot * (kSlot * 2) + u0 * 256) ^ u * 32);
+        // (four at once: one by one, each product waited for its own)
+#pragma unroll
+        for (int u = 0; u < 4; ++u) asm volatile("" : "+v"(b[u]));
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+          for (int y = 0; y < 2; ++y)
+            z[y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kf[y][u0 + u]),
+                                                           __builtin_bit_cast(bf16x8_t, b[u]), z[y],
+                                                           0, 0, 0);
+      }
+      slot = slot == kRing - 1 ? 0 : slot + 1;
+      const int p_low = x.first + now.j,
+                p_high = p_low + small_div(now.r + min(now.left, kCols) - 1, inv_G);
+      if (!(t_high <= p_low && (t_low > p_high - rk.window || t_high < rk.sinks))) {
+        const int p = max(p_low + small_div(now.r + min(c32, now.left - 1), inv_G), -1);
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          const uint32_t seen = window_bits(t[y][0], p, rk.window, rk.sinks) |
+                                window_bits(t[y][1], p, rk.window, rk.sinks) << 16;
+          const uint32_t mine = seen >> (4 * hf);
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            z[y][r] = (mine >> (8 * (r / 4) + r % 4) & 1) ? z[y][r] : -INFINITY;
+        }
+      }
+#pragma unroll
+      for (int y = 0; y < 2; ++y)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          w[y][r] =
+              fmaf(__builtin_amdgcn_exp2f(fmaf(z[y][r], scale_log2, -st[0])), inv, w[y][r]);
+      next(now);
     }
-    slot ^= 1;
-    const int p_low = x.first + c0 / G, p_high = x.first + min(c0 + kCols, c_end) / G;
-    if (!(t_high <= p_low && (t_low > p_high - rk.window || t_high < rk.sinks))) {
-      const int p = max(x.first + j, -1);
-      const uint32_t seen = window_bits(t[0], p, rk.window, rk.sinks) |
-                            window_bits(t[1], p, rk.window, rk.sinks) << 16;
-      const uint32_t mine = seen >> (4 * hf);
+    // (a tile's keys in the order of its list)
+    float* const to = sums + (int64_t)item * kTileKeys + 64 * wv;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) z[r] = (mine >> (8 * (r / 4) + r % 4) & 1) ? z[r] : -INFINITY;
+    for (int y = 0; y < 2; ++y) {
+      const float out = column_sums(w[y], lane);
+      const int r = c32 >> 1;
+      if (!(lane & 1)) to[32 * y + 8 * (r / 4) + 4 * hf + r % 4] = out;
     }
-    const float inv = c0 + c32 < c_end ? st[1] : 0.f;
-#pragma unroll
-    for (int r = 0; r < 16; ++r)
-      w[r] = fmaf(__builtin_amdgcn_exp2f(fmaf(z[r], scale_log2, -st[0])), inv, w[r]);
-  }
-  // Sums over the 32 columns; lane r keeps key 8 (r / 4) + 4 hf + r % 4.
-  float out = 0.f;
-#pragma unroll
-  for (int r = 0; r < 16; ++r) {
-    float v = row_sum16(w[r]);
-    const auto sw =
-        __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    v = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
-    if (c32 == r) out = v;
-  }
-  if (c32 < 16) {
-    const int key = 8 * (c32 / 4) + 4 * hf + c32 % 4, b = key >> 4;
-    if (e0 + 2 * wv + b <= e_last)
-      sums[((int64_t)s * Hkv + g) * rk.max_blocks * kBlockTokens + (b ? t[1] : t[0]) + (key & 15)] =
-          out;
+    wait_vmcnt<0>();  // (the steps past the end)
+    __syncthreads();  // every wave is done with the ring
   }
 }
 
-// The key/value heads' sums of the blocks that a sequence's rows see, in order.
-__global__ __launch_bounds__(256) void window_weights_add_kernel(RowKeys rk, int Hkv,
-                                                                 const float* __restrict__ sums,
-                                                                 float* __restrict__ weights) {
-  const int s = blockIdx.y, at = blockIdx.x * 256 + threadIdx.x;
+// A key's sums of the parts and key/value heads, each wave every fourth in order, the
+// waves in order: a lane a key, 64 keys to a workgroup.
+__global__ __launch_bounds__(64 * kWaves) void window_weights_add_kernel(
+    RowKeys rk, int G, int Hkv, const float* __restrict__ sums, int64_t sums_cap,
+    const int32_t* __restrict__ items0, float* __restrict__ weights) {
+  __shared__ float sm[kWaves][64];
+  const int s = blockIdx.y, lane = threadIdx.x & 63;
+  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const SeqRows x = seq_rows(rk, s);
-  const int e = at / kBlockTokens;
-  if (e >= x.list.entries) return;
-  const int t = x.list.block(e) * kBlockTokens + at % kBlockTokens;
-  if (t > x.last) return;
-  const int64_t width = (int64_t)rk.max_blocks * kBlockTokens;
-  const float* from = sums + (int64_t)s * Hkv * width + t;
+  const int e = blockIdx.x * (64 / kBlockTokens) + lane / kBlockTokens;
+  const int tile = blockIdx.x / (kTileKeys / 64);
+  if ((int)blockIdx.x * (64 / kBlockTokens) >= x.list.entries) return;
+  const Parts y = seq_parts(rk, x, G);
+  int e_last, j0, j1;
+  tile_rows(rk, x, tile, e_last, j0, j1);
+  const int64_t item = items0[s] + (int64_t)Hkv * (tile < y.many
+                                                       ? tile * y.most
+                                                       : y.many * y.most + (tile - y.many) * y.few);
+  const int n = parts_of(max(j1 - j0, 0), G) * Hkv;
+  if (item + n > sums_cap) return;
+  const float* from = sums + item * kTileKeys + blockIdx.x % (kTileKeys / 64) * 64 + lane;
   float v = 0.f;
 #pragma unroll 8
-  for (int g = 0; g < Hkv; ++g) v += from[g * width];
+  for (int i = wv; i < n; i += kWaves) v += from[(int64_t)i * kTileKeys];
+  sm[wv][lane] = v;
+  __syncthreads();
+  if (wv != 0 || e >= x.list.entries) return;
+#pragma unroll
+  for (int u = 1; u < kWaves; ++u) v += sm[u][lane];
+  const int t = x.list.block(e) * kBlockTokens + lane % kBlockTokens;
   // (a token between the first ones and every row's window is seen by none)
-  if (v != 0.f) weights[s * width + t] += v;
+  if (t <= x.last && v != 0.f) weights[(int64_t)s * rk.max_blocks * kBlockTokens + t] += v;
 }
 
 constexpr int kRowsWaves = 8;
@@ -241,18 +411,37 @@ int64_t most_entries(const RowKeys& rk, int n_rows) {
 
 }  // namespace
 
+// The most items of any launch of a call of so many rows and sequences.
+int64_t window_weight_items(int64_t max_rows, int64_t max_seqs, int max_blocks, int Hq, int Hkv) {
+  int64_t seqs = max_seqs < kWindowLaunchSeqs ? max_seqs : kWindowLaunchSeqs;
+  if (max_rows < seqs) seqs = max_rows;
+  const int64_t tiles = (max_blocks + kTileBlocks - 1) / kTileBlocks;
+  const int64_t items = tiles * Hkv * (seqs + max_rows * (Hq / Hkv) / kPartCols);
+  return items < 0x7fffffff ? items : 0x7fffffff;
+}
+int64_t window_sums_bytes(int64_t items) { return items * kTileKeys * 4 + kWindowLaunchSeqs * 4; }
+
 hipError_t launch_window_weights_bf16(const uint16_t* q, const uint16_t* k_cache, const RowKeys& rk,
                                       int n_rows, int Hq, int Hkv, const float* stats, float* sums,
-                                      float* weights, int num_cus, hipStream_t st) {
+                                      int64_t items_cap, float* weights, int num_cus,
+                                      hipStream_t st) {
   if (n_rows <= 0 || rk.n_seqs <= 0) return hipSuccess;
-  const int64_t entries = most_entries(rk, n_rows);
-  const int64_t tiles = (entries + kTileBlocks - 1) / kTileBlocks * Hkv;
-  if (rk.n_seqs > 65535 || tiles > 0x7fffffff || Hq > 16 * Hkv) return hipErrorInvalidValue;
-  COCO_LAUNCH(window_weights_kernel, dim3((unsigned)tiles, rk.n_seqs), dim3(64 * kWaves), 0, st, q,
-              k_cache, rk, Hq, Hkv, kLog2e / sqrtf((float)HD), stats, sums);
-  COCO_LAUNCH_LAST(window_weights_add_kernel,
-                   dim3((unsigned)((entries * kBlockTokens + 255) / 256), rk.n_seqs), dim3(256), 0,
-                   st, rk, Hkv, sums, weights);
+  if (Hq > 16 * Hkv || num_cus <= 0) return hipErrorInvalidValue;
+  const int64_t entries = most_entries(rk, n_rows), width = (int64_t)rk.max_blocks * kBlockTokens;
+  int32_t* items0 = (int32_t*)(sums + items_cap * kTileKeys);
+  RowKeys part = rk;
+  for (int s0 = 0; s0 < rk.n_seqs; s0 += kWindowLaunchSeqs) {
+    part.seq_starts = rk.seq_starts + s0;
+    part.ctx_lens = rk.ctx_lens + s0;
+    part.block_table = rk.block_table + (int64_t)s0 * rk.max_blocks;
+    part.n_seqs = rk.n_seqs - s0 < kWindowLaunchSeqs ? rk.n_seqs - s0 : kWindowLaunchSeqs;
+    COCO_LAUNCH(window_weights_kernel, dim3(kWorkgroups * num_cus), dim3(64 * kWaves), 0, st, q,
+                k_cache, part, Hq, Hkv, kLog2e / sqrtf((float)HD), stats, sums, items_cap, items0);
+    COCO_LAUNCH_LAST(window_weights_add_kernel,
+                     dim3((unsigned)((entries * kBlockTokens + 63) / 64), part.n_seqs),
+                     dim3(64 * kWaves), 0, st, part, Hq / Hkv, Hkv, sums, items_cap, items0,
+                     weights + s0 * width);
+  }
   return hipGetLastError();
 }
 

@@ -68,6 +68,8 @@ def test_prompts_of_every_head_layout(dtype, hq, hkv, hd):
     (1500, 40, [2600, 300], [70, 300]),
     (ALL, 0, [1400], [1400]),                      # many tiles, in one part
     (130, 1, [1400, 5], [1300, 5]),
+    (40, 700, [1500, 640], [900, 640]),            # first tokens wider than the window
+    (300, 0, [2100], [2100]),
 ])
 def test_long_prompts(window, sinks, lens, rows):
     r = Rows("bf16", 4, 1, 128, lens, rows, window, sinks, seed=6)
