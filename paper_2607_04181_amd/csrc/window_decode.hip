@@ -210,64 +210,76 @@ __global__ __launch_bounds__(64 * kWaves, 3) void window_decode_kernel(DecodeArg
   }
 }
 
-// A row's maximum and sum of weights at one head, from its parts.
-__device__ __forceinline__ f32x2_t row_stats(const DecodeArgs& a, int64_t at, int G, int parts) {
-  float M = -INFINITY, L = 0.f;
-  for (int p = 0; p < parts; ++p) {
-    const f32x2_t ml = *(const f32x2_t*)(a.part_ml + 2 * (at + (int64_t)p * G));
-    const float m_new = fmaxf(M, ml[0]), ref = m_new == -INFINITY ? 0.f : m_new;
-    L = fmaf(L, __builtin_amdgcn_exp2f(M - ref), ml[1] * __builtin_amdgcn_exp2f(ml[0] - ref));
-    M = m_new;
-  }
-  return f32x2_t{M, L};
+// Two partial softmaxes in one: the maximum and sum of (M, L) and (m, l).
+__device__ __forceinline__ f32x2_t merge_stats(f32x2_t a, f32x2_t b) {
+  const float m = fmaxf(a[0], b[0]), ref = m == -INFINITY ? 0.f : m;
+  return f32x2_t{m, fmaf(a[1], __builtin_amdgcn_exp2f(a[0] - ref),
+                         b[1] * __builtin_amdgcn_exp2f(b[0] - ref))};
 }
 
-constexpr int kMergeHeads = 8;   // heads of a workgroup: 32 threads each, four dims a thread
-constexpr int kSumEntries = 16;  // blocks of a workgroup that adds up weights
+constexpr int kGroups = 8;        // of 32 threads, four dims a thread
+constexpr int kSumEntries = 16;   // blocks of a workgroup that adds up weights
+constexpr int kStatHeads = 32;    // heads whose maxima and sums it holds at a time
+constexpr int kStatThreads = 8;   // threads to one of those
 
-// Workgroups below `merges` of a row put its heads' parts together in order, four
-// loads at a time; the others add up the weights of kSumEntries of its blocks,
-// a lane four keys, each wave every fourth key/value head, in wave order.
+// Workgroups below `merges` (query heads) of a row put a head's parts together: each
+// group every eighth part, the groups in order. (One group to a head, four loads at a
+// time: 12.5 us for 4 rows of 32 parts on 64 heads, where this takes 5.0.) The others
+// add up the weights of kSumEntries of its blocks, a lane four keys, each wave every
+// fourth key/value head of kStatHeads query heads, in wave order.
 __global__ __launch_bounds__(256) void window_merge_kernel(DecodeArgs a, int merges) {
-  __shared__ f32x2_t sm_ml[kWaves][16];
-  __shared__ __attribute__((aligned(16))) f32x4_t sm_w[kWaves][kWave];
-  const int i = blockIdx.y, G = a.Hq / a.Hkv;
+  __shared__ f32x2_t sm_ml[kStatHeads];
+  __shared__ __attribute__((aligned(16))) f32x4_t sm_w[kGroups][32];
+  const int i = blockIdx.y, G = a.Hq / a.Hkv, tid = threadIdx.x;
   const RowKeys& rk = a.rk;
   const int p = row_slot(rk, i);
   const WindowList list = window_list(p, p, rk.window, rk.sinks);
   const int parts = max(1, (list.entries + kWindowPart - 1) / kWindowPart);
   if ((int)blockIdx.x < merges) {
-    const int head = blockIdx.x * kMergeHeads + (threadIdx.x >> 5);
-    const int dim = (threadIdx.x & 31) * 4;
-    if (head >= a.Hq) return;
+    const int head = blockIdx.x, group = tid >> 5, dim = (tid & 31) * 4;
     const int64_t at = ((int64_t)i * a.Hkv + head / G) * a.parts * G + head % G;
-    float M = -INFINITY, L = 0.f;
+    f32x2_t ml = {-INFINITY, 0.f};
     f32x4_t y = {0.f, 0.f, 0.f, 0.f};
-    for (int p0 = 0; p0 < parts; p0 += 4) {
+    for (int p0 = group; p0 < parts; p0 += 4 * kGroups) {
       f32x4_t v[4];
-      f32x2_t ml[4];
+      f32x2_t x[4];
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
-        const int64_t x = at + (int64_t)min(p0 + u, parts - 1) * G;
-        ml[u] = *(const f32x2_t*)(a.part_ml + 2 * x);
-        v[u] = *(const f32x4_t*)(a.part_o + x * HD + dim);
+        const int64_t y0 = at + (int64_t)min(p0 + u * kGroups, parts - 1) * G;
+        x[u] = *(const f32x2_t*)(a.part_ml + 2 * y0);
+        v[u] = *(const f32x4_t*)(a.part_o + y0 * HD + dim);
       }
-      float m_new = M;
+      float m = ml[0];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) m_new = fmaxf(m_new, ml[u][0]);
-      const float ref = m_new == -INFINITY ? 0.f : m_new;
-      const float alpha = __builtin_amdgcn_exp2f(M - ref);
+      for (int u = 0; u < 4; ++u) m = fmaxf(m, x[u][0]);
+      const float ref = m == -INFINITY ? 0.f : m, alpha = __builtin_amdgcn_exp2f(ml[0] - ref);
       y *= alpha;
-      L *= alpha;
+      ml[1] *= alpha;
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
-        if (p0 + u >= parts) break;
-        const float f = __builtin_amdgcn_exp2f(ml[u][0] - ref);
-        L = fmaf(f, ml[u][1], L);
+        if (p0 + u * kGroups >= parts) break;
+        const float f = __builtin_amdgcn_exp2f(x[u][0] - ref);
+        ml[1] = fmaf(f, x[u][1], ml[1]);
 #pragma unroll
         for (int r = 0; r < 4; ++r) y[r] = fmaf(f, v[u][r], y[r]);
       }
-      M = m_new;
+      ml[0] = m;
+    }
+    sm_w[group][tid & 31] = y;
+    if ((tid & 31) == 0) sm_ml[group] = ml;
+    __syncthreads();
+    if (group != 0) return;
+    const int groups = min(parts, kGroups);
+    float M = sm_ml[0][0], L = 0.f;
+    for (int u = 1; u < groups; ++u) M = fmaxf(M, sm_ml[u][0]);
+    const float ref = M == -INFINITY ? 0.f : M;
+    y = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    for (int u = 0; u < groups; ++u) {
+      const float f = __builtin_amdgcn_exp2f(sm_ml[u][0] - ref);
+      const f32x4_t v = sm_w[u][tid];
+      L = fmaf(f, sm_ml[u][1], L);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) y[r] = fmaf(f, v[r], y[r]);
     }
     const float inv = L == 0.f ? 0.f : 1.0f / L;
     store4(out_at(a, i, head, dim), y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv);
@@ -275,37 +287,53 @@ __global__ __launch_bounds__(256) void window_merge_kernel(DecodeArgs a, int mer
   }
   const int e0 = ((int)blockIdx.x - merges) * kSumEntries;
   if (e0 >= list.entries) return;
-  const int lane = threadIdx.x & 63;
-  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = tid & 63;
+  const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int e = e0 + lane / 4, t4 = lane % 4 * 4;
   const bool live = e < list.entries;
+  const int step = kStatHeads / G;  // (G <= 16)
   f32x4_t w = {0.f, 0.f, 0.f, 0.f};
-  for (int g = wv; g < a.Hkv; g += kWaves) {
-    const int64_t row = (int64_t)i * a.Hkv + g;
-    if (lane < G) {
-      f32x2_t ml = row_stats(a, row * a.parts * G + lane, G, parts);
-      ml[0] = ml[0] == -INFINITY ? 0.f : ml[0];
-      ml[1] = ml[1] == 0.f ? 0.f : 1.0f / ml[1];
-      sm_ml[wv][lane] = ml;
+  for (int g0 = 0; g0 < a.Hkv; g0 += step) {
+    // The heads' maxima and 1 / sums from their parts, eight threads to one.
+    const int h = tid / kStatThreads, g1 = min(step, a.Hkv - g0);
+    f32x2_t ml = {-INFINITY, 0.f};
+    if (h < g1 * G) {
+      const int64_t at = ((int64_t)i * a.Hkv + g0 + h / G) * a.parts * G + h % G;
+      for (int p0 = tid % kStatThreads; p0 < parts; p0 += kStatThreads)
+        ml = merge_stats(ml, *(const f32x2_t*)(a.part_ml + 2 * (at + (int64_t)p0 * G)));
     }
-    wave_lds_order();
-    const float* z0 =
-        a.scores + (row * ((int64_t)a.parts * kWindowPart) + (live ? e : e0)) * G * kBlockTokens + t4;
-    for (int h = 0; h < G; ++h) {
-      const f32x4_t z = *(const f32x4_t*)(z0 + h * kBlockTokens);
-      const f32x2_t ml = sm_ml[wv][h];
+    ml = merge_stats(ml, f32x2_t{row_swap<0xB1>(ml[0]), row_swap<0xB1>(ml[1])});
+    ml = merge_stats(ml, f32x2_t{row_swap<0x4E>(ml[0]), row_swap<0x4E>(ml[1])});
+    ml = merge_stats(ml, f32x2_t{row_swap<0x141>(ml[0]), row_swap<0x141>(ml[1])});
+    if (g0 > 0) __syncthreads();  // every wave is done with the heads before
+    if (tid % kStatThreads == 0)
+      sm_ml[h] = f32x2_t{ml[0] == -INFINITY ? 0.f : ml[0], ml[1] == 0.f ? 0.f : 1.0f / ml[1]};
+    __syncthreads();
+    for (int g = wv; g < g1; g += kWaves) {
+      const float* z0 = a.scores + (((int64_t)i * a.Hkv + g0 + g) * ((int64_t)a.parts * kWindowPart) +
+                                    (live ? e : e0)) * G * kBlockTokens + t4;
+      for (int h0 = 0; h0 < G; h0 += 4) {
+        f32x4_t z[4];
 #pragma unroll
-      for (int r = 0; r < 4; ++r)
-        w[r] = fmaf(__builtin_amdgcn_exp2f(fmaf(z[r], a.scale_log2, -ml[0])), ml[1], w[r]);
+        for (int u = 0; u < 4; ++u) z[u] = *(const f32x4_t*)(z0 + min(h0 + u, G - 1) * kBlockTokens);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          if (h0 + u >= G) break;
+          const f32x2_t x = sm_ml[g * G + h0 + u];
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            w[r] = fmaf(__builtin_amdgcn_exp2f(fmaf(z[u][r], a.scale_log2, -x[0])), x[1], w[r]);
+        }
+      }
     }
-    wave_lds_order();
   }
-  sm_w[wv][lane] = w;
+  f32x4_t* const sums = &sm_w[0][0];
+  sums[wv * kWave + lane] = w;
   __syncthreads();
   if (wv != 0 || !live) return;
-  f32x4_t sum = sm_w[0][lane];
+  f32x4_t sum = sums[lane];
 #pragma unroll
-  for (int u = 1; u < kWaves; ++u) sum += sm_w[u][lane];
+  for (int u = 1; u < kWaves; ++u) sum += sums[u * kWave + lane];
   const int t0 = list.block(e) * kBlockTokens;
   const uint32_t seen = window_bits(t0, p, rk.window, rk.sinks) >> t4;
   float* to = a.weights + (int64_t)i * rk.max_blocks * kBlockTokens + t0 + t4;
@@ -356,9 +384,8 @@ hipError_t launch_window_decode_bf16(const uint16_t* q, const uint16_t* k_cache,
     return hipGetLastError();
   }
   COCO_LAUNCH(window_decode_kernel, grid, dim3(64 * kWaves), 0, st, a);
-  const int merges = (Hq + kMergeHeads - 1) / kMergeHeads;
   const int sums = weights != nullptr ? parts * (kWindowPart / kSumEntries) : 0;
-  COCO_LAUNCH_LAST(window_merge_kernel, dim3(merges + sums, n_rows), dim3(256), 0, st, a, merges);
+  COCO_LAUNCH_LAST(window_merge_kernel, dim3(Hq + sums, n_rows), dim3(256), 0, st, a, Hq);
   return hipGetLastError();
 }
 

@@ -193,8 +193,9 @@ __global__ __launch_bounds__(64 * kWaves, kWorkgroups) void window_weights_kerne
     if (c0 >= cols) continue;
     // A step's columns, from row j's head r on, of `left`. Wave w brings columns 8 w .. + 7
     // as two halves of their dims, 128 bytes a column, so that a load is of whole lines
-    // (in operand order, 32 bytes of a line at a time, 51 us for 48). Chunk x of a half at x ^ (column % 8): rows of 128 bytes would meet in the
-    // same banks. Then the columns' statistics, two floats in each 32 bytes.
+    // (in operand order, 32 bytes of a line at a time, 51 us for 48). Chunk x of a half at
+    // x ^ (column % 8): rows of 128 bytes would meet in the same banks. Then the columns'
+    // statistics, two floats in each 32 bytes.
     struct Step {
       int j, r, left;
     };
