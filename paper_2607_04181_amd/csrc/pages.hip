@@ -322,6 +322,124 @@ __global__ __launch_bounds__(256) void page_compact_kernel(
   }
 }
 
+// The same for long lists: the tokens of 64 positions (32 where one takes more than 512
+// bytes of a head) at a time. A lane puts four tokens' elements of a dim of a value tile
+// together and stores them as one, where all four move (at a list's ends one by one).
+// What bounds it is a group's chain: list, table, tokens, their stores; the places of
+// a group are looked up while the tokens of the one before are on their way. 64 lists of
+// 2000 tokens out of 2200, 8 heads of 128 dims, 8 pools take 1087 us (3.9 TB/s; 16 at a
+// time 1852), one list of 4000 177 (867), but 64 of 6 tokens 41 in place of 19. The two
+// meet at 32 tokens (46 us for 64 lists): the room that a call has per list decides.
+constexpr int kFewKept = 32;  // tokens a list, on average
+template <typename T>
+constexpr int compact_tokens(int HS) {  // (held in registers)
+  return HS * sizeof(T) <= 16 ? 4 * kBlockTokens : 2 * kBlockTokens;
+}
+template <typename T, int HS>
+__global__ __launch_bounds__(256) void page_compact_long_kernel(
+    const int32_t* __restrict__ seq, const int32_t* __restrict__ base,
+    const int32_t* __restrict__ kept, const int32_t* __restrict__ starts, int n_kept,
+    const int32_t* __restrict__ table, int n_seqs, int max_blocks, int64_t num_blocks,
+    CachePools pools, int Hkv) {
+  constexpr int kTok = compact_tokens<T>(HS), kTile = kBlockTokens * 32 * HS;
+  constexpr int kPer = 16 / sizeof(T);                // elements of a piece
+  constexpr int kKeys = kTok * 32 * HS / kPer / 256;  // pieces of a thread
+  constexpr int kVals = kTok / 4 * HS / 8;            // its (four tokens, 32 dims) of a half wave
+  typedef T quad_t __attribute__((ext_vector_type(4)));
+  __shared__ int64_t from_s[2][kTok], to_s[2][kTok];  // tile << 4 | slot; -1: nothing moves
+  const int i = blockIdx.x, g = blockIdx.y, tid = threadIdx.x;
+  T* pool = (T*)pools.p[blockIdx.z];
+  const int row = seq[i];
+  const int k0 = max(starts[i], 0), k1 = min(starts[i + 1], n_kept), b0 = base[i];
+  if (row < 0 || row >= n_seqs || k0 >= k1) return;
+  const int32_t* bt = table + (int64_t)row * max_blocks;
+  const int last = max_blocks * kBlockTokens;
+  auto place = [&](int pos) -> int64_t {
+    if (pos < 0 || pos >= last) return -1;
+    const int blk = bt[pos / kBlockTokens];
+    return blk < 0 || blk >= num_blocks
+               ? -1
+               : (((int64_t)blk * Hkv + g) << 4 | (pos % kBlockTokens));
+  };
+  // Places of the group whose first position is d0 (of a block's start, or below the base).
+  auto look_up = [&](int64_t d0, int half) {
+    if (tid >= kTok) return;
+    const int64_t k = k0 + (d0 - b0) + tid;
+    const bool live = k >= k0 && k < k1;
+    const int pos = live ? kept[k] : -1, to = (int)(d0 + tid);
+    const bool moves = live && pos != to;
+    const int64_t f = moves ? place(pos) : -1, t = moves ? place(to) : -1;
+    from_s[half][tid] = t < 0 ? -1 : f;
+    to_s[half][tid] = f < 0 ? -1 : t;
+  };
+  const int64_t first = b0 & ~(kBlockTokens - 1), end = (int64_t)b0 + (k1 - k0);
+  look_up(first, 0);
+  __syncthreads();
+  int half = 0;
+  for (int64_t d0 = first; d0 < end; d0 += kTok, half ^= 1) {
+    const int64_t *from = from_s[half], *to = to_s[half];
+    if (blockIdx.z & 1) {
+      const int w = tid & 31;
+      quad_t r[kVals];
+#pragma unroll
+      for (int u = 0; u < kVals; ++u) {
+        const int unit = (tid >> 5) + 8 * u, t4 = unit % (kTok / 4) * 4, dims = unit / (kTok / 4);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int64_t f = max(from[t4 + e], (int64_t)0);  // (any place: not stored)
+          r[u][e] = pool[(f >> 4) * kTile + dims * 512 + ((int)f & 12) * 32 + w * 4 + ((int)f & 3)];
+        }
+      }
+      if (d0 + kTok < end) look_up(d0 + kTok, half ^ 1);
+      wait_vmcnt<0>();  // every value is here before any is overwritten
+      __syncthreads();
+#pragma unroll
+      for (int u = 0; u < kVals; ++u) {
+        const int unit = (tid >> 5) + 8 * u, t4 = unit % (kTok / 4) * 4, dims = unit / (kTok / 4);
+        int64_t t[4];
+        bool all = true;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          t[e] = to[t4 + e];
+          all = all && t[e] >= 0;
+        }
+        T* const x = pool + (int64_t)dims * 512 + w * 4;
+        if (all) {
+          *(quad_t*)(x + (t[0] >> 4) * kTile + ((int)t[0] & 12) * 32) = r[u];
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (t[e] >= 0) x[(t[e] >> 4) * kTile + ((int)t[e] & 12) * 32 + ((int)t[e] & 3)] = r[u][e];
+        }
+      }
+    } else {
+      // Piece c of a token: elements c kPer .. of it.
+      u32x4_t r[kKeys];
+      const auto at = [&](int64_t x, int c) -> u32x4_t* {
+        const int h = c * kPer;
+        return (u32x4_t*)(pool + (x >> 4) * kTile + (h >> 3) * 128 + ((int)x & 15) * 8 + (h & 7));
+      };
+#pragma unroll
+      for (int u = 0; u < kKeys; ++u) {
+        const int x = tid + 256 * u;
+        r[u] = *at(max(from[x % kTok], (int64_t)0), x / kTok);
+      }
+      if (d0 + kTok < end) look_up(d0 + kTok, half ^ 1);
+      wait_vmcnt<0>();
+      __syncthreads();
+#pragma unroll
+      for (int u = 0; u < kKeys; ++u) {
+        const int x = tid + 256 * u;
+        const int64_t t = to[x % kTok];
+        if (t >= 0) *at(t, x / kTok) = r[u];
+      }
+    }
+    // (The next group reads above everything that this one writes; the places of the
+    // one after it go where this one's were.)
+    __syncthreads();
+  }
+}
+
 }  // namespace
 
 hipError_t launch_page_plan(const PageArgs& a, hipStream_t st) {
@@ -371,9 +489,11 @@ hipError_t launch_page_compact(const int32_t* seq, const int32_t* base, const in
                                const CachePools& pools, int Hkv, int hd, hipStream_t st) {
   if (n <= 0 || n_kept <= 0) return hipSuccess;
   if (hd % 32 != 0 || hd > 256 || Hkv > 65535) return hipErrorInvalidValue;
+  const bool few = n_kept <= (int64_t)n * kFewKept;
 #define COCO_COMPACT(HS)                                                                        \
-  COCO_LAUNCH_LAST((page_compact_kernel<T, HS>), dim3(n, Hkv, pools.n), dim3(256), 0, st, seq,  \
-                   base, kept, starts, n_kept, table, n_seqs, max_blocks, num_blocks, pools, Hkv)
+  COCO_LAUNCH_LAST((few ? page_compact_kernel<T, HS> : page_compact_long_kernel<T, HS>),        \
+                   dim3(n, Hkv, pools.n), dim3(256), 0, st, seq, base, kept, starts, n_kept,    \
+                   table, n_seqs, max_blocks, num_blocks, pools, Hkv)
   COCO_BY_HEAD_DIM(COCO_COMPACT);
 #undef COCO_COMPACT
   return hipGetLastError();

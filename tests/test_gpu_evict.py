@@ -262,3 +262,46 @@ def test_a_bounded_cache_through_its_calls(dtype, hq, hkv, hd):
         tol = tolerance(dtype, ref, mean, size, len(at), hd)
         assert (np.abs(o[s].cpu().double().numpy() - ref) <= tol).all()
     assert np.abs((weights.cpu().numpy() - w1).sum(1) - hq).max() < 1e-3
+
+
+@pytest.mark.parametrize("dtype,hkv,hd", [("bf16", 3, 128), ("f32", 2, 32), ("f32", 1, 96), ("f32", 1, 160),
+                                          ("f32", 2, 256)])
+def test_lists_move_alike_however_long_the_calls_list_is(dtype, hkv, hd):
+    """Short and long lists, from bases anywhere in a block, with places that no block
+    holds, in calls with room for little more than them and for many more."""
+    rng = np.random.default_rng(hd)
+    #        base, candidates, share kept
+    cases = [(0, 40, 0.5), (37, 26, 0.3), (5, 1, 1.0), (16, 300, 0.7), (3, 64, 1.0), (8, 9, 0.0),
+             (100, 200, 0.1), (15, 17, 0.5), (31, 290, 0.9), (2, 66, 1.0)]
+    lens = [b + n for b, n, _ in cases]
+    width, nb = 24, sum(-(-n // B) for n in lens) + 2
+    c = Cache(dtype, hkv, hkv, hd, nb, width, n_layers=2, seed=9)
+    table = tables(rng, lens, width, nb)
+    whole = table.copy()
+    table[3, 9], table[8, 3], table[8, 12] = -1, nb, -5
+    for few in (True, False):
+        rows = rng.permutation(len(cases))
+        base = np.array([cases[r][0] for r in rows])
+        kept = [cases[r][0] + np.nonzero(rng.random(cases[r][1]) < cases[r][2])[0] for r in rows]
+        if few:
+            kept = [k[:28] for k in kept]
+        starts = np.concatenate([[0], np.cumsum([len(k) for k in kept])])
+        listed = np.concatenate(kept)
+        assert (len(listed) <= 32 * len(rows)) == few
+        before = [c.tokens(layer) for layer in range(2)]
+        for room in (len(listed), 40 * len(rows)) if few else (len(listed),):
+            for layer in range(2):
+                c.put(layer, *before[layer])
+            coco.coco_kv_compact(c.h, 0, 2, i32(rows), i32(base),
+                                 i32(np.concatenate([listed, np.full(max(room - len(listed), 0), 7)])),
+                                 i32(starts), i32(table))
+            torch.cuda.synchronize()
+            for layer in range(2):
+                for got, old in zip(c.tokens(layer), before[layer]):
+                    want = old.copy()
+                    for r, b, k in zip(rows, base, kept):
+                        to = b + np.arange(len(k))
+                        fine = (table[r, to // B] == whole[r, to // B]) & (table[r, k // B] == whole[r, k // B])
+                        to, k = to[fine], k[fine]
+                        want[table[r, to // B], to % B] = old[table[r, k // B], k % B]
+                    assert np.array_equal(got, want), (few, room, layer)
