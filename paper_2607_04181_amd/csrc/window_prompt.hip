@@ -26,11 +26,12 @@
 // takes no mask. Values that are not finite are looked for once, at the end: where a
 // sum is NaN, the item is done again with such values held apart.
 //
-// What bounds it: at 8000 tokens, 64 heads on 8 and a window of 4096, 400 GFLOP in 434
-// us (0.92 PFLOP/s, where a large product of matrices reaches 1.65). A step of 32 keys
-// takes 1930 cycles, 1024 of them products: a wave that is alone on its SIMD issues
-// about four vector instructions beside a product, and a step has 130 and 32
-// exponentials. 10 us of an item are its start and its end.
+// What bounds it: at 8000 tokens, 32 heads on 8 and a window of 4096, 400 GFLOP in 420
+// us (0.95 PFLOP/s, where a large product of matrices reaches 1.65). A step of 32 keys
+// is 1024 cycles of products for each SIMD and 1136 with the softmax beside them, and
+// with every CU at it the clock is at 1.6 to 1.7 GHz: 0.70 us, for 0.85 in the kernel.
+// Left out one by one, the operands from LDS are 9% of its time, the loads into LDS 6%
+// and the barriers 4%; 10 us of an item are its start and its end.
 //
 // The list of a sequence with at most kSplitCols columns is split into parts by a
 // rule on the sequence's own columns and list, merged by a second kernel in order:
@@ -208,14 +209,17 @@ __device__ __forceinline__ float column_top(float mx, float scale_log2) {
 __device__ __forceinline__ float next_max(const Cols& c, float top) {
   return top > c.m + kLazy ? top : c.m;
 }
-__device__ __forceinline__ void rescale(Cols& c, float m_new) {
-  if (__builtin_expect(__ballot(m_new != c.m) != 0, 0)) {
+__device__ __forceinline__ void rescale_if(bool moved, Cols& c, float m_new) {
+  if (__builtin_expect(moved, 0)) {
     const float alpha = __builtin_amdgcn_exp2f(c.m - m_new);
 #pragma unroll
     for (int i = 0; i < 4; ++i) c.acc[i] *= alpha;
     c.l *= alpha;
     c.m = m_new;
   }
+}
+__device__ __forceinline__ void rescale(Cols& c, float m_new) {
+  rescale_if(__ballot(m_new != c.m) != 0, c, m_new);
 }
 // Weights of 32 keys as operands of two products.
 __device__ __forceinline__ void weights_of(Cols& c, const f32x16_t& z, float scale_log2,
@@ -254,7 +258,7 @@ __device__ __forceinline__ void add_values(Cols& c, const u32x4_t v[2][2][2], co
 // Half a step: sixteen products, and beside each a sixteenth of the other tile's
 // softmax. The products: scores z of the next stage (k, q), then values v with
 // weights p for cv's columns. The softmax: weights w of scores zs for cs's columns.
-// m_next: cv's running max with the next scores. `lds(i)`: operand reads that go out
+// m_now: cs's running max with its scores; m_next: cv's with the next ones. `lds(i)`: operand reads that go out
 // behind product i.
 // Nothing is moved from one sixteenth to another: left to itself, the compiler puts
 // the products back to back and the exponentials behind them, and a wave that is
@@ -265,11 +269,12 @@ __device__ __forceinline__ void add_values(Cols& c, const u32x4_t v[2][2][2], co
 template <typename F>
 __device__ __forceinline__ void half_step(const u32x4_t k[8], const bf16x8_t q[8], f32x16_t& z,
                                           Cols& cv, const u32x4_t v[2][2][2], const u32x4_t p[2],
-                                          Cols& cs, const f32x16_t& zs, u32x4_t w[2], float& m_next,
-                                          float scale_log2, F lds) {
+                                          Cols& cs, const f32x16_t& zs, u32x4_t w[2], float m_now,
+                                          float& m_next, float scale_log2, F lds) {
   z = f32x16_t{};
+  const bool moved = __ballot(m_now != cs.m) != 0;
   float pr[16], ls = 0.f, mx = 0.f, top = 0.f;
-  float x = fmaf(zs[0], scale_log2, -cs.m);
+  float x = fmaf(zs[0], scale_log2, -m_now);
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
     if (i < 8)
@@ -281,7 +286,8 @@ __device__ __forceinline__ void half_step(const u32x4_t k[8], const bf16x8_t q[8
           __builtin_bit_cast(bf16x8_t, p[i >> 2 & 1]), cv.acc[i & 3], 0, 0, 0);
     lds(i);
     pr[i] = __builtin_amdgcn_exp2f(x);
-    if (i < 15) x = fmaf(zs[i + 1], scale_log2, -cs.m);
+    if (i < 15) x = fmaf(zs[i + 1], scale_log2, -m_now);
+    if (i == 7) rescale_if(moved, cs, m_now);  // (at the start, its branch waited: 571 us for 558)
     if (i >= 1) ls = i == 1 ? pr[0] : ls + pr[i - 1];
     if (i >= 2 && i % 2 == 0) w[i - 2 >> 3][i - 2 >> 1 & 3] = pack_bf16x2(pr[i - 2], pr[i - 1]);
     if (i == 9) mx = fmaxf(fmaxf(z[0], z[1]), z[2]);
@@ -591,22 +597,20 @@ __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a
       auto steps = [&](bool masked, int end) {
 #pragma unroll 1
         while (__builtin_expect_with_probability(st < end, 1, 0.99)) {
-          rescale(c[1], m1);
           const uint32_t v_at = v_lane + (st % kRing) * (kStage * 2);
-          half_step(kf, qf[0], z0, c[0], vf, pw[0], c[1], z1, pw[1], m0, a.scale_log2, [&](int i) {
+          half_step(kf, qf[0], z0, c[0], vf, pw[0], c[1], z1, pw[1], m1, m0, a.scale_log2, [&](int i) {
             if (i < 4) {
               read_v_part(v_at, 2 * i, vf);
               read_v_part(v_at, 2 * i + 1, vf);
             }
           });
           if (__builtin_expect(masked, 0)) mask(z0, m0, 0, st + 1);
-          rescale(c[0], m0);
           // begin(st), its loads beside the first products.
           arrive(st);
           const bf16_t* src = source(st + kRing - 1) + lane * 8;
           const uint32_t dst = place(st + kRing - 1);
           const uint32_t k_at = k_lane + (st + 2) % kRing * (kStage * 2);
-          half_step(kf, qf[1], z1, c[1], vf, pw[1], c[0], z0, pw[0], m1, a.scale_log2, [&](int i) {
+          half_step(kf, qf[1], z1, c[1], vf, pw[1], c[0], z0, pw[0], m0, m1, a.scale_log2, [&](int i) {
             if (i == 0) load_tile<0>(src, dst);
             if (i == 1) load_tile<1>(src, dst);
             if (i == 2) load_tile<2>(src, dst);
