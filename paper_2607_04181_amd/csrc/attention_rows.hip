@@ -1,6 +1,6 @@
 // fp32 attention of rows that do not see a plain causal prefix of the paged
 // cache: the nodes of a tree of drafted tokens, rows that attend selected blocks,
-// and rows that see a sliding window and a context's first tokens.
+// and single tokens that see a sliding window and a context's first tokens.
 //
 // One workgroup per row and GH query heads of one key/value head, eight waves
 // striding over the row's blocks with an online softmax each, merged in LDS in
@@ -68,8 +68,7 @@ __global__ __launch_bounds__(64 * kRowsWaves) void attn_rows_kernel(
   int entries;
   WindowList win{};
   if constexpr (MODE == kRowsWindow) {
-    n = min(max(rk.ctx_lens[s], 0), rk.max_blocks * kBlockTokens);
-    if (rk.seq_starts != nullptr) n = max(n + i + 1 - rk.seq_starts[s + 1], 0);
+    n = min(max(rk.ctx_lens[s], 0), rk.max_blocks * kBlockTokens);  // (a row per sequence)
     win = window_list(n - 1, n - 1, rk.window, rk.sinks);
   } else if constexpr (MODE == kRowsTree) {
     n = rk.ctx_lens[s];

@@ -438,6 +438,10 @@ int run_window(coco_layer* H, const coco_layer_weights& w, const void* q, void* 
                                      c.n_kv_heads, (bf16_t*)o, tiled, H->window_part_o,
                                      H->window_part_ml, H->window_parts, H->window_counts, stats,
                                      H->num_cus, st));
+  else if (seq_starts)
+    HIPCHK(launch_window_prompt_f32((const float*)q, (const float*)w.k_cache,
+                                    (const float*)w.v_cache, rk, n_rows, c.n_q_heads, c.n_kv_heads,
+                                    c.head_dim, (float*)o, stats, st));
   else
     HIPCHK(launch_attn_rows_f32((const float*)q, (const float*)w.k_cache, (const float*)w.v_cache,
                                 rk, n_rows, c.n_q_heads, c.n_kv_heads, c.head_dim, (float*)o,
@@ -450,8 +454,8 @@ int run_window(coco_layer* H, const coco_layer_weights& w, const void* q, void* 
                                       H->window_items, weights, H->num_cus, st));
   else
     HIPCHK(launch_window_weights_f32((const float*)q, (const float*)w.k_cache, rk, n_rows,
-                                     c.n_q_heads, c.n_kv_heads, c.head_dim, stats, weights,
-                                     H->num_cus, st));
+                                     c.n_q_heads, c.n_kv_heads, c.head_dim, stats, H->window_sums,
+                                     H->window_items, weights, H->num_cus, st));
   return COCO_OK;
 }
 
@@ -806,7 +810,11 @@ int coco_window_reserve(coco_layer_t H, int32_t max_rows, int32_t max_seqs, int3
   const bool weights = weigh != 0 || H->window_weigh;
   const coco_layer_config& c = H->cfg;
   const size_t stats = weights ? align256((size_t)rows * c.n_q_heads * 8) : 0;
-  if (c.dtype == COCO_BF16) {
+  const bool bf16 = c.dtype == COCO_BF16;
+  const int64_t items =
+      window_weight_items(rows, seqs, c.max_blocks_per_seq, c.n_q_heads, c.n_kv_heads, bf16);
+  const size_t sums = weights ? align256((size_t)window_sums_bytes(items, bf16)) : 0;
+  if (bf16) {
     // Single tokens and prompts use the same room in turn.
     const int64_t few = rows < seqs ? rows : seqs;
     const int64_t blocks = (int64_t)window_parts(INT32_MAX, 0, c.max_blocks_per_seq) * kWindowPart;
@@ -814,9 +822,6 @@ int coco_window_reserve(coco_layer_t H, int32_t max_rows, int32_t max_seqs, int3
     const int64_t prompt = window_column_parts(rows, seqs, c.n_q_heads, c.n_kv_heads);
     const int64_t parts = single > prompt ? single : prompt;
     const size_t o = align256((size_t)parts * c.head_dim * 4), ml = align256((size_t)parts * 8);
-    const int64_t items =
-        window_weight_items(rows, seqs, c.max_blocks_per_seq, c.n_q_heads, c.n_kv_heads);
-    const size_t sums = weights ? align256((size_t)window_sums_bytes(items)) : 0;
     const size_t scores =
         weights ? align256((size_t)few * c.n_q_heads * blocks * kBlockTokens * 4) : 0;
     const size_t both = stats + sums > scores ? stats + sums : scores;
@@ -825,7 +830,6 @@ int coco_window_reserve(coco_layer_t H, int32_t max_rows, int32_t max_seqs, int3
         grow(H, &H->window_ws, &H->window_bytes, o + ml + both + counts, counts);
     if (rc) return rc;
     H->window_parts = parts;
-    H->window_items = items;
     H->window_part_o = (float*)H->window_ws;
     H->window_part_ml = (float*)(H->window_ws + o);
     H->window_stats = (float*)(H->window_ws + o + ml);
@@ -833,10 +837,12 @@ int coco_window_reserve(coco_layer_t H, int32_t max_rows, int32_t max_seqs, int3
     H->window_scores = H->window_stats;
     H->window_counts = (int32_t*)(H->window_ws + o + ml + both);
   } else if (weights) {
-    const int rc = grow(H, &H->window_ws, &H->window_bytes, stats);
+    const int rc = grow(H, &H->window_ws, &H->window_bytes, stats + sums);
     if (rc) return rc;
     H->window_stats = (float*)H->window_ws;
+    H->window_sums = (float*)(H->window_ws + stats);
   }
+  H->window_items = items;
   H->window_rows = rows;
   H->window_seqs = seqs;
   H->window_weigh = weights;

@@ -440,19 +440,25 @@ hipError_t launch_window_prompt_bf16(const uint16_t* q, const uint16_t* k_cache,
                                      int Hkv, uint16_t* o, bool tiled, float* part_o,
                                      float* part_ml, int64_t part_cap, int32_t* counts,
                                      float* stats, int num_cus, hipStream_t st);
+// fp32 handles' prompts (their single tokens: launch_attn_rows_f32).
+hipError_t launch_window_prompt_f32(const float* q, const float* k_cache, const float* v_cache,
+                                    const RowKeys& rk, int n_rows, int Hq, int Hkv, int hd,
+                                    float* o, float* stats, hipStream_t st);
 // weights [n_seqs][max_blocks * 16] grow by the weights of the rows' keys, from
 // the rows' stats; sums: scratch of window_sums_bytes(items_cap), items_cap at least
 // window_weight_items of the call.
-int64_t window_weight_items(int64_t max_rows, int64_t max_seqs, int max_blocks, int Hq, int Hkv);
-int64_t window_sums_bytes(int64_t items);
+int64_t window_weight_items(int64_t max_rows, int64_t max_seqs, int max_blocks, int Hq, int Hkv,
+                            bool bf16);
+int64_t window_sums_bytes(int64_t items, bool bf16);
 hipError_t launch_window_weights_bf16(const uint16_t* q, const uint16_t* k_cache, const RowKeys& rk,
                                       int n_rows, int Hq, int Hkv, const float* stats, float* sums,
                                       int64_t items_cap, float* weights, int num_cus,
                                       hipStream_t st);
-// fp32 handles (the rows' attention is launch_attn_rows_f32).
+// fp32 handles; without seq_starts no sums are needed.
 hipError_t launch_window_weights_f32(const float* q, const float* k_cache, const RowKeys& rk,
                                      int n_rows, int Hq, int Hkv, int hd, const float* stats,
-                                     float* weights, int num_cus, hipStream_t st);
+                                     float* sums, int64_t items_cap, float* weights, int num_cus,
+                                     hipStream_t st);
 
 // ---------------------------------------------------------------- eviction
 struct EvictArgs {

@@ -17,7 +17,8 @@
 // 46 us, 4000 rows of a prompt 118: with 32 keys to a wave and all columns in one item
 // 57 and 393. Of the 46, the products are 10 and the vector instructions 20; the rest
 // are starts of items (tables, keys) and the last round, when some CUs have none.
-// fp32: a workgroup has 16 keys, its waves the key/value heads.
+// fp32: the same of 64 keys, 16 of them in a wave's registers; single tokens without a
+// second kernel.
 #include <math.h>
 
 #include "common.h"
@@ -37,7 +38,7 @@ constexpr int HD = 128;
 constexpr int kTile = kBlockTokens * HD;
 constexpr int kWaves = 4;
 constexpr int kTileBlocks = 4 * kWaves;  // blocks of a workgroup
-constexpr int kTileKeys = kTileBlocks * kBlockTokens;
+constexpr int kTileBlocksF32 = kWaves;
 constexpr int kCols = 32;                // columns of a step
 // Columns of an item: 4000 rows of 32 heads on 8 take 104 us with 512, 118 with 1024 and
 // 141 with 2048, 64 bytes of scratch a key for each; prompts of 64 rows are one item.
@@ -95,7 +96,7 @@ __device__ __forceinline__ float column_sums(const float w[16], int lane) {
   return x[0] + row_swap<0xB1>(x[0]);                                        // lane ^ 1
 }
 
-// A sequence's work: tile k, blocks k kTileBlocks .. of its list, in parts of kPartCols
+// A sequence's work: tile k, blocks k TB .. of its list, in parts of kPartCols
 // of the columns that can see it; key/value heads innermost. Tiles below `many` (those
 // with first tokens, which every row sees) have `most` parts at most, the others `few`.
 // A part past a tile's columns has no work and leaves no sums.
@@ -108,24 +109,82 @@ struct Parts {
 __device__ __forceinline__ int parts_of(int64_t rows, int G) {
   return (int)((rows * G + kPartCols - 1) / kPartCols);
 }
+template <int TB>
 __device__ __forceinline__ Parts seq_parts(const RowKeys& rk, const SeqRows& x, int G) {
   Parts y;
-  y.tiles = (x.list.entries + kTileBlocks - 1) / kTileBlocks;
+  y.tiles = (x.list.entries + TB - 1) / TB;
   const int first = min(rk.sinks / kBlockTokens + (rk.sinks % kBlockTokens != 0), x.list.entries);
-  y.many = (first + kTileBlocks - 1) / kTileBlocks;
+  y.many = (first + TB - 1) / TB;
   y.most = parts_of(x.n, G);
-  // (slots t .. t + 255: rows of slots t .. t + 254 + window)
-  const int64_t rows = (int64_t)rk.window + kTileKeys - 1;
+  // (slots t .. t + 16 TB - 1: rows of slots t .. t + 16 TB - 2 + window)
+  const int64_t rows = (int64_t)rk.window + TB * kBlockTokens - 1;
   y.few = parts_of(rows < x.n ? rows : x.n, G);
   return y;
 }
 // The rows j0 .. j1 - 1 that can see tile k, blocks e0 .. e_last of the list.
+template <int TB>
 __device__ __forceinline__ void tile_rows(const RowKeys& rk, const SeqRows& x, int k, int& e_last,
                                           int& j0, int& j1) {
-  const int e0 = k * kTileBlocks;
-  e_last = min(e0 + kTileBlocks, x.list.entries) - 1;
+  const int e0 = k * TB;
+  e_last = min(e0 + TB, x.list.entries) - 1;
   rows_of(rk, x, x.list.block(e0) * kBlockTokens,
           x.list.block(e_last) * kBlockTokens + kBlockTokens - 1, j0, j1);
+}
+
+// The sequences' items into seqs (and their first ones into items0); all of them. red:
+// one int per wave.
+template <int TB>
+__device__ __forceinline__ int plan_items(const RowKeys& rk, int G, int Hkv, SeqItems* seqs,
+                                          int* red, int32_t* items0) {
+  const int tid = threadIdx.x;
+  int total = 0;
+  for (int s0 = 0; s0 < rk.n_seqs; s0 += 64 * kWaves) {
+    SeqRows x{};
+    if (s0 + tid < rk.n_seqs) x = seq_rows(rk, s0 + tid);
+    const Parts y = seq_parts<TB>(rk, x, G);
+    const int items = (y.many * y.most + (y.tiles - y.many) * y.few) * Hkv;
+    const int item0 = block_prefix<kWaves>(items, red, total) - items;
+    if (s0 + tid < rk.n_seqs) {
+      seqs[s0 + tid] = SeqItems{x.row0, x.n, x.last, item0};
+      if (blockIdx.x == 0) items0[s0 + tid] = item0;
+    }
+  }
+  __syncthreads();
+  return total;
+}
+// An item: blocks e0 .. e_last of sequence s's list for key/value head g, columns c0 ..
+// of the `cols` from row j0 on. False: no work.
+struct Item {
+  int s, g, e0, e_last, j0, c0, cols;
+  SeqRows x;
+};
+template <int TB>
+__device__ __forceinline__ bool find_item(const RowKeys& rk, const SeqItems* seqs, int item, int G,
+                                          int Hkv, Item& it) {
+  const auto one = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+  int lo = 0, hi = rk.n_seqs - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (seqs[mid].item0 <= item) lo = mid; else hi = mid - 1;
+  }
+  it.s = one(lo);
+  SeqRows& x = it.x;
+  x.row0 = one(seqs[it.s].row0);
+  x.n = one(seqs[it.s].n);
+  x.last = one(seqs[it.s].last);
+  x.first = x.last + 1 - x.n;
+  x.list = window_list(max(x.first, -1), x.last, rk.window, rk.sinks);
+  const Parts y = seq_parts<TB>(rk, x, G);
+  const int at = one(item - seqs[it.s].item0), later = at / Hkv - y.many * y.most;
+  it.g = at % Hkv;
+  const int tile = later < 0 ? at / Hkv / y.most : y.many + later / y.few;
+  const int part = later < 0 ? at / Hkv % y.most : later % y.few;
+  int j1;
+  it.e0 = tile * TB;
+  tile_rows<TB>(rk, x, tile, it.e_last, it.j0, j1);
+  it.cols = max(j1 - it.j0, 0) * G;
+  it.c0 = part * kPartCols;
+  return it.c0 < it.cols;
 }
 
 __global__ __launch_bounds__(64 * kWaves, kWorkgroups) void window_weights_kernel(
@@ -140,19 +199,7 @@ __global__ __launch_bounds__(64 * kWaves, kWorkgroups) void window_weights_kerne
   const int tid = threadIdx.x, lane = tid & 63;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int c32 = lane & 31, hf = lane >> 5;
-  int total = 0;
-  for (int s0 = 0; s0 < rk.n_seqs; s0 += 64 * kWaves) {
-    SeqRows x{};
-    if (s0 + tid < rk.n_seqs) x = seq_rows(rk, s0 + tid);
-    const Parts y = seq_parts(rk, x, G);
-    const int items = (y.many * y.most + (y.tiles - y.many) * y.few) * Hkv;
-    const int item0 = block_prefix<kWaves>(items, red, total) - items;
-    if (s0 + tid < rk.n_seqs) {
-      seqs_s[s0 + tid] = SeqItems{x.row0, x.n, x.last, item0};
-      if (blockIdx.x == 0) items0[s0 + tid] = item0;
-    }
-  }
-  __syncthreads();
+  int total = plan_items<kTileBlocks>(rk, G, Hkv, seqs_s, red, items0);
   if (total > sums_cap) total = 0;  // more rows than the call named: no room for their sums
   // (The ring's address goes through a register of its own: the compiler would
   // otherwise wait for every load in flight before each operand read.)
@@ -161,36 +208,17 @@ __global__ __launch_bounds__(64 * kWaves, kWorkgroups) void window_weights_kerne
   // Dims 16 u + 8 hf .. of column c32: chunk 2 u + hf of its halves.
   const uint32_t q_at = ring_at + (c32 >> 3) * 2048 + (c32 & 7) * 128 + (hf ^ (c32 & 7)) * 16;
 
-  auto one = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
 #pragma unroll 1
   for (int item0 = 0, turn = blockIdx.x; item0 < total; item0 += gridDim.x) {
     // (Turned from round to round, by a multiple of the XCDs: a tile's later parts are the
     // ones without work, and a workgroup would get the same ones of several tiles.)
     const int item = item0 + turn;
     turn = (turn + kTurn) % gridDim.x;
-    if (item >= total) continue;
-    int lo = 0, hi = rk.n_seqs - 1;
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (seqs_s[mid].item0 <= item) lo = mid; else hi = mid - 1;
-    }
-    const int s = one(lo);
-    SeqRows x;
-    x.row0 = one(seqs_s[s].row0);
-    x.n = one(seqs_s[s].n);
-    x.last = one(seqs_s[s].last);
-    x.first = x.last + 1 - x.n;
-    x.list = window_list(max(x.first, -1), x.last, rk.window, rk.sinks);
-    const Parts y = seq_parts(rk, x, G);
-    const int at = one(item - seqs_s[s].item0), later = at / Hkv - y.many * y.most;
-    const int g = at % Hkv;
-    const int tile = later < 0 ? at / Hkv / y.most : y.many + later / y.few;
-    const int part = later < 0 ? at / Hkv % y.most : later % y.few;
-    const int e0 = tile * kTileBlocks;
-    int e_last, j0, j1;
-    tile_rows(rk, x, tile, e_last, j0, j1);
-    const int cols = max(j1 - j0, 0) * G, c0 = part * kPartCols;
-    if (c0 >= cols) continue;
+    Item it;
+    if (item >= total || !find_item<kTileBlocks>(rk, seqs_s, item, G, Hkv, it)) continue;
+    const SeqRows& x = it.x;
+    const int s = it.s, g = it.g, e0 = it.e0, e_last = it.e_last, j0 = it.j0, c0 = it.c0;
+
     // A step's columns, from row j's head r on, of `left`. Wave w brings columns 8 w .. + 7
     // as two halves of their dims, 128 bytes a column, so that a load is of whole lines
     // (in operand order, 32 bytes of a line at a time, 51 us for 48). Chunk x of a half at
@@ -217,7 +245,7 @@ __global__ __launch_bounds__(64 * kWaves, kWorkgroups) void window_weights_kerne
       __builtin_amdgcn_global_load_lds(stats_seq + head * 2 + (lane & 1),
                                        (lds_void_t*)(uintptr_t)to_stats, 4, 0, 0);
     };
-    Step now{j0 + c0 / G, c0 % G, min(cols - c0, kPartCols)}, ahead = now;
+    Step now{j0 + c0 / G, c0 % G, min(it.cols - c0, kPartCols)}, ahead = now;
     for (int i = 0; i < kRing - 1; ++i) {
       issue(ahead, i);
       if (ahead.left > kCols) next(ahead);
@@ -298,7 +326,7 @@ __global__ __launch_bounds__(64 * kWaves, kWorkgroups) void window_weights_kerne
       next(now);
     }
     // (a tile's keys in the order of its list)
-    float* const to = sums + (int64_t)item * kTileKeys + 64 * wv;
+    float* const to = sums + (int64_t)item * (kTileBlocks * kBlockTokens) + 64 * wv;
 #pragma unroll
     for (int y = 0; y < 2; ++y) {
       const float out = column_sums(w[y], lane);
@@ -310,11 +338,90 @@ __global__ __launch_bounds__(64 * kWaves, kWorkgroups) void window_weights_kerne
   }
 }
 
+// fp32: a workgroup's waves have a block of 16 keys each, and walk the item's columns 16
+// at a time, the keys' and the columns' operands from memory: S[16 keys][16 columns] =
+// K Q^T, 8 HS x mfma 16x16x4 of 32 cycles each, which bound it. 2000 rows of a prompt, 16
+// heads of 64 on 4, take 105 us (2680 with a workgroup that walked them for its 16 keys).
+template <int HS>
+__global__ __launch_bounds__(64 * kWaves, 2) void window_weights_rows_f32_kernel(
+    const float* __restrict__ q, const float* __restrict__ k_cache, RowKeys rk, int Hq, int Hkv,
+    float scale_log2, const float* __restrict__ stats, float* __restrict__ sums, int64_t sums_cap,
+    int32_t* __restrict__ items0) {
+  constexpr int hd = 32 * HS;
+  __shared__ SeqItems seqs_s[kWindowLaunchSeqs];
+  __shared__ int red[kWaves];
+  const int G = Hq / Hkv, lane = threadIdx.x & 63, c16 = lane & 15, j4 = lane >> 4;
+  const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int total = plan_items<kTileBlocksF32>(rk, G, Hkv, seqs_s, red, items0);
+  if (total > sums_cap) total = 0;  // more rows than the call named: no room for their sums
+#pragma unroll 1
+  for (int item0 = 0, turn = blockIdx.x; item0 < total; item0 += gridDim.x) {
+    const int item = item0 + turn;
+    turn = (turn + kTurn) % gridDim.x;
+    Item it;
+    if (item >= total || !find_item<kTileBlocksF32>(rk, seqs_s, item, G, Hkv, it)) continue;
+    const int b = it.x.list.block(min(it.e0 + wv, it.e_last)), t0 = b * kBlockTokens;
+    const int id = readable_block(rk.block_table[(int64_t)it.s * rk.max_blocks + b], rk.num_blocks);
+    const float* kb = k_cache + ((int64_t)id * Hkv + it.g) * (kBlockTokens * hd) + lane * 8;
+    f32x4_t kf[HS][2];
+#pragma unroll
+    for (int y = 0; y < HS; ++y) {
+      kf[y][0] = *(const f32x4_t*)(kb + y * 512);
+      kf[y][1] = *(const f32x4_t*)(kb + y * 512 + 4);
+    }
+    const int end = min(it.c0 + kPartCols, it.cols);
+    f32x4_t w = {0.f, 0.f, 0.f, 0.f}, qf[HS][2];
+    f32x2_t st;
+    int p;
+    const auto load = [&](int c0) {
+      const int c = min(c0 + c16, end - 1), j = it.j0 + c / G;
+      const int64_t head = (int64_t)(it.x.row0 + j) * Hq + it.g * G + c % G;
+      const float* qp = q + head * hd + 8 * j4;
+#pragma unroll
+      for (int y = 0; y < HS; ++y) {
+        qf[y][0] = *(const f32x4_t*)(qp + 32 * y);
+        qf[y][1] = *(const f32x4_t*)(qp + 32 * y + 4);
+      }
+      st = *(const f32x2_t*)(stats + head * 2);
+      if (c0 + c16 >= end) st[1] = 0.f;
+      p = max(it.x.first + j, -1);
+    };
+    load(it.c0);
+    for (int c0 = it.c0; c0 < end; c0 += 16) {
+      f32x4_t z = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int y = 0; y < HS; ++y)
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          z = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[y][e / 4][e % 4], qf[y][e / 4][e % 4], z, 0, 0,
+                                                   0);
+      const f32x2_t now = st;
+      const uint32_t seen = window_bits(t0, p, rk.window, rk.sinks) >> (4 * j4);
+      if (c0 + 16 < end) load(c0 + 16);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float x = seen >> r & 1 ? fmaf(z[r], scale_log2, -now[0]) : -INFINITY;
+        w[r] = fmaf(__builtin_amdgcn_exp2f(x), now[1], w[r]);
+      }
+    }
+    float out = 0.f;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const float v = row_sum16(w[r]);
+      if (c16 == r) out = v;
+    }
+    if (c16 < 4)
+      sums[(int64_t)item * (kTileBlocksF32 * kBlockTokens) + kBlockTokens * wv + 4 * j4 + c16] = out;
+  }
+}
+
 // A key's sums of the parts and key/value heads, each wave every fourth in order, the
 // waves in order: a lane a key, 64 keys to a workgroup.
+template <int TB>
 __global__ __launch_bounds__(64 * kWaves) void window_weights_add_kernel(
     RowKeys rk, int G, int Hkv, const float* __restrict__ sums, int64_t sums_cap,
     const int32_t* __restrict__ items0, float* __restrict__ weights) {
+  constexpr int kTileKeys = TB * kBlockTokens;
   __shared__ float sm[kWaves][64];
   const int s = blockIdx.y, lane = threadIdx.x & 63;
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -322,9 +429,9 @@ __global__ __launch_bounds__(64 * kWaves) void window_weights_add_kernel(
   const int e = blockIdx.x * (64 / kBlockTokens) + lane / kBlockTokens;
   const int tile = blockIdx.x / (kTileKeys / 64);
   if ((int)blockIdx.x * (64 / kBlockTokens) >= x.list.entries) return;
-  const Parts y = seq_parts(rk, x, G);
+  const Parts y = seq_parts<TB>(rk, x, G);
   int e_last, j0, j1;
-  tile_rows(rk, x, tile, e_last, j0, j1);
+  tile_rows<TB>(rk, x, tile, e_last, j0, j1);
   const int64_t item = items0[s] + (int64_t)Hkv * (tile < y.many
                                                        ? tile * y.most
                                                        : y.many * y.most + (tile - y.many) * y.few);
@@ -344,6 +451,7 @@ __global__ __launch_bounds__(64 * kWaves) void window_weights_add_kernel(
   if (t <= x.last && v != 0.f) weights[(int64_t)s * rk.max_blocks * kBlockTokens + t] += v;
 }
 
+// fp32, single tokens: a workgroup has 16 keys, its waves the key/value heads.
 constexpr int kRowsWaves = 8;
 
 // HS: head_dim / 32. Lane (t, j4): dims 32 p + 8 j4 .. + 7 of key t.
@@ -413,32 +521,36 @@ int64_t most_entries(const RowKeys& rk, int n_rows) {
 }  // namespace
 
 // The most items of any launch of a call of so many rows and sequences.
-int64_t window_weight_items(int64_t max_rows, int64_t max_seqs, int max_blocks, int Hq, int Hkv) {
+int64_t window_weight_items(int64_t max_rows, int64_t max_seqs, int max_blocks, int Hq, int Hkv,
+                            bool bf16) {
   int64_t seqs = max_seqs < kWindowLaunchSeqs ? max_seqs : kWindowLaunchSeqs;
   if (max_rows < seqs) seqs = max_rows;
-  const int64_t tiles = (max_blocks + kTileBlocks - 1) / kTileBlocks;
+  const int tb = bf16 ? kTileBlocks : kTileBlocksF32;
+  const int64_t tiles = (max_blocks + tb - 1) / tb;
   const int64_t items = tiles * Hkv * (seqs + max_rows * (Hq / Hkv) / kPartCols);
   return items < 0x7fffffff ? items : 0x7fffffff;
 }
-int64_t window_sums_bytes(int64_t items) { return items * kTileKeys * 4 + kWindowLaunchSeqs * 4; }
+int64_t window_sums_bytes(int64_t items, bool bf16) {
+  return items * (bf16 ? kTileBlocks : kTileBlocksF32) * kBlockTokens * 4 + kWindowLaunchSeqs * 4;
+}
 
-hipError_t launch_window_weights_bf16(const uint16_t* q, const uint16_t* k_cache, const RowKeys& rk,
-                                      int n_rows, int Hq, int Hkv, const float* stats, float* sums,
-                                      int64_t items_cap, float* weights, int num_cus,
-                                      hipStream_t st) {
-  if (n_rows <= 0 || rk.n_seqs <= 0) return hipSuccess;
-  if (Hq > 16 * Hkv || num_cus <= 0) return hipErrorInvalidValue;
+namespace {
+
+// run(the sequences' arrays, their number, items0, their weights) for each launch's
+// sequences, then their sums.
+template <int TB, typename F>
+hipError_t weigh_prompts(const RowKeys& rk, int n_rows, int Hq, int Hkv, float* sums,
+                         int64_t items_cap, float* weights, hipStream_t st, F run) {
   const int64_t entries = most_entries(rk, n_rows), width = (int64_t)rk.max_blocks * kBlockTokens;
-  int32_t* items0 = (int32_t*)(sums + items_cap * kTileKeys);
+  int32_t* items0 = (int32_t*)(sums + items_cap * (TB * kBlockTokens));
   RowKeys part = rk;
   for (int s0 = 0; s0 < rk.n_seqs; s0 += kWindowLaunchSeqs) {
     part.seq_starts = rk.seq_starts + s0;
     part.ctx_lens = rk.ctx_lens + s0;
     part.block_table = rk.block_table + (int64_t)s0 * rk.max_blocks;
     part.n_seqs = rk.n_seqs - s0 < kWindowLaunchSeqs ? rk.n_seqs - s0 : kWindowLaunchSeqs;
-    COCO_LAUNCH(window_weights_kernel, dim3(kWorkgroups * num_cus), dim3(64 * kWaves), 0, st, q,
-                k_cache, part, Hq, Hkv, kLog2e / sqrtf((float)HD), stats, sums, items_cap, items0);
-    COCO_LAUNCH_LAST(window_weights_add_kernel,
+    run(part, items0);
+    COCO_LAUNCH_LAST(window_weights_add_kernel<TB>,
                      dim3((unsigned)((entries * kBlockTokens + 63) / 64), part.n_seqs),
                      dim3(64 * kWaves), 0, st, part, Hq / Hkv, Hkv, sums, items_cap, items0,
                      weights + s0 * width);
@@ -446,17 +558,42 @@ hipError_t launch_window_weights_bf16(const uint16_t* q, const uint16_t* k_cache
   return hipGetLastError();
 }
 
+}  // namespace
+
+hipError_t launch_window_weights_bf16(const uint16_t* q, const uint16_t* k_cache, const RowKeys& rk,
+                                      int n_rows, int Hq, int Hkv, const float* stats, float* sums,
+                                      int64_t items_cap, float* weights, int num_cus,
+                                      hipStream_t st) {
+  if (n_rows <= 0 || rk.n_seqs <= 0) return hipSuccess;
+  if (Hq > 16 * Hkv || num_cus <= 0) return hipErrorInvalidValue;
+  return weigh_prompts<kTileBlocks>(
+      rk, n_rows, Hq, Hkv, sums, items_cap, weights, st, [&](const RowKeys& part, int32_t* items0) {
+        COCO_LAUNCH(window_weights_kernel, dim3(kWorkgroups * num_cus), dim3(64 * kWaves), 0, st, q,
+                    k_cache, part, Hq, Hkv, kLog2e / sqrtf((float)HD), stats, sums, items_cap,
+                    items0);
+      });
+}
+
 hipError_t launch_window_weights_f32(const float* q, const float* k_cache, const RowKeys& rk,
                                      int n_rows, int Hq, int Hkv, int hd, const float* stats,
-                                     float* weights, int num_cus, hipStream_t st) {
+                                     float* sums, int64_t items_cap, float* weights, int num_cus,
+                                     hipStream_t st) {
   typedef float T;
   if (n_rows <= 0 || rk.n_seqs <= 0) return hipSuccess;
-  const int64_t entries = most_entries(rk, n_rows);
-  if (rk.n_seqs > 65535 || hd % 32 != 0) return hipErrorInvalidValue;
+  if (rk.n_seqs > 65535 || hd % 32 != 0 || num_cus <= 0) return hipErrorInvalidValue;
   const float scale_log2 = kLog2e / sqrtf((float)hd);
 #define COCO_WEIGH(HS)                                                                           \
-  COCO_LAUNCH_LAST((window_weights_f32_kernel<HS>), dim3((unsigned)entries, rk.n_seqs),          \
-                   dim3(64 * kRowsWaves), 0, st, q, k_cache, rk, Hq, Hkv, scale_log2, stats, weights)
+  if (rk.seq_starts != nullptr)                                                                  \
+    return weigh_prompts<kTileBlocksF32>(                                                        \
+        rk, n_rows, Hq, Hkv, sums, items_cap, weights, st,                                       \
+        [&](const RowKeys& part, int32_t* items0) {                                              \
+          COCO_LAUNCH((window_weights_rows_f32_kernel<HS>), dim3(kWorkgroups * num_cus),         \
+                      dim3(64 * kWaves), 0, st, q, k_cache, part, Hq, Hkv, scale_log2, stats,    \
+                      sums, items_cap, items0);                                                  \
+        });                                                                                      \
+  COCO_LAUNCH_LAST((window_weights_f32_kernel<HS>),                                              \
+                   dim3((unsigned)most_entries(rk, n_rows), rk.n_seqs), dim3(64 * kRowsWaves),   \
+                   0, st, q, k_cache, rk, Hq, Hkv, scale_log2, stats, weights)
   COCO_BY_HEAD_DIM(COCO_WEIGH);
 #undef COCO_WEIGH
   return hipGetLastError();
