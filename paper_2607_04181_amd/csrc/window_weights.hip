@@ -19,6 +19,7 @@
 // are starts of items (tables, keys) and the last round, when some CUs have none.
 // fp32: the same of 64 keys, 16 of them in a wave's registers; single tokens without a
 // second kernel.
+#include <limits.h>
 #include <math.h>
 
 #include "common.h"
@@ -131,11 +132,12 @@ __device__ __forceinline__ void tile_rows(const RowKeys& rk, const SeqRows& x, i
           x.list.block(e_last) * kBlockTokens + kBlockTokens - 1, j0, j1);
 }
 
-// The sequences' items into seqs (and their first ones into items0); all of them. red:
-// one int per wave.
+// The sequences' items into seqs, and their first ones into items0 for the sums' kernel;
+// all of them. More than `cap` (more rows than the call named: no room for their sums):
+// none, for it too. red: one int per wave.
 template <int TB>
-__device__ __forceinline__ int plan_items(const RowKeys& rk, int G, int Hkv, SeqItems* seqs,
-                                          int* red, int32_t* items0) {
+__device__ __forceinline__ int plan_items(const RowKeys& rk, int G, int Hkv, int64_t cap,
+                                          SeqItems* seqs, int* red, int32_t* items0) {
   const int tid = threadIdx.x;
   int total = 0;
   for (int s0 = 0; s0 < rk.n_seqs; s0 += 64 * kWaves) {
@@ -144,13 +146,13 @@ __device__ __forceinline__ int plan_items(const RowKeys& rk, int G, int Hkv, Seq
     const Parts y = seq_parts<TB>(rk, x, G);
     const int items = (y.many * y.most + (y.tiles - y.many) * y.few) * Hkv;
     const int item0 = block_prefix<kWaves>(items, red, total) - items;
-    if (s0 + tid < rk.n_seqs) {
-      seqs[s0 + tid] = SeqItems{x.row0, x.n, x.last, item0};
-      if (blockIdx.x == 0) items0[s0 + tid] = item0;
-    }
+    if (s0 + tid < rk.n_seqs) seqs[s0 + tid] = SeqItems{x.row0, x.n, x.last, item0};
   }
   __syncthreads();
-  return total;
+  if (blockIdx.x == 0)
+    for (int s = tid; s < rk.n_seqs; s += 64 * kWaves)
+      items0[s] = total > cap ? INT_MAX : seqs[s].item0;
+  return total > cap ? 0 : total;
 }
 // An item: blocks e0 .. e_last of sequence s's list for key/value head g, columns c0 ..
 // of the `cols` from row j0 on. False: no work.
@@ -199,8 +201,7 @@ __global__ __launch_bounds__(64 * kWaves, kWorkgroups) void window_weights_kerne
   const int tid = threadIdx.x, lane = tid & 63;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int c32 = lane & 31, hf = lane >> 5;
-  int total = plan_items<kTileBlocks>(rk, G, Hkv, seqs_s, red, items0);
-  if (total > sums_cap) total = 0;  // more rows than the call named: no room for their sums
+  const int total = plan_items<kTileBlocks>(rk, G, Hkv, sums_cap, seqs_s, red, items0);
   // (The ring's address goes through a register of its own: the compiler would
   // otherwise wait for every load in flight before each operand read.)
   uint32_t ring_at = (uint32_t)(uintptr_t)(lds_void_t*)ring;
@@ -352,8 +353,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void window_weights_rows_f32_kernel
   __shared__ int red[kWaves];
   const int G = Hq / Hkv, lane = threadIdx.x & 63, c16 = lane & 15, j4 = lane >> 4;
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  int total = plan_items<kTileBlocksF32>(rk, G, Hkv, seqs_s, red, items0);
-  if (total > sums_cap) total = 0;  // more rows than the call named: no room for their sums
+  const int total = plan_items<kTileBlocksF32>(rk, G, Hkv, sums_cap, seqs_s, red, items0);
 #pragma unroll 1
   for (int item0 = 0, turn = blockIdx.x; item0 < total; item0 += gridDim.x) {
     const int item = item0 + turn;

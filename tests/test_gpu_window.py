@@ -77,6 +77,18 @@ def test_long_prompts(window, sinks, lens, rows):
     r.check()
 
 
+@pytest.mark.parametrize("window,sinks,lens,rows", [
+    (ALL, 0, [1400, 9], [1400, 9]),
+    (130, 1, [1100, 5], [1000, 5]),
+    (40, 300, [700], [650]),
+])
+@pytest.mark.parametrize("hq,hkv,hd", [(4, 1, 64), (5, 1, 32)])
+def test_long_prompts_of_f32(hq, hkv, hd, window, sinks, lens, rows):
+    r = Rows("f32", hq, hkv, hd, lens, rows, window, sinks, seed=17)
+    r.run()
+    r.check()
+
+
 def test_rows_before_the_context_see_nothing():
     # More rows than cached tokens: those without a slot.
     for dtype, hd in (("bf16", 128), ("f32", 64)):
@@ -177,10 +189,11 @@ def test_captured_calls_replay_as_they_ran(dtype, hd, rows):
         torch.cuda.synchronize()
 
 
-def test_many_sequences():
+@pytest.mark.parametrize("dtype,hd", [("bf16", 128), ("f32", 32)])
+def test_many_sequences(dtype, hd):
     # More than a launch of the prompts' kernel takes.
     lens = [(7 * s) % 40 + 3 for s in range(1500)]
-    r = Rows("bf16", 2, 1, 128, lens, [1 + s % 3 for s in range(1500)], 12, 2, seed=12)
+    r = Rows(dtype, 2, 1, hd, lens, [1 + s % 3 for s in range(1500)], 12, 2, seed=12)
     r.run()
     r.check()
 

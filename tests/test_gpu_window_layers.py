@@ -293,6 +293,18 @@ def test_generation_goes_on_over_what_an_eviction_kept(name):
         lens, pos = lens + 1, pos + 1
 
 
+@pytest.mark.parametrize("priors,rows", [PROMPTS, SINGLE], ids=["prompts", "single"])
+@pytest.mark.parametrize("name", ["bf16", "f32"])
+def test_timing_counts_the_attention_of_a_layer_once(name, priors, rows):
+    x = Layers(SHAPES[name], f"wt_{name}", priors, rows, 70, 3, seed=87)
+    coco.coco_layer_set_timing(x.rep.h, True)
+    x.forward(x.hidden, x.weights)
+    got = coco.coco_layer_read_timing(x.rep.h)
+    coco.coco_layer_set_timing(x.rep.h, False)
+    ms, launches = got["attention"]
+    assert launches == 2 and 0 < ms < 50
+
+
 def test_refusals():
     x = Layers(SHAPES["bf16"], "rf", [40, 30], [12, 20], 16, 2, seed=86, n_layers=1)
     t, h = x.t, x.rep.h
