@@ -484,16 +484,18 @@ int coco_window_reserve(coco_layer_t h, int32_t max_rows, int32_t max_seqs, int3
  * Slots count what is cached, wherever its position was: after evictions the
  * window is over the tokens that are left.
  *   q, o and rows past the sequences as in coco_tree_attention (bf16: the softmax
- *   weights of calls without seq_starts keep 16 bits for their product with the
- *   values, prompts' are rounded to bf16). A row that attends nothing (slot below
- *   0) gives zeros, what a row does not attend may hold anything, and table
- *   entries that no row of a sequence reaches are not read.
+ *   weights of calls without seq_starts, and of sequences of at most 64 rows times
+ *   query heads per key/value head, keep 16 bits for their product with the values,
+ *   other prompts' are rounded to bf16). A row that attends nothing (slot below 0)
+ *   gives zeros, what a row does not attend may hold anything, and table entries
+ *   that no row of a sequence reaches are not read.
  *   weights [n_seqs][max_blocks_per_seq * 16] fp32, 16-byte aligned, or NULL:
  *   weights[s][t] grows by the softmax weights of slot t, added up over the rows of
  *   sequence s and the query heads (in fp32, in a fixed order); other places are
  *   left as they are.
  * A sequence's results do not depend on the others of the call; how its rows are
- * spread over calls changes their rounding. Needs coco_window_reserve (COCO_ESTATE
+ * spread over calls changes their rounding, and so can a call of one sequence that
+ * names more rows than it has. Needs coco_window_reserve (COCO_ESTATE
  * without). */
 int coco_window_attention(coco_layer_t h, int32_t layer, const void* q, void* o, int32_t n_rows,
                           const int32_t* seq_starts, int32_t n_seqs, const int32_t* block_table,

@@ -34,12 +34,14 @@
 // and the barriers 4%; 10 us of an item are its start and its end.
 //
 // The list of a sequence with at most kSplitCols columns is split into parts by a
-// rule on the sequence's own columns and list, merged by a second kernel in order:
-// a row's bits depend on its sequence's rows and length alone.
+// rule on the sequence's own columns and list, merged by another kernel in order:
+// a row's bits depend on its sequence's rows and length alone. (Those with at most
+// kFewCols are not of this kernel.)
 #include <math.h>
 
 #include "common.h"
 #include "kernels.h"
+#include "window_prompt.h"
 
 namespace coco {
 
@@ -56,59 +58,13 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * kWave;
 constexpr int kCols = 64;                   // columns of a wave
-constexpr int kTileCols = kWaves * kCols;   // of a workgroup
+static_assert(kTileCols == kWaves * kCols, "columns of a workgroup");
 constexpr int kTile = kBlockTokens * HD;
 constexpr int kRing = 8;                    // stages in LDS
 constexpr int kStage = 4 * kTile;           // elements: keys and values of two blocks
 constexpr int kXCDs = 8;
 constexpr int kMaxSeqs = kWindowLaunchSeqs;
 constexpr float kLazy = 8.f;                // log2 units a running max may lag
-
-// Parts of a list of `entries` blocks for `cols` columns: blocks of one part (a
-// multiple of a stage's two).
-constexpr int kSplitCols = 512, kPartBlocks = 64, kMaxParts = 16;
-__host__ __device__ __forceinline__ int window_part(int64_t cols, int entries) {
-  if (cols > kSplitCols) return entries > 0 ? (entries + 1) / 2 * 2 : 2;
-  const int least = (entries + kMaxParts - 1) / kMaxParts;
-  return least > kPartBlocks ? (least + 1) / 2 * 2 : kPartBlocks;
-}
-
-struct PromptArgs {
-  const bf16_t* q;
-  const bf16_t* k_cache;
-  const bf16_t* v_cache;
-  RowKeys rk;
-  int Hq, Hkv;
-  float scale_log2;
-  bf16_t* o;
-  bool tiled;        // o in tile order
-  float* part_o;     // [column part][HD]
-  float* part_ml;    // [column part][2]
-  int64_t part_cap;  // column parts they hold
-  int32_t* counts;   // [0 .. 7] items drawn, [8] workgroups that are done
-  float* stats;      // [rows][Hq][2] or null
-};
-
-// A sequence's rows: N of slots first .. first + N - 1, C columns per key/value
-// head in `tiles` workgroup tiles, and the parts of its list. item0, part0: its
-// first work item and column part.
-struct PromptSeq {
-  int row0, n, first, tiles, part, splits, item0, part0;
-};
-__device__ __forceinline__ PromptSeq prompt_seq(const RowKeys& rk, int s, int G) {
-  PromptSeq x;
-  x.row0 = rk.seq_starts[s];
-  x.n = max(rk.seq_starts[s + 1] - x.row0, 0);
-  const int len = min(max(rk.ctx_lens[s], 0), rk.max_blocks * kBlockTokens);
-  x.first = len - x.n;
-  const int64_t cols = (int64_t)x.n * G;
-  x.tiles = (int)((cols + kTileCols - 1) / kTileCols);
-  const int entries = window_list(max(x.first, -1), len - 1, rk.window, rk.sinks).entries;
-  x.part = window_part(cols, entries);
-  x.splits = max(1, (entries + x.part - 1) / x.part);
-  x.item0 = x.part0 = 0;
-  return x;
-}
 
 // Piece i of four, 1 KB each, of a cache tile into LDS at byte `to`.
 template <int I>
@@ -365,7 +321,7 @@ __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a
   for (int s0 = 0; s0 < rk.n_seqs; s0 += kThreads) {
     const int s = s0 + tid;
     PromptSeq x{};
-    if (s < rk.n_seqs) x = prompt_seq(rk, s, G);
+    if (s < rk.n_seqs) x = prompt_seq(rk, s, G, a.few);
     const int ni = x.tiles * x.splits * a.Hkv;
     const int np = x.splits > 1 ? x.n * a.Hq * x.splits : 0;
     x.item0 = block_prefix<kWaves>(ni, red, total) - ni;
@@ -779,7 +735,7 @@ __global__ __launch_bounds__(kMergeThreads) void window_prompt_merge_kernel(Prom
   for (int s0 = 0; s0 < rk.n_seqs && rows <= (int)blockIdx.x; s0 += kMergeThreads) {
     int n = 0, np = 0;
     if (s0 + tid < rk.n_seqs) {
-      const PromptSeq y = prompt_seq(rk, s0 + tid, G);
+      const PromptSeq y = prompt_seq(rk, s0 + tid, G, a.few);
       n = y.splits > 1 ? y.n : 0;
       np = y.splits > 1 ? y.n * a.Hq * y.splits : 0;
     }
@@ -809,7 +765,7 @@ __global__ __launch_bounds__(kMergeThreads) void window_prompt_merge_kernel(Prom
   __syncthreads();
   const int s = found[0];
   if (s < 0) return;
-  const PromptSeq x = prompt_seq(rk, s, G);
+  const PromptSeq x = prompt_seq(rk, s, G, a.few);
   const int row = x.row0 + found[1];
   const int head = blockIdx.y * kMergeHeads + tid / 32, dim = tid % 32 * 4;
   if (head >= a.Hq) return;
@@ -882,10 +838,14 @@ hipError_t launch_window_prompt_bf16(const uint16_t* q, const uint16_t* k_cache,
   a.part_cap = part_cap;
   a.counts = counts;
   a.stats = stats;
+  // A sequence alone in its call (padding aside) is of one kind by the call's rows, and
+  // takes one kernel: the other costs 4 us to find nothing.
+  const bool many = (int64_t)n_rows * (Hq / Hkv) > kFewCols;
+  a.few = many && rk.n_seqs == 1 ? 0 : kFewCols;
   // Whether any sequence's list can be in parts.
   const int64_t w = ((int64_t)rk.window + n_rows + 2 * kBlockTokens - 2) / kBlockTokens +
                     ((int64_t)rk.sinks + kBlockTokens - 1) / kBlockTokens;
-  const bool parts = w > kPartBlocks && rk.max_blocks > kPartBlocks;
+  const bool parts = w > kFewPart && rk.max_blocks > kFewPart;
   // One workgroup per CU; batches of more than kMaxSeqs sequences in several
   // launches, which share the partial buffers in turn.
   for (int s0 = 0; s0 < rk.n_seqs; s0 += kMaxSeqs) {
@@ -893,14 +853,19 @@ hipError_t launch_window_prompt_bf16(const uint16_t* q, const uint16_t* k_cache,
     a.rk.ctx_lens = rk.ctx_lens + s0;
     a.rk.block_table = rk.block_table + (int64_t)s0 * rk.max_blocks;
     a.rk.n_seqs = rk.n_seqs - s0 < kMaxSeqs ? rk.n_seqs - s0 : kMaxSeqs;
-    if (parts) {
+    if (a.few > 0) {
+      const hipError_t e = launch_window_few(a, num_cus, !many && !parts, st);
+      if (e != hipSuccess) return e;
+    }
+    if (many && parts)
       COCO_LAUNCH(window_prompt_kernel, dim3(num_cus), dim3(kThreads), 0, st, a);
+    else if (many)
+      COCO_LAUNCH_LAST(window_prompt_kernel, dim3(num_cus), dim3(kThreads), 0, st, a);
+    if (parts) {
       const int64_t most = (int64_t)a.rk.n_seqs * (kSplitCols / (Hq / Hkv));
       COCO_LAUNCH_LAST(window_prompt_merge_kernel,
                        dim3(most < n_rows ? (int)most : n_rows, (Hq + kMergeHeads - 1) / kMergeHeads),
                        dim3(kMergeThreads), 0, st, a);
-    } else {
-      COCO_LAUNCH_LAST(window_prompt_kernel, dim3(num_cus), dim3(kThreads), 0, st, a);
     }
   }
   return hipGetLastError();

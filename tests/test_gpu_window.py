@@ -89,6 +89,34 @@ def test_long_prompts_of_f32(hq, hkv, hd, window, sinks, lens, rows):
     r.check()
 
 
+FEW = [(2000, 16), (700, 17), (1100, 1), (33, 5), (520, 12), (9, 9), (3, 2)]
+
+
+@pytest.mark.parametrize("window,sinks", [(ALL, 0), (100, 20), (17, 0), (600, 3)])
+@pytest.mark.parametrize("hq,hkv", [(4, 1), (8, 2), (5, 1), (16, 1)])
+def test_sequences_of_few_rows(hq, hkv, window, sinks):
+    """Up to 64 columns and just above, in one call and each in its own, padded."""
+    r = Rows("bf16", hq, hkv, 128, *zip(*FEW), window, sinks, seed=18, pad=2)
+    r.run()
+    r.check()
+    ref, tol = r.expect()[:2]
+    for s, (n, rows) in enumerate(FEW):
+        at = slice(int(r.first[s]), int(r.first[s + 1]))
+        for pad in (0, 1, 40):
+            q = torch.cat([r.q[at], r.q[:1].expand(pad, -1, -1)])
+            o = torch.full_like(q, 5.0)
+            w = torch.from_numpy(r.before[s:s + 1]).float().cuda()
+            coco.coco_window_reserve(r.c.h, rows + pad, 1, True)
+            coco.coco_window_attention(r.c.h, 0, q, o, i32([0, rows]), i32(r.table[s:s + 1]),
+                                       i32(r.lens[s:s + 1]), window, sinks, w)
+            torch.cuda.synchronize()
+            assert (o[rows:] == 5.0).all()
+            if (rows + pad) * (hq // hkv) <= 64 or rows * (hq // hkv) > 64:
+                assert torch.equal(o[:rows], r.o[at]) and torch.equal(w[0], r.weights[s])
+            else:  # of one kind by the call's rows: within the bound of the exact result too
+                assert (np.abs(o[:rows].cpu().double().numpy() - ref[at]) <= tol[at]).all()
+
+
 def test_rows_before_the_context_see_nothing():
     # More rows than cached tokens: those without a slot.
     for dtype, hd in (("bf16", 128), ("f32", 64)):
@@ -98,7 +126,7 @@ def test_rows_before_the_context_see_nothing():
         assert (r.o[:5] == 0).all()
 
 
-@pytest.mark.parametrize("rows", [None, [90]])
+@pytest.mark.parametrize("rows", [None, [90], [20]])
 @pytest.mark.parametrize("dtype,hd", [("bf16", 128), ("f32", 64)])
 def test_values_that_are_not_finite_reach_the_rows_that_see_them(dtype, hd, rows):
     r = Rows(dtype, 4, 2, hd, [200], rows, 40, 6, seed=8, weigh=False, poison=False)
