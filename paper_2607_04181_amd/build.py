@@ -27,8 +27,7 @@ SOURCES = ["rows.hip", "gemm_skinny.hip", "gemm_prefill_qkv.hip", "gemm_prefill_
            "gemm_prefill_swiglu.hip", "gemm_prefill_scatter.hip", "gemm_prefill_partial.hip",
            "attention.hip", "layer_f32.hip", "pages.hip", "attention_rows.hip", "tree_attention.hip",
            "block_select.hip", "sparse_attention.hip", "window_decode.hip", "window_prompt.hip",
-           "window_few.hip", "window_prompt_f32.hip",
-           "window_weights.hip", "evict.hip",
+           "window_few.hip", "window_prompt_f32.hip", "window_weights.hip", "evict.hip",
            "coco_api.hip", "cache_api.hip", "probe.hip", "scaling.cpp"]
 
 # Products that write vector registers of their own choice: the prompt windows' scores

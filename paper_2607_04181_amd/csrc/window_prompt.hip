@@ -26,8 +26,8 @@
 // takes no mask. Values that are not finite are looked for once, at the end: where a
 // sum is NaN, the item is done again with such values held apart.
 //
-// What bounds it: at 8000 tokens, 32 heads on 8 and a window of 4096, 400 GFLOP in 420
-// us (0.95 PFLOP/s, where a large product of matrices reaches 1.65). A step of 32 keys
+// What bounds it: at 8000 tokens, 32 heads on 8 and a window of 4096, 400 GFLOP in 409
+// us (0.98 PFLOP/s, where a large product of matrices reaches 1.57). A step of 32 keys
 // is 1024 cycles of products for each SIMD and 1136 with the softmax beside them, and
 // with every CU at it the clock is at 1.6 to 1.7 GHz: 0.70 us, for 0.85 in the kernel.
 // Left out one by one, the operands from LDS are 9% of its time, the loads into LDS 6%
