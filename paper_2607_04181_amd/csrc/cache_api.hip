@@ -819,7 +819,8 @@ int coco_window_reserve(coco_layer_t H, int32_t max_rows, int32_t max_seqs, int3
     const int64_t few = rows < seqs ? rows : seqs;
     const int64_t blocks = (int64_t)window_parts(INT32_MAX, 0, c.max_blocks_per_seq) * kWindowPart;
     const int64_t single = few * c.n_q_heads * (blocks / kWindowPart);
-    const int64_t prompt = window_column_parts(rows, seqs, c.n_q_heads, c.n_kv_heads);
+    const int64_t prompt = window_column_parts(rows, seqs, c.max_blocks_per_seq, c.n_q_heads,
+                                               c.n_kv_heads);
     const int64_t parts = single > prompt ? single : prompt;
     const size_t o = align256((size_t)parts * c.head_dim * 4), ml = align256((size_t)parts * 8);
     const size_t scores =

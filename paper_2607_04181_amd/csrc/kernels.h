@@ -434,7 +434,7 @@ hipError_t launch_window_decode_bf16(const uint16_t* q, const uint16_t* k_cache,
 // [rows][Hq][2]: each row's running maximum (in powers of two) and 1 / its sum
 // of weights (0: it sees nothing).
 constexpr int kWindowCounts = 16, kWindowLaunchSeqs = 512;
-int64_t window_column_parts(int64_t max_rows, int64_t max_seqs, int Hq, int Hkv);
+int64_t window_column_parts(int64_t max_rows, int64_t max_seqs, int max_blocks, int Hq, int Hkv);
 hipError_t launch_window_prompt_bf16(const uint16_t* q, const uint16_t* k_cache,
                                      const uint16_t* v_cache, const RowKeys& rk, int n_rows, int Hq,
                                      int Hkv, uint16_t* o, bool tiled, float* part_o,

@@ -810,10 +810,19 @@ __global__ __launch_bounds__(kMergeThreads) void window_prompt_merge_kernel(Prom
 
 }  // namespace
 
-// The most that any call of so many rows and sequences can need.
-int64_t window_column_parts(int64_t max_rows, int64_t max_seqs, int Hq, int Hkv) {
-  const int64_t cols = max_seqs * Hkv * kSplitCols;
-  return (cols < max_rows * Hq ? cols : max_rows * Hq) * kMaxParts;
+// The most that any call of so many rows and sequences can need: columns of sequences of
+// few rows in parts of kFewPart blocks at least, those of the others of kPartBlocks.
+int64_t window_column_parts(int64_t max_rows, int64_t max_seqs, int max_blocks, int Hq, int Hkv) {
+  const auto columns = [&](int64_t most) {
+    const int64_t cols = max_seqs * Hkv * most;
+    return cols < max_rows * Hq ? cols : max_rows * Hq;
+  };
+  const auto parts = [&](int blocks) {
+    const int n = (max_blocks + blocks - 1) / blocks;
+    return n < kMaxParts ? n : kMaxParts;
+  };
+  const int64_t few = columns(kFewCols);
+  return few * parts(kFewPart) + (columns(kSplitCols) - few) * parts(kPartBlocks);
 }
 
 hipError_t launch_window_prompt_bf16(const uint16_t* q, const uint16_t* k_cache,
