@@ -7,7 +7,7 @@
 // eight bits at a time from counts of the candidates' digits, and how many of
 // those with key T are taken; a second one per row writes the list, each after a
 // sum over the counts of the requests before its own, and moves the weights.
-// Both hold a row of up to 32768 tokens in registers, read once; what they take
+// The first holds a row of up to 32768 tokens in registers, read once; what both take
 // is launches, barriers and one read of a few KB per row, not its bytes.
 #include "common.h"
 #include "kernels.h"
@@ -16,9 +16,10 @@ namespace coco {
 
 namespace {
 
-constexpr int kThreads = 1024, kWaves = kThreads / kWave;
-constexpr int kStep = 4 * kThreads;  // slots of a step: four per thread
-constexpr int kHeld = 8;             // steps whose keys stay in registers
+// Tables of at most kFewTokens: 256 threads, whose barriers are shorter (64 rows of 280
+// tokens 9.3 us for both kernels, with 1024 threads 12.8; of 1000 9.5 and 12.9; of 2200, in
+// steps, 15.2 and 13.0).
+constexpr int kFewTokens = 1024;
 
 // Larger weight, larger key; both zeros alike, NaN lowest.
 __device__ __forceinline__ uint32_t weight_key(float w) {
@@ -49,7 +50,11 @@ __device__ __forceinline__ f32x4_t load_weights(const Row& r, int t) {
 }
 
 // plan[i]: T, how many of key T stay, base, tokens listed.
+template <int kThreads>
 __global__ __launch_bounds__(kThreads) void evict_plan_kernel(EvictArgs a) {
+  // Steps whose keys stay in registers.
+  constexpr int kHeld = 4 * kThreads > kFewTokens ? 8 : 1;
+  constexpr int kWaves = kThreads / kWave, kStep = 4 * kThreads;  // slots: four per thread
   __shared__ int hist[256];
   __shared__ int found[2], base_s, red[kWaves];
   const int i = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
@@ -179,6 +184,7 @@ __global__ __launch_bounds__(kThreads) void evict_plan_kernel(EvictArgs a) {
 }
 
 // Sum over the workgroup's threads.
+template <int kWaves>
 __device__ __forceinline__ int64_t block_total(int64_t x, int64_t* red) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o, kWave);
@@ -191,7 +197,9 @@ __device__ __forceinline__ int64_t block_total(int64_t x, int64_t* red) {
   return sum;
 }
 
+template <int kThreads>
 __global__ __launch_bounds__(kThreads) void evict_list_kernel(EvictArgs a) {
+  constexpr int kWaves = kThreads / kWave, kStep = 4 * kThreads;  // slots: four per thread
   __shared__ int64_t red64[kWaves];
   __shared__ int red[2][kWaves];
   const int i = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
@@ -204,7 +212,7 @@ __global__ __launch_bounds__(kThreads) void evict_list_kernel(EvictArgs a) {
   int64_t mine = 0;
   for (int j0 = 0; j0 < i; j0 += kThreads)
     mine += j0 + tid < i ? (int64_t)a.plan[4 * (int64_t)(j0 + tid) + 3] : 0;
-  int64_t start = block_total(mine, red64);
+  int64_t start = block_total<kWaves>(mine, red64);
   bool served = start + count <= a.n_kept;
   if (start > a.n_kept) {
     // Some request before does not fit: the list ends where it would begin. (Sums
@@ -289,8 +297,13 @@ __global__ __launch_bounds__(kThreads) void evict_list_kernel(EvictArgs a) {
 
 hipError_t launch_evict(const EvictArgs& a, hipStream_t st) {
   if (a.n <= 0) return hipSuccess;
-  COCO_LAUNCH(evict_plan_kernel, dim3(a.n), dim3(kThreads), 0, st, a);
-  COCO_LAUNCH_LAST(evict_list_kernel, dim3(a.n), dim3(kThreads), 0, st, a);
+  if ((int64_t)a.max_blocks * kBlockTokens <= kFewTokens) {
+    COCO_LAUNCH(evict_plan_kernel<256>, dim3(a.n), dim3(256), 0, st, a);
+    COCO_LAUNCH_LAST(evict_list_kernel<256>, dim3(a.n), dim3(256), 0, st, a);
+  } else {
+    COCO_LAUNCH(evict_plan_kernel<1024>, dim3(a.n), dim3(1024), 0, st, a);
+    COCO_LAUNCH_LAST(evict_list_kernel<1024>, dim3(a.n), dim3(1024), 0, st, a);
+  }
   return hipGetLastError();
 }
 

@@ -105,6 +105,18 @@ def test_choice(kind, first, last):
     e.check()
 
 
+@pytest.mark.parametrize("kind", ["heavy", "ties", "zeros", "odd"])
+@pytest.mark.parametrize("width", [64, 65])
+def test_choice_in_narrow_tables(kind, width):
+    rng = np.random.default_rng(4)
+    lens = [0, 1, 2, 255, 256, 257, 900, 1000, 1023, 1024]
+    for first, last in ((0, 0), (4, 30), (0, 200), (700, 3)):
+        e = Evict(lens, [0, 0, 1, 100, 255, 3, 64, 999, 512, 1000], first, last,
+                  heavy(rng, lens, width, kind), width=width)
+        e.run()
+        e.check()
+
+
 def test_choice_of_long_rows():
     # More slots than a workgroup keeps in registers.
     rng = np.random.default_rng(2)
