@@ -16,10 +16,11 @@ namespace coco {
 
 namespace {
 
-// Tables of at most kFewTokens: 256 threads, whose barriers are shorter (64 rows of 280
-// tokens 9.3 us for both kernels, with 1024 threads 12.8; of 1000 9.5 and 12.9; of 2200, in
+constexpr int kAllThreads = 1024;
+// Rows of at most kFewTokens go on with 256 threads, whose barriers are shorter (64 rows of
+// 280 tokens 9.1 us for both kernels, with 1024 threads 12.8; of 1000 9.3 and 12.9; of 2200, in
 // steps, 15.2 and 13.0).
-constexpr int kFewTokens = 1024;
+constexpr int kFewTokens = 1024, kFewThreads = 256;
 
 // Larger weight, larger key; both zeros alike, NaN lowest.
 __device__ __forceinline__ uint32_t weight_key(float w) {
@@ -51,15 +52,13 @@ __device__ __forceinline__ f32x4_t load_weights(const Row& r, int t) {
 
 // plan[i]: T, how many of key T stay, base, tokens listed.
 template <int kThreads>
-__global__ __launch_bounds__(kThreads) void evict_plan_kernel(EvictArgs a) {
-  // Steps whose keys stay in registers.
-  constexpr int kHeld = 4 * kThreads > kFewTokens ? 8 : 1;
+__device__ __forceinline__ void plan_row(const EvictArgs& a, const Row& r) {
+  constexpr int kHeld = kThreads == kAllThreads ? 8 : 1;  // steps whose keys stay in registers
   constexpr int kWaves = kThreads / kWave, kStep = 4 * kThreads;  // slots: four per thread
   __shared__ int hist[256];
   __shared__ int found[2], base_s, red[kWaves];
   const int i = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const Row r = evict_row(a, i);
   uint32_t* plan = a.plan + 4 * (int64_t)i;
   if (r.keep >= r.len) {
     if (tid == 0) {
@@ -183,6 +182,14 @@ __global__ __launch_bounds__(kThreads) void evict_plan_kernel(EvictArgs a) {
   }
 }
 
+__global__ __launch_bounds__(kAllThreads) void evict_plan_kernel(EvictArgs a) {
+  const Row r = evict_row(a, blockIdx.x);
+  if (r.len > kFewTokens)
+    plan_row<kAllThreads>(a, r);
+  else if (threadIdx.x < kFewThreads)  // (the other waves end, and no barrier counts them)
+    plan_row<kFewThreads>(a, r);
+}
+
 // Sum over the workgroup's threads.
 template <int kWaves>
 __device__ __forceinline__ int64_t block_total(int64_t x, int64_t* red) {
@@ -198,13 +205,12 @@ __device__ __forceinline__ int64_t block_total(int64_t x, int64_t* red) {
 }
 
 template <int kThreads>
-__global__ __launch_bounds__(kThreads) void evict_list_kernel(EvictArgs a) {
+__device__ __forceinline__ void list_row(const EvictArgs& a, const Row& r) {
   constexpr int kWaves = kThreads / kWave, kStep = 4 * kThreads;  // slots: four per thread
   __shared__ int64_t red64[kWaves];
   __shared__ int red[2][kWaves];
   const int i = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
   const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const Row r = evict_row(a, i);
   const uint32_t T = a.plan[4 * (int64_t)i];
   const int take = a.plan[4 * (int64_t)i + 1], base = a.plan[4 * (int64_t)i + 2],
             count = a.plan[4 * (int64_t)i + 3];
@@ -293,17 +299,20 @@ __global__ __launch_bounds__(kThreads) void evict_list_kernel(EvictArgs a) {
     for (int t = r.keep + tid; t < r.len; t += kThreads) w_out[t] = 0.f;
 }
 
+__global__ __launch_bounds__(kAllThreads) void evict_list_kernel(EvictArgs a) {
+  const Row r = evict_row(a, blockIdx.x);
+  if (r.len > kFewTokens)
+    list_row<kAllThreads>(a, r);
+  else if (threadIdx.x < kFewThreads)
+    list_row<kFewThreads>(a, r);
+}
+
 }  // namespace
 
 hipError_t launch_evict(const EvictArgs& a, hipStream_t st) {
   if (a.n <= 0) return hipSuccess;
-  if ((int64_t)a.max_blocks * kBlockTokens <= kFewTokens) {
-    COCO_LAUNCH(evict_plan_kernel<256>, dim3(a.n), dim3(256), 0, st, a);
-    COCO_LAUNCH_LAST(evict_list_kernel<256>, dim3(a.n), dim3(256), 0, st, a);
-  } else {
-    COCO_LAUNCH(evict_plan_kernel<1024>, dim3(a.n), dim3(1024), 0, st, a);
-    COCO_LAUNCH_LAST(evict_list_kernel<1024>, dim3(a.n), dim3(1024), 0, st, a);
-  }
+  COCO_LAUNCH(evict_plan_kernel, dim3(a.n), dim3(kAllThreads), 0, st, a);
+  COCO_LAUNCH_LAST(evict_list_kernel, dim3(a.n), dim3(kAllThreads), 0, st, a);
   return hipGetLastError();
 }
 
