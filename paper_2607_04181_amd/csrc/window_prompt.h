@@ -39,10 +39,10 @@ struct PromptArgs {
 };
 
 // A sequence's rows: N of slots first .. first + N - 1, C columns per key/value
-// head in `tiles` workgroup tiles (0: few), and the parts of its list. item0, part0:
-// its first work item and column part.
+// head in `tiles` workgroup tiles (0: few), the parts of its list, and the blocks
+// of the longest item. item0, part0: its first work item and column part.
 struct PromptSeq {
-  int row0, n, first, tiles, part, splits, item0, part0;
+  int row0, n, first, tiles, part, splits, longest, item0, part0;
 };
 __device__ __forceinline__ PromptSeq prompt_seq(const RowKeys& rk, int s, int G, int few) {
   PromptSeq x;
@@ -55,6 +55,9 @@ __device__ __forceinline__ PromptSeq prompt_seq(const RowKeys& rk, int s, int G,
   const int entries = window_list(max(x.first, -1), len - 1, rk.window, rk.sinks).entries;
   x.part = window_part(cols, entries, few);
   x.splits = max(1, (entries + x.part - 1) / x.part);
+  // (the last tile's)
+  const int tile0 = max(max(x.first, len - kTileCols / G), -1);
+  x.longest = min(window_list(tile0, len - 1, rk.window, rk.sinks).entries, x.part);
   x.item0 = x.part0 = 0;
   return x;
 }
