@@ -472,8 +472,8 @@ int coco_layer_sparse_forward(coco_layer_t h, int32_t layer, void* hidden, int64
  * 65535) sequences, and, with weigh, for their weights (as coco_tree_reserve).
  * A bf16 handle holds 4 bytes per query head and slot of a block-table row for
  * each of min(max_rows, max_seqs) sequences then, any handle 4 bytes per key/value
- * head and slot for each of 512 of them and for each 1024 of max_rows times the
- * query heads per key/value head. */
+ * head and slot for each of 512 of them and for each 256 (fp32: 128) of max_rows
+ * times the query heads per key/value head. */
 int coco_window_reserve(coco_layer_t h, int32_t max_rows, int32_t max_seqs, int32_t weigh);
 
 /* Attention of rows over the newest `window` tokens of layer `layer`'s cache and

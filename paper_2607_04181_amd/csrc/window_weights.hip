@@ -14,7 +14,7 @@
 // workgroups to a CU take such pieces in turn, one's products (16 of 33 cycles a step)
 // beside the others' exponentials (32 of 8, and 64 multiply-adds of 4), which bound it.
 // 16 sequences of 36 to 64 rows (32 heads on 8, 58500 cached tokens between them) take
-// 46 us, 4000 rows of a prompt 118: with 32 keys to a wave and all columns in one item
+// 46 us, 4000 rows of a prompt 102: with 32 keys to a wave and all columns in one item
 // 57 and 393. Of the 46, the products are 10 and the vector instructions 20; the rest
 // are starts of items (tables, keys) and the last round, when some CUs have none.
 // fp32: the same of 64 keys, 16 of them in a wave's registers; single tokens without a
@@ -41,9 +41,13 @@ constexpr int kWaves = 4;
 constexpr int kTileBlocks = 4 * kWaves;  // blocks of a workgroup
 constexpr int kTileBlocksF32 = kWaves;
 constexpr int kCols = 32;                // columns of a step
-// Columns of an item: 4000 rows of 32 heads on 8 take 104 us with 512, 118 with 1024 and
-// 141 with 2048, 64 bytes of scratch a key for each; prompts of 64 rows are one item.
-constexpr int kPartCols = 1024;
+// Columns of an item, by the blocks of its tile. bf16: 497 rows of 32 heads on 8 over 1300
+// tokens take 39 us with 1024, 25 with 512 and 20 with 256, 4000 rows 117, 105 and 102, 8000
+// with a window of 1024 103, 111 and 112; fp32: 135 rows of 16 heads of 64 on 4 in each of two
+// sequences 28 us with 1024, 19.5 with 256, 14.5 with 128. Scratch is 4 bytes a key for each
+// item and key/value head.
+template <int TB>
+constexpr int kPartCols = TB == kTileBlocks ? 256 : 128;
 constexpr int kTurn = 8 * 37;
 constexpr int kRing = 3;                 // steps in LDS
 constexpr int kSlot = kCols * HD + kCols * 16;  // elements of one: queries, then statistics
@@ -97,7 +101,7 @@ __device__ __forceinline__ float column_sums(const float w[16], int lane) {
   return x[0] + row_swap<0xB1>(x[0]);                                        // lane ^ 1
 }
 
-// A sequence's work: tile k, blocks k TB .. of its list, in parts of kPartCols
+// A sequence's work: tile k, blocks k TB .. of its list, in parts of kPartCols<TB>
 // of the columns that can see it; key/value heads innermost. Tiles below `many` (those
 // with first tokens, which every row sees) have `most` parts at most, the others `few`.
 // A part past a tile's columns has no work and leaves no sums.
@@ -107,8 +111,9 @@ struct SeqItems {
 struct Parts {
   int tiles, many, most, few;
 };
+template <int TB>
 __device__ __forceinline__ int parts_of(int64_t rows, int G) {
-  return (int)((rows * G + kPartCols - 1) / kPartCols);
+  return (int)((rows * G + kPartCols<TB> - 1) / kPartCols<TB>);
 }
 template <int TB>
 __device__ __forceinline__ Parts seq_parts(const RowKeys& rk, const SeqRows& x, int G) {
@@ -116,10 +121,10 @@ __device__ __forceinline__ Parts seq_parts(const RowKeys& rk, const SeqRows& x, 
   y.tiles = (x.list.entries + TB - 1) / TB;
   const int first = min(rk.sinks / kBlockTokens + (rk.sinks % kBlockTokens != 0), x.list.entries);
   y.many = (first + TB - 1) / TB;
-  y.most = parts_of(x.n, G);
+  y.most = parts_of<TB>(x.n, G);
   // (slots t .. t + 16 TB - 1: rows of slots t .. t + 16 TB - 2 + window)
   const int64_t rows = (int64_t)rk.window + TB * kBlockTokens - 1;
-  y.few = parts_of(rows < x.n ? rows : x.n, G);
+  y.few = parts_of<TB>(rows < x.n ? rows : x.n, G);
   return y;
 }
 // The rows j0 .. j1 - 1 that can see tile k, blocks e0 .. e_last of the list.
@@ -185,7 +190,7 @@ __device__ __forceinline__ bool find_item(const RowKeys& rk, const SeqItems* seq
   it.e0 = tile * TB;
   tile_rows<TB>(rk, x, tile, it.e_last, it.j0, j1);
   it.cols = max(j1 - it.j0, 0) * G;
-  it.c0 = part * kPartCols;
+  it.c0 = part * kPartCols<TB>;
   return it.c0 < it.cols;
 }
 
@@ -246,7 +251,7 @@ __global__ __launch_bounds__(64 * kWaves, kWorkgroups) void window_weights_kerne
       __builtin_amdgcn_global_load_lds(stats_seq + head * 2 + (lane & 1),
                                        (lds_void_t*)(uintptr_t)to_stats, 4, 0, 0);
     };
-    Step now{j0 + c0 / G, c0 % G, min(it.cols - c0, kPartCols)}, ahead = now;
+    Step now{j0 + c0 / G, c0 % G, min(it.cols - c0, kPartCols<kTileBlocks>)}, ahead = now;
     for (int i = 0; i < kRing - 1; ++i) {
       issue(ahead, i);
       if (ahead.left > kCols) next(ahead);
@@ -342,7 +347,7 @@ __global__ __launch_bounds__(64 * kWaves, kWorkgroups) void window_weights_kerne
 // fp32: a workgroup's waves have a block of 16 keys each, and walk the item's columns 16
 // at a time, the keys' and the columns' operands from memory: S[16 keys][16 columns] =
 // K Q^T, 8 HS x mfma 16x16x4 of 32 cycles each, which bound it. 2000 rows of a prompt, 16
-// heads of 64 on 4, take 105 us (2680 with a workgroup that walked them for its 16 keys).
+// heads of 64 on 4, take 89 us (2680 with a workgroup that walked them for its 16 keys).
 template <int HS>
 __global__ __launch_bounds__(64 * kWaves, 2) void window_weights_rows_f32_kernel(
     const float* __restrict__ q, const float* __restrict__ k_cache, RowKeys rk, int Hq, int Hkv,
@@ -369,7 +374,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void window_weights_rows_f32_kernel
       kf[y][0] = *(const f32x4_t*)(kb + y * 512);
       kf[y][1] = *(const f32x4_t*)(kb + y * 512 + 4);
     }
-    const int end = min(it.c0 + kPartCols, it.cols);
+    const int end = min(it.c0 + kPartCols<kTileBlocksF32>, it.cols);
     f32x4_t w = {0.f, 0.f, 0.f, 0.f}, qf[HS][2];
     f32x2_t st;
     int p;
@@ -435,7 +440,7 @@ __global__ __launch_bounds__(64 * kWaves) void window_weights_add_kernel(
   const int64_t item = items0[s] + (int64_t)Hkv * (tile < y.many
                                                        ? tile * y.most
                                                        : y.many * y.most + (tile - y.many) * y.few);
-  const int n = parts_of(max(j1 - j0, 0), G) * Hkv;
+  const int n = parts_of<TB>(max(j1 - j0, 0), G) * Hkv;
   if (item + n > sums_cap) return;
   const float* from = sums + item * kTileKeys + blockIdx.x % (kTileKeys / 64) * 64 + lane;
   float v = 0.f;
@@ -526,8 +531,9 @@ int64_t window_weight_items(int64_t max_rows, int64_t max_seqs, int max_blocks, 
   int64_t seqs = max_seqs < kWindowLaunchSeqs ? max_seqs : kWindowLaunchSeqs;
   if (max_rows < seqs) seqs = max_rows;
   const int tb = bf16 ? kTileBlocks : kTileBlocksF32;
+  const int part = bf16 ? kPartCols<kTileBlocks> : kPartCols<kTileBlocksF32>;
   const int64_t tiles = (max_blocks + tb - 1) / tb;
-  const int64_t items = tiles * Hkv * (seqs + max_rows * (Hq / Hkv) / kPartCols);
+  const int64_t items = tiles * Hkv * (seqs + max_rows * (Hq / Hkv) / part);
   return items < 0x7fffffff ? items : 0x7fffffff;
 }
 int64_t window_sums_bytes(int64_t items, bool bf16) {
