@@ -409,7 +409,8 @@ __global__ __launch_bounds__(256) void page_compact_long_kernel(
         } else {
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            if (t[e] >= 0) x[(t[e] >> 4) * kTile + ((int)t[e] & 12) * 32 + ((int)t[e] & 3)] = r[u][e];
+            if (t[e] >= 0)
+              x[(t[e] >> 4) * kTile + ((int)t[e] & 12) * 32 + ((int)t[e] & 3)] = r[u][e];
         }
       }
     } else {

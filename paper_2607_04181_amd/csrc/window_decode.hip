@@ -310,12 +310,13 @@ __global__ __launch_bounds__(256) void window_merge_kernel(DecodeArgs a, int mer
       sm_ml[h] = f32x2_t{ml[0] == -INFINITY ? 0.f : ml[0], ml[1] == 0.f ? 0.f : 1.0f / ml[1]};
     __syncthreads();
     for (int g = wv; g < g1; g += kWaves) {
-      const float* z0 = a.scores + (((int64_t)i * a.Hkv + g0 + g) * ((int64_t)a.parts * kWindowPart) +
-                                    (live ? e : e0)) * G * kBlockTokens + t4;
+      const int64_t row = ((int64_t)i * a.Hkv + g0 + g) * ((int64_t)a.parts * kWindowPart);
+      const float* z0 = a.scores + (row + (live ? e : e0)) * G * kBlockTokens + t4;
       for (int h0 = 0; h0 < G; h0 += 4) {
         f32x4_t z[4];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) z[u] = *(const f32x4_t*)(z0 + min(h0 + u, G - 1) * kBlockTokens);
+        for (int u = 0; u < 4; ++u)
+          z[u] = *(const f32x4_t*)(z0 + min(h0 + u, G - 1) * kBlockTokens);
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
           if (h0 + u >= G) break;

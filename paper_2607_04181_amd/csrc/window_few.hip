@@ -99,12 +99,11 @@ __global__ __launch_bounds__(kThreads, kWorkgroups) void window_few_kernel(Promp
     // This lane's column (one past the last repeats it).
     const int c = c0 + min(c16, last), j = small_div(c, inv_G);
     const int p = max(first + j, -1);
+    const bf16_t* qp = a.q + ((int64_t)(row0 + j) * a.Hq + g * G + (c - j * G)) * HD + 8 * j4;
     bf16x8_t qf[4];
 #pragma unroll
     for (int x = 0; x < 4; ++x)
-      qf[x] = __builtin_bit_cast(
-          bf16x8_t, *(const u32x4_t*)(a.q + ((int64_t)(row0 + j) * a.Hq + g * G + (c - j * G)) * HD +
-                                      32 * x + 8 * j4));
+      qf[x] = __builtin_bit_cast(bf16x8_t, *(const u32x4_t*)(qp + 32 * x));
     float m = -INFINITY, l = 0.f;
     f32x4_t acc[8];
 #pragma unroll
@@ -112,13 +111,14 @@ __global__ __launch_bounds__(kThreads, kWorkgroups) void window_few_kernel(Promp
 
     // Block x of the wave's: of the sequence, and, 64 at a time in the lanes, of the pool.
     const auto block = [&](int x) { return list.block(e0 + wv + kWaves * x); };
+    const int32_t* bt = rk.block_table + (int64_t)s * rk.max_blocks;
     int ids = 0;
     const auto load = [&](Tile& t, int x) {
       if (x % kWave == 0)
-        ids = readable_block(rk.block_table[(int64_t)s * rk.max_blocks + block(min(x + lane, n_all - 1))],
-                             rk.num_blocks);
+        ids = readable_block(bt[block(min(x + lane, n_all - 1))], rk.num_blocks);
       const int64_t tile = ((int64_t)__builtin_amdgcn_readlane(ids, x % kWave) * a.Hkv + g) * kTile;
-      const u32x4_t *kp = (const u32x4_t*)(a.k_cache + tile), *vp = (const u32x4_t*)(a.v_cache + tile);
+      const u32x4_t* kp = (const u32x4_t*)(a.k_cache + tile);
+      const u32x4_t* vp = (const u32x4_t*)(a.v_cache + tile);
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
         t.k[u] = kp[64 * u + lane];
@@ -129,8 +129,8 @@ __global__ __launch_bounds__(kThreads, kWorkgroups) void window_few_kernel(Promp
       f32x4_t z = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int u = 0; u < 4; ++u)
-        z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, t.k[u]), qf[u], z, 0,
-                                                    0, 0);
+        z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, t.k[u]), qf[u], z,
+                                                    0, 0, 0);
       const int t0 = block(x) * kBlockTokens;
       const bool whole = t0 + kBlockTokens - 1 <= p_low &&
                          (t0 > p_high - rk.window || t0 + kBlockTokens - 1 < rk.sinks);
@@ -170,7 +170,8 @@ __global__ __launch_bounds__(kThreads, kWorkgroups) void window_few_kernel(Promp
         uint32_t n[4];
 #pragma unroll
         for (int r = 0; r < 4; ++r) n[r] = seen >> r & 1 ? (pr[r] != 0.f ? 0x3F80u : 0x4580u) : 0u;
-        const s16x4_t nb = __builtin_bit_cast(s16x4_t, u32x2_t{n[0] | n[1] << 16, n[2] | n[3] << 16});
+        const s16x4_t nb =
+            __builtin_bit_cast(s16x4_t, u32x2_t{n[0] | n[1] << 16, n[2] | n[3] << 16});
 #pragma unroll
         for (int u = 0; u < 8; ++u) {
           const uint32_t w0 = t.v[u / 2][u % 2 * 2], w1 = t.v[u / 2][u % 2 * 2 + 1];
@@ -197,10 +198,11 @@ __global__ __launch_bounds__(kThreads, kWorkgroups) void window_few_kernel(Promp
       for (int y = 0; y < 2; ++y) {
         const s16x4_t pb = __builtin_bit_cast(s16x4_t, u32x2_t{p01[y], p23[y]});
 #pragma unroll
-        for (int u = 0; u < 8; ++u)
-          acc[u] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(
-              __builtin_bit_cast(s16x4_t, u32x2_t{t.v[u / 2][u % 2 * 2], t.v[u / 2][u % 2 * 2 + 1]}),
-              pb, acc[u], 0, 0, 0);
+        for (int u = 0; u < 8; ++u) {
+          const u32x2_t v = {t.v[u / 2][u % 2 * 2], t.v[u / 2][u % 2 * 2 + 1]};
+          acc[u] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4_t, v), pb,
+                                                             acc[u], 0, 0, 0);
+        }
       }
     };
     Tile ta, tb;

@@ -197,7 +197,8 @@ __device__ __forceinline__ f32x16_t scores_of(const u32x4_t k[8], const bf16x8_t
   f32x16_t z = {};
 #pragma unroll
   for (int i = 0; i < 8; ++i)
-    z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, k[i]), q[i], z, 0, 0, 0);
+    z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, k[i]), q[i], z, 0, 0,
+                                                0);
   return z;
 }
 // O^T += V^T P^T.
@@ -214,8 +215,8 @@ __device__ __forceinline__ void add_values(Cols& c, const u32x4_t v[2][2][2], co
 // Half a step: sixteen products, and beside each a sixteenth of the other tile's
 // softmax. The products: scores z of the next stage (k, q), then values v with
 // weights p for cv's columns. The softmax: weights w of scores zs for cs's columns.
-// m_now: cs's running max with its scores; m_next: cv's with the next ones. `lds(i)`: operand reads that go out
-// behind product i.
+// m_now: cs's running max with its scores; m_next: cv's with the next ones. `lds(i)`:
+// operand reads that go out behind product i.
 // Nothing is moved from one sixteenth to another: left to itself, the compiler puts
 // the products back to back and the exponentials behind them, and a wave that is
 // alone on its SIMD then has one pipe idle at a time. A product takes 33 cycles and
@@ -250,7 +251,8 @@ __device__ __forceinline__ void half_step(const u32x4_t k[8], const bf16x8_t q[8
     if (i == 10) mx = fmaxf(fmaxf(mx, z[3]), z[4]);
     if (i == 11) mx = fmaxf(fmaxf(fmaxf(fmaxf(mx, z[5]), z[6]), z[7]), z[8]);
     if (i == 12) mx = fmaxf(fmaxf(mx, z[9]), z[10]);
-    if (i == 13) mx = fmaxf(fmaxf(fmaxf(fmaxf(fmaxf(fmaxf(mx, z[11]), z[12]), z[13]), z[14]), z[15]), kNoMax);
+    if (i == 13)
+      mx = fmaxf(fmaxf(fmaxf(fmaxf(fmaxf(fmaxf(mx, z[11]), z[12]), z[13]), z[14]), z[15]), kNoMax);
     if (i == 14) top = column_top(mx, scale_log2);
     // (here, not where they are used)
     asm volatile("" : "+v"(pr[i]), "+v"(x), "+v"(ls), "+v"(mx));
@@ -336,7 +338,8 @@ __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a
   for (int s = tid; s < rk.n_seqs; s += kThreads) {
     const int mine = items_s[s];
     int before = 0;
-    for (int t = 0; t < rk.n_seqs; ++t) before += items_s[t] > mine || (items_s[t] == mine && t < s);
+    for (int t = 0; t < rk.n_seqs; ++t)
+      before += items_s[t] > mine || (items_s[t] == mine && t < s);
     order_s[before] = s;
   }
   __syncthreads();
@@ -575,25 +578,28 @@ __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a
 #pragma unroll 1
         while (__builtin_expect_with_probability(st < end, 1, 0.99)) {
           const uint32_t v_at = v_lane + (st % kRing) * (kStage * 2);
-          half_step(kf, qf[0], z0, c[0], vf, pw[0], c[1], z1, pw[1], m1, m0, a.scale_log2, [&](int i) {
+          const auto values = [&](int i) {
             if (i < 4) {
               read_v_part(v_at, 2 * i, vf);
               read_v_part(v_at, 2 * i + 1, vf);
             }
-          });
+          };
+          half_step(kf, qf[0], z0, c[0], vf, pw[0], c[1], z1, pw[1], m1, m0, a.scale_log2, values);
           if (__builtin_expect(masked, 0)) mask(z0, m0, 0, st + 1);
           // begin(st), its loads beside the first products.
           arrive(st);
           const bf16_t* src = source(st + kRing - 1) + lane * 8;
           const uint32_t dst = place(st + kRing - 1);
           const uint32_t k_at = k_lane + (st + 2) % kRing * (kStage * 2);
-          half_step(kf, qf[1], z1, c[1], vf, pw[1], c[0], z0, pw[0], m0, m1, a.scale_log2, [&](int i) {
+          const auto stage_and_keys = [&](int i) {
             if (i == 0) load_tile<0>(src, dst);
             if (i == 1) load_tile<1>(src, dst);
             if (i == 2) load_tile<2>(src, dst);
             if (i == 3) load_tile<3>(src, dst);
             if (i >= 2 && i < 10) kf[i - 2] = read_k_part(k_at, i - 2);
-          });
+          };
+          half_step(kf, qf[1], z1, c[1], vf, pw[1], c[0], z0, pw[0], m0, m1, a.scale_log2,
+                    stage_and_keys);
           ++st;
           if (__builtin_expect(masked, 0)) mask(z1, m1, 1, st);
         }
@@ -894,7 +900,8 @@ hipError_t launch_window_prompt_bf16(const uint16_t* q, const uint16_t* k_cache,
     if (parts) {
       const int64_t most = (int64_t)a.rk.n_seqs * (kSplitCols / (Hq / Hkv));
       COCO_LAUNCH_LAST(window_prompt_merge_kernel,
-                       dim3(most < n_rows ? (int)most : n_rows, (Hq + kMergeHeads - 1) / kMergeHeads),
+                       dim3(most < n_rows ? (int)most : n_rows,
+                            (Hq + kMergeHeads - 1) / kMergeHeads),
                        dim3(kMergeThreads), 0, st, a);
     }
   }

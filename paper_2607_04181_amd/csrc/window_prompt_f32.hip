@@ -46,7 +46,8 @@ __device__ __forceinline__ float odd_count(float v) {
 constexpr int waves_of(int HS) { return HS <= 5 ? 8 : 4; }
 
 template <int HS>
-__global__ __launch_bounds__(64 * waves_of(HS), HS <= 2 ? 4 : HS <= 5 ? 2 : 1) void window_prompt_f32_kernel(
+__global__ __launch_bounds__(64 * waves_of(HS),
+                             HS <= 2 ? 4 : HS <= 5 ? 2 : 1) void window_prompt_f32_kernel(
     const float* __restrict__ q, const float* __restrict__ k_cache,
     const float* __restrict__ v_cache, RowKeys rk, int n_rows, int Hq, int Hkv, int chunks,
     float scale_log2, float* __restrict__ o, float* __restrict__ stats) {

@@ -295,7 +295,7 @@ __global__ __launch_bounds__(64 * kWaves, kWorkgroups) void window_weights_kerne
       for (int u0 = 0; u0 < 8; u0 += 4) {
         u32x4_t b[4];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) 
+        for (int u = 0; u < 4; ++u)
           b[u] = *(const lds_u32x4_t*)(uintptr_t)((q_at + slot * (kSlot * 2) + u0 * 256) ^ u * 32);
         // (four at once: one by one, each product waited for its own)
 #pragma unroll
@@ -304,9 +304,9 @@ __global__ __launch_bounds__(64 * kWaves, kWorkgroups) void window_weights_kerne
         for (int u = 0; u < 4; ++u)
 #pragma unroll
           for (int y = 0; y < 2; ++y)
-            z[y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kf[y][u0 + u]),
-                                                           __builtin_bit_cast(bf16x8_t, b[u]), z[y],
-                                                           0, 0, 0);
+            z[y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                __builtin_bit_cast(bf16x8_t, kf[y][u0 + u]), __builtin_bit_cast(bf16x8_t, b[u]),
+                z[y], 0, 0, 0);
       }
       slot = slot == kRing - 1 ? 0 : slot + 1;
       const int p_low = x.first + now.j,
@@ -398,8 +398,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void window_weights_rows_f32_kernel
       for (int y = 0; y < HS; ++y)
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-          z = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[y][e / 4][e % 4], qf[y][e / 4][e % 4], z, 0, 0,
-                                                   0);
+          z = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[y][e / 4][e % 4], qf[y][e / 4][e % 4], z, 0,
+                                                   0, 0);
       const f32x2_t now = st;
       const uint32_t seen = window_bits(t0, p, rk.window, rk.sinks) >> (4 * j4);
       if (c0 + 16 < end) load(c0 + 16);
@@ -415,8 +415,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void window_weights_rows_f32_kernel
       const float v = row_sum16(w[r]);
       if (c16 == r) out = v;
     }
-    if (c16 < 4)
-      sums[(int64_t)item * (kTileBlocksF32 * kBlockTokens) + kBlockTokens * wv + 4 * j4 + c16] = out;
+    float* const to = sums + (int64_t)item * (kTileBlocksF32 * kBlockTokens) + kBlockTokens * wv;
+    if (c16 < 4) to[4 * j4 + c16] = out;
   }
 }
 
