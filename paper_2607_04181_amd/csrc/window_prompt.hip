@@ -48,6 +48,7 @@ namespace coco {
 namespace {
 
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
+typedef int i32x4_t __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) void lds_void_t;
 typedef __attribute__((address_space(3))) bf16_t lds_bf16_t;
 typedef __attribute__((address_space(3))) u32x2_t lds_u32x2_t;
@@ -64,6 +65,7 @@ constexpr int kRing = 8;                    // stages in LDS
 constexpr int kStage = 4 * kTile;           // elements: keys and values of two blocks
 constexpr int kXCDs = 8;
 constexpr int kMaxSeqs = kWindowLaunchSeqs;
+static_assert(kMaxSeqs == 512, "a sequence's place among them takes 9 bits");
 constexpr float kLazy = 8.f;                // log2 units a running max may lag
 
 // Piece i of four, 1 KB each, of a cache tile into LDS at byte `to`.
@@ -309,7 +311,7 @@ __device__ __forceinline__ void add_odd(Cols& c, const u32x4_t v[2][2][2], const
 __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a) {
   __shared__ __attribute__((aligned(16))) bf16_t ring[kRing * kStage];
   __shared__ PromptSeq seqs_s[kMaxSeqs];
-  __shared__ int order_s[kMaxSeqs], items_s[kMaxSeqs];
+  __shared__ __attribute__((aligned(16))) int order_s[kMaxSeqs], items_s[kMaxSeqs];
   __shared__ int red[kWaves], next_s[2], bad_s[2];
   const RowKeys& rk = a.rk;
   const int tid = threadIdx.x, lane = tid & 63;
@@ -329,17 +331,20 @@ __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a
     if (s < rk.n_seqs) x = prompt_seq(rk, s, G, a.few);
     const int np = x.splits > 1 ? x.n * a.Hq * x.splits : 0;
     x.part0 = block_prefix<kWaves>(np, red, n_parts) - np;
-    if (s < rk.n_seqs) {
-      seqs_s[s] = x;
-      items_s[s] = x.longest;
-    }
+    // (unlike keys: of equal lengths the first in the call; behind the last none)
+    if (s < rk.n_seqs) seqs_s[s] = x;
+    if (s < (rk.n_seqs + 3) / 4 * 4)
+      items_s[s] = s < rk.n_seqs ? min(x.longest, 0x3FFFFF) << 9 | (511 - s) : -1;
   }
   __syncthreads();
   for (int s = tid; s < rk.n_seqs; s += kThreads) {
     const int mine = items_s[s];
     int before = 0;
-    for (int t = 0; t < rk.n_seqs; ++t)
-      before += items_s[t] > mine || (items_s[t] == mine && t < s);
+#pragma unroll 4
+    for (int t = 0; t < rk.n_seqs; t += 4) {
+      const i32x4_t v = *(const i32x4_t*)&items_s[t];
+      before += (v[0] > mine) + (v[1] > mine) + (v[2] > mine) + (v[3] > mine);
+    }
     order_s[before] = s;
   }
   __syncthreads();
