@@ -287,7 +287,7 @@ __global__ __launch_bounds__(64 * kWaves, kWorkgroups) void window_weights_kerne
       stage_barrier();  // the step is here, and the slot of the one before free
       const lds_bf16_t* from = (const lds_bf16_t*)(uintptr_t)(ring_at + slot * (kSlot * 2));
       const f32x2_t st = *(const lds_f32x2_t*)(from + kCols * HD + c32 * 16);
-      const float inv = c32 < now.left ? st[1] : 0.f;
+      float inv = c32 < now.left ? st[1] : 0.f;
       issue(ahead, slot == 0 ? kRing - 1 : slot - 1);
       if (ahead.left > kCols) next(ahead);
       f32x16_t z[2] = {};
@@ -313,6 +313,10 @@ __global__ __launch_bounds__(64 * kWaves, kWorkgroups) void window_weights_kerne
                 p_high = p_low + small_div(now.r + min(now.left, kCols) - 1, inv_G);
       if (!(t_high <= p_low && (t_low > p_high - rk.window || t_high < rk.sinks))) {
         const int p = max(p_low + small_div(now.r + min(c32, now.left - 1), inv_G), -1);
+        // A row whose sum is NaN (a score of NaN or +inf) has an inverse of NaN, and 0 times
+        // it would reach the keys that it does not see: its seen scores carry the NaN.
+        const float odd = inv == inv ? 0.f : inv;
+        inv = inv == inv ? inv : 1.f;
 #pragma unroll
         for (int y = 0; y < 2; ++y) {
           const uint32_t seen = window_bits(t[y][0], p, rk.window, rk.sinks) |
@@ -320,7 +324,7 @@ __global__ __launch_bounds__(64 * kWaves, kWorkgroups) void window_weights_kerne
           const uint32_t mine = seen >> (4 * hf);
 #pragma unroll
           for (int r = 0; r < 16; ++r)
-            z[y][r] = (mine >> (8 * (r / 4) + r % 4) & 1) ? z[y][r] : -INFINITY;
+            z[y][r] = (mine >> (8 * (r / 4) + r % 4) & 1) ? z[y][r] + odd : -INFINITY;
         }
       }
 #pragma unroll
@@ -405,8 +409,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void window_weights_rows_f32_kernel
       if (c0 + 16 < end) load(c0 + 16);
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const float x = seen >> r & 1 ? fmaf(z[r], scale_log2, -now[0]) : -INFINITY;
-        w[r] = fmaf(__builtin_amdgcn_exp2f(x), now[1], w[r]);
+        // (0 of 1 / sum, which may be NaN, for a key that the row does not see)
+        const bool sees = seen >> r & 1;
+        const float x = sees ? fmaf(z[r], scale_log2, -now[0]) : -INFINITY;
+        w[r] = fmaf(__builtin_amdgcn_exp2f(x), sees ? now[1] : 0.f, w[r]);
       }
     }
     float out = 0.f;
