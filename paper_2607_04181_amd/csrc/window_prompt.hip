@@ -185,9 +185,10 @@ __device__ __forceinline__ void weights_of(Cols& c, const f32x16_t& z, float sca
   float pr[16];
 #pragma unroll
   for (int r = 0; r < 16; ++r) pr[r] = __builtin_amdgcn_exp2f(fmaf(z[r], scale_log2, -c.m));
-  float ls = 0.f;
+  // (in half_step's order: an item that is done again has the same bits)
+  float ls = pr[0];
 #pragma unroll
-  for (int r = 0; r < 16; r += 4) ls += (pr[r] + pr[r + 1]) + (pr[r + 2] + pr[r + 3]);
+  for (int r = 1; r < 16; ++r) ls += pr[r];
   c.l += ls;
 #pragma unroll
   for (int j = 0; j < 2; ++j)
