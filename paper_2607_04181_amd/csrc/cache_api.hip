@@ -418,6 +418,7 @@ int run_window(coco_layer* H, const coco_layer_weights& w, const void* q, void* 
   RowKeys rk = row_keys(H, seq_starts, n_seqs, bt, ctx, w.num_blocks);
   rk.window = window;
   rk.sinks = n_sinks;
+  rk.rows = n_rows;
   const bool bf16 = c.dtype == COCO_BF16;
   if (bf16 && !seq_starts) {
     HIPCHK(launch_window_decode_bf16(

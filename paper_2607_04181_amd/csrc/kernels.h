@@ -379,6 +379,7 @@ struct RowKeys {
   const int32_t* selected = nullptr;    // blocks: [rows][Hkv][top], -1: none
   int top = 0;
   int window = 0, sinks = 0;            // window: > 0 (seq_starts null: row i is sequence i)
+  int rows = 0;                         // window: the call's; no sequence has others
 };
 // fp32 handles, tree, blocks and window. q, o [rows][Hq][hd]. stats (window; may be
 // null): as launch_window_prompt_bf16 writes them.

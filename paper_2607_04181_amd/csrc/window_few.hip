@@ -65,14 +65,15 @@ __global__ __launch_bounds__(kThreads, kWorkgroups) void window_few_kernel(Promp
     const int s = s0 + tid;
     PromptSeq x{};
     if (s < rk.n_seqs) x = prompt_seq(rk, s, G, a.few);
-    const int ni = x.tiles == 0 ? (x.n * G + kCols - 1) / kCols * x.splits * a.Hkv : 0;
-    const int np = x.splits > 1 ? x.n * a.Hq * x.splits : 0;
-    x.item0 = block_prefix<kWaves>(ni, red, total) - ni;
+    const int np = column_parts(x, a.Hq);
     x.part0 = block_prefix<kWaves>(np, red, n_parts) - np;
+    const int ni = x.tiles == 0 && parts_fit(a, x)
+                       ? (x.n * G + kCols - 1) / kCols * x.splits * a.Hkv
+                       : 0;
+    x.item0 = block_prefix<kWaves>(ni, red, total) - ni;
     if (s < rk.n_seqs) seqs_s[s] = x;
   }
   __syncthreads();
-  if (n_parts > a.part_cap) total = 0;  // more rows than the call named: no room for their parts
 
   const auto one = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
 #pragma unroll 1

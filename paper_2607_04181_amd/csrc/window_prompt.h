@@ -44,10 +44,20 @@ struct PromptArgs {
 struct PromptSeq {
   int row0, n, first, tiles, part, splits, longest, item0, part0;
 };
+// Column parts that a sequence needs, and whether the scratch has them behind those of the
+// sequences before: rows of the call that several sequences claim may not fit, and the
+// kernels and the merge leave the same sequences out.
+__device__ __forceinline__ int column_parts(const PromptSeq& x, int Hq) {
+  return x.splits > 1 ? x.n * Hq * x.splits : 0;
+}
+__device__ __forceinline__ bool parts_fit(const PromptArgs& a, const PromptSeq& x) {
+  return (int64_t)x.part0 + column_parts(x, a.Hq) <= a.part_cap;
+}
 __device__ __forceinline__ PromptSeq prompt_seq(const RowKeys& rk, int s, int G, int few) {
   PromptSeq x;
-  x.row0 = rk.seq_starts[s];
-  x.n = max(rk.seq_starts[s + 1] - x.row0, 0);
+  // (q, o and the scratch have room for the call's rows, whatever seq_starts says)
+  x.row0 = min(max(rk.seq_starts[s], 0), rk.rows);
+  x.n = max(min(rk.seq_starts[s + 1], rk.rows) - x.row0, 0);
   const int len = min(max(rk.ctx_lens[s], 0), rk.max_blocks * kBlockTokens);
   x.first = len - x.n;
   const int64_t cols = (int64_t)x.n * G;

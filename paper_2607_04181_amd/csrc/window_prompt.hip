@@ -330,8 +330,9 @@ __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a
     const int s = s0 + tid;
     PromptSeq x{};
     if (s < rk.n_seqs) x = prompt_seq(rk, s, G, a.few);
-    const int np = x.splits > 1 ? x.n * a.Hq * x.splits : 0;
+    const int np = column_parts(x, a.Hq);
     x.part0 = block_prefix<kWaves>(np, red, n_parts) - np;
+    if (!parts_fit(a, x)) x.tiles = 0;
     // (unlike keys: of equal lengths the first in the call; behind the last none)
     if (s < rk.n_seqs) seqs_s[s] = x;
     if (s < (rk.n_seqs + 3) / 4 * 4)
@@ -359,7 +360,6 @@ __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a
     if (r0 + tid < rk.n_seqs) items_s[r0 + tid] = item0;
   }
   __syncthreads();
-  if (n_parts > a.part_cap) total = 0;  // more rows than the call named: no room for their parts
 
   // (The ring's address goes through a register of its own: the compiler would
   // otherwise wait for every load in flight before each operand read.)
@@ -770,7 +770,7 @@ __global__ __launch_bounds__(kMergeThreads) void window_prompt_merge_kernel(Prom
     if (s0 + tid < rk.n_seqs) {
       const PromptSeq y = prompt_seq(rk, s0 + tid, G, a.few);
       n = y.splits > 1 ? y.n : 0;
-      np = y.splits > 1 ? y.n * a.Hq * y.splits : 0;
+      np = column_parts(y, a.Hq);
     }
     int row1 = wave_scan(n), part1 = wave_scan(np);
     if (lane == kWave - 1) {
@@ -798,12 +798,13 @@ __global__ __launch_bounds__(kMergeThreads) void window_prompt_merge_kernel(Prom
   __syncthreads();
   const int s = found[0];
   if (s < 0) return;
-  const PromptSeq x = prompt_seq(rk, s, G, a.few);
+  PromptSeq x = prompt_seq(rk, s, G, a.few);
+  x.part0 = found[2];
+  if (!parts_fit(a, x)) return;
   const int row = x.row0 + found[1];
   const int head = blockIdx.y * kMergeHeads + tid / 32, dim = tid % 32 * 4;
   if (head >= a.Hq) return;
-  const int64_t idx = (int64_t)found[2] + ((int64_t)found[1] * a.Hq + head) * x.splits;
-  if (idx + x.splits > a.part_cap) return;  // (as the parts' kernel)
+  const int64_t idx = (int64_t)x.part0 + ((int64_t)found[1] * a.Hq + head) * x.splits;
   float M = -INFINITY, L = 0.f;
   f32x4_t y = {0.f, 0.f, 0.f, 0.f};
   for (int p0 = 0; p0 < x.splits; p0 += 4) {

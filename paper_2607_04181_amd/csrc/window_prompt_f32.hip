@@ -49,7 +49,7 @@ template <int HS>
 __global__ __launch_bounds__(64 * waves_of(HS),
                              HS <= 2 ? 4 : HS <= 5 ? 2 : 1) void window_prompt_f32_kernel(
     const float* __restrict__ q, const float* __restrict__ k_cache,
-    const float* __restrict__ v_cache, RowKeys rk, int n_rows, int Hq, int Hkv, int chunks,
+    const float* __restrict__ v_cache, RowKeys rk, int Hq, int Hkv, int chunks,
     float scale_log2, float* __restrict__ o, float* __restrict__ stats) {
   constexpr int hd = 32 * HS, TC = 16, kPitch = hd + 4, kWaves = waves_of(HS);
   __shared__ __attribute__((aligned(16))) float sm_o[kWaves][TC][kPitch];
@@ -61,10 +61,11 @@ __global__ __launch_bounds__(64 * waves_of(HS),
   const int G = Hq / Hkv, heads = min(G, TC), rows = TC / heads;
   const int g = blockIdx.y / chunks, head0 = blockIdx.y % chunks * heads;
   const int left = min(G - head0, heads);
-  const int row_end = min(min((int)blockIdx.x * rows + rows, n_rows), rk.seq_starts[rk.n_seqs]);
+  const int row_end = min(min((int)blockIdx.x * rows + rows, rk.rows), rk.seq_starts[rk.n_seqs]);
   // (A workgroup's rows may be of several sequences: one after the other.)
   for (int row0 = blockIdx.x * rows; row0 < row_end;) {
-    const int s = row_to_seq(rk.seq_starts, rk.n_seqs, row0), seq_end = rk.seq_starts[s + 1];
+    const int s = row_to_seq(rk.seq_starts, rk.n_seqs, row0);
+    const int seq_end = min(rk.seq_starts[s + 1], rk.rows);
     const int row1 = min(row_end, seq_end);
     if (row1 <= row0) break;
     const int len = min(max(rk.ctx_lens[s], 0), rk.max_blocks * kBlockTokens);
@@ -237,7 +238,7 @@ hipError_t launch_window_prompt_f32(const float* q, const float* k_cache, const 
 #define COCO_PROMPT(HS)                                                                         \
   COCO_LAUNCH_LAST((window_prompt_f32_kernel<HS>),                                              \
                    dim3((n_rows + rows - 1) / rows, Hkv * chunks), dim3(64 * waves_of(HS)), 0,  \
-                   st, q, k_cache, v_cache, rk, n_rows, Hq, Hkv, chunks, scale_log2, o, stats)
+                   st, q, k_cache, v_cache, rk, Hq, Hkv, chunks, scale_log2, o, stats)
   COCO_BY_HEAD_DIM(COCO_PROMPT);
 #undef COCO_PROMPT
   return hipGetLastError();

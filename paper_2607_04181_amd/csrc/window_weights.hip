@@ -61,8 +61,8 @@ struct SeqRows {
 };
 __device__ __forceinline__ SeqRows seq_rows(const RowKeys& rk, int s) {
   SeqRows x;
-  x.row0 = rk.seq_starts ? rk.seq_starts[s] : s;
-  x.n = rk.seq_starts ? max(rk.seq_starts[s + 1] - x.row0, 0) : 1;
+  x.row0 = rk.seq_starts ? min(max(rk.seq_starts[s], 0), rk.rows) : s;
+  x.n = rk.seq_starts ? max(min(rk.seq_starts[s + 1], rk.rows) - x.row0, 0) : 1;
   x.last = min(max(rk.ctx_lens[s], 0), rk.max_blocks * kBlockTokens) - 1;
   x.first = x.last + 1 - x.n;
   // (rows before the context's start see nothing)
@@ -138,8 +138,8 @@ __device__ __forceinline__ void tile_rows(const RowKeys& rk, const SeqRows& x, i
 }
 
 // The sequences' items into seqs, and their first ones into items0 for the sums' kernel;
-// all of them. More than `cap` (more rows than the call named: no room for their sums):
-// none, for it too. red: one int per wave.
+// all of them. More than `cap` (rows that several sequences claim: no room for their
+// sums): none, for it too. red: one int per wave.
 template <int TB>
 __device__ __forceinline__ int plan_items(const RowKeys& rk, int G, int Hkv, int64_t cap,
                                           SeqItems* seqs, int* red, int32_t* items0) {
