@@ -591,10 +591,12 @@ int coco_kv_compact(coco_layer_t H, int32_t first_layer, int32_t n_layers, const
       return rc;
     if (ks[0] != 0 || ks[n] < 0 || ks[n] > n_kept)
       return fail(COCO_EINVAL, "kept_starts must run from 0 to at most n_kept");
+    // (before any list is read: one that ended behind the next one's start could pass the last)
+    for (int i = 0; i < n; ++i)
+      if (ks[i + 1] < ks[i]) return fail(COCO_EINVAL, "kept_starts not monotone at %d", i);
     k.resize(ks[n]);  // (places behind the last list may hold anything)
     if ((rc = check_range("kept", k, 0, (int64_t)c.max_blocks_per_seq * kBlockTokens))) return rc;
     for (int i = 0; i < n; ++i) {
-      if (ks[i + 1] < ks[i]) return fail(COCO_EINVAL, "kept_starts not monotone at %d", i);
       for (int j = ks[i]; j < ks[i + 1]; ++j)
         if (k[j] < b[i] + (j - ks[i]) || (j > ks[i] && k[j] <= k[j - 1]))
           return fail(COCO_EINVAL, "kept[%d] = %d is not ascending from base_lens[%d] = %d", j,
