@@ -531,8 +531,10 @@ int validate_batch(coco_layer* H, int64_t hidden_rows, const int32_t* row_idx, i
   if (rows && rows->window > 0)
     return validate_window(H, n_rows, positions, seq_starts, n_seqs, block_table, ctx_lens,
                            rows->window, rows->n_sinks, min_blocks, st);
-  for (int s = 0; s < n_seqs; ++s) {
+  // (before any sequence's positions are read: one could pass the last row)
+  for (int s = 0; s < n_seqs; ++s)
     if (ss[s + 1] < ss[s]) return fail(COCO_EINVAL, "seq_starts not monotone at %d", s);
+  for (int s = 0; s < n_seqs; ++s) {
     if (cl[s] < 1 || cl[s] > c.max_blocks_per_seq * kBlockTokens)
       return fail(COCO_EINVAL, "ctx_lens[%d] = %d out of range", s, cl[s]);
     for (int i = ss[s]; i < ss[s + 1]; ++i) {

@@ -6,6 +6,8 @@ import torch
 
 import paper_2607_04181_amd as coco
 from cache_ref import Cache, i32, tables
+from harness import Replica, ragged_prefill_batch, small_bf16_shape
+from workloads import device as WD
 
 pytestmark = pytest.mark.gpu
 
@@ -20,3 +22,16 @@ def test_compaction_names_starts_out_of_order(starts):
         coco.coco_kv_compact(c.h, 0, 1, i32([0, 1]), i32([0, 0]), i32([1, 2, 3]), i32(starts), table)
     torch.cuda.synchronize()
     assert all(torch.equal(p, q) for p, q in zip(before, c.pools[0]))
+
+
+@pytest.mark.parametrize("starts", [[0, 90, 12], [0, 2 ** 30, 12], [0, -3, 12]])
+def test_layers_name_starts_out_of_order(starts):
+    b = ragged_prefill_batch(31, [20, 3], [5, 7], 64)
+    rep = Replica.for_batch(small_bf16_shape(), "vs", 1, b)
+    hidden = WD.hidden_tensor(rep.shape, "vs", b.hidden_rows)
+    before = hidden.clone()
+    coco.coco_layer_set_validate(rep.h, True)
+    with pytest.raises(coco.CocoError, match="seq_starts not monotone"):
+        rep.forward(0, hidden, dict(WD.batch_tensors(b), seq_starts=i32(starts)))
+    torch.cuda.synchronize()
+    assert torch.equal(hidden, before)
