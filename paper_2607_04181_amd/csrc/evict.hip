@@ -288,7 +288,8 @@ __device__ __forceinline__ void list_row(const EvictArgs& a, const Row& r) {
     }
 #pragma unroll
     for (int u = 0; u < 4; ++u)
-      if (stays[u]) {
+      // (at < count but for a row that another request of the call has moved meanwhile)
+      if (stays[u] && at < count) {
         a.kept[start + at] = t + u;
         if (w_out != nullptr) w_out[base + at] = w[u];
         ++at;
