@@ -468,8 +468,9 @@ __global__ __launch_bounds__(kThreads, 1) void window_prompt_kernel(PromptArgs a
     // Stages that every column of the wave sees whole: from..to. (Among the window's
     // blocks only; slots above p - window for the latest row, up to p for the first.)
     const int p_low = max(it.first + it.j_tile + small_div(it.r_tile + wave0, inv_G), -1),
-              p_high = it.first + it.j_tile +
-                       small_div(it.r_tile + min(wave0 + kCols - 1, last), inv_G);
+              p_high = max(it.first + it.j_tile +
+                               small_div(it.r_tile + min(wave0 + kCols - 1, last), inv_G),
+                           -1);  // (p_high - window does not overflow)
     const int b_low = max(p_high - rk.window + kBlockTokens, 0) / kBlockTokens,
               b_high = (p_low + 1) / kBlockTokens - 1;
     const int from = (it.list.head + max(b_low - it.list.first, 0) - it.e0 + 1) >> 1,

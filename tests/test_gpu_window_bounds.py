@@ -34,3 +34,13 @@ def test_rows_that_are_not_the_calls_are_left_as_they_are(dtype, hq, hkv, hd, le
         coco.coco_window_attention(r.c.h, 0, r.q[:n], ref, i32(starts), table, ctx, ALL, 0, w_ref)
         torch.cuda.synchronize()
         assert torch.equal(o[:at], ref[:at]) and torch.equal(w[:len(whole)], w_ref[:len(whole)])
+
+
+@pytest.mark.parametrize("window,sinks", [(ALL, 0), (ALL, ALL), (ALL - 7, 3), (1, ALL)])
+@pytest.mark.parametrize("rows", [[700, 300, 40], [5, 30, 9]])
+@pytest.mark.parametrize("dtype,hq,hkv,hd", [("bf16", 4, 2, 128), ("f32", 4, 2, 64)])
+def test_rows_before_the_context_with_the_widest_windows(dtype, hq, hkv, hd, rows, window, sinks):
+    r = Rows(dtype, hq, hkv, hd, [3, 20, 0], rows, window, sinks, seed=25, poison=False)
+    r.run()
+    r.check()
+    assert (r.o[:max(rows[0] - 3, 0)] == 0).all()
