@@ -470,10 +470,16 @@ int coco_layer_sparse_forward(coco_layer_t h, int32_t layer, void* hidden, int64
 
 /* Make room for window calls of up to max_rows rows and max_seqs (at most
  * 65535) sequences, and, with weigh, for their weights (as coco_tree_reserve).
- * A bf16 handle holds 4 bytes per query head and slot of a block-table row for
- * each of min(max_rows, max_seqs) sequences then, any handle 4 bytes per key/value
- * head and slot for each of 512 of them and for each 256 (fp32: 128) of max_rows
- * times the query heads per key/value head. */
+ * With weigh a bf16 handle holds 4 bytes per query head and slot of a block-table
+ * row for each of min(max_rows, max_seqs) sequences, any handle 4 bytes per
+ * key/value head and slot for each of 512 of them and for each 256 (fp32: 128) of
+ * max_rows times the query heads per key/value head. A bf16 handle always holds
+ * partial results of 520 bytes: of min(max_rows, max_seqs) single tokens one per
+ * query head and 512 slots of a table row, or, where that is more, of prompts' rows
+ * times query heads, at most 512 (per key/value head) of a sequence, one each per
+ * 1024 slots, 16 at most (of the first 64 per 512 slots): with 32 query heads on 8
+ * and table rows of 16400 slots 35 MB for 64 rows of 64 sequences, 2.2 GB for 8192
+ * rows of them. */
 int coco_window_reserve(coco_layer_t h, int32_t max_rows, int32_t max_seqs, int32_t weigh);
 
 /* Attention of rows over the newest `window` tokens of layer `layer`'s cache and
@@ -528,7 +534,9 @@ int coco_layer_window_forward(coco_layer_t h, int32_t first_layer, int32_t n_lay
  *   weights        move with the tokens; 0 from B to L - 1
  * The tokens themselves move by coco_kv_compact, and the pages behind new_lens go
  * by coco_kv_free. Lists are written in order until one does not fit; that row
- * and those behind it that would list any keep everything. At most max_seqs
+ * and those behind it that would list any keep everything. (A list is as long as
+ * its budget at most; validation mode, which does not know the lists, refuses a
+ * call whose room is below the budgets of its rows with L > B.) At most max_seqs
  * requests of distinct rows; rows out of range count as empty. new_lens must not
  * overlap ctx_lens. */
 int coco_kv_evict(coco_layer_t h, const int32_t* seq_idx, const int32_t* keep_lens, int32_t n,

@@ -179,7 +179,10 @@ __device__ __forceinline__ void rescale_if(bool moved, Cols& c, float m_new) {
 __device__ __forceinline__ void rescale(Cols& c, float m_new) {
   rescale_if(__ballot(m_new != c.m) != 0, c, m_new);
 }
-// Weights of 32 keys as operands of two products.
+// Weights of 32 keys as operands of two products: rounded to bf16 once (2^-8 of a weight at
+// most, and as the layers' attention does), where single tokens and few rows hold two parts.
+// Those are bound by the cache's bytes; here a second part would be 24 products for 16 in a
+// half step, whose products bound it, and 16 registers of a wave that uses 510 of its 512.
 __device__ __forceinline__ void weights_of(Cols& c, const f32x16_t& z, float scale_log2,
                                            u32x4_t p[2]) {
   float pr[16];

@@ -12,11 +12,12 @@
 // over the columns it keeps; the 32 lanes' sums meet once, at the end, and the sums of
 // the heads, and of the parts of many columns, in a second kernel, in order. Three
 // workgroups to a CU take such pieces in turn, one's products (16 of 33 cycles a step)
-// beside the others' exponentials (32 of 8, and 64 multiply-adds of 4), which bound it.
+// beside the others' exponentials and multiply-adds (32 of 8 and 64 of 4), as long.
 // 16 sequences of 36 to 64 rows (32 heads on 8, 58500 cached tokens between them) take
 // 46 us, 4000 rows of a prompt 102: with 32 keys to a wave and all columns in one item
-// 57 and 393. Of the 46, the products are 10 and the vector instructions 20; the rest
-// are starts of items (tables, keys) and the last round, when some CUs have none.
+// 57 and 393. Of the 46, the products are 10 and the vector instructions 20. What bounds
+// it is the rest: starts of items (tables, then keys, then the first columns, with nothing
+// of the next item ahead) and the last round, when some CUs have none.
 // fp32: the same of 64 keys, 16 of them in a wave's registers; single tokens without a
 // second kernel.
 #include <limits.h>
@@ -350,8 +351,10 @@ __global__ __launch_bounds__(64 * kWaves, kWorkgroups) void window_weights_kerne
 
 // fp32: a workgroup's waves have a block of 16 keys each, and walk the item's columns 16
 // at a time, the keys' and the columns' operands from memory: S[16 keys][16 columns] =
-// K Q^T, 8 HS x mfma 16x16x4 of 32 cycles each, which bound it. 2000 rows of a prompt, 16
-// heads of 64 on 4, take 89 us (2680 with a workgroup that walked them for its 16 keys).
+// K Q^T, 8 HS x mfma 16x16x4 of 32 cycles each. 2000 rows of a prompt, 16 heads of 64 on
+// 4, take 84 to 89 us (2680 with a workgroup that walked them for its 16 keys). The matrix
+// units are busy for 31% of it; the waves wait for half of their time: at the items' starts,
+// and for columns that are asked for one step, 16 products on one accumulator, ahead.
 template <int HS>
 __global__ __launch_bounds__(64 * kWaves, 2) void window_weights_rows_f32_kernel(
     const float* __restrict__ q, const float* __restrict__ k_cache, RowKeys rk, int Hq, int Hkv,
